@@ -20,6 +20,9 @@
  *   20. backward of the max-pooled lookup   21, 22. the backward in two halves (plan / apply)
  *   23, 24. run index of a batch (adjacent rows holding one list)   25. lookup and expand in one pass
  *   26. the backward's plan of a batch with a run index
+ * and what a sequence model does with the rows of its unique lists:
+ *   27, 28. layer norm and its gradients   29, 30. softmax cross entropy against a table and its gradients
+ *   31, 32. attention inside lists and its gradients
  *
  * General rules
  *   - Every array argument marked "device" is a pointer into GPU memory owned by the caller and
@@ -96,6 +99,9 @@ typedef enum {
 /* Largest number of features per call and largest row size in bytes (D * element size). */
 #define RECD_MAX_FEATURES 1024
 #define RECD_MAX_ROW_BYTES 4096
+/* Largest row, in elements, of calls 29 and 30, and largest head of calls 31 and 32. */
+#define RECD_MAX_DENSE_D 256
+#define RECD_MAX_HEAD_DIM 128
 
 /* Create a context bound to `device` and to `hip_stream` (a hipStream_t passed as void*; NULL =
  * the default stream).  `workspace_hint_bytes` pre-allocates the device workspace (0 = grow on
@@ -562,6 +568,88 @@ recd_status recd_build_ikjt_noalloc(recd_ctx *ctx, int F, int64_t B, int64_t N,
                                     const int64_t *values, const int64_t *offsets,
                                     int64_t *u_values, int64_t *u_offsets, int32_t *inverse,
                                     int64_t *feat_uoff);
+
+/* ---- Dense operators on the rows of lists ----------------------------------------------------------------------
+ * What a sequence model does with the rows of call 6, once per unique list: normalise them, let the rows of a list
+ * attend to each other, score rows against a whole table.  For all of them:
+ *   - activations and their gradients are fp32, fp16 or bf16 (`dtype`), parameters of the layer norm and all statistics
+ *     fp32; sums, maxima and statistics are held in fp32 and rounded once at the end (fp16 and bf16 probabilities
+ *     are also rounded to the type where they enter a matrix product);
+ *   - row pointers are aligned to 16 bytes, and a row's (a head's) bytes are a multiple of 16;
+ *   - sums are taken in an order that depends on the sizes and types alone: the same call gives the same bits;
+ *   - calls use the context's workspace as stated, growing it on demand, and so drop a pending backward plan.
+ *     Inside a captured graph the workspace must be large enough already (an earlier call of the sizes made it so). */
+
+/* 27. Layer norm of the rows of x [n, D] (device, D * element size at most RECD_MAX_ROW_BYTES):
+ *       y = (x - mean) / sqrt(mean((x - mean)^2) + eps) * weight + bias
+ *     weight, bias: device fp32 [D], NULL = ones, zeros.  y: device [n, D]; may be x.
+ *     stats: device fp32 [n, 2], receives {mean, 1 / sqrt(...)} of every row for call 28, or NULL.  No workspace. */
+recd_status recd_layer_norm(recd_ctx *ctx, int64_t n, int D, recd_dtype dtype, const void *x, const float *weight,
+                            const float *bias, float eps, void *y, float *stats);
+
+/* 28. Gradients of call 27.  grad_y, grad_x: device [n, D] of dtype (grad_x may be grad_y).
+ *     grad_weight, grad_bias: device fp32 [D], overwritten with the sums over all rows; either or both may be NULL.
+ *     Workspace: up to 64 * D bytes for every compute unit. */
+recd_status recd_layer_norm_backward(recd_ctx *ctx, int64_t n, int D, recd_dtype dtype, const void *x, const float *weight,
+                                     const float *stats, const void *grad_y, void *grad_x, float *grad_weight,
+                                     float *grad_bias);
+
+/* 29. Softmax cross entropy of rows x [n, D] against the V rows of a table as the vocabulary; the logits
+ *     z[i, v] = scale * <x_i, table_v> are never stored (scale: not 0).  D at most RECD_MAX_DENSE_D; V and n below 2^31.
+ *     targets: device int64 [n], a row of the table each; a negative one marks a row without a target (loss 0, no
+ *     gradients).  So does one of V and more, unless RECD_OPT_VALIDATE is set (RECD_EBOUNDS).
+ *     loss: device fp32 [n], lse[i] - z[i, targets[i]].   lse: device fp32 [n], log(sum over v of exp(z[i, v])).
+ *     mean_row: device fp32 [n, D] or NULL; receives sum over v of exp(z[i, v] - lse[i]) * table_v, from which call 30
+ *     has the gradient by x without a second pass over the table.
+ *     Workspace: the splits' maxima and sums, and with mean_row their means: less than 4 * (D + 2) * 4 bytes a row
+ *     and compute unit. */
+recd_status recd_vocab_loss(recd_ctx *ctx, int64_t n, int64_t V, int D, recd_dtype dtype, const void *x, const void *table,
+                            const int64_t *targets, float scale, float *loss, float *lse, float *mean_row);
+
+/* 30. Gradients of call 29 for grad_loss (device fp32 [n]: the weight of every row's loss).
+ *     lse, mean_row: from call 29 on the same inputs (mean_row is read for grad_x only).
+ *     grad_x: device [n, D] of dtype, or NULL.   grad_table: device [V, D] of dtype, overwritten (every row), or NULL.
+ *     Workspace: 12 bytes a row. */
+recd_status recd_vocab_loss_backward(recd_ctx *ctx, int64_t n, int64_t V, int D, recd_dtype dtype, const void *x,
+                                     const void *table, const int64_t *targets, float scale, const float *lse,
+                                     const float *mean_row, const float *grad_loss, void *grad_x, void *grad_table);
+
+/* 31. Attention inside lists: no row sees another list's.  List l has the query rows q_offsets[l] .. q_offsets[l+1] and the
+ *     key rows k_offsets[l] .. k_offsets[l+1]; its last query stands at its last key: pos_i = nk - nq + i.
+ *       z_ij = scale * <q_i, k_j>;  with softcap: z_ij = softcap * tanh(z_ij / softcap)
+ *       then, with slopes: z_ij -= slopes[head] * |pos_i - j|
+ *       visible keys: all of the list's; causal: j <= pos_i, or j < prefix[l] where prefix is given
+ *       out_i = sum over the visible j of softmax(z_i)_j v_j;  a row that sees no key gives 0 (and lse = -inf)
+ *     Heads: query head h reads key head h / (heads / kv_heads).  One query row per list is the form for serving a new
+ *     token; keys are split over blocks where there are few tiles. */
+typedef struct recd_attention {
+    int heads, kv_heads, head_dim;         /* heads a multiple of kv_heads; head_dim at most RECD_MAX_HEAD_DIM */
+    recd_dtype dtype;
+    int64_t lists;
+    int64_t max_q, max_k;                  /* upper bounds of a list's query and key rows */
+    int64_t q_rows, k_rows;                /* rows of all lists: q_offsets[lists], k_offsets[lists] */
+    const int64_t *q_offsets, *k_offsets;  /* device [lists + 1], from 0, not falling; may be one array (call 1's u_offsets) */
+    int64_t q_stride, k_stride, v_stride;  /* elements from row to row; the heads of a row lie densely */
+    float scale, softcap;                  /* softcap 0 = none */
+    const float *slopes;                   /* device fp32 [heads], or NULL */
+    const int32_t *prefix;                 /* device [lists], or NULL; needs causal */
+    int causal;
+} recd_attention;
+
+/*     q [q_rows, heads, head_dim], k and v [k_rows, kv_heads, head_dim]: device, rows apart by their strides.
+ *     out: device [q_rows, heads, head_dim], dense.   lse: device fp32 [q_rows, heads] for call 32, or NULL.
+ *     Workspace: 8 bytes for every list and every 32 query rows of a key head, and where keys are split the splits'
+ *     partial rows in fp32.  RECD_OPT_VALIDATE checks the offsets and bounds. */
+recd_status recd_list_attention(recd_ctx *ctx, const recd_attention *a, const void *q, const void *k, const void *v, void *out,
+                                float *lse);
+
+/* 32. Gradients of call 31 (none by slopes).  out, lse: from call 31.  grad_out: device, dense as out.
+ *     grad_q, grad_k, grad_v: device, rows apart by their own strides (elements), every row overwritten; key heads
+ *     add up their query heads in fp32.
+ *     Workspace: 4 bytes a query row and head, and 16 bytes for every list and 32 rows. */
+recd_status recd_list_attention_backward(recd_ctx *ctx, const recd_attention *a, const void *q, const void *k, const void *v,
+                                         const void *out, const float *lse, const void *grad_out, void *grad_q, void *grad_k,
+                                         void *grad_v, int64_t grad_q_stride, int64_t grad_k_stride, int64_t grad_v_stride);
 
 #ifdef __cplusplus
 }

@@ -1,0 +1,911 @@
+// Attention inside the lists of jagged rows, and its gradients.
+//
+// List l has nq query rows and nk key rows; its last query stands at its last key: pos_i = nk - nq + i.
+//   z_ij = cap * tanh(scale * q_i . k_j / cap) - slope * |pos_i - j|   (without the tanh where cap = 0)
+//   visible: j < lim_i, lim_i = max(pos_i + 1, prefix) with a causal mask, else nk
+//   p_ij = exp(z_ij - lse_i) over the visible j, o_i = sum_j p_ij v_j;  a row that sees nothing gives o_i = 0
+//   dv_j = sum_i p_ij g_i,  dp_ij = g_i . v_j,  ds_ij = scale * p_ij * (dp_ij - g_i . o_i) * (1 - tanh^2)
+//   dq_i = sum_j ds_ij k_j,  dk_j = sum_i ds_ij q_i
+//
+// The query heads that share a key head are rows of one problem: row r of a (list, key head) is query r / group under
+// head r % group of the group.  A tile of one head then reads every key once for the whole group, and the
+// gradients by keys and values add the group up in their sums.
+//
+// Three kernels of one shape: 32 rows of the kept side (queries; in the last kernel keys) a wave in registers, the other
+// side streamed through LDS once for scores (by rows) and once for the sums (by columns); the scores never leave
+// their lane (recd_mfma.h).  The forward kernel keeps a running maximum and sum.  The backward pass computes the scores
+// twice, once for dq and once for dk and dv: 14 nq nk d operations a head instead of 10, and no atomics, so
+// the results depend on the sizes alone.
+//
+// Tiles of lists are found without a scan: the tiles of list l take the slots from floor(rows before l / R) + l on,
+// which never overlap as ceil(n / R) <= floor((before + n) / R) - floor(before / R) + 1.
+#include "recd_internal.h"
+#include "recd_mfma.h"
+
+#include <math.h>
+
+namespace {
+
+constexpr float kSlack = 8.0f;  // see the running maximum of the forward kernel
+template <typename T> constexpr bool kHalf = std::is_same<T, _Float16>::value;
+// fp16 exponentials are held 2^7 times larger by the forward pass (at most 2^15 with the slack) and probabilities
+// 2^15 times by the backward pass, so that small ones keep their bits
+template <typename T> constexpr float kLift = kHalf<T> ? 7.0f : 0.0f;
+template <typename T> constexpr float kLiftP = kHalf<T> ? 15.0f : 0.0f;
+
+struct Args {
+    int G, group, d;              // key heads, query heads of each, elements of a head
+    int64_t lists, slots;
+    const int2 *tiles;            // {list or -1, tile} of every slot, or null: tiles_per_list slots for every list
+    int tiles_per_list, splits;
+    const int64_t *q_offsets, *k_offsets;
+    const void *q, *k, *v, *out_in, *g;
+    int64_t q_stride, k_stride, v_stride, gq_stride, gk_stride, gv_stride;
+    float scale, cap;
+    const float *slopes;
+    const int32_t *prefix;
+    int causal;
+    void *out, *gq, *gk, *gv;
+    float *lse;
+    const float *lse_in, *delta;  // [q rows][H]
+    const float *lift;            // fp16 backward: the power of two that ds is held larger by, else null
+    float *part_m, *part_l, *part_o;
+    int64_t part_rows;            // q rows * H
+};
+
+// One (list, key head).
+struct Problem {
+    int64_t q0, k0;
+    int nq, nk, rows, head0, pos0, prefix;
+    bool causal;
+
+    __device__ inline int query(int row, int group) const { return group == 1 ? row : row / group; }
+    // keys [0, limit) are visible to the row; does not fall with the row
+    __device__ inline int limit(int row, int group) const
+    {
+        if (!causal)
+            return nk;
+        const int past = pos0 + query(row, group) + 1, to = past > prefix ? past : prefix;
+        return to < 0 ? 0 : to > nk ? nk : to;
+    }
+};
+
+// The block's tile: false where the slot holds none.  Slots go round the dies; the heads of a slot, whose rows share
+// cache lines, follow each other on one die; the last slots (the longest lists' ends) come first.
+__device__ inline bool find_tile(const Args &a, Problem &p, int &head, int &tile, int &split)
+{
+    const int64_t at = blockIdx.x >> 3;
+    const int64_t unit = at / a.G * 8 + (blockIdx.x & 7);
+    head = (int)(at % a.G);
+    if (unit >= a.slots * a.splits)
+        return false;
+    split = (int)(unit % a.splits);
+    const int64_t slot = a.slots - 1 - unit / a.splits;
+    int64_t list;
+    if (a.tiles) {
+        const int2 t = a.tiles[slot];
+        if (t.x < 0)
+            return false;
+        list = t.x;
+        tile = t.y;
+    } else {
+        list = slot / a.tiles_per_list;
+        tile = (int)(slot % a.tiles_per_list);
+    }
+    p.q0 = a.q_offsets[list];
+    p.k0 = a.k_offsets[list];
+    p.nq = (int)(a.q_offsets[list + 1] - p.q0);
+    p.nk = (int)(a.k_offsets[list + 1] - p.k0);
+    p.rows = p.nq * a.group;
+    p.head0 = head * a.group;
+    p.pos0 = p.nk - p.nq;
+    p.causal = a.causal;
+    p.prefix = a.prefix ? a.prefix[list] : 0;
+    return true;
+}
+
+// Rows of a tile from memory into registers and on into LDS; row(r) gives the address of row r, or null.
+template <typename T, int ROWS, int DP, int THREADS> struct Stream {
+    using Tile = RecdTile<T, ROWS, DP>;
+    using Piece = typename Tile::Piece;
+    static constexpr int PT = (Tile::PIECES + THREADS - 1) / THREADS;
+    Piece held[PT];
+
+    template <typename Row> __device__ inline void load(int d, Row row)
+    {
+        constexpr int PR = DP / Tile::E;
+#pragma unroll
+        for (int i = 0; i < PT; i++) {
+            const int piece = threadIdx.x + i * THREADS, at = piece % PR * Tile::E;
+            held[i] = Piece{};
+            if (piece < Tile::PIECES && at < d) {
+                const T *p = row(piece / PR);
+                if (p)
+                    held[i] = *reinterpret_cast<const Piece *>(p + at);
+            }
+        }
+    }
+    __device__ inline void store(Tile &t)
+    {
+#pragma unroll
+        for (int i = 0; i < PT; i++)
+            if (threadIdx.x + i * THREADS < (unsigned)Tile::PIECES)
+                t.put(threadIdx.x + i * THREADS, held[i]);
+    }
+};
+
+__device__ inline float tanh_of(float x)
+{
+    return 1.0f - 2.0f * __builtin_amdgcn_rcpf(1.0f + recd_exp2(x * (2.0f * kRecdLog2e)));
+}
+
+template <typename T> __device__ inline void store4(T *p, float a, float b, float c, float d)
+{
+    T out[4] = {(T)a, (T)b, (T)c, (T)d};
+    __builtin_memcpy(p, out, sizeof out);
+}
+
+// A head's columns of one row: registers of `sums` are rows of the head's elements.
+template <typename T, int DT> __device__ inline void store_columns(T *row, const recd_f32x16 (&o)[DT], float f, int d, int lane)
+{
+#pragma unroll
+    for (int t = 0; t < DT; t++)
+        for (int r = 0; r < 16; r += 4) {
+            const int col = 32 * t + recd_sums_row(r, lane);
+            if (col < d)
+                store4<T>(row + col, o[t][r] * f, o[t][r + 1] * f, o[t][r + 2] * f, o[t][r + 3] * f);
+        }
+}
+
+template <typename T, int DP, int NW, int BK> __global__ __launch_bounds__(64 * NW) void k_attention(Args a)
+{
+    constexpr int KS = DP / 16, DT = DP / 32, THREADS = 64 * NW;
+    using Mma = RecdMma<T>;
+    using Frag = typename Mma::Frag;
+    __shared__ RecdTile<T, BK, DP> kt, vt;
+    Problem p;
+    int head, tile, split;
+    if (!find_tile(a, p, head, tile, split))
+        return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int first = tile * 32 * NW, end = first + 32 * NW < p.rows ? first + 32 * NW : p.rows;  // the block's rows
+    if (first >= end)
+        return;
+    const int row0 = first + 32 * wave, row = row0 + (lane & 31);
+    const bool there = row < p.rows;
+    const int query = p.query(row, a.group), head_in = row - query * a.group;
+    const int lim = there ? p.limit(row, a.group) : 0;
+    const int wave_end = row0 < p.rows ? p.limit(row0 + 32 < p.rows ? row0 + 31 : p.rows - 1, a.group) : 0;
+    const int wave_full = row0 + 32 <= p.rows ? p.limit(row0, a.group) : 0;  // keys that every row sees
+    const int tiles = (p.limit(end - 1, a.group) + BK - 1) / BK;
+    const int t0 = (int)((int64_t)tiles * split / a.splits), t1 = (int)((int64_t)tiles * (split + 1) / a.splits);
+    const int H = a.G * a.group;
+    const int64_t q_row = p.q0 + query, at_row = q_row * H + p.head0 + head_in;
+    const float slope = a.slopes && there ? a.slopes[p.head0 + head_in] * kRecdLog2e : 0.0f;
+    const int pos = p.pos0 + query;
+    const float c = a.scale * kRecdLog2e, cap = a.cap * kRecdLog2e, to_cap = a.cap != 0.0f ? a.scale / a.cap : 0.0f;
+
+    Frag qf[KS];
+    for (int k = 0; k < KS; k++)
+        qf[k] = recd_row_frag<T>((const T *)a.q + q_row * a.q_stride + (int64_t)(p.head0 + head_in) * a.d, 16 * k, a.d, there,
+                                 lane);
+    float m = -INFINITY, l = 0.0f;
+    recd_f32x16 o[DT];
+    for (int d = 0; d < DT; d++)
+        o[d] = recd_f32x16{};
+    Stream<T, BK, DP, THREADS> ks, vs;
+    auto load = [&](int t) {
+        ks.load(a.d, [&](int r) -> const T * {
+            const int j = t * BK + r;
+            return j < p.nk ? (const T *)a.k + (p.k0 + j) * a.k_stride + (int64_t)head * a.d : nullptr;
+        });
+        vs.load(a.d, [&](int r) -> const T * {
+            const int j = t * BK + r;
+            return j < p.nk ? (const T *)a.v + (p.k0 + j) * a.v_stride + (int64_t)head * a.d : nullptr;
+        });
+    };
+    if (t0 < t1)
+        load(t0);
+    for (int t = t0; t < t1; t++) {
+        __syncthreads();
+        ks.store(kt);
+        vs.store(vt);
+        __syncthreads();
+        if (t + 1 < t1)
+            load(t + 1);
+#pragma unroll
+        for (int st = 0; st < BK / 32; st++) {
+            const int j0 = t * BK + 32 * st;
+            if (j0 >= wave_end)
+                break;
+            recd_f32x16 s = {};
+#pragma unroll
+            for (int k = 0; k < KS; k++)
+                s = Mma::mul(kt.rows(32 * st, 16 * k, lane), qf[k], s);
+            if (a.cap != 0.0f)
+                for (int r = 0; r < 16; r++)
+                    s[r] = cap * tanh_of(s[r] * to_cap);
+            else
+                for (int r = 0; r < 16; r++)
+                    s[r] *= c;
+            if (a.slopes)
+                for (int r = 0; r < 16; r++)
+                    s[r] -= slope * fabsf((float)(pos - j0 - recd_sums_row(r, lane)));
+            if (j0 + 32 > wave_full)
+                for (int r = 0; r < 16; r++)
+                    if (j0 + recd_sums_row(r, lane) >= lim)
+                        s[r] = -INFINITY;
+            float top = s[0];
+            for (int r = 1; r < 16; r++)
+                top = fmaxf(top, s[r]);
+            top = fmaxf(top, __shfl_xor(top, 32)) - kLift<T>;
+            // the maximum moves only where it grows by more than 2^kSlack: the sums are rarely rescaled
+            if (__any(top > m + kSlack)) {
+                const float now = fmaxf(m, top);
+                const float f = now == m ? 1.0f : recd_exp2(m - now);
+                m = now;
+                l *= f;
+                for (int d = 0; d < DT; d++)
+                    for (int r = 0; r < 16; r++)
+                        o[d][r] *= f;
+            }
+            const float from = m == -INFINITY ? 0.0f : m;  // a row that has seen nothing yet
+            for (int r = 0; r < 16; r++) {
+                s[r] = recd_exp2(s[r] - from);
+                l += s[r];
+            }
+#pragma unroll
+            for (int h = 0; h < 2; h++) {
+                const Frag pf = recd_sums_frag<T>(s, h);
+#pragma unroll
+                for (int d = 0; d < DT; d++)
+                    o[d] = Mma::mul(vt.columns(32 * st + 16 * h, 32 * d, lane), pf, o[d]);
+            }
+        }
+    }
+    l += __shfl_xor(l, 32);
+    if (!there)
+        return;
+    if (a.splits > 1) {
+        const int64_t at = split * a.part_rows + at_row;
+        if (lane < 32) {
+            a.part_m[at] = m;
+            a.part_l[at] = l;
+        }
+        store_columns<float, DT>(a.part_o + at * a.d, o, 1.0f, a.d, lane);
+        return;
+    }
+    if (a.lse && lane < 32)
+        a.lse[at_row] = (m + log2f(l)) * kRecdLn2;  // -inf where l = 0
+    store_columns<T, DT>((T *)a.out + at_row * a.d, o, l == 0.0f ? 0.0f : 1.0f / l, a.d, lane);
+}
+
+// Joins the splits of the forward pass: 2^dlog threads a row, four elements each.
+template <typename T>
+__global__ __launch_bounds__(256) void k_attention_join(int64_t rows, int d, int dlog, int splits,
+                                                        const float *__restrict__ part_m, const float *__restrict__ part_l,
+                                                        const float *__restrict__ part_o, T *out, float *lse)
+{
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i >> dlog;
+    const int col = (int)(i & ((1 << dlog) - 1)) * 4;
+    if (row >= rows || col >= d)
+        return;
+    float m = -INFINITY;
+    for (int s = 0; s < splits; s++)
+        m = fmaxf(m, part_m[s * rows + row]);
+    const float from = m == -INFINITY ? 0.0f : m;
+    float l = 0.0f;
+    recd_f32x4 o = {};
+    for (int s = 0; s < splits; s++) {
+        const float f = recd_exp2(part_m[s * rows + row] - from);
+        l += f * part_l[s * rows + row];
+        const recd_f32x4 x = *reinterpret_cast<const recd_f32x4 *>(part_o + (s * rows + row) * d + col);
+        for (int e = 0; e < 4; e++)
+            o[e] += f * x[e];
+    }
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    store4<T>(out + row * d + col, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
+    if (lse && col == 0)
+        lse[row] = (m + log2f(l)) * kRecdLn2;
+}
+
+// {list, tile} of the slots of tiles of R rows; `group` rows for every entry of the offsets.
+__global__ void k_attention_tiles(int64_t lists, int64_t slots, int group, int R, const int64_t *__restrict__ offsets,
+                                  int2 *tiles)
+{
+    const int64_t list = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
+    if (list >= lists)
+        return;
+    const int64_t b = offsets[list] * group, e = offsets[list + 1] * group;
+    const int64_t s0 = b / R + list, n = (e - b + R - 1) / R;
+    const int64_t s1 = list + 1 < lists ? e / R + list + 1 : slots;
+    for (int64_t s = s0 < 0 ? 0 : s0; s < s1 && s < slots; s++)
+        tiles[s] = s - s0 < n ? make_int2((int)list, (int)(s - s0)) : make_int2(-1, 0);
+}
+
+// delta = sum over a head of g * o: 2^dlog lanes a row, a piece of 16 bytes each.
+template <typename T>
+__global__ __launch_bounds__(256) void k_attention_delta(int64_t rows, int d, int dlog, const T *__restrict__ out,
+                                                         const T *__restrict__ g, float *delta)
+{
+    constexpr int E = 16 / sizeof(T);
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i >> dlog;
+    const int col = (int)(i & ((1 << dlog) - 1)) * E;
+    float s = 0.0f;
+    if (row < rows && col < d) {
+        float x[E], y[E];
+        recd_load16(out + row * d + col, x);
+        recd_load16(g + row * d + col, y);
+        for (int e = 0; e < E; e++)
+            s += x[e] * y[e];
+    }
+    for (int o = (1 << dlog) >> 1; o; o >>= 1)
+        s += __shfl_xor(s, o);
+    if (row < rows && col == 0)
+        delta[row] = s;
+}
+
+// fp16: the largest |g| and |v| (as bits, whose order is the numbers'), and from them the power of two for ds.
+__global__ void k_attention_clear(uint32_t *tops)
+{
+    if (threadIdx.x < 2)
+        tops[threadIdx.x] = 0;
+}
+
+__global__ __launch_bounds__(256) void k_attention_tops(int64_t rows, int width, int64_t stride, const _Float16 *__restrict__ x,
+                                                        uint32_t *top)
+{
+    const int pieces = width / 8;
+    float t = 0.0f;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * pieces; i += (int64_t)gridDim.x * 256) {
+        float v[8];
+        recd_load16(x + i / pieces * stride + i % pieces * 8, v);
+        for (int e = 0; e < 8; e++)
+            t = fmaxf(t, fabsf(v[e]));
+    }
+    for (int o = 32; o; o >>= 1)
+        t = fmaxf(t, __shfl_xor(t, o));
+    if ((threadIdx.x & 63) == 0 && t > 0.0f)
+        atomicMax(top, __float_as_uint(t));
+}
+
+// |ds / scale| <= 2 d max|g| max|v|: brought below 2^15
+__global__ void k_attention_lift(int d, const uint32_t *tops, float *lift)
+{
+    const float bound = 2.0f * (float)d * __uint_as_float(tops[0]) * __uint_as_float(tops[1]);
+    int e = 15;
+    if (bound > 0.0f && bound < INFINITY)
+        frexpf(bound, &e);
+    e = 15 - e;
+    *lift = ldexpf(1.0f, e > 60 ? 60 : e);
+}
+
+// p and, over sums, ds without the scale, of one score: z = scale * q . k and dp = g . v
+struct Score {
+    float p, ds;
+};
+__device__ inline Score score_of(const Args &a, float qk, float dp, float from, float delta, float slope, int far, bool sees)
+{
+    float z, t = 0.0f;
+    if (a.cap != 0.0f) {
+        t = tanh_of(qk * (a.scale / a.cap));
+        z = a.cap * kRecdLog2e * t;
+    } else
+        z = qk * (a.scale * kRecdLog2e);
+    if (a.slopes)
+        z -= slope * fabsf((float)far);
+    const float p = sees ? recd_exp2(z - from) : 0.0f;
+    float ds = sees ? p * (dp - delta) : 0.0f;
+    if (a.cap != 0.0f)
+        ds *= 1.0f - t * t;
+    return {p, ds};
+}
+
+template <typename T, int DP, int NW, int BK> __global__ __launch_bounds__(64 * NW) void k_attention_grad_q(Args a)
+{
+    constexpr int KS = DP / 16, DT = DP / 32, THREADS = 64 * NW;
+    using Mma = RecdMma<T>;
+    using Frag = typename Mma::Frag;
+    __shared__ RecdTile<T, BK, DP> kt, vt;
+    Problem p;
+    int head, tile, split;
+    if (!find_tile(a, p, head, tile, split))
+        return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int first = tile * 32 * NW, end = first + 32 * NW < p.rows ? first + 32 * NW : p.rows;
+    if (first >= end)
+        return;
+    const int row0 = first + 32 * wave, row = row0 + (lane & 31);
+    const bool there = row < p.rows;
+    const int query = p.query(row, a.group), head_in = row - query * a.group;
+    const int lim = there ? p.limit(row, a.group) : 0;
+    const int wave_end = row0 < p.rows ? p.limit(row0 + 32 < p.rows ? row0 + 31 : p.rows - 1, a.group) : 0;
+    const int tiles = (p.limit(end - 1, a.group) + BK - 1) / BK;
+    const int H = a.G * a.group;
+    const int64_t q_row = p.q0 + query, at_row = q_row * H + p.head0 + head_in;
+    const float slope = a.slopes && there ? a.slopes[p.head0 + head_in] * kRecdLog2e : 0.0f;
+    const int pos = p.pos0 + query;
+    float from = there ? a.lse_in[at_row] * kRecdLog2e : 0.0f;
+    const float delta = there ? a.delta[at_row] : 0.0f;
+    if (from == -INFINITY)
+        from = 0.0f;  // sees nothing
+    const float lift = kHalf<T> ? *a.lift : 1.0f;
+
+    Frag qf[KS], gf[KS];
+    for (int k = 0; k < KS; k++) {
+        qf[k] = recd_row_frag<T>((const T *)a.q + q_row * a.q_stride + (int64_t)(p.head0 + head_in) * a.d, 16 * k, a.d, there,
+                                 lane);
+        gf[k] = recd_row_frag<T>((const T *)a.g + at_row * a.d, 16 * k, a.d, there, lane);
+    }
+    recd_f32x16 o[DT];
+    for (int d = 0; d < DT; d++)
+        o[d] = recd_f32x16{};
+    Stream<T, BK, DP, THREADS> ks, vs;
+    auto load = [&](int t) {
+        ks.load(a.d, [&](int r) -> const T * {
+            const int j = t * BK + r;
+            return j < p.nk ? (const T *)a.k + (p.k0 + j) * a.k_stride + (int64_t)head * a.d : nullptr;
+        });
+        vs.load(a.d, [&](int r) -> const T * {
+            const int j = t * BK + r;
+            return j < p.nk ? (const T *)a.v + (p.k0 + j) * a.v_stride + (int64_t)head * a.d : nullptr;
+        });
+    };
+    if (tiles > 0)
+        load(0);
+    for (int t = 0; t < tiles; t++) {
+        __syncthreads();
+        ks.store(kt);
+        vs.store(vt);
+        __syncthreads();
+        if (t + 1 < tiles)
+            load(t + 1);
+#pragma unroll
+        for (int st = 0; st < BK / 32; st++) {
+            const int j0 = t * BK + 32 * st;
+            if (j0 >= wave_end)
+                break;
+            recd_f32x16 s = {}, dp = {};
+#pragma unroll
+            for (int k = 0; k < KS; k++) {
+                s = Mma::mul(kt.rows(32 * st, 16 * k, lane), qf[k], s);
+                dp = Mma::mul(vt.rows(32 * st, 16 * k, lane), gf[k], dp);
+            }
+            for (int r = 0; r < 16; r++) {
+                const int j = j0 + recd_sums_row(r, lane);
+                s[r] = score_of(a, s[r], dp[r], from, delta, slope, pos - j, j < lim).ds * lift;
+            }
+#pragma unroll
+            for (int h = 0; h < 2; h++) {
+                const Frag sf = recd_sums_frag<T>(s, h);
+#pragma unroll
+                for (int d = 0; d < DT; d++)
+                    o[d] = Mma::mul(kt.columns(32 * st + 16 * h, 32 * d, lane), sf, o[d]);
+            }
+        }
+    }
+    if (there)
+        store_columns<T, DT>((T *)a.gq + q_row * a.gq_stride + (int64_t)(p.head0 + head_in) * a.d, o, a.scale / lift, a.d, lane);
+}
+
+// Keys stay, queries and their gradients stream past.
+template <typename T, int DP, int NW, int BQ> __global__ __launch_bounds__(64 * NW) void k_attention_grad_kv(Args a)
+{
+    constexpr int KS = DP / 16, DT = DP / 32, THREADS = 64 * NW;
+    using Mma = RecdMma<T>;
+    using Frag = typename Mma::Frag;
+    __shared__ RecdTile<T, BQ, DP> qt, gt;
+    __shared__ alignas(16) float row_from[BQ], row_delta[BQ], row_slope[BQ];
+    __shared__ alignas(16) int row_lim[BQ], row_pos[BQ];
+    Problem p;
+    int head, tile, split;
+    if (!find_tile(a, p, head, tile, split))
+        return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int first = tile * 32 * NW;
+    if (first >= p.nk)
+        return;
+    const int j0 = first + 32 * wave, j = j0 + (lane & 31);
+    const bool there = j < p.nk;
+    const int H = a.G * a.group;
+    Frag kf[KS], vf[KS];
+    for (int k = 0; k < KS; k++) {
+        kf[k] = recd_row_frag<T>((const T *)a.k + (p.k0 + j) * a.k_stride + (int64_t)head * a.d, 16 * k, a.d, there, lane);
+        vf[k] = recd_row_frag<T>((const T *)a.v + (p.k0 + j) * a.v_stride + (int64_t)head * a.d, 16 * k, a.d, there, lane);
+    }
+    recd_f32x16 dk[DT], dv[DT];
+    for (int d = 0; d < DT; d++)
+        dk[d] = dv[d] = recd_f32x16{};
+    const float lift = kHalf<T> ? *a.lift : 1.0f, lift_p = recd_exp2(kLiftP<T>);
+    // the first row that sees the block's first key
+    int from_row = 0;
+    if (p.causal && p.prefix <= first && first > p.pos0)
+        from_row = (int)((int64_t)(first - p.pos0) * a.group < p.rows ? (first - p.pos0) * a.group : p.rows);
+    const int tiles = (p.rows + BQ - 1) / BQ;
+    Stream<T, BQ, DP, THREADS> qs, gs;
+    float n_from = 0.0f, n_delta = 0.0f, n_slope = 0.0f;
+    int n_lim = 0, n_pos = 0;
+    auto load = [&](int t) {
+        auto at = [&](int r, int &query, int &h) {
+            query = p.query(r, a.group);
+            h = p.head0 + r - query * a.group;
+        };
+        qs.load(a.d, [&](int r) -> const T * {
+            int query, h;
+            at(t * BQ + r, query, h);
+            return t * BQ + r < p.rows ? (const T *)a.q + (p.q0 + query) * a.q_stride + (int64_t)h * a.d : nullptr;
+        });
+        gs.load(a.d, [&](int r) -> const T * {
+            int query, h;
+            at(t * BQ + r, query, h);
+            return t * BQ + r < p.rows ? (const T *)a.g + ((p.q0 + query) * H + h) * a.d : nullptr;
+        });
+        const int r = t * BQ + threadIdx.x;
+        n_from = n_delta = n_slope = 0.0f;
+        n_lim = n_pos = 0;
+        if (threadIdx.x < BQ && r < p.rows) {
+            int query, h;
+            at(r, query, h);
+            n_from = a.lse_in[(p.q0 + query) * H + h] * kRecdLog2e;
+            if (n_from == -INFINITY)
+                n_from = 0.0f;
+            n_delta = a.delta[(p.q0 + query) * H + h];
+            n_slope = a.slopes ? a.slopes[h] * kRecdLog2e : 0.0f;
+            n_lim = p.limit(r, a.group);
+            n_pos = p.pos0 + query;
+        }
+    };
+    const int t0 = from_row / BQ;
+    if (t0 < tiles)
+        load(t0);
+    for (int t = t0; t < tiles; t++) {
+        __syncthreads();
+        qs.store(qt);
+        gs.store(gt);
+        if (threadIdx.x < BQ) {
+            row_from[threadIdx.x] = n_from;
+            row_delta[threadIdx.x] = n_delta;
+            row_slope[threadIdx.x] = n_slope;
+            row_lim[threadIdx.x] = n_lim;
+            row_pos[threadIdx.x] = n_pos;
+        }
+        __syncthreads();
+        if (t + 1 < tiles)
+            load(t + 1);
+        if (j0 >= p.nk)
+            continue;
+#pragma unroll
+        for (int st = 0; st < BQ / 32; st++) {
+            if (row_lim[32 * st + 31] <= j0 && t * BQ + 32 * st + 32 <= p.rows)
+                continue;  // no row sees the wave's keys
+            recd_f32x16 s = {}, dp = {};
+#pragma unroll
+            for (int k = 0; k < KS; k++) {
+                s = Mma::mul(qt.rows(32 * st, 16 * k, lane), kf[k], s);
+                dp = Mma::mul(gt.rows(32 * st, 16 * k, lane), vf[k], dp);
+            }
+#pragma unroll
+            for (int r = 0; r < 16; r++) {
+                const int row = 32 * st + recd_sums_row(r, lane);
+                const Score x = score_of(a, s[r], dp[r], row_from[row], row_delta[row], row_slope[row], row_pos[row] - j,
+                                         j < row_lim[row]);
+                s[r] = x.p * lift_p;
+                dp[r] = x.ds * lift;
+            }
+#pragma unroll
+            for (int h = 0; h < 2; h++) {
+                const Frag pf = recd_sums_frag<T>(s, h), sf = recd_sums_frag<T>(dp, h);
+#pragma unroll
+                for (int d = 0; d < DT; d++) {
+                    dv[d] = Mma::mul(gt.columns(32 * st + 16 * h, 32 * d, lane), pf, dv[d]);
+                    dk[d] = Mma::mul(qt.columns(32 * st + 16 * h, 32 * d, lane), sf, dk[d]);
+                }
+            }
+        }
+    }
+    if (!there)
+        return;
+    store_columns<T, DT>((T *)a.gk + (p.k0 + j) * a.gk_stride + (int64_t)head * a.d, dk, a.scale / lift, a.d, lane);
+    store_columns<T, DT>((T *)a.gv + (p.k0 + j) * a.gv_stride + (int64_t)head * a.d, dv, 1.0f / lift_p, a.d, lane);
+}
+
+// Offsets that do not rise from 0 to the number of rows, or pass the caller's bound of a list's length.
+__global__ void k_validate_list_offsets(int64_t lists, int64_t rows, int64_t most, const int64_t *offsets, int *err)
+{
+    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i <= lists; i += (int64_t)gridDim.x * blockDim.x) {
+        const int64_t at = offsets[i];
+        if ((i == 0 && at != 0) || (i == lists && at != rows))
+            atomicOr(err, 1);
+        if (i < lists && (offsets[i + 1] < at || offsets[i + 1] - at > most))
+            atomicOr(err, 1);
+    }
+}
+
+recd_status check_attention(recd_ctx *ctx, const recd_attention *a, const void *q, const void *k, const void *v)
+{
+    if (!ctx)
+        return RECD_EINVAL;
+    if (!a)
+        return recd_fail(ctx, RECD_EINVAL, "null pointer argument");
+    if ((int)a->dtype < 0 || (int)a->dtype > 2)
+        return recd_fail(ctx, RECD_EINVAL, "unknown dtype");
+    if (a->heads <= 0 || a->kv_heads <= 0 || a->heads % a->kv_heads != 0 || a->heads > 4096)
+        return recd_fail(ctx, RECD_EINVAL, "heads=%d must be a multiple of kv_heads=%d, and at most 4096", a->heads, a->kv_heads);
+    const int64_t es = (int64_t)elem_size(a->dtype);
+    if (a->head_dim <= 0 || a->head_dim > RECD_MAX_HEAD_DIM || a->head_dim * es % 16 != 0)
+        return recd_fail(ctx, RECD_EINVAL, "head_dim=%d: a head's bytes must be a multiple of 16, and head_dim at most %d",
+                         a->head_dim, RECD_MAX_HEAD_DIM);
+    if (a->lists < 0 || a->max_q < 0 || a->max_k < 0 || a->q_rows < 0 || a->k_rows < 0)
+        return recd_fail(ctx, RECD_EINVAL, "lists, max_q, max_k, q_rows or k_rows < 0");
+    const int64_t most = ((int64_t)1 << 31) - 1;
+    if (a->lists > most / 2 || a->max_q > most / a->heads || a->max_k > most)
+        return recd_fail(ctx, RECD_EINVAL, "lists, max_q * heads or max_k of 2^31 and more");
+    if (!(a->softcap >= 0.0f) || a->softcap == INFINITY)
+        return recd_fail(ctx, RECD_EINVAL, "softcap must be 0 (none) or positive");
+    if (a->prefix && !a->causal)
+        return recd_fail(ctx, RECD_EINVAL, "prefix needs causal");
+    if (a->lists == 0 ? a->q_rows || a->k_rows : !a->q_offsets || !a->k_offsets)
+        return recd_fail(ctx, RECD_EINVAL, "rows without lists, or null offsets");
+    if ((a->q_rows && !q) || (a->k_rows && (!k || !v)))
+        return recd_fail(ctx, RECD_EINVAL, "null pointer argument");
+    if (a->q_stride < (int64_t)a->heads * a->head_dim || a->k_stride < (int64_t)a->kv_heads * a->head_dim ||
+        a->v_stride < (int64_t)a->kv_heads * a->head_dim)
+        return recd_fail(ctx, RECD_EINVAL, "a stride is less than a row");
+    if (((uintptr_t)q | (uintptr_t)k | (uintptr_t)v) % 16 || (a->q_stride | a->k_stride | a->v_stride) * es % 16)
+        return recd_fail(ctx, RECD_EINVAL, "q, k, v and their strides must be aligned to 16 bytes");
+    return RECD_OK;
+}
+
+recd_status validate_lists(recd_ctx *ctx, const recd_attention *a)
+{
+    ctx->plan.valid = false;
+    RECD_TRY(recd_reserve(ctx, 512));
+    int *err = reinterpret_cast<int *>(ctx->ws);
+    RECD_HIP(ctx, hipMemsetAsync(err, 0, sizeof(int), ctx->stream));
+    hipLaunchKernelGGL(k_validate_list_offsets, dim3(64), dim3(256), 0, ctx->stream, a->lists, a->q_rows, a->max_q,
+                       a->q_offsets, err);
+    hipLaunchKernelGGL(k_validate_list_offsets, dim3(64), dim3(256), 0, ctx->stream, a->lists, a->k_rows, a->max_k,
+                       a->k_offsets, err);
+    RECD_HIP(ctx, hipGetLastError());
+    ctx->host_pinned[0] = 0;
+    RECD_HIP(ctx, hipMemcpyAsync(ctx->host_pinned, err, sizeof(int), hipMemcpyDeviceToHost, ctx->stream));
+    RECD_HIP(ctx, hipStreamSynchronize(ctx->stream));
+    if ((int)ctx->host_pinned[0])
+        return recd_fail(ctx, RECD_EBOUNDS, "offsets do not rise from 0 to the rows, or a list is longer than its bound");
+    return RECD_OK;
+}
+
+Args common_args(const recd_attention *d, const void *q, const void *k, const void *v)
+{
+    Args a{};
+    a.G = d->kv_heads;
+    a.group = d->heads / d->kv_heads;
+    a.d = d->head_dim;
+    a.lists = d->lists;
+    a.splits = 1;
+    a.q_offsets = d->q_offsets;
+    a.k_offsets = d->k_offsets;
+    a.q = q;
+    a.k = k;
+    a.v = v;
+    a.q_stride = d->q_stride;
+    a.k_stride = d->k_stride;
+    a.v_stride = d->v_stride;
+    a.scale = d->scale;
+    a.cap = d->softcap;
+    a.slopes = d->slopes;
+    a.prefix = d->prefix;
+    a.causal = d->causal != 0;
+    a.part_rows = d->q_rows * d->heads;
+    return a;
+}
+
+// How the tiles of one side are listed: waves of 32 rows a tile, and slots.
+struct Tiling {
+    int waves, tiles_per_list;
+    int64_t slots;
+    bool table;
+};
+
+Tiling tiling(const recd_attention *d, int64_t rows, int64_t most, int group)
+{
+    Tiling t;
+    t.waves = most * group <= 64 ? 1 : 4;
+    const int64_t R = 32 * t.waves, per = (most * group + R - 1) / R;
+    t.slots = rows * group / R + d->lists;
+    t.table = d->lists * per > t.slots;
+    if (!t.table)
+        t.slots = d->lists * per;
+    t.tiles_per_list = (int)(per > 0 ? per : 1);
+    return t;
+}
+
+int log2_of(int n)
+{
+    int l = 0;
+    while ((1 << l) < n)
+        l++;
+    return l;
+}
+
+unsigned grid_of(const Args &a) { return (unsigned)((a.slots * a.splits + 7) / 8 * 8 * a.G); }
+
+enum Which { FORWARD, GRAD_Q, GRAD_KV };
+
+template <typename T, int DP, int NW> void launch_one(Which w, const Args &a, hipStream_t st)
+{
+    constexpr int B = sizeof(T) == 4 || NW == 1 ? 32 : 64;  // streamed rows of a tile
+    const dim3 grid(grid_of(a)), block(64 * NW);
+    if (w == FORWARD)
+        hipLaunchKernelGGL((k_attention<T, DP, NW, B>), grid, block, 0, st, a);
+    else if (w == GRAD_Q)
+        hipLaunchKernelGGL((k_attention_grad_q<T, DP, NW, B>), grid, block, 0, st, a);
+    else
+        hipLaunchKernelGGL((k_attention_grad_kv<T, DP, NW, 32>), grid, block, 0, st, a);
+}
+
+template <typename T> void launch(Which w, const Args &a, int waves, hipStream_t st)
+{
+    if (a.slots * a.splits == 0)
+        return;
+    if (a.d <= 32)
+        waves == 1 ? launch_one<T, 32, 1>(w, a, st) : launch_one<T, 32, 4>(w, a, st);
+    else if (a.d <= 64)
+        waves == 1 ? launch_one<T, 64, 1>(w, a, st) : launch_one<T, 64, 4>(w, a, st);
+    else
+        waves == 1 ? launch_one<T, 128, 1>(w, a, st) : launch_one<T, 128, 4>(w, a, st);
+}
+
+void launch_tiles(const recd_attention *d, const Tiling &t, int group, const int64_t *offsets, int2 *tiles, hipStream_t st)
+{
+    if (t.table)
+        hipLaunchKernelGGL(k_attention_tiles, dim3((unsigned)((d->lists + 255) / 256)), dim3(256), 0, st, d->lists, t.slots, group,
+                           32 * t.waves, offsets, tiles);
+}
+
+} // namespace
+
+extern "C" {
+
+recd_status recd_list_attention(recd_ctx *ctx, const recd_attention *d, const void *q, const void *k, const void *v, void *out,
+                                float *lse)
+{
+    RECD_TRY(check_attention(ctx, d, q, k, v));
+    if (d->q_rows && !out)
+        return recd_fail(ctx, RECD_EINVAL, "null pointer argument");
+    if ((uintptr_t)out % 16)
+        return recd_fail(ctx, RECD_EINVAL, "out must be aligned to 16 bytes");
+    if (d->lists == 0 || d->q_rows == 0)
+        return RECD_OK;
+    RECD_HIP(ctx, hipSetDevice(ctx->device));
+    if (ctx->validate)
+        RECD_TRY(validate_lists(ctx, d));
+    Args a = common_args(d, q, k, v);
+    a.out = out;
+    a.lse = lse;
+    const Tiling t = tiling(d, d->q_rows, d->max_q, a.group);
+    a.slots = t.slots;
+    a.tiles_per_list = t.tiles_per_list;
+    // few tiles: a tile's keys are split over blocks, at least 256 keys each
+    const int64_t blocks = (int64_t)ctx->num_cu * 4, have = t.slots * a.G > 0 ? t.slots * a.G : 1;
+    int64_t splits = (blocks + have - 1) / have;
+    if (splits > d->max_k / 256)
+        splits = d->max_k / 256;
+    a.splits = (int)(splits < 1 ? 1 : splits);
+    if (a.slots * a.splits / 8 + 1 > ((int64_t)1 << 27) / a.G)
+        return recd_fail(ctx, RECD_EINVAL, "too many tiles");
+    int2 *tiles;
+    auto carve = [&](WsCarver &c) {
+        tiles = t.table ? c.take<int2>(t.slots) : nullptr;
+        a.part_m = a.splits > 1 ? c.take<float>(a.splits * a.part_rows) : nullptr;
+        a.part_l = a.splits > 1 ? c.take<float>(a.splits * a.part_rows) : nullptr;
+        a.part_o = a.splits > 1 ? c.take<float>(a.splits * a.part_rows * a.d) : nullptr;
+    };
+    WsCarver size(nullptr);
+    carve(size);
+    if (size.off) {
+        ctx->plan.valid = false;  // tiles and parts overwrite the workspace a backward plan would live in
+        RECD_TRY(recd_reserve(ctx, size.off));
+    }
+    WsCarver c(ctx->ws);
+    carve(c);
+    a.tiles = tiles;
+    launch_tiles(d, t, a.group, d->q_offsets, tiles, ctx->stream);
+    recd_with_type(d->dtype, [&](auto e) {
+        using T = decltype(e);
+        launch<T>(FORWARD, a, t.waves, ctx->stream);
+        if (a.splits > 1) {
+            const int dlog = log2_of(a.d / 4);
+            hipLaunchKernelGGL((k_attention_join<T>), dim3((unsigned)(((a.part_rows << dlog) + 255) / 256)), dim3(256), 0,
+                               ctx->stream, a.part_rows, a.d, dlog, a.splits, a.part_m, a.part_l, a.part_o, (T *)out, lse);
+        }
+    });
+    RECD_HIP(ctx, hipGetLastError());
+    return RECD_OK;
+}
+
+recd_status recd_list_attention_backward(recd_ctx *ctx, const recd_attention *d, const void *q, const void *k, const void *v,
+                                         const void *out, const float *lse, const void *grad_out, void *grad_q, void *grad_k,
+                                         void *grad_v, int64_t grad_q_stride, int64_t grad_k_stride, int64_t grad_v_stride)
+{
+    RECD_TRY(check_attention(ctx, d, q, k, v));
+    if ((d->q_rows && (!out || !lse || !grad_out || !grad_q)) || (d->k_rows && (!grad_k || !grad_v)))
+        return recd_fail(ctx, RECD_EINVAL, "null pointer argument");
+    if (grad_q_stride < (int64_t)d->heads * d->head_dim || grad_k_stride < (int64_t)d->kv_heads * d->head_dim ||
+        grad_v_stride < (int64_t)d->kv_heads * d->head_dim)
+        return recd_fail(ctx, RECD_EINVAL, "a stride is less than a row");
+    if (((uintptr_t)out | (uintptr_t)grad_out | (uintptr_t)grad_q | (uintptr_t)grad_k | (uintptr_t)grad_v) % 16 ||
+        (grad_q_stride | grad_k_stride | grad_v_stride) * (int64_t)elem_size(d->dtype) % 16)
+        return recd_fail(ctx, RECD_EINVAL, "out, the gradients and their strides must be aligned to 16 bytes");
+    if (d->lists == 0)
+        return RECD_OK;
+    RECD_HIP(ctx, hipSetDevice(ctx->device));
+    if (ctx->validate)
+        RECD_TRY(validate_lists(ctx, d));
+    Args a = common_args(d, q, k, v);
+    a.out_in = out;
+    a.lse_in = lse;
+    a.g = grad_out;
+    a.gq = grad_q;
+    a.gk = grad_k;
+    a.gv = grad_v;
+    a.gq_stride = grad_q_stride;
+    a.gk_stride = grad_k_stride;
+    a.gv_stride = grad_v_stride;
+    const Tiling tq = tiling(d, d->q_rows, d->max_q, a.group), tk = tiling(d, d->k_rows, d->max_k, 1);
+    if (tq.slots / 8 + 1 > ((int64_t)1 << 27) / a.G || tk.slots / 8 + 1 > ((int64_t)1 << 27) / a.G)
+        return recd_fail(ctx, RECD_EINVAL, "too many tiles");
+    const bool half = d->dtype == RECD_F16;
+    int2 *tiles_q, *tiles_k;
+    float *delta, *lift;
+    uint32_t *tops;
+    auto carve = [&](WsCarver &c) {
+        tiles_q = tq.table ? c.take<int2>(tq.slots) : nullptr;
+        tiles_k = tk.table ? c.take<int2>(tk.slots) : nullptr;
+        delta = c.take<float>(a.part_rows);
+        tops = half ? c.take<uint32_t>(2) : nullptr;
+        lift = half ? c.take<float>(1) : nullptr;
+    };
+    WsCarver size(nullptr);
+    carve(size);
+    ctx->plan.valid = false;
+    RECD_TRY(recd_reserve(ctx, size.off));
+    WsCarver c(ctx->ws);
+    carve(c);
+    a.delta = delta;
+    a.lift = lift;
+    hipStream_t st = ctx->stream;
+    if (half) {
+        hipLaunchKernelGGL(k_attention_clear, dim3(1), dim3(64), 0, st, tops);
+        if (d->q_rows)
+            hipLaunchKernelGGL(k_attention_tops, dim3((unsigned)ctx->num_cu), dim3(256), 0, st, d->q_rows * d->heads, a.d, a.d,
+                               (const _Float16 *)grad_out, tops);
+        if (d->k_rows)
+            hipLaunchKernelGGL(k_attention_tops, dim3((unsigned)ctx->num_cu), dim3(256), 0, st, d->k_rows, a.G * a.d, d->v_stride,
+                               (const _Float16 *)v, tops + 1);
+        hipLaunchKernelGGL(k_attention_lift, dim3(1), dim3(1), 0, st, a.d, tops, lift);
+    }
+    launch_tiles(d, tq, a.group, d->q_offsets, tiles_q, st);
+    launch_tiles(d, tk, 1, d->k_offsets, tiles_k, st);
+    recd_with_type(d->dtype, [&](auto e) {
+        using T = decltype(e);
+        const int dlog = log2_of(a.d * (int)sizeof(T) / 16);
+        if (d->q_rows) {
+            hipLaunchKernelGGL((k_attention_delta<T>), dim3((unsigned)(((a.part_rows << dlog) + 255) / 256)), dim3(256), 0, st,
+                               a.part_rows, a.d, dlog, (const T *)out, (const T *)grad_out, delta);
+            a.tiles = tiles_q;
+            a.slots = tq.slots;
+            a.tiles_per_list = tq.tiles_per_list;
+            launch<T>(GRAD_Q, a, tq.waves, st);
+        }
+        a.tiles = tiles_k;
+        a.slots = tk.slots;
+        a.tiles_per_list = tk.tiles_per_list;
+        if (d->k_rows)
+            launch<T>(GRAD_KV, a, tk.waves, st);
+    });
+    RECD_HIP(ctx, hipGetLastError());
+    return RECD_OK;
+}
+
+} // extern "C"

@@ -1,0 +1,125 @@
+// Matrix products on tiles of 32 x 32 with the contraction in steps of 16, for fp16, bf16 and fp32 operands and
+// fp32 sums.
+//
+// Every operator here has one side that stays in registers (32 columns, one a lane of each half wave) and streams
+// the other through LDS, twice over: once by rows (a product over the row's elements gives scores, 32 streamed rows
+// by 32 columns) and once by columns (a product over the streamed rows, with what became of the scores).
+//   A (streamed): lane l holds row l & 31, elements k = (l >> 5) * 8 .. + 8 of the step
+//   B (kept):     lane l holds column l & 31, the same elements k
+//   sums:         lane l holds column l & 31, register r holds row 8 * (r >> 2) + 4 * (l >> 5) + (r & 3)
+// The second product contracts over the streamed rows in the order in which the sums' registers hold them, so the
+// scores go from sums to B without leaving their lane: step m takes registers 8m .. 8m + 7, and the A operand's
+// element e is then row 16m + 8 * (e >> 2) + 4 * (l >> 5) + (e & 3) of column l & 31.  16-bit columns are read by the LDS's
+// transposing loads, which hand a lane four rows of its column.
+#pragma once
+
+#include "recd_vec.h"
+
+typedef float recd_f32x16 __attribute__((ext_vector_type(16)));
+typedef float recd_f32x8 __attribute__((ext_vector_type(8)));
+typedef short recd_s16x4 __attribute__((ext_vector_type(4)));
+
+template <typename T> struct RecdMma;
+
+template <> struct RecdMma<_Float16> {
+    using Frag = recd_f16x8;
+    static __device__ inline recd_f32x16 mul(Frag a, Frag b, recd_f32x16 c)
+    {
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+    }
+};
+template <> struct RecdMma<__bf16> {
+    using Frag = recd_bf16x8;
+    static __device__ inline recd_f32x16 mul(Frag a, Frag b, recd_f32x16 c)
+    {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+    }
+};
+template <> struct RecdMma<float> {
+    using Frag = recd_f32x8;
+    // step e contracts element e of the lower half wave's eight and of the upper's
+    static __device__ inline recd_f32x16 mul(Frag a, Frag b, recd_f32x16 c)
+    {
+#pragma unroll
+        for (int e = 0; e < 8; e++)
+            c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], b[e], c, 0, 0, 0);
+        return c;
+    }
+};
+
+// A tile of ROWS rows of DP elements in LDS.  16 bytes between the rows spread the lanes' reads over the banks.
+template <typename T, int ROWS, int DP> struct RecdTile {
+    static constexpr int E = 16 / sizeof(T), LD = DP + E, PIECES = ROWS * (DP / E);
+    using Frag = typename RecdMma<T>::Frag;
+    using Piece = typename RecdPiece<T>::type;
+    alignas(16) T at[ROWS * LD];
+
+    // elements k0 .. k0 + 16 of the 32 rows from row0 on
+    __device__ inline Frag rows(int row0, int k0, int lane) const
+    {
+        return *reinterpret_cast<const Frag *>(at + (row0 + (lane & 31)) * LD + k0 + (lane >> 5) * 8);
+    }
+    // columns d0 .. d0 + 32 of the 16 rows from row0 on, in the order of the sums' registers
+    __device__ inline Frag columns(int row0, int d0, int lane) const
+    {
+        if constexpr (sizeof(T) == 4) {
+            Frag f;
+            const T *p = at + (row0 + 4 * (lane >> 5)) * LD + d0 + (lane & 31);
+#pragma unroll
+            for (int e = 0; e < 8; e++)
+                f[e] = p[(8 * (e >> 2) + (e & 3)) * LD];
+            return f;
+        } else {
+            // 16 lanes name four rows of 16 columns, 8 bytes each; each of them receives one column
+            using Half = __attribute__((address_space(3))) recd_s16x4;
+            const int i = lane & 15;
+            const T *p = at + (row0 + 4 * (lane >> 5) + (i >> 2)) * LD + d0 + 16 * ((lane >> 4) & 1) + 4 * (i & 3);
+            union {
+                recd_s16x4 half[2];
+                Frag f;
+            } u;
+            u.half[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Half *)(p));
+            u.half[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Half *)(p + 8 * LD));
+            return u.f;
+        }
+    }
+    __device__ inline void put(int piece, Piece v)
+    {
+        constexpr int PR = DP / E;
+        *reinterpret_cast<Piece *>(at + (piece / PR) * LD + (piece % PR) * E) = v;
+    }
+};
+
+// The step's 16 elements from k0 on of a row in global memory (8 a half wave), zero from element D on.
+template <typename T> __device__ inline typename RecdMma<T>::Frag recd_row_frag(const T *row, int k0, int D, bool there, int lane)
+{
+    constexpr int E = 16 / sizeof(T);
+    union {
+        typename RecdPiece<T>::type piece[8 / E];
+        typename RecdMma<T>::Frag f;
+    } u;
+#pragma unroll
+    for (int i = 0; i < 8 / E; i++) {
+        const int k = k0 + (lane >> 5) * 8 + i * E;
+        u.piece[i] = typename RecdPiece<T>::type{};
+        if (there && k < D)
+            u.piece[i] = *reinterpret_cast<const typename RecdPiece<T>::type *>(row + k);
+    }
+    return u.f;
+}
+
+// Sums' registers 8m .. 8m + 7 as the B operand of a product over streamed rows.
+template <typename T> __device__ inline typename RecdMma<T>::Frag recd_sums_frag(const recd_f32x16 &s, int m)
+{
+    typename RecdMma<T>::Frag f;
+#pragma unroll
+    for (int e = 0; e < 8; e++)
+        f[e] = (T)s[8 * m + e];
+    return f;
+}
+
+// Row of a sums' register within its 32.
+__device__ inline int recd_sums_row(int r, int lane) { return 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3); }
+
+constexpr float kRecdLog2e = 1.4426950408889634f, kRecdLn2 = 0.6931471805599453f;
+__device__ inline float recd_exp2(float x) { return __builtin_amdgcn_exp2f(x); }

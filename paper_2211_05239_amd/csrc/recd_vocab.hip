@@ -1,0 +1,642 @@
+// Softmax cross entropy of rows x [n, D] against a whole table [V, D] as the vocabulary, and its gradients.
+//
+//   z_iv = scale * x_i . W_v,  lse_i = log sum_v exp(z_iv),  loss_i = lse_i - z_i,t(i)
+//   p_iv = exp(z_iv - lse_i),  m_i = sum_v p_iv W_v
+//   gx_i = scale * g_i * (m_i - W_t(i)),  gW_v = scale * sum_i g_i * (p_iv - [t(i) = v]) * x_i
+//
+// The logits [n, V] are never stored.  The forward pass streams the table once past rows that stay in registers,
+// with a running maximum and sum per row; for training it carries the softmax-weighted mean m_i of the table's rows
+// along, as a second product with the scores' exponentials, so that the gradient by x is one subtraction later and
+// the backward pass needs one recomputation of the scores instead of two: 8 n V D operations for both passes, where
+// 6 are needed at least.  The backward pass turns the sides round: table rows stay in registers, and the rows x
+// stream past them.  Both passes are bound by the matrix cores and the exponentials beside them.
+//
+// The vocabulary is cut into splits where there are few rows; their (maximum, sum, mean) are joined in the order of the
+// splits.  Exponentials are rounded to the tables' type for the second product, as the other operand of the matrix
+// cores has it; fp16 ones are scaled by powers of two so that small ones keep their bits.  Sums, maxima and products'
+// sums are held in fp32.
+#include "recd_internal.h"
+#include "recd_mfma.h"
+
+#include <math.h>
+
+namespace {
+
+constexpr int kBlock = 256, kWaves = 4;
+// A row's running maximum is moved only where a new one exceeds it by this many powers of two: the exponentials stay
+// far inside the range, and the sums are rarely rescaled.
+constexpr float kSlack = 8.0f;
+// fp16 exponentials are held 2^7 times larger: at most 2^15 with the slack, and exact to 2^-31 of the maximum.
+template <typename T> constexpr float kLift = std::is_same<T, _Float16>::value ? 7.0f : 0.0f;
+
+// Streamed rows [row0, row0 + ROWS) of a matrix [n, D] into registers and from there into a tile.
+template <typename T, int ROWS, int DP> struct Stream {
+    using Tile = RecdTile<T, ROWS, DP>;
+    static constexpr int PT = (Tile::PIECES + kBlock - 1) / kBlock;
+    typename Tile::Piece held[PT];
+
+    __device__ inline void load(const T *m, int64_t row0, int64_t n, int D)
+    {
+        constexpr int PR = DP / Tile::E;
+#pragma unroll
+        for (int i = 0; i < PT; i++) {
+            const int piece = threadIdx.x + i * kBlock;
+            const int64_t row = row0 + piece / PR;
+            const int at = piece % PR * Tile::E;
+            held[i] = typename Tile::Piece{};
+            if (piece < Tile::PIECES && row < n && at < D)
+                held[i] = *reinterpret_cast<const typename Tile::Piece *>(m + row * D + at);
+        }
+    }
+    __device__ inline void store(Tile &t)
+    {
+#pragma unroll
+        for (int i = 0; i < PT; i++)
+            if (threadIdx.x + i * kBlock < (unsigned)Tile::PIECES)
+                t.put(threadIdx.x + i * kBlock, held[i]);
+    }
+};
+
+template <typename Frag> __device__ inline Frag negated(Frag f)
+{
+    for (int e = 0; e < 8; e++)
+        f[e] = -f[e];
+    return f;
+}
+
+struct ForwardArgs {
+    int64_t n, V;
+    int D;
+    float c;            // |scale| * log2(e); the sign goes into the kept side
+    bool negative;
+    const void *x, *table;
+    int row_blocks, splits;
+    int64_t tiles_per_split;
+    float *part_m, *part_l, *part_o;  // [parts][n] and [parts][n][D]: maximum (in powers of two), sum, weighted sum
+};
+
+// 32 * N rows a wave.  SHARE: the block's waves hold the same rows and take turns at the table's rows, each a part
+// of its own (few rows); otherwise they hold different rows and all see every table row.
+template <typename T, int DP, int N, bool SHARE, bool MEAN>
+__global__ __launch_bounds__(kBlock) void k_vocab_forward(ForwardArgs a)
+{
+    constexpr int VT = SHARE ? 128 : (sizeof(T) == 4 && DP == 256 ? 32 : 64);
+    constexpr int KS = DP / 16, DT = DP / 32;
+    using Mma = RecdMma<T>;
+    using Frag = typename Mma::Frag;
+    __shared__ RecdTile<T, VT, DP> tile;
+    // the row blocks of one split side by side on one die, whose L2 then serves the split's rows to all of them
+    const int xcd = blockIdx.x & 7, at = blockIdx.x >> 3;
+    const int rb = at % a.row_blocks, split = at / a.row_blocks * 8 + xcd;
+    if (split >= a.splits)
+        return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t row0 = (int64_t)rb * (SHARE ? 32 * N : 32 * N * kWaves) + (SHARE ? 0 : wave * 32 * N);
+    const int64_t tiles = (a.V + VT - 1) / VT, t0 = split * a.tiles_per_split;
+    const int64_t t1 = t0 + a.tiles_per_split < tiles ? t0 + a.tiles_per_split : tiles;
+
+    Frag xf[N][KS];
+    for (int j = 0; j < N; j++) {
+        const int64_t row = row0 + 32 * j + (lane & 31);
+        for (int k = 0; k < KS; k++) {
+            xf[j][k] = recd_row_frag<T>((const T *)a.x + row * a.D, 16 * k, a.D, row < a.n, lane);
+            if (a.negative)
+                xf[j][k] = negated(xf[j][k]);
+        }
+    }
+    float m[N], l[N];
+    recd_f32x16 o[N][MEAN ? DT : 1];
+    for (int j = 0; j < N; j++) {
+        m[j] = -INFINITY;
+        l[j] = 0.0f;
+        for (int d = 0; d < (MEAN ? DT : 1); d++)
+            o[j][d] = recd_f32x16{};
+    }
+    Stream<T, VT, DP> stream;
+    if (t0 < t1)
+        stream.load((const T *)a.table, t0 * VT, a.V, a.D);
+    for (int64_t t = t0; t < t1; t++) {
+        __syncthreads();
+        stream.store(tile);
+        __syncthreads();
+        if (t + 1 < t1)
+            stream.load((const T *)a.table, (t + 1) * VT, a.V, a.D);
+        if (row0 >= a.n)
+            continue;
+        for (int st = SHARE ? wave : 0; st < VT / 32; st += SHARE ? kWaves : 1) {
+            recd_f32x16 s[N];
+            for (int j = 0; j < N; j++)
+                s[j] = recd_f32x16{};
+#pragma unroll
+            for (int k = 0; k < KS; k++) {
+                const Frag w = tile.rows(32 * st, 16 * k, lane);
+                for (int j = 0; j < N; j++)
+                    s[j] = Mma::mul(w, xf[j][k], s[j]);
+            }
+            const int64_t left = a.V - (t * VT + 32 * st);
+            if (left < 32)
+                for (int j = 0; j < N; j++)
+                    for (int r = 0; r < 16; r++)
+                        if (recd_sums_row(r, lane) >= left)
+                            s[j][r] = -INFINITY;
+#pragma unroll
+            for (int j = 0; j < N; j++) {
+                float top = s[j][0];
+                for (int r = 1; r < 16; r++)
+                    top = fmaxf(top, s[j][r]);
+                top = fmaxf(top, __shfl_xor(top, 32)) * a.c - kLift<T>;
+                if (__any(top > m[j] + kSlack)) {
+                    const float now = fmaxf(m[j], top);
+                    const float f = now == m[j] ? 1.0f : recd_exp2(m[j] - now);
+                    m[j] = now;
+                    l[j] *= f;
+                    if constexpr (MEAN)
+                        for (int d = 0; d < DT; d++)
+                            for (int r = 0; r < 16; r++)
+                                o[j][d][r] *= f;
+                }
+                const float from = m[j] == -INFINITY ? 0.0f : m[j];  // a row of logits that are all -inf
+                float sum = 0.0f;
+                for (int r = 0; r < 16; r++) {
+                    s[j][r] = recd_exp2(s[j][r] * a.c - from);
+                    sum += s[j][r];
+                }
+                l[j] += sum;
+            }
+            if constexpr (MEAN) {
+#pragma unroll
+                for (int h = 0; h < 2; h++) {
+                    Frag p[N];
+                    for (int j = 0; j < N; j++)
+                        p[j] = recd_sums_frag<T>(s[j], h);
+#pragma unroll
+                    for (int d = 0; d < DT; d++) {
+                        const Frag w = tile.columns(32 * st + 16 * h, 32 * d, lane);
+                        for (int j = 0; j < N; j++)
+                            o[j][d] = Mma::mul(w, p[j], o[j][d]);
+                    }
+                }
+            }
+        }
+    }
+    const int64_t part = SHARE ? (int64_t)split * kWaves + wave : split;
+    for (int j = 0; j < N; j++) {
+        const int64_t row = row0 + 32 * j + (lane & 31);
+        const float sum = l[j] + __shfl_xor(l[j], 32);
+        if (row >= a.n)
+            continue;
+        if (lane < 32) {
+            a.part_m[part * a.n + row] = m[j];
+            a.part_l[part * a.n + row] = sum;
+        }
+        if constexpr (MEAN)
+            for (int d = 0; d < DT; d++)
+                for (int r = 0; r < 16; r += 4) {
+                    const int col = 32 * d + recd_sums_row(r, lane);
+                    if (col < a.D)
+                        *reinterpret_cast<recd_f32x4 *>(a.part_o + (part * a.n + row) * a.D + col) =
+                            recd_f32x4{o[j][d][r], o[j][d][r + 1], o[j][d][r + 2], o[j][d][r + 3]};
+                }
+    }
+}
+
+__device__ inline float wave_max(float v)
+{
+    for (int o = 32; o; o >>= 1)
+        v = fmaxf(v, __shfl_xor(v, o));
+    return v;
+}
+
+__device__ inline float wave_sum(float v)
+{
+    for (int o = 32; o; o >>= 1)
+        v += __shfl_xor(v, o);
+    return v;
+}
+
+// Joins the parts of a row: a wave per row.
+template <typename T>
+__global__ __launch_bounds__(kBlock) void k_vocab_join(int64_t n, int64_t V, int D, float scale, int parts,
+                                                       const float *__restrict__ part_m, const float *__restrict__ part_l,
+                                                       const float *__restrict__ part_o, const T *__restrict__ x,
+                                                       const T *__restrict__ table, const int64_t *__restrict__ targets,
+                                                       float *loss, float *lse, float *mean_row)
+{
+    constexpr int E = 16 / sizeof(T);
+    const int lane = threadIdx.x & 63;
+    const int64_t row = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6);
+    if (row >= n)
+        return;
+    float m = -INFINITY;
+    for (int p = lane; p < parts; p += 64)
+        m = fmaxf(m, part_m[p * n + row]);
+    m = wave_max(m);
+    const float from = m == -INFINITY ? 0.0f : m;
+    float l = 0.0f;
+    for (int p = lane; p < parts; p += 64)
+        l += recd_exp2(part_m[p * n + row] - from) * part_l[p * n + row];
+    l = wave_sum(l);
+    const int64_t t = targets[row];
+    float dot = 0.0f;
+    if (t >= 0 && t < V)
+        for (int v = lane; v < D / E; v += 64) {
+            float a[E], b[E];
+            recd_load16(x + row * D + v * E, a);
+            recd_load16(table + t * D + v * E, b);
+            for (int e = 0; e < E; e++)
+                dot += a[e] * b[e];
+        }
+    dot = wave_sum(dot);
+    const float total = (m + log2f(l)) * kRecdLn2;
+    if (lane == 0) {
+        lse[row] = total;
+        loss[row] = t >= 0 && t < V ? total - scale * dot : 0.0f;
+    }
+    if (!mean_row)
+        return;
+    const float inv = 1.0f / l;
+    for (int d = lane; d < D; d += 64) {
+        float s = 0.0f;
+#pragma unroll 4
+        for (int p = 0; p < parts; p++)
+            s += recd_exp2(part_m[p * n + row] - from) * part_o[(p * n + row) * D + d];
+        mean_row[row * D + d] = s * inv;
+    }
+}
+
+// The power of two that brings the largest |grad_loss| into [2^13, 2^14): fp16 products of it with probabilities neither
+// overflow nor lose bits that matter beside the largest.
+__global__ __launch_bounds__(1024) void k_vocab_lift(int64_t n, const float *__restrict__ grad_loss, float *lift)
+{
+    __shared__ float tops[16];
+    float top = 0.0f;
+    for (int64_t i = threadIdx.x; i < n; i += 1024)
+        top = fmaxf(top, fabsf(grad_loss[i]));
+    top = wave_max(top);
+    if ((threadIdx.x & 63) == 0)
+        tops[threadIdx.x >> 6] = top;
+    __syncthreads();
+    if (threadIdx.x)
+        return;
+    for (int i = 0; i < 16; i++)
+        top = fmaxf(top, tops[i]);
+    int e = 0;
+    frexpf(top, &e);
+    e = 14 - (top > 0.0f && top < INFINITY ? e : 14);
+    *lift = ldexpf(1.0f, e > 100 ? 100 : e);
+}
+
+// What the table's gradient needs of a row (its lse in powers of two, its weight, its target), and the gradient by the row:
+// a wave per row.
+template <typename T>
+__global__ __launch_bounds__(kBlock) void k_vocab_rows(int64_t n, int64_t V, int D, float scale, const T *__restrict__ table,
+                                                       const int64_t *__restrict__ targets, const float *__restrict__ lse,
+                                                       const float *__restrict__ mean_row,
+                                                       const float *__restrict__ grad_loss, const float *__restrict__ lift,
+                                                       float *row_lse, float *row_g, int32_t *row_t, T *grad_x)
+{
+    constexpr int E = 16 / sizeof(T);
+    const int lane = threadIdx.x & 63;
+    const int64_t row = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6);
+    if (row >= n)
+        return;
+    const int64_t t = targets[row];
+    const bool has = t >= 0 && t < V;
+    const float g = has ? grad_loss[row] : 0.0f;
+    if (lane == 0 && row_g) {
+        row_lse[row] = lse[row] * kRecdLog2e;
+        row_g[row] = lift ? g * *lift : g;
+        row_t[row] = has ? (int32_t)t : -1;
+    }
+    if (!grad_x)
+        return;
+    for (int v = lane; v < D / E; v += 64) {
+        float a[E], b[E];
+        for (int e = 0; e < E; e++)
+            a[e] = b[e] = 0.0f;
+        if (has) {
+            recd_load16(table + t * D + v * E, b);
+            for (int e = 0; e < E; e++)
+                a[e] = mean_row[row * D + v * E + e];
+        }
+        for (int e = 0; e < E; e++)
+            a[e] = scale * g * (a[e] - b[e]);
+        recd_store16(grad_x + row * D + v * E, a);
+    }
+}
+
+struct TableGradArgs {
+    int64_t n, V;
+    int D;
+    float c, scale;
+    bool negative;
+    const void *x, *table;
+    const float *row_lse, *row_g, *lift;
+    const int32_t *row_t;
+    void *grad_table;
+};
+
+// 32 * N table rows a wave; the rows x stream past them.
+template <typename T, int DP, int N> __global__ __launch_bounds__(kBlock) void k_vocab_grad_table(TableGradArgs a)
+{
+    constexpr int XT = sizeof(T) == 4 && DP == 256 ? 32 : 64;
+    constexpr int KS = DP / 16, DT = DP / 32;
+    using Mma = RecdMma<T>;
+    using Frag = typename Mma::Frag;
+    __shared__ RecdTile<T, XT, DP> tile;
+    __shared__ alignas(16) float lse[XT], g[XT];
+    __shared__ int32_t target[XT];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t v0 = (int64_t)blockIdx.x * 32 * N * kWaves + wave * 32 * N;
+    Frag wf[N][KS];
+    recd_f32x16 o[N][DT];
+    for (int j = 0; j < N; j++) {
+        const int64_t v = v0 + 32 * j + (lane & 31);
+        for (int k = 0; k < KS; k++) {
+            wf[j][k] = recd_row_frag<T>((const T *)a.table + v * a.D, 16 * k, a.D, v < a.V, lane);
+            if (a.negative)
+                wf[j][k] = negated(wf[j][k]);
+        }
+        for (int d = 0; d < DT; d++)
+            o[j][d] = recd_f32x16{};
+    }
+    const int64_t tiles = (a.n + XT - 1) / XT;
+    Stream<T, XT, DP> stream;
+    float next_lse = 0.0f, next_g = 0.0f;
+    int32_t next_t = -1;
+    auto load = [&](int64_t t) {
+        stream.load((const T *)a.x, t * XT, a.n, a.D);
+        const int64_t row = t * XT + threadIdx.x;
+        const bool there = threadIdx.x < XT && row < a.n;
+        next_lse = there ? a.row_lse[row] : 0.0f;
+        next_g = there ? a.row_g[row] : 0.0f;
+        next_t = there ? a.row_t[row] : -1;
+    };
+    load(0);
+    for (int64_t t = 0; t < tiles; t++) {
+        __syncthreads();
+        stream.store(tile);
+        if (threadIdx.x < XT) {
+            lse[threadIdx.x] = next_lse;
+            g[threadIdx.x] = next_g;
+            target[threadIdx.x] = next_t;
+        }
+        __syncthreads();
+        if (t + 1 < tiles)
+            load(t + 1);
+        if (v0 >= a.V)
+            continue;
+#pragma unroll
+        for (int st = 0; st < XT / 32; st++) {
+            recd_f32x16 s[N];
+            for (int j = 0; j < N; j++)
+                s[j] = recd_f32x16{};
+#pragma unroll
+            for (int k = 0; k < KS; k++) {
+                const Frag x = tile.rows(32 * st, 16 * k, lane);
+                for (int j = 0; j < N; j++)
+                    s[j] = Mma::mul(x, wf[j][k], s[j]);
+            }
+            const int32_t tg = target[32 * st + (lane & 31)];
+            const bool hit = __any(tg >= v0 && tg < v0 + 32 * N);  // one of these rows' targets is among the wave's
+            for (int r = 0; r < 16; r += 4) {
+                const int row = 32 * st + recd_sums_row(r, lane);
+                const recd_f32x4 from = *reinterpret_cast<const recd_f32x4 *>(lse + row);
+                const recd_f32x4 by = *reinterpret_cast<const recd_f32x4 *>(g + row);
+                for (int q = 0; q < 4; q++)
+                    for (int j = 0; j < N; j++)
+                        s[j][r + q] = recd_exp2(s[j][r + q] * a.c - from[q]) * by[q];
+            }
+            if (hit)
+                for (int j = 0; j < N; j++)
+                    for (int r = 0; r < 16; r++) {
+                        const int row = 32 * st + recd_sums_row(r, lane);
+                        if (target[row] == v0 + 32 * j + (lane & 31))
+                            s[j][r] -= g[row];
+                    }
+#pragma unroll
+            for (int h = 0; h < 2; h++) {
+                Frag p[N];
+                for (int j = 0; j < N; j++)
+                    p[j] = recd_sums_frag<T>(s[j], h);
+#pragma unroll
+                for (int d = 0; d < DT; d++) {
+                    const Frag x = tile.columns(32 * st + 16 * h, 32 * d, lane);
+                    for (int j = 0; j < N; j++)
+                        o[j][d] = Mma::mul(x, p[j], o[j][d]);
+                }
+            }
+        }
+    }
+    const float back = a.lift ? a.scale / *a.lift : a.scale;
+    for (int j = 0; j < N; j++) {
+        const int64_t v = v0 + 32 * j + (lane & 31);
+        if (v >= a.V)
+            continue;
+        for (int d = 0; d < DT; d++)
+            for (int r = 0; r < 16; r += 4) {
+                const int col = 32 * d + recd_sums_row(r, lane);
+                if (col >= a.D)
+                    continue;
+                T out[4];
+                for (int q = 0; q < 4; q++)
+                    out[q] = (T)(o[j][d][r + q] * back);
+                __builtin_memcpy((T *)a.grad_table + v * a.D + col, out, sizeof out);
+            }
+    }
+}
+
+// Targets that are no row's sign and lie beyond the table.
+__global__ void k_validate_targets(int64_t n, int64_t V, const int64_t *targets, int *err)
+{
+    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += (int64_t)gridDim.x * blockDim.x)
+        if (targets[i] >= V)
+            atomicOr(err, 1);
+}
+
+recd_status check_vocab(recd_ctx *ctx, int64_t n, int64_t V, int D, recd_dtype dt, float scale)
+{
+    if (!ctx)
+        return RECD_EINVAL;
+    if (n < 0 || V < 0 || V > ((int64_t)1 << 31) - 1 || n > ((int64_t)1 << 31) - 1)
+        return recd_fail(ctx, RECD_EINVAL, "n=%lld or V=%lld outside [0, 2^31)", (long long)n, (long long)V);
+    if ((int)dt < 0 || (int)dt > 2)
+        return recd_fail(ctx, RECD_EINVAL, "unknown dtype");
+    if (!(fabsf(scale) > 0.0f) || !(fabsf(scale) < INFINITY))
+        return recd_fail(ctx, RECD_EINVAL, "scale must be finite and not 0");
+    if (D <= 0 || D * elem_size(dt) % 16 != 0 || D > RECD_MAX_DENSE_D)
+        return recd_fail(ctx, RECD_EINVAL, "D=%d: row bytes must be a multiple of 16, and D at most %d", D, RECD_MAX_DENSE_D);
+    return RECD_OK;
+}
+
+recd_status validate_targets(recd_ctx *ctx, int64_t n, int64_t V, const int64_t *targets)
+{
+    ctx->plan.valid = false;
+    RECD_TRY(recd_reserve(ctx, 512));
+    int *err = reinterpret_cast<int *>(ctx->ws);
+    RECD_HIP(ctx, hipMemsetAsync(err, 0, sizeof(int), ctx->stream));
+    hipLaunchKernelGGL(k_validate_targets, dim3(64), dim3(256), 0, ctx->stream, n, V, targets, err);
+    RECD_HIP(ctx, hipGetLastError());
+    ctx->host_pinned[0] = 0;
+    RECD_HIP(ctx, hipMemcpyAsync(ctx->host_pinned, err, sizeof(int), hipMemcpyDeviceToHost, ctx->stream));
+    RECD_HIP(ctx, hipStreamSynchronize(ctx->stream));
+    if ((int)ctx->host_pinned[0])
+        return recd_fail(ctx, RECD_EBOUNDS, "a target is not a row of the table");
+    return RECD_OK;
+}
+
+// How a forward call is cut.
+struct ForwardShape {
+    bool share;
+    int row_blocks, splits;
+    int64_t tiles_per_split;
+    int parts;
+};
+
+ForwardShape forward_shape(const recd_ctx *ctx, int64_t n, int64_t V, int D, recd_dtype dt)
+{
+    const bool f32 = dt == RECD_F32;
+    const int per_wave = f32 || D > 128 ? 32 : 64;
+    ForwardShape s;
+    s.share = n <= 128;
+    const int vt = s.share ? 128 : (f32 && D > 128 ? 32 : 64);
+    const int64_t rows = s.share ? per_wave : per_wave * kWaves, tiles = (V + vt - 1) / vt;
+    s.row_blocks = (int)((n + rows - 1) / rows);
+    // two blocks a CU, in splits of at least two tiles
+    int64_t splits = (2 * ctx->num_cu + s.row_blocks - 1) / s.row_blocks;
+    if (splits > (tiles + 1) / 2)
+        splits = (tiles + 1) / 2;
+    if (splits < 1)
+        splits = 1;
+    s.tiles_per_split = (tiles + splits - 1) / splits;
+    s.splits = (int)((tiles + s.tiles_per_split - 1) / s.tiles_per_split);
+    s.parts = s.share ? s.splits * kWaves : s.splits;
+    return s;
+}
+
+template <typename T, int DP, int N> void launch_forward(const ForwardArgs &a, bool share, hipStream_t st)
+{
+    const dim3 grid((unsigned)((a.splits + 7) / 8 * 8 * a.row_blocks));
+    const bool mean = a.part_o != nullptr;
+    if (share && mean)
+        hipLaunchKernelGGL((k_vocab_forward<T, DP, N, true, true>), grid, dim3(kBlock), 0, st, a);
+    else if (share)
+        hipLaunchKernelGGL((k_vocab_forward<T, DP, N, true, false>), grid, dim3(kBlock), 0, st, a);
+    else if (mean)
+        hipLaunchKernelGGL((k_vocab_forward<T, DP, N, false, true>), grid, dim3(kBlock), 0, st, a);
+    else
+        hipLaunchKernelGGL((k_vocab_forward<T, DP, N, false, false>), grid, dim3(kBlock), 0, st, a);
+}
+
+template <typename T, int DP, int N> void launch_grad_table(const TableGradArgs &a, hipStream_t st)
+{
+    const int rows = 32 * N * kWaves;
+    hipLaunchKernelGGL((k_vocab_grad_table<T, DP, N>), dim3((unsigned)((a.V + rows - 1) / rows)), dim3(kBlock), 0, st, a);
+}
+
+} // namespace
+
+extern "C" {
+
+recd_status recd_vocab_loss(recd_ctx *ctx, int64_t n, int64_t V, int D, recd_dtype dt, const void *x, const void *table,
+                            const int64_t *targets, float scale, float *loss, float *lse, float *mean_row)
+{
+    RECD_TRY(check_vocab(ctx, n, V, D, dt, scale));
+    if (n == 0)
+        return RECD_OK;
+    if (V == 0)
+        return recd_fail(ctx, RECD_EINVAL, "a vocabulary without rows");
+    if (!x || !table || !targets || !loss || !lse)
+        return recd_fail(ctx, RECD_EINVAL, "null pointer argument");
+    if (((uintptr_t)x | (uintptr_t)table) % 16)
+        return recd_fail(ctx, RECD_EINVAL, "x and table must be aligned to 16 bytes");
+    RECD_HIP(ctx, hipSetDevice(ctx->device));
+    if (ctx->validate)
+        RECD_TRY(validate_targets(ctx, n, V, targets));
+    const ForwardShape s = forward_shape(ctx, n, V, D, dt);
+    WsCarver size(nullptr);
+    auto carve = [&](WsCarver &c, ForwardArgs &a) {
+        a.part_m = c.take<float>((size_t)s.parts * n);
+        a.part_l = c.take<float>((size_t)s.parts * n);
+        a.part_o = mean_row ? c.take<float>((size_t)s.parts * n * D) : nullptr;
+    };
+    ForwardArgs a{n, V, D, fabsf(scale) * kRecdLog2e, scale < 0, x, table, s.row_blocks, s.splits, s.tiles_per_split};
+    carve(size, a);
+    ctx->plan.valid = false;  // the parts overwrite the workspace a backward plan would live in
+    RECD_TRY(recd_reserve(ctx, size.off));
+    WsCarver c(ctx->ws);
+    carve(c, a);
+    recd_with_type(dt, [&](auto t) {
+        using T = decltype(t);
+        constexpr int N = sizeof(T) == 4 ? 1 : 2;
+        if (D <= 64)
+            launch_forward<T, 64, N>(a, s.share, ctx->stream);
+        else if (D <= 128)
+            launch_forward<T, 128, N>(a, s.share, ctx->stream);
+        else
+            launch_forward<T, 256, 1>(a, s.share, ctx->stream);
+        hipLaunchKernelGGL((k_vocab_join<T>), dim3((unsigned)((n + kWaves - 1) / kWaves)), dim3(kBlock), 0, ctx->stream, n, V,
+                           D, scale, s.parts, a.part_m, a.part_l, a.part_o, (const T *)x, (const T *)table, targets, loss,
+                           lse, mean_row);
+    });
+    RECD_HIP(ctx, hipGetLastError());
+    return RECD_OK;
+}
+
+recd_status recd_vocab_loss_backward(recd_ctx *ctx, int64_t n, int64_t V, int D, recd_dtype dt, const void *x,
+                                     const void *table, const int64_t *targets, float scale, const float *lse,
+                                     const float *mean_row, const float *grad_loss, void *grad_x, void *grad_table)
+{
+    RECD_TRY(check_vocab(ctx, n, V, D, dt, scale));
+    if (V == 0 && n > 0)
+        return recd_fail(ctx, RECD_EINVAL, "a vocabulary without rows");
+    if (!grad_x && !grad_table && n > 0)
+        return recd_fail(ctx, RECD_EINVAL, "neither grad_x nor grad_table");
+    if (n > 0 && (!x || !table || !targets || !lse || !grad_loss || (grad_x && !mean_row)))
+        return recd_fail(ctx, RECD_EINVAL, "null pointer argument");
+    if (((uintptr_t)x | (uintptr_t)table | (uintptr_t)grad_x | (uintptr_t)grad_table) % 16)
+        return recd_fail(ctx, RECD_EINVAL, "x, table and their gradients must be aligned to 16 bytes");
+    if (V == 0 || (n == 0 && !grad_table))
+        return RECD_OK;
+    RECD_HIP(ctx, hipSetDevice(ctx->device));
+    if (ctx->validate && n > 0)
+        RECD_TRY(validate_targets(ctx, n, V, targets));
+    const bool lifted = dt == RECD_F16 && grad_table && n > 0;
+    WsCarver size(nullptr);
+    float *row_lse, *row_g, *lift;
+    int32_t *row_t;
+    auto carve = [&](WsCarver &c) {
+        row_lse = grad_table ? c.take<float>(n) : nullptr;
+        row_g = grad_table ? c.take<float>(n) : nullptr;
+        row_t = grad_table ? c.take<int32_t>(n) : nullptr;
+        lift = lifted ? c.take<float>(1) : nullptr;
+    };
+    carve(size);
+    ctx->plan.valid = false;
+    RECD_TRY(recd_reserve(ctx, size.off));
+    WsCarver c(ctx->ws);
+    carve(c);
+    if (lifted)
+        hipLaunchKernelGGL(k_vocab_lift, dim3(1), dim3(1024), 0, ctx->stream, n, grad_loss, lift);
+    recd_with_type(dt, [&](auto t) {
+        using T = decltype(t);
+        if (n > 0)
+            hipLaunchKernelGGL((k_vocab_rows<T>), dim3((unsigned)((n + kWaves - 1) / kWaves)), dim3(kBlock), 0, ctx->stream, n,
+                               V, D, scale, (const T *)table, targets, lse, mean_row, grad_loss, lift, row_lse, row_g, row_t,
+                               (T *)grad_x);
+        if (!grad_table)
+            return;
+        TableGradArgs a{n, V, D, fabsf(scale) * kRecdLog2e, scale, scale < 0, x, table, row_lse, row_g, lift, row_t, grad_table};
+        constexpr int N = sizeof(T) == 4 ? 1 : 2;
+        if (D <= 64)
+            launch_grad_table<T, 64, N>(a, ctx->stream);
+        else if (D <= 128)
+            launch_grad_table<T, 128, N>(a, ctx->stream);
+        else
+            launch_grad_table<T, 256, 1>(a, ctx->stream);
+    });
+    RECD_HIP(ctx, hipGetLastError());
+    return RECD_OK;
+}
+
+} // extern "C"

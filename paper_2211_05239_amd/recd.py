@@ -52,8 +52,19 @@ EXPORTED = [
     "recd_kjt_pooled_lookup_weighted", "recd_backward_dedup_weighted", "recd_backward_dedup_max",
     "recd_last_ikjt_counts", "recd_backward_plan", "recd_backward_apply", "recd_build_ikjt_noalloc",
     "recd_build_ikjt_runs", "recd_ikjt_run_index", "recd_pooled_lookup_expand", "recd_last_ikjt_run_count",
-    "recd_backward_plan_runs",
+    "recd_backward_plan_runs", "recd_layer_norm", "recd_layer_norm_backward", "recd_vocab_loss",
+    "recd_vocab_loss_backward", "recd_list_attention", "recd_list_attention_backward",
 ]
+
+
+class _Attention(C.Structure):
+    """recd_attention of the header."""
+    _fields_ = [("heads", C.c_int), ("kv_heads", C.c_int), ("head_dim", C.c_int), ("dtype", C.c_int),
+                ("lists", C.c_int64), ("max_q", C.c_int64), ("max_k", C.c_int64), ("q_rows", C.c_int64),
+                ("k_rows", C.c_int64), ("q_offsets", C.c_void_p), ("k_offsets", C.c_void_p),
+                ("q_stride", C.c_int64), ("k_stride", C.c_int64), ("v_stride", C.c_int64), ("scale", C.c_float),
+                ("softcap", C.c_float), ("slopes", C.c_void_p), ("prefix", C.c_void_p), ("causal", C.c_int)]
+
 
 _vp = C.c_void_p
 _lib.recd_create.argtypes = [C.POINTER(_vp), C.c_int, _vp, C.c_size_t]
@@ -114,6 +125,12 @@ _lib.recd_pooled_lookup_partial.argtypes = [_vp, C.c_int, C.c_int, C.c_int, C.c_
 _lib.recd_backward_sequence_dedup.argtypes = [_vp, C.c_int, C.c_int64, C.c_int64, C.c_int, _vp, _vp, _vp, _vp, _vp,
                                               _vp, _vp, C.c_int64, C.c_int64, _vp, _vp, _vp, _vp, _vp, _vp,
                                               C.c_float, C.c_float, _vp]
+_lib.recd_layer_norm.argtypes = [_vp, C.c_int64, C.c_int, C.c_int, _vp, _vp, _vp, C.c_float, _vp, _vp]
+_lib.recd_layer_norm_backward.argtypes = [_vp, C.c_int64, C.c_int, C.c_int] + [_vp] * 7
+_lib.recd_vocab_loss.argtypes = [_vp, C.c_int64, C.c_int64, C.c_int, C.c_int, _vp, _vp, _vp, C.c_float, _vp, _vp, _vp]
+_lib.recd_vocab_loss_backward.argtypes = [_vp, C.c_int64, C.c_int64, C.c_int, C.c_int, _vp, _vp, _vp, C.c_float] + [_vp] * 5
+_lib.recd_list_attention.argtypes = [_vp, C.POINTER(_Attention)] + [_vp] * 5
+_lib.recd_list_attention_backward.argtypes = [_vp, C.POINTER(_Attention)] + [_vp] * 9 + [C.c_int64] * 3
 _lib.recd_internal_kernel_ms.argtypes = [_vp, C.c_int, C.c_int, C.POINTER(C.c_double), C.POINTER(C.c_double),
                                          C.POINTER(C.c_int)]
 _lib.recd_internal_kernel_ms.restype = C.c_int
@@ -135,6 +152,18 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
         return None
     assert t.is_cuda and t.is_contiguous()
     return t.data_ptr()
+
+
+def _param(t: Optional[torch.Tensor], n: int) -> Optional[int]:
+    assert t is None or (t.dtype == torch.float32 and t.numel() == n)
+    return _ptr(t)
+
+
+def _rows_ptr(t: torch.Tensor):
+    """(address, elements from row to row) of rows [n, heads, head_dim] that lie densely inside a row."""
+    assert t.is_cuda and t.dim() == 3
+    assert t.stride(2) == 1 and (t.stride(1) == t.shape[2] or t.shape[1] == 1)
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
 
 
 def workspace_bytes(F: int, B: int, N: int, D: int) -> int:
@@ -452,3 +481,72 @@ class Context:
             _ptr(u_values), _ptr(u_offsets), rows_arr, U_cap, M_cap, _ptr(grad_emb), _ptr(touched_rows),
             _ptr(feat_roff), _ptr(grad_rows), tabs, state, lr, eps, host))
         return int(host[0]) if want_count else None
+
+    # -- dense operators on the rows of lists ---------------------------------------------------
+    def layer_norm(self, x, weight, bias, eps: float, y, stats=None):
+        """y = layer norm of the rows of x [n, D]; stats (float32 [n, 2]: mean, 1 / deviation) for the backward."""
+        n, D = x.shape
+        assert y.shape == x.shape and y.dtype == x.dtype and (stats is None or stats.numel() >= 2 * n)
+        self._check(_lib.recd_layer_norm(self._h, n, D, _DT[x.dtype], _ptr(x), _param(weight, D), _param(bias, D), eps,
+                                         _ptr(y), _ptr(stats)))
+
+    def layer_norm_backward(self, x, weight, stats, grad_y, grad_x, grad_weight=None, grad_bias=None):
+        n, D = x.shape
+        assert grad_y.shape == x.shape == grad_x.shape and grad_y.dtype == x.dtype == grad_x.dtype
+        assert stats.numel() >= 2 * n and stats.dtype == torch.float32
+        self._check(_lib.recd_layer_norm_backward(self._h, n, D, _DT[x.dtype], _ptr(x), _param(weight, D), _ptr(stats),
+                                                  _ptr(grad_y), _ptr(grad_x), _param(grad_weight, D), _param(grad_bias, D)))
+
+    def vocab_loss(self, x, table, targets, scale: float, loss, lse, mean_row=None):
+        """Softmax cross entropy of the rows x [n, D] against all rows of table [V, D]; mean_row (float32 [n, D]) for the
+        backward."""
+        n, D = x.shape
+        assert table.shape[1] == D and table.dtype == x.dtype and targets.dtype == torch.int64
+        assert targets.numel() == n and loss.numel() == n and lse.numel() == n and loss.dtype == lse.dtype == torch.float32
+        assert mean_row is None or (mean_row.numel() == n * D and mean_row.dtype == torch.float32)
+        self._check(_lib.recd_vocab_loss(self._h, n, table.shape[0], D, _DT[x.dtype], _ptr(x), _ptr(table), _ptr(targets),
+                                         scale, _ptr(loss), _ptr(lse), _ptr(mean_row)))
+
+    def vocab_loss_backward(self, x, table, targets, scale: float, lse, mean_row, grad_loss, grad_x, grad_table):
+        n, D = x.shape
+        assert table.shape[1] == D and table.dtype == x.dtype and targets.dtype == torch.int64 and targets.numel() == n
+        assert lse.numel() == n and grad_loss.numel() == n and lse.dtype == grad_loss.dtype == torch.float32
+        assert mean_row is None or (mean_row.numel() == n * D and mean_row.dtype == torch.float32)
+        assert grad_x is None or (grad_x.shape == x.shape and grad_x.dtype == x.dtype)
+        assert grad_table is None or (grad_table.shape == table.shape and grad_table.dtype == x.dtype)
+        self._check(_lib.recd_vocab_loss_backward(self._h, n, table.shape[0], D, _DT[x.dtype], _ptr(x), _ptr(table),
+                                                  _ptr(targets), scale, _ptr(lse), _ptr(mean_row), _ptr(grad_loss),
+                                                  _ptr(grad_x), _ptr(grad_table)))
+
+    @staticmethod
+    def _attention(q, k, v, q_offsets, k_offsets, max_q, max_k, scale, softcap, slopes, causal, prefix):
+        H, d = q.shape[1:]
+        assert k.shape == v.shape and k.shape[2] == d and q.dtype == k.dtype == v.dtype
+        assert q_offsets.dtype == k_offsets.dtype == torch.int64 and q_offsets.numel() == k_offsets.numel()
+        lists = q_offsets.numel() - 1
+        assert slopes is None or (slopes.numel() == H and slopes.dtype == torch.float32)
+        assert prefix is None or (prefix.numel() >= lists and prefix.dtype == torch.int32)
+        (pq, sq), (pk, sk), (pv, sv) = _rows_ptr(q), _rows_ptr(k), _rows_ptr(v)
+        return _Attention(H, k.shape[1], d, _DT[q.dtype], lists, max_q, max_k, q.shape[0], k.shape[0], _ptr(q_offsets),
+                          _ptr(k_offsets), sq, sk, sv, scale, softcap, _ptr(slopes), _ptr(prefix), int(causal)), pq, pk, pv
+
+    def list_attention(self, q, k, v, q_offsets, k_offsets, max_q: int, max_k: int, out, lse=None, *, scale: float,
+                       softcap: float = 0.0, slopes=None, causal: bool = False, prefix=None):
+        """Attention inside every list: q [Q, H, d], k and v [K, G, d] (rows may be strided), out [Q, H, d]; lse (float32
+        [Q, H]) for the backward."""
+        a, pq, pk, pv = self._attention(q, k, v, q_offsets, k_offsets, max_q, max_k, scale, softcap, slopes, causal, prefix)
+        assert out.shape == q.shape and out.dtype == q.dtype
+        assert lse is None or (lse.numel() == q.shape[0] * q.shape[1] and lse.dtype == torch.float32)
+        self._check(_lib.recd_list_attention(self._h, C.byref(a), pq, pk, pv, _ptr(out), _ptr(lse)))
+
+    def list_attention_backward(self, q, k, v, q_offsets, k_offsets, max_q: int, max_k: int, out, lse, grad_out, grad_q,
+                                grad_k, grad_v, *, scale: float, softcap: float = 0.0, slopes=None, causal: bool = False,
+                                prefix=None):
+        """Gradients of list_attention; grad_q, grad_k and grad_v may be strided as q, k and v may."""
+        a, pq, pk, pv = self._attention(q, k, v, q_offsets, k_offsets, max_q, max_k, scale, softcap, slopes, causal, prefix)
+        assert out.shape == q.shape == grad_out.shape == grad_q.shape and grad_k.shape == k.shape == grad_v.shape
+        assert out.dtype == q.dtype == grad_out.dtype == grad_q.dtype == grad_k.dtype == grad_v.dtype
+        assert lse.numel() == q.shape[0] * q.shape[1] and lse.dtype == torch.float32
+        (gq, sq), (gk, sk), (gv, sv) = _rows_ptr(grad_q), _rows_ptr(grad_k), _rows_ptr(grad_v)
+        self._check(_lib.recd_list_attention_backward(self._h, C.byref(a), pq, pk, pv, _ptr(out), _ptr(lse), _ptr(grad_out),
+                                                      gq, gk, gv, sq, sk, sv))
