@@ -1,0 +1,327 @@
+"""Attention inside lists, its gradients, and what the calls refuse, against 64 bits."""
+import pytest
+import torch
+
+from tests import dense_util as du
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    from paper_2211_05239_amd import recd
+    c = recd.Context(0)
+    yield c
+    c.close()
+
+
+def offsets(lens):
+    return torch.cat([torch.zeros(1, dtype=torch.int64), torch.tensor(lens, dtype=torch.int64).cumsum(0)])
+
+
+def run(ctx, q, k, v, qo, ko, how, g=None, max_q=None, max_k=None):
+    dev = lambda t: t.cuda() if isinstance(t, torch.Tensor) else t  # noqa: E731
+    q, k, v, g, qo, ko = (dev(t) for t in (q, k, v, g, qo, ko))
+    how = {n: dev(x) for n, x in how.items()}
+    max_q = int(qo.diff().max()) if max_q is None else max_q
+    max_k = int(ko.diff().max()) if max_k is None else max_k
+    nan = float("nan")
+    got = {"out": torch.full(q.shape, nan, dtype=q.dtype, device="cuda"), "lse": torch.full(q.shape[:2], nan, device="cuda")}
+    ctx.list_attention(q, k, v, qo, ko, max_q, max_k, got["out"], got["lse"], **how)
+    plain = torch.full(q.shape, nan, dtype=q.dtype, device="cuda")
+    ctx.list_attention(q, k, v, qo, ko, max_q, max_k, plain, **how)
+    assert du.same_bits(plain, got["out"])
+    if g is not None:
+        for n, t in (("grad_q", q), ("grad_k", k), ("grad_v", v)):
+            got[n] = torch.full(t.shape, nan, dtype=q.dtype, device="cuda")
+        ctx.list_attention_backward(q, k, v, qo, ko, max_q, max_k, got["out"], got["lse"], g, got["grad_q"], got["grad_k"],
+                                    got["grad_v"], **how)
+    torch.cuda.synchronize()
+    return got
+
+
+def check(ctx, lq, lk, H, G, d, dt, how, seed=1, train=True, std=1.0, **kw):
+    qo, ko = offsets(lq), offsets(lk)
+    Q, K = int(qo[-1]), int(ko[-1])
+    q, k, v = du.rand((Q, H, d), dt, seed, std), du.rand((K, G, d), dt, seed + 1, std), du.rand((K, G, d), dt, seed + 2)
+    g = du.rand((Q, H, d), dt, seed + 3) if train else None
+    how = dict(dict(scale=d ** -0.5), **how)
+    ref = du.attention_ref(q, k, v, qo, ko, g=g, **how)
+    got = run(ctx, q, k, v, qo, ko, how, g, **kw)
+    for n, t in got.items():
+        if n == "lse":
+            none = ref[n][0] == -float("inf")
+            assert torch.equal(t.cpu() == -float("inf"), none)
+            du.within(t.cpu()[~none], ref[n][0][~none], ref[n][1][~none], what=n)
+        else:
+            du.within(t, *ref[n], what=n)
+    return got
+
+
+SLOPES = lambda H: 2.0 ** (-8.0 * torch.arange(1, H + 1) / H)  # noqa: E731
+
+
+# lengths: none, one, edges of tiles of 32, 64 and 128 rows, several tiles
+LENGTHS = {"small": [0, 1, 2, 31, 0, 32, 33, 5], "mid": [63, 1, 64, 65, 100], "long": [129, 300, 0, 7, 128], "one": [1],
+           "none": [0, 0, 3, 0]}
+
+
+@pytest.mark.parametrize("dt", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("lens", list(LENGTHS))
+@pytest.mark.parametrize("d", [16, 64, 128])
+@pytest.mark.parametrize("causal", [False, True])
+def test_lengths(ctx, dt, lens, d, causal):
+    check(ctx, LENGTHS[lens], LENGTHS[lens], 2, 2, d, dt, dict(causal=causal))
+
+
+@pytest.mark.parametrize("dt", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("what", ["cap", "slopes", "prefix", "all", "all_not_causal"])
+def test_caps_biases_and_prefixes(ctx, dt, what):
+    lens = [70, 3, 0, 33, 150]
+    prefix = torch.tensor([40, 0, 5, 200, 1], dtype=torch.int32)   # one longer than its list
+    how = {"cap": dict(softcap=3.0, causal=True), "slopes": dict(slopes=SLOPES(4), causal=True),
+           "prefix": dict(causal=True, prefix=prefix),
+           "all": dict(softcap=3.0, slopes=SLOPES(4), causal=True, prefix=prefix),
+           "all_not_causal": dict(softcap=3.0, slopes=SLOPES(4))}[what]
+    check(ctx, lens, lens, 4, 2, 40, dt, how, std=2.0)
+
+
+@pytest.mark.parametrize("dt", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("H,G", [(1, 1), (6, 3), (8, 1), (5, 1), (12, 4)])
+def test_shared_heads(ctx, dt, H, G):
+    check(ctx, [20, 47, 1, 90], [20, 47, 1, 90], H, G, 24, dt, dict(causal=True, slopes=SLOPES(H)))
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("causal", [False, True])
+def test_queries_and_keys_of_different_lengths(ctx, dt, causal):
+    """More queries than keys leave the first ones of a causal list without any key; so do lists without keys."""
+    lq, lk = [10, 50, 3, 0, 7, 200, 1, 40], [30, 20, 0, 9, 7, 65, 300, 39]
+    prefix = torch.tensor([0, 0, 2, 1, 0, 3, 0, 100], dtype=torch.int32) if causal else None
+    got = check(ctx, lq, lk, 4, 2, 32, dt, dict(causal=causal, prefix=prefix))
+    if causal:
+        assert not got["out"][10:40].any() and not got["grad_q"][10:40].any()   # 30 queries before the first key
+        assert not got["out"][60:63].any()                                      # no keys at all
+
+
+# keys are split over blocks where there are few tiles
+@pytest.mark.parametrize("dt", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("lk,H,G", [([700, 1, 0, 2100], 8, 2), ([5000], 1, 1), ([257, 512], 3, 3), ([4097], 20, 1)])
+def test_one_query_per_list(ctx, dt, lk, H, G):
+    check(ctx, [1] * len(lk), lk, H, G, 64, dt, dict(causal=True, softcap=5.0), train=False)
+    check(ctx, [1] * len(lk), lk, H, G, 128, dt, dict(slopes=SLOPES(H)), train=False)
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_splits_with_several_queries(ctx, dt):
+    """Few tiles of longer queries: splits that lie behind a row's last key leave it alone."""
+    check(ctx, [600, 40], [1300, 900], 2, 1, 32, dt, dict(causal=True), train=False)
+    check(ctx, [900], [900], 1, 1, 16, dt, dict(causal=True, prefix=torch.tensor([300], dtype=torch.int32)), train=False)
+
+
+def test_bounds_may_be_larger_than_the_lists(ctx):
+    lens = [5, 60, 0, 33]
+    a = check(ctx, lens, lens, 2, 2, 32, "bf16", dict(causal=True))
+    b = check(ctx, lens, lens, 2, 2, 32, "bf16", dict(causal=True), max_q=5000, max_k=60_000)
+    for n in ("out", "grad_q", "grad_k", "grad_v"):
+        assert (a[n].float() - b[n].float()).norm() <= 0.02 * a[n].float().norm()
+
+
+@pytest.mark.parametrize("dt", ["f32", "f16", "bf16"])
+def test_rows_apart_by_strides(ctx, dt):
+    """Queries, keys and values in one array, gradients in another, and rows that are not neighbours."""
+    lens, H, G, d = [33, 2, 100], 4, 2, 32
+    o = offsets(lens)
+    K = int(o[-1])
+    both = du.rand((K, H + 2 * G, d), dt, 5).cuda()
+    q, k, v = both[:, :H], both[:, H:H + G], both[:, H + G:]
+    g = du.rand((K, H, d), dt, 6).cuda()
+    how = dict(scale=0.2, causal=True)
+    want = run(ctx, q.contiguous(), k.contiguous(), v.contiguous(), o, o, how, g)
+    gb = torch.full((K, H + 2 * G, d), float("nan"), dtype=both.dtype, device="cuda")
+    wide = torch.full((K, 3, H, d), 7.0, dtype=both.dtype, device="cuda")
+    wide[:, 1] = q
+    out, lse = torch.empty_like(want["out"]), torch.empty_like(want["lse"])
+    oc = o.cuda()
+    ctx.list_attention(wide[:, 1], k, v, oc, oc, 100, 100, out, lse, **how)
+    ctx.list_attention_backward(wide[:, 1], k, v, oc, oc, 100, 100, out, lse, g, gb[:, :H], gb[:, H:H + G], gb[:, H + G:], **how)
+    for got, n in ((out, "out"), (gb[:, :H], "grad_q"), (gb[:, H:H + G], "grad_k"), (gb[:, H + G:], "grad_v")):
+        assert torch.equal(got, want[n]), n
+
+
+@pytest.mark.parametrize("power", [-18, 6])
+def test_fp16_gradients_of_any_size(ctx, power):
+    """Gradients of the output that are far from 1 neither vanish nor overflow inside."""
+    o = offsets([90, 40])
+    q, k, v = (du.rand((130, 2, 64), "f16", s) for s in (1, 2, 3))
+    g = (du.rand((130, 2, 64), "f16", 4).double() * 2.0 ** power).half()
+    how = dict(scale=0.125, causal=True)
+    ref = du.attention_ref(q, k, v, o, o, g=g, **how)
+    got = run(ctx, q, k, v, o, o, how, g)
+    for n in ("grad_q", "grad_k", "grad_v"):
+        du.within(got[n], *ref[n], what=n)
+
+
+def test_large_scores(ctx):
+    """Scores of hundreds that rise along the keys move the running maximum at every tile."""
+    o = offsets([300])
+    q, k, v = (du.rand((300, 1, 32), "f32", s) for s in (1, 2, 3))
+    q, k = q.abs(), k.abs() * torch.linspace(0.1, 40, 300)[:, None, None]
+    how = dict(scale=0.5)
+    ref = du.attention_ref(q, k, v, o, o, **how)
+    got = run(ctx, q, k, v, o, o, how)
+    du.within(got["out"], *ref["out"], what="out")
+    du.within(got["lse"], *ref["lse"], what="lse")
+
+
+def test_lists_do_not_touch_each_other(ctx):
+    """A list of NaN and infinities leaves the lists around it as they are, forward and backward."""
+    lens = [40, 17, 66]
+    o = offsets(lens)
+    q, k, v, g = (du.rand((123, 2, 32), "bf16", s) for s in (1, 2, 3, 4))
+    how = dict(scale=0.3, causal=True)
+    want = run(ctx, q, k, v, o, o, how, g)
+    for t in (q, k, v, g):
+        t[40:57] = float("nan")
+        t[45] = float("inf")
+    got = run(ctx, q, k, v, o, o, how, g)
+    rows = torch.ones(123, dtype=torch.bool)
+    rows[40:57] = False
+    rows = rows.cuda()
+    for n in want:
+        assert torch.equal(got[n][rows], want[n][rows]), n
+
+
+def test_same_bits_again(ctx):
+    lens = [300, 5, 0, 77, 129]
+    a = check(ctx, lens, lens, 4, 2, 64, "bf16", dict(causal=True, softcap=4.0))
+    b = check(ctx, lens, lens, 4, 2, 64, "bf16", dict(causal=True, softcap=4.0))
+    for n in a:
+        assert torch.equal(a[n], b[n]), n
+
+
+def test_gradients_against_differences(ctx):
+    """Central differences of sum(g * out) in fp32: off by the outputs' rounding over the step and its square."""
+    lq, lk = [3, 2], [4, 3]
+    qo, ko = offsets(lq), offsets(lk)
+    q, k, v, g = (du.rand(s, "f32", i) for i, s in enumerate(((5, 2, 4), (7, 1, 4), (7, 1, 4), (5, 2, 4))))
+    how = dict(scale=0.6, softcap=2.0, slopes=SLOPES(2), causal=True, prefix=torch.tensor([1, 0], dtype=torch.int32))
+    got = run(ctx, q, k, v, qo, ko, how, g)
+    h = 2.0 ** -7
+
+    def value():
+        return float((run(ctx, q, k, v, qo, ko, how)["out"].double().cpu() * g.double()).sum())
+
+    for name, t in (("grad_q", q), ("grad_k", k), ("grad_v", v)):
+        flat = t.view(-1)
+        for i in range(flat.numel()):
+            old = float(flat[i])
+            flat[i] = old + h
+            up = value()
+            flat[i] = old - h
+            down = value()
+            flat[i] = old
+            assert abs((up - down) / (2 * h) - float(got[name].view(-1)[i])) < 2e-3, (name, i)
+
+
+def test_a_cache_beyond_2_to_31_elements(ctx):
+    """Keys and values whose positions pass 32 bits: rows 16 K elements apart, the second list behind 2^31."""
+    rows, wide, d = 150_000, 16_384, 64
+    cache = torch.empty(rows, wide // d, d, dtype=torch.float16, device="cuda")
+    k, v = cache[:, :2], cache[:, -2:]
+    n = [rows - 700, 700]
+    o = offsets(n)
+    kc, vc = du.rand((rows, 2, d), "f16", 1, 0.5), du.rand((rows, 2, d), "f16", 2)
+    k.copy_(kc.cuda())
+    v.copy_(vc.cuda())
+    q = du.rand((2, 4, d), "f16", 3)
+    qo = offsets([1, 1])
+    how = dict(scale=0.125, causal=True)
+    ref = du.attention_ref(q, kc, vc, qo, o, **how)
+    out = torch.empty(2, 4, d, dtype=torch.float16, device="cuda")
+    ctx.list_attention(q.cuda(), k, v, qo.cuda(), o.cuda(), 1, rows, out, **how)
+    du.within(out, *ref["out"], what="out")
+
+
+def test_another_stream_and_a_graph(ctx):
+    from paper_2211_05239_amd import recd
+    lens = [90, 3, 0, 200]
+    o = offsets(lens).cuda()
+    q, k, v, g = (du.rand((293, 2, 32), "f16", s).cuda() for s in (1, 2, 3, 4))
+    how = dict(scale=0.3, causal=True)
+    want = run(ctx, q, k, v, o, o, how, g)
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        c = recd.Context(0)
+        got = {n: torch.zeros_like(t) for n, t in want.items()}
+
+        def step():
+            c.list_attention(q, k, v, o, o, 200, 200, got["out"], got["lse"], **how)
+            c.list_attention_backward(q, k, v, o, o, 200, 200, got["out"], got["lse"], g, got["grad_q"], got["grad_k"],
+                                      got["grad_v"], **how)
+
+        step()
+        s.synchronize()
+        for n in want:
+            assert torch.equal(got[n], want[n]), n
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            step()
+        for i in range(4):
+            for t in got.values():
+                t.fill_(float("nan"))
+            graph.replay()
+            s.synchronize()
+            for n in want:
+                assert torch.equal(got[n], want[n]), (i, n)
+            run(c, q, k, v, o, o, how, g)
+        c.close()
+
+
+def test_validation(ctx):
+    from paper_2211_05239_amd import recd
+    q = du.rand((10, 1, 16), "f32", 1)
+    ctx.set_option(recd.RECD_OPT_VALIDATE, 1)
+    try:
+        run(ctx, q, q, q, offsets([4, 6]), offsets([4, 6]), dict(scale=1.0), q)
+        for bad, most in ((torch.tensor([0, 11, 10]), 11), (torch.tensor([1, 4, 10]), 10), (torch.tensor([0, 4, 9]), 10),
+                          (offsets([4, 6]), 5)):
+            with pytest.raises(recd.RecdError) as e:
+                run(ctx, q, q, q, bad, bad, dict(scale=1.0), q, max_q=most, max_k=most)
+            assert e.value.status == recd.RECD_EBOUNDS
+    finally:
+        ctx.set_option(recd.RECD_OPT_VALIDATE, 0)
+
+
+def test_refusals(ctx):
+    import ctypes as C
+
+    from paper_2211_05239_amd import recd
+    lib, h = recd._lib, ctx._h
+    buf = torch.zeros(4096, device="cuda")
+    p = buf.data_ptr()
+    good = dict(heads=2, kv_heads=2, head_dim=16, dtype=0, lists=1, max_q=4, max_k=4, q_rows=4, k_rows=4, q_offsets=p,
+                k_offsets=p, q_stride=32, k_stride=32, v_stride=32, scale=1.0, softcap=0.0, slopes=None, prefix=None, causal=1)
+
+    def forward(ctx_=h, q=p, k=p, v=p, out=p, **kw):
+        a = recd._Attention(**dict(good, **kw))
+        return lib.recd_list_attention(ctx_, C.byref(a), q, k, v, out, None)
+
+    def backward(out=p, lse=p, g=p, gq=p, gk=p, gv=p, s=(32, 32, 32), **kw):
+        a = recd._Attention(**dict(good, **kw))
+        return lib.recd_list_attention_backward(h, C.byref(a), p, p, p, out, lse, g, gq, gk, gv, *s)
+
+    bad = recd.RECD_EINVAL
+    for kw in (dict(ctx_=None), dict(heads=0), dict(heads=3), dict(kv_heads=0), dict(head_dim=0), dict(head_dim=6),
+               dict(head_dim=132, q_stride=1000, k_stride=1000, v_stride=1000), dict(head_dim=12, dtype=1), dict(dtype=3),
+               dict(lists=-1), dict(max_q=-1), dict(max_k=-1), dict(q_rows=-1), dict(k_rows=-1), dict(lists=0),
+               dict(q_offsets=None), dict(k_offsets=None), dict(q_stride=28), dict(k_stride=16), dict(v_stride=31),
+               dict(q_stride=34), dict(softcap=-1.0), dict(softcap=float("nan")), dict(softcap=float("inf")),
+               dict(prefix=p, causal=0), dict(q=None), dict(k=None), dict(v=None), dict(out=None), dict(q=p + 4),
+               dict(out=p + 4), dict(max_q=1 << 31), dict(lists=1 << 31)):
+        assert forward(**kw) == bad, kw
+    for kw in (dict(out=None), dict(lse=None), dict(g=None), dict(gq=None), dict(gk=None), dict(gv=None), dict(gk=p + 8),
+               dict(s=(28, 32, 32)), dict(s=(32, 16, 32)), dict(s=(32, 32, 33)), dict(head_dim=6)):
+        assert backward(**kw) == bad, kw
+    assert lib.recd_list_attention(h, None, p, p, p, p, None) == bad
+    assert forward(lists=0, q_rows=0, k_rows=0, q_offsets=None, k_offsets=None, q=None, k=None, v=None, out=None) == recd.RECD_OK

@@ -1,0 +1,261 @@
+"""Softmax cross entropy against a table, its gradients, and what the calls refuse, against 64 bits."""
+import pytest
+import torch
+
+from tests import dense_util as du
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    from paper_2211_05239_amd import recd
+    c = recd.Context(0)
+    yield c
+    c.close()
+
+
+def data(n, V, D, dt, seed, std=1.5, ignored=True):
+    x, table = du.rand((n, D), dt, seed), du.rand((V, D), dt, seed + 1, std / D ** 0.5)
+    g = torch.Generator().manual_seed(seed + 2)
+    t = torch.randint(0, V, (n,), generator=g)
+    if ignored:
+        t[::5] = -1
+    t[1::7] = V - 1
+    return x, table, t, du.rand((n,), "f32", seed + 3, 0.5, 1.0)
+
+
+def run(ctx, x, table, t, scale, gl, device=True):
+    x, table, t, gl = (a.cuda() for a in (x, table, t, gl)) if device else (x, table, t, gl)
+    n, D = x.shape
+    nan = float("nan")
+    got = {"loss": torch.full((n,), nan, device="cuda"), "lse": torch.full((n,), nan, device="cuda"),
+           "grad_x": torch.full_like(x, nan), "grad_table": torch.full_like(table, nan)}
+    mean = torch.full((n, D), nan, device="cuda")
+    ctx.vocab_loss(x, table, t, scale, got["loss"], got["lse"], mean)
+    loss, lse = torch.full((n,), nan, device="cuda"), torch.full((n,), nan, device="cuda")
+    ctx.vocab_loss(x, table, t, scale, loss, lse)
+    ctx.vocab_loss_backward(x, table, t, scale, got["lse"], mean, gl, got["grad_x"], got["grad_table"])
+    torch.cuda.synchronize()
+    return got, {"loss": loss, "lse": lse}
+
+
+def check(ctx, x, table, t, scale, gl):
+    ref = du.loss_ref(x, table, t, scale, gl)
+    got, without = run(ctx, x, table, t, scale, gl)
+    for k, v in got.items():
+        du.within(v, *ref[k], what=k)
+    for k, v in without.items():
+        du.within(v, *ref[k], what=k + " without the gradient")
+    return got
+
+
+# rows: one, a tile's edges, few (waves share them) and many; vocabularies: one row, a tile's edges, several splits
+@pytest.mark.parametrize("dt", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("n,V,D", [(1, 1, 16), (1, 31, 64), (33, 32, 24), (5, 33, 128), (64, 129, 40), (65, 1000, 96),
+                                   (128, 257, 128), (129, 999, 72), (300, 4097, 64), (257, 130, 200), (40, 3001, 256),
+                                   (700, 640, 256)])
+def test_sizes(ctx, dt, n, V, D):
+    check(ctx, *data(n, V, D, dt, n + V)[:3], 1.0, data(n, V, D, dt, n + V)[3])
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("scale", [-0.7, 0.05, 20.0])
+def test_scales(ctx, dt, scale):
+    """A negative scale turns the maximum round; a large one makes single probabilities near 1."""
+    x, table, t, gl = data(150, 500, 64, dt, 9)
+    check(ctx, x, table, t, scale, gl)
+
+
+@pytest.mark.parametrize("dt", ["f16", "bf16"])
+def test_many_rows_share_a_target(ctx, dt):
+    """One table row is almost every row's target: what is left of the sum beside the targets' weights has to be right."""
+    x, table, t, gl = data(600, 300, 64, dt, 3, ignored=False)
+    t[:550] = 17
+    check(ctx, x, table, t, 1.0, gl)
+
+
+@pytest.mark.parametrize("power", [-30, 10])
+def test_fp16_weights_of_any_size(ctx, power):
+    """Small and large weights of the loss neither vanish nor overflow inside; the result's own range decides."""
+    x, table, t, gl = data(90, 400, 64, "f16", 4)
+    gl = gl * 2.0 ** power
+    ref = du.loss_ref(x, table, t, 1.0, gl)
+    got, _ = run(ctx, x, table, t, 1.0, gl)
+    for k in ("grad_x", "grad_table"):
+        du.within(got[k], *ref[k], what=k)
+
+
+def test_rows_without_any_target(ctx):
+    x, table, t, gl = data(70, 200, 64, "bf16", 5)
+    t[:] = -100
+    got = check(ctx, x, table, t, 1.0, gl)
+    assert not got["loss"].any() and not got["grad_x"].any() and not got["grad_table"].any()
+
+
+def test_a_target_beyond_the_table(ctx):
+    from paper_2211_05239_amd import recd
+    x, table, t, gl = data(20, 50, 32, "f32", 6)
+    t[3] = 50
+    got = check(ctx, x, table, t, 1.0, gl)
+    assert got["loss"][3] == 0 and not got["grad_x"][3].any()
+    ctx.set_option(recd.RECD_OPT_VALIDATE, 1)
+    try:
+        with pytest.raises(recd.RecdError, match="target") as e:
+            run(ctx, x, table, t, 1.0, gl)
+        assert e.value.status == recd.RECD_EBOUNDS
+        t[3] = 49
+        run(ctx, x, table, t, 1.0, gl)
+    finally:
+        ctx.set_option(recd.RECD_OPT_VALIDATE, 0)
+
+
+def test_large_logits_do_not_overflow(ctx):
+    """Logits of several thousands, rising along the vocabulary, so that the running maximum moves again and again."""
+    x, table, _, gl = data(130, 700, 64, "f32", 8)
+    x, table = x.abs() * 20, table.abs() * torch.linspace(0, 40, 700)[:, None]
+    t = torch.arange(130) * 5 % 700
+    check(ctx, x.contiguous(), table.contiguous(), t, 1.0, gl)
+
+
+def test_a_row_that_is_not_finite_stays_by_itself(ctx):
+    x, table, t, gl = data(200, 300, 64, "f32", 8)
+    x[7, 2] = float("nan")
+    t[7] = -1
+    got, _ = run(ctx, x, table, t, 1.0, gl)
+    others = torch.arange(200, device="cuda") != 7
+    assert got["lse"][7].isnan() and got["lse"][others].isfinite().all() and got["grad_x"][others].isfinite().all()
+
+
+def test_same_bits_again(ctx):
+    x, table, t, gl = data(500, 5000, 128, "bf16", 11)
+    a, _ = run(ctx, x, table, t, 1.0, gl)
+    b, _ = run(ctx, x, table, t, 1.0, gl)
+    for k in a:
+        assert torch.equal(a[k], b[k]), k
+
+
+def test_only_one_gradient(ctx):
+    x, table, t, gl = (a.cuda() for a in data(140, 900, 64, "f16", 12))
+    want, _ = run(ctx, x, table, t, 1.0, gl, device=False)
+    mean = torch.empty(140, 64, device="cuda")
+    loss, lse = torch.empty(140, device="cuda"), torch.empty(140, device="cuda")
+    ctx.vocab_loss(x, table, t, 1.0, loss, lse, mean)
+    gx, gt = torch.empty_like(x), torch.empty_like(table)
+    ctx.vocab_loss_backward(x, table, t, 1.0, lse, mean, gl, gx, None)
+    ctx.vocab_loss_backward(x, table, t, 1.0, lse, None, gl, None, gt)
+    assert torch.equal(gx, want["grad_x"]) and torch.equal(gt, want["grad_table"])
+
+
+def test_no_rows(ctx):
+    table = du.rand((40, 64), "bf16", 1).cuda()
+    x, e = torch.empty(0, 64, dtype=torch.bfloat16, device="cuda"), torch.empty(0, device="cuda")
+    t = torch.empty(0, dtype=torch.int64, device="cuda")
+    gt = torch.full_like(table, 3.0)
+    ctx.vocab_loss(x, table, t, 1.0, e, e)
+    ctx.vocab_loss_backward(x, table, t, 1.0, e, torch.empty(0, 64, device="cuda"), e, x.clone(), gt)
+    assert not gt.any()
+
+
+def test_gradients_against_differences(ctx):
+    """Central differences of the weighted loss in fp32: off by the losses' rounding over the step and its square."""
+    x, table, t, gl = data(5, 9, 8, "f32", 13, ignored=False)
+    got, _ = run(ctx, x, table, t, 1.0, gl)
+    h = 2.0 ** -7
+
+    def value():
+        loss, lse = torch.empty(5, device="cuda"), torch.empty(5, device="cuda")
+        ctx.vocab_loss(x.cuda(), table.cuda(), t.cuda(), 1.0, loss, lse)
+        return float((loss.double().cpu() * gl.double()).sum())
+
+    for name, a in (("grad_x", x), ("grad_table", table)):
+        flat = a.view(-1)
+        for i in range(flat.numel()):
+            old = float(flat[i])
+            flat[i] = old + h
+            up = value()
+            flat[i] = old - h
+            down = value()
+            flat[i] = old
+            assert abs((up - down) / (2 * h) - float(got[name].view(-1)[i])) < 2e-3, (name, i)
+
+
+def test_a_table_beyond_2_to_31_elements(ctx):
+    """Rows whose positions pass 32 bits: the last rows hold the only logits that count."""
+    V, D = 17_000_000, 128
+    table = torch.zeros(V, D, dtype=torch.bfloat16, device="cuda")
+    x = du.rand((6, D), "bf16", 1, 1.0)
+    tail = du.rand((1000, D), "bf16", 2, 1.0)
+    table[V - 1000:] = tail.cuda()
+    t = torch.tensor([V - 1, V - 1000, 3, V - 5, V - 500, -1])
+    got, _ = run(ctx, x.cuda(), table, t.cuda(), 2.0, torch.ones(6).cuda(), device=False)
+    z = 2.0 * (x.double() @ tail.double().t())
+    lse = torch.logsumexp(torch.cat([z, torch.full((6, 1), float(torch.tensor(V - 1000.0).log()), dtype=torch.float64)], 1), 1)
+    picked = torch.tensor([z[0, 999], z[1, 0], 0.0, z[3, 995], z[4, 500], 0.0], dtype=torch.float64)
+    assert (got["lse"].double().cpu() - lse).abs().max() < 1e-4
+    assert (got["loss"].double().cpu() - torch.where(t >= 0, lse - picked, 0.0)).abs().max() < 1e-4
+    p = (z - lse[:, None]).exp()
+    g = torch.tensor([1, 1, 1, 1, 1, 0], dtype=torch.float64)
+    w = p * g[:, None]
+    for i, at in enumerate((999, 0, None, 995, 500)):
+        if at is not None:
+            w[i, at] -= 1.0
+    ref = 2.0 * (w.t() @ x.double())
+    assert (got["grad_table"][V - 1000:].double().cpu() - ref).norm() < 6e-3 * ref.norm()
+    ref3 = -2.0 * x[2].double()
+    assert (got["grad_table"][3].double().cpu() - ref3).norm() < 6e-3 * ref3.norm()
+
+
+def test_replayed_from_a_graph(ctx):
+    """A captured step on a context that has seen the sizes, replayed with other work and synchronisations in between."""
+    from paper_2211_05239_amd import recd
+    x, table, t, gl = (a.cuda() for a in data(300, 2000, 64, "f16", 14))
+    n, D = x.shape
+    want, _ = run(ctx, x, table, t, 1.0, gl, device=False)
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        c = recd.Context(0)
+        out = [torch.zeros(n, device="cuda"), torch.zeros(n, device="cuda"), torch.zeros(n, D, device="cuda"),
+               torch.zeros_like(x), torch.zeros_like(table)]
+
+        def step():
+            c.vocab_loss(x, table, t, 1.0, out[0], out[1], out[2])
+            c.vocab_loss_backward(x, table, t, 1.0, out[1], out[2], gl, out[3], out[4])
+
+        step()
+        s.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            step()
+        for i in range(4):
+            for o in out:
+                o.fill_(float("nan"))
+            graph.replay()
+            s.synchronize()
+            for o, k in ((out[0], "loss"), (out[1], "lse"), (out[3], "grad_x"), (out[4], "grad_table")):
+                assert torch.equal(o, want[k]), (i, k)
+            run(c, x, table, t, 1.0, gl, device=False)
+        c.close()
+
+
+def test_refusals(ctx):
+    from paper_2211_05239_amd import recd
+    lib, h = recd._lib, ctx._h
+    a = torch.zeros(4096, device="cuda")
+    p = a.data_ptr()
+
+    def forward(n=4, V=8, D=64, dt=0, x=p, table=p, t=p, scale=1.0, loss=p, lse=p, ctx_=h):
+        return lib.recd_vocab_loss(ctx_, n, V, D, dt, x, table, t, scale, loss, lse, None)
+
+    def backward(n=4, V=8, D=64, dt=0, lse=p, mean=p, gl=p, gx=p, gt=p, scale=1.0):
+        return lib.recd_vocab_loss_backward(h, n, V, D, dt, p, p, p, scale, lse, mean, gl, gx, gt)
+
+    for kw in (dict(ctx_=None), dict(n=-1), dict(V=-1), dict(V=0), dict(V=1 << 31), dict(n=1 << 31), dict(D=0), dict(D=6),
+               dict(D=260), dict(D=12, dt=1), dict(dt=3), dict(x=None), dict(table=None), dict(t=None), dict(loss=None),
+               dict(lse=None), dict(x=p + 4), dict(table=p + 8), dict(scale=0.0), dict(scale=float("nan")),
+               dict(scale=float("inf"))):
+        assert forward(**kw) == recd.RECD_EINVAL, kw
+    for kw in (dict(D=260), dict(lse=None), dict(gl=None), dict(mean=None), dict(gx=None, gt=None), dict(gx=p + 4),
+               dict(gt=p + 2), dict(V=0), dict(scale=0.0)):
+        assert backward(**kw) == recd.RECD_EINVAL, kw
+    assert forward(n=0, x=None, t=None, loss=None, lse=None) == recd.RECD_OK
