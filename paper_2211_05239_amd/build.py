@@ -10,6 +10,9 @@ LIB = os.path.join(HERE, "librecd.so")
 SOURCES = sorted(glob.glob(os.path.join(HERE, "csrc", "*.hip")))
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++20", "-fPIC", "-shared",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
+         # sums of matrix products in ordinary registers wherever vector instructions use them next: otherwise a kernel
+         # that needs more than 256 registers moves every one of them between the two halves of the register file
+         "-mllvm", "-amdgpu-mfma-vgpr-form=1",
          "-Wall", "-Wno-unused-function", "-Wno-pass-failed",
          "-I", os.path.join(ROOT, "include"), "-I", os.path.join(HERE, "csrc")]
 FLAGS += os.environ.get("RECD_EXTRA_HIPCC_FLAGS", "").split()  # e.g. -D switches of an experiment

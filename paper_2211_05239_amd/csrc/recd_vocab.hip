@@ -30,9 +30,9 @@ constexpr float kSlack = 8.0f;
 template <typename T> constexpr float kLift = std::is_same<T, _Float16>::value ? 7.0f : 0.0f;
 
 // Streamed rows [row0, row0 + ROWS) of a matrix [n, D] into registers and from there into a tile.
-template <typename T, int ROWS, int DP> struct Stream {
+template <typename T, int ROWS, int DP, int THREADS = kBlock> struct Stream {
     using Tile = RecdTile<T, ROWS, DP>;
-    static constexpr int PT = (Tile::PIECES + kBlock - 1) / kBlock;
+    static constexpr int PT = (Tile::PIECES + THREADS - 1) / THREADS;
     typename Tile::Piece held[PT];
 
     __device__ inline void load(const T *m, int64_t row0, int64_t n, int D)
@@ -40,7 +40,7 @@ template <typename T, int ROWS, int DP> struct Stream {
         constexpr int PR = DP / Tile::E;
 #pragma unroll
         for (int i = 0; i < PT; i++) {
-            const int piece = threadIdx.x + i * kBlock;
+            const int piece = threadIdx.x + i * THREADS;
             const int64_t row = row0 + piece / PR;
             const int at = piece % PR * Tile::E;
             held[i] = typename Tile::Piece{};
@@ -52,8 +52,8 @@ template <typename T, int ROWS, int DP> struct Stream {
     {
 #pragma unroll
         for (int i = 0; i < PT; i++)
-            if (threadIdx.x + i * kBlock < (unsigned)Tile::PIECES)
-                t.put(threadIdx.x + i * kBlock, held[i]);
+            if (threadIdx.x + i * THREADS < (unsigned)Tile::PIECES)
+                t.put(threadIdx.x + i * THREADS, held[i]);
     }
 };
 
@@ -63,6 +63,11 @@ template <typename Frag> __device__ inline Frag negated(Frag f)
         f[e] = -f[e];
     return f;
 }
+
+// Tiles of 32 kept rows in a wave, and waves in a block.
+template <typename T, int DP> constexpr int kTiles = 1;
+template <typename T, int DP> constexpr int kManyWaves = sizeof(T) == 4 ? 4 : 8;
+template <typename T, int DP> constexpr int kFewTiles = sizeof(T) == 4 || DP > 128 ? 1 : 2;
 
 struct ForwardArgs {
     int64_t n, V;
@@ -75,12 +80,10 @@ struct ForwardArgs {
     float *part_m, *part_l, *part_o;  // [parts][n] and [parts][n][D]: maximum (in powers of two), sum, weighted sum
 };
 
-// 32 * N rows a wave.  SHARE: the block's waves hold the same rows and take turns at the table's rows, each a part
-// of its own (few rows); otherwise they hold different rows and all see every table row.
-template <typename T, int DP, int N, bool SHARE, bool MEAN>
-__global__ __launch_bounds__(kBlock) void k_vocab_forward(ForwardArgs a)
+// Few rows: the block's waves hold the same 32 * N rows and take turns at the table's rows, each a part of its own.
+template <typename T, int DP, int N, bool MEAN> __global__ __launch_bounds__(kBlock) void k_vocab_forward_few(ForwardArgs a)
 {
-    constexpr int VT = SHARE ? 128 : (sizeof(T) == 4 && DP == 256 ? 32 : 64);
+    constexpr int VT = 128;
     constexpr int KS = DP / 16, DT = DP / 32;
     using Mma = RecdMma<T>;
     using Frag = typename Mma::Frag;
@@ -91,7 +94,7 @@ __global__ __launch_bounds__(kBlock) void k_vocab_forward(ForwardArgs a)
     if (split >= a.splits)
         return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t row0 = (int64_t)rb * (SHARE ? 32 * N : 32 * N * kWaves) + (SHARE ? 0 : wave * 32 * N);
+    const int64_t row0 = (int64_t)rb * 32 * N;
     const int64_t tiles = (a.V + VT - 1) / VT, t0 = split * a.tiles_per_split;
     const int64_t t1 = t0 + a.tiles_per_split < tiles ? t0 + a.tiles_per_split : tiles;
 
@@ -121,9 +124,8 @@ __global__ __launch_bounds__(kBlock) void k_vocab_forward(ForwardArgs a)
         __syncthreads();
         if (t + 1 < t1)
             stream.load((const T *)a.table, (t + 1) * VT, a.V, a.D);
-        if (row0 >= a.n)
-            continue;
-        for (int st = SHARE ? wave : 0; st < VT / 32; st += SHARE ? kWaves : 1) {
+        {
+            const int st = wave;
             recd_f32x16 s[N];
             for (int j = 0; j < N; j++)
                 s[j] = recd_f32x16{};
@@ -179,7 +181,7 @@ __global__ __launch_bounds__(kBlock) void k_vocab_forward(ForwardArgs a)
             }
         }
     }
-    const int64_t part = SHARE ? (int64_t)split * kWaves + wave : split;
+    const int64_t part = (int64_t)split * kWaves + wave;
     for (int j = 0; j < N; j++) {
         const int64_t row = row0 + 32 * j + (lane & 31);
         const float sum = l[j] + __shfl_xor(l[j], 32);
@@ -191,6 +193,188 @@ __global__ __launch_bounds__(kBlock) void k_vocab_forward(ForwardArgs a)
         }
         if constexpr (MEAN)
             for (int d = 0; d < DT; d++)
+                for (int r = 0; r < 16; r += 4) {
+                    const int col = 32 * d + recd_sums_row(r, lane);
+                    if (col < a.D)
+                        *reinterpret_cast<recd_f32x4 *>(a.part_o + (part * a.n + row) * a.D + col) =
+                            recd_f32x4{o[j][d][r], o[j][d][r + 1], o[j][d][r + 2], o[j][d][r + 3]};
+                }
+    }
+}
+
+// 32 * N rows a wave, other ones in every wave of a block; all of them see every table row of the split.
+//
+// The loop is pipelined over subtiles of 32 table rows: one turn multiplies the next subtile's scores and the current
+// one's sums while the current scores become exponentials, so that matrix cores and vector units have work of one
+// basic block to interleave.  The check of the running maximum stands behind it, the only branch.  Three tiles in LDS let
+// a wave store the next tile while another one is still at the last but one: one barrier a tile.
+template <typename T, int DP, int N, int W, bool MEAN>
+__global__ __launch_bounds__(64 * W) void k_vocab_forward(ForwardArgs a)
+{
+    constexpr int VT = sizeof(T) == 4 && DP > 128 ? 32 : 64;
+    constexpr int TURNS = VT / 32;
+    constexpr int KS = DP / 16, DT = DP / 32, BUFS = 3;
+    using Mma = RecdMma<T>;
+    using Frag = typename Mma::Frag;
+    __shared__ RecdTile<T, VT, DP> tiles_lds[BUFS];
+    // the row blocks of one split side by side on one die, whose L2 then serves the split's rows to all of them
+    const int xcd = blockIdx.x & 7, at = blockIdx.x >> 3;
+    const int rb = at % a.row_blocks, split = at / a.row_blocks * 8 + xcd;
+    if (split >= a.splits)
+        return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t row0 = ((int64_t)rb * W + wave) * 32 * N;
+    const int64_t tiles = (a.V + VT - 1) / VT, t0 = split * a.tiles_per_split;
+    const int64_t t1 = t0 + a.tiles_per_split < tiles ? t0 + a.tiles_per_split : tiles;
+
+    Frag xf[N][KS];
+#pragma unroll
+    for (int j = 0; j < N; j++) {
+        const int64_t row = row0 + 32 * j + (lane & 31);
+#pragma unroll
+        for (int k = 0; k < KS; k++) {
+            xf[j][k] = recd_row_frag<T>((const T *)a.x + row * a.D, 16 * k, a.D, row < a.n, lane);
+            if (a.negative)
+                xf[j][k] = negated(xf[j][k]);
+        }
+    }
+    float m[N], l[N];
+    recd_f32x16 o[N][MEAN ? DT : 1], s[2][N];
+#pragma unroll
+    for (int j = 0; j < N; j++) {
+        m[j] = -INFINITY;
+        l[j] = 0.0f;
+#pragma unroll
+        for (int d = 0; d < (MEAN ? DT : 1); d++)
+            o[j][d] = recd_f32x16{};
+    }
+    auto scores = [&](const RecdTile<T, VT, DP> &tile, int row, recd_f32x16(&out)[N]) {
+#pragma unroll
+        for (int j = 0; j < N; j++)
+            out[j] = recd_f32x16{};
+#pragma unroll
+        for (int k = 0; k < KS; k++) {
+            const Frag w = tile.rows(row, 16 * k, lane);
+#pragma unroll
+            for (int j = 0; j < N; j++)
+                out[j] = Mma::mul(w, xf[j][k], out[j]);
+        }
+    };
+    // rows behind the table's end count as -inf; the maximum moves where new scores are far above it
+    auto settle = [&](int64_t v0, recd_f32x16(&x)[N]) {
+        if (a.V - v0 < 32) {
+            asm volatile("");  // a branch: the last subtile alone pays for the comparisons
+            const int left = (int)(a.V - v0);
+#pragma unroll
+            for (int j = 0; j < N; j++)
+#pragma unroll
+                for (int r = 0; r < 16; r++)
+                    x[j][r] = recd_sums_row(r, lane) >= left ? -INFINITY : x[j][r];
+        }
+        float top[N];
+        bool above = false;
+#pragma unroll
+        for (int j = 0; j < N; j++) {
+            top[j] = x[j][0];
+#pragma unroll
+            for (int r = 1; r < 16; r++)
+                top[j] = fmaxf(top[j], x[j][r]);
+            top[j] = fmaxf(top[j], __shfl_xor(top[j], 32)) * a.c - kLift<T>;
+            above |= top[j] > m[j] + kSlack;
+        }
+        if (__any(above))
+#pragma unroll
+            for (int j = 0; j < N; j++) {
+                const float now = fmaxf(m[j], top[j]);
+                const float f = now == m[j] ? 1.0f : recd_exp2(m[j] - now);
+                m[j] = now;
+                l[j] *= f;
+                if constexpr (MEAN)
+#pragma unroll
+                    for (int d = 0; d < DT; d++)
+#pragma unroll
+                        for (int r = 0; r < 16; r++)
+                            o[j][d][r] *= f;
+            }
+    };
+    Stream<T, VT, DP, 64 * W> stream;
+    const T *table = (const T *)a.table;
+    if (t0 < t1) {
+        stream.load(table, t0 * VT, a.V, a.D);
+        stream.store(tiles_lds[0]);
+        if (t0 + 1 < t1)
+            stream.load(table, (t0 + 1) * VT, a.V, a.D);
+        __syncthreads();
+        scores(tiles_lds[0], 0, s[0]);
+        settle(t0 * VT, s[0]);
+    }
+    int buf = 0;
+    for (int64_t t = t0; t < t1; t++) {
+        const int next = buf + 1 == BUFS ? 0 : buf + 1;
+        if (t + 1 < t1) {
+            stream.store(tiles_lds[next]);
+            if (t + 2 < t1)
+                stream.load(table, (t + 2) * VT, a.V, a.D);
+        }
+#pragma unroll
+        for (int st = 0; st < TURNS; st++) {
+            constexpr int kLast = TURNS - 1;
+            const int now = TURNS == 1 ? 0 : st & 1, then = TURNS == 1 ? 1 : 1 - now;
+            if (st == kLast)
+                __syncthreads();
+            scores(st == kLast ? tiles_lds[next] : tiles_lds[buf], st == kLast ? 0 : 32 * (st + 1), s[then]);
+#pragma unroll
+            for (int j = 0; j < N; j++) {
+                const float from = m[j] == -INFINITY ? 0.0f : m[j];  // a row of logits that are all -inf
+                float sum = 0.0f;
+#pragma unroll
+                for (int r = 0; r < 16; r++) {
+                    s[now][j][r] = recd_exp2(s[now][j][r] * a.c - from);
+                    sum += s[now][j][r];
+                }
+                l[j] += sum;
+            }
+            if constexpr (MEAN) {
+#pragma unroll
+                for (int h = 0; h < 2; h++) {
+                    Frag p[N];
+#pragma unroll
+                    for (int j = 0; j < N; j++)
+                        p[j] = recd_sums_frag<T>(s[now][j], h);
+#pragma unroll
+                    for (int d = 0; d < DT; d++) {
+                        const Frag w = tiles_lds[buf].columns(32 * st + 16 * h, 32 * d, lane);
+#pragma unroll
+                        for (int j = 0; j < N; j++)
+                            o[j][d] = Mma::mul(w, p[j], o[j][d]);
+                    }
+                }
+            }
+            // behind the last tile these are scores of what an older tile left in LDS, and nobody reads them
+            if (st != kLast || t + 1 < t1)
+                settle(st == kLast ? (t + 1) * VT : t * VT + 32 * (st + 1), s[then]);
+            if constexpr (TURNS == 1)
+#pragma unroll
+                for (int j = 0; j < N; j++)
+                    s[0][j] = s[1][j];
+        }
+        buf = next;
+    }
+    const int64_t part = split;
+#pragma unroll
+    for (int j = 0; j < N; j++) {
+        const int64_t row = row0 + 32 * j + (lane & 31);
+        const float sum = l[j] + __shfl_xor(l[j], 32);
+        if (row >= a.n)
+            continue;
+        if (lane < 32) {
+            a.part_m[part * a.n + row] = m[j];
+            a.part_l[part * a.n + row] = sum;
+        }
+        if constexpr (MEAN)
+#pragma unroll
+            for (int d = 0; d < DT; d++)
+#pragma unroll
                 for (int r = 0; r < 16; r += 4) {
                     const int col = 32 * d + recd_sums_row(r, lane);
                     if (col < a.D)
@@ -336,109 +520,160 @@ struct TableGradArgs {
     void *grad_table;
 };
 
-// 32 * N table rows a wave; the rows x stream past them.
-template <typename T, int DP, int N> __global__ __launch_bounds__(kBlock) void k_vocab_grad_table(TableGradArgs a)
+// 32 * N table rows a wave; the rows x stream past them, pipelined as in the forward kernel.  The targets' weights
+// are taken off in a product of their own, in the few subtiles that hold a target of the wave's rows, and in two
+// roundings of which the second takes up what the first leaves: they are most of a row that is a target.
+template <typename T, int DP, int N, int W> __global__ __launch_bounds__(64 * W) void k_vocab_grad_table(TableGradArgs a)
 {
-    constexpr int XT = sizeof(T) == 4 && DP == 256 ? 32 : 64;
-    constexpr int KS = DP / 16, DT = DP / 32;
+    constexpr int XT = sizeof(T) == 4 && DP > 128 ? 32 : 64;
+    constexpr int KS = DP / 16, DT = DP / 32, TURNS = XT / 32;
     using Mma = RecdMma<T>;
     using Frag = typename Mma::Frag;
-    __shared__ RecdTile<T, XT, DP> tile;
-    __shared__ alignas(16) float lse[XT], g[XT];
-    __shared__ int32_t target[XT];
+    __shared__ RecdTile<T, XT, DP> tiles_lds[3];
+    __shared__ alignas(16) float lse[3][XT], g[3][XT];
+    __shared__ int32_t target[3][XT];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t v0 = (int64_t)blockIdx.x * 32 * N * kWaves + wave * 32 * N;
+    const int64_t v0 = ((int64_t)blockIdx.x * W + wave) * 32 * N;
     Frag wf[N][KS];
-    recd_f32x16 o[N][DT];
+    recd_f32x16 o[N][DT], s[2][N];
+#pragma unroll
     for (int j = 0; j < N; j++) {
         const int64_t v = v0 + 32 * j + (lane & 31);
+#pragma unroll
         for (int k = 0; k < KS; k++) {
             wf[j][k] = recd_row_frag<T>((const T *)a.table + v * a.D, 16 * k, a.D, v < a.V, lane);
             if (a.negative)
                 wf[j][k] = negated(wf[j][k]);
         }
+#pragma unroll
         for (int d = 0; d < DT; d++)
             o[j][d] = recd_f32x16{};
     }
-    const int64_t tiles = (a.n + XT - 1) / XT;
-    Stream<T, XT, DP> stream;
+    const int tiles = (int)((a.n + XT - 1) / XT);
+    Stream<T, XT, DP, 64 * W> stream;
     float next_lse = 0.0f, next_g = 0.0f;
     int32_t next_t = -1;
-    auto load = [&](int64_t t) {
-        stream.load((const T *)a.x, t * XT, a.n, a.D);
-        const int64_t row = t * XT + threadIdx.x;
+    auto load = [&](int t) {
+        stream.load((const T *)a.x, (int64_t)t * XT, a.n, a.D);
+        const int64_t row = (int64_t)t * XT + threadIdx.x;
         const bool there = threadIdx.x < XT && row < a.n;
         next_lse = there ? a.row_lse[row] : 0.0f;
         next_g = there ? a.row_g[row] : 0.0f;
         next_t = there ? a.row_t[row] : -1;
     };
-    load(0);
-    for (int64_t t = 0; t < tiles; t++) {
-        __syncthreads();
-        stream.store(tile);
+    auto store = [&](int b) {
+        stream.store(tiles_lds[b]);
         if (threadIdx.x < XT) {
-            lse[threadIdx.x] = next_lse;
-            g[threadIdx.x] = next_g;
-            target[threadIdx.x] = next_t;
+            lse[b][threadIdx.x] = next_lse;
+            g[b][threadIdx.x] = next_g;
+            target[b][threadIdx.x] = next_t;
         }
-        __syncthreads();
-        if (t + 1 < tiles)
-            load(t + 1);
-        if (v0 >= a.V)
-            continue;
+    };
+    auto scores = [&](const RecdTile<T, XT, DP> &tile, int row, recd_f32x16(&out)[N]) {
 #pragma unroll
-        for (int st = 0; st < XT / 32; st++) {
-            recd_f32x16 s[N];
+        for (int j = 0; j < N; j++)
+            out[j] = recd_f32x16{};
+#pragma unroll
+        for (int k = 0; k < KS; k++) {
+            const Frag x = tile.rows(row, 16 * k, lane);
+#pragma unroll
             for (int j = 0; j < N; j++)
-                s[j] = recd_f32x16{};
+                out[j] = Mma::mul(x, wf[j][k], out[j]);
+        }
+    };
+    if (tiles > 0) {
+        load(0);
+        store(0);
+        if (tiles > 1)
+            load(1);
+        __syncthreads();
+        scores(tiles_lds[0], 0, s[0]);
+    }
+    int buf = 0;
+    for (int t = 0; t < tiles; t++) {
+        const int next = buf + 1 == 3 ? 0 : buf + 1;
+        if (t + 1 < tiles) {
+            store(next);
+            if (t + 2 < tiles)
+                load(t + 2);
+        }
 #pragma unroll
-            for (int k = 0; k < KS; k++) {
-                const Frag x = tile.rows(32 * st, 16 * k, lane);
-                for (int j = 0; j < N; j++)
-                    s[j] = Mma::mul(x, wf[j][k], s[j]);
-            }
-            const int32_t tg = target[32 * st + (lane & 31)];
-            const bool hit = __any(tg >= v0 && tg < v0 + 32 * N);  // one of these rows' targets is among the wave's
+        for (int st = 0; st < TURNS; st++) {
+            constexpr int kLast = TURNS - 1;
+            const int now = TURNS == 1 ? 0 : st & 1, then = TURNS == 1 ? 1 : 1 - now;
+            if (st == kLast)
+                __syncthreads();
+            // (behind the last tile: of what an older tile left in LDS, for nobody)
+            scores(st == kLast ? tiles_lds[next] : tiles_lds[buf], st == kLast ? 0 : 32 * (st + 1), s[then]);
+#pragma unroll
             for (int r = 0; r < 16; r += 4) {
                 const int row = 32 * st + recd_sums_row(r, lane);
-                const recd_f32x4 from = *reinterpret_cast<const recd_f32x4 *>(lse + row);
-                const recd_f32x4 by = *reinterpret_cast<const recd_f32x4 *>(g + row);
+                const recd_f32x4 from = *reinterpret_cast<const recd_f32x4 *>(&lse[buf][row]);
+                const recd_f32x4 by = *reinterpret_cast<const recd_f32x4 *>(&g[buf][row]);
+#pragma unroll
                 for (int q = 0; q < 4; q++)
+#pragma unroll
                     for (int j = 0; j < N; j++)
-                        s[j][r + q] = recd_exp2(s[j][r + q] * a.c - from[q]) * by[q];
+                        s[now][j][r + q] = recd_exp2(s[now][j][r + q] * a.c - from[q]) * by[q];
             }
-            if (hit)
-                for (int j = 0; j < N; j++)
-                    for (int r = 0; r < 16; r++) {
-                        const int row = 32 * st + recd_sums_row(r, lane);
-                        if (target[row] == v0 + 32 * j + (lane & 31))
-                            s[j][r] -= g[row];
-                    }
 #pragma unroll
             for (int h = 0; h < 2; h++) {
                 Frag p[N];
+#pragma unroll
                 for (int j = 0; j < N; j++)
-                    p[j] = recd_sums_frag<T>(s[j], h);
+                    p[j] = recd_sums_frag<T>(s[now][j], h);
 #pragma unroll
                 for (int d = 0; d < DT; d++) {
-                    const Frag x = tile.columns(32 * st + 16 * h, 32 * d, lane);
+                    const Frag x = tiles_lds[buf].columns(32 * st + 16 * h, 32 * d, lane);
+#pragma unroll
                     for (int j = 0; j < N; j++)
                         o[j][d] = Mma::mul(x, p[j], o[j][d]);
                 }
             }
+            const int32_t mine = target[buf][32 * st + (lane & 31)];
+            if (__any(mine >= v0 && mine < v0 + 32 * N))
+#pragma unroll
+                for (int j = 0; j < N; j++)
+#pragma unroll
+                    for (int h = 0; h < 2; h++) {
+                        Frag p[2];
+#pragma unroll
+                        for (int e = 0; e < 8; e++) {
+                            const int row = 32 * st + recd_sums_row(8 * h + e, lane);
+                            const float w = target[buf][row] == v0 + 32 * j + (lane & 31) ? -g[buf][row] : 0.0f;
+                            p[0][e] = (T)w;
+                            p[1][e] = (T)(w - (float)p[0][e]);
+                        }
+#pragma unroll
+                        for (int d = 0; d < DT; d++) {
+                            const Frag x = tiles_lds[buf].columns(32 * st + 16 * h, 32 * d, lane);
+                            o[j][d] = Mma::mul(x, p[0], o[j][d]);
+                            if constexpr (sizeof(T) == 2)
+                                o[j][d] = Mma::mul(x, p[1], o[j][d]);
+                        }
+                    }
+            if constexpr (TURNS == 1)
+#pragma unroll
+                for (int j = 0; j < N; j++)
+                    s[0][j] = s[1][j];
         }
+        buf = next;
     }
     const float back = a.lift ? a.scale / *a.lift : a.scale;
+#pragma unroll
     for (int j = 0; j < N; j++) {
         const int64_t v = v0 + 32 * j + (lane & 31);
         if (v >= a.V)
             continue;
+#pragma unroll
         for (int d = 0; d < DT; d++)
+#pragma unroll
             for (int r = 0; r < 16; r += 4) {
                 const int col = 32 * d + recd_sums_row(r, lane);
                 if (col >= a.D)
                     continue;
                 T out[4];
+#pragma unroll
                 for (int q = 0; q < 4; q++)
                     out[q] = (T)(o[j][d][r + q] * back);
                 __builtin_memcpy((T *)a.grad_table + v * a.D + col, out, sizeof out);
@@ -485,6 +720,23 @@ recd_status validate_targets(recd_ctx *ctx, int64_t n, int64_t V, const int64_t 
     return RECD_OK;
 }
 
+// The tiles' width for rows of D elements.
+template <typename F> void with_width(int D, F f)
+{
+    if (D <= 32)
+        f(std::integral_constant<int, 32>{});
+    else if (D <= 64)
+        f(std::integral_constant<int, 64>{});
+    else if (D <= 96)
+        f(std::integral_constant<int, 96>{});
+    else if (D <= 128)
+        f(std::integral_constant<int, 128>{});
+    else if (D <= 192)
+        f(std::integral_constant<int, 192>{});
+    else
+        f(std::integral_constant<int, 256>{});
+}
+
 // How a forward call is cut.
 struct ForwardShape {
     bool share;
@@ -493,45 +745,54 @@ struct ForwardShape {
     int parts;
 };
 
-ForwardShape forward_shape(const recd_ctx *ctx, int64_t n, int64_t V, int D, recd_dtype dt)
+ForwardShape forward_shape(const recd_ctx *ctx, int64_t n, int64_t V, int D, recd_dtype dt, bool mean)
 {
     const bool f32 = dt == RECD_F32;
-    const int per_wave = f32 || D > 128 ? 32 : 64;
+    const int per_few = f32 || D > 128 ? 32 : 64;
     ForwardShape s;
     s.share = n <= 128;
     const int vt = s.share ? 128 : (f32 && D > 128 ? 32 : 64);
-    const int64_t rows = s.share ? per_wave : per_wave * kWaves, tiles = (V + vt - 1) / vt;
+    const int64_t rows = s.share ? per_few : (f32 ? 128 : 256), tiles = (V + vt - 1) / vt;
     s.row_blocks = (int)((n + rows - 1) / rows);
-    // two blocks a CU, in splits of at least two tiles
-    int64_t splits = (2 * ctx->num_cu + s.row_blocks - 1) / s.row_blocks;
-    if (splits > (tiles + 1) / 2)
-        splits = (tiles + 1) / 2;
-    if (splits < 1)
-        splits = 1;
+    // A die takes every eighth split, all row blocks of it, and holds one or two blocks a CU at a time (the registers of
+    // the sums decide): the number of splits whose rounds are fullest, few of them before many whose parts have to
+    // be joined; at least two tiles each.
+    const int64_t at_once = (int64_t)ctx->num_cu / 8 * (mean && D > 64 ? 1 : 2);
+    int64_t splits = 1;
+    double best = 1e30;
+    for (int64_t k = 1; k <= 16 * at_once && k * s.row_blocks <= 64 * at_once && (k == 1 || 2 * k <= tiles); k++) {
+        const int64_t rounds = ((k + 7) / 8 * s.row_blocks + at_once - 1) / at_once;
+        const double cost = (double)rounds / (double)k + 1e-4 * (double)k;
+        if (cost < best) {
+            best = cost;
+            splits = k;
+        }
+    }
     s.tiles_per_split = (tiles + splits - 1) / splits;
     s.splits = (int)((tiles + s.tiles_per_split - 1) / s.tiles_per_split);
     s.parts = s.share ? s.splits * kWaves : s.splits;
     return s;
 }
 
-template <typename T, int DP, int N> void launch_forward(const ForwardArgs &a, bool share, hipStream_t st)
+template <typename T, int DP> void launch_forward(const ForwardArgs &a, bool share, hipStream_t st)
 {
     const dim3 grid((unsigned)((a.splits + 7) / 8 * 8 * a.row_blocks));
     const bool mean = a.part_o != nullptr;
+    constexpr int N = kTiles<T, DP>, W = kManyWaves<T, DP>;
     if (share && mean)
-        hipLaunchKernelGGL((k_vocab_forward<T, DP, N, true, true>), grid, dim3(kBlock), 0, st, a);
+        hipLaunchKernelGGL((k_vocab_forward_few<T, DP, kFewTiles<T, DP>, true>), grid, dim3(kBlock), 0, st, a);
     else if (share)
-        hipLaunchKernelGGL((k_vocab_forward<T, DP, N, true, false>), grid, dim3(kBlock), 0, st, a);
+        hipLaunchKernelGGL((k_vocab_forward_few<T, DP, kFewTiles<T, DP>, false>), grid, dim3(kBlock), 0, st, a);
     else if (mean)
-        hipLaunchKernelGGL((k_vocab_forward<T, DP, N, false, true>), grid, dim3(kBlock), 0, st, a);
+        hipLaunchKernelGGL((k_vocab_forward<T, DP, N, W, true>), grid, dim3(64 * W), 0, st, a);
     else
-        hipLaunchKernelGGL((k_vocab_forward<T, DP, N, false, false>), grid, dim3(kBlock), 0, st, a);
+        hipLaunchKernelGGL((k_vocab_forward<T, DP, N, W, false>), grid, dim3(64 * W), 0, st, a);
 }
 
-template <typename T, int DP, int N> void launch_grad_table(const TableGradArgs &a, hipStream_t st)
+template <typename T, int DP> void launch_grad_table(const TableGradArgs &a, hipStream_t st)
 {
-    const int rows = 32 * N * kWaves;
-    hipLaunchKernelGGL((k_vocab_grad_table<T, DP, N>), dim3((unsigned)((a.V + rows - 1) / rows)), dim3(kBlock), 0, st, a);
+    constexpr int N = kTiles<T, DP>, W = kManyWaves<T, DP>, rows = 32 * N * W;
+    hipLaunchKernelGGL((k_vocab_grad_table<T, DP, N, W>), dim3((unsigned)((a.V + rows - 1) / rows)), dim3(64 * W), 0, st, a);
 }
 
 } // namespace
@@ -553,7 +814,7 @@ recd_status recd_vocab_loss(recd_ctx *ctx, int64_t n, int64_t V, int D, recd_dty
     RECD_HIP(ctx, hipSetDevice(ctx->device));
     if (ctx->validate)
         RECD_TRY(validate_targets(ctx, n, V, targets));
-    const ForwardShape s = forward_shape(ctx, n, V, D, dt);
+    const ForwardShape s = forward_shape(ctx, n, V, D, dt, mean_row != nullptr);
     WsCarver size(nullptr);
     auto carve = [&](WsCarver &c, ForwardArgs &a) {
         a.part_m = c.take<float>((size_t)s.parts * n);
@@ -568,13 +829,7 @@ recd_status recd_vocab_loss(recd_ctx *ctx, int64_t n, int64_t V, int D, recd_dty
     carve(c, a);
     recd_with_type(dt, [&](auto t) {
         using T = decltype(t);
-        constexpr int N = sizeof(T) == 4 ? 1 : 2;
-        if (D <= 64)
-            launch_forward<T, 64, N>(a, s.share, ctx->stream);
-        else if (D <= 128)
-            launch_forward<T, 128, N>(a, s.share, ctx->stream);
-        else
-            launch_forward<T, 256, 1>(a, s.share, ctx->stream);
+        with_width(D, [&](auto w) { launch_forward<T, w.value>(a, s.share, ctx->stream); });
         hipLaunchKernelGGL((k_vocab_join<T>), dim3((unsigned)((n + kWaves - 1) / kWaves)), dim3(kBlock), 0, ctx->stream, n, V,
                            D, scale, s.parts, a.part_m, a.part_l, a.part_o, (const T *)x, (const T *)table, targets, loss,
                            lse, mean_row);
@@ -627,13 +882,7 @@ recd_status recd_vocab_loss_backward(recd_ctx *ctx, int64_t n, int64_t V, int D,
         if (!grad_table)
             return;
         TableGradArgs a{n, V, D, fabsf(scale) * kRecdLog2e, scale, scale < 0, x, table, row_lse, row_g, lift, row_t, grad_table};
-        constexpr int N = sizeof(T) == 4 ? 1 : 2;
-        if (D <= 64)
-            launch_grad_table<T, 64, N>(a, ctx->stream);
-        else if (D <= 128)
-            launch_grad_table<T, 128, N>(a, ctx->stream);
-        else
-            launch_grad_table<T, 256, 1>(a, ctx->stream);
+        with_width(D, [&](auto w) { launch_grad_table<T, w.value>(a, ctx->stream); });
     });
     RECD_HIP(ctx, hipGetLastError());
     return RECD_OK;
