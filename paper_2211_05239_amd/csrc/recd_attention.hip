@@ -230,10 +230,10 @@ template <typename T, int DP, int NW, int BK> __global__ __launch_bounds__(64 * 
                     s[r] *= c;
             if (a.slopes)
                 for (int r = 0; r < 16; r++)
-                    s[r] -= slope * fabsf((float)(pos - j0 - recd_sums_row(r, lane)));
+                    s[r] -= slope * fabsf((float)(pos - j0 - recd_score_row(r, lane)));
             if (j0 + 32 > wave_full)
                 for (int r = 0; r < 16; r++)
-                    if (j0 + recd_sums_row(r, lane) >= lim)
+                    if (j0 + recd_score_row(r, lane) >= lim)
                         s[r] = -INFINITY;
             float top = s[0];
             for (int r = 1; r < 16; r++)
@@ -472,7 +472,7 @@ template <typename T, int DP, int NW, int BK> __global__ __launch_bounds__(64 * 
                 dp = Mma::mul(vt.rows(32 * st, 16 * k, lane), gf[k], dp);
             }
             for (int r = 0; r < 16; r++) {
-                const int j = j0 + recd_sums_row(r, lane);
+                const int j = j0 + recd_score_row(r, lane);
                 s[r] = score_of(a, s[r], dp[r], from, delta, slope, pos - j, j < lim).ds * lift;
             }
 #pragma unroll
@@ -586,7 +586,7 @@ template <typename T, int DP, int NW, int BQ> __global__ __launch_bounds__(64 * 
             }
 #pragma unroll
             for (int r = 0; r < 16; r++) {
-                const int row = 32 * st + recd_sums_row(r, lane);
+                const int row = 32 * st + recd_score_row(r, lane);
                 const Score x = score_of(a, s[r], dp[r], row_from[row], row_delta[row], row_slope[row], row_pos[row] - j,
                                          j < row_lim[row]);
                 s[r] = x.p * lift_p;

@@ -8,9 +8,12 @@
 //   B (kept):     lane l holds column l & 31, the same elements k
 //   sums:         lane l holds column l & 31, register r holds row 8 * (r >> 2) + 4 * (l >> 5) + (r & 3)
 // The second product contracts over the streamed rows in the order in which the sums' registers hold them, so the
-// scores go from sums to B without leaving their lane: step m takes registers 8m .. 8m + 7, and the A operand's
-// element e is then row 16m + 8 * (e >> 2) + 4 * (l >> 5) + (e & 3) of column l & 31.  16-bit columns are read by the LDS's
-// transposing loads, which hand a lane four rows of its column.
+// scores go from sums to B without leaving their lane: step m takes registers 8m .. 8m + 7.  16-bit columns are read
+// by the LDS's transposing loads, which hand a lane four rows of its column.
+// Which streamed row stands in which row of the product is free.  Rows lie 4 banks of 4 bytes apart (modulo 32, by 16
+// bytes of padding), which suits the reads by rows, 16 bytes from each of 8 rows at a time; the transposing reads
+// take 32 bytes from each of 4 rows, which must be 2 rows apart not to meet: row 4h + b of 8 rows of the product is
+// row 2b + h of the tile.  (With rows in order the reads lost 56 % of the LDS's busy cycles to conflicts.)
 #pragma once
 
 #include "recd_vec.h"
@@ -47,7 +50,15 @@ template <> struct RecdMma<float> {
     }
 };
 
-// A tile of ROWS rows of DP elements in LDS.  16 bytes between the rows spread the lanes' reads over the banks.
+// The tile's row (of 32) in row i of the product.
+__device__ inline int recd_tile_row(int i) { return (i & ~7) | (i & 3) << 1 | (i >> 2 & 1); }
+// The row of the product that tile row i stands in.
+__device__ inline int recd_product_row(int i) { return (i & ~7) | (i & 1) << 2 | (i >> 1 & 3); }
+// Row of the product in a sums' register, and the tile's row in a score's.
+__device__ inline int recd_sums_row(int r, int lane) { return 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3); }
+__device__ inline int recd_score_row(int r, int lane) { return 8 * (r >> 2) + 2 * (r & 3) + (lane >> 5); }
+
+// A tile of ROWS rows of DP elements in LDS.
 template <typename T, int ROWS, int DP> struct RecdTile {
     static constexpr int E = 16 / sizeof(T), LD = DP + E, PIECES = ROWS * (DP / E);
     using Frag = typename RecdMma<T>::Frag;
@@ -57,23 +68,23 @@ template <typename T, int ROWS, int DP> struct RecdTile {
     // elements k0 .. k0 + 16 of the 32 rows from row0 on
     __device__ inline Frag rows(int row0, int k0, int lane) const
     {
-        return *reinterpret_cast<const Frag *>(at + (row0 + (lane & 31)) * LD + k0 + (lane >> 5) * 8);
+        return *reinterpret_cast<const Frag *>(at + (row0 + recd_tile_row(lane & 31)) * LD + k0 + (lane >> 5) * 8);
     }
     // columns d0 .. d0 + 32 of the 16 rows from row0 on, in the order of the sums' registers
     __device__ inline Frag columns(int row0, int d0, int lane) const
     {
         if constexpr (sizeof(T) == 4) {
             Frag f;
-            const T *p = at + (row0 + 4 * (lane >> 5)) * LD + d0 + (lane & 31);
+            const T *p = at + (row0 + (lane >> 5)) * LD + d0 + (lane & 31);
 #pragma unroll
             for (int e = 0; e < 8; e++)
-                f[e] = p[(8 * (e >> 2) + (e & 3)) * LD];
+                f[e] = p[(8 * (e >> 2) + 2 * (e & 3)) * LD];
             return f;
         } else {
             // 16 lanes name four rows of 16 columns, 8 bytes each; each of them receives one column
             using Half = __attribute__((address_space(3))) recd_s16x4;
             const int i = lane & 15;
-            const T *p = at + (row0 + 4 * (lane >> 5) + (i >> 2)) * LD + d0 + 16 * ((lane >> 4) & 1) + 4 * (i & 3);
+            const T *p = at + (row0 + (lane >> 5) + 2 * (i >> 2)) * LD + d0 + 16 * ((lane >> 4) & 1) + 4 * (i & 3);
             union {
                 recd_s16x4 half[2];
                 Frag f;
@@ -117,9 +128,6 @@ template <typename T> __device__ inline typename RecdMma<T>::Frag recd_sums_frag
         f[e] = (T)s[8 * m + e];
     return f;
 }
-
-// Row of a sums' register within its 32.
-__device__ inline int recd_sums_row(int r, int lane) { return 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3); }
 
 constexpr float kRecdLog2e = 1.4426950408889634f, kRecdLn2 = 0.6931471805599453f;
 __device__ inline float recd_exp2(float x) { return __builtin_amdgcn_exp2f(x); }

@@ -139,7 +139,7 @@ template <typename T, int DP, int N, bool MEAN> __global__ __launch_bounds__(kBl
             if (left < 32)
                 for (int j = 0; j < N; j++)
                     for (int r = 0; r < 16; r++)
-                        if (recd_sums_row(r, lane) >= left)
+                        if (recd_score_row(r, lane) >= left)
                             s[j][r] = -INFINITY;
 #pragma unroll
             for (int j = 0; j < N; j++) {
@@ -269,7 +269,7 @@ __global__ __launch_bounds__(64 * W) void k_vocab_forward(ForwardArgs a)
             for (int j = 0; j < N; j++)
 #pragma unroll
                 for (int r = 0; r < 16; r++)
-                    x[j][r] = recd_sums_row(r, lane) >= left ? -INFINITY : x[j][r];
+                    x[j][r] = recd_score_row(r, lane) >= left ? -INFINITY : x[j][r];
         }
         float top[N];
         bool above = false;
@@ -564,9 +564,10 @@ template <typename T, int DP, int N, int W> __global__ __launch_bounds__(64 * W)
     auto store = [&](int b) {
         stream.store(tiles_lds[b]);
         if (threadIdx.x < XT) {
-            lse[b][threadIdx.x] = next_lse;
-            g[b][threadIdx.x] = next_g;
-            target[b][threadIdx.x] = next_t;
+            const int i = recd_product_row(threadIdx.x);  // a lane reads those of four neighbouring sums at a time
+            lse[b][i] = next_lse;
+            g[b][i] = next_g;
+            target[b][i] = next_t;
         }
     };
     auto scores = [&](const RecdTile<T, XT, DP> &tile, int row, recd_f32x16(&out)[N]) {
