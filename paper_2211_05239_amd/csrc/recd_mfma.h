@@ -10,10 +10,11 @@
 // The second product contracts over the streamed rows in the order in which the sums' registers hold them, so the
 // scores go from sums to B without leaving their lane: step m takes registers 8m .. 8m + 7.  16-bit columns are read
 // by the LDS's transposing loads, which hand a lane four rows of its column.
-// Which streamed row stands in which row of the product is free.  Rows lie 4 banks of 4 bytes apart (modulo 32, by 16
-// bytes of padding), which suits the reads by rows, 16 bytes from each of 8 rows at a time; the transposing reads
-// take 32 bytes from each of 4 rows, which must be 2 rows apart not to meet: row 4h + b of 8 rows of the product is
-// row 2b + h of the tile.  (With rows in order the reads lost 56 % of the LDS's busy cycles to conflicts.)
+// Which streamed row stands in which row of the product is free.  Rows lie an odd multiple of 4 banks (of 64, 4 bytes
+// each) apart by 16 bytes of padding, which suits the reads by rows, 16 bytes from each of 16 rows at a time; the
+// transposing reads take 64 bytes from each of 4 rows at a time, which must lie 4 rows apart not to meet.  So rows
+// 0 .. 3 of the product are rows 0, 4, 8, 12 of the tile, and so on (recd_tile_row).  With rows in order 56 % of the LDS's
+// busy cycles were conflicts, with rows two apart 30 %, so none.
 #pragma once
 
 #include "recd_vec.h"
@@ -51,12 +52,12 @@ template <> struct RecdMma<float> {
 };
 
 // The tile's row (of 32) in row i of the product.
-__device__ inline int recd_tile_row(int i) { return (i & ~7) | (i & 3) << 1 | (i >> 2 & 1); }
+__device__ inline int recd_tile_row(int i) { return (i & 16) | (i & 3) << 2 | (i >> 3 & 1) << 1 | (i >> 2 & 1); }
 // The row of the product that tile row i stands in.
-__device__ inline int recd_product_row(int i) { return (i & ~7) | (i & 1) << 2 | (i >> 1 & 3); }
+__device__ inline int recd_product_row(int i) { return (i & ~15) | (i >> 1 & 1) << 3 | (i & 1) << 2 | (i >> 2 & 3); }
 // Row of the product in a sums' register, and the tile's row in a score's.
 __device__ inline int recd_sums_row(int r, int lane) { return 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3); }
-__device__ inline int recd_score_row(int r, int lane) { return 8 * (r >> 2) + 2 * (r & 3) + (lane >> 5); }
+__device__ inline int recd_score_row(int r, int lane) { return 16 * (r >> 3) + 4 * (r & 3) + 2 * (r >> 2 & 1) + (lane >> 5); }
 
 // A tile of ROWS rows of DP elements in LDS.
 template <typename T, int ROWS, int DP> struct RecdTile {
@@ -78,19 +79,19 @@ template <typename T, int ROWS, int DP> struct RecdTile {
             const T *p = at + (row0 + (lane >> 5)) * LD + d0 + (lane & 31);
 #pragma unroll
             for (int e = 0; e < 8; e++)
-                f[e] = p[(8 * (e >> 2) + 2 * (e & 3)) * LD];
+                f[e] = p[(2 * (e >> 2) + 4 * (e & 3)) * LD];
             return f;
         } else {
             // 16 lanes name four rows of 16 columns, 8 bytes each; each of them receives one column
             using Half = __attribute__((address_space(3))) recd_s16x4;
             const int i = lane & 15;
-            const T *p = at + (row0 + (lane >> 5) + 2 * (i >> 2)) * LD + d0 + 16 * ((lane >> 4) & 1) + 4 * (i & 3);
+            const T *p = at + (row0 + (lane >> 5) + 4 * (i >> 2)) * LD + d0 + 16 * ((lane >> 4) & 1) + 4 * (i & 3);
             union {
                 recd_s16x4 half[2];
                 Frag f;
             } u;
             u.half[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Half *)(p));
-            u.half[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Half *)(p + 8 * LD));
+            u.half[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Half *)(p + 2 * LD));
             return u.f;
         }
     }
