@@ -33,11 +33,14 @@ template <typename T> constexpr bool kHalf = std::is_same<T, _Float16>::value;
 template <typename T> constexpr float kLift = kHalf<T> ? 7.0f : 0.0f;
 template <typename T> constexpr float kLiftP = kHalf<T> ? 15.0f : 0.0f;
 
+constexpr int kMostSorted = 1024;  // lists whose tiles are put in the order of their work
+
 struct Args {
     int G, group, d;              // key heads, query heads of each, elements of a head
     int64_t lists, slots;
     const int2 *tiles;            // {list or -1, tile} of every slot, or null: tiles_per_list slots for every list
     int tiles_per_list, splits;
+    bool last_first;              // without a table: a list's last tiles hold the most work
     const int64_t *q_offsets, *k_offsets;
     const void *q, *k, *v, *out_in, *g;
     int64_t q_stride, k_stride, v_stride, gq_stride, gk_stride, gv_stride;
@@ -71,7 +74,7 @@ struct Problem {
 };
 
 // The block's tile: false where the slot holds none.  Slots go round the dies; the heads of a slot, whose rows share
-// cache lines, follow each other on one die; the last slots (the longest lists' ends) come first.
+// cache lines, follow each other on one die.  Without a table the lists' tiles with the most work come first.
 __device__ inline bool find_tile(const Args &a, Problem &p, int &head, int &tile, int &split)
 {
     const int64_t at = blockIdx.x >> 3;
@@ -80,7 +83,7 @@ __device__ inline bool find_tile(const Args &a, Problem &p, int &head, int &tile
     if (unit >= a.slots * a.splits)
         return false;
     split = (int)(unit % a.splits);
-    const int64_t slot = a.slots - 1 - unit / a.splits;
+    const int64_t slot = unit / a.splits;
     int64_t list;
     if (a.tiles) {
         const int2 t = a.tiles[slot];
@@ -89,8 +92,10 @@ __device__ inline bool find_tile(const Args &a, Problem &p, int &head, int &tile
         list = t.x;
         tile = t.y;
     } else {
-        list = slot / a.tiles_per_list;
-        tile = (int)(slot % a.tiles_per_list);
+        list = slot % a.lists;
+        tile = (int)(slot / a.lists);
+        if (a.last_first)
+            tile = a.tiles_per_list - 1 - tile;
     }
     p.q0 = a.q_offsets[list];
     p.k0 = a.k_offsets[list];
@@ -134,10 +139,26 @@ template <typename T, int ROWS, int DP, int THREADS> struct Stream {
     }
 };
 
-__device__ inline float tanh_of(float x)
-{
-    return 1.0f - 2.0f * __builtin_amdgcn_rcpf(1.0f + recd_exp2(x * (2.0f * kRecdLog2e)));
-}
+// cap * log2(e) * tanh(x) + more from x' = 2 log2(e) x, and a quarter of the derivative, (1 - tanh^2) / 4.
+// tanh(x) = 1 - 2 r with r = 1 / (1 + e^2x), off by 2^-23 wherever x lies.  That is enough beside 16-bit operands; for fp32
+// small x take Lambert's continued fraction, x (945 + 105 x^2 + x^4) / (945 + 420 x^2 + 15 x^4), off by 2e-9 of x at 1/2.
+template <typename T> struct Capped {
+    float cap, cap_n2;  // cap * log2(e) and -2 times that
+    __device__ inline explicit Capped(float c) : cap(c * kRecdLog2e), cap_n2(-2.0f * c * kRecdLog2e) {}
+    __device__ inline float value(float x2, float more, float &quarter) const
+    {
+        const float r = __builtin_amdgcn_rcpf(1.0f + recd_exp2(x2));
+        quarter = r - r * r;
+        if constexpr (sizeof(T) == 4) {
+            const float x = x2 * (0.5f * kRecdLn2), y = x * x;
+            float t = 1.0f - 2.0f * r;
+            if (fabsf(x) < 0.5f)
+                t = x * (945.0f + y * (105.0f + y)) / (945.0f + y * (420.0f + 15.0f * y));
+            return cap * t + more;
+        }
+        return cap_n2 * r + (cap + more);
+    }
+};
 
 template <typename T> __device__ inline void store4(T *p, float a, float b, float c, float d)
 {
@@ -157,12 +178,21 @@ template <typename T, int DT> __device__ inline void store_columns(T *row, const
         }
 }
 
-template <typename T, int DP, int NW, int BK> __global__ __launch_bounds__(64 * NW) void k_attention(Args a)
+// Waves that a SIMD is to hold at once, as far as the registers go round: two hide each other's waits and fill the
+// matrix cores and the vector units in turn.
+template <typename T, int DP, int NW> constexpr int kResident = (sizeof(T) == 4 && DP > 32) || (NW == 1 && DP > 64) ? 1 : 2;
+
+// 32 query rows a wave.  The loop is pipelined over tiles of 32 keys: one turn multiplies the next tile's scores and the
+// current one's sums while the current scores become exponentials.  The caps, biases and masks of the next scores, and
+// the check of the running maximum, stand behind it.  Three buffers in LDS make it one barrier a turn; a block of one wave
+// needs two and none.
+template <typename T, int DP, int NW, bool CAP>
+__global__ __launch_bounds__(64 * NW, (kResident<T, DP, NW>)) void k_attention(Args a)
 {
-    constexpr int KS = DP / 16, DT = DP / 32, THREADS = 64 * NW;
+    constexpr int KS = DP / 16, DT = DP / 32, THREADS = 64 * NW, BUFS = NW == 1 ? 2 : 3;
     using Mma = RecdMma<T>;
     using Frag = typename Mma::Frag;
-    __shared__ RecdTile<T, BK, DP> kt, vt;
+    __shared__ RecdTile<T, 32, DP> kt[BUFS], vt[BUFS];
     Problem p;
     int head, tile, split;
     if (!find_tile(a, p, head, tile, split))
@@ -175,93 +205,151 @@ template <typename T, int DP, int NW, int BK> __global__ __launch_bounds__(64 * 
     const bool there = row < p.rows;
     const int query = p.query(row, a.group), head_in = row - query * a.group;
     const int lim = there ? p.limit(row, a.group) : 0;
-    const int wave_end = row0 < p.rows ? p.limit(row0 + 32 < p.rows ? row0 + 31 : p.rows - 1, a.group) : 0;
+    const int wave_last = row0 + 31 < p.rows ? row0 + 31 : p.rows - 1;
+    const int wave_end = row0 < p.rows ? p.limit(wave_last, a.group) : 0;
     const int wave_full = row0 + 32 <= p.rows ? p.limit(row0, a.group) : 0;  // keys that every row sees
-    const int tiles = (p.limit(end - 1, a.group) + BK - 1) / BK;
+    const int tiles = (p.limit(end - 1, a.group) + 31) / 32;
     const int t0 = (int)((int64_t)tiles * split / a.splits), t1 = (int)((int64_t)tiles * (split + 1) / a.splits);
+    const int wave_t1 = (wave_end + 31) / 32 < t1 ? (wave_end + 31) / 32 : t1;
     const int H = a.G * a.group;
     const int64_t q_row = p.q0 + query, at_row = q_row * H + p.head0 + head_in;
     const float slope = a.slopes && there ? a.slopes[p.head0 + head_in] * kRecdLog2e : 0.0f;
     const int pos = p.pos0 + query;
-    const float c = a.scale * kRecdLog2e, cap = a.cap * kRecdLog2e, to_cap = a.cap != 0.0f ? a.scale / a.cap : 0.0f;
+    const int pos_min = p.pos0 + p.query(row0, a.group), pos_max = p.pos0 + p.query(wave_last, a.group);
+    // the sign of the scale goes into the queries; what is neither capped nor biased stays unscaled until the exponent
+    const float scale = fabsf(a.scale), c = scale * kRecdLog2e;
+    const bool plain = !CAP && !a.slopes && c > 0.0f;
+    const float by = plain ? c : 1.0f;
+    const Capped<T> capped(a.cap);
+    const float to_cap = CAP ? 2.0f * kRecdLog2e * scale / a.cap : 0.0f;
 
     Frag qf[KS];
-    for (int k = 0; k < KS; k++)
+#pragma unroll
+    for (int k = 0; k < KS; k++) {
         qf[k] = recd_row_frag<T>((const T *)a.q + q_row * a.q_stride + (int64_t)(p.head0 + head_in) * a.d, 16 * k, a.d, there,
                                  lane);
+        if (a.scale < 0.0f)
+            qf[k] = recd_negated(qf[k]);
+    }
     float m = -INFINITY, l = 0.0f;
-    recd_f32x16 o[DT];
+    recd_f32x16 o[DT], s[2];
+#pragma unroll
     for (int d = 0; d < DT; d++)
         o[d] = recd_f32x16{};
-    Stream<T, BK, DP, THREADS> ks, vs;
+    Stream<T, 32, DP, THREADS> ks, vs;
     auto load = [&](int t) {
         ks.load(a.d, [&](int r) -> const T * {
-            const int j = t * BK + r;
+            const int j = t * 32 + r;
             return j < p.nk ? (const T *)a.k + (p.k0 + j) * a.k_stride + (int64_t)head * a.d : nullptr;
         });
         vs.load(a.d, [&](int r) -> const T * {
-            const int j = t * BK + r;
+            const int j = t * 32 + r;
             return j < p.nk ? (const T *)a.v + (p.k0 + j) * a.v_stride + (int64_t)head * a.d : nullptr;
         });
     };
-    if (t0 < t1)
-        load(t0);
-    for (int t = t0; t < t1; t++) {
-        __syncthreads();
-        ks.store(kt);
-        vs.store(vt);
-        __syncthreads();
-        if (t + 1 < t1)
-            load(t + 1);
+    auto scores = [&](const RecdTile<T, 32, DP> &keys, recd_f32x16 &x) {
+        x = recd_f32x16{};
 #pragma unroll
-        for (int st = 0; st < BK / 32; st++) {
-            const int j0 = t * BK + 32 * st;
-            if (j0 >= wave_end)
-                break;
-            recd_f32x16 s = {};
+        for (int k = 0; k < KS; k++)
+            x = Mma::mul(keys.rows(0, 16 * k, lane), qf[k], x);
+    };
+    auto settle = [&](int j0, recd_f32x16 &x) {
+        if (!plain) {
+            if (!a.slopes) {
 #pragma unroll
-            for (int k = 0; k < KS; k++)
-                s = Mma::mul(kt.rows(32 * st, 16 * k, lane), qf[k], s);
-            if (a.cap != 0.0f)
-                for (int r = 0; r < 16; r++)
-                    s[r] = cap * tanh_of(s[r] * to_cap);
-            else
-                for (int r = 0; r < 16; r++)
-                    s[r] *= c;
-            if (a.slopes)
-                for (int r = 0; r < 16; r++)
-                    s[r] -= slope * fabsf((float)(pos - j0 - recd_score_row(r, lane)));
-            if (j0 + 32 > wave_full)
-                for (int r = 0; r < 16; r++)
-                    if (j0 + recd_score_row(r, lane) >= lim)
-                        s[r] = -INFINITY;
-            float top = s[0];
-            for (int r = 1; r < 16; r++)
-                top = fmaxf(top, s[r]);
-            top = fmaxf(top, __shfl_xor(top, 32)) - kLift<T>;
-            // the maximum moves only where it grows by more than 2^kSlack: the sums are rarely rescaled
-            if (__any(top > m + kSlack)) {
-                const float now = fmaxf(m, top);
-                const float f = now == m ? 1.0f : recd_exp2(m - now);
-                m = now;
-                l *= f;
-                for (int d = 0; d < DT; d++)
-                    for (int r = 0; r < 16; r++)
-                        o[d][r] *= f;
-            }
-            const float from = m == -INFINITY ? 0.0f : m;  // a row that has seen nothing yet
-            for (int r = 0; r < 16; r++) {
-                s[r] = recd_exp2(s[r] - from);
-                l += s[r];
-            }
+                for (int r = 0; r < 16; r++) {
+                    float unused;
+                    x[r] = CAP ? capped.value(x[r] * to_cap, 0.0f, unused) : x[r] * c;
+                }
+            } else if (j0 + 31 <= pos_min || j0 >= pos_max) {  // all keys on one side of all queries: the distance is linear
+                const float sl = j0 >= pos_max ? -slope : slope, at0 = sl * (float)(j0 + (lane >> 5) - pos);
 #pragma unroll
-            for (int h = 0; h < 2; h++) {
-                const Frag pf = recd_sums_frag<T>(s, h);
+                for (int r = 0; r < 16; r++) {
+                    float unused;
+                    const float bias = sl * (float)recd_score_row(r, 0) + at0;
+                    x[r] = CAP ? capped.value(x[r] * to_cap, bias, unused) : x[r] * c + bias;
+                }
+            } else {
 #pragma unroll
-                for (int d = 0; d < DT; d++)
-                    o[d] = Mma::mul(vt.columns(32 * st + 16 * h, 32 * d, lane), pf, o[d]);
+                for (int r = 0; r < 16; r++) {
+                    float unused;
+                    const float bias = -slope * fabsf((float)(pos - j0 - recd_score_row(r, lane)));
+                    x[r] = CAP ? capped.value(x[r] * to_cap, bias, unused) : x[r] * c + bias;
+                }
             }
         }
+        if (j0 + 32 > wave_full) {
+            asm volatile("");  // a branch: only the tiles at the mask's edge pay for it
+#pragma unroll
+            for (int r = 0; r < 16; r++)
+                x[r] = j0 + recd_score_row(r, lane) >= lim ? -INFINITY : x[r];
+        }
+        float top = x[0];
+#pragma unroll
+        for (int r = 1; r < 16; r++)
+            top = fmaxf(top, x[r]);
+        top = fmaxf(top, __shfl_xor(top, 32)) * by - kLift<T>;
+        // the maximum moves only where it grows by more than 2^kSlack: the sums are rarely rescaled
+        if (__any(top > m + kSlack)) {
+            const float now = fmaxf(m, top);
+            const float f = now == m ? 1.0f : recd_exp2(m - now);
+            m = now;
+            l *= f;
+#pragma unroll
+            for (int d = 0; d < DT; d++)
+#pragma unroll
+                for (int r = 0; r < 16; r++)
+                    o[d][r] *= f;
+        }
+    };
+    if (t0 < t1) {
+        load(t0);
+        ks.store(kt[0]);
+        vs.store(vt[0]);
+        if (t0 + 1 < t1)
+            load(t0 + 1);
+        __syncthreads();
+        if (t0 < wave_t1) {
+            scores(kt[0], s[0]);
+            settle(t0 * 32, s[0]);
+        }
+    }
+    int buf = 0;
+    auto turn = [&](int t, recd_f32x16 &now, recd_f32x16 &then) {
+        const int next = buf + 1 == BUFS ? 0 : buf + 1;
+        if (t + 1 < t1) {
+            ks.store(kt[next]);
+            vs.store(vt[next]);
+            if (t + 2 < t1)
+                load(t + 2);
+        }
+        __syncthreads();
+        if (t < wave_t1) {
+            scores(kt[next], then);  // (behind the wave's last tile: of what lies there, for nobody)
+            const float from = m == -INFINITY ? 0.0f : m;  // a row that has seen nothing yet
+            float sum = 0.0f;
+#pragma unroll
+            for (int r = 0; r < 16; r++) {
+                now[r] = recd_exp2(now[r] * by - from);
+                sum += now[r];
+            }
+            l += sum;
+#pragma unroll
+            for (int h = 0; h < 2; h++) {
+                const Frag pf = recd_sums_frag<T>(now, h);
+#pragma unroll
+                for (int d = 0; d < DT; d++)
+                    o[d] = Mma::mul(vt[buf].columns(16 * h, 32 * d, lane), pf, o[d]);
+            }
+            if (t + 1 < wave_t1)
+                settle((t + 1) * 32, then);
+        }
+        buf = next;
+    };
+    for (int t = t0; t < t1; t += 2) {
+        turn(t, s[0], s[1]);
+        if (t + 1 < t1)
+            turn(t + 1, s[1], s[0]);
     }
     l += __shfl_xor(l, 32);
     if (!there)
@@ -323,6 +411,75 @@ __global__ void k_attention_tiles(int64_t lists, int64_t slots, int group, int R
         tiles[s] = s - s0 < n ? make_int2((int)list, (int)(s - s0)) : make_int2(-1, 0);
 }
 
+// The same for few lists (one block), in the order of the tiles' work, most first: lists of a few very different lengths
+// would otherwise leave most compute units to wait for the last long one.  `keys`: the tiles are of keys.  Tiles of
+// about equal work stand in any order.
+__global__ __launch_bounds__(1024) void k_attention_tiles_by_work(int lists, int slots, int group, int R, bool keys, bool causal,
+                                                                  const int64_t *__restrict__ q_offsets,
+                                                                  const int64_t *__restrict__ k_offsets,
+                                                                  const int32_t *__restrict__ prefix, int2 *tiles)
+{
+    __shared__ int nq[kMostSorted], nk[kMostSorted], pre[kMostSorted], count[256], most, total;
+    if (threadIdx.x < 256)
+        count[threadIdx.x] = 0;
+    if (threadIdx.x == 0)
+        most = 1;
+    __syncthreads();
+    int top = 1;
+    for (int l = threadIdx.x; l < lists; l += 1024) {
+        nq[l] = (int)(q_offsets[l + 1] - q_offsets[l]);
+        nk[l] = (int)(k_offsets[l + 1] - k_offsets[l]);
+        pre[l] = prefix ? prefix[l] : 0;
+        const int n = keys ? nq[l] : nk[l];
+        top = n > top ? n : top;
+    }
+    atomicMax(&most, top);
+    __syncthreads();
+    // rows (of queries or keys) that tile i of list l goes through, in 256ths of the longest list's
+    auto bucket = [&](int l, int i) {
+        int64_t work;
+        if (keys) {
+            const int first = i * R, pos0 = nk[l] - nq[l];
+            work = causal && pre[l] <= first && first > pos0 ? nq[l] - (first - pos0) : nq[l];
+        } else {
+            int64_t last = (int64_t)(i + 1) * R / group;
+            last = last < nq[l] ? last : nq[l];
+            int64_t end = nk[l] - nq[l] + last;
+            end = end > pre[l] ? end : pre[l];
+            work = causal && end < nk[l] ? end : nk[l];
+        }
+        work = work < 0 ? 0 : work;
+        return 255 - (int)(work * 255 / most);
+    };
+    const int lane = threadIdx.x & 31;
+    for (int l = threadIdx.x >> 5; l < lists; l += 32) {
+        const int n = ((keys ? nk[l] : nq[l] * group) + R - 1) / R;
+        for (int i = lane; i < n; i += 32)
+            atomicAdd(&count[bucket(l, i)], 1);
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        int at = 0;
+        for (int b = 0; b < 256; b++) {
+            const int n = count[b];
+            count[b] = at;
+            at += n;
+        }
+        total = at;
+    }
+    __syncthreads();
+    for (int l = threadIdx.x >> 5; l < lists; l += 32) {
+        const int n = ((keys ? nk[l] : nq[l] * group) + R - 1) / R;
+        for (int i = lane; i < n; i += 32) {
+            const int at = atomicAdd(&count[bucket(l, i)], 1);
+            if (at < slots)
+                tiles[at] = make_int2(l, i);
+        }
+    }
+    for (int s = total + threadIdx.x; s < slots; s += 1024)
+        tiles[s] = make_int2(-1, 0);
+}
+
 // delta = sum over a head of g * o: 2^dlog lanes a row, a piece of 16 bytes each.
 template <typename T>
 __global__ __launch_bounds__(256) void k_attention_delta(int64_t rows, int d, int dlog, const T *__restrict__ out,
@@ -380,33 +537,14 @@ __global__ void k_attention_lift(int d, const uint32_t *tops, float *lift)
     *lift = ldexpf(1.0f, e > 60 ? 60 : e);
 }
 
-// p and, over sums, ds without the scale, of one score: z = scale * q . k and dp = g . v
-struct Score {
-    float p, ds;
-};
-__device__ inline Score score_of(const Args &a, float qk, float dp, float from, float delta, float slope, int far, bool sees)
+// 32 query rows a wave, keys and values stream past.
+template <typename T, int DP, int NW, bool CAP>
+__global__ __launch_bounds__(64 * NW, (kResident<T, DP, NW>)) void k_attention_grad_q(Args a)
 {
-    float z, t = 0.0f;
-    if (a.cap != 0.0f) {
-        t = tanh_of(qk * (a.scale / a.cap));
-        z = a.cap * kRecdLog2e * t;
-    } else
-        z = qk * (a.scale * kRecdLog2e);
-    if (a.slopes)
-        z -= slope * fabsf((float)far);
-    const float p = sees ? recd_exp2(z - from) : 0.0f;
-    float ds = sees ? p * (dp - delta) : 0.0f;
-    if (a.cap != 0.0f)
-        ds *= 1.0f - t * t;
-    return {p, ds};
-}
-
-template <typename T, int DP, int NW, int BK> __global__ __launch_bounds__(64 * NW) void k_attention_grad_q(Args a)
-{
-    constexpr int KS = DP / 16, DT = DP / 32, THREADS = 64 * NW;
+    constexpr int KS = DP / 16, DT = DP / 32, THREADS = 64 * NW, BUFS = NW == 1 ? 1 : 2;
     using Mma = RecdMma<T>;
     using Frag = typename Mma::Frag;
-    __shared__ RecdTile<T, BK, DP> kt, vt;
+    __shared__ RecdTile<T, 32, DP> kt[BUFS], vt[BUFS];
     Problem p;
     int head, tile, split;
     if (!find_tile(a, p, head, tile, split))
@@ -419,84 +557,109 @@ template <typename T, int DP, int NW, int BK> __global__ __launch_bounds__(64 * 
     const bool there = row < p.rows;
     const int query = p.query(row, a.group), head_in = row - query * a.group;
     const int lim = there ? p.limit(row, a.group) : 0;
-    const int wave_end = row0 < p.rows ? p.limit(row0 + 32 < p.rows ? row0 + 31 : p.rows - 1, a.group) : 0;
-    const int tiles = (p.limit(end - 1, a.group) + BK - 1) / BK;
+    const int wave_last = row0 + 31 < p.rows ? row0 + 31 : p.rows - 1;
+    const int wave_end = row0 < p.rows ? p.limit(wave_last, a.group) : 0;
+    const int wave_full = row0 + 32 <= p.rows ? p.limit(row0, a.group) : 0;
+    const int tiles = (p.limit(end - 1, a.group) + 31) / 32;
     const int H = a.G * a.group;
     const int64_t q_row = p.q0 + query, at_row = q_row * H + p.head0 + head_in;
     const float slope = a.slopes && there ? a.slopes[p.head0 + head_in] * kRecdLog2e : 0.0f;
     const int pos = p.pos0 + query;
+    const int pos_min = p.pos0 + p.query(row0, a.group), pos_max = p.pos0 + p.query(wave_last, a.group);
     float from = there ? a.lse_in[at_row] * kRecdLog2e : 0.0f;
-    const float delta = there ? a.delta[at_row] : 0.0f;
     if (from == -INFINITY)
         from = 0.0f;  // sees nothing
-    const float lift = kHalf<T> ? *a.lift : 1.0f;
+    const float lift = kHalf<T> ? *a.lift : 1.0f, delta = there ? a.delta[at_row] * lift : 0.0f;
+    const float c = a.scale * kRecdLog2e;
+    const Capped<T> capped(a.cap);
+    const float to_cap = CAP ? 2.0f * kRecdLog2e * a.scale / a.cap : 0.0f;
 
     Frag qf[KS], gf[KS];
+#pragma unroll
     for (int k = 0; k < KS; k++) {
         qf[k] = recd_row_frag<T>((const T *)a.q + q_row * a.q_stride + (int64_t)(p.head0 + head_in) * a.d, 16 * k, a.d, there,
                                  lane);
         gf[k] = recd_row_frag<T>((const T *)a.g + at_row * a.d, 16 * k, a.d, there, lane);
     }
     recd_f32x16 o[DT];
+#pragma unroll
     for (int d = 0; d < DT; d++)
         o[d] = recd_f32x16{};
-    Stream<T, BK, DP, THREADS> ks, vs;
+    Stream<T, 32, DP, THREADS> ks, vs;
     auto load = [&](int t) {
         ks.load(a.d, [&](int r) -> const T * {
-            const int j = t * BK + r;
+            const int j = t * 32 + r;
             return j < p.nk ? (const T *)a.k + (p.k0 + j) * a.k_stride + (int64_t)head * a.d : nullptr;
         });
         vs.load(a.d, [&](int r) -> const T * {
-            const int j = t * BK + r;
+            const int j = t * 32 + r;
             return j < p.nk ? (const T *)a.v + (p.k0 + j) * a.v_stride + (int64_t)head * a.d : nullptr;
         });
     };
     if (tiles > 0)
         load(0);
     for (int t = 0; t < tiles; t++) {
-        __syncthreads();
-        ks.store(kt);
-        vs.store(vt);
+        const int buf = BUFS == 1 ? 0 : t & 1;
+        ks.store(kt[buf]);
+        vs.store(vt[buf]);
         __syncthreads();
         if (t + 1 < tiles)
             load(t + 1);
+        const int j0 = t * 32;
+        if (j0 >= wave_end)
+            continue;
+        recd_f32x16 s = {}, dp = {};
 #pragma unroll
-        for (int st = 0; st < BK / 32; st++) {
-            const int j0 = t * BK + 32 * st;
-            if (j0 >= wave_end)
-                break;
-            recd_f32x16 s = {}, dp = {};
+        for (int k = 0; k < KS; k++) {
+            s = Mma::mul(kt[buf].rows(0, 16 * k, lane), qf[k], s);
+            dp = Mma::mul(vt[buf].rows(0, 16 * k, lane), gf[k], dp);
+        }
+        // the exponent's argument without the bias's distance, then p, then ds
+        auto ds_of = [&](float x, float d, float bias) {
+            float quarter = 1.0f;
+            const float z = CAP ? capped.value(x * to_cap, bias, quarter) : x * c + bias;
+            return recd_exp2(z) * (d * lift - delta) * quarter;
+        };
+        if (j0 + 32 <= wave_full && (!a.slopes || j0 + 31 <= pos_min || j0 >= pos_max)) {
+            const float sl = j0 >= pos_max ? -slope : slope, at0 = sl * (float)(j0 + (lane >> 5) - pos) - from;
 #pragma unroll
-            for (int k = 0; k < KS; k++) {
-                s = Mma::mul(kt.rows(32 * st, 16 * k, lane), qf[k], s);
-                dp = Mma::mul(vt.rows(32 * st, 16 * k, lane), gf[k], dp);
-            }
+            for (int r = 0; r < 16; r++)
+                s[r] = ds_of(s[r], dp[r], a.slopes ? sl * (float)recd_score_row(r, 0) + at0 : at0);
+        } else {
+#pragma unroll
             for (int r = 0; r < 16; r++) {
                 const int j = j0 + recd_score_row(r, lane);
-                s[r] = score_of(a, s[r], dp[r], from, delta, slope, pos - j, j < lim).ds * lift;
+                const float x = ds_of(s[r], dp[r], -slope * fabsf((float)(pos - j)) - from);
+                s[r] = j < lim ? x : 0.0f;
             }
+        }
 #pragma unroll
-            for (int h = 0; h < 2; h++) {
-                const Frag sf = recd_sums_frag<T>(s, h);
+        for (int h = 0; h < 2; h++) {
+            const Frag sf = recd_sums_frag<T>(s, h);
 #pragma unroll
-                for (int d = 0; d < DT; d++)
-                    o[d] = Mma::mul(kt.columns(32 * st + 16 * h, 32 * d, lane), sf, o[d]);
-            }
+            for (int d = 0; d < DT; d++)
+                o[d] = Mma::mul(kt[buf].columns(16 * h, 32 * d, lane), sf, o[d]);
         }
     }
     if (there)
-        store_columns<T, DT>((T *)a.gq + q_row * a.gq_stride + (int64_t)(p.head0 + head_in) * a.d, o, a.scale / lift, a.d, lane);
+        store_columns<T, DT>((T *)a.gq + q_row * a.gq_stride + (int64_t)(p.head0 + head_in) * a.d, o,
+                             (CAP ? 4.0f : 1.0f) * a.scale / lift, a.d, lane);
 }
 
-// Keys stay, queries and their gradients stream past.
-template <typename T, int DP, int NW, int BQ> __global__ __launch_bounds__(64 * NW) void k_attention_grad_kv(Args a)
+// Keys stay, queries and their gradients stream past.  What a score needs of its row stands in LDS in the order of
+// the sums' registers: four neighbours are read at a time.
+template <typename T, int DP, int NW, bool CAP>
+__global__ __launch_bounds__(64 * NW, (kResident<T, DP, NW>)) void k_attention_grad_kv(Args a)
 {
-    constexpr int KS = DP / 16, DT = DP / 32, THREADS = 64 * NW;
+    constexpr int KS = DP / 16, DT = DP / 32, THREADS = 64 * NW, BUFS = NW == 1 ? 1 : 2;
     using Mma = RecdMma<T>;
     using Frag = typename Mma::Frag;
-    __shared__ RecdTile<T, BQ, DP> qt, gt;
-    __shared__ alignas(16) float row_from[BQ], row_delta[BQ], row_slope[BQ];
-    __shared__ alignas(16) int row_lim[BQ], row_pos[BQ];
+    // Wide 16-bit heads: the kept keys' values stay in LDS, as the registers hold two sums of the head's width besides.
+    constexpr bool VALUES = sizeof(T) == 2 && DP > 64 && NW > 1;
+    __shared__ RecdTile<T, 32, DP> qt[BUFS], gt[BUFS];
+    __shared__ RecdTile<T, VALUES ? 32 * NW : 1, DP> values;
+    __shared__ alignas(16) float row_from[BUFS][32], row_delta[BUFS][32], row_slope[BUFS][32];
+    __shared__ alignas(16) int row_lim[BUFS][32], row_pos[BUFS][32];
     Problem p;
     int head, tile, split;
     if (!find_tile(a, p, head, tile, split))
@@ -508,21 +671,31 @@ template <typename T, int DP, int NW, int BQ> __global__ __launch_bounds__(64 * 
     const int j0 = first + 32 * wave, j = j0 + (lane & 31);
     const bool there = j < p.nk;
     const int H = a.G * a.group;
-    Frag kf[KS], vf[KS];
+    Frag kf[KS], vf[VALUES ? 1 : KS];
+    T *const value = values.at + (VALUES ? (32 * wave + (lane & 31)) * values.LD + (lane >> 5) * 8 : 0);
+#pragma unroll
     for (int k = 0; k < KS; k++) {
         kf[k] = recd_row_frag<T>((const T *)a.k + (p.k0 + j) * a.k_stride + (int64_t)head * a.d, 16 * k, a.d, there, lane);
-        vf[k] = recd_row_frag<T>((const T *)a.v + (p.k0 + j) * a.v_stride + (int64_t)head * a.d, 16 * k, a.d, there, lane);
+        vf[VALUES ? 0 : k] = recd_row_frag<T>((const T *)a.v + (p.k0 + j) * a.v_stride + (int64_t)head * a.d, 16 * k, a.d, there,
+                                              lane);
+        if constexpr (VALUES)
+            *reinterpret_cast<Frag *>(value + 16 * k) = vf[0];  // read by this lane alone
     }
     recd_f32x16 dk[DT], dv[DT];
+#pragma unroll
     for (int d = 0; d < DT; d++)
         dk[d] = dv[d] = recd_f32x16{};
-    const float lift = kHalf<T> ? *a.lift : 1.0f, lift_p = recd_exp2(kLiftP<T>);
+    // probabilities are held 2^kLiftP larger, by their exponents; ds by that and, from dp on, the rest of its lift
+    const float lift = kHalf<T> ? *a.lift : 1.0f, lift_dp = lift * recd_exp2(-kLiftP<T>);
+    const float c = a.scale * kRecdLog2e;
+    const Capped<T> capped(a.cap);
+    const float to_cap = CAP ? 2.0f * kRecdLog2e * a.scale / a.cap : 0.0f;
     // the first row that sees the block's first key
     int from_row = 0;
     if (p.causal && p.prefix <= first && first > p.pos0)
         from_row = (int)((int64_t)(first - p.pos0) * a.group < p.rows ? (first - p.pos0) * a.group : p.rows);
-    const int tiles = (p.rows + BQ - 1) / BQ;
-    Stream<T, BQ, DP, THREADS> qs, gs;
+    const int tiles = (p.rows + 31) / 32;
+    Stream<T, 32, DP, THREADS> qs, gs;
     float n_from = 0.0f, n_delta = 0.0f, n_slope = 0.0f;
     int n_lim = 0, n_pos = 0;
     auto load = [&](int t) {
@@ -532,81 +705,110 @@ template <typename T, int DP, int NW, int BQ> __global__ __launch_bounds__(64 * 
         };
         qs.load(a.d, [&](int r) -> const T * {
             int query, h;
-            at(t * BQ + r, query, h);
-            return t * BQ + r < p.rows ? (const T *)a.q + (p.q0 + query) * a.q_stride + (int64_t)h * a.d : nullptr;
+            at(t * 32 + r, query, h);
+            return t * 32 + r < p.rows ? (const T *)a.q + (p.q0 + query) * a.q_stride + (int64_t)h * a.d : nullptr;
         });
         gs.load(a.d, [&](int r) -> const T * {
             int query, h;
-            at(t * BQ + r, query, h);
-            return t * BQ + r < p.rows ? (const T *)a.g + ((p.q0 + query) * H + h) * a.d : nullptr;
+            at(t * 32 + r, query, h);
+            return t * 32 + r < p.rows ? (const T *)a.g + ((p.q0 + query) * H + h) * a.d : nullptr;
         });
-        const int r = t * BQ + threadIdx.x;
+        const int r = t * 32 + threadIdx.x;
         n_from = n_delta = n_slope = 0.0f;
         n_lim = n_pos = 0;
-        if (threadIdx.x < BQ && r < p.rows) {
+        if (threadIdx.x < 32 && r < p.rows) {
             int query, h;
             at(r, query, h);
             n_from = a.lse_in[(p.q0 + query) * H + h] * kRecdLog2e;
-            if (n_from == -INFINITY)
-                n_from = 0.0f;
-            n_delta = a.delta[(p.q0 + query) * H + h];
+            n_from = (n_from == -INFINITY ? 0.0f : -n_from) + kLiftP<T>;
+            n_delta = a.delta[(p.q0 + query) * H + h] * lift_dp;
             n_slope = a.slopes ? a.slopes[h] * kRecdLog2e : 0.0f;
             n_lim = p.limit(r, a.group);
             n_pos = p.pos0 + query;
         }
     };
-    const int t0 = from_row / BQ;
+    const int t0 = from_row / 32;
     if (t0 < tiles)
         load(t0);
     for (int t = t0; t < tiles; t++) {
-        __syncthreads();
-        qs.store(qt);
-        gs.store(gt);
-        if (threadIdx.x < BQ) {
-            row_from[threadIdx.x] = n_from;
-            row_delta[threadIdx.x] = n_delta;
-            row_slope[threadIdx.x] = n_slope;
-            row_lim[threadIdx.x] = n_lim;
-            row_pos[threadIdx.x] = n_pos;
+        const int buf = BUFS == 1 ? 0 : t & 1;
+        qs.store(qt[buf]);
+        gs.store(gt[buf]);
+        if (threadIdx.x < 32) {
+            const int i = recd_product_row(threadIdx.x);
+            row_from[buf][i] = n_from;
+            row_delta[buf][i] = n_delta;
+            row_slope[buf][i] = n_slope;
+            row_lim[buf][i] = n_lim;
+            row_pos[buf][i] = n_pos;
         }
         __syncthreads();
         if (t + 1 < tiles)
             load(t + 1);
-        if (j0 >= p.nk)
+        const bool whole = t * 32 + 32 <= p.rows;
+        // (tile rows 0 and 31 are the product's rows 0 and 31, and limits and positions do not fall)
+        if (j0 >= p.nk || (whole && row_lim[buf][31] <= j0))
             continue;
+        recd_f32x16 s = {}, dp = {};
 #pragma unroll
-        for (int st = 0; st < BQ / 32; st++) {
-            if (row_lim[32 * st + 31] <= j0 && t * BQ + 32 * st + 32 <= p.rows)
-                continue;  // no row sees the wave's keys
-            recd_f32x16 s = {}, dp = {};
+        for (int k = 0; k < KS; k++) {
+            s = Mma::mul(qt[buf].rows(0, 16 * k, lane), kf[k], s);
+            if constexpr (VALUES)
+                dp = Mma::mul(gt[buf].rows(0, 16 * k, lane), *reinterpret_cast<const Frag *>(value + 16 * k), dp);
+            else
+                dp = Mma::mul(gt[buf].rows(0, 16 * k, lane), vf[k], dp);
+        }
+        auto scored = [&](int r, float x, float d, float bias, float delta) {
+            float quarter = 1.0f;
+            const float z = CAP ? capped.value(x * to_cap, bias, quarter) : x * c + bias;
+            s[r] = recd_exp2(z);
+            dp[r] = s[r] * (d * lift_dp - delta) * quarter;
+        };
+        const bool below = whole && j0 + 31 <= row_pos[buf][0], above = whole && j0 >= row_pos[buf][31];
+        const bool seen = whole && j0 + 32 <= row_lim[buf][0];
+        if (seen && (!a.slopes || below || above)) {
+            const float jf = (float)(below ? j : -j), sign = below ? -1.0f : 1.0f;
 #pragma unroll
-            for (int k = 0; k < KS; k++) {
-                s = Mma::mul(qt.rows(32 * st, 16 * k, lane), kf[k], s);
-                dp = Mma::mul(gt.rows(32 * st, 16 * k, lane), vf[k], dp);
+            for (int r = 0; r < 16; r += 4) {
+                const int row = recd_sums_row(r, lane);
+                const recd_f32x4 from = *reinterpret_cast<const recd_f32x4 *>(&row_from[buf][row]);
+                const recd_f32x4 delta = *reinterpret_cast<const recd_f32x4 *>(&row_delta[buf][row]);
+                if (a.slopes) {
+                    const recd_f32x4 sl = *reinterpret_cast<const recd_f32x4 *>(&row_slope[buf][row]);
+#pragma unroll
+                    for (int q = 0; q < 4; q++)
+                        scored(r + q, s[r + q], dp[r + q], from[q] + sl[q] * (jf + sign * (float)row_pos[buf][row + q]), delta[q]);
+                } else {
+#pragma unroll
+                    for (int q = 0; q < 4; q++)
+                        scored(r + q, s[r + q], dp[r + q], from[q], delta[q]);
+                }
             }
+        } else {
 #pragma unroll
             for (int r = 0; r < 16; r++) {
-                const int row = 32 * st + recd_score_row(r, lane);
-                const Score x = score_of(a, s[r], dp[r], row_from[row], row_delta[row], row_slope[row], row_pos[row] - j,
-                                         j < row_lim[row]);
-                s[r] = x.p * lift_p;
-                dp[r] = x.ds * lift;
+                const int row = recd_sums_row(r, lane);
+                scored(r, s[r], dp[r], row_from[buf][row] - row_slope[buf][row] * fabsf((float)(row_pos[buf][row] - j)),
+                       row_delta[buf][row]);
+                if (j >= row_lim[buf][row])
+                    s[r] = dp[r] = 0.0f;
             }
+        }
 #pragma unroll
-            for (int h = 0; h < 2; h++) {
-                const Frag pf = recd_sums_frag<T>(s, h), sf = recd_sums_frag<T>(dp, h);
+        for (int h = 0; h < 2; h++) {
+            const Frag pf = recd_sums_frag<T>(s, h), sf = recd_sums_frag<T>(dp, h);
 #pragma unroll
-                for (int d = 0; d < DT; d++) {
-                    dv[d] = Mma::mul(gt.columns(32 * st + 16 * h, 32 * d, lane), pf, dv[d]);
-                    dk[d] = Mma::mul(qt.columns(32 * st + 16 * h, 32 * d, lane), sf, dk[d]);
-                }
+            for (int d = 0; d < DT; d++) {
+                dv[d] = Mma::mul(gt[buf].columns(16 * h, 32 * d, lane), pf, dv[d]);
+                dk[d] = Mma::mul(qt[buf].columns(16 * h, 32 * d, lane), sf, dk[d]);
             }
         }
     }
     if (!there)
         return;
-    store_columns<T, DT>((T *)a.gk + (p.k0 + j) * a.gk_stride + (int64_t)head * a.d, dk, a.scale / lift, a.d, lane);
-    store_columns<T, DT>((T *)a.gv + (p.k0 + j) * a.gv_stride + (int64_t)head * a.d, dv, 1.0f / lift_p, a.d, lane);
+    store_columns<T, DT>((T *)a.gk + (p.k0 + j) * a.gk_stride + (int64_t)head * a.d, dk, (CAP ? 4.0f : 1.0f) * a.scale / lift, a.d,
+                         lane);
+    store_columns<T, DT>((T *)a.gv + (p.k0 + j) * a.gv_stride + (int64_t)head * a.d, dv, recd_exp2(-kLiftP<T>), a.d, lane);
 }
 
 // Offsets that do not rise from 0 to the number of rows, or pass the caller's bound of a list's length.
@@ -697,6 +899,7 @@ Args common_args(const recd_attention *d, const void *q, const void *k, const vo
     a.prefix = d->prefix;
     a.causal = d->causal != 0;
     a.part_rows = d->q_rows * d->heads;
+    a.last_first = true;
     return a;
 }
 
@@ -710,7 +913,7 @@ struct Tiling {
 Tiling tiling(const recd_attention *d, int64_t rows, int64_t most, int group)
 {
     Tiling t;
-    t.waves = most * group <= 64 ? 1 : 4;
+    t.waves = most * group <= 64 || rows * group <= 48 * d->lists ? 1 : 4;
     const int64_t R = 32 * t.waves, per = (most * group + R - 1) / R;
     t.slots = rows * group / R + d->lists;
     t.table = d->lists * per > t.slots;
@@ -732,16 +935,23 @@ unsigned grid_of(const Args &a) { return (unsigned)((a.slots * a.splits + 7) / 8
 
 enum Which { FORWARD, GRAD_Q, GRAD_KV };
 
-template <typename T, int DP, int NW> void launch_one(Which w, const Args &a, hipStream_t st)
+template <typename T, int DP, int NW, bool CAP> void launch_one(Which w, const Args &a, hipStream_t st)
 {
-    constexpr int B = sizeof(T) == 4 || NW == 1 ? 32 : 64;  // streamed rows of a tile
     const dim3 grid(grid_of(a)), block(64 * NW);
     if (w == FORWARD)
-        hipLaunchKernelGGL((k_attention<T, DP, NW, B>), grid, block, 0, st, a);
+        hipLaunchKernelGGL((k_attention<T, DP, NW, CAP>), grid, block, 0, st, a);
     else if (w == GRAD_Q)
-        hipLaunchKernelGGL((k_attention_grad_q<T, DP, NW, B>), grid, block, 0, st, a);
+        hipLaunchKernelGGL((k_attention_grad_q<T, DP, NW, CAP>), grid, block, 0, st, a);
     else
-        hipLaunchKernelGGL((k_attention_grad_kv<T, DP, NW, 32>), grid, block, 0, st, a);
+        hipLaunchKernelGGL((k_attention_grad_kv<T, DP, NW, CAP>), grid, block, 0, st, a);
+}
+
+template <typename T, int DP> void launch_width(Which w, const Args &a, int waves, hipStream_t st)
+{
+    if (a.cap != 0.0f)
+        waves == 1 ? launch_one<T, DP, 1, true>(w, a, st) : launch_one<T, DP, 4, true>(w, a, st);
+    else
+        waves == 1 ? launch_one<T, DP, 1, false>(w, a, st) : launch_one<T, DP, 4, false>(w, a, st);
 }
 
 template <typename T> void launch(Which w, const Args &a, int waves, hipStream_t st)
@@ -749,18 +959,21 @@ template <typename T> void launch(Which w, const Args &a, int waves, hipStream_t
     if (a.slots * a.splits == 0)
         return;
     if (a.d <= 32)
-        waves == 1 ? launch_one<T, 32, 1>(w, a, st) : launch_one<T, 32, 4>(w, a, st);
+        launch_width<T, 32>(w, a, waves, st);
     else if (a.d <= 64)
-        waves == 1 ? launch_one<T, 64, 1>(w, a, st) : launch_one<T, 64, 4>(w, a, st);
+        launch_width<T, 64>(w, a, waves, st);
     else
-        waves == 1 ? launch_one<T, 128, 1>(w, a, st) : launch_one<T, 128, 4>(w, a, st);
+        launch_width<T, 128>(w, a, waves, st);
 }
 
-void launch_tiles(const recd_attention *d, const Tiling &t, int group, const int64_t *offsets, int2 *tiles, hipStream_t st)
+void launch_tiles(const recd_attention *d, const Tiling &t, int group, bool keys, int2 *tiles, hipStream_t st)
 {
-    if (t.table)
+    if (t.table && d->lists <= kMostSorted && t.slots < ((int64_t)1 << 30))
+        hipLaunchKernelGGL(k_attention_tiles_by_work, dim3(1), dim3(1024), 0, st, (int)d->lists, (int)t.slots, group, 32 * t.waves,
+                           keys, d->causal != 0, d->q_offsets, d->k_offsets, d->prefix, tiles);
+    else if (t.table)
         hipLaunchKernelGGL(k_attention_tiles, dim3((unsigned)((d->lists + 255) / 256)), dim3(256), 0, st, d->lists, t.slots, group,
-                           32 * t.waves, offsets, tiles);
+                           32 * t.waves, keys ? d->k_offsets : d->q_offsets, tiles);
 }
 
 } // namespace
@@ -810,7 +1023,7 @@ recd_status recd_list_attention(recd_ctx *ctx, const recd_attention *d, const vo
     WsCarver c(ctx->ws);
     carve(c);
     a.tiles = tiles;
-    launch_tiles(d, t, a.group, d->q_offsets, tiles, ctx->stream);
+    launch_tiles(d, t, a.group, false, tiles, ctx->stream);
     recd_with_type(d->dtype, [&](auto e) {
         using T = decltype(e);
         launch<T>(FORWARD, a, t.waves, ctx->stream);
@@ -885,8 +1098,8 @@ recd_status recd_list_attention_backward(recd_ctx *ctx, const recd_attention *d,
                                (const _Float16 *)v, tops + 1);
         hipLaunchKernelGGL(k_attention_lift, dim3(1), dim3(1), 0, st, a.d, tops, lift);
     }
-    launch_tiles(d, tq, a.group, d->q_offsets, tiles_q, st);
-    launch_tiles(d, tk, 1, d->k_offsets, tiles_k, st);
+    launch_tiles(d, tq, a.group, false, tiles_q, st);
+    launch_tiles(d, tk, 1, true, tiles_k, st);
     recd_with_type(d->dtype, [&](auto e) {
         using T = decltype(e);
         const int dlog = log2_of(a.d * (int)sizeof(T) / 16);
@@ -899,6 +1112,7 @@ recd_status recd_list_attention_backward(recd_ctx *ctx, const recd_attention *d,
             launch<T>(GRAD_Q, a, tq.waves, st);
         }
         a.tiles = tiles_k;
+        a.last_first = false;
         a.slots = tk.slots;
         a.tiles_per_list = tk.tiles_per_list;
         if (d->k_rows)

@@ -120,6 +120,14 @@ template <typename T> __device__ inline typename RecdMma<T>::Frag recd_row_frag(
     return u.f;
 }
 
+template <typename Frag> __device__ inline Frag recd_negated(Frag f)
+{
+#pragma unroll
+    for (int e = 0; e < 8; e++)
+        f[e] = -f[e];
+    return f;
+}
+
 // Sums' registers 8m .. 8m + 7 as the B operand of a product over streamed rows.
 template <typename T> __device__ inline typename RecdMma<T>::Frag recd_sums_frag(const recd_f32x16 &s, int m)
 {

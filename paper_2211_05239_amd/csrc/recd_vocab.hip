@@ -57,13 +57,6 @@ template <typename T, int ROWS, int DP, int THREADS = kBlock> struct Stream {
     }
 };
 
-template <typename Frag> __device__ inline Frag negated(Frag f)
-{
-    for (int e = 0; e < 8; e++)
-        f[e] = -f[e];
-    return f;
-}
-
 // Tiles of 32 kept rows in a wave, and waves in a block.
 template <typename T, int DP> constexpr int kTiles = 1;
 template <typename T, int DP> constexpr int kManyWaves = sizeof(T) == 4 ? 4 : 8;
@@ -104,7 +97,7 @@ template <typename T, int DP, int N, bool MEAN> __global__ __launch_bounds__(kBl
         for (int k = 0; k < KS; k++) {
             xf[j][k] = recd_row_frag<T>((const T *)a.x + row * a.D, 16 * k, a.D, row < a.n, lane);
             if (a.negative)
-                xf[j][k] = negated(xf[j][k]);
+                xf[j][k] = recd_negated(xf[j][k]);
         }
     }
     float m[N], l[N];
@@ -235,7 +228,7 @@ __global__ __launch_bounds__(64 * W) void k_vocab_forward(ForwardArgs a)
         for (int k = 0; k < KS; k++) {
             xf[j][k] = recd_row_frag<T>((const T *)a.x + row * a.D, 16 * k, a.D, row < a.n, lane);
             if (a.negative)
-                xf[j][k] = negated(xf[j][k]);
+                xf[j][k] = recd_negated(xf[j][k]);
         }
     }
     float m[N], l[N];
@@ -543,7 +536,7 @@ template <typename T, int DP, int N, int W> __global__ __launch_bounds__(64 * W)
         for (int k = 0; k < KS; k++) {
             wf[j][k] = recd_row_frag<T>((const T *)a.table + v * a.D, 16 * k, a.D, v < a.V, lane);
             if (a.negative)
-                wf[j][k] = negated(wf[j][k]);
+                wf[j][k] = recd_negated(wf[j][k]);
         }
 #pragma unroll
         for (int d = 0; d < DT; d++)
