@@ -109,19 +109,20 @@ __device__ inline bool find_tile(const Args &a, Problem &p, int &head, int &tile
     return true;
 }
 
-// Rows of a tile from memory into registers and on into LDS; row(r) gives the address of row r, or null.
+// Rows of a tile from memory into registers and on into LDS, by THREADS threads of which this is `tid`; row(r) gives the
+// address of row r, or null.
 template <typename T, int ROWS, int DP, int THREADS> struct Stream {
     using Tile = RecdTile<T, ROWS, DP>;
     using Piece = typename Tile::Piece;
     static constexpr int PT = (Tile::PIECES + THREADS - 1) / THREADS;
     Piece held[PT];
 
-    template <typename Row> __device__ inline void load(int d, Row row)
+    template <typename Row> __device__ inline void load(int tid, int d, Row row)
     {
         constexpr int PR = DP / Tile::E;
 #pragma unroll
         for (int i = 0; i < PT; i++) {
-            const int piece = threadIdx.x + i * THREADS, at = piece % PR * Tile::E;
+            const int piece = tid + i * THREADS, at = piece % PR * Tile::E;
             held[i] = Piece{};
             if (piece < Tile::PIECES && at < d) {
                 const T *p = row(piece / PR);
@@ -130,14 +131,58 @@ template <typename T, int ROWS, int DP, int THREADS> struct Stream {
             }
         }
     }
-    __device__ inline void store(Tile &t)
+    __device__ inline void store(int tid, Tile &t)
     {
 #pragma unroll
         for (int i = 0; i < PT; i++)
-            if (threadIdx.x + i * THREADS < (unsigned)Tile::PIECES)
-                t.put(threadIdx.x + i * THREADS, held[i]);
+            if (tid + i * THREADS < Tile::PIECES)
+                t.put(tid + i * THREADS, held[i]);
     }
 };
+
+// How a block's waves divide a tile: KEPT groups of 32 kept rows, times PHASES that divide the streamed rows and whose
+// sums are joined at the end.  With one group every wave streams tiles of its own and waits for nobody; with several, the
+// block streams tiles of 32 * PHASES rows that all groups read.
+template <typename T, int DP, int KEPT, int PHASES> struct Shape {
+    static constexpr bool SHARED = KEPT > 1;
+    static constexpr int ROWS = SHARED ? 32 * PHASES : 32, LOADERS = SHARED ? 64 * KEPT * PHASES : 64;
+    static constexpr int OWN = SHARED ? 1 : PHASES;  // tiles side by side in LDS
+    using Tile = RecdTile<T, ROWS, DP>;
+    using Load = Stream<T, ROWS, DP, LOADERS>;
+
+    // what the streaming threads wrote is there for the readers
+    static __device__ inline void sync()
+    {
+        if constexpr (SHARED)
+            __syncthreads();
+        else {
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+        }
+    }
+};
+
+// Adds the phases' sums up into phase 0's, in their order.  pool: 64 * 16 * DT floats for every group.
+template <int DT, int PHASES> __device__ inline void join_sums(recd_f32x16 (&o)[DT], float *pool, int group, int phase, int lane)
+{
+    float *mine = pool + group * (64 * 16 * DT) + lane;
+    for (int ph = 1; ph < PHASES; ph++) {
+        __syncthreads();
+        if (phase == ph)
+#pragma unroll
+            for (int d = 0; d < DT; d++)
+#pragma unroll
+                for (int r = 0; r < 16; r++)
+                    mine[64 * (16 * d + r)] = o[d][r];
+        __syncthreads();
+        if (phase == 0)
+#pragma unroll
+            for (int d = 0; d < DT; d++)
+#pragma unroll
+                for (int r = 0; r < 16; r++)
+                    o[d][r] += mine[64 * (16 * d + r)];
+    }
+}
 
 // cap * log2(e) * tanh(x) + more from x' = 2 log2(e) x, and a quarter of the derivative, (1 - tanh^2) / 4.
 // tanh(x) = 1 - 2 r with r = 1 / (1 + e^2x), off by 2^-23 wherever x lies.  That is enough beside 16-bit operands; for fp32
@@ -180,28 +225,34 @@ template <typename T, int DT> __device__ inline void store_columns(T *row, const
 
 // Waves that a SIMD is to hold at once, as far as the registers go round: two hide each other's waits and fill the
 // matrix cores and the vector units in turn.
-template <typename T, int DP, int NW> constexpr int kResident = (sizeof(T) == 4 && DP > 32) || (NW == 1 && DP > 64) ? 1 : 2;
+template <typename T, int DP, int KEPT> constexpr int kResident = (sizeof(T) == 4 && DP > 32) || (KEPT == 1 && DP > 64) ? 1 : 2;
 
 // 32 query rows a wave.  The loop is pipelined over tiles of 32 keys: one turn multiplies the next tile's scores and the
 // current one's sums while the current scores become exponentials.  The caps, biases and masks of the next scores, and
-// the check of the running maximum, stand behind it.  Three buffers in LDS make it one barrier a turn; a block of one wave
-// needs two and none.
-template <typename T, int DP, int NW, bool CAP>
-__global__ __launch_bounds__(64 * NW, (kResident<T, DP, NW>)) void k_attention(Args a)
+// the check of the running maximum, stand behind it.  Three buffers in LDS make it one barrier a turn; waves that stream for
+// themselves need two and none.
+template <typename T, int DP, int KEPT, int PHASES, bool CAP>
+__global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void k_attention(Args a)
 {
-    constexpr int KS = DP / 16, DT = DP / 32, THREADS = 64 * NW, BUFS = NW == 1 ? 2 : 3;
+    using S = Shape<T, DP, KEPT, PHASES>;
+    static_assert(KEPT == 1 || PHASES == 1);
+    constexpr int KS = DP / 16, DT = DP / 32, BUFS = S::SHARED ? 3 : 2;
     using Mma = RecdMma<T>;
     using Frag = typename Mma::Frag;
-    __shared__ RecdTile<T, 32, DP> kt[BUFS], vt[BUFS];
+    __shared__ struct {
+        typename S::Tile k[S::OWN][BUFS], v[S::OWN][BUFS];
+    } lds;
     Problem p;
     int head, tile, split;
     if (!find_tile(a, p, head, tile, split))
         return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int first = tile * 32 * NW, end = first + 32 * NW < p.rows ? first + 32 * NW : p.rows;  // the block's rows
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, kept = wave % KEPT, phase = wave / KEPT;
+    const int tid = S::SHARED ? threadIdx.x : lane;
+    typename S::Tile *const kt = lds.k[S::SHARED ? 0 : phase], *const vt = lds.v[S::SHARED ? 0 : phase];
+    const int first = tile * 32 * KEPT, end = first + 32 * KEPT < p.rows ? first + 32 * KEPT : p.rows;  // the block's rows
     if (first >= end)
         return;
-    const int row0 = first + 32 * wave, row = row0 + (lane & 31);
+    const int row0 = first + 32 * kept, row = row0 + (lane & 31);
     const bool there = row < p.rows;
     const int query = p.query(row, a.group), head_in = row - query * a.group;
     const int lim = there ? p.limit(row, a.group) : 0;
@@ -209,7 +260,8 @@ __global__ __launch_bounds__(64 * NW, (kResident<T, DP, NW>)) void k_attention(A
     const int wave_end = row0 < p.rows ? p.limit(wave_last, a.group) : 0;
     const int wave_full = row0 + 32 <= p.rows ? p.limit(row0, a.group) : 0;  // keys that every row sees
     const int tiles = (p.limit(end - 1, a.group) + 31) / 32;
-    const int t0 = (int)((int64_t)tiles * split / a.splits), t1 = (int)((int64_t)tiles * (split + 1) / a.splits);
+    const int part = split * PHASES + phase, parts = a.splits * PHASES;
+    const int t0 = (int)((int64_t)tiles * part / parts), t1 = (int)((int64_t)tiles * (part + 1) / parts);
     const int wave_t1 = (wave_end + 31) / 32 < t1 ? (wave_end + 31) / 32 : t1;
     const int H = a.G * a.group;
     const int64_t q_row = p.q0 + query, at_row = q_row * H + p.head0 + head_in;
@@ -236,18 +288,18 @@ __global__ __launch_bounds__(64 * NW, (kResident<T, DP, NW>)) void k_attention(A
 #pragma unroll
     for (int d = 0; d < DT; d++)
         o[d] = recd_f32x16{};
-    Stream<T, 32, DP, THREADS> ks, vs;
+    typename S::Load ks, vs;
     auto load = [&](int t) {
-        ks.load(a.d, [&](int r) -> const T * {
+        ks.load(tid, a.d, [&](int r) -> const T * {
             const int j = t * 32 + r;
             return j < p.nk ? (const T *)a.k + (p.k0 + j) * a.k_stride + (int64_t)head * a.d : nullptr;
         });
-        vs.load(a.d, [&](int r) -> const T * {
+        vs.load(tid, a.d, [&](int r) -> const T * {
             const int j = t * 32 + r;
             return j < p.nk ? (const T *)a.v + (p.k0 + j) * a.v_stride + (int64_t)head * a.d : nullptr;
         });
     };
-    auto scores = [&](const RecdTile<T, 32, DP> &keys, recd_f32x16 &x) {
+    auto scores = [&](const typename S::Tile &keys, recd_f32x16 &x) {
         x = recd_f32x16{};
 #pragma unroll
         for (int k = 0; k < KS; k++)
@@ -304,11 +356,11 @@ __global__ __launch_bounds__(64 * NW, (kResident<T, DP, NW>)) void k_attention(A
     };
     if (t0 < t1) {
         load(t0);
-        ks.store(kt[0]);
-        vs.store(vt[0]);
+        ks.store(tid, kt[0]);
+        vs.store(tid, vt[0]);
         if (t0 + 1 < t1)
             load(t0 + 1);
-        __syncthreads();
+        S::sync();
         if (t0 < wave_t1) {
             scores(kt[0], s[0]);
             settle(t0 * 32, s[0]);
@@ -318,12 +370,12 @@ __global__ __launch_bounds__(64 * NW, (kResident<T, DP, NW>)) void k_attention(A
     auto turn = [&](int t, recd_f32x16 &now, recd_f32x16 &then) {
         const int next = buf + 1 == BUFS ? 0 : buf + 1;
         if (t + 1 < t1) {
-            ks.store(kt[next]);
-            vs.store(vt[next]);
+            ks.store(tid, kt[next]);
+            vs.store(tid, vt[next]);
             if (t + 2 < t1)
                 load(t + 2);
         }
-        __syncthreads();
+        S::sync();
         if (t < wave_t1) {
             scores(kt[next], then);  // (behind the wave's last tile: of what lies there, for nobody)
             const float from = m == -INFINITY ? 0.0f : m;  // a row that has seen nothing yet
@@ -352,7 +404,35 @@ __global__ __launch_bounds__(64 * NW, (kResident<T, DP, NW>)) void k_attention(A
             turn(t + 1, s[1], s[0]);
     }
     l += __shfl_xor(l, 32);
-    if (!there)
+    if constexpr (PHASES > 1) {  // in the order of the phases: the larger maximum, both sums scaled to it
+        float *const pool = reinterpret_cast<float *>(&lds);
+        static_assert(sizeof(lds) >= 64 * (16 * DT + 2) * sizeof(float));
+        for (int ph = 1; ph < PHASES; ph++) {
+            __syncthreads();
+            if (phase == ph) {
+                pool[lane] = m;
+                pool[64 + lane] = l;
+#pragma unroll
+                for (int d = 0; d < DT; d++)
+#pragma unroll
+                    for (int r = 0; r < 16; r++)
+                        pool[64 * (2 + 16 * d + r) + lane] = o[d][r];
+            }
+            __syncthreads();
+            if (phase == 0) {
+                const float other = pool[lane], top = fmaxf(m, other), from = top == -INFINITY ? 0.0f : top;
+                const float f = recd_exp2(m - from), g = recd_exp2(other - from);
+                m = top;
+                l = l * f + pool[64 + lane] * g;
+#pragma unroll
+                for (int d = 0; d < DT; d++)
+#pragma unroll
+                    for (int r = 0; r < 16; r++)
+                        o[d][r] = o[d][r] * f + pool[64 * (2 + 16 * d + r) + lane] * g;
+            }
+        }
+    }
+    if (!there || phase)
         return;
     if (a.splits > 1) {
         const int64_t at = split * a.part_rows + at_row;
@@ -538,29 +618,35 @@ __global__ void k_attention_lift(int d, const uint32_t *tops, float *lift)
 }
 
 // 32 query rows a wave, keys and values stream past.
-template <typename T, int DP, int NW, bool CAP>
-__global__ __launch_bounds__(64 * NW, (kResident<T, DP, NW>)) void k_attention_grad_q(Args a)
+template <typename T, int DP, int KEPT, int PHASES, bool CAP>
+__global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void k_attention_grad_q(Args a)
 {
-    constexpr int KS = DP / 16, DT = DP / 32, THREADS = 64 * NW, BUFS = NW == 1 ? 1 : 2;
+    using S = Shape<T, DP, KEPT, PHASES>;
+    static_assert(KEPT == 1 || PHASES == 1);
+    constexpr int KS = DP / 16, DT = DP / 32, BUFS = S::SHARED ? 2 : 1;
     using Mma = RecdMma<T>;
     using Frag = typename Mma::Frag;
-    __shared__ RecdTile<T, 32, DP> kt[BUFS], vt[BUFS];
+    __shared__ struct {
+        typename S::Tile k[S::OWN][BUFS], v[S::OWN][BUFS];
+    } lds;
     Problem p;
     int head, tile, split;
     if (!find_tile(a, p, head, tile, split))
         return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int first = tile * 32 * NW, end = first + 32 * NW < p.rows ? first + 32 * NW : p.rows;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, kept = wave % KEPT, phase = wave / KEPT;
+    const int tid = S::SHARED ? threadIdx.x : lane;
+    typename S::Tile *const kt = lds.k[S::SHARED ? 0 : phase], *const vt = lds.v[S::SHARED ? 0 : phase];
+    const int first = tile * 32 * KEPT, end = first + 32 * KEPT < p.rows ? first + 32 * KEPT : p.rows;
     if (first >= end)
         return;
-    const int row0 = first + 32 * wave, row = row0 + (lane & 31);
+    const int row0 = first + 32 * kept, row = row0 + (lane & 31);
     const bool there = row < p.rows;
     const int query = p.query(row, a.group), head_in = row - query * a.group;
     const int lim = there ? p.limit(row, a.group) : 0;
     const int wave_last = row0 + 31 < p.rows ? row0 + 31 : p.rows - 1;
     const int wave_end = row0 < p.rows ? p.limit(wave_last, a.group) : 0;
     const int wave_full = row0 + 32 <= p.rows ? p.limit(row0, a.group) : 0;
-    const int tiles = (p.limit(end - 1, a.group) + 31) / 32;
+    const int tiles = (p.limit(end - 1, a.group) + 31) / 32, t0 = tiles * phase / PHASES, t1 = tiles * (phase + 1) / PHASES;
     const int H = a.G * a.group;
     const int64_t q_row = p.q0 + query, at_row = q_row * H + p.head0 + head_in;
     const float slope = a.slopes && there ? a.slopes[p.head0 + head_in] * kRecdLog2e : 0.0f;
@@ -585,25 +671,27 @@ __global__ __launch_bounds__(64 * NW, (kResident<T, DP, NW>)) void k_attention_g
 #pragma unroll
     for (int d = 0; d < DT; d++)
         o[d] = recd_f32x16{};
-    Stream<T, 32, DP, THREADS> ks, vs;
+    typename S::Load ks, vs;
     auto load = [&](int t) {
-        ks.load(a.d, [&](int r) -> const T * {
+        ks.load(tid, a.d, [&](int r) -> const T * {
             const int j = t * 32 + r;
             return j < p.nk ? (const T *)a.k + (p.k0 + j) * a.k_stride + (int64_t)head * a.d : nullptr;
         });
-        vs.load(a.d, [&](int r) -> const T * {
+        vs.load(tid, a.d, [&](int r) -> const T * {
             const int j = t * 32 + r;
             return j < p.nk ? (const T *)a.v + (p.k0 + j) * a.v_stride + (int64_t)head * a.d : nullptr;
         });
     };
-    if (tiles > 0)
-        load(0);
-    for (int t = 0; t < tiles; t++) {
+    if (t0 < t1)
+        load(t0);
+    for (int t = t0; t < t1; t++) {
         const int buf = BUFS == 1 ? 0 : t & 1;
-        ks.store(kt[buf]);
-        vs.store(vt[buf]);
-        __syncthreads();
-        if (t + 1 < tiles)
+        if constexpr (BUFS == 1)
+            S::sync();
+        ks.store(tid, kt[buf]);
+        vs.store(tid, vt[buf]);
+        S::sync();
+        if (t + 1 < t1)
             load(t + 1);
         const int j0 = t * 32;
         if (j0 >= wave_end)
@@ -641,45 +729,61 @@ __global__ __launch_bounds__(64 * NW, (kResident<T, DP, NW>)) void k_attention_g
                 o[d] = Mma::mul(kt[buf].columns(16 * h, 32 * d, lane), sf, o[d]);
         }
     }
-    if (there)
+    if constexpr (PHASES > 1) {
+        static_assert(sizeof(lds) >= 64 * 16 * DT * sizeof(float));
+        join_sums<DT, PHASES>(o, reinterpret_cast<float *>(&lds), 0, phase, lane);
+    }
+    if (there && phase == 0)
         store_columns<T, DT>((T *)a.gq + q_row * a.gq_stride + (int64_t)(p.head0 + head_in) * a.d, o,
                              (CAP ? 4.0f : 1.0f) * a.scale / lift, a.d, lane);
 }
 
 // Keys stay, queries and their gradients stream past.  What a score needs of its row stands in LDS in the order of
 // the sums' registers: four neighbours are read at a time.
-template <typename T, int DP, int NW, bool CAP>
-__global__ __launch_bounds__(64 * NW, (kResident<T, DP, NW>)) void k_attention_grad_kv(Args a)
+template <typename T, int DP, int KEPT, int PHASES, bool CAP>
+__global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void k_attention_grad_kv(Args a)
 {
-    constexpr int KS = DP / 16, DT = DP / 32, THREADS = 64 * NW, BUFS = NW == 1 ? 1 : 2;
+    using S = Shape<T, DP, KEPT, PHASES>;
+    constexpr int KS = DP / 16, DT = DP / 32, BUFS = S::SHARED ? 2 : 1;
     using Mma = RecdMma<T>;
     using Frag = typename Mma::Frag;
-    // Wide 16-bit heads: the kept keys' values stay in LDS, as the registers hold two sums of the head's width besides.
-    constexpr bool VALUES = sizeof(T) == 2 && DP > 64 && NW > 1;
-    __shared__ RecdTile<T, 32, DP> qt[BUFS], gt[BUFS];
-    __shared__ RecdTile<T, VALUES ? 32 * NW : 1, DP> values;
-    __shared__ alignas(16) float row_from[BUFS][32], row_delta[BUFS][32], row_slope[BUFS][32];
-    __shared__ alignas(16) int row_lim[BUFS][32], row_pos[BUFS][32];
+    // Wide heads with two phases: the kept keys and values stay in LDS, read as operands from there, as the registers
+    // hold two sums of the head's width besides.
+    constexpr bool IN_LDS = S::SHARED && PHASES > 1;
+    __shared__ struct {
+        typename S::Tile q[S::OWN][BUFS], g[S::OWN][BUFS];
+        RecdTile<T, IN_LDS ? 32 * KEPT : 1, DP> k, v;
+        alignas(16) float from[S::OWN][BUFS][S::ROWS], delta[S::OWN][BUFS][S::ROWS], slope[S::OWN][BUFS][S::ROWS];
+        alignas(16) int lim[S::OWN][BUFS][S::ROWS], pos[S::OWN][BUFS][S::ROWS];
+    } lds;
     Problem p;
     int head, tile, split;
     if (!find_tile(a, p, head, tile, split))
         return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int first = tile * 32 * NW;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, kept = wave % KEPT, phase = wave / KEPT;
+    const int tid = S::SHARED ? threadIdx.x : lane, own = S::SHARED ? 0 : phase;
+    typename S::Tile *const qt = lds.q[own], *const gt = lds.g[own];
+    const auto row_from = lds.from[own], row_delta = lds.delta[own], row_slope = lds.slope[own];
+    const auto row_lim = lds.lim[own], row_pos = lds.pos[own];
+    const int first = tile * 32 * KEPT;
     if (first >= p.nk)
         return;
-    const int j0 = first + 32 * wave, j = j0 + (lane & 31);
+    const int j0 = first + 32 * kept, j = j0 + (lane & 31);
     const bool there = j < p.nk;
     const int H = a.G * a.group;
-    Frag kf[KS], vf[VALUES ? 1 : KS];
-    T *const value = values.at + (VALUES ? (32 * wave + (lane & 31)) * values.LD + (lane >> 5) * 8 : 0);
+    Frag kf[IN_LDS ? 1 : KS], vf[IN_LDS ? 1 : KS];
+    const int kept_at = IN_LDS ? (32 * kept + (lane & 31)) * lds.k.LD + (lane >> 5) * 8 : 0;
 #pragma unroll
     for (int k = 0; k < KS; k++) {
-        kf[k] = recd_row_frag<T>((const T *)a.k + (p.k0 + j) * a.k_stride + (int64_t)head * a.d, 16 * k, a.d, there, lane);
-        vf[VALUES ? 0 : k] = recd_row_frag<T>((const T *)a.v + (p.k0 + j) * a.v_stride + (int64_t)head * a.d, 16 * k, a.d, there,
-                                              lane);
-        if constexpr (VALUES)
-            *reinterpret_cast<Frag *>(value + 16 * k) = vf[0];  // read by this lane alone
+        const int i = IN_LDS ? 0 : k;
+        if (IN_LDS && k % PHASES != phase)
+            continue;  // the phases share the writing
+        kf[i] = recd_row_frag<T>((const T *)a.k + (p.k0 + j) * a.k_stride + (int64_t)head * a.d, 16 * k, a.d, there, lane);
+        vf[i] = recd_row_frag<T>((const T *)a.v + (p.k0 + j) * a.v_stride + (int64_t)head * a.d, 16 * k, a.d, there, lane);
+        if constexpr (IN_LDS) {
+            *reinterpret_cast<Frag *>(lds.k.at + kept_at + 16 * k) = kf[0];
+            *reinterpret_cast<Frag *>(lds.v.at + kept_at + 16 * k) = vf[0];
+        }
     }
     recd_f32x16 dk[DT], dv[DT];
 #pragma unroll
@@ -694,8 +798,12 @@ __global__ __launch_bounds__(64 * NW, (kResident<T, DP, NW>)) void k_attention_g
     int from_row = 0;
     if (p.causal && p.prefix <= first && first > p.pos0)
         from_row = (int)((int64_t)(first - p.pos0) * a.group < p.rows ? (first - p.pos0) * a.group : p.rows);
-    const int tiles = (p.rows + 31) / 32;
-    Stream<T, 32, DP, THREADS> qs, gs;
+    // (a wave that streams for itself takes its part of the tiles, a phase of a block its 32 rows of every tile)
+    const int tiles = (p.rows + S::ROWS - 1) / S::ROWS, from_tile = from_row / S::ROWS, n_tiles = tiles - from_tile;
+    const int t0 = S::SHARED ? from_tile : from_tile + n_tiles * phase / PHASES;
+    const int t1 = S::SHARED ? tiles : from_tile + n_tiles * (phase + 1) / PHASES;
+    const int sub = S::SHARED ? 32 * phase : 0;
+    typename S::Load qs, gs;
     float n_from = 0.0f, n_delta = 0.0f, n_slope = 0.0f;
     int n_lim = 0, n_pos = 0;
     auto load = [&](int t) {
@@ -703,20 +811,20 @@ __global__ __launch_bounds__(64 * NW, (kResident<T, DP, NW>)) void k_attention_g
             query = p.query(r, a.group);
             h = p.head0 + r - query * a.group;
         };
-        qs.load(a.d, [&](int r) -> const T * {
+        qs.load(tid, a.d, [&](int r) -> const T * {
             int query, h;
-            at(t * 32 + r, query, h);
-            return t * 32 + r < p.rows ? (const T *)a.q + (p.q0 + query) * a.q_stride + (int64_t)h * a.d : nullptr;
+            at(t * S::ROWS + r, query, h);
+            return t * S::ROWS + r < p.rows ? (const T *)a.q + (p.q0 + query) * a.q_stride + (int64_t)h * a.d : nullptr;
         });
-        gs.load(a.d, [&](int r) -> const T * {
+        gs.load(tid, a.d, [&](int r) -> const T * {
             int query, h;
-            at(t * 32 + r, query, h);
-            return t * 32 + r < p.rows ? (const T *)a.g + ((p.q0 + query) * H + h) * a.d : nullptr;
+            at(t * S::ROWS + r, query, h);
+            return t * S::ROWS + r < p.rows ? (const T *)a.g + ((p.q0 + query) * H + h) * a.d : nullptr;
         });
-        const int r = t * 32 + threadIdx.x;
+        const int r = t * S::ROWS + tid;
         n_from = n_delta = n_slope = 0.0f;
         n_lim = n_pos = 0;
-        if (threadIdx.x < 32 && r < p.rows) {
+        if (tid < S::ROWS && r < p.rows) {
             int query, h;
             at(r, query, h);
             n_from = a.lse_in[(p.q0 + query) * H + h] * kRecdLog2e;
@@ -727,36 +835,43 @@ __global__ __launch_bounds__(64 * NW, (kResident<T, DP, NW>)) void k_attention_g
             n_pos = p.pos0 + query;
         }
     };
-    const int t0 = from_row / 32;
-    if (t0 < tiles)
+    if (t0 < t1)
         load(t0);
-    for (int t = t0; t < tiles; t++) {
+    for (int t = t0; t < t1; t++) {
         const int buf = BUFS == 1 ? 0 : t & 1;
-        qs.store(qt[buf]);
-        gs.store(gt[buf]);
-        if (threadIdx.x < 32) {
-            const int i = recd_product_row(threadIdx.x);
+        if constexpr (BUFS == 1)
+            S::sync();
+        qs.store(tid, qt[buf]);
+        gs.store(tid, gt[buf]);
+        if (tid < S::ROWS) {
+            const int i = recd_product_row(tid);
             row_from[buf][i] = n_from;
             row_delta[buf][i] = n_delta;
             row_slope[buf][i] = n_slope;
             row_lim[buf][i] = n_lim;
             row_pos[buf][i] = n_pos;
         }
-        __syncthreads();
-        if (t + 1 < tiles)
+        S::sync();
+        if (t + 1 < t1)
             load(t + 1);
-        const bool whole = t * 32 + 32 <= p.rows;
+        const int row0 = t * S::ROWS + sub;
+        const bool whole = row0 + 32 <= p.rows;
         // (tile rows 0 and 31 are the product's rows 0 and 31, and limits and positions do not fall)
-        if (j0 >= p.nk || (whole && row_lim[buf][31] <= j0))
+        if (j0 >= p.nk || row0 >= p.rows || (whole && row_lim[buf][sub + 31] <= j0))
             continue;
         recd_f32x16 s = {}, dp = {};
 #pragma unroll
         for (int k = 0; k < KS; k++) {
-            s = Mma::mul(qt[buf].rows(0, 16 * k, lane), kf[k], s);
-            if constexpr (VALUES)
-                dp = Mma::mul(gt[buf].rows(0, 16 * k, lane), *reinterpret_cast<const Frag *>(value + 16 * k), dp);
-            else
-                dp = Mma::mul(gt[buf].rows(0, 16 * k, lane), vf[k], dp);
+            Frag key, value;
+            if constexpr (IN_LDS) {
+                key = *reinterpret_cast<const Frag *>(lds.k.at + kept_at + 16 * k);
+                value = *reinterpret_cast<const Frag *>(lds.v.at + kept_at + 16 * k);
+            } else {
+                key = kf[k];
+                value = vf[k];
+            }
+            s = Mma::mul(qt[buf].rows(sub, 16 * k, lane), key, s);
+            dp = Mma::mul(gt[buf].rows(sub, 16 * k, lane), value, dp);
         }
         auto scored = [&](int r, float x, float d, float bias, float delta) {
             float quarter = 1.0f;
@@ -764,13 +879,13 @@ __global__ __launch_bounds__(64 * NW, (kResident<T, DP, NW>)) void k_attention_g
             s[r] = recd_exp2(z);
             dp[r] = s[r] * (d * lift_dp - delta) * quarter;
         };
-        const bool below = whole && j0 + 31 <= row_pos[buf][0], above = whole && j0 >= row_pos[buf][31];
-        const bool seen = whole && j0 + 32 <= row_lim[buf][0];
+        const bool below = whole && j0 + 31 <= row_pos[buf][sub], above = whole && j0 >= row_pos[buf][sub + 31];
+        const bool seen = whole && j0 + 32 <= row_lim[buf][sub];
         if (seen && (!a.slopes || below || above)) {
             const float jf = (float)(below ? j : -j), sign = below ? -1.0f : 1.0f;
 #pragma unroll
             for (int r = 0; r < 16; r += 4) {
-                const int row = recd_sums_row(r, lane);
+                const int row = sub + recd_sums_row(r, lane);
                 const recd_f32x4 from = *reinterpret_cast<const recd_f32x4 *>(&row_from[buf][row]);
                 const recd_f32x4 delta = *reinterpret_cast<const recd_f32x4 *>(&row_delta[buf][row]);
                 if (a.slopes) {
@@ -787,7 +902,7 @@ __global__ __launch_bounds__(64 * NW, (kResident<T, DP, NW>)) void k_attention_g
         } else {
 #pragma unroll
             for (int r = 0; r < 16; r++) {
-                const int row = recd_sums_row(r, lane);
+                const int row = sub + recd_sums_row(r, lane);
                 scored(r, s[r], dp[r], row_from[buf][row] - row_slope[buf][row] * fabsf((float)(row_pos[buf][row] - j)),
                        row_delta[buf][row]);
                 if (j >= row_lim[buf][row])
@@ -799,12 +914,17 @@ __global__ __launch_bounds__(64 * NW, (kResident<T, DP, NW>)) void k_attention_g
             const Frag pf = recd_sums_frag<T>(s, h), sf = recd_sums_frag<T>(dp, h);
 #pragma unroll
             for (int d = 0; d < DT; d++) {
-                dv[d] = Mma::mul(gt[buf].columns(16 * h, 32 * d, lane), pf, dv[d]);
-                dk[d] = Mma::mul(qt[buf].columns(16 * h, 32 * d, lane), sf, dk[d]);
+                dv[d] = Mma::mul(gt[buf].columns(sub + 16 * h, 32 * d, lane), pf, dv[d]);
+                dk[d] = Mma::mul(qt[buf].columns(sub + 16 * h, 32 * d, lane), sf, dk[d]);
             }
         }
     }
-    if (!there)
+    if constexpr (PHASES > 1) {
+        static_assert(sizeof(lds) >= KEPT * 64 * 16 * DT * sizeof(float));
+        join_sums<DT, PHASES>(dk, reinterpret_cast<float *>(&lds), kept, phase, lane);
+        join_sums<DT, PHASES>(dv, reinterpret_cast<float *>(&lds), kept, phase, lane);
+    }
+    if (!there || phase)
         return;
     store_columns<T, DT>((T *)a.gk + (p.k0 + j) * a.gk_stride + (int64_t)head * a.d, dk, (CAP ? 4.0f : 1.0f) * a.scale / lift, a.d,
                          lane);
@@ -903,19 +1023,40 @@ Args common_args(const recd_attention *d, const void *q, const void *k, const vo
     return a;
 }
 
-// How the tiles of one side are listed: waves of 32 rows a tile, and slots.
+enum Which { FORWARD, GRAD_Q, GRAD_KV };
+
+// How a kernel's blocks divide their tiles: one wave; one group of 32 kept rows in phases; four groups (and, for the wide
+// 16-bit heads of the gradients by keys and values, two phases).
+enum Division { ONE_WAVE, PHASES, GROUPS };
+
+// How the tiles of one side are listed: the kept rows of a tile, and slots.
 struct Tiling {
-    int waves, tiles_per_list;
+    Division division;
+    int R, tiles_per_list;
     int64_t slots;
     bool table;
 };
 
-Tiling tiling(const recd_attention *d, int64_t rows, int64_t most, int group)
+// Lists of few rows (here and on the other side) give every tile to a wave of its own; so many tiles that four groups in a
+// block fill the card share what they stream; in between a tile's streamed rows are divided among the waves.
+Tiling tiling(const recd_ctx *ctx, const recd_attention *d, int64_t rows, int64_t most, int group, int64_t others,
+              int64_t most_others, int waves = 4)
 {
     Tiling t;
-    t.waves = most * group <= 64 || rows * group <= 48 * d->lists ? 1 : 4;
-    const int64_t R = 32 * t.waves, per = (most * group + R - 1) / R;
-    t.slots = rows * group / R + d->lists;
+    const int64_t per_four = (most * group + 127) / 128;
+    int64_t four = rows * group / 128 + d->lists;
+    if (four > d->lists * per_four)
+        four = d->lists * per_four;
+    const bool few = most * group <= 64 || rows * group <= 48 * d->lists;
+    if (few && (most_others <= 128 || others <= 64 * d->lists))
+        t.division = ONE_WAVE;
+    else if (few || four * d->kv_heads * waves < 12 * ctx->num_cu)
+        t.division = PHASES;
+    else
+        t.division = GROUPS;
+    t.R = t.division == GROUPS ? 128 : 32;
+    const int64_t per = (most * group + t.R - 1) / t.R;
+    t.slots = rows * group / t.R + d->lists;
     t.table = d->lists * per > t.slots;
     if (!t.table)
         t.slots = d->lists * per;
@@ -933,47 +1074,62 @@ int log2_of(int n)
 
 unsigned grid_of(const Args &a) { return (unsigned)((a.slots * a.splits + 7) / 8 * 8 * a.G); }
 
-enum Which { FORWARD, GRAD_Q, GRAD_KV };
-
-template <typename T, int DP, int NW, bool CAP> void launch_one(Which w, const Args &a, hipStream_t st)
+template <typename T, int DP, bool CAP> void launch_one(Which w, const Args &a, Division v, hipStream_t st)
 {
-    const dim3 grid(grid_of(a)), block(64 * NW);
-    if (w == FORWARD)
-        hipLaunchKernelGGL((k_attention<T, DP, NW, CAP>), grid, block, 0, st, a);
-    else if (w == GRAD_Q)
-        hipLaunchKernelGGL((k_attention_grad_q<T, DP, NW, CAP>), grid, block, 0, st, a);
-    else
-        hipLaunchKernelGGL((k_attention_grad_kv<T, DP, NW, CAP>), grid, block, 0, st, a);
+    constexpr int P = sizeof(T) == 4 && DP > 64 ? 2 : 4, KV = sizeof(T) == 2 && DP > 64 ? 2 : 1;
+    const dim3 grid(grid_of(a));
+#define RECD_LAUNCH(kernel, kept, phases) \
+    hipLaunchKernelGGL((kernel<T, DP, kept, phases, CAP>), grid, dim3(64 * kept * phases), 0, st, a)
+    if (w == FORWARD) {
+        if (v == ONE_WAVE)
+            RECD_LAUNCH(k_attention, 1, 1);
+        else if (v == PHASES)
+            RECD_LAUNCH(k_attention, 1, P);
+        else
+            RECD_LAUNCH(k_attention, 4, 1);
+    } else if (w == GRAD_Q) {
+        if (v == ONE_WAVE)
+            RECD_LAUNCH(k_attention_grad_q, 1, 1);
+        else if (v == PHASES)
+            RECD_LAUNCH(k_attention_grad_q, 1, P);
+        else
+            RECD_LAUNCH(k_attention_grad_q, 4, 1);
+    } else {
+        if (v == ONE_WAVE)
+            RECD_LAUNCH(k_attention_grad_kv, 1, 1);
+        else if (v == PHASES)
+            RECD_LAUNCH(k_attention_grad_kv, 1, P);
+        else
+            RECD_LAUNCH(k_attention_grad_kv, 4, KV);
+    }
+#undef RECD_LAUNCH
 }
 
-template <typename T, int DP> void launch_width(Which w, const Args &a, int waves, hipStream_t st)
+template <typename T, int DP> void launch_width(Which w, const Args &a, Division v, hipStream_t st)
 {
-    if (a.cap != 0.0f)
-        waves == 1 ? launch_one<T, DP, 1, true>(w, a, st) : launch_one<T, DP, 4, true>(w, a, st);
-    else
-        waves == 1 ? launch_one<T, DP, 1, false>(w, a, st) : launch_one<T, DP, 4, false>(w, a, st);
+    a.cap != 0.0f ? launch_one<T, DP, true>(w, a, v, st) : launch_one<T, DP, false>(w, a, v, st);
 }
 
-template <typename T> void launch(Which w, const Args &a, int waves, hipStream_t st)
+template <typename T> void launch(Which w, const Args &a, Division v, hipStream_t st)
 {
     if (a.slots * a.splits == 0)
         return;
     if (a.d <= 32)
-        launch_width<T, 32>(w, a, waves, st);
+        launch_width<T, 32>(w, a, v, st);
     else if (a.d <= 64)
-        launch_width<T, 64>(w, a, waves, st);
+        launch_width<T, 64>(w, a, v, st);
     else
-        launch_width<T, 128>(w, a, waves, st);
+        launch_width<T, 128>(w, a, v, st);
 }
 
 void launch_tiles(const recd_attention *d, const Tiling &t, int group, bool keys, int2 *tiles, hipStream_t st)
 {
     if (t.table && d->lists <= kMostSorted && t.slots < ((int64_t)1 << 30))
-        hipLaunchKernelGGL(k_attention_tiles_by_work, dim3(1), dim3(1024), 0, st, (int)d->lists, (int)t.slots, group, 32 * t.waves,
+        hipLaunchKernelGGL(k_attention_tiles_by_work, dim3(1), dim3(1024), 0, st, (int)d->lists, (int)t.slots, group, t.R,
                            keys, d->causal != 0, d->q_offsets, d->k_offsets, d->prefix, tiles);
     else if (t.table)
         hipLaunchKernelGGL(k_attention_tiles, dim3((unsigned)((d->lists + 255) / 256)), dim3(256), 0, st, d->lists, t.slots, group,
-                           32 * t.waves, keys ? d->k_offsets : d->q_offsets, tiles);
+                           t.R, keys ? d->k_offsets : d->q_offsets, tiles);
 }
 
 } // namespace
@@ -996,11 +1152,11 @@ recd_status recd_list_attention(recd_ctx *ctx, const recd_attention *d, const vo
     Args a = common_args(d, q, k, v);
     a.out = out;
     a.lse = lse;
-    const Tiling t = tiling(d, d->q_rows, d->max_q, a.group);
+    const Tiling t = tiling(ctx, d, d->q_rows, d->max_q, a.group, d->k_rows, d->max_k);
     a.slots = t.slots;
     a.tiles_per_list = t.tiles_per_list;
     // few tiles: a tile's keys are split over blocks, at least 256 keys each
-    const int64_t blocks = (int64_t)ctx->num_cu * 4, have = t.slots * a.G > 0 ? t.slots * a.G : 1;
+    const int64_t blocks = (int64_t)ctx->num_cu * 2, have = t.slots * a.G > 0 ? t.slots * a.G : 1;
     int64_t splits = (blocks + have - 1) / have;
     if (splits > d->max_k / 256)
         splits = d->max_k / 256;
@@ -1026,7 +1182,7 @@ recd_status recd_list_attention(recd_ctx *ctx, const recd_attention *d, const vo
     launch_tiles(d, t, a.group, false, tiles, ctx->stream);
     recd_with_type(d->dtype, [&](auto e) {
         using T = decltype(e);
-        launch<T>(FORWARD, a, t.waves, ctx->stream);
+        launch<T>(FORWARD, a, t.division, ctx->stream);
         if (a.splits > 1) {
             const int dlog = log2_of(a.d / 4);
             hipLaunchKernelGGL((k_attention_join<T>), dim3((unsigned)(((a.part_rows << dlog) + 255) / 256)), dim3(256), 0,
@@ -1065,7 +1221,9 @@ recd_status recd_list_attention_backward(recd_ctx *ctx, const recd_attention *d,
     a.gq_stride = grad_q_stride;
     a.gk_stride = grad_k_stride;
     a.gv_stride = grad_v_stride;
-    const Tiling tq = tiling(d, d->q_rows, d->max_q, a.group), tk = tiling(d, d->k_rows, d->max_k, 1);
+    const Tiling tq = tiling(ctx, d, d->q_rows, d->max_q, a.group, d->k_rows, d->max_k);
+    const Tiling tk = tiling(ctx, d, d->k_rows, d->max_k, 1, d->q_rows * a.group, d->max_q * a.group,
+                             d->dtype != RECD_F32 && a.d > 64 ? 8 : 4);
     if (tq.slots / 8 + 1 > ((int64_t)1 << 27) / a.G || tk.slots / 8 + 1 > ((int64_t)1 << 27) / a.G)
         return recd_fail(ctx, RECD_EINVAL, "too many tiles");
     const bool half = d->dtype == RECD_F16;
@@ -1109,14 +1267,14 @@ recd_status recd_list_attention_backward(recd_ctx *ctx, const recd_attention *d,
             a.tiles = tiles_q;
             a.slots = tq.slots;
             a.tiles_per_list = tq.tiles_per_list;
-            launch<T>(GRAD_Q, a, tq.waves, st);
+            launch<T>(GRAD_Q, a, tq.division, st);
         }
         a.tiles = tiles_k;
         a.last_first = false;
         a.slots = tk.slots;
         a.tiles_per_list = tk.tiles_per_list;
         if (d->k_rows)
-            launch<T>(GRAD_KV, a, tk.waves, st);
+            launch<T>(GRAD_KV, a, tk.division, st);
     });
     RECD_HIP(ctx, hipGetLastError());
     return RECD_OK;
