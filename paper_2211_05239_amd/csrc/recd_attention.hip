@@ -246,7 +246,8 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
     int head, tile, split;
     if (!find_tile(a, p, head, tile, split))
         return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, kept = wave % KEPT, phase = wave / KEPT;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int kept = wave % KEPT, phase = wave / KEPT;
     const int tid = S::SHARED ? threadIdx.x : lane;
     typename S::Tile *const kt = lds.k[S::SHARED ? 0 : phase], *const vt = lds.v[S::SHARED ? 0 : phase];
     const int first = tile * 32 * KEPT, end = first + 32 * KEPT < p.rows ? first + 32 * KEPT : p.rows;  // the block's rows
@@ -266,8 +267,7 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
     const int H = a.G * a.group;
     const int64_t q_row = p.q0 + query, at_row = q_row * H + p.head0 + head_in;
     const float slope = a.slopes && there ? a.slopes[p.head0 + head_in] * kRecdLog2e : 0.0f;
-    const int pos = p.pos0 + query;
-    const int pos_min = p.pos0 + p.query(row0, a.group), pos_max = p.pos0 + p.query(wave_last, a.group);
+    const float posf = (float)(p.pos0 + query);
     // the sign of the scale goes into the queries; what is neither capped nor biased stays unscaled until the exponent
     const float scale = fabsf(a.scale), c = scale * kRecdLog2e;
     const bool plain = !CAP && !a.slopes && c > 0.0f;
@@ -306,28 +306,19 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
             x = Mma::mul(keys.rows(0, 16 * k, lane), qf[k], x);
     };
     auto settle = [&](int j0, recd_f32x16 &x) {
-        if (!plain) {
-            if (!a.slopes) {
+        if (a.slopes) {
+            const float far = posf - (float)(j0 + (lane >> 5));
 #pragma unroll
-                for (int r = 0; r < 16; r++) {
-                    float unused;
-                    x[r] = CAP ? capped.value(x[r] * to_cap, 0.0f, unused) : x[r] * c;
-                }
-            } else if (j0 + 31 <= pos_min || j0 >= pos_max) {  // all keys on one side of all queries: the distance is linear
-                const float sl = j0 >= pos_max ? -slope : slope, at0 = sl * (float)(j0 + (lane >> 5) - pos);
+            for (int r = 0; r < 16; r++) {
+                const float bias = -slope * fabsf(far - (float)recd_score_row(r, 0));
+                float unused;
+                x[r] = CAP ? capped.value(x[r] * to_cap, bias, unused) : x[r] * c + bias;
+            }
+        } else if (!plain) {
 #pragma unroll
-                for (int r = 0; r < 16; r++) {
-                    float unused;
-                    const float bias = sl * (float)recd_score_row(r, 0) + at0;
-                    x[r] = CAP ? capped.value(x[r] * to_cap, bias, unused) : x[r] * c + bias;
-                }
-            } else {
-#pragma unroll
-                for (int r = 0; r < 16; r++) {
-                    float unused;
-                    const float bias = -slope * fabsf((float)(pos - j0 - recd_score_row(r, lane)));
-                    x[r] = CAP ? capped.value(x[r] * to_cap, bias, unused) : x[r] * c + bias;
-                }
+            for (int r = 0; r < 16; r++) {
+                float unused;
+                x[r] = CAP ? capped.value(x[r] * to_cap, 0.0f, unused) : x[r] * c;
             }
         }
         if (j0 + 32 > wave_full) {
@@ -633,7 +624,8 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
     int head, tile, split;
     if (!find_tile(a, p, head, tile, split))
         return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, kept = wave % KEPT, phase = wave / KEPT;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int kept = wave % KEPT, phase = wave / KEPT;
     const int tid = S::SHARED ? threadIdx.x : lane;
     typename S::Tile *const kt = lds.k[S::SHARED ? 0 : phase], *const vt = lds.v[S::SHARED ? 0 : phase];
     const int first = tile * 32 * KEPT, end = first + 32 * KEPT < p.rows ? first + 32 * KEPT : p.rows;
@@ -650,8 +642,7 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
     const int H = a.G * a.group;
     const int64_t q_row = p.q0 + query, at_row = q_row * H + p.head0 + head_in;
     const float slope = a.slopes && there ? a.slopes[p.head0 + head_in] * kRecdLog2e : 0.0f;
-    const int pos = p.pos0 + query;
-    const int pos_min = p.pos0 + p.query(row0, a.group), pos_max = p.pos0 + p.query(wave_last, a.group);
+    const float posf = (float)(p.pos0 + query);
     float from = there ? a.lse_in[at_row] * kRecdLog2e : 0.0f;
     if (from == -INFINITY)
         from = 0.0f;  // sees nothing
@@ -702,24 +693,27 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
             s = Mma::mul(kt[buf].rows(0, 16 * k, lane), qf[k], s);
             dp = Mma::mul(vt[buf].rows(0, 16 * k, lane), gf[k], dp);
         }
-        // the exponent's argument without the bias's distance, then p, then ds
-        auto ds_of = [&](float x, float d, float bias) {
+        // the exponent, then p, then ds
+        auto ds_of = [&](float x, float d, float more) {
             float quarter = 1.0f;
-            const float z = CAP ? capped.value(x * to_cap, bias, quarter) : x * c + bias;
+            const float z = CAP ? capped.value(x * to_cap, more, quarter) : x * c + more;
             return recd_exp2(z) * (d * lift - delta) * quarter;
         };
-        if (j0 + 32 <= wave_full && (!a.slopes || j0 + 31 <= pos_min || j0 >= pos_max)) {
-            const float sl = j0 >= pos_max ? -slope : slope, at0 = sl * (float)(j0 + (lane >> 5) - pos) - from;
+        if (a.slopes) {
+            const float far = posf - (float)(j0 + (lane >> 5));
 #pragma unroll
             for (int r = 0; r < 16; r++)
-                s[r] = ds_of(s[r], dp[r], a.slopes ? sl * (float)recd_score_row(r, 0) + at0 : at0);
+                s[r] = ds_of(s[r], dp[r], -slope * fabsf(far - (float)recd_score_row(r, 0)) - from);
         } else {
 #pragma unroll
-            for (int r = 0; r < 16; r++) {
-                const int j = j0 + recd_score_row(r, lane);
-                const float x = ds_of(s[r], dp[r], -slope * fabsf((float)(pos - j)) - from);
-                s[r] = j < lim ? x : 0.0f;
-            }
+            for (int r = 0; r < 16; r++)
+                s[r] = ds_of(s[r], dp[r], -from);
+        }
+        if (j0 + 32 > wave_full) {
+            asm volatile("");  // a branch: only the tiles at the mask's edge pay for it
+#pragma unroll
+            for (int r = 0; r < 16; r++)
+                s[r] = j0 + recd_score_row(r, lane) >= lim ? 0.0f : s[r];
         }
 #pragma unroll
         for (int h = 0; h < 2; h++) {
@@ -754,22 +748,26 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
         typename S::Tile q[S::OWN][BUFS], g[S::OWN][BUFS];
         RecdTile<T, IN_LDS ? 32 * KEPT : 1, DP> k, v;
         alignas(16) float from[S::OWN][BUFS][S::ROWS], delta[S::OWN][BUFS][S::ROWS], slope[S::OWN][BUFS][S::ROWS];
-        alignas(16) int lim[S::OWN][BUFS][S::ROWS], pos[S::OWN][BUFS][S::ROWS];
+        alignas(16) float pos[S::OWN][BUFS][S::ROWS];
+        alignas(16) int lim[S::OWN][BUFS][S::ROWS];
     } lds;
     Problem p;
     int head, tile, split;
     if (!find_tile(a, p, head, tile, split))
         return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, kept = wave % KEPT, phase = wave / KEPT;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int kept = wave % KEPT, phase = wave / KEPT;
     const int tid = S::SHARED ? threadIdx.x : lane, own = S::SHARED ? 0 : phase;
     typename S::Tile *const qt = lds.q[own], *const gt = lds.g[own];
     const auto row_from = lds.from[own], row_delta = lds.delta[own], row_slope = lds.slope[own];
-    const auto row_lim = lds.lim[own], row_pos = lds.pos[own];
+    const auto row_pos = lds.pos[own];
+    const auto row_lim = lds.lim[own];
     const int first = tile * 32 * KEPT;
     if (first >= p.nk)
         return;
     const int j0 = first + 32 * kept, j = j0 + (lane & 31);
     const bool there = j < p.nk;
+    const float jf = (float)j;
     const int H = a.G * a.group;
     Frag kf[IN_LDS ? 1 : KS], vf[IN_LDS ? 1 : KS];
     const int kept_at = IN_LDS ? (32 * kept + (lane & 31)) * lds.k.LD + (lane >> 5) * 8 : 0;
@@ -805,7 +803,8 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
     const int sub = S::SHARED ? 32 * phase : 0;
     typename S::Load qs, gs;
     float n_from = 0.0f, n_delta = 0.0f, n_slope = 0.0f;
-    int n_lim = 0, n_pos = 0;
+    float n_pos = 0.0f;
+    int n_lim = 0;
     auto load = [&](int t) {
         auto at = [&](int r, int &query, int &h) {
             query = p.query(r, a.group);
@@ -823,7 +822,8 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
         });
         const int r = t * S::ROWS + tid;
         n_from = n_delta = n_slope = 0.0f;
-        n_lim = n_pos = 0;
+        n_pos = 0.0f;
+        n_lim = 0;
         if (tid < S::ROWS && r < p.rows) {
             int query, h;
             at(r, query, h);
@@ -832,7 +832,7 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
             n_delta = a.delta[(p.q0 + query) * H + h] * lift_dp;
             n_slope = a.slopes ? a.slopes[h] * kRecdLog2e : 0.0f;
             n_lim = p.limit(r, a.group);
-            n_pos = p.pos0 + query;
+            n_pos = (float)(p.pos0 + query);
         }
     };
     if (t0 < t1)
@@ -856,8 +856,8 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
             load(t + 1);
         const int row0 = t * S::ROWS + sub;
         const bool whole = row0 + 32 <= p.rows;
-        // (tile rows 0 and 31 are the product's rows 0 and 31, and limits and positions do not fall)
-        if (j0 >= p.nk || row0 >= p.rows || (whole && row_lim[buf][sub + 31] <= j0))
+        // (tile row 31 is the product's row 31, and limits do not fall: what it does not see, no row sees)
+        if (j0 >= p.nk || row0 >= p.rows || (whole && __builtin_amdgcn_readfirstlane(row_lim[buf][sub + 31]) <= j0))
             continue;
         recd_f32x16 s = {}, dp = {};
 #pragma unroll
@@ -873,41 +873,42 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
             s = Mma::mul(qt[buf].rows(sub, 16 * k, lane), key, s);
             dp = Mma::mul(gt[buf].rows(sub, 16 * k, lane), value, dp);
         }
-        auto scored = [&](int r, float x, float d, float bias, float delta) {
+        auto score = [&](int r, float more, float delta) {
             float quarter = 1.0f;
-            const float z = CAP ? capped.value(x * to_cap, bias, quarter) : x * c + bias;
+            const float z = CAP ? capped.value(s[r] * to_cap, more, quarter) : s[r] * c + more;
             s[r] = recd_exp2(z);
-            dp[r] = s[r] * (d * lift_dp - delta) * quarter;
+            dp[r] = s[r] * (dp[r] * lift_dp - delta) * quarter;
         };
-        const bool below = whole && j0 + 31 <= row_pos[buf][sub], above = whole && j0 >= row_pos[buf][sub + 31];
-        const bool seen = whole && j0 + 32 <= row_lim[buf][sub];
-        if (seen && (!a.slopes || below || above)) {
-            const float jf = (float)(below ? j : -j), sign = below ? -1.0f : 1.0f;
+        if (a.slopes) {
 #pragma unroll
             for (int r = 0; r < 16; r += 4) {
                 const int row = sub + recd_sums_row(r, lane);
                 const recd_f32x4 from = *reinterpret_cast<const recd_f32x4 *>(&row_from[buf][row]);
                 const recd_f32x4 delta = *reinterpret_cast<const recd_f32x4 *>(&row_delta[buf][row]);
-                if (a.slopes) {
-                    const recd_f32x4 sl = *reinterpret_cast<const recd_f32x4 *>(&row_slope[buf][row]);
+                const recd_f32x4 slope = *reinterpret_cast<const recd_f32x4 *>(&row_slope[buf][row]);
+                const recd_f32x4 pos = *reinterpret_cast<const recd_f32x4 *>(&row_pos[buf][row]);
 #pragma unroll
-                    for (int q = 0; q < 4; q++)
-                        scored(r + q, s[r + q], dp[r + q], from[q] + sl[q] * (jf + sign * (float)row_pos[buf][row + q]), delta[q]);
-                } else {
-#pragma unroll
-                    for (int q = 0; q < 4; q++)
-                        scored(r + q, s[r + q], dp[r + q], from[q], delta[q]);
-                }
+                for (int q = 0; q < 4; q++)
+                    score(r + q, from[q] - slope[q] * fabsf(pos[q] - jf), delta[q]);
             }
         } else {
 #pragma unroll
-            for (int r = 0; r < 16; r++) {
+            for (int r = 0; r < 16; r += 4) {
                 const int row = sub + recd_sums_row(r, lane);
-                scored(r, s[r], dp[r], row_from[buf][row] - row_slope[buf][row] * fabsf((float)(row_pos[buf][row] - j)),
-                       row_delta[buf][row]);
-                if (j >= row_lim[buf][row])
-                    s[r] = dp[r] = 0.0f;
+                const recd_f32x4 from = *reinterpret_cast<const recd_f32x4 *>(&row_from[buf][row]);
+                const recd_f32x4 delta = *reinterpret_cast<const recd_f32x4 *>(&row_delta[buf][row]);
+#pragma unroll
+                for (int q = 0; q < 4; q++)
+                    score(r + q, from[q], delta[q]);
             }
+        }
+        // (tile row 0 is the product's row 0, and limits do not fall: what its rows all see, the others see)
+        if (!whole || __builtin_amdgcn_readfirstlane(row_lim[buf][sub]) < j0 + 32) {
+            asm volatile("");
+#pragma unroll
+            for (int r = 0; r < 16; r++)
+                if (j >= row_lim[buf][sub + recd_sums_row(r, lane)])
+                    s[r] = dp[r] = 0.0f;
         }
 #pragma unroll
         for (int h = 0; h < 2; h++) {
