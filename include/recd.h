@@ -629,7 +629,7 @@ typedef struct recd_attention {
     int64_t max_q, max_k;                  /* upper bounds of a list's query and key rows */
     int64_t q_rows, k_rows;                /* rows of all lists: q_offsets[lists], k_offsets[lists] */
     const int64_t *q_offsets, *k_offsets;  /* device [lists + 1], from 0, not falling; may be one array (call 1's u_offsets) */
-    int64_t q_stride, k_stride, v_stride;  /* elements from row to row; the heads of a row lie densely */
+    int64_t q_stride, k_stride, v_stride;  /* elements from row to row, less than 16 MiB; the heads of a row lie densely */
     float scale, softcap;                  /* softcap 0 = none */
     const float *slopes;                   /* device fp32 [heads], or NULL */
     const int32_t *prefix;                 /* device [lists], or NULL; needs causal */

@@ -37,9 +37,11 @@ constexpr int kMostSorted = 1024;  // lists whose tiles are put in the order of 
 
 struct Args {
     int G, group, d;              // key heads, query heads of each, elements of a head
+    uint32_t by_group;            // ceil(2^32 / group)
     int64_t lists, slots;
     const int2 *tiles;            // {list or -1, tile} of every slot, or null: tiles_per_list slots for every list
     int tiles_per_list, splits;
+    int heads;                    // key heads that a block goes through (of one wave; else 1)
     bool last_first;              // without a table: a list's last tiles hold the most work
     const int64_t *q_offsets, *k_offsets;
     const void *q, *k, *v, *out_in, *g;
@@ -49,87 +51,100 @@ struct Args {
     const int32_t *prefix;
     int causal;
     void *out, *gq, *gk, *gv;
-    float *lse;
-    const float *lse_in, *delta;  // [q rows][H]
+    float *lse, *delta;           // [q rows][H]
+    const float *lse_in;
     const float *lift;            // fp16 backward: the power of two that ds is held larger by, else null
     float *part_m, *part_l, *part_o;
     int64_t part_rows;            // q rows * H
 };
 
-// One (list, key head).
+// One list.
 struct Problem {
     int64_t q0, k0;
-    int nq, nk, rows, head0, pos0, prefix;
+    int nq, nk, rows, pos0, prefix;
     bool causal;
 
     __device__ inline int query(int row, int group) const { return group == 1 ? row : row / group; }
     // keys [0, limit) are visible to the row; does not fall with the row
-    __device__ inline int limit(int row, int group) const
+    __device__ inline int limit(int row, int group) const { return causal ? limit_at(query(row, group)) : nk; }
+    __device__ inline int limit_at(int query) const
     {
         if (!causal)
             return nk;
-        const int past = pos0 + query(row, group) + 1, to = past > prefix ? past : prefix;
+        const int past = pos0 + query + 1, to = past > prefix ? past : prefix;
         return to < 0 ? 0 : to > nk ? nk : to;
     }
 };
 
+// The value of the wave's first lane, which all lanes hold.
+__device__ inline int64_t uniform(int64_t v)
+{
+    return (int64_t)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)v);
+}
+
 // The block's tile: false where the slot holds none.  Slots go round the dies; the heads of a slot, whose rows share
 // cache lines, follow each other on one die.  Without a table the lists' tiles with the most work come first.
-__device__ inline bool find_tile(const Args &a, Problem &p, int &head, int &tile, int &split)
+__device__ inline bool find_tile(const Args &a, Problem &p, int &head, int &head_end, int &tile, int &split)
 {
-    const int64_t at = blockIdx.x >> 3;
-    const int64_t unit = at / a.G * 8 + (blockIdx.x & 7);
-    head = (int)(at % a.G);
-    if (unit >= a.slots * a.splits)
+    const uint32_t at = blockIdx.x >> 3, turns = a.heads == 1 ? a.G : (a.G + a.heads - 1) / a.heads;
+    const uint32_t round = turns == 1 ? at : at / turns;
+    const uint32_t unit = round * 8 + (blockIdx.x & 7);
+    head = (int)(at - round * turns) * a.heads;
+    head_end = head + a.heads < a.G ? head + a.heads : a.G;
+    if (unit >= (uint32_t)a.slots * a.splits)
         return false;
-    split = (int)(unit % a.splits);
-    const int64_t slot = unit / a.splits;
-    int64_t list;
+    const uint32_t slot = a.splits == 1 ? unit : unit / a.splits;
+    split = (int)(unit - slot * a.splits);
+    int list;
     if (a.tiles) {
         const int2 t = a.tiles[slot];
-        if (t.x < 0)
+        list = __builtin_amdgcn_readfirstlane(t.x);
+        tile = __builtin_amdgcn_readfirstlane(t.y);
+        if (list < 0)
             return false;
-        list = t.x;
-        tile = t.y;
     } else {
-        list = slot % a.lists;
-        tile = (int)(slot / a.lists);
+        tile = a.tiles_per_list == 1 ? 0 : slot / (uint32_t)a.lists;
+        list = slot - tile * (uint32_t)a.lists;
         if (a.last_first)
             tile = a.tiles_per_list - 1 - tile;
     }
-    p.q0 = a.q_offsets[list];
-    p.k0 = a.k_offsets[list];
-    p.nq = (int)(a.q_offsets[list + 1] - p.q0);
-    p.nk = (int)(a.k_offsets[list + 1] - p.k0);
+    p.q0 = uniform(a.q_offsets[list]);
+    p.k0 = uniform(a.k_offsets[list]);
+    p.nq = (int)(uniform(a.q_offsets[list + 1]) - p.q0);
+    p.nk = (int)(uniform(a.k_offsets[list + 1]) - p.k0);
     p.rows = p.nq * a.group;
-    p.head0 = head * a.group;
     p.pos0 = p.nk - p.nq;
     p.causal = a.causal;
-    p.prefix = a.prefix ? a.prefix[list] : 0;
+    p.prefix = a.prefix ? __builtin_amdgcn_readfirstlane(a.prefix[list]) : 0;
     return true;
 }
 
-// Rows of a tile from memory into registers and on into LDS, by THREADS threads of which this is `tid`; row(r) gives the
-// address of row r, or null.
+// Rows of a tile from memory into registers and on into LDS, by THREADS threads of which this is `tid`.  A thread's
+// addresses are 32-bit offsets from the tile's first row, which is the same for all: bytes(r) is that of row r < 128.  Rows
+// behind the last one and elements behind a head's last one are read from the last one's place instead: their
+// scores are masked, or meet zeros in the other operand, or belong to sums that nobody stores.
 template <typename T, int ROWS, int DP, int THREADS> struct Stream {
     using Tile = RecdTile<T, ROWS, DP>;
     using Piece = typename Tile::Piece;
     static constexpr int PT = (Tile::PIECES + THREADS - 1) / THREADS;
     Piece held[PT];
 
-    template <typename Row> __device__ inline void load(int tid, int d, Row row)
+    template <typename Bytes> __device__ inline void load(int tid, const T *first, int rows, int d, Bytes bytes)
     {
         constexpr int PR = DP / Tile::E;
 #pragma unroll
         for (int i = 0; i < PT; i++) {
-            const int piece = tid + i * THREADS, at = piece % PR * Tile::E;
-            held[i] = Piece{};
-            if (piece < Tile::PIECES && at < d) {
-                const T *p = row(piece / PR);
-                if (p)
-                    held[i] = *reinterpret_cast<const Piece *>(p + at);
+            const int piece = tid + i * THREADS, at = piece % PR * Tile::E, r = piece / PR;
+            if (piece < Tile::PIECES) {
+                const uint32_t off = bytes(r < rows ? r : rows - 1) + (uint32_t)((at < d ? at : d - Tile::E) * (int)sizeof(T));
+                held[i] = *reinterpret_cast<const Piece *>(reinterpret_cast<const char *>(first) + off);
             }
         }
+    }
+    // rows that lie `stride` bytes (less than 2^24) apart
+    __device__ inline void load_rows(int tid, const T *first, int rows, int d, uint32_t stride)
+    {
+        load(tid, first, rows, d, [=](int r) { return (uint32_t)__umul24(r, stride); });
     }
     __device__ inline void store(int tid, Tile &t)
     {
@@ -244,7 +259,8 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
     } lds;
     Problem p;
     int head, tile, split;
-    if (!find_tile(a, p, head, tile, split))
+    int head_end;
+    if (!find_tile(a, p, head, head_end, tile, split))
         return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int kept = wave % KEPT, phase = wave / KEPT;
@@ -265,8 +281,8 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
     const int t0 = (int)((int64_t)tiles * part / parts), t1 = (int)((int64_t)tiles * (part + 1) / parts);
     const int wave_t1 = (wave_end + 31) / 32 < t1 ? (wave_end + 31) / 32 : t1;
     const int H = a.G * a.group;
-    const int64_t q_row = p.q0 + query, at_row = q_row * H + p.head0 + head_in;
-    const float slope = a.slopes && there ? a.slopes[p.head0 + head_in] * kRecdLog2e : 0.0f;
+    const int64_t q_row = p.q0 + query, at_row = q_row * H + head * a.group + head_in;
+    const float slope = a.slopes && there ? a.slopes[head * a.group + head_in] * kRecdLog2e : 0.0f;
     const float posf = (float)(p.pos0 + query);
     // the sign of the scale goes into the queries; what is neither capped nor biased stays unscaled until the exponent
     const float scale = fabsf(a.scale), c = scale * kRecdLog2e;
@@ -278,7 +294,7 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
     Frag qf[KS];
 #pragma unroll
     for (int k = 0; k < KS; k++) {
-        qf[k] = recd_row_frag<T>((const T *)a.q + q_row * a.q_stride + (int64_t)(p.head0 + head_in) * a.d, 16 * k, a.d, there,
+        qf[k] = recd_row_frag<T>((const T *)a.q + q_row * a.q_stride + (int64_t)(head * a.group + head_in) * a.d, 16 * k, a.d, there,
                                  lane);
         if (a.scale < 0.0f)
             qf[k] = recd_negated(qf[k]);
@@ -290,14 +306,9 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
         o[d] = recd_f32x16{};
     typename S::Load ks, vs;
     auto load = [&](int t) {
-        ks.load(tid, a.d, [&](int r) -> const T * {
-            const int j = t * 32 + r;
-            return j < p.nk ? (const T *)a.k + (p.k0 + j) * a.k_stride + (int64_t)head * a.d : nullptr;
-        });
-        vs.load(tid, a.d, [&](int r) -> const T * {
-            const int j = t * 32 + r;
-            return j < p.nk ? (const T *)a.v + (p.k0 + j) * a.v_stride + (int64_t)head * a.d : nullptr;
-        });
+        const int64_t at = p.k0 + t * 32;
+        ks.load_rows(tid, (const T *)a.k + at * a.k_stride + head * a.d, p.nk - t * 32, a.d, (uint32_t)a.k_stride * sizeof(T));
+        vs.load_rows(tid, (const T *)a.v + at * a.v_stride + head * a.d, p.nk - t * 32, a.d, (uint32_t)a.v_stride * sizeof(T));
     };
     auto scores = [&](const typename S::Tile &keys, recd_f32x16 &x) {
         x = recd_f32x16{};
@@ -439,6 +450,169 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
     store_columns<T, DT>((T *)a.out + at_row * a.d, o, l == 0.0f ? 0.0f : 1.0f / l, a.d, lane);
 }
 
+// The forward kernel for lists of few rows: a wave to itself goes through one head after the other, whose rows are on
+// their way while it works at the one before, so that a wave finds its list once for all of them.
+template <typename T, int DP, bool CAP> __global__ __launch_bounds__(64, (kResident<T, DP, 1>)) void k_attention_one(Args a)
+{
+    constexpr int KS = DP / 16, DT = DP / 32;
+    using Mma = RecdMma<T>;
+    using Frag = typename Mma::Frag;
+    using S = Shape<T, DP, 1, 1>;
+    __shared__ typename S::Tile kt, vt;
+    Problem p;
+    int head, head_end, tile, split;
+    if (!find_tile(a, p, head, head_end, tile, split))
+        return;
+    const int lane = threadIdx.x, row0 = tile * 32, row = row0 + (lane & 31);
+    if (row0 >= p.rows)
+        return;
+    const bool there = row < p.rows;
+    const int query = p.query(row, a.group), head_in = row - query * a.group;
+    const int lim = there ? p.limit(row, a.group) : 0;
+    const int full = row0 + 32 <= p.rows ? p.limit(row0, a.group) : 0;
+    const int end = p.limit(row0 + 31 < p.rows ? row0 + 31 : p.rows - 1, a.group), tiles = (end + 31) / 32;
+    const int t0 = (int)((int64_t)tiles * split / a.splits), t1 = (int)((int64_t)tiles * (split + 1) / a.splits);
+    const int H = a.G * a.group;
+    const int64_t q_row = p.q0 + query;
+    const float posf = (float)(p.pos0 + query);
+    const float c = a.scale * kRecdLog2e;
+    const Capped<T> capped(a.cap);
+    const float to_cap = CAP ? 2.0f * kRecdLog2e * a.scale / a.cap : 0.0f;
+    Frag qf[KS], qn[KS];
+    float slope = 0.0f, slope_n = 0.0f, m = -INFINITY, l = 0.0f;
+    recd_f32x16 o[DT];
+    typename S::Load ks, vs;
+    auto load_q = [&](int hd) {
+        const int h = hd * a.group + head_in;
+#pragma unroll
+        for (int k = 0; k < KS; k++)
+            qn[k] = recd_row_frag<T>((const T *)a.q + q_row * a.q_stride + (int64_t)h * a.d, 16 * k, a.d, there, lane);
+        slope_n = a.slopes && there ? a.slopes[h] * kRecdLog2e : 0.0f;
+    };
+    auto load = [&](int hd, int t) {
+        const int64_t at = p.k0 + t * 32;
+        ks.load_rows(lane, (const T *)a.k + at * a.k_stride + hd * a.d, p.nk - t * 32, a.d, (uint32_t)a.k_stride * sizeof(T));
+        vs.load_rows(lane, (const T *)a.v + at * a.v_stride + hd * a.d, p.nk - t * 32, a.d, (uint32_t)a.v_stride * sizeof(T));
+    };
+    auto take = [&]() {
+        slope = slope_n;
+        m = -INFINITY;
+        l = 0.0f;
+#pragma unroll
+        for (int k = 0; k < KS; k++)
+            qf[k] = qn[k];
+#pragma unroll
+        for (int d = 0; d < DT; d++)
+            o[d] = recd_f32x16{};
+    };
+    auto write = [&]() {
+        const float sum = l + __shfl_xor(l, 32);
+        const int64_t at_row = q_row * H + head * a.group + head_in;
+        if (!there)
+            return;
+        if (a.splits > 1) {
+            const int64_t at = split * a.part_rows + at_row;
+            if (lane < 32) {
+                a.part_m[at] = m;
+                a.part_l[at] = sum;
+            }
+            store_columns<float, DT>(a.part_o + at * a.d, o, 1.0f, a.d, lane);
+            return;
+        }
+        if (a.lse && lane < 32)
+            a.lse[at_row] = (m + log2f(sum)) * kRecdLn2;  // -inf where the sum is 0
+        store_columns<T, DT>((T *)a.out + at_row * a.d, o, sum == 0.0f ? 0.0f : 1.0f / sum, a.d, lane);
+    };
+    load_q(head);
+    if (t0 < t1)
+        load(head, t0);
+    take();
+    if (t0 == t1)
+        for (; head + 1 < head_end; head++)  // no keys
+            write();
+    for (int t = t0; t < t1;) {
+        S::sync();
+        ks.store(lane, kt);
+        vs.store(lane, vt);
+        S::sync();
+        const bool last = t + 1 == t1, more = last && head + 1 < head_end;
+        if (!last || more)
+            load(more ? head + 1 : head, more ? t0 : t + 1);
+        if (more)
+            load_q(head + 1);
+        const int j0 = t * 32;
+        recd_f32x16 s = {};
+#pragma unroll
+        for (int k = 0; k < KS; k++)
+            s = Mma::mul(kt.rows(0, 16 * k, lane), qf[k], s);
+        auto finish = [&](auto registers) {
+            constexpr int NR = registers.value;
+            if (a.slopes) {
+                const float far = posf - (float)(j0 + (lane >> 5));
+#pragma unroll
+                for (int r = 0; r < NR; r++) {
+                    const float bias = -slope * fabsf(far - (float)recd_score_row(r, 0));
+                    float unused;
+                    s[r] = CAP ? capped.value(s[r] * to_cap, bias, unused) : s[r] * c + bias;
+                }
+            } else {
+#pragma unroll
+                for (int r = 0; r < NR; r++) {
+                    float unused;
+                    s[r] = CAP ? capped.value(s[r] * to_cap, 0.0f, unused) : s[r] * c;
+                }
+            }
+            if (j0 + 2 * NR > full) {
+                asm volatile("");
+                const int to = lim - j0 - (lane >> 5);
+#pragma unroll
+                for (int r = 0; r < NR; r++)
+                    s[r] = recd_score_row(r, 0) >= to ? -INFINITY : s[r];
+            }
+            float top = s[0];
+#pragma unroll
+            for (int r = 1; r < NR; r++)
+                top = fmaxf(top, s[r]);
+            top = fmaxf(top, __shfl_xor(top, 32)) - kLift<T>;
+            const float now = fmaxf(m, top), from = now == -INFINITY ? 0.0f : now;
+            if (t > t0) {
+                const float f = recd_exp2(m - from);
+                l *= f;
+#pragma unroll
+                for (int d = 0; d < DT; d++)
+#pragma unroll
+                    for (int r = 0; r < 16; r++)
+                        o[d][r] *= f;
+            }
+            m = now;
+#pragma unroll
+            for (int r = 0; r < NR; r++) {
+                s[r] = recd_exp2(s[r] - from);
+                l += s[r];
+            }
+#pragma unroll
+            for (int h = 0; h < NR / 8; h++) {
+                const Frag pf = recd_sums_frag<T>(s, h);
+#pragma unroll
+                for (int d = 0; d < DT; d++)
+                    o[d] = Mma::mul(vt.columns(16 * h, 32 * d, lane), pf, o[d]);
+            }
+        };
+        if (end - j0 <= 16)  // the other registers hold no key of the list
+            finish(std::integral_constant<int, 8>{});
+        else
+            finish(std::integral_constant<int, 16>{});
+        t++;
+        if (more) {
+            write();
+            head++;
+            t = t0;
+            take();
+        }
+    }
+    write();
+}
+
 // Joins the splits of the forward pass: 2^dlog threads a row, four elements each.
 template <typename T>
 __global__ __launch_bounds__(256) void k_attention_join(int64_t rows, int d, int dlog, int splits,
@@ -468,29 +642,40 @@ __global__ __launch_bounds__(256) void k_attention_join(int64_t rows, int d, int
         lse[row] = (m + log2f(l)) * kRecdLn2;
 }
 
-// {list, tile} of the slots of tiles of R rows; `group` rows for every entry of the offsets.
-__global__ void k_attention_tiles(int64_t lists, int64_t slots, int group, int R, const int64_t *__restrict__ offsets,
-                                  int2 *tiles)
+// A side whose tiles are listed.  `keys`: its tiles are of keys, else of queries, `group` rows each.
+struct Side {
+    int64_t slots;
+    int group, R;
+    bool keys;
+    int2 *tiles;
+};
+
+// {list, tile} of a side's slots; a row of blocks for each side.
+__global__ __launch_bounds__(256) void k_attention_tiles(int64_t lists, const int64_t *__restrict__ q_offsets,
+                                                         const int64_t *__restrict__ k_offsets, Side one, Side two)
 {
+    const Side &side = blockIdx.y ? two : one;
+    const int64_t *offsets = side.keys ? k_offsets : q_offsets;
     const int64_t list = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
     if (list >= lists)
         return;
-    const int64_t b = offsets[list] * group, e = offsets[list + 1] * group;
-    const int64_t s0 = b / R + list, n = (e - b + R - 1) / R;
-    const int64_t s1 = list + 1 < lists ? e / R + list + 1 : slots;
-    for (int64_t s = s0 < 0 ? 0 : s0; s < s1 && s < slots; s++)
-        tiles[s] = s - s0 < n ? make_int2((int)list, (int)(s - s0)) : make_int2(-1, 0);
+    const int64_t b = offsets[list] * side.group, e = offsets[list + 1] * side.group;
+    const int64_t s0 = b / side.R + list, n = (e - b + side.R - 1) / side.R;
+    const int64_t s1 = list + 1 < lists ? e / side.R + list + 1 : side.slots;
+    for (int64_t s = s0 < 0 ? 0 : s0; s < s1 && s < side.slots; s++)
+        side.tiles[s] = s - s0 < n ? make_int2((int)list, (int)(s - s0)) : make_int2(-1, 0);
 }
 
-// The same for few lists (one block), in the order of the tiles' work, most first: lists of a few very different lengths
-// would otherwise leave most compute units to wait for the last long one.  `keys`: the tiles are of keys.  Tiles of
-// about equal work stand in any order.
-__global__ __launch_bounds__(1024) void k_attention_tiles_by_work(int lists, int slots, int group, int R, bool keys, bool causal,
-                                                                  const int64_t *__restrict__ q_offsets,
+// The same for few lists (a block for each side), in the order of the tiles' work, most first: lists of a few very
+// different lengths would otherwise leave most compute units to wait for the last long one.  Tiles of about equal work
+// stand in any order.
+__global__ __launch_bounds__(1024) void k_attention_tiles_by_work(int lists, bool causal, const int64_t *__restrict__ q_offsets,
                                                                   const int64_t *__restrict__ k_offsets,
-                                                                  const int32_t *__restrict__ prefix, int2 *tiles)
+                                                                  const int32_t *__restrict__ prefix, Side one, Side two)
 {
-    __shared__ int nq[kMostSorted], nk[kMostSorted], pre[kMostSorted], count[256], most, total;
+    __shared__ int nq[kMostSorted], nk[kMostSorted], pre[kMostSorted], count[256], wave_sum[4], most;
+    const Side &side = blockIdx.x ? two : one;
+    const int group = side.group, R = side.R;
     if (threadIdx.x < 256)
         count[threadIdx.x] = 0;
     if (threadIdx.x == 0)
@@ -501,76 +686,64 @@ __global__ __launch_bounds__(1024) void k_attention_tiles_by_work(int lists, int
         nq[l] = (int)(q_offsets[l + 1] - q_offsets[l]);
         nk[l] = (int)(k_offsets[l + 1] - k_offsets[l]);
         pre[l] = prefix ? prefix[l] : 0;
-        const int n = keys ? nq[l] : nk[l];
+        const int n = side.keys ? nq[l] : nk[l];
         top = n > top ? n : top;
     }
     atomicMax(&most, top);
     __syncthreads();
     // rows (of queries or keys) that tile i of list l goes through, in 256ths of the longest list's
+    const float unit = 255.0f / (float)most;
     auto bucket = [&](int l, int i) {
-        int64_t work;
-        if (keys) {
+        int work;
+        if (side.keys) {
             const int first = i * R, pos0 = nk[l] - nq[l];
             work = causal && pre[l] <= first && first > pos0 ? nq[l] - (first - pos0) : nq[l];
         } else {
-            int64_t last = (int64_t)(i + 1) * R / group;
+            int last = group == 1 ? (i + 1) * R : (int)((int64_t)(i + 1) * R / group);
             last = last < nq[l] ? last : nq[l];
-            int64_t end = nk[l] - nq[l] + last;
+            int end = nk[l] - nq[l] + last;
             end = end > pre[l] ? end : pre[l];
             work = causal && end < nk[l] ? end : nk[l];
         }
-        work = work < 0 ? 0 : work;
-        return 255 - (int)(work * 255 / most);
+        const int b = 255 - (int)((float)(work < 0 ? 0 : work) * unit);
+        return b < 0 ? 0 : b;
     };
     const int lane = threadIdx.x & 31;
     for (int l = threadIdx.x >> 5; l < lists; l += 32) {
-        const int n = ((keys ? nk[l] : nq[l] * group) + R - 1) / R;
+        const int n = ((side.keys ? nk[l] : nq[l] * group) + R - 1) / R;
         for (int i = lane; i < n; i += 32)
             atomicAdd(&count[bucket(l, i)], 1);
     }
     __syncthreads();
-    if (threadIdx.x == 0) {
-        int at = 0;
-        for (int b = 0; b < 256; b++) {
-            const int n = count[b];
-            count[b] = at;
-            at += n;
+    // where every bucket starts
+    int mine = 0, sum = 0;
+    if (threadIdx.x < 256) {
+        sum = mine = count[threadIdx.x];
+        for (int o = 1; o < 64; o <<= 1) {
+            const int other = __shfl_up(sum, o);
+            sum += (int)(threadIdx.x & 63) >= o ? other : 0;
         }
-        total = at;
+        if ((threadIdx.x & 63) == 63)
+            wave_sum[threadIdx.x >> 6] = sum;
     }
     __syncthreads();
+    if (threadIdx.x < 256) {
+        for (int w = 0; w < (int)(threadIdx.x >> 6); w++)
+            sum += wave_sum[w];
+        count[threadIdx.x] = sum - mine;
+    }
+    const int total = wave_sum[0] + wave_sum[1] + wave_sum[2] + wave_sum[3];
+    __syncthreads();
     for (int l = threadIdx.x >> 5; l < lists; l += 32) {
-        const int n = ((keys ? nk[l] : nq[l] * group) + R - 1) / R;
+        const int n = ((side.keys ? nk[l] : nq[l] * group) + R - 1) / R;
         for (int i = lane; i < n; i += 32) {
             const int at = atomicAdd(&count[bucket(l, i)], 1);
-            if (at < slots)
-                tiles[at] = make_int2(l, i);
+            if (at < side.slots)
+                side.tiles[at] = make_int2(l, i);
         }
     }
-    for (int s = total + threadIdx.x; s < slots; s += 1024)
-        tiles[s] = make_int2(-1, 0);
-}
-
-// delta = sum over a head of g * o: 2^dlog lanes a row, a piece of 16 bytes each.
-template <typename T>
-__global__ __launch_bounds__(256) void k_attention_delta(int64_t rows, int d, int dlog, const T *__restrict__ out,
-                                                         const T *__restrict__ g, float *delta)
-{
-    constexpr int E = 16 / sizeof(T);
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i >> dlog;
-    const int col = (int)(i & ((1 << dlog) - 1)) * E;
-    float s = 0.0f;
-    if (row < rows && col < d) {
-        float x[E], y[E];
-        recd_load16(out + row * d + col, x);
-        recd_load16(g + row * d + col, y);
-        for (int e = 0; e < E; e++)
-            s += x[e] * y[e];
-    }
-    for (int o = (1 << dlog) >> 1; o; o >>= 1)
-        s += __shfl_xor(s, o);
-    if (row < rows && col == 0)
-        delta[row] = s;
+    for (int64_t s = total + threadIdx.x; s < side.slots; s += 1024)
+        side.tiles[s] = make_int2(-1, 0);
 }
 
 // fp16: the largest |g| and |v| (as bits, whose order is the numbers'), and from them the power of two for ds.
@@ -614,6 +787,7 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
 {
     using S = Shape<T, DP, KEPT, PHASES>;
     static_assert(KEPT == 1 || PHASES == 1);
+    constexpr bool ONE = KEPT * PHASES == 1;
     constexpr int KS = DP / 16, DT = DP / 32, BUFS = S::SHARED ? 2 : 1;
     using Mma = RecdMma<T>;
     using Frag = typename Mma::Frag;
@@ -621,8 +795,8 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
         typename S::Tile k[S::OWN][BUFS], v[S::OWN][BUFS];
     } lds;
     Problem p;
-    int head, tile, split;
-    if (!find_tile(a, p, head, tile, split))
+    int head0, head_end, tile, split;
+    if (!find_tile(a, p, head0, head_end, tile, split))
         return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int kept = wave % KEPT, phase = wave / KEPT;
@@ -640,53 +814,86 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
     const int wave_full = row0 + 32 <= p.rows ? p.limit(row0, a.group) : 0;
     const int tiles = (p.limit(end - 1, a.group) + 31) / 32, t0 = tiles * phase / PHASES, t1 = tiles * (phase + 1) / PHASES;
     const int H = a.G * a.group;
-    const int64_t q_row = p.q0 + query, at_row = q_row * H + p.head0 + head_in;
-    const float slope = a.slopes && there ? a.slopes[p.head0 + head_in] * kRecdLog2e : 0.0f;
+    const int64_t q_row = p.q0 + query;
     const float posf = (float)(p.pos0 + query);
-    float from = there ? a.lse_in[at_row] * kRecdLog2e : 0.0f;
-    if (from == -INFINITY)
-        from = 0.0f;  // sees nothing
-    const float lift = kHalf<T> ? *a.lift : 1.0f, delta = there ? a.delta[at_row] * lift : 0.0f;
+    const float lift = kHalf<T> ? *a.lift : 1.0f;
     const float c = a.scale * kRecdLog2e;
     const Capped<T> capped(a.cap);
     const float to_cap = CAP ? 2.0f * kRecdLog2e * a.scale / a.cap : 0.0f;
 
-    Frag qf[KS], gf[KS];
+    Frag qf[KS], gf[KS], qn[KS], gn[KS];
+    float slope_n = 0.0f, from_n = 0.0f, delta_n = 0.0f, slope = 0.0f, from = 0.0f, delta = 0.0f;
+    typename S::Load ks, vs;
+    // a head's queries, gradients and delta = g . o (which the gradients by keys need too)
+    auto load_q = [&](int head) {
+        const int h = head * a.group + head_in;
+        const int64_t at = q_row * H + h;
+        delta_n = 0.0f;
 #pragma unroll
-    for (int k = 0; k < KS; k++) {
-        qf[k] = recd_row_frag<T>((const T *)a.q + q_row * a.q_stride + (int64_t)(p.head0 + head_in) * a.d, 16 * k, a.d, there,
-                                 lane);
-        gf[k] = recd_row_frag<T>((const T *)a.g + at_row * a.d, 16 * k, a.d, there, lane);
-    }
+        for (int k = 0; k < KS; k++) {
+            qn[k] = recd_row_frag<T>((const T *)a.q + q_row * a.q_stride + (int64_t)h * a.d, 16 * k, a.d, there, lane);
+            gn[k] = recd_row_frag<T>((const T *)a.g + at * a.d, 16 * k, a.d, there, lane);
+            const Frag o = recd_row_frag<T>((const T *)a.out_in + at * a.d, 16 * k, a.d, there, lane);
+#pragma unroll
+            for (int e = 0; e < 8; e++)
+                delta_n += (float)gn[k][e] * (float)o[e];
+        }
+        delta_n += __shfl_xor(delta_n, 32);
+        if (there && lane < 32 && phase == 0)
+            a.delta[at] = delta_n;
+        slope_n = a.slopes && there ? a.slopes[h] * kRecdLog2e : 0.0f;
+        from_n = there ? a.lse_in[at] * kRecdLog2e : 0.0f;
+    };
+    auto load = [&](int head, int t) {
+        const int64_t at = p.k0 + t * 32;
+        ks.load_rows(tid, (const T *)a.k + at * a.k_stride + head * a.d, p.nk - t * 32, a.d, (uint32_t)a.k_stride * sizeof(T));
+        vs.load_rows(tid, (const T *)a.v + at * a.v_stride + head * a.d, p.nk - t * 32, a.d, (uint32_t)a.v_stride * sizeof(T));
+    };
+    auto take = [&]() {
+        slope = slope_n;
+        from = from_n == -INFINITY ? 0.0f : from_n;  // (a row that sees nothing)
+        delta = delta_n * lift;
+#pragma unroll
+        for (int k = 0; k < KS; k++) {
+            qf[k] = qn[k];
+            gf[k] = gn[k];
+        }
+    };
     recd_f32x16 o[DT];
+    int head = head0;
+    load_q(head);
+    if (t0 < t1)
+        load(head, t0);
+    take();
 #pragma unroll
     for (int d = 0; d < DT; d++)
         o[d] = recd_f32x16{};
-    typename S::Load ks, vs;
-    auto load = [&](int t) {
-        ks.load(tid, a.d, [&](int r) -> const T * {
-            const int j = t * 32 + r;
-            return j < p.nk ? (const T *)a.k + (p.k0 + j) * a.k_stride + (int64_t)head * a.d : nullptr;
-        });
-        vs.load(tid, a.d, [&](int r) -> const T * {
-            const int j = t * 32 + r;
-            return j < p.nk ? (const T *)a.v + (p.k0 + j) * a.v_stride + (int64_t)head * a.d : nullptr;
-        });
+    auto write = [&]() {
+        if (there && phase == 0)
+            store_columns<T, DT>((T *)a.gq + q_row * a.gq_stride + (int64_t)(head * a.group + head_in) * a.d, o,
+                                 (CAP ? 4.0f : 1.0f) * a.scale / lift, a.d, lane);
     };
-    if (t0 < t1)
-        load(t0);
-    for (int t = t0; t < t1; t++) {
+    if (t0 == t1)
+        for (; ONE && head + 1 < head_end; head++) {  // no keys: zeros
+            write();
+            load_q(head + 1);
+        }
+    // one wave goes through the tiles of one head after the other
+    for (int t = t0; t < t1;) {
         const int buf = BUFS == 1 ? 0 : t & 1;
         if constexpr (BUFS == 1)
             S::sync();
         ks.store(tid, kt[buf]);
         vs.store(tid, vt[buf]);
         S::sync();
-        if (t + 1 < t1)
-            load(t + 1);
+        const bool last = t + 1 == t1, more = ONE && last && head + 1 < head_end;
+        if (!last || more)
+            load(more ? head + 1 : head, more ? t0 : t + 1);
+        if constexpr (ONE)
+            if (more)
+                load_q(head + 1);
         const int j0 = t * 32;
-        if (j0 >= wave_end)
-            continue;
+        if (j0 < wave_end) {
         recd_f32x16 s = {}, dp = {};
 #pragma unroll
         for (int k = 0; k < KS; k++) {
@@ -699,37 +906,55 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
             const float z = CAP ? capped.value(x * to_cap, more, quarter) : x * c + more;
             return recd_exp2(z) * (d * lift - delta) * quarter;
         };
-        if (a.slopes) {
-            const float far = posf - (float)(j0 + (lane >> 5));
+        auto finish = [&](auto registers) {
+            constexpr int NR = registers.value;
+            if (a.slopes) {
+                const float far = posf - (float)(j0 + (lane >> 5));
 #pragma unroll
-            for (int r = 0; r < 16; r++)
-                s[r] = ds_of(s[r], dp[r], -slope * fabsf(far - (float)recd_score_row(r, 0)) - from);
-        } else {
+                for (int r = 0; r < NR; r++)
+                    s[r] = ds_of(s[r], dp[r], -slope * fabsf(far - (float)recd_score_row(r, 0)) - from);
+            } else {
 #pragma unroll
-            for (int r = 0; r < 16; r++)
-                s[r] = ds_of(s[r], dp[r], -from);
+                for (int r = 0; r < NR; r++)
+                    s[r] = ds_of(s[r], dp[r], -from);
+            }
+            if (j0 + 2 * NR > wave_full) {
+                asm volatile("");  // a branch: only the tiles at the mask's edge pay for it
+                const int to = lim - j0 - (lane >> 5);
+#pragma unroll
+                for (int r = 0; r < NR; r++)
+                    s[r] = recd_score_row(r, 0) >= to ? 0.0f : s[r];
+            }
+#pragma unroll
+            for (int h = 0; h < NR / 8; h++) {
+                const Frag sf = recd_sums_frag<T>(s, h);
+#pragma unroll
+                for (int d = 0; d < DT; d++)
+                    o[d] = Mma::mul(kt[buf].columns(16 * h, 32 * d, lane), sf, o[d]);
+            }
+        };
+        if (ONE && wave_end - j0 <= 16)  // the other registers hold no key of the list
+            finish(std::integral_constant<int, 8>{});
+        else
+            finish(std::integral_constant<int, 16>{});
         }
-        if (j0 + 32 > wave_full) {
-            asm volatile("");  // a branch: only the tiles at the mask's edge pay for it
+        t++;
+        if constexpr (ONE)
+            if (more) {
+                write();
+                head++;
+                t = t0;
+                take();
 #pragma unroll
-            for (int r = 0; r < 16; r++)
-                s[r] = j0 + recd_score_row(r, lane) >= lim ? 0.0f : s[r];
-        }
-#pragma unroll
-        for (int h = 0; h < 2; h++) {
-            const Frag sf = recd_sums_frag<T>(s, h);
-#pragma unroll
-            for (int d = 0; d < DT; d++)
-                o[d] = Mma::mul(kt[buf].columns(16 * h, 32 * d, lane), sf, o[d]);
-        }
+                for (int d = 0; d < DT; d++)
+                    o[d] = recd_f32x16{};
+            }
     }
     if constexpr (PHASES > 1) {
         static_assert(sizeof(lds) >= 64 * 16 * DT * sizeof(float));
         join_sums<DT, PHASES>(o, reinterpret_cast<float *>(&lds), 0, phase, lane);
     }
-    if (there && phase == 0)
-        store_columns<T, DT>((T *)a.gq + q_row * a.gq_stride + (int64_t)(p.head0 + head_in) * a.d, o,
-                             (CAP ? 4.0f : 1.0f) * a.scale / lift, a.d, lane);
+    write();
 }
 
 // Keys stay, queries and their gradients stream past.  What a score needs of its row stands in LDS in the order of
@@ -738,6 +963,7 @@ template <typename T, int DP, int KEPT, int PHASES, bool CAP>
 __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void k_attention_grad_kv(Args a)
 {
     using S = Shape<T, DP, KEPT, PHASES>;
+    constexpr bool ONE = KEPT * PHASES == 1;
     constexpr int KS = DP / 16, DT = DP / 32, BUFS = S::SHARED ? 2 : 1;
     using Mma = RecdMma<T>;
     using Frag = typename Mma::Frag;
@@ -752,8 +978,8 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
         alignas(16) int lim[S::OWN][BUFS][S::ROWS];
     } lds;
     Problem p;
-    int head, tile, split;
-    if (!find_tile(a, p, head, tile, split))
+    int head0, head_end, tile, split;
+    if (!find_tile(a, p, head0, head_end, tile, split))
         return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int kept = wave % KEPT, phase = wave / KEPT;
@@ -769,24 +995,22 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
     const bool there = j < p.nk;
     const float jf = (float)j;
     const int H = a.G * a.group;
-    Frag kf[IN_LDS ? 1 : KS], vf[IN_LDS ? 1 : KS];
+    Frag kf[IN_LDS ? 1 : KS], vf[IN_LDS ? 1 : KS], kn[IN_LDS ? 1 : KS], vn[IN_LDS ? 1 : KS];
     const int kept_at = IN_LDS ? (32 * kept + (lane & 31)) * lds.k.LD + (lane >> 5) * 8 : 0;
+    auto load_kept = [&](int head) {
 #pragma unroll
-    for (int k = 0; k < KS; k++) {
-        const int i = IN_LDS ? 0 : k;
-        if (IN_LDS && k % PHASES != phase)
-            continue;  // the phases share the writing
-        kf[i] = recd_row_frag<T>((const T *)a.k + (p.k0 + j) * a.k_stride + (int64_t)head * a.d, 16 * k, a.d, there, lane);
-        vf[i] = recd_row_frag<T>((const T *)a.v + (p.k0 + j) * a.v_stride + (int64_t)head * a.d, 16 * k, a.d, there, lane);
-        if constexpr (IN_LDS) {
-            *reinterpret_cast<Frag *>(lds.k.at + kept_at + 16 * k) = kf[0];
-            *reinterpret_cast<Frag *>(lds.v.at + kept_at + 16 * k) = vf[0];
+        for (int k = 0; k < KS; k++) {
+            const int i = IN_LDS ? 0 : k;
+            if (IN_LDS && k % PHASES != phase)
+                continue;  // the phases share the writing
+            kn[i] = recd_row_frag<T>((const T *)a.k + (p.k0 + j) * a.k_stride + (int64_t)head * a.d, 16 * k, a.d, there, lane);
+            vn[i] = recd_row_frag<T>((const T *)a.v + (p.k0 + j) * a.v_stride + (int64_t)head * a.d, 16 * k, a.d, there, lane);
+            if constexpr (IN_LDS) {
+                *reinterpret_cast<Frag *>(lds.k.at + kept_at + 16 * k) = kn[0];
+                *reinterpret_cast<Frag *>(lds.v.at + kept_at + 16 * k) = vn[0];
+            }
         }
-    }
-    recd_f32x16 dk[DT], dv[DT];
-#pragma unroll
-    for (int d = 0; d < DT; d++)
-        dk[d] = dv[d] = recd_f32x16{};
+    };
     // probabilities are held 2^kLiftP larger, by their exponents; ds by that and, from dp on, the rest of its lift
     const float lift = kHalf<T> ? *a.lift : 1.0f, lift_dp = lift * recd_exp2(-kLiftP<T>);
     const float c = a.scale * kRecdLog2e;
@@ -805,39 +1029,61 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
     float n_from = 0.0f, n_delta = 0.0f, n_slope = 0.0f;
     float n_pos = 0.0f;
     int n_lim = 0;
-    auto load = [&](int t) {
-        auto at = [&](int r, int &query, int &h) {
-            query = p.query(r, a.group);
-            h = p.head0 + r - query * a.group;
+    auto load = [&](int head, int t) {
+        // the tile's first row is head `odd` of its query's; row r is then query (odd + r) / group from there
+        const int row = t * S::ROWS, q_first = p.query(row, a.group), odd = row - q_first * a.group;
+        auto query_of = [&](int r) { return a.group == 1 ? r : (int)__umulhi(odd + r, a.by_group); };
+        auto rows_at = [&](uint32_t stride) {
+            return [=](int r) {
+                const int query = query_of(r);
+                return (uint32_t)__umul24(query, stride) + (uint32_t)((odd + r - query * a.group) * a.d * (int)sizeof(T));
+            };
         };
-        qs.load(tid, a.d, [&](int r) -> const T * {
-            int query, h;
-            at(t * S::ROWS + r, query, h);
-            return t * S::ROWS + r < p.rows ? (const T *)a.q + (p.q0 + query) * a.q_stride + (int64_t)h * a.d : nullptr;
-        });
-        gs.load(tid, a.d, [&](int r) -> const T * {
-            int query, h;
-            at(t * S::ROWS + r, query, h);
-            return t * S::ROWS + r < p.rows ? (const T *)a.g + ((p.q0 + query) * H + h) * a.d : nullptr;
-        });
-        const int r = t * S::ROWS + tid;
+        const int64_t at = p.q0 + q_first;
+        qs.load(tid, (const T *)a.q + at * a.q_stride + head * a.group * a.d, p.rows - row, a.d,
+                rows_at((uint32_t)a.q_stride * sizeof(T)));
+        gs.load(tid, (const T *)a.g + (at * H + head * a.group) * a.d, p.rows - row, a.d, rows_at(H * a.d * sizeof(T)));
         n_from = n_delta = n_slope = 0.0f;
         n_pos = 0.0f;
         n_lim = 0;
-        if (tid < S::ROWS && r < p.rows) {
-            int query, h;
-            at(r, query, h);
+        if (tid < S::ROWS && row + tid < p.rows) {
+            const int in = query_of(tid), query = q_first + in, h = head * a.group + odd + tid - in * a.group;
             n_from = a.lse_in[(p.q0 + query) * H + h] * kRecdLog2e;
             n_from = (n_from == -INFINITY ? 0.0f : -n_from) + kLiftP<T>;
             n_delta = a.delta[(p.q0 + query) * H + h] * lift_dp;
             n_slope = a.slopes ? a.slopes[h] * kRecdLog2e : 0.0f;
-            n_lim = p.limit(r, a.group);
+            n_lim = p.limit_at(query);
             n_pos = (float)(p.pos0 + query);
         }
     };
+    int head = head0;
+    load_kept(head);
     if (t0 < t1)
-        load(t0);
-    for (int t = t0; t < t1; t++) {
+        load(head, t0);
+    auto take = [&]() {
+        if constexpr (!IN_LDS)
+#pragma unroll
+            for (int k = 0; k < KS; k++) {
+                kf[k] = kn[k];
+                vf[k] = vn[k];
+            }
+    };
+    take();
+    recd_f32x16 dk[DT], dv[DT];
+#pragma unroll
+    for (int d = 0; d < DT; d++)
+        dk[d] = dv[d] = recd_f32x16{};
+    auto write = [&]() {
+        if (!there || phase)
+            return;
+        store_columns<T, DT>((T *)a.gk + (p.k0 + j) * a.gk_stride + (int64_t)head * a.d, dk, (CAP ? 4.0f : 1.0f) * a.scale / lift,
+                             a.d, lane);
+        store_columns<T, DT>((T *)a.gv + (p.k0 + j) * a.gv_stride + (int64_t)head * a.d, dv, recd_exp2(-kLiftP<T>), a.d, lane);
+    };
+    if (t0 == t1)
+        for (; ONE && head + 1 < head_end; head++)  // no queries see these keys: zeros
+            write();
+    for (int t = t0; t < t1;) {
         const int buf = BUFS == 1 ? 0 : t & 1;
         if constexpr (BUFS == 1)
             S::sync();
@@ -852,13 +1098,16 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
             row_pos[buf][i] = n_pos;
         }
         S::sync();
-        if (t + 1 < t1)
-            load(t + 1);
+        const bool last = t + 1 == t1, more = ONE && last && head + 1 < head_end;
+        if (!last || more)
+            load(more ? head + 1 : head, more ? t0 : t + 1);
+        if constexpr (ONE)
+            if (more)
+                load_kept(head + 1);
         const int row0 = t * S::ROWS + sub;
         const bool whole = row0 + 32 <= p.rows;
         // (tile row 31 is the product's row 31, and limits do not fall: what it does not see, no row sees)
-        if (j0 >= p.nk || row0 >= p.rows || (whole && __builtin_amdgcn_readfirstlane(row_lim[buf][sub + 31]) <= j0))
-            continue;
+        if (j0 < p.nk && row0 < p.rows && !(whole && __builtin_amdgcn_readfirstlane(row_lim[buf][sub + 31]) <= j0)) {
         recd_f32x16 s = {}, dp = {};
 #pragma unroll
         for (int k = 0; k < KS; k++) {
@@ -879,57 +1128,72 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
             s[r] = recd_exp2(z);
             dp[r] = s[r] * (dp[r] * lift_dp - delta) * quarter;
         };
-        if (a.slopes) {
+        auto finish = [&](auto registers) {
+            constexpr int NR = registers.value;
+            if (a.slopes) {
 #pragma unroll
-            for (int r = 0; r < 16; r += 4) {
-                const int row = sub + recd_sums_row(r, lane);
-                const recd_f32x4 from = *reinterpret_cast<const recd_f32x4 *>(&row_from[buf][row]);
-                const recd_f32x4 delta = *reinterpret_cast<const recd_f32x4 *>(&row_delta[buf][row]);
-                const recd_f32x4 slope = *reinterpret_cast<const recd_f32x4 *>(&row_slope[buf][row]);
-                const recd_f32x4 pos = *reinterpret_cast<const recd_f32x4 *>(&row_pos[buf][row]);
+                for (int r = 0; r < NR; r += 4) {
+                    const int row = sub + recd_sums_row(r, lane);
+                    const recd_f32x4 from = *reinterpret_cast<const recd_f32x4 *>(&row_from[buf][row]);
+                    const recd_f32x4 delta = *reinterpret_cast<const recd_f32x4 *>(&row_delta[buf][row]);
+                    const recd_f32x4 slope = *reinterpret_cast<const recd_f32x4 *>(&row_slope[buf][row]);
+                    const recd_f32x4 pos = *reinterpret_cast<const recd_f32x4 *>(&row_pos[buf][row]);
 #pragma unroll
-                for (int q = 0; q < 4; q++)
-                    score(r + q, from[q] - slope[q] * fabsf(pos[q] - jf), delta[q]);
+                    for (int q = 0; q < 4; q++)
+                        score(r + q, from[q] - slope[q] * fabsf(pos[q] - jf), delta[q]);
+                }
+            } else {
+#pragma unroll
+                for (int r = 0; r < NR; r += 4) {
+                    const int row = sub + recd_sums_row(r, lane);
+                    const recd_f32x4 from = *reinterpret_cast<const recd_f32x4 *>(&row_from[buf][row]);
+                    const recd_f32x4 delta = *reinterpret_cast<const recd_f32x4 *>(&row_delta[buf][row]);
+#pragma unroll
+                    for (int q = 0; q < 4; q++)
+                        score(r + q, from[q], delta[q]);
+                }
             }
-        } else {
+            // (tile row 0 is the product's row 0, and limits do not fall: what its rows all see, the others see)
+            if (!whole || __builtin_amdgcn_readfirstlane(row_lim[buf][sub]) < j0 + 32) {
+                asm volatile("");
 #pragma unroll
-            for (int r = 0; r < 16; r += 4) {
-                const int row = sub + recd_sums_row(r, lane);
-                const recd_f32x4 from = *reinterpret_cast<const recd_f32x4 *>(&row_from[buf][row]);
-                const recd_f32x4 delta = *reinterpret_cast<const recd_f32x4 *>(&row_delta[buf][row]);
-#pragma unroll
-                for (int q = 0; q < 4; q++)
-                    score(r + q, from[q], delta[q]);
+                for (int r = 0; r < NR; r++)
+                    if (j >= row_lim[buf][sub + recd_sums_row(r, lane)])
+                        s[r] = dp[r] = 0.0f;
             }
-        }
-        // (tile row 0 is the product's row 0, and limits do not fall: what its rows all see, the others see)
-        if (!whole || __builtin_amdgcn_readfirstlane(row_lim[buf][sub]) < j0 + 32) {
-            asm volatile("");
 #pragma unroll
-            for (int r = 0; r < 16; r++)
-                if (j >= row_lim[buf][sub + recd_sums_row(r, lane)])
-                    s[r] = dp[r] = 0.0f;
-        }
+            for (int h = 0; h < NR / 8; h++) {
+                const Frag pf = recd_sums_frag<T>(s, h), sf = recd_sums_frag<T>(dp, h);
 #pragma unroll
-        for (int h = 0; h < 2; h++) {
-            const Frag pf = recd_sums_frag<T>(s, h), sf = recd_sums_frag<T>(dp, h);
-#pragma unroll
-            for (int d = 0; d < DT; d++) {
-                dv[d] = Mma::mul(gt[buf].columns(sub + 16 * h, 32 * d, lane), pf, dv[d]);
-                dk[d] = Mma::mul(qt[buf].columns(sub + 16 * h, 32 * d, lane), sf, dk[d]);
+                for (int d = 0; d < DT; d++) {
+                    dv[d] = Mma::mul(gt[buf].columns(sub + 16 * h, 32 * d, lane), pf, dv[d]);
+                    dk[d] = Mma::mul(qt[buf].columns(sub + 16 * h, 32 * d, lane), sf, dk[d]);
+                }
             }
+        };
+        if (ONE && p.rows - row0 <= 16)  // the other registers hold no row of the list
+            finish(std::integral_constant<int, 8>{});
+        else
+            finish(std::integral_constant<int, 16>{});
         }
+        t++;
+        if constexpr (ONE)
+            if (more) {
+                write();
+                head++;
+                t = t0;
+                take();
+#pragma unroll
+                for (int d = 0; d < DT; d++)
+                    dk[d] = dv[d] = recd_f32x16{};
+            }
     }
     if constexpr (PHASES > 1) {
         static_assert(sizeof(lds) >= KEPT * 64 * 16 * DT * sizeof(float));
         join_sums<DT, PHASES>(dk, reinterpret_cast<float *>(&lds), kept, phase, lane);
         join_sums<DT, PHASES>(dv, reinterpret_cast<float *>(&lds), kept, phase, lane);
     }
-    if (!there || phase)
-        return;
-    store_columns<T, DT>((T *)a.gk + (p.k0 + j) * a.gk_stride + (int64_t)head * a.d, dk, (CAP ? 4.0f : 1.0f) * a.scale / lift, a.d,
-                         lane);
-    store_columns<T, DT>((T *)a.gv + (p.k0 + j) * a.gv_stride + (int64_t)head * a.d, dv, recd_exp2(-kLiftP<T>), a.d, lane);
+    write();
 }
 
 // Offsets that do not rise from 0 to the number of rows, or pass the caller's bound of a list's length.
@@ -974,6 +1238,8 @@ recd_status check_attention(recd_ctx *ctx, const recd_attention *a, const void *
     if (a->q_stride < (int64_t)a->heads * a->head_dim || a->k_stride < (int64_t)a->kv_heads * a->head_dim ||
         a->v_stride < (int64_t)a->kv_heads * a->head_dim)
         return recd_fail(ctx, RECD_EINVAL, "a stride is less than a row");
+    if (a->q_stride * es >= 1 << 24 || a->k_stride * es >= 1 << 24 || a->v_stride * es >= 1 << 24)
+        return recd_fail(ctx, RECD_EINVAL, "rows 16 MiB apart and more");
     if (((uintptr_t)q | (uintptr_t)k | (uintptr_t)v) % 16 || (a->q_stride | a->k_stride | a->v_stride) * es % 16)
         return recd_fail(ctx, RECD_EINVAL, "q, k, v and their strides must be aligned to 16 bytes");
     return RECD_OK;
@@ -1004,6 +1270,7 @@ Args common_args(const recd_attention *d, const void *q, const void *k, const vo
     a.G = d->kv_heads;
     a.group = d->heads / d->kv_heads;
     a.d = d->head_dim;
+    a.by_group = (uint32_t)((((uint64_t)1 << 32) + a.group - 1) / a.group);
     a.lists = d->lists;
     a.splits = 1;
     a.q_offsets = d->q_offsets;
@@ -1021,6 +1288,7 @@ Args common_args(const recd_attention *d, const void *q, const void *k, const vo
     a.causal = d->causal != 0;
     a.part_rows = d->q_rows * d->heads;
     a.last_first = true;
+    a.heads = 1;
     return a;
 }
 
@@ -1073,7 +1341,18 @@ int log2_of(int n)
     return l;
 }
 
-unsigned grid_of(const Args &a) { return (unsigned)((a.slots * a.splits + 7) / 8 * 8 * a.G); }
+unsigned grid_of(const Args &a) { return (unsigned)((a.slots * a.splits + 7) / 8 * 8 * ((a.G + a.heads - 1) / a.heads)); }
+
+// Key heads that a block of one wave goes through, the next head's rows on their way while it works at one: as many as
+// leave two rounds of waves (about twelve a compute unit at a time).
+int heads_at_once(const recd_ctx *ctx, const Tiling &t, int G, int64_t lists)
+{
+    int heads = 1;
+    while (t.division == ONE_WAVE && heads < G && (t.slots - lists / 2) * ((G + 2 * heads - 1) / (2 * heads)) >= (int64_t)ctx->num_cu * 24)
+        heads *= 2;
+    return heads;
+}
+
 
 template <typename T, int DP, bool CAP> void launch_one(Which w, const Args &a, Division v, hipStream_t st)
 {
@@ -1083,7 +1362,7 @@ template <typename T, int DP, bool CAP> void launch_one(Which w, const Args &a, 
     hipLaunchKernelGGL((kernel<T, DP, kept, phases, CAP>), grid, dim3(64 * kept * phases), 0, st, a)
     if (w == FORWARD) {
         if (v == ONE_WAVE)
-            RECD_LAUNCH(k_attention, 1, 1);
+            hipLaunchKernelGGL((k_attention_one<T, DP, CAP>), grid, dim3(64), 0, st, a);
         else if (v == PHASES)
             RECD_LAUNCH(k_attention, 1, P);
         else
@@ -1123,14 +1402,18 @@ template <typename T> void launch(Which w, const Args &a, Division v, hipStream_
         launch_width<T, 128>(w, a, v, st);
 }
 
-void launch_tiles(const recd_attention *d, const Tiling &t, int group, bool keys, int2 *tiles, hipStream_t st)
+// Lists the tiles of up to two sides that have a table.
+void launch_tiles(const recd_attention *d, const Side *sides, int n, hipStream_t st)
 {
-    if (t.table && d->lists <= kMostSorted && t.slots < ((int64_t)1 << 30))
-        hipLaunchKernelGGL(k_attention_tiles_by_work, dim3(1), dim3(1024), 0, st, (int)d->lists, (int)t.slots, group, t.R,
-                           keys, d->causal != 0, d->q_offsets, d->k_offsets, d->prefix, tiles);
-    else if (t.table)
-        hipLaunchKernelGGL(k_attention_tiles, dim3((unsigned)((d->lists + 255) / 256)), dim3(256), 0, st, d->lists, t.slots, group,
-                           t.R, keys ? d->k_offsets : d->q_offsets, tiles);
+    if (n == 0)
+        return;
+    const Side &one = sides[0], &two = sides[n - 1];
+    if (d->lists <= kMostSorted && one.slots < ((int64_t)1 << 30) && two.slots < ((int64_t)1 << 30))
+        hipLaunchKernelGGL(k_attention_tiles_by_work, dim3(n), dim3(1024), 0, st, (int)d->lists, d->causal != 0, d->q_offsets,
+                           d->k_offsets, d->prefix, one, two);
+    else
+        hipLaunchKernelGGL(k_attention_tiles, dim3((unsigned)((d->lists + 255) / 256), n), dim3(256), 0, st, d->lists, d->q_offsets,
+                           d->k_offsets, one, two);
 }
 
 } // namespace
@@ -1156,6 +1439,7 @@ recd_status recd_list_attention(recd_ctx *ctx, const recd_attention *d, const vo
     const Tiling t = tiling(ctx, d, d->q_rows, d->max_q, a.group, d->k_rows, d->max_k);
     a.slots = t.slots;
     a.tiles_per_list = t.tiles_per_list;
+    a.heads = heads_at_once(ctx, t, a.G, d->lists);
     // few tiles: a tile's keys are split over blocks, at least 256 keys each
     const int64_t blocks = (int64_t)ctx->num_cu * 2, have = t.slots * a.G > 0 ? t.slots * a.G : 1;
     int64_t splits = (blocks + have - 1) / have;
@@ -1180,7 +1464,8 @@ recd_status recd_list_attention(recd_ctx *ctx, const recd_attention *d, const vo
     WsCarver c(ctx->ws);
     carve(c);
     a.tiles = tiles;
-    launch_tiles(d, t, a.group, false, tiles, ctx->stream);
+    const Side side{t.slots, a.group, t.R, false, tiles};
+    launch_tiles(d, &side, t.table ? 1 : 0, ctx->stream);
     recd_with_type(d->dtype, [&](auto e) {
         using T = decltype(e);
         launch<T>(FORWARD, a, t.division, ctx->stream);
@@ -1257,23 +1542,27 @@ recd_status recd_list_attention_backward(recd_ctx *ctx, const recd_attention *d,
                                (const _Float16 *)v, tops + 1);
         hipLaunchKernelGGL(k_attention_lift, dim3(1), dim3(1), 0, st, a.d, tops, lift);
     }
-    launch_tiles(d, tq, a.group, false, tiles_q, st);
-    launch_tiles(d, tk, 1, true, tiles_k, st);
+    Side sides[2];
+    int listed = 0;
+    if (tq.table)
+        sides[listed++] = Side{tq.slots, a.group, tq.R, false, tiles_q};
+    if (tk.table)
+        sides[listed++] = Side{tk.slots, 1, tk.R, true, tiles_k};
+    launch_tiles(d, sides, listed, st);
     recd_with_type(d->dtype, [&](auto e) {
         using T = decltype(e);
-        const int dlog = log2_of(a.d * (int)sizeof(T) / 16);
         if (d->q_rows) {
-            hipLaunchKernelGGL((k_attention_delta<T>), dim3((unsigned)(((a.part_rows << dlog) + 255) / 256)), dim3(256), 0, st,
-                               a.part_rows, a.d, dlog, (const T *)out, (const T *)grad_out, delta);
             a.tiles = tiles_q;
             a.slots = tq.slots;
             a.tiles_per_list = tq.tiles_per_list;
+            a.heads = heads_at_once(ctx, tq, a.G, d->lists);
             launch<T>(GRAD_Q, a, tq.division, st);
         }
         a.tiles = tiles_k;
         a.last_first = false;
         a.slots = tk.slots;
         a.tiles_per_list = tk.tiles_per_list;
+        a.heads = heads_at_once(ctx, tk, a.G, d->lists);
         if (d->k_rows)
             launch<T>(GRAD_KV, a, tk.division, st);
     });
