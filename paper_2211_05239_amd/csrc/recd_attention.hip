@@ -278,7 +278,8 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
     const int wave_full = row0 + 32 <= p.rows ? p.limit(row0, a.group) : 0;  // keys that every row sees
     const int tiles = (p.limit(end - 1, a.group) + 31) / 32;
     const int part = split * PHASES + phase, parts = a.splits * PHASES;
-    const int t0 = (int)((int64_t)tiles * part / parts), t1 = (int)((int64_t)tiles * (part + 1) / parts);
+    const int each = parts == 1 ? tiles : (tiles + parts - 1) / parts;  // tiles of a part
+    const int t0 = part * each < tiles ? part * each : tiles, t1 = t0 + each < tiles ? t0 + each : tiles;
     const int wave_t1 = (wave_end + 31) / 32 < t1 ? (wave_end + 31) / 32 : t1;
     const int H = a.G * a.group;
     const int64_t q_row = p.q0 + query, at_row = q_row * H + head * a.group + head_in;
@@ -452,7 +453,7 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
 
 // The forward kernel for lists of few rows: a wave to itself goes through one head after the other, whose rows are on
 // their way while it works at the one before, so that a wave finds its list once for all of them.
-template <typename T, int DP, bool CAP> __global__ __launch_bounds__(64, (kResident<T, DP, 1>)) void k_attention_one(Args a)
+template <typename T, int DP, bool CAP> __global__ __launch_bounds__(64, (sizeof(T) == 2 && DP <= 32 ? 4 : kResident<T, DP, 1>)) void k_attention_one(Args a)
 {
     constexpr int KS = DP / 16, DT = DP / 32;
     using Mma = RecdMma<T>;
@@ -471,7 +472,8 @@ template <typename T, int DP, bool CAP> __global__ __launch_bounds__(64, (kResid
     const int lim = there ? p.limit(row, a.group) : 0;
     const int full = row0 + 32 <= p.rows ? p.limit(row0, a.group) : 0;
     const int end = p.limit(row0 + 31 < p.rows ? row0 + 31 : p.rows - 1, a.group), tiles = (end + 31) / 32;
-    const int t0 = (int)((int64_t)tiles * split / a.splits), t1 = (int)((int64_t)tiles * (split + 1) / a.splits);
+    const int each = a.splits == 1 ? tiles : (tiles + a.splits - 1) / a.splits;  // tiles of a split
+    const int t0 = split * each < tiles ? split * each : tiles, t1 = t0 + each < tiles ? t0 + each : tiles;
     const int H = a.G * a.group;
     const int64_t q_row = p.q0 + query;
     const float posf = (float)(p.pos0 + query);
@@ -795,8 +797,8 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
         typename S::Tile k[S::OWN][BUFS], v[S::OWN][BUFS];
     } lds;
     Problem p;
-    int head0, head_end, tile, split;
-    if (!find_tile(a, p, head0, head_end, tile, split))
+    int head, head_end, tile, split;
+    if (!find_tile(a, p, head, head_end, tile, split))
         return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int kept = wave % KEPT, phase = wave / KEPT;
@@ -821,79 +823,52 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
     const Capped<T> capped(a.cap);
     const float to_cap = CAP ? 2.0f * kRecdLog2e * a.scale / a.cap : 0.0f;
 
-    Frag qf[KS], gf[KS], qn[KS], gn[KS];
-    float slope_n = 0.0f, from_n = 0.0f, delta_n = 0.0f, slope = 0.0f, from = 0.0f, delta = 0.0f;
+    // delta = g . o, which the gradients by keys need too
+    const int h = head * a.group + head_in;
+    const int64_t at_row = q_row * H + h;
+    Frag qf[KS], gf[KS];
+    float delta = 0.0f;
+#pragma unroll
+    for (int k = 0; k < KS; k++) {
+        qf[k] = recd_row_frag<T>((const T *)a.q + q_row * a.q_stride + (int64_t)h * a.d, 16 * k, a.d, there, lane);
+        gf[k] = recd_row_frag<T>((const T *)a.g + at_row * a.d, 16 * k, a.d, there, lane);
+        const Frag out = recd_row_frag<T>((const T *)a.out_in + at_row * a.d, 16 * k, a.d, there, lane);
+#pragma unroll
+        for (int e = 0; e < 8; e++)
+            delta += (float)gf[k][e] * (float)out[e];
+    }
+    delta += __shfl_xor(delta, 32);
+    if (there && lane < 32 && phase == 0)
+        a.delta[at_row] = delta;
+    delta *= lift;
+    const float slope = a.slopes && there ? a.slopes[h] * kRecdLog2e : 0.0f;
+    float from = there ? a.lse_in[at_row] * kRecdLog2e : 0.0f;
+    if (from == -INFINITY)
+        from = 0.0f;  // sees nothing
+    recd_f32x16 o[DT];
+#pragma unroll
+    for (int d = 0; d < DT; d++)
+        o[d] = recd_f32x16{};
     typename S::Load ks, vs;
-    // a head's queries, gradients and delta = g . o (which the gradients by keys need too)
-    auto load_q = [&](int head) {
-        const int h = head * a.group + head_in;
-        const int64_t at = q_row * H + h;
-        delta_n = 0.0f;
-#pragma unroll
-        for (int k = 0; k < KS; k++) {
-            qn[k] = recd_row_frag<T>((const T *)a.q + q_row * a.q_stride + (int64_t)h * a.d, 16 * k, a.d, there, lane);
-            gn[k] = recd_row_frag<T>((const T *)a.g + at * a.d, 16 * k, a.d, there, lane);
-            const Frag o = recd_row_frag<T>((const T *)a.out_in + at * a.d, 16 * k, a.d, there, lane);
-#pragma unroll
-            for (int e = 0; e < 8; e++)
-                delta_n += (float)gn[k][e] * (float)o[e];
-        }
-        delta_n += __shfl_xor(delta_n, 32);
-        if (there && lane < 32 && phase == 0)
-            a.delta[at] = delta_n;
-        slope_n = a.slopes && there ? a.slopes[h] * kRecdLog2e : 0.0f;
-        from_n = there ? a.lse_in[at] * kRecdLog2e : 0.0f;
-    };
-    auto load = [&](int head, int t) {
+    auto load = [&](int t) {
         const int64_t at = p.k0 + t * 32;
         ks.load_rows(tid, (const T *)a.k + at * a.k_stride + head * a.d, p.nk - t * 32, a.d, (uint32_t)a.k_stride * sizeof(T));
         vs.load_rows(tid, (const T *)a.v + at * a.v_stride + head * a.d, p.nk - t * 32, a.d, (uint32_t)a.v_stride * sizeof(T));
     };
-    auto take = [&]() {
-        slope = slope_n;
-        from = from_n == -INFINITY ? 0.0f : from_n;  // (a row that sees nothing)
-        delta = delta_n * lift;
-#pragma unroll
-        for (int k = 0; k < KS; k++) {
-            qf[k] = qn[k];
-            gf[k] = gn[k];
-        }
-    };
-    recd_f32x16 o[DT];
-    int head = head0;
-    load_q(head);
     if (t0 < t1)
-        load(head, t0);
-    take();
-#pragma unroll
-    for (int d = 0; d < DT; d++)
-        o[d] = recd_f32x16{};
-    auto write = [&]() {
-        if (there && phase == 0)
-            store_columns<T, DT>((T *)a.gq + q_row * a.gq_stride + (int64_t)(head * a.group + head_in) * a.d, o,
-                                 (CAP ? 4.0f : 1.0f) * a.scale / lift, a.d, lane);
-    };
-    if (t0 == t1)
-        for (; ONE && head + 1 < head_end; head++) {  // no keys: zeros
-            write();
-            load_q(head + 1);
-        }
-    // one wave goes through the tiles of one head after the other
-    for (int t = t0; t < t1;) {
+        load(t0);
+    for (int t = t0; t < t1; t++) {
         const int buf = BUFS == 1 ? 0 : t & 1;
         if constexpr (BUFS == 1)
             S::sync();
         ks.store(tid, kt[buf]);
         vs.store(tid, vt[buf]);
         S::sync();
-        const bool last = t + 1 == t1, more = ONE && last && head + 1 < head_end;
-        if (!last || more)
-            load(more ? head + 1 : head, more ? t0 : t + 1);
-        if constexpr (ONE)
-            if (more)
-                load_q(head + 1);
+        if (t + 1 < t1)
+            load(t + 1);
         const int j0 = t * 32;
-        if (j0 < wave_end) {
+        if (j0 >= wave_end)
+            continue;
         recd_f32x16 s = {}, dp = {};
 #pragma unroll
         for (int k = 0; k < KS; k++) {
@@ -937,24 +912,14 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
             finish(std::integral_constant<int, 8>{});
         else
             finish(std::integral_constant<int, 16>{});
-        }
-        t++;
-        if constexpr (ONE)
-            if (more) {
-                write();
-                head++;
-                t = t0;
-                take();
-#pragma unroll
-                for (int d = 0; d < DT; d++)
-                    o[d] = recd_f32x16{};
-            }
     }
     if constexpr (PHASES > 1) {
         static_assert(sizeof(lds) >= 64 * 16 * DT * sizeof(float));
         join_sums<DT, PHASES>(o, reinterpret_cast<float *>(&lds), 0, phase, lane);
     }
-    write();
+    if (there && phase == 0)
+        store_columns<T, DT>((T *)a.gq + q_row * a.gq_stride + (int64_t)h * a.d, o, (CAP ? 4.0f : 1.0f) * a.scale / lift, a.d,
+                             lane);
 }
 
 // Keys stay, queries and their gradients stream past.  What a score needs of its row stands in LDS in the order of
@@ -963,7 +928,6 @@ template <typename T, int DP, int KEPT, int PHASES, bool CAP>
 __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void k_attention_grad_kv(Args a)
 {
     using S = Shape<T, DP, KEPT, PHASES>;
-    constexpr bool ONE = KEPT * PHASES == 1;
     constexpr int KS = DP / 16, DT = DP / 32, BUFS = S::SHARED ? 2 : 1;
     using Mma = RecdMma<T>;
     using Frag = typename Mma::Frag;
@@ -978,8 +942,8 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
         alignas(16) int lim[S::OWN][BUFS][S::ROWS];
     } lds;
     Problem p;
-    int head0, head_end, tile, split;
-    if (!find_tile(a, p, head0, head_end, tile, split))
+    int head, head_end, tile, split;
+    if (!find_tile(a, p, head, head_end, tile, split))
         return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int kept = wave % KEPT, phase = wave / KEPT;
@@ -995,22 +959,24 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
     const bool there = j < p.nk;
     const float jf = (float)j;
     const int H = a.G * a.group;
-    Frag kf[IN_LDS ? 1 : KS], vf[IN_LDS ? 1 : KS], kn[IN_LDS ? 1 : KS], vn[IN_LDS ? 1 : KS];
+    Frag kf[IN_LDS ? 1 : KS], vf[IN_LDS ? 1 : KS];
     const int kept_at = IN_LDS ? (32 * kept + (lane & 31)) * lds.k.LD + (lane >> 5) * 8 : 0;
-    auto load_kept = [&](int head) {
 #pragma unroll
-        for (int k = 0; k < KS; k++) {
-            const int i = IN_LDS ? 0 : k;
-            if (IN_LDS && k % PHASES != phase)
-                continue;  // the phases share the writing
-            kn[i] = recd_row_frag<T>((const T *)a.k + (p.k0 + j) * a.k_stride + (int64_t)head * a.d, 16 * k, a.d, there, lane);
-            vn[i] = recd_row_frag<T>((const T *)a.v + (p.k0 + j) * a.v_stride + (int64_t)head * a.d, 16 * k, a.d, there, lane);
-            if constexpr (IN_LDS) {
-                *reinterpret_cast<Frag *>(lds.k.at + kept_at + 16 * k) = kn[0];
-                *reinterpret_cast<Frag *>(lds.v.at + kept_at + 16 * k) = vn[0];
-            }
+    for (int k = 0; k < KS; k++) {
+        const int i = IN_LDS ? 0 : k;
+        if (IN_LDS && k % PHASES != phase)
+            continue;  // the phases share the writing
+        kf[i] = recd_row_frag<T>((const T *)a.k + (p.k0 + j) * a.k_stride + (int64_t)head * a.d, 16 * k, a.d, there, lane);
+        vf[i] = recd_row_frag<T>((const T *)a.v + (p.k0 + j) * a.v_stride + (int64_t)head * a.d, 16 * k, a.d, there, lane);
+        if constexpr (IN_LDS) {
+            *reinterpret_cast<Frag *>(lds.k.at + kept_at + 16 * k) = kf[0];
+            *reinterpret_cast<Frag *>(lds.v.at + kept_at + 16 * k) = vf[0];
         }
-    };
+    }
+    recd_f32x16 dk[DT], dv[DT];
+#pragma unroll
+    for (int d = 0; d < DT; d++)
+        dk[d] = dv[d] = recd_f32x16{};
     // probabilities are held 2^kLiftP larger, by their exponents; ds by that and, from dp on, the rest of its lift
     const float lift = kHalf<T> ? *a.lift : 1.0f, lift_dp = lift * recd_exp2(-kLiftP<T>);
     const float c = a.scale * kRecdLog2e;
@@ -1029,7 +995,7 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
     float n_from = 0.0f, n_delta = 0.0f, n_slope = 0.0f;
     float n_pos = 0.0f;
     int n_lim = 0;
-    auto load = [&](int head, int t) {
+    auto load = [&](int t) {
         // the tile's first row is head `odd` of its query's; row r is then query (odd + r) / group from there
         const int row = t * S::ROWS, q_first = p.query(row, a.group), odd = row - q_first * a.group;
         auto query_of = [&](int r) { return a.group == 1 ? r : (int)__umulhi(odd + r, a.by_group); };
@@ -1056,34 +1022,9 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
             n_pos = (float)(p.pos0 + query);
         }
     };
-    int head = head0;
-    load_kept(head);
     if (t0 < t1)
-        load(head, t0);
-    auto take = [&]() {
-        if constexpr (!IN_LDS)
-#pragma unroll
-            for (int k = 0; k < KS; k++) {
-                kf[k] = kn[k];
-                vf[k] = vn[k];
-            }
-    };
-    take();
-    recd_f32x16 dk[DT], dv[DT];
-#pragma unroll
-    for (int d = 0; d < DT; d++)
-        dk[d] = dv[d] = recd_f32x16{};
-    auto write = [&]() {
-        if (!there || phase)
-            return;
-        store_columns<T, DT>((T *)a.gk + (p.k0 + j) * a.gk_stride + (int64_t)head * a.d, dk, (CAP ? 4.0f : 1.0f) * a.scale / lift,
-                             a.d, lane);
-        store_columns<T, DT>((T *)a.gv + (p.k0 + j) * a.gv_stride + (int64_t)head * a.d, dv, recd_exp2(-kLiftP<T>), a.d, lane);
-    };
-    if (t0 == t1)
-        for (; ONE && head + 1 < head_end; head++)  // no queries see these keys: zeros
-            write();
-    for (int t = t0; t < t1;) {
+        load(t0);
+    for (int t = t0; t < t1; t++) {
         const int buf = BUFS == 1 ? 0 : t & 1;
         if constexpr (BUFS == 1)
             S::sync();
@@ -1098,16 +1039,13 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
             row_pos[buf][i] = n_pos;
         }
         S::sync();
-        const bool last = t + 1 == t1, more = ONE && last && head + 1 < head_end;
-        if (!last || more)
-            load(more ? head + 1 : head, more ? t0 : t + 1);
-        if constexpr (ONE)
-            if (more)
-                load_kept(head + 1);
+        if (t + 1 < t1)
+            load(t + 1);
         const int row0 = t * S::ROWS + sub;
         const bool whole = row0 + 32 <= p.rows;
         // (tile row 31 is the product's row 31, and limits do not fall: what it does not see, no row sees)
-        if (j0 < p.nk && row0 < p.rows && !(whole && __builtin_amdgcn_readfirstlane(row_lim[buf][sub + 31]) <= j0)) {
+        if (j0 >= p.nk || row0 >= p.rows || (whole && __builtin_amdgcn_readfirstlane(row_lim[buf][sub + 31]) <= j0))
+            continue;
         recd_f32x16 s = {}, dp = {};
 #pragma unroll
         for (int k = 0; k < KS; k++) {
@@ -1128,72 +1066,57 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
             s[r] = recd_exp2(z);
             dp[r] = s[r] * (dp[r] * lift_dp - delta) * quarter;
         };
-        auto finish = [&](auto registers) {
-            constexpr int NR = registers.value;
-            if (a.slopes) {
+        if (a.slopes) {
 #pragma unroll
-                for (int r = 0; r < NR; r += 4) {
-                    const int row = sub + recd_sums_row(r, lane);
-                    const recd_f32x4 from = *reinterpret_cast<const recd_f32x4 *>(&row_from[buf][row]);
-                    const recd_f32x4 delta = *reinterpret_cast<const recd_f32x4 *>(&row_delta[buf][row]);
-                    const recd_f32x4 slope = *reinterpret_cast<const recd_f32x4 *>(&row_slope[buf][row]);
-                    const recd_f32x4 pos = *reinterpret_cast<const recd_f32x4 *>(&row_pos[buf][row]);
+            for (int r = 0; r < 16; r += 4) {
+                const int row = sub + recd_sums_row(r, lane);
+                const recd_f32x4 from = *reinterpret_cast<const recd_f32x4 *>(&row_from[buf][row]);
+                const recd_f32x4 delta = *reinterpret_cast<const recd_f32x4 *>(&row_delta[buf][row]);
+                const recd_f32x4 slope = *reinterpret_cast<const recd_f32x4 *>(&row_slope[buf][row]);
+                const recd_f32x4 pos = *reinterpret_cast<const recd_f32x4 *>(&row_pos[buf][row]);
 #pragma unroll
-                    for (int q = 0; q < 4; q++)
-                        score(r + q, from[q] - slope[q] * fabsf(pos[q] - jf), delta[q]);
-                }
-            } else {
-#pragma unroll
-                for (int r = 0; r < NR; r += 4) {
-                    const int row = sub + recd_sums_row(r, lane);
-                    const recd_f32x4 from = *reinterpret_cast<const recd_f32x4 *>(&row_from[buf][row]);
-                    const recd_f32x4 delta = *reinterpret_cast<const recd_f32x4 *>(&row_delta[buf][row]);
-#pragma unroll
-                    for (int q = 0; q < 4; q++)
-                        score(r + q, from[q], delta[q]);
-                }
+                for (int q = 0; q < 4; q++)
+                    score(r + q, from[q] - slope[q] * fabsf(pos[q] - jf), delta[q]);
             }
-            // (tile row 0 is the product's row 0, and limits do not fall: what its rows all see, the others see)
-            if (!whole || __builtin_amdgcn_readfirstlane(row_lim[buf][sub]) < j0 + 32) {
-                asm volatile("");
+        } else {
 #pragma unroll
-                for (int r = 0; r < NR; r++)
-                    if (j >= row_lim[buf][sub + recd_sums_row(r, lane)])
-                        s[r] = dp[r] = 0.0f;
+            for (int r = 0; r < 16; r += 4) {
+                const int row = sub + recd_sums_row(r, lane);
+                const recd_f32x4 from = *reinterpret_cast<const recd_f32x4 *>(&row_from[buf][row]);
+                const recd_f32x4 delta = *reinterpret_cast<const recd_f32x4 *>(&row_delta[buf][row]);
+#pragma unroll
+                for (int q = 0; q < 4; q++)
+                    score(r + q, from[q], delta[q]);
             }
-#pragma unroll
-            for (int h = 0; h < NR / 8; h++) {
-                const Frag pf = recd_sums_frag<T>(s, h), sf = recd_sums_frag<T>(dp, h);
-#pragma unroll
-                for (int d = 0; d < DT; d++) {
-                    dv[d] = Mma::mul(gt[buf].columns(sub + 16 * h, 32 * d, lane), pf, dv[d]);
-                    dk[d] = Mma::mul(qt[buf].columns(sub + 16 * h, 32 * d, lane), sf, dk[d]);
-                }
-            }
-        };
-        if (ONE && p.rows - row0 <= 16)  // the other registers hold no row of the list
-            finish(std::integral_constant<int, 8>{});
-        else
-            finish(std::integral_constant<int, 16>{});
         }
-        t++;
-        if constexpr (ONE)
-            if (more) {
-                write();
-                head++;
-                t = t0;
-                take();
+        // (tile row 0 is the product's row 0, and limits do not fall: what its rows all see, the others see)
+        if (!whole || __builtin_amdgcn_readfirstlane(row_lim[buf][sub]) < j0 + 32) {
+            asm volatile("");
 #pragma unroll
-                for (int d = 0; d < DT; d++)
-                    dk[d] = dv[d] = recd_f32x16{};
+            for (int r = 0; r < 16; r++)
+                if (j >= row_lim[buf][sub + recd_sums_row(r, lane)])
+                    s[r] = dp[r] = 0.0f;
+        }
+#pragma unroll
+        for (int h = 0; h < 2; h++) {
+            const Frag pf = recd_sums_frag<T>(s, h), sf = recd_sums_frag<T>(dp, h);
+#pragma unroll
+            for (int d = 0; d < DT; d++) {
+                dv[d] = Mma::mul(gt[buf].columns(sub + 16 * h, 32 * d, lane), pf, dv[d]);
+                dk[d] = Mma::mul(qt[buf].columns(sub + 16 * h, 32 * d, lane), sf, dk[d]);
             }
+        }
     }
     if constexpr (PHASES > 1) {
         static_assert(sizeof(lds) >= KEPT * 64 * 16 * DT * sizeof(float));
         join_sums<DT, PHASES>(dk, reinterpret_cast<float *>(&lds), kept, phase, lane);
         join_sums<DT, PHASES>(dv, reinterpret_cast<float *>(&lds), kept, phase, lane);
     }
-    write();
+    if (!there || phase)
+        return;
+    store_columns<T, DT>((T *)a.gk + (p.k0 + j) * a.gk_stride + (int64_t)head * a.d, dk, (CAP ? 4.0f : 1.0f) * a.scale / lift, a.d,
+                         lane);
+    store_columns<T, DT>((T *)a.gv + (p.k0 + j) * a.gv_stride + (int64_t)head * a.d, dv, recd_exp2(-kLiftP<T>), a.d, lane);
 }
 
 // Offsets that do not rise from 0 to the number of rows, or pass the caller's bound of a list's length.
@@ -1344,11 +1267,11 @@ int log2_of(int n)
 unsigned grid_of(const Args &a) { return (unsigned)((a.slots * a.splits + 7) / 8 * 8 * ((a.G + a.heads - 1) / a.heads)); }
 
 // Key heads that a block of one wave goes through, the next head's rows on their way while it works at one: as many as
-// leave two rounds of waves (about twelve a compute unit at a time).
+// leave four rounds of waves (about twelve a compute unit at a time).
 int heads_at_once(const recd_ctx *ctx, const Tiling &t, int G, int64_t lists)
 {
     int heads = 1;
-    while (t.division == ONE_WAVE && heads < G && (t.slots - lists / 2) * ((G + 2 * heads - 1) / (2 * heads)) >= (int64_t)ctx->num_cu * 24)
+    while (t.division == ONE_WAVE && heads < G && (t.slots - lists / 2) * ((G + 2 * heads - 1) / (2 * heads)) >= (int64_t)ctx->num_cu * 48)
         heads *= 2;
     return heads;
 }
@@ -1555,14 +1478,12 @@ recd_status recd_list_attention_backward(recd_ctx *ctx, const recd_attention *d,
             a.tiles = tiles_q;
             a.slots = tq.slots;
             a.tiles_per_list = tq.tiles_per_list;
-            a.heads = heads_at_once(ctx, tq, a.G, d->lists);
             launch<T>(GRAD_Q, a, tq.division, st);
         }
         a.tiles = tiles_k;
         a.last_first = false;
         a.slots = tk.slots;
         a.tiles_per_list = tk.tiles_per_list;
-        a.heads = heads_at_once(ctx, tk, a.G, d->lists);
         if (d->k_rows)
             launch<T>(GRAD_KV, a, tk.division, st);
     });
