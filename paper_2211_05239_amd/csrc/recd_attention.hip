@@ -119,42 +119,6 @@ __device__ inline bool find_tile(const Args &a, Problem &p, int &head, int &head
     return true;
 }
 
-// Rows of a tile from memory into registers and on into LDS, by THREADS threads of which this is `tid`.  A thread's
-// addresses are 32-bit offsets from the tile's first row, which is the same for all: bytes(r) is that of row r < 128.  Rows
-// behind the last one and elements behind a head's last one are read from the last one's place instead: their
-// scores are masked, or meet zeros in the other operand, or belong to sums that nobody stores.
-template <typename T, int ROWS, int DP, int THREADS> struct Stream {
-    using Tile = RecdTile<T, ROWS, DP>;
-    using Piece = typename Tile::Piece;
-    static constexpr int PT = (Tile::PIECES + THREADS - 1) / THREADS;
-    Piece held[PT];
-
-    template <typename Bytes> __device__ inline void load(int tid, const T *first, int rows, int d, Bytes bytes)
-    {
-        constexpr int PR = DP / Tile::E;
-#pragma unroll
-        for (int i = 0; i < PT; i++) {
-            const int piece = tid + i * THREADS, at = piece % PR * Tile::E, r = piece / PR;
-            if (piece < Tile::PIECES) {
-                const uint32_t off = bytes(r < rows ? r : rows - 1) + (uint32_t)((at < d ? at : d - Tile::E) * (int)sizeof(T));
-                held[i] = *reinterpret_cast<const Piece *>(reinterpret_cast<const char *>(first) + off);
-            }
-        }
-    }
-    // rows that lie `stride` bytes (less than 2^24) apart
-    __device__ inline void load_rows(int tid, const T *first, int rows, int d, uint32_t stride)
-    {
-        load(tid, first, rows, d, [=](int r) { return (uint32_t)__umul24(r, stride); });
-    }
-    __device__ inline void store(int tid, Tile &t)
-    {
-#pragma unroll
-        for (int i = 0; i < PT; i++)
-            if (tid + i * THREADS < Tile::PIECES)
-                t.put(tid + i * THREADS, held[i]);
-    }
-};
-
 // How a block's waves divide a tile: KEPT groups of 32 kept rows, times PHASES that divide the streamed rows and whose
 // sums are joined at the end.  With one group every wave streams tiles of its own and waits for nobody; with several, the
 // block streams tiles of 32 * PHASES rows that all groups read.
@@ -163,17 +127,15 @@ template <typename T, int DP, int KEPT, int PHASES> struct Shape {
     static constexpr int ROWS = SHARED ? 32 * PHASES : 32, LOADERS = SHARED ? 64 * KEPT * PHASES : 64;
     static constexpr int OWN = SHARED ? 1 : PHASES;  // tiles side by side in LDS
     using Tile = RecdTile<T, ROWS, DP>;
-    using Load = Stream<T, ROWS, DP, LOADERS>;
+    using Load = RecdStream<T, ROWS, DP, LOADERS>;
 
     // what the streaming threads wrote is there for the readers
     static __device__ inline void sync()
     {
         if constexpr (SHARED)
             __syncthreads();
-        else {
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            __builtin_amdgcn_wave_barrier();
-        }
+        else
+            recd_wave_sync();
     }
 };
 
@@ -1240,9 +1202,10 @@ Tiling tiling(const recd_ctx *ctx, const recd_attention *d, int64_t rows, int64_
     if (four > d->lists * per_four)
         four = d->lists * per_four;
     const bool few = most * group <= 64 || rows * group <= 48 * d->lists;
-    if (few && (most_others <= 128 || others <= 64 * d->lists))
+    const bool wide = d->dtype == RECD_F32 && d->head_dim > 64;  // tiles of 17 KB: phases would leave two waves to a compute unit
+    if (few && (wide || most_others <= 128 || others <= 64 * d->lists))
         t.division = ONE_WAVE;
-    else if (few || four * d->kv_heads * waves < 12 * ctx->num_cu)
+    else if (!wide && (few || four * d->kv_heads * waves < 12 * ctx->num_cu))
         t.division = PHASES;
     else
         t.division = GROUPS;
@@ -1279,30 +1242,34 @@ int heads_at_once(const recd_ctx *ctx, const Tiling &t, int G, int64_t lists)
 
 template <typename T, int DP, bool CAP> void launch_one(Which w, const Args &a, Division v, hipStream_t st)
 {
-    constexpr int P = sizeof(T) == 4 && DP > 64 ? 2 : 4, KV = sizeof(T) == 2 && DP > 64 ? 2 : 1;
+    constexpr int KV = sizeof(T) == 2 && DP > 64 ? 2 : 1;
+    constexpr bool WIDE = sizeof(T) == 4 && DP > 64;
     const dim3 grid(grid_of(a));
 #define RECD_LAUNCH(kernel, kept, phases) \
     hipLaunchKernelGGL((kernel<T, DP, kept, phases, CAP>), grid, dim3(64 * kept * phases), 0, st, a)
     if (w == FORWARD) {
         if (v == ONE_WAVE)
             hipLaunchKernelGGL((k_attention_one<T, DP, CAP>), grid, dim3(64), 0, st, a);
-        else if (v == PHASES)
-            RECD_LAUNCH(k_attention, 1, P);
-        else
+        else if (v == PHASES) {
+            if constexpr (!WIDE)
+                RECD_LAUNCH(k_attention, 1, 4);
+        } else
             RECD_LAUNCH(k_attention, 4, 1);
     } else if (w == GRAD_Q) {
         if (v == ONE_WAVE)
             RECD_LAUNCH(k_attention_grad_q, 1, 1);
-        else if (v == PHASES)
-            RECD_LAUNCH(k_attention_grad_q, 1, P);
-        else
+        else if (v == PHASES) {
+            if constexpr (!WIDE)
+                RECD_LAUNCH(k_attention_grad_q, 1, 4);
+        } else
             RECD_LAUNCH(k_attention_grad_q, 4, 1);
     } else {
         if (v == ONE_WAVE)
             RECD_LAUNCH(k_attention_grad_kv, 1, 1);
-        else if (v == PHASES)
-            RECD_LAUNCH(k_attention_grad_kv, 1, P);
-        else
+        else if (v == PHASES) {
+            if constexpr (!WIDE)
+                RECD_LAUNCH(k_attention_grad_kv, 1, 4);
+        } else
             RECD_LAUNCH(k_attention_grad_kv, 4, KV);
     }
 #undef RECD_LAUNCH
@@ -1364,7 +1331,7 @@ recd_status recd_list_attention(recd_ctx *ctx, const recd_attention *d, const vo
     a.tiles_per_list = t.tiles_per_list;
     a.heads = heads_at_once(ctx, t, a.G, d->lists);
     // few tiles: a tile's keys are split over blocks, at least 256 keys each
-    const int64_t blocks = (int64_t)ctx->num_cu * 2, have = t.slots * a.G > 0 ? t.slots * a.G : 1;
+    const int64_t blocks = (int64_t)ctx->num_cu * (t.division == ONE_WAVE ? 8 : 2), have = t.slots * a.G > 0 ? t.slots * a.G : 1;
     int64_t splits = (blocks + have - 1) / have;
     if (splits > d->max_k / 256)
         splits = d->max_k / 256;

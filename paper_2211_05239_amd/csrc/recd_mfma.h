@@ -102,6 +102,49 @@ template <typename T, int ROWS, int DP> struct RecdTile {
     }
 };
 
+// Rows of a tile from memory into registers and on into LDS, by THREADS threads of which this is `tid`.  A thread's
+// addresses are 32-bit offsets from the tile's first row, which is the same for all: bytes(r) is that of row r < 128.  Rows
+// behind the last one and elements behind a head's last one are read from the last one's place instead: their
+// scores are masked, or meet zeros in the other operand, or belong to sums that nobody stores.
+template <typename T, int ROWS, int DP, int THREADS> struct RecdStream {
+    using Tile = RecdTile<T, ROWS, DP>;
+    using Piece = typename Tile::Piece;
+    static constexpr int PT = (Tile::PIECES + THREADS - 1) / THREADS;
+    Piece held[PT];
+
+    template <typename Bytes> __device__ inline void load(int tid, const T *first, int rows, int d, Bytes bytes)
+    {
+        constexpr int PR = DP / Tile::E;
+#pragma unroll
+        for (int i = 0; i < PT; i++) {
+            const int piece = tid + i * THREADS, at = piece % PR * Tile::E, r = piece / PR;
+            if (piece < Tile::PIECES) {
+                const uint32_t off = bytes(r < rows ? r : rows - 1) + (uint32_t)((at < d ? at : d - Tile::E) * (int)sizeof(T));
+                held[i] = *reinterpret_cast<const Piece *>(reinterpret_cast<const char *>(first) + off);
+            }
+        }
+    }
+    // rows that lie `stride` bytes (less than 2^24) apart
+    __device__ inline void load_rows(int tid, const T *first, int rows, int d, uint32_t stride)
+    {
+        load(tid, first, rows, d, [=](int r) { return (uint32_t)__umul24(r, stride); });
+    }
+    __device__ inline void store(int tid, Tile &t)
+    {
+#pragma unroll
+        for (int i = 0; i < PT; i++)
+            if (tid + i * THREADS < Tile::PIECES)
+                t.put(tid + i * THREADS, held[i]);
+    }
+};
+
+// What the wave's lanes wrote to LDS is there for its other lanes; what they read has been read.
+__device__ inline void recd_wave_sync()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
 // The step's 16 elements from k0 on of a row in global memory (8 a half wave), zero from element D on.
 template <typename T> __device__ inline typename RecdMma<T>::Frag recd_row_frag(const T *row, int k0, int D, bool there, int lane)
 {

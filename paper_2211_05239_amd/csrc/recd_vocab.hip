@@ -29,38 +29,13 @@ constexpr float kSlack = 8.0f;
 // fp16 exponentials are held 2^7 times larger: at most 2^15 with the slack, and exact to 2^-31 of the maximum.
 template <typename T> constexpr float kLift = std::is_same<T, _Float16>::value ? 7.0f : 0.0f;
 
-// Streamed rows [row0, row0 + ROWS) of a matrix [n, D] into registers and from there into a tile.
-template <typename T, int ROWS, int DP, int THREADS = kBlock> struct Stream {
-    using Tile = RecdTile<T, ROWS, DP>;
-    static constexpr int PT = (Tile::PIECES + THREADS - 1) / THREADS;
-    typename Tile::Piece held[PT];
-
-    __device__ inline void load(const T *m, int64_t row0, int64_t n, int D)
-    {
-        constexpr int PR = DP / Tile::E;
-#pragma unroll
-        for (int i = 0; i < PT; i++) {
-            const int piece = threadIdx.x + i * THREADS;
-            const int64_t row = row0 + piece / PR;
-            const int at = piece % PR * Tile::E;
-            held[i] = typename Tile::Piece{};
-            if (piece < Tile::PIECES && row < n && at < D)
-                held[i] = *reinterpret_cast<const typename Tile::Piece *>(m + row * D + at);
-        }
-    }
-    __device__ inline void store(Tile &t)
-    {
-#pragma unroll
-        for (int i = 0; i < PT; i++)
-            if (threadIdx.x + i * THREADS < (unsigned)Tile::PIECES)
-                t.put(threadIdx.x + i * THREADS, held[i]);
-    }
-};
-
 // Tiles of 32 kept rows in a wave, and waves in a block.
 template <typename T, int DP> constexpr int kTiles = 1;
-template <typename T, int DP> constexpr int kManyWaves = sizeof(T) == 4 ? 4 : 8;
-template <typename T, int DP> constexpr int kFewTiles = sizeof(T) == 4 || DP > 128 ? 1 : 2;
+template <typename T, int DP> constexpr int kManyWaves = sizeof(T) == 4 || DP > 192 ? 4 : 8;
+template <typename T, int DP> constexpr int kFewTiles = sizeof(T) * DP > 256 ? 1 : 2;
+
+// Rows of a tile that are there, of `left` behind its first.
+__device__ inline int rows_left(int64_t left) { return left < 128 ? (int)left : 128; }
 
 struct ForwardArgs {
     int64_t n, V;
@@ -73,27 +48,32 @@ struct ForwardArgs {
     float *part_m, *part_l, *part_o;  // [parts][n] and [parts][n][D]: maximum (in powers of two), sum, weighted sum
 };
 
-// Few rows: the block's waves hold the same 32 * N rows and take turns at the table's rows, each a part of its own.
+// Few rows: the block's waves hold the same 32 * N rows and each streams table rows of its own, 32 at a time through LDS
+// of its own, so that nobody waits for anybody.  Their sums are joined at the end.
 template <typename T, int DP, int N, bool MEAN> __global__ __launch_bounds__(kBlock) void k_vocab_forward_few(ForwardArgs a)
 {
-    constexpr int VT = 128;
     constexpr int KS = DP / 16, DT = DP / 32;
     using Mma = RecdMma<T>;
     using Frag = typename Mma::Frag;
-    __shared__ RecdTile<T, VT, DP> tile;
-    // the row blocks of one split side by side on one die, whose L2 then serves the split's rows to all of them
+    __shared__ union {
+        RecdTile<T, 32, DP> tile[kWaves];
+        float join[64 * (2 + (MEAN ? 16 * DT : 0))];
+    } lds;
     const int xcd = blockIdx.x & 7, at = blockIdx.x >> 3;
     const int rb = at % a.row_blocks, split = at / a.row_blocks * 8 + xcd;
     if (split >= a.splits)
         return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t row0 = (int64_t)rb * 32 * N;
-    const int64_t tiles = (a.V + VT - 1) / VT, t0 = split * a.tiles_per_split;
+    const int64_t tiles = (a.V + 127) / 128, t0 = split * a.tiles_per_split;
     const int64_t t1 = t0 + a.tiles_per_split < tiles ? t0 + a.tiles_per_split : tiles;
+    RecdTile<T, 32, DP> &tile = lds.tile[wave];
 
     Frag xf[N][KS];
+#pragma unroll
     for (int j = 0; j < N; j++) {
         const int64_t row = row0 + 32 * j + (lane & 31);
+#pragma unroll
         for (int k = 0; k < KS; k++) {
             xf[j][k] = recd_row_frag<T>((const T *)a.x + row * a.D, 16 * k, a.D, row < a.n, lane);
             if (a.negative)
@@ -102,94 +82,145 @@ template <typename T, int DP, int N, bool MEAN> __global__ __launch_bounds__(kBl
     }
     float m[N], l[N];
     recd_f32x16 o[N][MEAN ? DT : 1];
+#pragma unroll
     for (int j = 0; j < N; j++) {
         m[j] = -INFINITY;
         l[j] = 0.0f;
+#pragma unroll
         for (int d = 0; d < (MEAN ? DT : 1); d++)
             o[j][d] = recd_f32x16{};
     }
-    Stream<T, VT, DP> stream;
+    RecdStream<T, 32, DP, 64> stream;
+    auto load = [&](int64_t t) {
+        const int64_t first = t * 128 + 32 * wave;
+        if (first < a.V)
+            stream.load_rows(lane, (const T *)a.table + first * a.D, rows_left(a.V - first), a.D, a.D * sizeof(T));
+    };
     if (t0 < t1)
-        stream.load((const T *)a.table, t0 * VT, a.V, a.D);
+        load(t0);
     for (int64_t t = t0; t < t1; t++) {
-        __syncthreads();
-        stream.store(tile);
-        __syncthreads();
+        const int64_t left = a.V - (t * 128 + 32 * wave);
+        if (left <= 0)
+            break;
+        recd_wave_sync();
+        stream.store(lane, tile);
+        recd_wave_sync();
         if (t + 1 < t1)
-            stream.load((const T *)a.table, (t + 1) * VT, a.V, a.D);
-        {
-            const int st = wave;
-            recd_f32x16 s[N];
+            load(t + 1);
+        recd_f32x16 s[N];
+#pragma unroll
+        for (int j = 0; j < N; j++)
+            s[j] = recd_f32x16{};
+#pragma unroll
+        for (int k = 0; k < KS; k++) {
+            const Frag w = tile.rows(0, 16 * k, lane);
+#pragma unroll
             for (int j = 0; j < N; j++)
-                s[j] = recd_f32x16{};
+                s[j] = Mma::mul(w, xf[j][k], s[j]);
+        }
+        if (left < 32) {
+            asm volatile("");
 #pragma unroll
-            for (int k = 0; k < KS; k++) {
-                const Frag w = tile.rows(32 * st, 16 * k, lane);
-                for (int j = 0; j < N; j++)
-                    s[j] = Mma::mul(w, xf[j][k], s[j]);
+            for (int j = 0; j < N; j++)
+#pragma unroll
+                for (int r = 0; r < 16; r++)
+                    s[j][r] = recd_score_row(r, lane) >= (int)left ? -INFINITY : s[j][r];
+        }
+#pragma unroll
+        for (int j = 0; j < N; j++) {
+            float top = s[j][0];
+#pragma unroll
+            for (int r = 1; r < 16; r++)
+                top = fmaxf(top, s[j][r]);
+            top = fmaxf(top, __shfl_xor(top, 32)) * a.c - kLift<T>;
+            if (__any(top > m[j] + kSlack)) {
+                const float now = fmaxf(m[j], top);
+                const float f = now == m[j] ? 1.0f : recd_exp2(m[j] - now);
+                m[j] = now;
+                l[j] *= f;
+                if constexpr (MEAN)
+#pragma unroll
+                    for (int d = 0; d < DT; d++)
+#pragma unroll
+                        for (int r = 0; r < 16; r++)
+                            o[j][d][r] *= f;
             }
-            const int64_t left = a.V - (t * VT + 32 * st);
-            if (left < 32)
-                for (int j = 0; j < N; j++)
-                    for (int r = 0; r < 16; r++)
-                        if (recd_score_row(r, lane) >= left)
-                            s[j][r] = -INFINITY;
+            const float from = m[j] == -INFINITY ? 0.0f : m[j];  // a row of logits that are all -inf
+            float sum = 0.0f;
 #pragma unroll
-            for (int j = 0; j < N; j++) {
-                float top = s[j][0];
-                for (int r = 1; r < 16; r++)
-                    top = fmaxf(top, s[j][r]);
-                top = fmaxf(top, __shfl_xor(top, 32)) * a.c - kLift<T>;
-                if (__any(top > m[j] + kSlack)) {
-                    const float now = fmaxf(m[j], top);
-                    const float f = now == m[j] ? 1.0f : recd_exp2(m[j] - now);
-                    m[j] = now;
-                    l[j] *= f;
-                    if constexpr (MEAN)
-                        for (int d = 0; d < DT; d++)
-                            for (int r = 0; r < 16; r++)
-                                o[j][d][r] *= f;
-                }
-                const float from = m[j] == -INFINITY ? 0.0f : m[j];  // a row of logits that are all -inf
-                float sum = 0.0f;
-                for (int r = 0; r < 16; r++) {
-                    s[j][r] = recd_exp2(s[j][r] * a.c - from);
-                    sum += s[j][r];
-                }
-                l[j] += sum;
+            for (int r = 0; r < 16; r++) {
+                s[j][r] = recd_exp2(s[j][r] * a.c - from);
+                sum += s[j][r];
             }
-            if constexpr (MEAN) {
+            l[j] += sum;
+        }
+        if constexpr (MEAN) {
 #pragma unroll
-                for (int h = 0; h < 2; h++) {
-                    Frag p[N];
+            for (int h = 0; h < 2; h++) {
+                Frag p[N];
+#pragma unroll
+                for (int j = 0; j < N; j++)
+                    p[j] = recd_sums_frag<T>(s[j], h);
+#pragma unroll
+                for (int d = 0; d < DT; d++) {
+                    const Frag w = tile.columns(16 * h, 32 * d, lane);
+#pragma unroll
                     for (int j = 0; j < N; j++)
-                        p[j] = recd_sums_frag<T>(s[j], h);
-#pragma unroll
-                    for (int d = 0; d < DT; d++) {
-                        const Frag w = tile.columns(32 * st + 16 * h, 32 * d, lane);
-                        for (int j = 0; j < N; j++)
-                            o[j][d] = Mma::mul(w, p[j], o[j][d]);
-                    }
+                        o[j][d] = Mma::mul(w, p[j], o[j][d]);
                 }
             }
         }
     }
-    const int64_t part = (int64_t)split * kWaves + wave;
+    // the waves' sums, in their order, into the first one's
+#pragma unroll
+    for (int j = 0; j < N; j++) {
+        l[j] += __shfl_xor(l[j], 32);
+        for (int w = 1; w < kWaves; w++) {
+            __syncthreads();
+            if (wave == w) {
+                lds.join[lane] = m[j];
+                lds.join[64 + lane] = l[j];
+                if constexpr (MEAN)
+#pragma unroll
+                    for (int d = 0; d < DT; d++)
+#pragma unroll
+                        for (int r = 0; r < 16; r++)
+                            lds.join[64 * (2 + 16 * d + r) + lane] = o[j][d][r];
+            }
+            __syncthreads();
+            if (wave == 0) {
+                const float other = lds.join[lane], top = fmaxf(m[j], other), from = top == -INFINITY ? 0.0f : top;
+                const float f = recd_exp2(m[j] - from), g = recd_exp2(other - from);
+                m[j] = top;
+                l[j] = l[j] * f + lds.join[64 + lane] * g;
+                if constexpr (MEAN)
+#pragma unroll
+                    for (int d = 0; d < DT; d++)
+#pragma unroll
+                        for (int r = 0; r < 16; r++)
+                            o[j][d][r] = o[j][d][r] * f + lds.join[64 * (2 + 16 * d + r) + lane] * g;
+            }
+        }
+    }
+    if (wave)
+        return;
+#pragma unroll
     for (int j = 0; j < N; j++) {
         const int64_t row = row0 + 32 * j + (lane & 31);
-        const float sum = l[j] + __shfl_xor(l[j], 32);
         if (row >= a.n)
             continue;
         if (lane < 32) {
-            a.part_m[part * a.n + row] = m[j];
-            a.part_l[part * a.n + row] = sum;
+            a.part_m[split * a.n + row] = m[j];
+            a.part_l[split * a.n + row] = l[j];
         }
         if constexpr (MEAN)
+#pragma unroll
             for (int d = 0; d < DT; d++)
+#pragma unroll
                 for (int r = 0; r < 16; r += 4) {
                     const int col = 32 * d + recd_sums_row(r, lane);
                     if (col < a.D)
-                        *reinterpret_cast<recd_f32x4 *>(a.part_o + (part * a.n + row) * a.D + col) =
+                        *reinterpret_cast<recd_f32x4 *>(a.part_o + (split * a.n + row) * a.D + col) =
                             recd_f32x4{o[j][d][r], o[j][d][r + 1], o[j][d][r + 2], o[j][d][r + 3]};
                 }
     }
@@ -215,7 +246,7 @@ __global__ __launch_bounds__(64 * W) void k_vocab_forward(ForwardArgs a)
     const int rb = at % a.row_blocks, split = at / a.row_blocks * 8 + xcd;
     if (split >= a.splits)
         return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t row0 = ((int64_t)rb * W + wave) * 32 * N;
     const int64_t tiles = (a.V + VT - 1) / VT, t0 = split * a.tiles_per_split;
     const int64_t t1 = t0 + a.tiles_per_split < tiles ? t0 + a.tiles_per_split : tiles;
@@ -290,13 +321,15 @@ __global__ __launch_bounds__(64 * W) void k_vocab_forward(ForwardArgs a)
                             o[j][d][r] *= f;
             }
     };
-    Stream<T, VT, DP, 64 * W> stream;
-    const T *table = (const T *)a.table;
+    RecdStream<T, VT, DP, 64 * W> stream;
+    auto load = [&](int64_t t) {
+        stream.load_rows(threadIdx.x, (const T *)a.table + t * VT * a.D, rows_left(a.V - t * VT), a.D, a.D * sizeof(T));
+    };
     if (t0 < t1) {
-        stream.load(table, t0 * VT, a.V, a.D);
-        stream.store(tiles_lds[0]);
+        load(t0);
+        stream.store(threadIdx.x, tiles_lds[0]);
         if (t0 + 1 < t1)
-            stream.load(table, (t0 + 1) * VT, a.V, a.D);
+            load(t0 + 1);
         __syncthreads();
         scores(tiles_lds[0], 0, s[0]);
         settle(t0 * VT, s[0]);
@@ -305,9 +338,9 @@ __global__ __launch_bounds__(64 * W) void k_vocab_forward(ForwardArgs a)
     for (int64_t t = t0; t < t1; t++) {
         const int next = buf + 1 == BUFS ? 0 : buf + 1;
         if (t + 1 < t1) {
-            stream.store(tiles_lds[next]);
+            stream.store(threadIdx.x, tiles_lds[next]);
             if (t + 2 < t1)
-                stream.load(table, (t + 2) * VT, a.V, a.D);
+                load(t + 2);
         }
 #pragma unroll
         for (int st = 0; st < TURNS; st++) {
@@ -404,15 +437,30 @@ __global__ __launch_bounds__(kBlock) void k_vocab_join(int64_t n, int64_t V, int
     const int64_t row = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6);
     if (row >= n)
         return;
-    float m = -INFINITY;
-    for (int p = lane; p < parts; p += 64)
-        m = fmaxf(m, part_m[p * n + row]);
+    // four parts a lane in flight
+    float m = -INFINITY, l = 0.0f;
+    for (int p0 = lane; p0 < parts; p0 += 256) {
+        float pm[4], pl[4], top = m;
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            const bool there = p0 + 64 * i < parts;
+            pm[i] = there ? part_m[(p0 + 64 * i) * n + row] : -INFINITY;
+            pl[i] = there ? part_l[(p0 + 64 * i) * n + row] : 0.0f;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; i++)
+            top = fmaxf(top, pm[i]);
+        const float from = top == -INFINITY ? 0.0f : top;
+        l *= recd_exp2(m - from);
+#pragma unroll
+        for (int i = 0; i < 4; i++)
+            l += recd_exp2(pm[i] - from) * pl[i];
+        m = top;
+    }
+    const float mine = m;
     m = wave_max(m);
     const float from = m == -INFINITY ? 0.0f : m;
-    float l = 0.0f;
-    for (int p = lane; p < parts; p += 64)
-        l += recd_exp2(part_m[p * n + row] - from) * part_l[p * n + row];
-    l = wave_sum(l);
+    l = wave_sum(l * recd_exp2(mine - from));
     const int64_t t = targets[row];
     float dot = 0.0f;
     if (t >= 0 && t < V)
@@ -525,7 +573,7 @@ template <typename T, int DP, int N, int W> __global__ __launch_bounds__(64 * W)
     __shared__ RecdTile<T, XT, DP> tiles_lds[3];
     __shared__ alignas(16) float lse[3][XT], g[3][XT];
     __shared__ int32_t target[3][XT];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t v0 = ((int64_t)blockIdx.x * W + wave) * 32 * N;
     Frag wf[N][KS];
     recd_f32x16 o[N][DT], s[2][N];
@@ -543,19 +591,19 @@ template <typename T, int DP, int N, int W> __global__ __launch_bounds__(64 * W)
             o[j][d] = recd_f32x16{};
     }
     const int tiles = (int)((a.n + XT - 1) / XT);
-    Stream<T, XT, DP, 64 * W> stream;
+    RecdStream<T, XT, DP, 64 * W> stream;
     float next_lse = 0.0f, next_g = 0.0f;
     int32_t next_t = -1;
     auto load = [&](int t) {
-        stream.load((const T *)a.x, (int64_t)t * XT, a.n, a.D);
+        stream.load_rows(threadIdx.x, (const T *)a.x + (int64_t)t * XT * a.D, rows_left(a.n - (int64_t)t * XT), a.D, a.D * sizeof(T));
         const int64_t row = (int64_t)t * XT + threadIdx.x;
         const bool there = threadIdx.x < XT && row < a.n;
-        next_lse = there ? a.row_lse[row] : 0.0f;
+        next_lse = there ? a.row_lse[row] : INFINITY;  // behind the last row: probability 0
         next_g = there ? a.row_g[row] : 0.0f;
         next_t = there ? a.row_t[row] : -1;
     };
     auto store = [&](int b) {
-        stream.store(tiles_lds[b]);
+        stream.store(threadIdx.x, tiles_lds[b]);
         if (threadIdx.x < XT) {
             const int i = recd_product_row(threadIdx.x);  // a lane reads those of four neighbouring sums at a time
             lse[b][i] = next_lse;
@@ -736,17 +784,16 @@ struct ForwardShape {
     bool share;
     int row_blocks, splits;
     int64_t tiles_per_split;
-    int parts;
 };
 
 ForwardShape forward_shape(const recd_ctx *ctx, int64_t n, int64_t V, int D, recd_dtype dt, bool mean)
 {
     const bool f32 = dt == RECD_F32;
-    const int per_few = f32 || D > 128 ? 32 : 64;
+    const int per_few = (f32 ? (D <= 32 ? 32 : (D + 31) / 32 * 32) * 4 : (D + 31) / 32 * 32 * 2) > 256 ? 32 : 64;
     ForwardShape s;
     s.share = n <= 128;
     const int vt = s.share ? 128 : (f32 && D > 128 ? 32 : 64);
-    const int64_t rows = s.share ? per_few : (f32 ? 128 : 256), tiles = (V + vt - 1) / vt;
+    const int64_t rows = s.share ? per_few : (f32 || D > 192 ? 128 : 256), tiles = (V + vt - 1) / vt;
     s.row_blocks = (int)((n + rows - 1) / rows);
     // A die takes every eighth split, all row blocks of it, and holds one or two blocks a CU at a time (the registers of
     // the sums decide): the number of splits whose rounds are fullest, few of them before many whose parts have to
@@ -764,7 +811,6 @@ ForwardShape forward_shape(const recd_ctx *ctx, int64_t n, int64_t V, int D, rec
     }
     s.tiles_per_split = (tiles + splits - 1) / splits;
     s.splits = (int)((tiles + s.tiles_per_split - 1) / s.tiles_per_split);
-    s.parts = s.share ? s.splits * kWaves : s.splits;
     return s;
 }
 
@@ -811,9 +857,9 @@ recd_status recd_vocab_loss(recd_ctx *ctx, int64_t n, int64_t V, int D, recd_dty
     const ForwardShape s = forward_shape(ctx, n, V, D, dt, mean_row != nullptr);
     WsCarver size(nullptr);
     auto carve = [&](WsCarver &c, ForwardArgs &a) {
-        a.part_m = c.take<float>((size_t)s.parts * n);
-        a.part_l = c.take<float>((size_t)s.parts * n);
-        a.part_o = mean_row ? c.take<float>((size_t)s.parts * n * D) : nullptr;
+        a.part_m = c.take<float>((size_t)s.splits * n);
+        a.part_l = c.take<float>((size_t)s.splits * n);
+        a.part_o = mean_row ? c.take<float>((size_t)s.splits * n * D) : nullptr;
     };
     ForwardArgs a{n, V, D, fabsf(scale) * kRecdLog2e, scale < 0, x, table, s.row_blocks, s.splits, s.tiles_per_split};
     carve(size, a);
@@ -825,7 +871,7 @@ recd_status recd_vocab_loss(recd_ctx *ctx, int64_t n, int64_t V, int D, recd_dty
         using T = decltype(t);
         with_width(D, [&](auto w) { launch_forward<T, w.value>(a, s.share, ctx->stream); });
         hipLaunchKernelGGL((k_vocab_join<T>), dim3((unsigned)((n + kWaves - 1) / kWaves)), dim3(kBlock), 0, ctx->stream, n, V,
-                           D, scale, s.parts, a.part_m, a.part_l, a.part_o, (const T *)x, (const T *)table, targets, loss,
+                           D, scale, s.splits, a.part_m, a.part_l, a.part_o, (const T *)x, (const T *)table, targets, loss,
                            lse, mean_row);
     });
     RECD_HIP(ctx, hipGetLastError());
