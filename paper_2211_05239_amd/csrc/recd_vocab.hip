@@ -32,7 +32,7 @@ template <typename T> constexpr float kLift = std::is_same<T, _Float16>::value ?
 // Tiles of 32 kept rows in a wave, and waves in a block.
 template <typename T, int DP> constexpr int kTiles = 1;
 template <typename T, int DP> constexpr int kManyWaves = sizeof(T) == 4 || DP > 192 ? 4 : 8;
-template <typename T, int DP> constexpr int kFewTiles = sizeof(T) * DP > 256 ? 1 : 2;
+template <typename T, int DP> constexpr int kFewTiles = sizeof(T) == 4 || DP > 128 ? 1 : 2;
 
 // Rows of a tile that are there, of `left` behind its first.
 __device__ inline int rows_left(int64_t left) { return left < 128 ? (int)left : 128; }
@@ -559,12 +559,17 @@ struct TableGradArgs {
     const float *row_lse, *row_g, *lift;
     const int32_t *row_t;
     void *grad_table;
+    int blocks;        // that share the work (groups of table rows times tiles of rows x) evenly
+    float *parts;      // [2 * blocks][rows of a group][D]: sums of groups that several blocks share
 };
+
+// The block that does unit `u` of the work.
+__host__ __device__ inline int64_t block_of(int64_t u, int64_t units, int64_t blocks) { return ((u + 1) * blocks - 1) / units; }
 
 // 32 * N table rows a wave; the rows x stream past them, pipelined as in the forward kernel.  The targets' weights
 // are taken off in a product of their own, in the few subtiles that hold a target of the wave's rows, and in two
 // roundings of which the second takes up what the first leaves: they are most of a row that is a target.
-template <typename T, int DP, int N, int W> __global__ __launch_bounds__(64 * W) void k_vocab_grad_table(TableGradArgs a)
+template <typename T, int DP, int N, int W, bool SHARED> __global__ __launch_bounds__(64 * W) void k_vocab_grad_table(TableGradArgs a)
 {
     constexpr int XT = sizeof(T) == 4 && DP > 128 ? 32 : 64;
     constexpr int KS = DP / 16, DT = DP / 32, TURNS = XT / 32;
@@ -574,23 +579,9 @@ template <typename T, int DP, int N, int W> __global__ __launch_bounds__(64 * W)
     __shared__ alignas(16) float lse[3][XT], g[3][XT];
     __shared__ int32_t target[3][XT];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t v0 = ((int64_t)blockIdx.x * W + wave) * 32 * N;
+    const int tiles = (int)((a.n + XT - 1) / XT);
     Frag wf[N][KS];
     recd_f32x16 o[N][DT], s[2][N];
-#pragma unroll
-    for (int j = 0; j < N; j++) {
-        const int64_t v = v0 + 32 * j + (lane & 31);
-#pragma unroll
-        for (int k = 0; k < KS; k++) {
-            wf[j][k] = recd_row_frag<T>((const T *)a.table + v * a.D, 16 * k, a.D, v < a.V, lane);
-            if (a.negative)
-                wf[j][k] = recd_negated(wf[j][k]);
-        }
-#pragma unroll
-        for (int d = 0; d < DT; d++)
-            o[j][d] = recd_f32x16{};
-    }
-    const int tiles = (int)((a.n + XT - 1) / XT);
     RecdStream<T, XT, DP, 64 * W> stream;
     float next_lse = 0.0f, next_g = 0.0f;
     int32_t next_t = -1;
@@ -623,103 +614,165 @@ template <typename T, int DP, int N, int W> __global__ __launch_bounds__(64 * W)
                 out[j] = Mma::mul(x, wf[j][k], out[j]);
         }
     };
-    if (tiles > 0) {
-        load(0);
-        store(0);
-        if (tiles > 1)
-            load(1);
-        __syncthreads();
-        scores(tiles_lds[0], 0, s[0]);
-    }
-    int buf = 0;
-    for (int t = 0; t < tiles; t++) {
-        const int next = buf + 1 == 3 ? 0 : buf + 1;
-        if (t + 1 < tiles) {
-            store(next);
-            if (t + 2 < tiles)
-                load(t + 2);
-        }
-#pragma unroll
-        for (int st = 0; st < TURNS; st++) {
-            constexpr int kLast = TURNS - 1;
-            const int now = TURNS == 1 ? 0 : st & 1, then = TURNS == 1 ? 1 : 1 - now;
-            if (st == kLast)
-                __syncthreads();
-            // (behind the last tile: of what an older tile left in LDS, for nobody)
-            scores(st == kLast ? tiles_lds[next] : tiles_lds[buf], st == kLast ? 0 : 32 * (st + 1), s[then]);
-#pragma unroll
-            for (int r = 0; r < 16; r += 4) {
-                const int row = 32 * st + recd_sums_row(r, lane);
-                const recd_f32x4 from = *reinterpret_cast<const recd_f32x4 *>(&lse[buf][row]);
-                const recd_f32x4 by = *reinterpret_cast<const recd_f32x4 *>(&g[buf][row]);
-#pragma unroll
-                for (int q = 0; q < 4; q++)
-#pragma unroll
-                    for (int j = 0; j < N; j++)
-                        s[now][j][r + q] = recd_exp2(s[now][j][r + q] * a.c - from[q]) * by[q];
-            }
-#pragma unroll
-            for (int h = 0; h < 2; h++) {
-                Frag p[N];
-#pragma unroll
-                for (int j = 0; j < N; j++)
-                    p[j] = recd_sums_frag<T>(s[now][j], h);
-#pragma unroll
-                for (int d = 0; d < DT; d++) {
-                    const Frag x = tiles_lds[buf].columns(32 * st + 16 * h, 32 * d, lane);
-#pragma unroll
-                    for (int j = 0; j < N; j++)
-                        o[j][d] = Mma::mul(x, p[j], o[j][d]);
-                }
-            }
-            const int32_t mine = target[buf][32 * st + (lane & 31)];
-            if (__any(mine >= v0 && mine < v0 + 32 * N))
-#pragma unroll
-                for (int j = 0; j < N; j++)
-#pragma unroll
-                    for (int h = 0; h < 2; h++) {
-                        Frag p[2];
-#pragma unroll
-                        for (int e = 0; e < 8; e++) {
-                            const int row = 32 * st + recd_sums_row(8 * h + e, lane);
-                            const float w = target[buf][row] == v0 + 32 * j + (lane & 31) ? -g[buf][row] : 0.0f;
-                            p[0][e] = (T)w;
-                            p[1][e] = (T)(w - (float)p[0][e]);
-                        }
-#pragma unroll
-                        for (int d = 0; d < DT; d++) {
-                            const Frag x = tiles_lds[buf].columns(32 * st + 16 * h, 32 * d, lane);
-                            o[j][d] = Mma::mul(x, p[0], o[j][d]);
-                            if constexpr (sizeof(T) == 2)
-                                o[j][d] = Mma::mul(x, p[1], o[j][d]);
-                        }
-                    }
-            if constexpr (TURNS == 1)
-#pragma unroll
-                for (int j = 0; j < N; j++)
-                    s[0][j] = s[1][j];
-        }
-        buf = next;
-    }
+    constexpr int R = 32 * N * W;  // table rows of a group
     const float back = a.lift ? a.scale / *a.lift : a.scale;
+    const int64_t groups = (a.V + R - 1) / R, units = groups * tiles;
+    const int64_t u1 = SHARED ? units * (blockIdx.x + 1) / a.blocks : 0;
+    int64_t u = SHARED ? units * blockIdx.x / a.blocks : 0;
+    do {
+        int64_t group = blockIdx.x;
+        int ta = 0, tb = tiles;
+        if constexpr (SHARED) {
+            group = u / tiles;
+            ta = (int)(u - group * tiles);
+            if (u1 - u < tiles - ta)
+                tb = ta + (int)(u1 - u);
+            u += tb - ta;
+        }
+        const bool whole = !SHARED || (ta == 0 && tb == tiles);
+        const int64_t v0 = (group * W + wave) * 32 * N;
 #pragma unroll
-    for (int j = 0; j < N; j++) {
-        const int64_t v = v0 + 32 * j + (lane & 31);
-        if (v >= a.V)
-            continue;
+        for (int j = 0; j < N; j++) {
+            const int64_t v = v0 + 32 * j + (lane & 31);
 #pragma unroll
-        for (int d = 0; d < DT; d++)
-#pragma unroll
-            for (int r = 0; r < 16; r += 4) {
-                const int col = 32 * d + recd_sums_row(r, lane);
-                if (col >= a.D)
-                    continue;
-                T out[4];
-#pragma unroll
-                for (int q = 0; q < 4; q++)
-                    out[q] = (T)(o[j][d][r + q] * back);
-                __builtin_memcpy((T *)a.grad_table + v * a.D + col, out, sizeof out);
+            for (int k = 0; k < KS; k++) {
+                wf[j][k] = recd_row_frag<T>((const T *)a.table + v * a.D, 16 * k, a.D, v < a.V, lane);
+                if (a.negative)
+                    wf[j][k] = recd_negated(wf[j][k]);
             }
+#pragma unroll
+            for (int d = 0; d < DT; d++)
+                o[j][d] = recd_f32x16{};
+        }
+        if constexpr (SHARED)
+            __syncthreads();  // the last group's readers are through
+        if (ta < tb) {
+            load(ta);
+            store(0);
+            if (ta + 1 < tb)
+                load(ta + 1);
+            __syncthreads();
+            scores(tiles_lds[0], 0, s[0]);
+        }
+        int buf = 0;
+        for (int t = ta; t < tb; t++) {
+            const int next = buf + 1 == 3 ? 0 : buf + 1;
+            if (t + 1 < tb) {
+                store(next);
+                if (t + 2 < tb)
+                    load(t + 2);
+            }
+#pragma unroll
+            for (int st = 0; st < TURNS; st++) {
+                constexpr int kLast = TURNS - 1;
+                const int now = TURNS == 1 ? 0 : st & 1, then = TURNS == 1 ? 1 : 1 - now;
+                if (st == kLast)
+                    __syncthreads();
+                // (behind the last tile: of what an older tile left in LDS, for nobody)
+                scores(st == kLast ? tiles_lds[next] : tiles_lds[buf], st == kLast ? 0 : 32 * (st + 1), s[then]);
+#pragma unroll
+                for (int r = 0; r < 16; r += 4) {
+                    const int row = 32 * st + recd_sums_row(r, lane);
+                    const recd_f32x4 from = *reinterpret_cast<const recd_f32x4 *>(&lse[buf][row]);
+                    const recd_f32x4 by = *reinterpret_cast<const recd_f32x4 *>(&g[buf][row]);
+#pragma unroll
+                    for (int q = 0; q < 4; q++)
+#pragma unroll
+                        for (int j = 0; j < N; j++)
+                            s[now][j][r + q] = recd_exp2(s[now][j][r + q] * a.c - from[q]) * by[q];
+                }
+#pragma unroll
+                for (int h = 0; h < 2; h++) {
+                    Frag p[N];
+#pragma unroll
+                    for (int j = 0; j < N; j++)
+                        p[j] = recd_sums_frag<T>(s[now][j], h);
+#pragma unroll
+                    for (int d = 0; d < DT; d++) {
+                        const Frag x = tiles_lds[buf].columns(32 * st + 16 * h, 32 * d, lane);
+#pragma unroll
+                        for (int j = 0; j < N; j++)
+                            o[j][d] = Mma::mul(x, p[j], o[j][d]);
+                    }
+                }
+                const int32_t mine = target[buf][32 * st + (lane & 31)];
+                if (__any(mine >= v0 && mine < v0 + 32 * N))
+#pragma unroll
+                    for (int j = 0; j < N; j++)
+#pragma unroll
+                        for (int h = 0; h < 2; h++) {
+                            Frag p[2];
+#pragma unroll
+                            for (int e = 0; e < 8; e++) {
+                                const int row = 32 * st + recd_sums_row(8 * h + e, lane);
+                                const float w = target[buf][row] == v0 + 32 * j + (lane & 31) ? -g[buf][row] : 0.0f;
+                                p[0][e] = (T)w;
+                                p[1][e] = (T)(w - (float)p[0][e]);
+                            }
+#pragma unroll
+                            for (int d = 0; d < DT; d++) {
+                                const Frag x = tiles_lds[buf].columns(32 * st + 16 * h, 32 * d, lane);
+                                o[j][d] = Mma::mul(x, p[0], o[j][d]);
+                                if constexpr (sizeof(T) == 2)
+                                    o[j][d] = Mma::mul(x, p[1], o[j][d]);
+                            }
+                        }
+                if constexpr (TURNS == 1)
+#pragma unroll
+                    for (int j = 0; j < N; j++)
+                        s[0][j] = s[1][j];
+            }
+            buf = next;
+        }
+#pragma unroll
+        for (int j = 0; j < N; j++) {
+            const int64_t v = v0 + 32 * j + (lane & 31);
+            if (v >= a.V)
+                continue;
+            float *part = whole ? nullptr : a.parts + ((2 * (int64_t)blockIdx.x + (ta == 0)) * R + (wave * N + j) * 32 + (lane & 31)) * a.D;
+#pragma unroll
+            for (int d = 0; d < DT; d++)
+#pragma unroll
+                for (int r = 0; r < 16; r += 4) {
+                    const int col = 32 * d + recd_sums_row(r, lane);
+                    if (col >= a.D)
+                        continue;
+                    if (!whole) {
+                        *reinterpret_cast<recd_f32x4 *>(part + col) =
+                            recd_f32x4{o[j][d][r], o[j][d][r + 1], o[j][d][r + 2], o[j][d][r + 3]};
+                        continue;
+                    }
+                    T out[4];
+#pragma unroll
+                    for (int q = 0; q < 4; q++)
+                        out[q] = (T)(o[j][d][r + q] * back);
+                    __builtin_memcpy((T *)a.grad_table + v * a.D + col, out, sizeof out);
+                }
+        }
+    } while (SHARED && u < u1);
+}
+
+// Adds up the parts of the groups that several blocks share, in the blocks' order: a block of threads per group.
+template <typename T>
+__global__ __launch_bounds__(kBlock) void k_vocab_join_table(TableGradArgs a, int R, int64_t each, int64_t units)
+{
+    const int64_t first = blockIdx.x * each, b0 = block_of(first, units, a.blocks), b1 = block_of(first + each - 1, units, a.blocks);
+    if (b0 == b1)
+        return;
+    const float back = a.lift ? a.scale / *a.lift : a.scale;
+    const int64_t v0 = (int64_t)blockIdx.x * R;
+    const int rows = a.V - v0 < R ? (int)(a.V - v0) : R, pieces = rows * a.D / 4;
+    for (int i = threadIdx.x; i < pieces; i += kBlock) {
+        recd_f32x4 s = reinterpret_cast<const recd_f32x4 *>(a.parts + (2 * b0 + 1) * R * a.D)[i];
+        for (int64_t b = b0 + 1; b <= b1; b++) {
+            const recd_f32x4 x = reinterpret_cast<const recd_f32x4 *>(a.parts + 2 * b * R * a.D)[i];
+            for (int e = 0; e < 4; e++)
+                s[e] += x[e];
+        }
+        T out[4];
+        for (int e = 0; e < 4; e++)
+            out[e] = (T)(s[e] * back);
+        __builtin_memcpy((T *)a.grad_table + v0 * a.D + 4 * i, out, sizeof out);
     }
 }
 
@@ -789,7 +842,7 @@ struct ForwardShape {
 ForwardShape forward_shape(const recd_ctx *ctx, int64_t n, int64_t V, int D, recd_dtype dt, bool mean)
 {
     const bool f32 = dt == RECD_F32;
-    const int per_few = (f32 ? (D <= 32 ? 32 : (D + 31) / 32 * 32) * 4 : (D + 31) / 32 * 32 * 2) > 256 ? 32 : 64;
+    const int per_few = f32 || D > 128 ? 32 : 64;
     ForwardShape s;
     s.share = n <= 128;
     const int vt = s.share ? 128 : (f32 && D > 128 ? 32 : 64);
@@ -829,10 +882,52 @@ template <typename T, int DP> void launch_forward(const ForwardArgs &a, bool sha
         hipLaunchKernelGGL((k_vocab_forward<T, DP, N, W, false>), grid, dim3(64 * W), 0, st, a);
 }
 
-template <typename T, int DP> void launch_grad_table(const TableGradArgs &a, hipStream_t st)
+// How the table's gradient is cut: blocks that are on the card at a time take equal shares of all (group of table rows,
+// tile of rows x) where the last round of whole groups would leave more of the card idle than it costs to write the
+// shared groups' parts and add them up (16 bytes an element, at about 4.5 TB/s; the sums run at about 0.9 PFLOP/s, 0.1 in
+// fp32), else one block a group.
+struct TableShape {
+    int R;             // table rows of a group
+    int64_t each, units;
+    int blocks;
+    bool shared;
+};
+
+template <typename T, int DP> TableShape table_shape(const recd_ctx *ctx, int64_t n, int64_t V, int D)
 {
-    constexpr int N = kTiles<T, DP>, W = kManyWaves<T, DP>, rows = 32 * N * W;
-    hipLaunchKernelGGL((k_vocab_grad_table<T, DP, N, W>), dim3((unsigned)((a.V + rows - 1) / rows)), dim3(64 * W), 0, st, a);
+    constexpr int N = kTiles<T, DP>, W = kManyWaves<T, DP>, XT = sizeof(T) == 4 && DP > 128 ? 32 : 64;
+    static const int resident = [] {
+        int b = 0;
+        if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&b, (const void *)k_vocab_grad_table<T, DP, N, W, true>, 64 * W, 0) != hipSuccess) {
+            (void)hipGetLastError();
+            b = 1;
+        }
+        return b > 0 ? b : 1;
+    }();
+    TableShape s;
+    s.R = 32 * N * W;
+    const int64_t groups = (V + s.R - 1) / s.R, slots = (int64_t)ctx->num_cu * resident;
+    s.each = n > 0 ? (n + XT - 1) / XT : 1;
+    s.units = groups * s.each;
+    const double work = 4.0 * (double)n * (double)V * D / (sizeof(T) == 4 ? 1e14 : 9e14);
+    const double idle = (double)((groups + slots - 1) / slots * slots) / (double)groups - 1.0;
+    // (a block that may go through several groups is 15 % slower in 16 bits)
+    const double gain = (idle - (sizeof(T) == 2 ? 0.15 : 0.0)) * work;
+    s.shared = n > 0 && s.units >= slots && gain > (double)(slots * s.R) * D * 16 / 4.5e12 + 5e-6;
+    s.blocks = (int)(s.shared ? slots : groups);
+    return s;
+}
+
+template <typename T, int DP> void launch_grad_table(const TableGradArgs &a, const TableShape &s, hipStream_t st)
+{
+    constexpr int N = kTiles<T, DP>, W = kManyWaves<T, DP>;
+    if (s.shared)
+        hipLaunchKernelGGL((k_vocab_grad_table<T, DP, N, W, true>), dim3((unsigned)s.blocks), dim3(64 * W), 0, st, a);
+    else
+        hipLaunchKernelGGL((k_vocab_grad_table<T, DP, N, W, false>), dim3((unsigned)s.blocks), dim3(64 * W), 0, st, a);
+    if (s.shared)
+        hipLaunchKernelGGL((k_vocab_join_table<T>), dim3((unsigned)((a.V + s.R - 1) / s.R)), dim3(kBlock), 0, st, a, s.R, s.each,
+                           s.units);
 }
 
 } // namespace
@@ -898,9 +993,13 @@ recd_status recd_vocab_loss_backward(recd_ctx *ctx, int64_t n, int64_t V, int D,
         RECD_TRY(validate_targets(ctx, n, V, targets));
     const bool lifted = dt == RECD_F16 && grad_table && n > 0;
     WsCarver size(nullptr);
-    float *row_lse, *row_g, *lift;
+    float *row_lse, *row_g, *lift, *parts;
     int32_t *row_t;
+    TableShape shape{};
+    if (grad_table)
+        recd_with_type(dt, [&](auto t) { with_width(D, [&](auto w) { shape = table_shape<decltype(t), w.value>(ctx, n, V, D); }); });
     auto carve = [&](WsCarver &c) {
+        parts = shape.shared ? c.take<float>((size_t)2 * shape.blocks * shape.R * D) : nullptr;
         row_lse = grad_table ? c.take<float>(n) : nullptr;
         row_g = grad_table ? c.take<float>(n) : nullptr;
         row_t = grad_table ? c.take<int32_t>(n) : nullptr;
@@ -921,8 +1020,8 @@ recd_status recd_vocab_loss_backward(recd_ctx *ctx, int64_t n, int64_t V, int D,
                                (T *)grad_x);
         if (!grad_table)
             return;
-        TableGradArgs a{n, V, D, fabsf(scale) * kRecdLog2e, scale, scale < 0, x, table, row_lse, row_g, lift, row_t, grad_table};
-        with_width(D, [&](auto w) { launch_grad_table<T, w.value>(a, ctx->stream); });
+        TableGradArgs a{n, V, D, fabsf(scale) * kRecdLog2e, scale, scale < 0, x, table, row_lse, row_g, lift, row_t, grad_table, shape.blocks, parts};
+        with_width(D, [&](auto w) { launch_grad_table<T, w.value>(a, shape, ctx->stream); });
     });
     RECD_HIP(ctx, hipGetLastError());
     return RECD_OK;

@@ -59,6 +59,16 @@ def test_sizes(ctx, dt, n, V, D):
     check(ctx, *data(n, V, D, dt, n + V)[:3], 1.0, data(n, V, D, dt, n + V)[3])
 
 
+# small tables and many rows: the table's gradient is cut across its rows, and their parts are added up
+@pytest.mark.parametrize("dt,n,V,D", [("f32", 2000, 9000, 64), ("f16", 3000, 9001, 128), ("bf16", 2999, 5000, 96)])
+def test_table_rows_that_several_blocks_share(ctx, dt, n, V, D):
+    x, table, t, gl = data(n, V, D, dt, 21)
+    a = check(ctx, x, table, t, 1.0, gl)
+    b, _ = run(ctx, x, table, t, 1.0, gl)
+    for k in a:
+        assert torch.equal(a[k], b[k]), k
+
+
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
 @pytest.mark.parametrize("scale", [-0.7, 0.05, 20.0])
 def test_scales(ctx, dt, scale):
