@@ -161,12 +161,16 @@ template <int DT, int PHASES> __device__ inline void join_sums(recd_f32x16 (&o)[
     }
 }
 
-// cap * log2(e) * tanh(x) + more from x' = 2 log2(e) x, and a quarter of the derivative, (1 - tanh^2) / 4.
-// tanh(x) = 1 - 2 r with r = 1 / (1 + e^2x), off by 2^-23 wherever x lies.  That is enough beside 16-bit operands; for fp32
-// small x take Lambert's continued fraction, x (945 + 105 x^2 + x^4) / (945 + 420 x^2 + 15 x^4), off by 2e-9 of x at 1/2.
+// cap * log2(e) * tanh(x) + (more - base) from x' = 2 log2(e) x, and a quarter of the derivative, (1 - tanh^2) / 4.
+// tanh(x) = 1 - 2 r with r = 1 / (1 + e^2x), off by 2^-23 wherever x lies.  That is enough beside 16-bit operands, where the
+// caller's `more` also brings the 1 along (base = cap * log2(e)).  For fp32 small x take Lambert's continued fraction,
+// x (945 + 105 x^2 + x^4) / (945 + 420 x^2 + 15 x^4), off by 2e-9 of x at 1/2.
 template <typename T> struct Capped {
-    float cap, cap_n2;  // cap * log2(e) and -2 times that
-    __device__ inline explicit Capped(float c) : cap(c * kRecdLog2e), cap_n2(-2.0f * c * kRecdLog2e) {}
+    float cap, cap_n2, base;  // cap * log2(e), -2 times that, and what `more` has to hold besides
+    __device__ inline Capped(float c, bool used)
+        : cap(c * kRecdLog2e), cap_n2(-2.0f * c * kRecdLog2e), base(used && sizeof(T) == 2 ? c * kRecdLog2e : 0.0f)
+    {
+    }
     __device__ inline float value(float x2, float more, float &quarter) const
     {
         const float r = __builtin_amdgcn_rcpf(1.0f + recd_exp2(x2));
@@ -178,7 +182,7 @@ template <typename T> struct Capped {
                 t = x * (945.0f + y * (105.0f + y)) / (945.0f + y * (420.0f + 15.0f * y));
             return cap * t + more;
         }
-        return cap_n2 * r + (cap + more);
+        return cap_n2 * r + more;
     }
 };
 
@@ -251,7 +255,7 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
     const float scale = fabsf(a.scale), c = scale * kRecdLog2e;
     const bool plain = !CAP && !a.slopes && c > 0.0f;
     const float by = plain ? c : 1.0f;
-    const Capped<T> capped(a.cap);
+    const Capped<T> capped(a.cap, CAP);
     const float to_cap = CAP ? 2.0f * kRecdLog2e * scale / a.cap : 0.0f;
 
     Frag qf[KS];
@@ -284,7 +288,7 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
             const float far = posf - (float)(j0 + (lane >> 5));
 #pragma unroll
             for (int r = 0; r < 16; r++) {
-                const float bias = -slope * fabsf(far - (float)recd_score_row(r, 0));
+                const float bias = capped.base - slope * fabsf(far - (float)recd_score_row(r, 0));
                 float unused;
                 x[r] = CAP ? capped.value(x[r] * to_cap, bias, unused) : x[r] * c + bias;
             }
@@ -292,7 +296,7 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
 #pragma unroll
             for (int r = 0; r < 16; r++) {
                 float unused;
-                x[r] = CAP ? capped.value(x[r] * to_cap, 0.0f, unused) : x[r] * c;
+                x[r] = CAP ? capped.value(x[r] * to_cap, capped.base, unused) : x[r] * c;
             }
         }
         if (j0 + 32 > wave_full) {
@@ -440,7 +444,7 @@ template <typename T, int DP, bool CAP> __global__ __launch_bounds__(64, (sizeof
     const int64_t q_row = p.q0 + query;
     const float posf = (float)(p.pos0 + query);
     const float c = a.scale * kRecdLog2e;
-    const Capped<T> capped(a.cap);
+    const Capped<T> capped(a.cap, CAP);
     const float to_cap = CAP ? 2.0f * kRecdLog2e * a.scale / a.cap : 0.0f;
     Frag qf[KS], qn[KS];
     float slope = 0.0f, slope_n = 0.0f, m = -INFINITY, l = 0.0f;
@@ -515,7 +519,7 @@ template <typename T, int DP, bool CAP> __global__ __launch_bounds__(64, (sizeof
                 const float far = posf - (float)(j0 + (lane >> 5));
 #pragma unroll
                 for (int r = 0; r < NR; r++) {
-                    const float bias = -slope * fabsf(far - (float)recd_score_row(r, 0));
+                    const float bias = capped.base - slope * fabsf(far - (float)recd_score_row(r, 0));
                     float unused;
                     s[r] = CAP ? capped.value(s[r] * to_cap, bias, unused) : s[r] * c + bias;
                 }
@@ -523,7 +527,7 @@ template <typename T, int DP, bool CAP> __global__ __launch_bounds__(64, (sizeof
 #pragma unroll
                 for (int r = 0; r < NR; r++) {
                     float unused;
-                    s[r] = CAP ? capped.value(s[r] * to_cap, 0.0f, unused) : s[r] * c;
+                    s[r] = CAP ? capped.value(s[r] * to_cap, capped.base, unused) : s[r] * c;
                 }
             }
             if (j0 + 2 * NR > full) {
@@ -782,7 +786,7 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
     const float posf = (float)(p.pos0 + query);
     const float lift = kHalf<T> ? *a.lift : 1.0f;
     const float c = a.scale * kRecdLog2e;
-    const Capped<T> capped(a.cap);
+    const Capped<T> capped(a.cap, CAP);
     const float to_cap = CAP ? 2.0f * kRecdLog2e * a.scale / a.cap : 0.0f;
 
     // delta = g . o, which the gradients by keys need too
@@ -807,6 +811,7 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
     float from = there ? a.lse_in[at_row] * kRecdLog2e : 0.0f;
     if (from == -INFINITY)
         from = 0.0f;  // sees nothing
+    from = capped.base - from;
     recd_f32x16 o[DT];
 #pragma unroll
     for (int d = 0; d < DT; d++)
@@ -849,11 +854,11 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
                 const float far = posf - (float)(j0 + (lane >> 5));
 #pragma unroll
                 for (int r = 0; r < NR; r++)
-                    s[r] = ds_of(s[r], dp[r], -slope * fabsf(far - (float)recd_score_row(r, 0)) - from);
+                    s[r] = ds_of(s[r], dp[r], from - slope * fabsf(far - (float)recd_score_row(r, 0)));
             } else {
 #pragma unroll
                 for (int r = 0; r < NR; r++)
-                    s[r] = ds_of(s[r], dp[r], -from);
+                    s[r] = ds_of(s[r], dp[r], from);
             }
             if (j0 + 2 * NR > wave_full) {
                 asm volatile("");  // a branch: only the tiles at the mask's edge pay for it
@@ -942,7 +947,7 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
     // probabilities are held 2^kLiftP larger, by their exponents; ds by that and, from dp on, the rest of its lift
     const float lift = kHalf<T> ? *a.lift : 1.0f, lift_dp = lift * recd_exp2(-kLiftP<T>);
     const float c = a.scale * kRecdLog2e;
-    const Capped<T> capped(a.cap);
+    const Capped<T> capped(a.cap, CAP);
     const float to_cap = CAP ? 2.0f * kRecdLog2e * a.scale / a.cap : 0.0f;
     // the first row that sees the block's first key
     int from_row = 0;
@@ -977,7 +982,7 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
         if (tid < S::ROWS && row + tid < p.rows) {
             const int in = query_of(tid), query = q_first + in, h = head * a.group + odd + tid - in * a.group;
             n_from = a.lse_in[(p.q0 + query) * H + h] * kRecdLog2e;
-            n_from = (n_from == -INFINITY ? 0.0f : -n_from) + kLiftP<T>;
+            n_from = (n_from == -INFINITY ? 0.0f : -n_from) + (kLiftP<T> + capped.base);
             n_delta = a.delta[(p.q0 + query) * H + h] * lift_dp;
             n_slope = a.slopes ? a.slopes[h] * kRecdLog2e : 0.0f;
             n_lim = p.limit_at(query);
