@@ -181,8 +181,9 @@ __global__ __launch_bounds__(1024) void k_sum_parts(int blocks, int D, const flo
         grad_bias[col - D] = s;
 }
 
-// Lanes and pieces of a row: as few idle lanes as possible; of equal ones two pieces a lane, whose two loads are in
-// flight together.
+// Lanes and pieces of a row: as few idle lanes as possible, and of equal ones the fewest pieces a lane. With two pieces a lane
+// where one would do, forward and backward of 300 007 rows of 64 bf16 take 63 us against 48, of 128 elements 101 against 92;
+// with four, 134 and 164.
 struct Shape {
     int P, glog;
 };
@@ -191,7 +192,7 @@ Shape row_shape(int vecs)
 {
     Shape best{0, 0};
     int cost = 1 << 30;
-    for (int P : {2, 1, 3, 4}) {
+    for (int P : {1, 2, 3, 4}) {
         int glog = 0;
         while ((P << glog) < vecs)
             glog++;
