@@ -1197,20 +1197,32 @@ struct Tiling {
 };
 
 // Lists of few rows (here and on the other side) give every tile to a wave of its own; so many tiles that four groups in a
-// block fill the card share what they stream; in between a tile's streamed rows are divided among the waves.
+// block fill the card share what they stream; in between a tile's streamed rows are divided among the waves. In us,
+// forward and backward, bf16, lists that attend to themselves under the causal mask, one wave / phases / groups:
+//   2000 lists of 80 rows, 4 heads of 32       43, 134 / 127, 262 / 48, 145
+//   64 lists of 300, 4 heads on 2 of 64        18, 50 / 32, 66 / 14, 50
+//   8 lists of up to 4096, 8 on 4 heads of 128  317, 883 / 342, 905 / 135, 423
+// and single rows, 8 heads on 2 of 64: 2000 lists of 100 keys 24 / 44 / 35, 37 lists of up to 16 384 53 / 39 / 58.
+// Where phases give way to groups: a block of phases holds the parts of four waves in the LDS that a block of groups
+// shares, and wide heads leave fewer of them to a compute unit, so the number of groups' blocks from which the groups
+// are faster falls with the width. Phases against groups, gradients by keys at lists of 400 rows, in us:
+//   bf16, heads of 32:   256 blocks 11 / 19, 512 blocks 18 / 20, 768 blocks 24 / 21
+//   bf16, heads of 64:   256 blocks 19 / 24, 512 blocks 34 / 27
+//   bf16, heads of 128:  64 blocks 19 / 23, 128 blocks 27 / 24, 256 blocks 48 / 26
+//   fp32, heads of 32:   256 blocks 28 / 42, 512 blocks 51 / 53, and the forward pass 22 / 24 and 35 / 33
+//   fp32, heads of 64:   256 blocks 60 / 71, 512 blocks 112 / 90, and the forward pass 42 / 39 and 77 / 57
 Tiling tiling(const recd_ctx *ctx, const recd_attention *d, int64_t rows, int64_t most, int group, int64_t others,
-              int64_t most_others, int waves = 4)
+              int64_t most_others)
 {
     Tiling t;
-    const int64_t per_four = (most * group + 127) / 128;
-    int64_t four = rows * group / 128 + d->lists;
-    if (four > d->lists * per_four)
-        four = d->lists * per_four;
-    const bool few = most * group <= 64 || rows * group <= 48 * d->lists;
-    const bool wide = d->dtype == RECD_F32 && d->head_dim > 64;  // tiles of 17 KB: phases would leave two waves to a compute unit
+    // groups' blocks, each counted for as much as its list is long beside the longest, which they wait for
+    const double blocks = (double)(rows * group) / 128 * d->kv_heads * ((double)others / ((double)d->lists * (double)(most_others > 0 ? most_others : 1)));
+    const bool f32 = d->dtype == RECD_F32, few = most * group <= 64 || rows * group <= 48 * d->lists;
+    const bool wide = f32 && d->head_dim > 64;  // tiles of 17 KB: phases would leave two waves to a compute unit
+    const int quarters = d->head_dim <= 32 ? (f32 ? 6 : 8) : d->head_dim <= 64 ? (f32 ? 4 : 5) : 2;
     if (few && (wide || most_others <= 128 || others <= 64 * d->lists))
         t.division = ONE_WAVE;
-    else if (!wide && (few || four * d->kv_heads * waves < 12 * ctx->num_cu))
+    else if (!wide && (few || 4 * blocks < (double)quarters * ctx->num_cu))
         t.division = PHASES;
     else
         t.division = GROUPS;
@@ -1403,8 +1415,7 @@ recd_status recd_list_attention_backward(recd_ctx *ctx, const recd_attention *d,
     a.gk_stride = grad_k_stride;
     a.gv_stride = grad_v_stride;
     const Tiling tq = tiling(ctx, d, d->q_rows, d->max_q, a.group, d->k_rows, d->max_k);
-    const Tiling tk = tiling(ctx, d, d->k_rows, d->max_k, 1, d->q_rows * a.group, d->max_q * a.group,
-                             d->dtype != RECD_F32 && a.d > 64 ? 8 : 4);
+    const Tiling tk = tiling(ctx, d, d->k_rows, d->max_k, 1, d->q_rows * a.group, d->max_q * a.group);
     if (tq.slots / 8 + 1 > ((int64_t)1 << 27) / a.G || tk.slots / 8 + 1 > ((int64_t)1 << 27) / a.G)
         return recd_fail(ctx, RECD_EINVAL, "too many tiles");
     const bool half = d->dtype == RECD_F16;
