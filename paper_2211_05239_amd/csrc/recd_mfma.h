@@ -129,6 +129,8 @@ template <typename T, int ROWS, int DP, int THREADS> struct RecdStream {
     {
         load(tid, first, rows, d, [=](int r) { return (uint32_t)__umul24(r, stride); });
     }
+    // the tile's row of a thread's piece i
+    static __device__ inline int row(int tid, int i) { return (tid + i * THREADS) / (DP / Tile::E); }
     __device__ inline void store(int tid, Tile &t)
     {
 #pragma unroll

@@ -489,14 +489,16 @@ __global__ __launch_bounds__(kBlock) void k_vocab_join(int64_t n, int64_t V, int
     }
 }
 
-// The power of two that brings the largest |grad_loss| into [2^13, 2^14): fp16 products of it with probabilities neither
-// overflow nor lose bits that matter beside the largest.
-__global__ __launch_bounds__(1024) void k_vocab_lift(int64_t n, const float *__restrict__ grad_loss, float *lift)
+// The power of two that brings the largest |grad_loss| of the rows with a target into [2^13, 2^14): fp16 products of it with
+// probabilities neither overflow nor lose bits that matter beside the largest.
+__global__ __launch_bounds__(1024) void k_vocab_lift(int64_t n, int64_t V, const int64_t *__restrict__ targets,
+                                                     const float *__restrict__ grad_loss, float *lift)
 {
     __shared__ float tops[16];
     float top = 0.0f;
     for (int64_t i = threadIdx.x; i < n; i += 1024)
-        top = fmaxf(top, fabsf(grad_loss[i]));
+        if ((uint64_t)targets[i] < (uint64_t)V)
+            top = fmaxf(top, fabsf(grad_loss[i]));
     top = wave_max(top);
     if ((threadIdx.x & 63) == 0)
         tops[threadIdx.x >> 6] = top;
@@ -529,7 +531,7 @@ __global__ __launch_bounds__(kBlock) void k_vocab_rows(int64_t n, int64_t V, int
     const bool has = t >= 0 && t < V;
     const float g = has ? grad_loss[row] : 0.0f;
     if (lane == 0 && row_g) {
-        row_lse[row] = lse[row] * kRecdLog2e;
+        row_lse[row] = has ? lse[row] * kRecdLog2e : INFINITY;
         row_g[row] = lift ? g * *lift : g;
         row_t[row] = has ? (int32_t)t : -1;
     }
@@ -584,9 +586,15 @@ template <typename T, int DP, int N, int W, bool SHARED> __global__ __launch_bou
     recd_f32x16 o[N][DT], s[2][N];
     RecdStream<T, XT, DP, 64 * W> stream;
     float next_lse = 0.0f, next_g = 0.0f;
-    int32_t next_t = -1;
+    int32_t next_t = -1, piece_t[decltype(stream)::PT];
     auto load = [&](int t) {
-        stream.load_rows(threadIdx.x, (const T *)a.x + (int64_t)t * XT * a.D, rows_left(a.n - (int64_t)t * XT), a.D, a.D * sizeof(T));
+        const int left = rows_left(a.n - (int64_t)t * XT);
+#pragma unroll
+        for (int i = 0; i < decltype(stream)::PT; i++) {
+            const int r = stream.row(threadIdx.x, i);
+            piece_t[i] = (a.row_t + (int64_t)t * XT)[r < left ? r : left - 1];
+        }
+        stream.load_rows(threadIdx.x, (const T *)a.x + (int64_t)t * XT * a.D, left, a.D, a.D * sizeof(T));
         const int64_t row = (int64_t)t * XT + threadIdx.x;
         const bool there = threadIdx.x < XT && row < a.n;
         next_lse = there ? a.row_lse[row] : INFINITY;  // behind the last row: probability 0
@@ -594,6 +602,10 @@ template <typename T, int DP, int N, int W, bool SHARED> __global__ __launch_bou
         next_t = there ? a.row_t[row] : -1;
     };
     auto store = [&](int b) {
+        // a row without a target may hold anything: it counts as zeros, which no probability turns into a NaN
+#pragma unroll
+        for (int i = 0; i < decltype(stream)::PT; i++)
+            stream.held[i] = piece_t[i] < 0 ? typename decltype(stream)::Piece{} : stream.held[i];
         stream.store(threadIdx.x, tiles_lds[b]);
         if (threadIdx.x < XT) {
             const int i = recd_product_row(threadIdx.x);  // a lane reads those of four neighbouring sums at a time
@@ -1013,7 +1025,7 @@ recd_status recd_vocab_loss_backward(recd_ctx *ctx, int64_t n, int64_t V, int D,
     WsCarver c(ctx->ws);
     carve(c);
     if (lifted)
-        hipLaunchKernelGGL(k_vocab_lift, dim3(1), dim3(1024), 0, ctx->stream, n, grad_loss, lift);
+        hipLaunchKernelGGL(k_vocab_lift, dim3(1), dim3(1024), 0, ctx->stream, n, V, targets, grad_loss, lift);
     recd_with_type(dt, [&](auto t) {
         using T = decltype(t);
         if (n > 0)

@@ -137,6 +137,23 @@ def test_a_row_that_is_not_finite_stays_by_itself(ctx):
     assert got["lse"][7].isnan() and got["lse"][others].isfinite().all() and got["grad_x"][others].isfinite().all()
 
 
+@pytest.mark.parametrize("dt", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("n,V,D", [(90, 300, 64), (700, 3000, 128), (300, 500, 200)])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+def test_rows_without_a_target_may_hold_anything(ctx, dt, n, V, D, bad):
+    """Neither their elements nor their losses' weights reach a gradient."""
+    x, table, t, gl = data(n, V, D, dt, 8)
+    ref = du.loss_ref(x, table, t, 1.0, gl)
+    x[t < 0, ::2] = bad
+    gl[t < 0] = bad
+    got, _ = run(ctx, x, table, t, 1.0, gl)
+    du.within(got["grad_table"], *ref["grad_table"], what="grad_table")
+    du.within(got["grad_x"], *ref["grad_x"], what="grad_x")
+    has = t >= 0
+    du.within(got["loss"].cpu(), *ref["loss"], what="loss")
+    du.within(got["lse"].cpu()[has], ref["lse"][0][has], ref["lse"][1][has], what="lse")
+
+
 def test_same_bits_again(ctx):
     x, table, t, gl = data(500, 5000, 128, "bf16", 11)
     a, _ = run(ctx, x, table, t, 1.0, gl)
