@@ -204,6 +204,144 @@ template <typename T, int DT> __device__ inline void store_columns(T *row, const
         }
 }
 
+// What is masked enters the products with weight 0, which is not enough where it is an infinity or a NaN: 0 * NaN is a NaN,
+// in rows of the tile that do not see it.  Sums that are not finite are therefore thrown away and their rows done again,
+// one at a time by the whole wave and over what they see alone.  The check costs an addition a sum at the kernel's end;
+// the way of one row, which only such data takes, is plain.
+//
+// The rows (lanes of the tile's sums) that are to be done again, a bit each.
+template <int DT> __device__ inline uint32_t not_finite(const recd_f32x16 (&o)[DT], bool there)
+{
+    float s = 0.0f;
+#pragma unroll
+    for (int t = 0; t < DT; t++)
+#pragma unroll
+        for (int r = 0; r < 16; r++)
+            s += o[t][r] * 0.0f;
+    const uint64_t lanes = __ballot(there && !(s == 0.0f));
+    return (uint32_t)lanes | (uint32_t)(lanes >> 32);
+}
+
+// <x, y> of two heads, in every lane.
+template <typename T> __device__ inline float wave_dot(const T *x, const T *y, int d, int lane)
+{
+    float s = 0.0f;
+    for (int e = lane; e < d; e += 64)
+        s += (float)x[e] * (float)y[e];
+    for (int o = 32; o; o >>= 1)
+        s += __shfl_xor(s, o);
+    return s;
+}
+
+// The score of query row `query`, head h, and key j in powers of two, and its derivative by the scaled product.
+__device__ inline float plain_score(const Args &a, const Problem &p, float dot, int query, int h, int j, float &slope_of)
+{
+    float z = dot * a.scale;
+    slope_of = 1.0f;
+    if (a.cap > 0.0f) {
+        const float t = tanhf(z / a.cap);
+        slope_of = 1.0f - t * t;
+        z = a.cap * t;
+    }
+    if (a.slopes)
+        z -= a.slopes[h] * fabsf((float)(p.pos0 + query - j));
+    return z * kRecdLog2e;
+}
+
+// Row `row` of the forward pass over the keys [j0, j1) of those it sees.
+template <typename T> __device__ void attend_again(const Args &a, const Problem &p, int head, int row, int j0, int j1, int split, int lane)
+{
+    const int query = p.query(row, a.group), h = head * a.group + row - query * a.group, lim = p.limit(row, a.group);
+    const int64_t at_row = (p.q0 + query) * (a.G * a.group) + h;
+    const T *q = (const T *)a.q + (p.q0 + query) * a.q_stride + (int64_t)h * a.d;
+    float m = -INFINITY, l = 0.0f, o[2] = {0.0f, 0.0f}, unused;
+    for (int j = j0; j < j1 && j < lim; j++) {
+        const T *k = (const T *)a.k + (p.k0 + j) * a.k_stride + (int64_t)head * a.d;
+        const T *v = (const T *)a.v + (p.k0 + j) * a.v_stride + (int64_t)head * a.d;
+        const float z = plain_score(a, p, wave_dot(q, k, a.d, lane), query, h, j, unused);
+        const float now = fmaxf(m, z), from = now == -INFINITY ? 0.0f : now, f = recd_exp2(m - from), w = recd_exp2(z - from);
+        m = now;
+        l = l * f + w;
+        for (int i = 0; i < 2; i++)
+            if (lane + 64 * i < a.d)
+                o[i] = o[i] * f + w * (float)v[lane + 64 * i];
+    }
+    const int64_t at = split * a.part_rows + at_row;
+    if (lane == 0 && a.splits > 1) {
+        a.part_m[at] = m;
+        a.part_l[at] = l;
+    } else if (lane == 0 && a.lse) {
+        a.lse[at_row] = (m + log2f(l)) * kRecdLn2;
+    }
+    for (int i = 0; i < 2; i++) {
+        const int e = lane + 64 * i;
+        if (e >= a.d)
+            continue;
+        if (a.splits > 1)
+            a.part_o[at * a.d + e] = o[i];
+        else
+            ((T *)a.out)[at_row * a.d + e] = (T)(l == 0.0f ? 0.0f : o[i] / l);
+    }
+}
+
+// The weights of the pair (row, key j) in the gradients: p for dv, ds / scale for dq and dk.
+template <typename T>
+__device__ inline void pair_again(const Args &a, const Problem &p, int head, int row, int j, int lane, float &weight, float &ds)
+{
+    const int query = p.query(row, a.group), h = head * a.group + row - query * a.group;
+    const int64_t at_row = (p.q0 + query) * (a.G * a.group) + h;
+    const T *k = (const T *)a.k + (p.k0 + j) * a.k_stride + (int64_t)head * a.d;
+    const T *v = (const T *)a.v + (p.k0 + j) * a.v_stride + (int64_t)head * a.d;
+    const T *q = (const T *)a.q + (p.q0 + query) * a.q_stride + (int64_t)h * a.d, *g = (const T *)a.g + at_row * a.d;
+    const T *out = (const T *)a.out_in + at_row * a.d;
+    float slope_of;
+    const float z = plain_score(a, p, wave_dot(q, k, a.d, lane), query, h, j, slope_of);
+    weight = recd_exp2(z - a.lse_in[at_row] * kRecdLog2e);
+    ds = weight * (wave_dot(g, v, a.d, lane) - wave_dot(g, out, a.d, lane)) * slope_of;
+}
+
+// Row `row` of the gradients by queries.
+template <typename T> __device__ void grad_q_again(const Args &a, const Problem &p, int head, int row, int lane)
+{
+    const int query = p.query(row, a.group), h = head * a.group + row - query * a.group, lim = p.limit(row, a.group);
+    float o[2] = {0.0f, 0.0f}, weight, ds;
+    for (int j = 0; j < lim; j++) {
+        pair_again<T>(a, p, head, row, j, lane, weight, ds);
+        for (int i = 0; i < 2; i++)
+            if (lane + 64 * i < a.d)
+                o[i] += ds * (float)((const T *)a.k + (p.k0 + j) * a.k_stride + (int64_t)head * a.d)[lane + 64 * i];
+    }
+    for (int i = 0; i < 2; i++)
+        if (lane + 64 * i < a.d)
+            ((T *)a.gq + (p.q0 + query) * a.gq_stride + (int64_t)h * a.d)[lane + 64 * i] = (T)(o[i] * a.scale);
+}
+
+// Key j of the gradients by keys and values.
+template <typename T> __device__ void grad_kv_again(const Args &a, const Problem &p, int head, int j, int lane)
+{
+    float dk[2] = {0.0f, 0.0f}, dv[2] = {0.0f, 0.0f}, weight, ds;
+    for (int row = 0; row < p.rows; row++) {
+        if (p.limit(row, a.group) <= j)
+            continue;
+        pair_again<T>(a, p, head, row, j, lane, weight, ds);
+        const int query = p.query(row, a.group), h = head * a.group + row - query * a.group;
+        for (int i = 0; i < 2; i++) {
+            const int e = lane + 64 * i;
+            if (e < a.d) {
+                dk[i] += ds * (float)((const T *)a.q + (p.q0 + query) * a.q_stride + (int64_t)h * a.d)[e];
+                dv[i] += weight * (float)((const T *)a.g + ((p.q0 + query) * (a.G * a.group) + h) * a.d)[e];
+            }
+        }
+    }
+    for (int i = 0; i < 2; i++) {
+        const int e = lane + 64 * i;
+        if (e < a.d) {
+            ((T *)a.gk + (p.k0 + j) * a.gk_stride + (int64_t)head * a.d)[e] = (T)(dk[i] * a.scale);
+            ((T *)a.gv + (p.k0 + j) * a.gv_stride + (int64_t)head * a.d)[e] = (T)dv[i];
+        }
+    }
+}
+
 // Waves that a SIMD is to hold at once, as far as the registers go round: two hide each other's waits and fill the
 // matrix cores and the vector units in turn.
 template <typename T, int DP, int KEPT> constexpr int kResident = (sizeof(T) == 4 && DP > 32) || (KEPT == 1 && DP > 64) ? 1 : 2;
@@ -401,20 +539,25 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
             }
         }
     }
-    if (!there || phase)
+    if (phase)
         return;
-    if (a.splits > 1) {
-        const int64_t at = split * a.part_rows + at_row;
-        if (lane < 32) {
-            a.part_m[at] = m;
-            a.part_l[at] = l;
+    uint32_t again = not_finite<DT>(o, there);
+    if (there && !(again >> (lane & 31) & 1)) {
+        if (a.splits > 1) {
+            const int64_t at = split * a.part_rows + at_row;
+            if (lane < 32) {
+                a.part_m[at] = m;
+                a.part_l[at] = l;
+            }
+            store_columns<float, DT>(a.part_o + at * a.d, o, 1.0f, a.d, lane);
+        } else {
+            if (a.lse && lane < 32)
+                a.lse[at_row] = (m + log2f(l)) * kRecdLn2;  // -inf where l = 0
+            store_columns<T, DT>((T *)a.out + at_row * a.d, o, l == 0.0f ? 0.0f : 1.0f / l, a.d, lane);
         }
-        store_columns<float, DT>(a.part_o + at * a.d, o, 1.0f, a.d, lane);
-        return;
     }
-    if (a.lse && lane < 32)
-        a.lse[at_row] = (m + log2f(l)) * kRecdLn2;  // -inf where l = 0
-    store_columns<T, DT>((T *)a.out + at_row * a.d, o, l == 0.0f ? 0.0f : 1.0f / l, a.d, lane);
+    for (; again; again &= again - 1)
+        attend_again<T>(a, p, head, row0 + __ffs(again) - 1, split * PHASES * each * 32, (split + 1) * PHASES * each * 32, split, lane);
 }
 
 // The forward kernel for lists of few rows: a wave to itself goes through one head after the other, whose rows are on
@@ -473,9 +616,11 @@ template <typename T, int DP, bool CAP> __global__ __launch_bounds__(64, (sizeof
         for (int d = 0; d < DT; d++)
             o[d] = recd_f32x16{};
     };
+    uint32_t again = 0;  // the rows of any head
     auto write = [&]() {
         const float sum = l + __shfl_xor(l, 32);
         const int64_t at_row = q_row * H + head * a.group + head_in;
+        again |= not_finite<DT>(o, there);
         if (!there)
             return;
         if (a.splits > 1) {
@@ -579,6 +724,13 @@ template <typename T, int DP, bool CAP> __global__ __launch_bounds__(64, (sizeof
         }
     }
     write();
+    if (!again)
+        return;
+    __threadfence_block();  // the rows' first sums are written
+    find_tile(a, p, head, head_end, tile, split);
+    for (; head < head_end; head++)
+        for (uint32_t rows = again; rows; rows &= rows - 1)
+            attend_again<T>(a, p, head, row0 + __ffs(rows) - 1, split * each * 32, (split + 1) * each * 32, split, lane);
 }
 
 // Joins the splits of the forward pass: 2^dlog threads a row, four elements each.
@@ -714,7 +866,7 @@ __global__ __launch_bounds__(1024) void k_attention_tiles_by_work(int lists, boo
         side.tiles[s] = make_int2(-1, 0);
 }
 
-// fp16: the largest |g| and |v| (as bits, whose order is the numbers'), and from them the power of two for ds.
+// fp16: the largest finite |g| and |v| (as bits, whose order is the numbers'), and from them the power of two for ds.
 __global__ void k_attention_clear(uint32_t *tops)
 {
     if (threadIdx.x < 2)
@@ -730,7 +882,7 @@ __global__ __launch_bounds__(256) void k_attention_tops(int64_t rows, int width,
         float v[8];
         recd_load16(x + i / pieces * stride + i % pieces * 8, v);
         for (int e = 0; e < 8; e++)
-            t = fmaxf(t, fabsf(v[e]));
+            t = fmaxf(t, fabsf(v[e]) < INFINITY ? fabsf(v[e]) : 0.0f);
     }
     for (int o = 32; o; o >>= 1)
         t = fmaxf(t, __shfl_xor(t, o));
@@ -884,9 +1036,14 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
         static_assert(sizeof(lds) >= 64 * 16 * DT * sizeof(float));
         join_sums<DT, PHASES>(o, reinterpret_cast<float *>(&lds), 0, phase, lane);
     }
-    if (there && phase == 0)
+    if (phase)
+        return;
+    uint32_t again = not_finite<DT>(o, there);
+    if (there && !(again >> (lane & 31) & 1))
         store_columns<T, DT>((T *)a.gq + q_row * a.gq_stride + (int64_t)h * a.d, o, (CAP ? 4.0f : 1.0f) * a.scale / lift, a.d,
                              lane);
+    for (; again; again &= again - 1)
+        grad_q_again<T>(a, p, head, row0 + __ffs(again) - 1, lane);
 }
 
 // Keys stay, queries and their gradients stream past.  What a score needs of its row stands in LDS in the order of
@@ -1079,11 +1236,16 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
         join_sums<DT, PHASES>(dk, reinterpret_cast<float *>(&lds), kept, phase, lane);
         join_sums<DT, PHASES>(dv, reinterpret_cast<float *>(&lds), kept, phase, lane);
     }
-    if (!there || phase)
+    if (phase)
         return;
-    store_columns<T, DT>((T *)a.gk + (p.k0 + j) * a.gk_stride + (int64_t)head * a.d, dk, (CAP ? 4.0f : 1.0f) * a.scale / lift, a.d,
-                         lane);
-    store_columns<T, DT>((T *)a.gv + (p.k0 + j) * a.gv_stride + (int64_t)head * a.d, dv, recd_exp2(-kLiftP<T>), a.d, lane);
+    uint32_t again = not_finite<DT>(dk, there) | not_finite<DT>(dv, there);
+    if (there && !(again >> (lane & 31) & 1)) {
+        store_columns<T, DT>((T *)a.gk + (p.k0 + j) * a.gk_stride + (int64_t)head * a.d, dk, (CAP ? 4.0f : 1.0f) * a.scale / lift,
+                             a.d, lane);
+        store_columns<T, DT>((T *)a.gv + (p.k0 + j) * a.gv_stride + (int64_t)head * a.d, dv, recd_exp2(-kLiftP<T>), a.d, lane);
+    }
+    for (; again; again &= again - 1)
+        grad_kv_again<T>(a, p, head, j0 + __ffs(again) - 1, lane);
 }
 
 // Offsets that do not rise from 0 to the number of rows, or pass the caller's bound of a list's length.

@@ -192,6 +192,48 @@ def test_lists_do_not_touch_each_other(ctx):
         assert torch.equal(got[n][rows], want[n][rows]), n
 
 
+# lists of few rows (a wave to a tile); of single rows whose keys are divided; of tiles in phases; of whole groups
+PLANTED = {"short": ([20, 45, 7], [20, 45, 7], 2, 2), "single": ([1, 3, 1], [700, 900, 300], 4, 2),
+           "phases": ([150, 260, 40], [150, 260, 40], 2, 1), "groups": ([260] * 40, [260] * 40, 8, 4)}
+
+
+@pytest.mark.parametrize("dt", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("name", list(PLANTED))
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("softcap", [0.0, 5.0])
+def test_what_is_masked_may_hold_anything(ctx, dt, name, bad, softcap):
+    """A key and a value that are not finite reach the rows that see them alone; so do a query and its gradient."""
+    lq, lk, H, G = PLANTED[name]
+    d = 128 if name == "groups" else 40
+    qo, ko = offsets(lq), offsets(lk)
+    Q, K = int(qo[-1]), int(ko[-1])
+    q, k, v, g = du.rand((Q, H, d), dt, 1), du.rand((K, G, d), dt, 2), du.rand((K, G, d), dt, 3), du.rand((Q, H, d), dt, 4)
+    how = dict(scale=d ** -0.5, causal=True, softcap=softcap)
+    ref = du.attention_ref(q, k, v, qo, ko, g=g, **how)
+    j = lk[1] - 2 if lq[1] < 5 else lk[1] // 2 + 3  # of the second list
+    i = j - (lk[1] - lq[1])                          # the first query that sees it
+    k1, v1 = k.clone(), v.clone()
+    k1[int(ko[1]) + j, :, ::3] = bad
+    v1[int(ko[1]) + j, :, 1::2] = bad
+    got = run(ctx, q, k1, v1, qo, ko, how, g)
+    rows = torch.ones(Q, dtype=torch.bool)
+    rows[int(qo[1]) + i:int(qo[2])] = False
+    for n in ("out", "grad_q"):
+        du.within(got[n][rows.cuda()], ref[n][0][rows], ref[n][1][rows], what=n + " beside keys")
+    du.within(got["lse"].cpu()[rows], ref["lse"][0][rows], ref["lse"][1][rows], what="lse beside keys")
+    assert not got["out"][int(qo[1]) + i:int(qo[2]), :, 1::2].isfinite().any()
+    q1, g1 = q.clone(), g.clone()
+    q1[int(qo[1]) + i, :, ::3] = bad
+    g1[int(qo[1]) + i, :, 1::2] = bad
+    got = run(ctx, q1, k, v, qo, ko, how, g1)
+    rows = torch.arange(Q) != int(qo[1]) + i
+    keys = torch.ones(K, dtype=torch.bool)
+    keys[int(ko[1]):int(ko[1]) + j + 1] = False
+    for n, there in (("out", rows), ("grad_q", rows), ("grad_k", keys), ("grad_v", keys)):
+        du.within(got[n][there.cuda()], ref[n][0][there], ref[n][1][there], what=n + " beside a query")
+    assert not got["grad_v"][int(ko[1]):int(ko[1]) + j + 1, :, 1::2].isfinite().any()
+
+
 def test_same_bits_again(ctx):
     lens = [300, 5, 0, 77, 129]
     a = check(ctx, lens, lens, 4, 2, 64, "bf16", dict(causal=True, softcap=4.0))
