@@ -597,19 +597,21 @@ recd_status recd_layer_norm_backward(recd_ctx *ctx, int64_t n, int D, recd_dtype
 /* 29. Softmax cross entropy of rows x [n, D] against the V rows of a table as the vocabulary; the logits
  *     z[i, v] = scale * <x_i, table_v> are never stored (scale: not 0).  D at most RECD_MAX_DENSE_D; V and n below 2^31.
  *     targets: device int64 [n], a row of the table each; a negative one marks a row without a target (loss 0, no
- *     gradients).  So does one of V and more, unless RECD_OPT_VALIDATE is set (RECD_EBOUNDS).
+ *     gradients, and its elements and its grad_loss reach no other row's and not the table's).  So does one of V and
+ *     more, unless RECD_OPT_VALIDATE is set (RECD_EBOUNDS).
  *     loss: device fp32 [n], lse[i] - z[i, targets[i]].   lse: device fp32 [n], log(sum over v of exp(z[i, v])).
  *     mean_row: device fp32 [n, D] or NULL; receives sum over v of exp(z[i, v] - lse[i]) * table_v, from which call 30
  *     has the gradient by x without a second pass over the table.
- *     Workspace: the splits' maxima and sums, and with mean_row their means: less than 4 * (D + 2) * 4 bytes a row
- *     and compute unit. */
+ *     Workspace: the splits' maxima and sums, and with mean_row their means: splits * n * (D + 2) * 4 bytes, where splits
+ *     times row blocks (of 32 to 256 rows) are at most 16 to a compute unit. */
 recd_status recd_vocab_loss(recd_ctx *ctx, int64_t n, int64_t V, int D, recd_dtype dtype, const void *x, const void *table,
                             const int64_t *targets, float scale, float *loss, float *lse, float *mean_row);
 
 /* 30. Gradients of call 29 for grad_loss (device fp32 [n]: the weight of every row's loss).
  *     lse, mean_row: from call 29 on the same inputs (mean_row is read for grad_x only).
  *     grad_x: device [n, D] of dtype, or NULL.   grad_table: device [V, D] of dtype, overwritten (every row), or NULL.
- *     Workspace: 12 bytes a row. */
+ *     Workspace: 12 bytes a row, and where few groups of table rows (R = 128 or 256) are shared between blocks their parts:
+ *     8 * R * D bytes for every block that the card holds at a time. */
 recd_status recd_vocab_loss_backward(recd_ctx *ctx, int64_t n, int64_t V, int D, recd_dtype dtype, const void *x,
                                      const void *table, const int64_t *targets, float scale, const float *lse,
                                      const float *mean_row, const float *grad_loss, void *grad_x, void *grad_table);
@@ -620,6 +622,7 @@ recd_status recd_vocab_loss_backward(recd_ctx *ctx, int64_t n, int64_t V, int D,
  *       then, with slopes: z_ij -= slopes[head] * |pos_i - j|
  *       visible keys: all of the list's; causal: j <= pos_i, or j < prefix[l] where prefix is given
  *       out_i = sum over the visible j of softmax(z_i)_j v_j;  a row that sees no key gives 0 (and lse = -inf)
+ *     What a row does not see does not reach it, be it infinite or NaN (nor its gradients; such tiles take a slow way).
  *     Heads: query head h reads key head h / (heads / kv_heads).  One query row per list is the form for serving a new
  *     token; keys are split over blocks where there are few tiles. */
 typedef struct recd_attention {
@@ -638,15 +641,16 @@ typedef struct recd_attention {
 
 /*     q [q_rows, heads, head_dim], k and v [k_rows, kv_heads, head_dim]: device, rows apart by their strides.
  *     out: device [q_rows, heads, head_dim], dense.   lse: device fp32 [q_rows, heads] for call 32, or NULL.
- *     Workspace: 8 bytes for every list and every 32 query rows of a key head, and where keys are split the splits'
- *     partial rows in fp32.  RECD_OPT_VALIDATE checks the offsets and bounds. */
+ *     Workspace: 8 bytes for every list and every 32 query rows of a key head, and where keys are split
+ *     splits * q_rows * heads * (head_dim + 2) * 4 bytes (there are few query rows then, and at least 512 keys to a split).  RECD_OPT_VALIDATE checks the offsets and bounds. */
 recd_status recd_list_attention(recd_ctx *ctx, const recd_attention *a, const void *q, const void *k, const void *v, void *out,
                                 float *lse);
 
 /* 32. Gradients of call 31 (none by slopes).  out, lse: from call 31.  grad_out: device, dense as out.
  *     grad_q, grad_k, grad_v: device, rows apart by their own strides (elements), every row overwritten; key heads
  *     add up their query heads in fp32.
- *     Workspace: 4 bytes a query row and head, and 16 bytes for every list and 32 rows. */
+ *     Workspace: 4 bytes a query row and head, and 8 bytes for every list and every 32 query rows of a key head, and again
+ *     for every list and 32 key rows. */
 recd_status recd_list_attention_backward(recd_ctx *ctx, const recd_attention *a, const void *q, const void *k, const void *v,
                                          const void *out, const float *lse, const void *grad_out, void *grad_q, void *grad_k,
                                          void *grad_v, int64_t grad_q_stride, int64_t grad_k_stride, int64_t grad_v_stride);

@@ -33,6 +33,7 @@ template <typename T> constexpr bool kHalf = std::is_same<T, _Float16>::value;
 template <typename T> constexpr float kLift = kHalf<T> ? 7.0f : 0.0f;
 template <typename T> constexpr float kLiftP = kHalf<T> ? 15.0f : 0.0f;
 
+constexpr int kMostSplits = 1024;  // parts of a tile's keys
 constexpr int kMostSorted = 1024;  // lists whose tiles are put in the order of their work
 
 struct Args {
@@ -733,7 +734,7 @@ template <typename T, int DP, bool CAP> __global__ __launch_bounds__(64, (sizeof
             attend_again<T>(a, p, head, row0 + __ffs(rows) - 1, split * each * 32, (split + 1) * each * 32, split, lane);
 }
 
-// Joins the splits of the forward pass: 2^dlog threads a row, four elements each.
+// Joins the splits of the forward pass where they are few: 2^dlog threads a row, four elements each.
 template <typename T>
 __global__ __launch_bounds__(256) void k_attention_join(int64_t rows, int d, int dlog, int splits,
                                                         const float *__restrict__ part_m, const float *__restrict__ part_l,
@@ -759,6 +760,73 @@ __global__ __launch_bounds__(256) void k_attention_join(int64_t rows, int d, int
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
     store4<T>(out + row * d + col, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
     if (lse && col == 0)
+        lse[row] = (m + log2f(l)) * kRecdLn2;
+}
+
+// The same for many splits: a block a row, the splits dealt to its threads (one thread to a split for the
+// weights, 2^dlog threads with four elements each for the sums), so that no chain of loads is as long as the splits are
+// many.  A whole call with it and with the other, one query of 8 heads of 64 fp16 against 30 000 keys (58 splits) 14 and 30 us,
+// against 200 000 (256 splits) 29 and 113.
+template <typename T>
+__global__ __launch_bounds__(256) void k_attention_join_many(int64_t rows, int d, int dlog, int splits,
+                                                             const float *__restrict__ part_m, const float *__restrict__ part_l,
+                                                             const float *__restrict__ part_o, T *out, float *lse)
+{
+    __shared__ float f[kMostSplits], wave_m[4], wave_l[4];
+    __shared__ recd_f32x4 sums[256];
+    const int tid = threadIdx.x, wave = tid >> 6;
+    const int64_t row = blockIdx.x;
+    float m = -INFINITY;
+    for (int s = tid; s < splits; s += 256) {
+        f[s] = part_m[s * rows + row];
+        m = fmaxf(m, f[s]);
+    }
+    for (int o = 32; o; o >>= 1)
+        m = fmaxf(m, __shfl_xor(m, o));
+    if ((tid & 63) == 0)
+        wave_m[wave] = m;
+    __syncthreads();
+    m = fmaxf(fmaxf(wave_m[0], wave_m[1]), fmaxf(wave_m[2], wave_m[3]));
+    const float from = m == -INFINITY ? 0.0f : m;
+    float l = 0.0f;
+    for (int s = tid; s < splits; s += 256) {
+        f[s] = recd_exp2(f[s] - from);
+        l += f[s] * part_l[s * rows + row];
+    }
+    for (int o = 32; o; o >>= 1)
+        l += __shfl_xor(l, o);
+    if ((tid & 63) == 0)
+        wave_l[wave] = l;
+    __syncthreads();
+    l = wave_l[0] + wave_l[1] + wave_l[2] + wave_l[3];
+    const int col = (tid & ((1 << dlog) - 1)) * 4, lot = tid >> dlog, lots = 256 >> dlog;
+    recd_f32x4 o = {};
+    if (col < d)
+        for (int s0 = lot; s0 < splits; s0 += 4 * lots) {
+            recd_f32x4 x[4];
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                const int s = s0 + i * lots < splits ? s0 + i * lots : s0;
+                x[i] = *reinterpret_cast<const recd_f32x4 *>(part_o + (s * rows + row) * d + col);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; i++)
+                if (s0 + i * lots < splits)
+#pragma unroll
+                    for (int e = 0; e < 4; e++)
+                        o[e] += f[s0 + i * lots] * x[i][e];
+        }
+    sums[tid] = o;
+    __syncthreads();
+    if (lot || col >= d)
+        return;
+    for (int i = 1; i < lots; i++)
+#pragma unroll
+        for (int e = 0; e < 4; e++)
+            o[e] += sums[(i << dlog) + tid][e];
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    store4<T>(out + row * d + col, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
+    if (lse && tid == 0)
         lse[row] = (m + log2f(l)) * kRecdLn2;
 }
 
@@ -1509,11 +1577,15 @@ recd_status recd_list_attention(recd_ctx *ctx, const recd_attention *d, const vo
     a.slots = t.slots;
     a.tiles_per_list = t.tiles_per_list;
     a.heads = heads_at_once(ctx, t, a.G, d->lists);
-    // few tiles: a tile's keys are split over blocks, at least 256 keys each
+    // Few tiles: a tile's keys are split over blocks, at least 512 keys each (one query against 30 000 keys 14 us, with 256
+    // 14, with 1024 17; 8 against 16 384 each 20.7, 22.3, 20.5), until two blocks a compute unit are at work (37 queries
+    // against up to 16 384 keys 43 us, with one 46, with four 46); tiles of one wave eight.
     const int64_t blocks = (int64_t)ctx->num_cu * (t.division == ONE_WAVE ? 8 : 2), have = t.slots * a.G > 0 ? t.slots * a.G : 1;
     int64_t splits = (blocks + have - 1) / have;
-    if (splits > d->max_k / 256)
-        splits = d->max_k / 256;
+    if (splits > d->max_k / 512)
+        splits = d->max_k / 512;
+    if (splits > kMostSplits)
+        splits = kMostSplits;
     a.splits = (int)(splits < 1 ? 1 : splits);
     if (a.slots * a.splits / 8 + 1 > ((int64_t)1 << 27) / a.G)
         return recd_fail(ctx, RECD_EINVAL, "too many tiles");
@@ -1540,8 +1612,12 @@ recd_status recd_list_attention(recd_ctx *ctx, const recd_attention *d, const vo
         launch<T>(FORWARD, a, t.division, ctx->stream);
         if (a.splits > 1) {
             const int dlog = log2_of(a.d / 4);
-            hipLaunchKernelGGL((k_attention_join<T>), dim3((unsigned)(((a.part_rows << dlog) + 255) / 256)), dim3(256), 0,
-                               ctx->stream, a.part_rows, a.d, dlog, a.splits, a.part_m, a.part_l, a.part_o, (T *)out, lse);
+            if (a.splits > 8)
+                hipLaunchKernelGGL((k_attention_join_many<T>), dim3((unsigned)a.part_rows), dim3(256), 0, ctx->stream, a.part_rows,
+                                   a.d, dlog, a.splits, a.part_m, a.part_l, a.part_o, (T *)out, lse);
+            else
+                hipLaunchKernelGGL((k_attention_join<T>), dim3((unsigned)(((a.part_rows << dlog) + 255) / 256)), dim3(256), 0,
+                                   ctx->stream, a.part_rows, a.d, dlog, a.splits, a.part_m, a.part_l, a.part_o, (T *)out, lse);
         }
     });
     RECD_HIP(ctx, hipGetLastError());

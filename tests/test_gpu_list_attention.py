@@ -192,6 +192,13 @@ def test_lists_do_not_touch_each_other(ctx):
         assert torch.equal(got[n][rows], want[n][rows]), n
 
 
+@pytest.mark.parametrize("dt", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("H,G,d", [(1, 1, 128), (4, 1, 24), (6, 3, 64)])
+def test_many_splits(ctx, dt, H, G, d):
+    """Single tokens whose keys are cut into more splits than a thread group goes through, an empty list and a short one."""
+    check(ctx, [1, 1, 1, 0, 1], [9000, 0, 700, 5, 3], H, G, d, dt, dict(causal=True, softcap=3.0, slopes=SLOPES(H) / 64), train=False)
+
+
 # lists of few rows (a wave to a tile); of single rows whose keys are divided; of tiles in phases; of whole groups
 PLANTED = {"short": ([20, 45, 7], [20, 45, 7], 2, 2), "single": ([1, 3, 1], [700, 900, 300], 4, 2),
            "phases": ([150, 260, 40], [150, 260, 40], 2, 1), "groups": ([260] * 40, [260] * 40, 8, 4)}
