@@ -589,7 +589,7 @@ recd_status recd_layer_norm(recd_ctx *ctx, int64_t n, int D, recd_dtype dtype, c
 
 /* 28. Gradients of call 27.  grad_y, grad_x: device [n, D] of dtype (grad_x may be grad_y).
  *     grad_weight, grad_bias: device fp32 [D], overwritten with the sums over all rows; either or both may be NULL.
- *     Workspace: up to 64 * D bytes for every compute unit. */
+ *     Workspace: up to 32 * D bytes for every compute unit. */
 recd_status recd_layer_norm_backward(recd_ctx *ctx, int64_t n, int D, recd_dtype dtype, const void *x, const float *weight,
                                      const float *stats, const void *grad_y, void *grad_x, float *grad_weight,
                                      float *grad_bias);

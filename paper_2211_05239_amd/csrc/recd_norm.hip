@@ -4,8 +4,8 @@
 //   with u = g * w:  gx = rstd * (u - mean(u) - h * mean(u * h)),  gw = sum over rows of g * h,  gb = sum of g
 //
 // Both directions are bound by HBM traffic: the forward pass reads a row and writes one, the backward pass reads
-// two and writes one.  300 007 x 128 bf16: 34 us forward (154 MB, 4.5 TB/s), 56 us backward (230 MB, 4.1 TB/s; a large copy
-// reaches 4.7), and 6 us for the sums of the weight's and the bias's gradients.  A row lives in the registers of 2^glog lanes, `P` pieces of 16 bytes in each, from its only
+// two and writes one.  300 007 x 128 bf16: 33 us forward (154 MB, 4.7 TB/s, what a large copy reaches), 49 us backward (230 MB,
+// 4.7 TB/s), and 5 us for the sums of the weight's and the bias's gradients.  A row lives in the registers of 2^glog lanes, `P` pieces of 16 bytes in each, from its only
 // read to its write: the variance is taken about the mean from the registers, in 32 bits, not from a sum of squares.
 // The weight and the bias of a lane's columns stay in its registers over all rows that the lane group takes.
 // The sums over the rows: every lane adds up its columns over its group's rows, a block adds up its groups (lane
@@ -184,7 +184,7 @@ __global__ __launch_bounds__(1024) void k_sum_parts(int blocks, int D, const flo
 
 // Lanes and pieces of a row: as few idle lanes as possible, and of equal ones the fewest pieces a lane. With two pieces a lane
 // where one would do, forward and backward of 300 007 rows of 64 bf16 take 63 us against 48, of 128 elements 101 against 92;
-// with four, 134 and 164.
+// with four, 134 and 164 (at eight blocks a compute unit).
 struct Shape {
     int P, glog;
 };
@@ -220,11 +220,12 @@ recd_status check_norm(recd_ctx *ctx, int64_t n, int D, recd_dtype dt)
     return RECD_OK;
 }
 
-// Blocks of a launch: eight a CU keep every wave slot of a row in flight, and their lanes read the weight once.
+// Blocks of a launch: four a compute unit, whose lanes read the weight once.  Forward and backward of 300 007 x 128 bf16 with
+// two, four, eight and sixteen: 115, 88, 97 and 109 us; 50 021 x 516 fp32 132, 101, 110 and 117; forward alone 45, 33, 34.
 int64_t norm_blocks(const recd_ctx *ctx, int64_t n, int glog)
 {
     const int64_t need = (n + (kBlock >> glog) - 1) / (kBlock >> glog);
-    const int64_t most = (int64_t)ctx->num_cu * 8;
+    const int64_t most = (int64_t)ctx->num_cu * 4;
     return need < most ? need : most;
 }
 
