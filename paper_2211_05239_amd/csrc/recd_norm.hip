@@ -4,9 +4,10 @@
 //   with u = g * w:  gx = rstd * (u - mean(u) - h * mean(u * h)),  gw = sum over rows of g * h,  gb = sum of g
 //
 // Both directions are bound by HBM traffic: the forward pass reads a row and writes one, the backward pass reads
-// two and writes one.  300 007 x 128 bf16: 33 us forward (154 MB, 4.7 TB/s, what a large copy reaches), 49 us backward (230 MB,
-// 4.7 TB/s), and 5 us for the sums of the weight's and the bias's gradients.  A row lives in the registers of 2^glog lanes, `P` pieces of 16 bytes in each, from its only
-// read to its write: the variance is taken about the mean from the registers, in 32 bits, not from a sum of squares.
+// two and writes one.  300 007 x 128 bf16: 33 us forward (154 MB, 4.7 TB/s, what a large copy reaches), 42 us backward (230 MB,
+// 5.5 TB/s, part of it from the caches), and 5 us for the sums of the weight's and the bias's gradients.
+// A row lives in the registers of 2^glog lanes, `P` pieces of 16 bytes in each, from its only read to its write: the variance is
+// taken about the mean from the registers, in 32 bits, not from a sum of squares.
 // The weight and the bias of a lane's columns stay in its registers over all rows that the lane group takes.
 // The sums over the rows: every lane adds up its columns over its group's rows, a block adds up its groups (lane
 // exchanges, then LDS), and a second launch adds up the blocks' rows of partial sums in their order, so the

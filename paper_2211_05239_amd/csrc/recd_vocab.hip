@@ -9,7 +9,12 @@
 // along, as a second product with the scores' exponentials, so that the gradient by x is one subtraction later and
 // the backward pass needs one recomputation of the scores instead of two: 8 n V D operations for both passes, where
 // 6 are needed at least.  The backward pass turns the sides round: table rows stay in registers, and the rows x
-// stream past them.  Both passes are bound by the matrix cores and the exponentials beside them.
+// stream past them.
+//
+// Both passes are bound by the matrix cores and the exponentials beside them.  4096 rows against 1 M x 128 bf16, 4 nVD
+// operations a pass: 1.82 ms forward with the mean row (1.15 PFLOP/s) and 2.0 ms for the table's gradient (1.05), at the
+// 1.9 GHz that the card's power leaves them, the matrix cores busy 55 % of the cycles; a large product reaches 1.38 PFLOP/s.
+// 1500 rows against 100 000 x 64 fp32: 334 and 348 us, 115 and 110 TFLOP/s of the 153 of a large product.
 //
 // The vocabulary is cut into splits where there are few rows; their (maximum, sum, mean) are joined in the order of the
 // splits.  Exponentials are rounded to the tables' type for the second product, as the other operand of the matrix
@@ -29,7 +34,9 @@ constexpr float kSlack = 8.0f;
 // fp16 exponentials are held 2^7 times larger: at most 2^15 with the slack, and exact to 2^-31 of the maximum.
 template <typename T> constexpr float kLift = std::is_same<T, _Float16>::value ? 7.0f : 0.0f;
 
-// Tiles of 32 kept rows in a wave, and waves in a block.
+// Tiles of 32 kept rows in a wave, and waves in a block.  Many rows: one tile, since the sums of two take the registers that let
+// two waves of a SIMD hide each other's waits, and as many waves as share what they stream; the wide and the fp32 kernels have
+// room for four.  Few rows: two tiles a wave, so that a table row that is read feeds both.
 template <typename T, int DP> constexpr int kTiles = 1;
 template <typename T, int DP> constexpr int kManyWaves = sizeof(T) == 4 || DP > 192 ? 4 : 8;
 template <typename T, int DP> constexpr int kFewTiles = sizeof(T) == 4 || DP > 128 ? 1 : 2;
@@ -49,7 +56,9 @@ struct ForwardArgs {
 };
 
 // Few rows: the block's waves hold the same 32 * N rows and each streams table rows of its own, 32 at a time through LDS
-// of its own, so that nobody waits for anybody.  Their sums are joined at the end.
+// of its own, so that nobody waits for anybody.  Their sums are joined at the end.  37 rows against 100 000 x 64 fp32 take 15 us
+// (25.6 MB, 1.7 TB/s), 32 against 300 000 x 128 bf16 33 (77 MB, 2.3 TB/s): bound by the chain of load, product and exponentials
+// of the few tiles that each wave has.
 template <typename T, int DP, int N, bool MEAN> __global__ __launch_bounds__(kBlock) void k_vocab_forward_few(ForwardArgs a)
 {
     constexpr int KS = DP / 16, DT = DP / 32;
@@ -899,7 +908,7 @@ template <typename T, int DP> void launch_forward(const ForwardArgs &a, bool sha
 // How the table's gradient is cut: blocks that are on the card at a time take equal shares of all (group of table rows,
 // tile of rows x) where the last round of whole groups would leave more of the card idle than it costs to write the
 // shared groups' parts and add them up (16 bytes an element, at about 4.5 TB/s; the sums run at about 0.9 PFLOP/s, 0.1 in
-// fp32), else one block a group.
+// fp32), else one block a group.  100 000 x 64 fp32, 1500 rows: 397 us against 447 (782 groups, 512 blocks at a time).
 struct TableShape {
     int R;             // table rows of a group
     int64_t each, units;
