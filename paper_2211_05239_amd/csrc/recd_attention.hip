@@ -27,8 +27,9 @@
 // What is rounded to 16 bits for them, beside the operands: the exponentials (as the second product's operand must be) and ds,
 // both with an error of half a unit in their last place, which sums average; and delta = g . o takes the output as it was
 // stored.  Gradients by queries and keys so lie 2.8e-3 (bf16, relative in the 2-norm) from the exact ones where the rounding of the
-// result alone is 1.7e-3.  delta from unrounded sums would take two products more in the gradients by queries (24 % on the whole
-// backward pass of long lists), and ds in two roundings as many again in both: neither is taken.  fp32 rounds nothing.
+// result alone is 1.7e-3.  delta from unrounded sums would take two products more in the gradients by queries (by their count
+// about a quarter of the backward pass of long lists), and ds in two roundings as many again in both: neither is taken.  fp32
+// rounds nothing.
 //
 // Tiles of lists are found without a scan: the tiles of list l take the slots from floor(rows before l / R) + l on,
 // which never overlap as ceil(n / R) <= floor((before + n) / R) - floor(before / R) + 1.
