@@ -222,7 +222,8 @@ template <typename T, int DT> __device__ inline void store_columns(T *row, const
 // What is masked enters the products with weight 0, which is not enough where it is an infinity or a NaN: 0 * NaN is a NaN,
 // in rows of the tile that do not see it.  Sums that are not finite are therefore thrown away and their rows done again,
 // one at a time by the whole wave and over what they see alone.  The check costs an addition a sum at the kernel's end;
-// the way of one row, which only such data takes, is plain.
+// the way of one row, which only such data takes, is plain.  Rows whose own scores hold a NaN (all of a model that has come
+// apart) are NaN throughout and are left as they are.
 //
 // The rows (lanes of the tile's sums) that are to be done again, a bit each.
 template <int DT> __device__ inline uint32_t not_finite(const recd_f32x16 (&o)[DT], bool there)
@@ -556,7 +557,7 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
     }
     if (phase)
         return;
-    uint32_t again = not_finite<DT>(o, there);
+    uint32_t again = not_finite<DT>(o, there && l == l);
     if (there && !(again >> (lane & 31) & 1)) {
         if (a.splits > 1) {
             const int64_t at = split * a.part_rows + at_row;
@@ -635,7 +636,7 @@ template <typename T, int DP, bool CAP> __global__ __launch_bounds__(64, (sizeof
     auto write = [&]() {
         const float sum = l + __shfl_xor(l, 32);
         const int64_t at_row = q_row * H + head * a.group + head_in;
-        again |= not_finite<DT>(o, there);
+        again |= not_finite<DT>(o, there && sum == sum);
         if (!there)
             return;
         if (a.splits > 1) {
@@ -1121,7 +1122,7 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
     }
     if (phase)
         return;
-    uint32_t again = not_finite<DT>(o, there);
+    uint32_t again = not_finite<DT>(o, there && (lim == 0 || (from == from && delta == delta)));
     if (there && !(again >> (lane & 31) & 1))
         store_columns<T, DT>((T *)a.gq + q_row * a.gq_stride + (int64_t)h * a.d, o, (CAP ? 4.0f : 1.0f) * a.scale / lift, a.d,
                              lane);
@@ -1322,6 +1323,11 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
     if (phase)
         return;
     uint32_t again = not_finite<DT>(dk, there) | not_finite<DT>(dv, there);
+    if (again) {  // the last row sees every key
+        const int64_t last = (p.q0 + p.nq - 1) * H + head * a.group;
+        const float lse = a.lse_in[last], delta = a.delta[last];
+        again = lse == lse && delta == delta ? again : 0;
+    }
     if (there && !(again >> (lane & 31) & 1)) {
         store_columns<T, DT>((T *)a.gk + (p.k0 + j) * a.gk_stride + (int64_t)head * a.d, dk, (CAP ? 4.0f : 1.0f) * a.scale / lift,
                              a.d, lane);

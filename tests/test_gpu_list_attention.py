@@ -241,6 +241,30 @@ def test_what_is_masked_may_hold_anything(ctx, dt, name, bad, softcap):
     assert not got["grad_v"][int(ko[1]):int(ko[1]) + j + 1, :, 1::2].isfinite().any()
 
 
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("name", list(PLANTED))
+def test_all_of_it_nan(ctx, dt, name):
+    """Lists of NaN alone: NaN in every row, in time."""
+    lq, lk, H, G = PLANTED[name]
+    nan = torch.full((1, 1, 64), float("nan"), dtype=du.rand((1,), dt, 1).dtype)
+    q, k = nan.expand(sum(lq), H, 64).contiguous(), nan.expand(sum(lk), G, 64).contiguous()
+    got = run(ctx, q, k, k.clone(), offsets(lq), offsets(lk), dict(scale=0.1, causal=True), q.clone())
+    for n, t in got.items():
+        assert t.isnan().all(), n
+
+
+def test_rows_too_far_apart_are_refused(ctx):
+    """Rows of 16 MiB and more from one to the next: offsets inside a tile are held in 32 bits."""
+    from paper_2211_05239_amd import recd
+    q = torch.zeros(3, 1, 16, device="cuda")
+    o = torch.tensor([0, 3], device="cuda")
+    wide = torch.empty_strided((3, 1, 16), (1 << 22, 16, 1), device="cuda")
+    for a in ((wide, q, q), (q, wide, q), (q, q, wide)):
+        with pytest.raises(recd.RecdError):
+            ctx.list_attention(*a, o, o, 3, 3, torch.empty_like(q), scale=1.0)
+    ctx.list_attention(q, q, q, o, o, 3, 3, torch.empty_like(q), scale=1.0)
+
+
 def test_same_bits_again(ctx):
     lens = [300, 5, 0, 77, 129]
     a = check(ctx, lens, lens, 4, 2, 64, "bf16", dict(causal=True, softcap=4.0))
