@@ -29,8 +29,11 @@ namespace {
 
 constexpr int kBlock = 256, kWaves = 4;
 // A row's running maximum is moved only where a new one exceeds it by this many powers of two: the exponentials stay
-// far inside the range, and the sums are rarely rescaled.
-constexpr float kSlack = 8.0f;
+// far inside the range, and the sums are rarely rescaled.  With the mean row in 16 bits that is one power: a logit that has more
+// than two thirds of the row's weight then stands at least one above any earlier one, becomes the maximum, and its exponential
+// 1 is exact.  The gradient m - W_t of a row that is predicted well is made of the others' weights, and a rounding of
+// the target's would be as large as all of them (with a slack of 8, and 1 - p_t = 1 %, the gradient by the row was off by up to 20 %).
+template <typename T, bool MEAN> constexpr float kSlack = MEAN && sizeof(T) == 2 ? 1.0f : 8.0f;
 // fp16 exponentials are held 2^7 times larger: at most 2^15 with the slack, and exact to 2^-31 of the maximum.
 template <typename T> constexpr float kLift = std::is_same<T, _Float16>::value ? 7.0f : 0.0f;
 
@@ -142,7 +145,7 @@ template <typename T, int DP, int N, bool MEAN> __global__ __launch_bounds__(kBl
             for (int r = 1; r < 16; r++)
                 top = fmaxf(top, s[j][r]);
             top = fmaxf(top, __shfl_xor(top, 32)) * a.c - kLift<T>;
-            if (__any(top > m[j] + kSlack)) {
+            if (__any(top > m[j] + kSlack<T, MEAN>)) {
                 const float now = fmaxf(m[j], top);
                 const float f = now == m[j] ? 1.0f : recd_exp2(m[j] - now);
                 m[j] = now;
@@ -313,7 +316,7 @@ __global__ __launch_bounds__(64 * W) void k_vocab_forward(ForwardArgs a)
             for (int r = 1; r < 16; r++)
                 top[j] = fmaxf(top[j], x[j][r]);
             top[j] = fmaxf(top[j], __shfl_xor(top[j], 32)) * a.c - kLift<T>;
-            above |= top[j] > m[j] + kSlack;
+            above |= top[j] > m[j] + kSlack<T, MEAN>;
         }
         if (__any(above))
 #pragma unroll
@@ -577,9 +580,10 @@ struct TableGradArgs {
 // The block that does unit `u` of the work.
 __host__ __device__ inline int64_t block_of(int64_t u, int64_t units, int64_t blocks) { return ((u + 1) * blocks - 1) / units; }
 
-// 32 * N table rows a wave; the rows x stream past them, pipelined as in the forward kernel.  The targets' weights
-// are taken off in a product of their own, in the few subtiles that hold a target of the wave's rows, and in two
-// roundings of which the second takes up what the first leaves: they are most of a row that is a target.
+// 32 * N table rows a wave; the rows x stream past them, pipelined as in the forward kernel.  A target's weight g (p - 1) enters
+// by a product of its own, in the few subtiles that hold a target of the wave's rows: the 1 is taken off before anything is
+// rounded, as p and 1 have hardly a bit between them where the model predicts well, and the difference goes in two
+// roundings of which the second takes up what the first leaves, as it is most of a row that is a target.
 template <typename T, int DP, int N, int W, bool SHARED> __global__ __launch_bounds__(64 * W) void k_vocab_grad_table(TableGradArgs a)
 {
     constexpr int XT = sizeof(T) == 4 && DP > 128 ? 32 : 64;
@@ -665,6 +669,34 @@ template <typename T, int DP, int N, int W, bool SHARED> __global__ __launch_bou
             for (int d = 0; d < DT; d++)
                 o[j][d] = recd_f32x16{};
         }
+        // the targets among the scores x of subtile st in buffer b: their products, and -inf in the scores' place, whose weight is 0
+        auto take_targets = [&](int b, int st, recd_f32x16(&x)[N]) {
+            const int32_t mine = target[b][32 * st + (lane & 31)];
+            if (!__any(mine >= v0 && mine < v0 + 32 * N))
+                return;
+#pragma unroll
+            for (int j = 0; j < N; j++)
+#pragma unroll
+                for (int h = 0; h < 2; h++) {
+                    Frag p[2];
+#pragma unroll
+                    for (int e = 0; e < 8; e++) {
+                        const int r = 8 * h + e, row = 32 * st + recd_sums_row(r, lane);
+                        const bool hit = target[b][row] == v0 + 32 * j + (lane & 31);
+                        const float w = hit ? (recd_exp2(x[j][r] * a.c - lse[b][row]) - 1.0f) * g[b][row] : 0.0f;
+                        x[j][r] = hit ? -INFINITY : x[j][r];
+                        p[0][e] = (T)w;
+                        p[1][e] = (T)(w - (float)p[0][e]);
+                    }
+#pragma unroll
+                    for (int d = 0; d < DT; d++) {
+                        const Frag rows = tiles_lds[b].columns(32 * st + 16 * h, 32 * d, lane);
+                        o[j][d] = Mma::mul(rows, p[0], o[j][d]);
+                        if constexpr (sizeof(T) == 2)
+                            o[j][d] = Mma::mul(rows, p[1], o[j][d]);
+                    }
+                }
+        };
         if constexpr (SHARED)
             __syncthreads();  // the last group's readers are through
         if (ta < tb) {
@@ -687,6 +719,7 @@ template <typename T, int DP, int N, int W, bool SHARED> __global__ __launch_bou
             for (int st = 0; st < TURNS; st++) {
                 constexpr int kLast = TURNS - 1;
                 const int now = TURNS == 1 ? 0 : st & 1, then = TURNS == 1 ? 1 : 1 - now;
+                take_targets(buf, st, s[now]);
                 if (st == kLast)
                     __syncthreads();
                 // (behind the last tile: of what an older tile left in LDS, for nobody)
@@ -716,28 +749,6 @@ template <typename T, int DP, int N, int W, bool SHARED> __global__ __launch_bou
                             o[j][d] = Mma::mul(x, p[j], o[j][d]);
                     }
                 }
-                const int32_t mine = target[buf][32 * st + (lane & 31)];
-                if (__any(mine >= v0 && mine < v0 + 32 * N))
-#pragma unroll
-                    for (int j = 0; j < N; j++)
-#pragma unroll
-                        for (int h = 0; h < 2; h++) {
-                            Frag p[2];
-#pragma unroll
-                            for (int e = 0; e < 8; e++) {
-                                const int row = 32 * st + recd_sums_row(8 * h + e, lane);
-                                const float w = target[buf][row] == v0 + 32 * j + (lane & 31) ? -g[buf][row] : 0.0f;
-                                p[0][e] = (T)w;
-                                p[1][e] = (T)(w - (float)p[0][e]);
-                            }
-#pragma unroll
-                            for (int d = 0; d < DT; d++) {
-                                const Frag x = tiles_lds[buf].columns(32 * st + 16 * h, 32 * d, lane);
-                                o[j][d] = Mma::mul(x, p[0], o[j][d]);
-                                if constexpr (sizeof(T) == 2)
-                                    o[j][d] = Mma::mul(x, p[1], o[j][d]);
-                            }
-                        }
                 if constexpr (TURNS == 1)
 #pragma unroll
                     for (int j = 0; j < N; j++)

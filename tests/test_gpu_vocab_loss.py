@@ -286,3 +286,54 @@ def test_refusals(ctx):
                dict(gt=p + 2), dict(V=0), dict(scale=0.0)):
         assert backward(**kw) == recd.RECD_EINVAL, kw
     assert forward(n=0, x=None, t=None, loss=None, lse=None) == recd.RECD_OK
+
+
+def confident(dt, seed, n=400, D=64):
+    """Rows that their model predicts well, 1 - p_t from a tenth to 1e-4: every target a table row of its own, behind one that
+    points the same way and stands 4 to 13 powers of two below it."""
+    half = 500
+    table = du.rand((2 * half, D), dt, seed)
+    table[:half] = (table[half:].double() * 0.7).to(table.dtype)
+    t = torch.randperm(half, generator=torch.Generator().manual_seed(seed))[:n] + half
+    w = table[t].double()
+    z = torch.linspace(10.0, 30.0, n, dtype=torch.float64)[:, None]
+    x = (w * z / w.square().sum(1, keepdim=True)).to(table.dtype)
+    return x, table, t, du.rand((n,), "f32", seed + 3, 0.1, 1.0)
+
+
+@pytest.mark.parametrize("dt", ["f16", "bf16"])
+@pytest.mark.parametrize("n,scale", [(400, 1.0), (200, 1.0), (400, -1.0)])   # (many rows, few rows, a negative scale)
+def test_rows_that_are_predicted_well(ctx, dt, n, scale):
+    """Gradients of a row in proportion to what is left to learn, 1 - p_t, not to 1.
+
+    The target's weight in the table's gradient is g (p_t - 1), subtracted before anything is rounded, and the row's gradient the
+    others' probabilities, each with its own rounding u; what fp32 leaves of a logit, dz, counts in full beside 1 - p_t.  A logit
+    is a sum of D / 16 matrix products of exact terms, each off by 2 E of what it has summed, and the steps of its exponent."""
+    x, table, t, gl = confident(dt, 31, n)
+    x = x if scale > 0 else -x
+    got = check(ctx, x, table, t, scale, gl)
+    u = du.U[x.dtype]
+    xd, w = x.double(), table.double()
+    z = scale * (xd @ w.t())
+    lse = torch.logsumexp(z, 1)
+    p = (z - lse[:, None]).exp()
+    rows = torch.arange(n)
+    pt = p[rows, t]
+    left = p.clone()
+    left[rows, t] = 0.0
+    rest = left.sum(1)                                                # 1 - p_t
+    assert rest.min() < 2e-4 and 0.04 < rest.max() < 0.2
+    D = x.shape[1]
+    dz = 2 * du.E * (D / 16 + 4) * (xd.abs() * w[t].abs()).sum(1) + 8 * du.E * (z[rows, t].abs() + lse.abs())
+    g = gl.double()
+    weights = left * g[:, None]
+    weights[rows, t] = -g * rest
+    want = scale * (weights.t() @ xd)[t]
+    off = (got["grad_table"].double().cpu()[t] - want).norm(dim=1)
+    shares = ((left * g[:, None]).t() @ xd.abs())[t].norm(dim=1) + (g * rest)[:, None].mul(xd.abs()).norm(dim=1)
+    bound = u * want.norm(dim=1) + u * shares + g * pt * dz * xd.norm(dim=1)
+    assert (off <= bound).all(), float((off / bound).max())
+    want = scale * g[:, None] * (left @ w - rest[:, None] * w[t])
+    off = (got["grad_x"].double().cpu() - want).norm(dim=1)
+    bound = u * want.norm(dim=1) + g * ((u * (left @ w.abs() + rest[:, None] * w[t].abs())).norm(dim=1) + (dz + 8 * du.E) * w[t].norm(dim=1))
+    assert (off <= bound).all(), float((off / bound).max())
