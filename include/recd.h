@@ -622,7 +622,8 @@ recd_status recd_vocab_loss_backward(recd_ctx *ctx, int64_t n, int64_t V, int D,
  *       then, with slopes: z_ij -= slopes[head] * |pos_i - j|
  *       visible keys: all of the list's; causal: j <= pos_i, or j < prefix[l] where prefix is given
  *       out_i = sum over the visible j of softmax(z_i)_j v_j;  a row that sees no key gives 0 (and lse = -inf)
- *     What a row does not see does not reach it, be it infinite or NaN (nor its gradients; such tiles take a slow way).
+ *     What a row does not see does not reach it, be it infinite or NaN, nor its gradients.  Gradients of what does see it
+ *     are not finite where the formula's are not; whether infinite or NaN is not said.
  *     Heads: query head h reads key head h / (heads / kv_heads).  One query row per list is the form for serving a new
  *     token; keys are split over blocks where there are few tiles. */
 typedef struct recd_attention {

@@ -220,141 +220,48 @@ template <typename T, int DT> __device__ inline void store_columns(T *row, const
 }
 
 // What is masked enters the products with weight 0, which is not enough where it is an infinity or a NaN: 0 * NaN is a NaN,
-// in rows of the tile that do not see it.  Sums that are not finite are therefore thrown away and their rows done again,
-// one at a time by the whole wave and over what they see alone.  The check costs an addition a sum at the kernel's end;
-// the way of one row, which only such data takes, is plain.  Rows whose own scores hold a NaN (all of a model that has come
-// apart) are NaN throughout and are left as they are.
-//
-// The rows (lanes of the tile's sums) that are to be done again, a bit each.
-template <int DT> __device__ inline uint32_t not_finite(const recd_f32x16 (&o)[DT], bool there)
+// in rows of the tile that do not see it.  Only tiles at the mask's edge hold what some of their rows see and others do not: the
+// streamed rows of those are looked through on their way to LDS, zeros take the place of what is not finite there (after the scores,
+// which need it as it is), and at the kernel's end every row is given what of it the row does see.  The looking through costs
+// three operations a word of such tiles, and what is found the reading of those tiles' rows once more, however much it is.
+
+// Whether any of a block's waves says so, or a wave that streams for itself.
+template <bool SHARED, int WAVES> __device__ inline bool any_wave(bool mine, int (&says)[WAVES], int wave, int lane)
 {
-    float s = 0.0f;
-#pragma unroll
-    for (int t = 0; t < DT; t++)
-#pragma unroll
-        for (int r = 0; r < 16; r++)
-            s += o[t][r] * 0.0f;
-    const uint64_t lanes = __ballot(there && !(s == 0.0f));
-    return (uint32_t)lanes | (uint32_t)(lanes >> 32);
+    if constexpr (SHARED) {
+        if (lane == 0)
+            says[wave] = mine;
+        __syncthreads();
+        int any = 0;
+        for (int w = 0; w < WAVES; w++)
+            any |= says[w];
+        return __builtin_amdgcn_readfirstlane(any) != 0;
+    }
+    return mine;
 }
 
-// <x, y> of two heads, in every lane.
-template <typename T> __device__ inline float wave_dot(const T *x, const T *y, int d, int lane)
+// Adds what is not finite in the streamed rows [s0, s1) to the sums of the lanes whose column sees it: itself under weights that
+// are positive, else a NaN.
+template <bool POSITIVE, typename T, int DT, typename Row, typename Sees>
+__device__ inline void add_not_finite(int s0, int s1, int d, Row row_of, Sees sees, recd_f32x16 (&o)[DT], int lane)
 {
-    float s = 0.0f;
-    for (int e = lane; e < d; e += 64)
-        s += (float)x[e] * (float)y[e];
-    for (int o = 32; o; o >>= 1)
-        s += __shfl_xor(s, o);
-    return s;
-}
-
-// The score of query row `query`, head h, and key j in powers of two, and its derivative by the scaled product.
-__device__ inline float plain_score(const Args &a, const Problem &p, float dot, int query, int h, int j, float &slope_of)
-{
-    float z = dot * a.scale;
-    slope_of = 1.0f;
-    if (a.cap > 0.0f) {
-        const float t = tanhf(z / a.cap);
-        slope_of = 1.0f - t * t;
-        z = a.cap * t;
-    }
-    if (a.slopes)
-        z -= a.slopes[h] * fabsf((float)(p.pos0 + query - j));
-    return z * kRecdLog2e;
-}
-
-// Row `row` of the forward pass over the keys [j0, j1) of those it sees.
-template <typename T> __device__ void attend_again(const Args &a, const Problem &p, int head, int row, int j0, int j1, int split, int lane)
-{
-    const int query = p.query(row, a.group), h = head * a.group + row - query * a.group, lim = p.limit(row, a.group);
-    const int64_t at_row = (p.q0 + query) * (a.G * a.group) + h;
-    const T *q = (const T *)a.q + (p.q0 + query) * a.q_stride + (int64_t)h * a.d;
-    float m = -INFINITY, l = 0.0f, o[2] = {0.0f, 0.0f}, unused;
-    for (int j = j0; j < j1 && j < lim; j++) {
-        const T *k = (const T *)a.k + (p.k0 + j) * a.k_stride + (int64_t)head * a.d;
-        const T *v = (const T *)a.v + (p.k0 + j) * a.v_stride + (int64_t)head * a.d;
-        const float z = plain_score(a, p, wave_dot(q, k, a.d, lane), query, h, j, unused);
-        const float now = fmaxf(m, z), from = now == -INFINITY ? 0.0f : now, f = recd_exp2(m - from), w = recd_exp2(z - from);
-        m = now;
-        l = l * f + w;
-        for (int i = 0; i < 2; i++)
-            if (lane + 64 * i < a.d)
-                o[i] = o[i] * f + w * (float)v[lane + 64 * i];
-    }
-    const int64_t at = split * a.part_rows + at_row;
-    if (lane == 0 && a.splits > 1) {
-        a.part_m[at] = m;
-        a.part_l[at] = l;
-    } else if (lane == 0 && a.lse) {
-        a.lse[at_row] = (m + log2f(l)) * kRecdLn2;
-    }
-    for (int i = 0; i < 2; i++) {
-        const int e = lane + 64 * i;
-        if (e >= a.d)
+    asm volatile("" : "+v"(lane));  // columns that no register holds through the kernel's loop
+#pragma unroll 1
+    for (int s = s0; s < s1; s++) {
+        if (!sees(s))
             continue;
-        if (a.splits > 1)
-            a.part_o[at * a.d + e] = o[i];
-        else
-            ((T *)a.out)[at_row * a.d + e] = (T)(l == 0.0f ? 0.0f : o[i] / l);
-    }
-}
-
-// The weights of the pair (row, key j) in the gradients: p for dv, ds / scale for dq and dk.
-template <typename T>
-__device__ inline void pair_again(const Args &a, const Problem &p, int head, int row, int j, int lane, float &weight, float &ds)
-{
-    const int query = p.query(row, a.group), h = head * a.group + row - query * a.group;
-    const int64_t at_row = (p.q0 + query) * (a.G * a.group) + h;
-    const T *k = (const T *)a.k + (p.k0 + j) * a.k_stride + (int64_t)head * a.d;
-    const T *v = (const T *)a.v + (p.k0 + j) * a.v_stride + (int64_t)head * a.d;
-    const T *q = (const T *)a.q + (p.q0 + query) * a.q_stride + (int64_t)h * a.d, *g = (const T *)a.g + at_row * a.d;
-    const T *out = (const T *)a.out_in + at_row * a.d;
-    float slope_of;
-    const float z = plain_score(a, p, wave_dot(q, k, a.d, lane), query, h, j, slope_of);
-    weight = recd_exp2(z - a.lse_in[at_row] * kRecdLog2e);
-    ds = weight * (wave_dot(g, v, a.d, lane) - wave_dot(g, out, a.d, lane)) * slope_of;
-}
-
-// Row `row` of the gradients by queries.
-template <typename T> __device__ void grad_q_again(const Args &a, const Problem &p, int head, int row, int lane)
-{
-    const int query = p.query(row, a.group), h = head * a.group + row - query * a.group, lim = p.limit(row, a.group);
-    float o[2] = {0.0f, 0.0f}, weight, ds;
-    for (int j = 0; j < lim; j++) {
-        pair_again<T>(a, p, head, row, j, lane, weight, ds);
-        for (int i = 0; i < 2; i++)
-            if (lane + 64 * i < a.d)
-                o[i] += ds * (float)((const T *)a.k + (p.k0 + j) * a.k_stride + (int64_t)head * a.d)[lane + 64 * i];
-    }
-    for (int i = 0; i < 2; i++)
-        if (lane + 64 * i < a.d)
-            ((T *)a.gq + (p.q0 + query) * a.gq_stride + (int64_t)h * a.d)[lane + 64 * i] = (T)(o[i] * a.scale);
-}
-
-// Key j of the gradients by keys and values.
-template <typename T> __device__ void grad_kv_again(const Args &a, const Problem &p, int head, int j, int lane)
-{
-    float dk[2] = {0.0f, 0.0f}, dv[2] = {0.0f, 0.0f}, weight, ds;
-    for (int row = 0; row < p.rows; row++) {
-        if (p.limit(row, a.group) <= j)
-            continue;
-        pair_again<T>(a, p, head, row, j, lane, weight, ds);
-        const int query = p.query(row, a.group), h = head * a.group + row - query * a.group;
-        for (int i = 0; i < 2; i++) {
-            const int e = lane + 64 * i;
-            if (e < a.d) {
-                dk[i] += ds * (float)((const T *)a.q + (p.q0 + query) * a.q_stride + (int64_t)h * a.d)[e];
-                dv[i] += weight * (float)((const T *)a.g + ((p.q0 + query) * (a.G * a.group) + h) * a.d)[e];
+        const T *row = row_of(s);
+#pragma unroll
+        for (int t = 0; t < DT; t++)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4) {
+                const int col = 32 * t + recd_sums_row(r, lane);
+                const T *four = row + (col < d ? col : 0);  // (behind the head's end: sums that nobody stores)
+                for (int q = 0; q < 4; q++) {
+                    const float x = (float)four[q];
+                    o[t][r + q] += POSITIVE ? (fabsf(x) < INFINITY ? 0.0f : x) : x - x;
+                }
             }
-        }
-    }
-    for (int i = 0; i < 2; i++) {
-        const int e = lane + 64 * i;
-        if (e < a.d) {
-            ((T *)a.gk + (p.k0 + j) * a.gk_stride + (int64_t)head * a.d)[e] = (T)(dk[i] * a.scale);
-            ((T *)a.gv + (p.k0 + j) * a.gv_stride + (int64_t)head * a.d)[e] = (T)dv[i];
-        }
     }
 }
 
@@ -377,6 +284,7 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
     __shared__ struct {
         typename S::Tile k[S::OWN][BUFS], v[S::OWN][BUFS];
     } lds;
+    __shared__ int says[KEPT * PHASES];
     Problem p;
     int head, tile, split;
     int head_end;
@@ -397,6 +305,7 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
     const int wave_end = row0 < p.rows ? p.limit(wave_last, a.group) : 0;
     const int wave_full = row0 + 32 <= p.rows ? p.limit(row0, a.group) : 0;  // keys that every row sees
     const int tiles = (p.limit(end - 1, a.group) + 31) / 32;
+    const int edge = p.limit(first, a.group) / 32;  // the block's first tile that not all of its rows see
     const int part = split * PHASES + phase, parts = a.splits * PHASES;
     const int each = parts == 1 ? tiles : (tiles + parts - 1) / parts;  // tiles of a part
     const int t0 = part * each < tiles ? part * each : tiles, t1 = t0 + each < tiles ? t0 + each : tiles;
@@ -477,10 +386,18 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
                     o[d][r] *= f;
         }
     };
+    bool odd = false;  // the wave's threads have seen what is not finite at the edge
+    auto store = [&](int t, int b) {
+        ks.store(tid, kt[b]);
+        vs.store(tid, vt[b]);
+        if (t >= edge && __any(vs.not_finite(tid))) {
+            vt[b].make_finite(tid, S::LOADERS);  // (what the thread has stored itself)
+            odd = true;
+        }
+    };
     if (t0 < t1) {
         load(t0);
-        ks.store(tid, kt[0]);
-        vs.store(tid, vt[0]);
+        store(t0, 0);
         if (t0 + 1 < t1)
             load(t0 + 1);
         S::sync();
@@ -493,8 +410,7 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
     auto turn = [&](int t, recd_f32x16 &now, recd_f32x16 &then) {
         const int next = buf + 1 == BUFS ? 0 : buf + 1;
         if (t + 1 < t1) {
-            ks.store(tid, kt[next]);
-            vs.store(tid, vt[next]);
+            store(t + 1, next);
             if (t + 2 < t1)
                 load(t + 2);
         }
@@ -525,6 +441,11 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
         turn(t, s[0], s[1]);
         if (t + 1 < t1)
             turn(t + 1, s[1], s[0]);
+    }
+    if (t1 > edge && any_wave<S::SHARED>(odd, says, wave, lane)) {
+        const T *values = (const T *)a.v + p.k0 * a.v_stride + head * a.d;
+        add_not_finite<true, T>(t0 > edge ? t0 * 32 : edge * 32, t1 * 32 < p.nk ? t1 * 32 : p.nk, a.d,
+                                [&](int j) { return values + j * a.v_stride; }, [&](int j) { return j < lim; }, o, lane);
     }
     l += __shfl_xor(l, 32);
     if constexpr (PHASES > 1) {  // in the order of the phases: the larger maximum, both sums scaled to it
@@ -557,23 +478,20 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
     }
     if (phase)
         return;
-    uint32_t again = not_finite<DT>(o, there && l == l);
-    if (there && !(again >> (lane & 31) & 1)) {
-        if (a.splits > 1) {
-            const int64_t at = split * a.part_rows + at_row;
-            if (lane < 32) {
-                a.part_m[at] = m;
-                a.part_l[at] = l;
-            }
-            store_columns<float, DT>(a.part_o + at * a.d, o, 1.0f, a.d, lane);
-        } else {
-            if (a.lse && lane < 32)
-                a.lse[at_row] = (m + log2f(l)) * kRecdLn2;  // -inf where l = 0
-            store_columns<T, DT>((T *)a.out + at_row * a.d, o, l == 0.0f ? 0.0f : 1.0f / l, a.d, lane);
+    if (!there)
+        return;
+    if (a.splits > 1) {
+        const int64_t at = split * a.part_rows + at_row;
+        if (lane < 32) {
+            a.part_m[at] = m;
+            a.part_l[at] = l;
         }
+        store_columns<float, DT>(a.part_o + at * a.d, o, 1.0f, a.d, lane);
+    } else {
+        if (a.lse && lane < 32)
+            a.lse[at_row] = (m + log2f(l)) * kRecdLn2;  // -inf where l = 0
+        store_columns<T, DT>((T *)a.out + at_row * a.d, o, l == 0.0f ? 0.0f : 1.0f / l, a.d, lane);
     }
-    for (; again; again &= again - 1)
-        attend_again<T>(a, p, head, row0 + __ffs(again) - 1, split * PHASES * each * 32, (split + 1) * PHASES * each * 32, split, lane);
 }
 
 // The forward kernel for lists of few rows: a wave to itself goes through one head after the other, whose rows are on
@@ -621,7 +539,9 @@ template <typename T, int DP, bool CAP> __global__ __launch_bounds__(64, (sizeof
         ks.load_rows(lane, (const T *)a.k + at * a.k_stride + hd * a.d, p.nk - t * 32, a.d, (uint32_t)a.k_stride * sizeof(T));
         vs.load_rows(lane, (const T *)a.v + at * a.v_stride + hd * a.d, p.nk - t * 32, a.d, (uint32_t)a.v_stride * sizeof(T));
     };
+    bool odd = false;  // something that is not finite in the head's tiles (few, and most of them at the mask's edge)
     auto take = [&]() {
+        odd = false;
         slope = slope_n;
         m = -INFINITY;
         l = 0.0f;
@@ -632,11 +552,9 @@ template <typename T, int DP, bool CAP> __global__ __launch_bounds__(64, (sizeof
         for (int d = 0; d < DT; d++)
             o[d] = recd_f32x16{};
     };
-    uint32_t again = 0;  // the rows of any head
     auto write = [&]() {
         const float sum = l + __shfl_xor(l, 32);
         const int64_t at_row = q_row * H + head * a.group + head_in;
-        again |= not_finite<DT>(o, there && sum == sum);
         if (!there)
             return;
         if (a.splits > 1) {
@@ -657,12 +575,13 @@ template <typename T, int DP, bool CAP> __global__ __launch_bounds__(64, (sizeof
         load(head, t0);
     take();
     if (t0 == t1)
-        for (; head + 1 < head_end; head++)  // no keys
+        for (; head < head_end; head++)  // no keys
             write();
     for (int t = t0; t < t1;) {
         S::sync();
         ks.store(lane, kt);
         vs.store(lane, vt);
+        const bool clear = __any(vs.not_finite(lane));
         S::sync();
         const bool last = t + 1 == t1, more = last && head + 1 < head_end;
         if (!last || more)
@@ -674,6 +593,11 @@ template <typename T, int DP, bool CAP> __global__ __launch_bounds__(64, (sizeof
 #pragma unroll
         for (int k = 0; k < KS; k++)
             s = Mma::mul(kt.rows(0, 16 * k, lane), qf[k], s);
+        if (clear) {
+            vt.make_finite(lane, 64);
+            S::sync();
+            odd = true;
+        }
         auto finish = [&](auto registers) {
             constexpr int NR = registers.value;
             if (a.slopes) {
@@ -732,21 +656,20 @@ template <typename T, int DP, bool CAP> __global__ __launch_bounds__(64, (sizeof
         else
             finish(std::integral_constant<int, 16>{});
         t++;
-        if (more) {
+        if (last) {
+            if (odd) {
+                const T *values = (const T *)a.v + p.k0 * a.v_stride + head * a.d;
+                add_not_finite<true, T>(t0 * 32, t1 * 32 < p.nk ? t1 * 32 : p.nk, a.d, [&](int j) { return values + j * a.v_stride; },
+                                        [&](int j) { return j < lim; }, o, lane);
+            }
             write();
+        }
+        if (more) {
             head++;
             t = t0;
             take();
         }
     }
-    write();
-    if (!again)
-        return;
-    __threadfence_block();  // the rows' first sums are written
-    find_tile(a, p, head, head_end, tile, split);
-    for (; head < head_end; head++)
-        for (uint32_t rows = again; rows; rows &= rows - 1)
-            attend_again<T>(a, p, head, row0 + __ffs(rows) - 1, split * each * 32, (split + 1) * each * 32, split, lane);
 }
 
 // Joins the splits of the forward pass where they are few: 2^dlog threads a row, four elements each.
@@ -998,6 +921,7 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
     __shared__ struct {
         typename S::Tile k[S::OWN][BUFS], v[S::OWN][BUFS];
     } lds;
+    __shared__ int says[2][KEPT * PHASES];
     Problem p;
     int head, head_end, tile, split;
     if (!find_tile(a, p, head, head_end, tile, split))
@@ -1017,6 +941,8 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
     const int wave_end = row0 < p.rows ? p.limit(wave_last, a.group) : 0;
     const int wave_full = row0 + 32 <= p.rows ? p.limit(row0, a.group) : 0;
     const int tiles = (p.limit(end - 1, a.group) + 31) / 32, t0 = tiles * phase / PHASES, t1 = tiles * (phase + 1) / PHASES;
+    // the block's first tile that not all of its rows see (a wave that has few tiles looks all of them through)
+    const int edge = ONE ? 0 : p.limit(first, a.group) / 32;
     const int H = a.G * a.group;
     const int64_t q_row = p.q0 + query;
     const float posf = (float)(p.pos0 + query);
@@ -1058,6 +984,7 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
         ks.load_rows(tid, (const T *)a.k + at * a.k_stride + head * a.d, p.nk - t * 32, a.d, (uint32_t)a.k_stride * sizeof(T));
         vs.load_rows(tid, (const T *)a.v + at * a.v_stride + head * a.d, p.nk - t * 32, a.d, (uint32_t)a.v_stride * sizeof(T));
     };
+    bool odd = false;  // something that is not finite in a tile at the edge
     if (t0 < t1)
         load(t0);
     for (int t = t0; t < t1; t++) {
@@ -1066,18 +993,31 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
             S::sync();
         ks.store(tid, kt[buf]);
         vs.store(tid, vt[buf]);
-        S::sync();
+        const bool clear = t >= edge && any_wave<S::SHARED>(__any(ks.not_finite(tid)), says[t & 1], wave, lane);
+        if (!S::SHARED || t < edge)
+            S::sync();
         if (t + 1 < t1)
             load(t + 1);
+        auto make_finite = [&]() {
+            S::sync();
+            kt[buf].make_finite(tid, S::LOADERS);
+            S::sync();
+            odd = true;
+        };
         const int j0 = t * 32;
-        if (j0 >= wave_end)
+        if (S::SHARED && j0 >= wave_end) {
+            if (clear)
+                make_finite();
             continue;
+        }
         recd_f32x16 s = {}, dp = {};
 #pragma unroll
         for (int k = 0; k < KS; k++) {
             s = Mma::mul(kt[buf].rows(0, 16 * k, lane), qf[k], s);
             dp = Mma::mul(vt[buf].rows(0, 16 * k, lane), gf[k], dp);
         }
+        if (clear)
+            make_finite();
         // the exponent, then p, then ds
         auto ds_of = [&](float x, float d, float more) {
             float quarter = 1.0f;
@@ -1116,18 +1056,20 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
         else
             finish(std::integral_constant<int, 16>{});
     }
+    if (odd) {
+        const T *keys = (const T *)a.k + p.k0 * a.k_stride + head * a.d;
+        add_not_finite<false, T>(t0 > edge ? t0 * 32 : edge * 32, t1 * 32 < p.nk ? t1 * 32 : p.nk, a.d,
+                                 [&](int j) { return keys + j * a.k_stride; }, [&](int j) { return j < lim; }, o, lane);
+    }
     if constexpr (PHASES > 1) {
         static_assert(sizeof(lds) >= 64 * 16 * DT * sizeof(float));
         join_sums<DT, PHASES>(o, reinterpret_cast<float *>(&lds), 0, phase, lane);
     }
     if (phase)
         return;
-    uint32_t again = not_finite<DT>(o, there && (lim == 0 || (from == from && delta == delta)));
-    if (there && !(again >> (lane & 31) & 1))
+    if (there)
         store_columns<T, DT>((T *)a.gq + q_row * a.gq_stride + (int64_t)h * a.d, o, (CAP ? 4.0f : 1.0f) * a.scale / lift, a.d,
                              lane);
-    for (; again; again &= again - 1)
-        grad_q_again<T>(a, p, head, row0 + __ffs(again) - 1, lane);
 }
 
 // Keys stay, queries and their gradients stream past.  What a score needs of its row stands in LDS in the order of
@@ -1149,6 +1091,7 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
         alignas(16) float pos[S::OWN][BUFS][S::ROWS];
         alignas(16) int lim[S::OWN][BUFS][S::ROWS];
     } lds;
+    __shared__ int says[2][KEPT * PHASES];
     Problem p;
     int head, head_end, tile, split;
     if (!find_tile(a, p, head, head_end, tile, split))
@@ -1199,6 +1142,14 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
     const int t0 = S::SHARED ? from_tile : from_tile + n_tiles * phase / PHASES;
     const int t1 = S::SHARED ? tiles : from_tile + n_tiles * (phase + 1) / PHASES;
     const int sub = S::SHARED ? 32 * phase : 0;
+    // rows from `whole_row` on see all of the block's keys; tiles with earlier ones, and a last one that is filled up, are at the edge
+    // (a wave that has few tiles looks all of them through)
+    const int keys_end = first + 32 * KEPT < p.nk ? first + 32 * KEPT : p.nk;
+    int whole_row = 0;
+    if (p.causal && p.prefix < keys_end && keys_end - 1 > p.pos0)
+        whole_row = (int)((int64_t)(keys_end - 1 - p.pos0) * a.group < p.rows ? (keys_end - 1 - p.pos0) * a.group : p.rows);
+    auto at_edge = [&](int t) { return KEPT * PHASES == 1 || t * S::ROWS < whole_row || (t + 1) * S::ROWS > p.rows; };
+    bool odd = false;  // something that is not finite in a tile at the edge
     typename S::Load qs, gs;
     float n_from = 0.0f, n_delta = 0.0f, n_slope = 0.0f;
     float n_pos = 0.0f;
@@ -1246,14 +1197,26 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
             row_lim[buf][i] = n_lim;
             row_pos[buf][i] = n_pos;
         }
-        S::sync();
+        const bool clear = at_edge(t) && any_wave<S::SHARED>(__any(qs.not_finite(tid) | gs.not_finite(tid)), says[t & 1], wave, lane);
+        if (!S::SHARED || !at_edge(t))
+            S::sync();
         if (t + 1 < t1)
             load(t + 1);
+        auto make_finite = [&]() {
+            S::sync();
+            qt[buf].make_finite(tid, S::LOADERS);
+            gt[buf].make_finite(tid, S::LOADERS);
+            S::sync();
+            odd = true;
+        };
         const int row0 = t * S::ROWS + sub;
         const bool whole = row0 + 32 <= p.rows;
         // (tile row 31 is the product's row 31, and limits do not fall: what it does not see, no row sees)
-        if (j0 >= p.nk || row0 >= p.rows || (whole && __builtin_amdgcn_readfirstlane(row_lim[buf][sub + 31]) <= j0))
+        if (j0 >= p.nk || row0 >= p.rows || (whole && __builtin_amdgcn_readfirstlane(row_lim[buf][sub + 31]) <= j0)) {
+            if (S::SHARED && clear)
+                make_finite();
             continue;
+        }
         recd_f32x16 s = {}, dp = {};
 #pragma unroll
         for (int k = 0; k < KS; k++) {
@@ -1268,6 +1231,8 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
             s = Mma::mul(qt[buf].rows(sub, 16 * k, lane), key, s);
             dp = Mma::mul(gt[buf].rows(sub, 16 * k, lane), value, dp);
         }
+        if (clear)
+            make_finite();
         auto score = [&](int r, float more, float delta) {
             float quarter = 1.0f;
             const float z = CAP ? capped.value(s[r] * to_cap, more, quarter) : s[r] * c + more;
@@ -1315,6 +1280,23 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
             }
         }
     }
+    if (odd) {
+        auto at = [&](const void *x, int64_t stride) {
+            return [=, &p, &a](int row) {
+                const int query = p.query(row, a.group), h = head * a.group + row - query * a.group;
+                return (const T *)x + (p.q0 + query) * stride + (int64_t)h * a.d;
+            };
+        };
+        auto sees = [&](int row) { return j < p.limit(row, a.group); };
+#pragma unroll 1
+        for (int t = t0; t < t1; t++) {
+            const int s0 = t * S::ROWS + sub, s1 = s0 + 32 < p.rows ? s0 + 32 : p.rows;
+            if (!at_edge(t))
+                continue;
+            add_not_finite<false, T>(s0, s1, a.d, at(a.q, a.q_stride), sees, dk, lane);
+            add_not_finite<true, T>(s0, s1, a.d, at(a.g, (int64_t)H * a.d), sees, dv, lane);
+        }
+    }
     if constexpr (PHASES > 1) {
         static_assert(sizeof(lds) >= KEPT * 64 * 16 * DT * sizeof(float));
         join_sums<DT, PHASES>(dk, reinterpret_cast<float *>(&lds), kept, phase, lane);
@@ -1322,19 +1304,11 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
     }
     if (phase)
         return;
-    uint32_t again = not_finite<DT>(dk, there) | not_finite<DT>(dv, there);
-    if (again) {  // the last row sees every key
-        const int64_t last = (p.q0 + p.nq - 1) * H + head * a.group;
-        const float lse = a.lse_in[last], delta = a.delta[last];
-        again = lse == lse && delta == delta ? again : 0;
-    }
-    if (there && !(again >> (lane & 31) & 1)) {
+    if (there) {
         store_columns<T, DT>((T *)a.gk + (p.k0 + j) * a.gk_stride + (int64_t)head * a.d, dk, (CAP ? 4.0f : 1.0f) * a.scale / lift,
                              a.d, lane);
         store_columns<T, DT>((T *)a.gv + (p.k0 + j) * a.gv_stride + (int64_t)head * a.d, dv, recd_exp2(-kLiftP<T>), a.d, lane);
     }
-    for (; again; again &= again - 1)
-        grad_kv_again<T>(a, p, head, j0 + __ffs(again) - 1, lane);
 }
 
 // Offsets that do not rise from 0 to the number of rows, or pass the caller's bound of a list's length.

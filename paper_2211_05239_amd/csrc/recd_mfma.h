@@ -59,6 +59,44 @@ __device__ inline int recd_product_row(int i) { return (i & ~15) | (i >> 1 & 1) 
 __device__ inline int recd_sums_row(int r, int lane) { return 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3); }
 __device__ inline int recd_score_row(int r, int lane) { return 16 * (r >> 3) + 4 * (r & 3) + 2 * (r >> 2 & 1) + (lane >> 5); }
 
+// 0 * x is a NaN where x is an infinity or a NaN: an operation a word, of one or two values, and `sum` stays 0 without them.
+typedef _Float16 recd_f16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 recd_bf16x2 __attribute__((ext_vector_type(2)));
+template <typename T> __device__ inline float recd_zeros(typename RecdPiece<T>::type v, float sum)
+{
+    const recd_u32x4 b = __builtin_bit_cast(recd_u32x4, v);
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        if constexpr (sizeof(T) == 4)
+            sum = __builtin_fmaf(v[i], 0.0f, sum);
+        else if constexpr (std::is_same<T, _Float16>::value)
+            sum = __builtin_amdgcn_fdot2(__builtin_bit_cast(recd_f16x2, (uint32_t)b[i]), recd_f16x2{}, sum, false);
+        else
+            sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(recd_bf16x2, (uint32_t)b[i]), recd_bf16x2{}, sum, false);
+    }
+    return sum;
+}
+// Infinities and NaN are the values whose exponent is all ones: one more carries into the sign's place.
+template <typename T> struct RecdExponent {
+    static constexpr bool HALF = std::is_same<T, _Float16>::value;
+    static constexpr uint32_t ALL = sizeof(T) == 4 ? 0x7f800000u : HALF ? 0x7c007c00u : 0x7f807f80u;
+    static constexpr uint32_t ONE = sizeof(T) == 4 ? 0x00800000u : HALF ? 0x04000400u : 0x00800080u;
+    static constexpr uint32_t SIGN = sizeof(T) == 4 ? 0x80000000u : 0x80008000u;
+    static constexpr int TOP = sizeof(T) == 4 ? 31 : 15;
+};
+// The piece with zeros in their place.
+template <typename T> __device__ inline typename RecdPiece<T>::type recd_finite(typename RecdPiece<T>::type v)
+{
+    using X = RecdExponent<T>;
+    recd_u32x4 b = __builtin_bit_cast(recd_u32x4, v);
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        const uint32_t hit = ((b[i] & X::ALL) + X::ONE) & X::SIGN;
+        b[i] &= ~((hit - (hit >> X::TOP)) | hit);
+    }
+    return __builtin_bit_cast(typename RecdPiece<T>::type, b);
+}
+
 // A tile of ROWS rows of DP elements in LDS.
 template <typename T, int ROWS, int DP> struct RecdTile {
     static constexpr int E = 16 / sizeof(T), LD = DP + E, PIECES = ROWS * (DP / E);
@@ -100,6 +138,15 @@ template <typename T, int ROWS, int DP> struct RecdTile {
         constexpr int PR = DP / E;
         *reinterpret_cast<Piece *>(at + (piece / PR) * LD + (piece % PR) * E) = v;
     }
+    // zeros in the place of all that is not finite, by `threads` threads of which this is `tid`, each in the pieces that it puts
+    __device__ inline void make_finite(int tid, int threads)
+    {
+        constexpr int PR = DP / E;
+        asm volatile("" : "+v"(tid));  // nothing of this is held in registers before it is needed
+#pragma unroll 1
+        for (int piece = tid; piece < PIECES; piece += threads)
+            put(piece, recd_finite<T>(*reinterpret_cast<const Piece *>(at + (piece / PR) * LD + (piece % PR) * E)));
+    }
 };
 
 // Rows of a tile from memory into registers and on into LDS, by THREADS threads of which this is `tid`.  A thread's
@@ -128,6 +175,16 @@ template <typename T, int ROWS, int DP, int THREADS> struct RecdStream {
     __device__ inline void load_rows(int tid, const T *first, int rows, int d, uint32_t stride)
     {
         load(tid, first, rows, d, [=](int r) { return (uint32_t)__umul24(r, stride); });
+    }
+    // whether the thread's pieces hold anything that is not finite
+    __device__ inline bool not_finite(int tid) const
+    {
+        float sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < PT; i++)
+            if (tid + i * THREADS < Tile::PIECES)
+                sum = recd_zeros<T>(held[i], sum);
+        return !(sum == 0.0f);
     }
     // the tile's row of a thread's piece i
     static __device__ inline int row(int tid, int i) { return (tid + i * THREADS) / (DP / Tile::E); }

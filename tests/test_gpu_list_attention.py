@@ -398,3 +398,75 @@ def test_refusals(ctx):
         assert backward(**kw) == bad, kw
     assert lib.recd_list_attention(h, None, p, p, p, p, None) == bad
     assert forward(lists=0, q_rows=0, k_rows=0, q_offsets=None, k_offsets=None, q=None, k=None, v=None, out=None) == recd.RECD_OK
+
+
+@pytest.mark.parametrize("dt", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("name", list(PLANTED))
+def test_an_infinity_that_is_seen_beside_a_nan_that_is_not(ctx, dt, name):
+    """A row that sees an infinite value gives that infinity, whatever lies in the places behind its last key."""
+    lq, lk, H, G = PLANTED[name]
+    d = 128 if name == "groups" else 40
+    qo, ko = offsets(lq), offsets(lk)
+    Q, K = int(qo[-1]), int(ko[-1])
+    q, k, v = du.rand((Q, H, d), dt, 1), du.rand((K, G, d), dt, 2), du.rand((K, G, d), dt, 3)
+    j = lk[1] - 2 if lq[1] < 5 else lk[1] // 2 + 3   # the infinity's key of the second list; behind it the NaN's
+    i = int(qo[1]) + j - (lk[1] - lq[1])             # the one query that sees the first and not the second
+    v[int(ko[1]) + j, :, 0] = float("inf")
+    v[int(ko[1]) + j, :, 1] = -float("inf")
+    v[int(ko[1]) + j + 1] = float("nan")
+    got = run(ctx, q, k, v, qo, ko, dict(scale=d ** -0.5, causal=True))
+    out = got["out"].cpu().double()
+    assert (out[i, :, 0] == float("inf")).all() and (out[i, :, 1] == -float("inf")).all() and out[i, :, 2:].isfinite().all()
+    assert out[i + 1:int(qo[2])].isnan().all()
+    rows = torch.ones(Q, dtype=torch.bool)
+    rows[i:int(qo[2])] = False
+    assert out[rows].isfinite().all()
+
+
+@pytest.mark.parametrize("dt", ["f32", "f16", "bf16"])
+def test_values_gradients_beside_an_infinite_output(ctx, dt):
+    """A last query whose output is infinite where its gradient is zero (so g . out is a NaN) hides no other row's NaN."""
+    n, d = 70, 32
+    o = offsets([n])
+    q, k, v, g = (du.rand((n, 1, d), dt, s) for s in (1, 2, 3, 4))
+    how = dict(scale=0.2, causal=True)
+    v[n - 1, 0, 0] = float("inf")          # the last query alone sees it
+    g[n - 1, 0, 0] = 0.0
+    g[40] = float("nan")
+    want = du.attention_ref(q, k, torch.nan_to_num(v, posinf=1.0), o, o, g=torch.nan_to_num(g), **how)
+    got = run(ctx, q, k, v, o, o, how, g)
+    assert got["grad_v"][:41].isnan().all()
+    du.within(got["grad_v"][41:], want["grad_v"][0][41:], want["grad_v"][1][41:], what="grad_v")
+
+
+@pytest.mark.parametrize("dt", ["f16", "bf16"])
+@pytest.mark.parametrize("where", ["gradient", "value", "everywhere"])
+def test_an_overflow_costs_a_few_passes(ctx, dt, where):
+    """One infinity in a long list's gradient or values, as after an overflow, or all of them: no more than a few times as long."""
+    n, H, G, d = 2048, 4, 2, 128
+    o = offsets([n]).cuda()
+    q, g = du.rand((n, H, d), dt, 1).cuda(), du.rand((n, H, d), dt, 4).cuda()
+    k, v = du.rand((n, G, d), dt, 2).cuda(), du.rand((n, G, d), dt, 3).cuda()
+    out, lse, gq, gk, gv = torch.empty_like(q), torch.empty(n, H, device="cuda"), torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
+
+    def took():
+        best = 1e9
+        for _ in range(5):
+            a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            torch.cuda.synchronize()
+            a.record()
+            ctx.list_attention(q, k, v, o, o, n, n, out, lse, scale=0.1, causal=True)
+            ctx.list_attention_backward(q, k, v, o, o, n, n, out, lse, g, gq, gk, gv, scale=0.1, causal=True)
+            b.record()
+            b.synchronize()
+            best = min(best, a.elapsed_time(b))
+        return best
+
+    clean = took()
+    if where == "gradient":
+        g[1200, 1, 5] = float("inf")
+    elif where == "value":
+        v[700, 1, 5] = float("inf")
+    else:
+        g[:] = float("inf")
+    assert took() < 6 * clean + 0.2
