@@ -43,7 +43,7 @@ namespace {
 constexpr float kSlack = 8.0f;  // see the running maximum of the forward kernel
 template <typename T> constexpr bool kHalf = std::is_same<T, _Float16>::value;
 // fp16 exponentials are held 2^7 times larger by the forward pass (at most 2^15 with the slack) and probabilities
-// 2^15 times by the backward pass, so that small ones keep their bits
+// 2^15 times by the backward pass, so that small ones keep their bits (ds: see keep_in_range)
 template <typename T> constexpr float kLift = kHalf<T> ? 7.0f : 0.0f;
 template <typename T> constexpr float kLiftP = kHalf<T> ? 15.0f : 0.0f;
 
@@ -68,7 +68,6 @@ struct Args {
     void *out, *gq, *gk, *gv;
     float *lse, *delta;           // [q rows][H]
     const float *lse_in;
-    const float *lift;            // fp16 backward: the power of two that ds is held larger by, else null
     float *part_m, *part_l, *part_o;
     int64_t part_rows;            // q rows * H
 };
@@ -873,39 +872,42 @@ __global__ __launch_bounds__(1024) void k_attention_tiles_by_work(int lists, boo
         side.tiles[s] = make_int2(-1, 0);
 }
 
-// fp16: the largest finite |g| and |v| (as bits, whose order is the numbers'), and from them the power of two for ds.
-__global__ void k_attention_clear(uint32_t *tops)
+// fp16 holds ds larger by a power of two of every column's own (a query's, a key's), which falls where a tile's largest
+// leaves the range: to between 2^10 and 2^11, so that few tiles pass 2^15 again.  Terms down to 2^-24 of a column's largest so keep
+// all their bits, whatever other rows, heads and lists hold.  Gives the factor by which x and the sums o have become smaller.
+constexpr float kFirstLift = 0x1p60f;  // products of two fp16 heads are less than 2^40
+template <int NR, int DT> __device__ inline float keep_in_range(recd_f32x16 &x, recd_f32x16 (&o)[DT])
 {
-    if (threadIdx.x < 2)
-        tops[threadIdx.x] = 0;
+    float top = fabsf(x[0]);
+#pragma unroll
+    for (int r = 1; r < NR; r++)
+        top = fmaxf(top, fabsf(x[r]));
+    top = fmaxf(top, __shfl_xor(top, 32));
+    const bool leaves = top > 0x1p15f && top < INFINITY;
+    if (!__any(leaves))
+        return 1.0f;
+    const float f = leaves ? __uint_as_float((264u << 23) - (__float_as_uint(top) & 0x7f800000u)) : 1.0f;
+#pragma unroll
+    for (int r = 0; r < NR; r++)
+        x[r] *= f;
+#pragma unroll
+    for (int t = 0; t < DT; t++)
+#pragma unroll
+        for (int r = 0; r < 16; r++)
+            o[t][r] *= f;
+    return f;
 }
 
-__global__ __launch_bounds__(256) void k_attention_tops(int64_t rows, int width, int64_t stride, const _Float16 *__restrict__ x,
-                                                        uint32_t *top)
-{
-    const int pieces = width / 8;
-    float t = 0.0f;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * pieces; i += (int64_t)gridDim.x * 256) {
-        float v[8];
-        recd_load16(x + i / pieces * stride + i % pieces * 8, v);
-        for (int e = 0; e < 8; e++)
-            t = fmaxf(t, fabsf(v[e]) < INFINITY ? fabsf(v[e]) : 0.0f);
-    }
-    for (int o = 32; o; o >>= 1)
-        t = fmaxf(t, __shfl_xor(t, o));
-    if ((threadIdx.x & 63) == 0 && t > 0.0f)
-        atomicMax(top, __float_as_uint(t));
-}
+// 1 / a power of two
+__device__ inline float inverse_power(float power) { return __uint_as_float((254u << 23) - __float_as_uint(power)); }
 
-// |ds / scale| <= 2 d max|g| max|v|: brought below 2^15
-__global__ void k_attention_lift(int d, const uint32_t *tops, float *lift)
+template <int DT> __device__ inline void scale_sums(recd_f32x16 (&o)[DT], float f)
 {
-    const float bound = 2.0f * (float)d * __uint_as_float(tops[0]) * __uint_as_float(tops[1]);
-    int e = 15;
-    if (bound > 0.0f && bound < INFINITY)
-        frexpf(bound, &e);
-    e = 15 - e;
-    *lift = ldexpf(1.0f, e > 60 ? 60 : e);
+#pragma unroll
+    for (int t = 0; t < DT; t++)
+#pragma unroll
+        for (int r = 0; r < 16; r++)
+            o[t][r] *= f;
 }
 
 // 32 query rows a wave, keys and values stream past.
@@ -946,7 +948,7 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
     const int H = a.G * a.group;
     const int64_t q_row = p.q0 + query;
     const float posf = (float)(p.pos0 + query);
-    const float lift = kHalf<T> ? *a.lift : 1.0f;
+    float lift = kHalf<T> ? kFirstLift : 1.0f;
     const float c = a.scale * kRecdLog2e;
     const Capped<T> capped(a.cap, CAP);
     const float to_cap = CAP ? 2.0f * kRecdLog2e * a.scale / a.cap : 0.0f;
@@ -1043,6 +1045,11 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
                 for (int r = 0; r < NR; r++)
                     s[r] = recd_score_row(r, 0) >= to ? 0.0f : s[r];
             }
+            if constexpr (kHalf<T>) {
+                const float f = keep_in_range<NR>(s, o);
+                lift *= f;
+                delta *= f;
+            }
 #pragma unroll
             for (int h = 0; h < NR / 8; h++) {
                 const Frag sf = recd_sums_frag<T>(s, h);
@@ -1061,6 +1068,8 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
         add_not_finite<false, T>(t0 > edge ? t0 * 32 : edge * 32, t1 * 32 < p.nk ? t1 * 32 : p.nk, a.d,
                                  [&](int j) { return keys + j * a.k_stride; }, [&](int j) { return j < lim; }, o, lane);
     }
+    if constexpr (kHalf<T>)
+        scale_sums<DT>(o, inverse_power(lift));
     if constexpr (PHASES > 1) {
         static_assert(sizeof(lds) >= 64 * 16 * DT * sizeof(float));
         join_sums<DT, PHASES>(o, reinterpret_cast<float *>(&lds), 0, phase, lane);
@@ -1068,8 +1077,7 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
     if (phase)
         return;
     if (there)
-        store_columns<T, DT>((T *)a.gq + q_row * a.gq_stride + (int64_t)h * a.d, o, (CAP ? 4.0f : 1.0f) * a.scale / lift, a.d,
-                             lane);
+        store_columns<T, DT>((T *)a.gq + q_row * a.gq_stride + (int64_t)h * a.d, o, (CAP ? 4.0f : 1.0f) * a.scale, a.d, lane);
 }
 
 // Keys stay, queries and their gradients stream past.  What a score needs of its row stands in LDS in the order of
@@ -1128,8 +1136,8 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
 #pragma unroll
     for (int d = 0; d < DT; d++)
         dk[d] = dv[d] = recd_f32x16{};
-    // probabilities are held 2^kLiftP larger, by their exponents; ds by that and, from dp on, the rest of its lift
-    const float lift = kHalf<T> ? *a.lift : 1.0f, lift_dp = lift * recd_exp2(-kLiftP<T>);
+    // probabilities are held 2^kLiftP larger, by their exponents; ds by that and the rest of its lift
+    float lift = kHalf<T> ? kFirstLift * 0x1p-15f : 1.0f;
     const float c = a.scale * kRecdLog2e;
     const Capped<T> capped(a.cap, CAP);
     const float to_cap = CAP ? 2.0f * kRecdLog2e * a.scale / a.cap : 0.0f;
@@ -1175,7 +1183,7 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
             const int in = query_of(tid), query = q_first + in, h = head * a.group + odd + tid - in * a.group;
             n_from = a.lse_in[(p.q0 + query) * H + h] * kRecdLog2e;
             n_from = (n_from == -INFINITY ? 0.0f : -n_from) + (kLiftP<T> + capped.base);
-            n_delta = a.delta[(p.q0 + query) * H + h] * lift_dp;
+            n_delta = a.delta[(p.q0 + query) * H + h];
             n_slope = a.slopes ? a.slopes[h] * kRecdLog2e : 0.0f;
             n_lim = p.limit_at(query);
             n_pos = (float)(p.pos0 + query);
@@ -1237,7 +1245,7 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
             float quarter = 1.0f;
             const float z = CAP ? capped.value(s[r] * to_cap, more, quarter) : s[r] * c + more;
             s[r] = recd_exp2(z);
-            dp[r] = s[r] * (dp[r] * lift_dp - delta) * quarter;
+            dp[r] = s[r] * (dp[r] - delta) * (kHalf<T> ? quarter * lift : quarter);
         };
         if (a.slopes) {
 #pragma unroll
@@ -1270,6 +1278,8 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
                 if (j >= row_lim[buf][sub + recd_sums_row(r, lane)])
                     s[r] = dp[r] = 0.0f;
         }
+        if constexpr (kHalf<T>)
+            lift *= keep_in_range<16>(dp, dk);
 #pragma unroll
         for (int h = 0; h < 2; h++) {
             const Frag pf = recd_sums_frag<T>(s, h), sf = recd_sums_frag<T>(dp, h);
@@ -1297,6 +1307,8 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
             add_not_finite<true, T>(s0, s1, a.d, at(a.g, (int64_t)H * a.d), sees, dv, lane);
         }
     }
+    if constexpr (kHalf<T>)
+        scale_sums<DT>(dk, inverse_power(lift) * 0x1p-15f);
     if constexpr (PHASES > 1) {
         static_assert(sizeof(lds) >= KEPT * 64 * 16 * DT * sizeof(float));
         join_sums<DT, PHASES>(dk, reinterpret_cast<float *>(&lds), kept, phase, lane);
@@ -1305,8 +1317,8 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
     if (phase)
         return;
     if (there) {
-        store_columns<T, DT>((T *)a.gk + (p.k0 + j) * a.gk_stride + (int64_t)head * a.d, dk, (CAP ? 4.0f : 1.0f) * a.scale / lift,
-                             a.d, lane);
+        store_columns<T, DT>((T *)a.gk + (p.k0 + j) * a.gk_stride + (int64_t)head * a.d, dk, (CAP ? 4.0f : 1.0f) * a.scale, a.d,
+                             lane);
         store_columns<T, DT>((T *)a.gv + (p.k0 + j) * a.gv_stride + (int64_t)head * a.d, dv, recd_exp2(-kLiftP<T>), a.d, lane);
     }
 }
@@ -1653,16 +1665,12 @@ recd_status recd_list_attention_backward(recd_ctx *ctx, const recd_attention *d,
     const Tiling tk = tiling(ctx, d, d->k_rows, d->max_k, 1, d->q_rows * a.group, d->max_q * a.group);
     if (tq.slots / 8 + 1 > ((int64_t)1 << 27) / a.G || tk.slots / 8 + 1 > ((int64_t)1 << 27) / a.G)
         return recd_fail(ctx, RECD_EINVAL, "too many tiles");
-    const bool half = d->dtype == RECD_F16;
     int2 *tiles_q, *tiles_k;
-    float *delta, *lift;
-    uint32_t *tops;
+    float *delta;
     auto carve = [&](WsCarver &c) {
         tiles_q = tq.table ? c.take<int2>(tq.slots) : nullptr;
         tiles_k = tk.table ? c.take<int2>(tk.slots) : nullptr;
         delta = c.take<float>(a.part_rows);
-        tops = half ? c.take<uint32_t>(2) : nullptr;
-        lift = half ? c.take<float>(1) : nullptr;
     };
     WsCarver size(nullptr);
     carve(size);
@@ -1671,18 +1679,7 @@ recd_status recd_list_attention_backward(recd_ctx *ctx, const recd_attention *d,
     WsCarver c(ctx->ws);
     carve(c);
     a.delta = delta;
-    a.lift = lift;
     hipStream_t st = ctx->stream;
-    if (half) {
-        hipLaunchKernelGGL(k_attention_clear, dim3(1), dim3(64), 0, st, tops);
-        if (d->q_rows)
-            hipLaunchKernelGGL(k_attention_tops, dim3((unsigned)ctx->num_cu), dim3(256), 0, st, d->q_rows * d->heads, a.d, a.d,
-                               (const _Float16 *)grad_out, tops);
-        if (d->k_rows)
-            hipLaunchKernelGGL(k_attention_tops, dim3((unsigned)ctx->num_cu), dim3(256), 0, st, d->k_rows, a.G * a.d, d->v_stride,
-                               (const _Float16 *)v, tops + 1);
-        hipLaunchKernelGGL(k_attention_lift, dim3(1), dim3(1), 0, st, a.d, tops, lift);
-    }
     Side sides[2];
     int listed = 0;
     if (tq.table)

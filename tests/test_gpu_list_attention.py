@@ -470,3 +470,60 @@ def test_an_overflow_costs_a_few_passes(ctx, dt, where):
     else:
         g[:] = float("inf")
     assert took() < 6 * clean + 0.2
+
+
+def scaled_rows(x, rows, by):
+    y = x.clone()
+    y[rows] = (y[rows].double() * by).to(y.dtype)
+    return y
+
+
+# (a wave to a tile, phases, groups)
+@pytest.mark.parametrize("lens,H,G,d", [([20, 45, 7], 2, 1, 32), ([150, 260, 40], 2, 1, 64), ([260] * 24, 8, 4, 128)])
+@pytest.mark.parametrize("where", ["both", "apart"])
+def test_fp16_gradients_of_lists_beside_much_larger_ones(ctx, lens, H, G, d, where):
+    """Values and gradients of one list (or of two) that are thousands of times as large leave the others' bits alone: each
+    list is held to the bound of its own data."""
+    o = offsets(lens)
+    K = int(o[-1])
+    q, k, v, g = du.rand((K, H, d), "f16", 1), du.rand((K, G, d), "f16", 2), du.rand((K, G, d), "f16", 3), du.rand((K, H, d), "f16", 4)
+    how = dict(scale=d ** -0.5, causal=True)
+    large = [1] if where == "both" else [0, 1]
+    v = scaled_rows(v, slice(int(o[1]), int(o[2])), 4000.0)
+    g = scaled_rows(g, slice(int(o[large[0]]), int(o[large[0] + 1])), 4000.0)
+    got = run(ctx, q, k, v, o, o, how, g)
+    for l in [l for l in range(len(lens)) if l != 1][:3]:
+        a, b = int(o[l]), int(o[l + 1])
+        ref = du.attention_ref(q[a:b], k[a:b], v[a:b], offsets([b - a]), offsets([b - a]), g=g[a:b], **how)
+        for n in ("grad_q", "grad_k", "grad_v"):
+            du.within(got[n][a:b], *ref[n], what=f"{n} of list {l}")
+
+
+@pytest.mark.parametrize("n,H,G,d", [(45, 2, 1, 32), (260, 2, 1, 64), (512, 1, 1, 128)])
+def test_fp16_gradients_before_a_large_last_row(ctx, n, H, G, d):
+    """Rows that do not see the last key keep the bits of their gradients, however large its value."""
+    o = offsets([n])
+    q, k, v, g = du.rand((n, H, d), "f16", 1), du.rand((n, G, d), "f16", 2), du.rand((n, G, d), "f16", 3), du.rand((n, H, d), "f16", 4)
+    how = dict(scale=d ** -0.5, causal=True)
+    ref = du.attention_ref(q[:-1], k[:-1], v[:-1], offsets([n - 1]), offsets([n - 1]), g=g[:-1], **how)
+    got = run(ctx, q, k, scaled_rows(v, slice(n - 1, n), 10_000.0), o, o, how, scaled_rows(g, slice(n - 1, n), 10_000.0))
+    du.within(got["grad_q"][:-1], *ref["grad_q"], what="grad_q")
+
+
+def test_fp16_gradients_of_rows_that_rise(ctx):
+    """Weights that grow along a list by 2^30 in all, small ones first and small ones last."""
+    n, d = 300, 64
+    o = offsets([n])
+    q, k, v = (du.rand((n, 1, d), "f16", s, 0.5) for s in (1, 2, 3))
+    how = dict(scale=0.125)
+    for up in (True, False):
+        size = 2.0 ** torch.linspace(-22, 8, n, dtype=torch.float64)
+        size = size if up else size.flip(0)
+        g = (du.rand((n, 1, d), "f16", 4).double() * size[:, None, None]).half()
+        ref = du.attention_ref(q, k, v, o, o, g=g, **how)
+        got = run(ctx, q, k, v, o, o, how, g)
+        for name in ("grad_q", "grad_k", "grad_v"):
+            du.within(got[name], *ref[name], what=name)
+        some = (g.double().abs().sum((1, 2)) > 0) & (size > 2.0 ** -10)
+        off = (got["grad_q"].double().cpu() - ref["grad_q"][0])[some].norm(dim=(1, 2)) / ref["grad_q"][0][some].norm(dim=(1, 2))
+        assert off.max() < 0.02      # every row to its own size (2^-11 in the operands, the output stored in 16 bits)
