@@ -541,7 +541,8 @@ __global__ __launch_bounds__(kBlock) void k_vocab_rows(int64_t n, int64_t V, int
         return;
     const int64_t t = targets[row];
     const bool has = t >= 0 && t < V;
-    const float g = has ? grad_loss[row] : 0.0f;
+    // (a row whose logits are not all numbers, or one of them infinite, has no gradient that is one)
+    const float g = !has ? 0.0f : fabsf(lse[row]) < INFINITY ? grad_loss[row] : NAN;
     if (lane == 0 && row_g) {
         row_lse[row] = has ? lse[row] * kRecdLog2e : INFINITY;
         row_g[row] = lift ? g * *lift : g;
@@ -576,6 +577,10 @@ struct TableGradArgs {
     int blocks;        // that share the work (groups of table rows times tiles of rows x) evenly
     float *parts;      // [2 * blocks][rows of a group][D]: sums of groups that several blocks share
 };
+
+// 2^x, and 0 for a NaN (the instruction's own clamp): a row without a target, which counts as zeros, has one as its score against a
+// table row that holds an infinity.  What a NaN in a score has to do it does by the row's weight.
+__device__ inline float probability(float x) { return __builtin_amdgcn_fmed3f(recd_exp2(x), 0.0f, 1.0f); }
 
 // The block that does unit `u` of the work.
 __host__ __device__ inline int64_t block_of(int64_t u, int64_t units, int64_t blocks) { return ((u + 1) * blocks - 1) / units; }
@@ -683,7 +688,7 @@ template <typename T, int DP, int N, int W, bool SHARED> __global__ __launch_bou
                     for (int e = 0; e < 8; e++) {
                         const int r = 8 * h + e, row = 32 * st + recd_sums_row(r, lane);
                         const bool hit = target[b][row] == v0 + 32 * j + (lane & 31);
-                        const float w = hit ? (recd_exp2(x[j][r] * a.c - lse[b][row]) - 1.0f) * g[b][row] : 0.0f;
+                        const float w = hit ? (probability(x[j][r] * a.c - lse[b][row]) - 1.0f) * g[b][row] : 0.0f;
                         x[j][r] = hit ? -INFINITY : x[j][r];
                         p[0][e] = (T)w;
                         p[1][e] = (T)(w - (float)p[0][e]);
@@ -733,7 +738,7 @@ template <typename T, int DP, int N, int W, bool SHARED> __global__ __launch_bou
                     for (int q = 0; q < 4; q++)
 #pragma unroll
                         for (int j = 0; j < N; j++)
-                            s[now][j][r + q] = recd_exp2(s[now][j][r + q] * a.c - from[q]) * by[q];
+                            s[now][j][r + q] = probability(s[now][j][r + q] * a.c - from[q]) * by[q];
                 }
 #pragma unroll
                 for (int h = 0; h < 2; h++) {

@@ -337,3 +337,41 @@ def test_rows_that_are_predicted_well(ctx, dt, n, scale):
     off = (got["grad_x"].double().cpu() - want).norm(dim=1)
     bound = u * want.norm(dim=1) + g * ((u * (left @ w.abs() + rest[:, None] * w[t].abs())).norm(dim=1) + (dz + 8 * du.E) * w[t].norm(dim=1))
     assert (off <= bound).all(), float((off / bound).max())
+
+
+def infinite_elements(ctx, dt, n, V, D, where):
+    """A table row that holds infinities at `where`, against rows that are positive there: its logits are -inf."""
+    x, table, t, gl = data(n, V, D, dt, 8)
+    x[:, where] = x[:, where].abs() + 0.1
+    t[t == 11] = 12
+    table[11, where] = -float("inf")
+    fine = table.clone()
+    fine[11, where] = -1000.0 if dt != "f32" else -1e6
+    ref = du.loss_ref(x, fine, t, 1.0, gl)
+    x, table, t, gl = (a.cuda() for a in (x, table, t, gl))
+    loss, lse = torch.empty(n, device="cuda"), torch.empty(n, device="cuda")
+    ctx.vocab_loss(x, table, t, 1.0, loss, lse)
+    du.within(loss, *ref["loss"], what="loss")
+    du.within(lse, *ref["lse"], what="lse")
+    gt = torch.empty_like(table)
+    ctx.vocab_loss_backward(x, table, t, 1.0, lse, None, gl, None, gt)
+    du.within(gt, *ref["grad_table"], what="grad_table")
+
+
+@pytest.mark.parametrize("dt", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("n,V,D", [(60, 400, 64), (300, 700, 128)])
+def test_infinite_elements_of_a_table_row(ctx, dt, n, V, D):
+    """Rows without a target leave such a row's gradient alone, too."""
+    infinite_elements(ctx, dt, n, V, D, slice(5, 8))
+
+
+@pytest.mark.parametrize("dt", ["f32", "f16", "bf16"])
+def test_a_row_with_a_target_that_is_not_finite(ctx, dt):
+    """What is wrong with a row that counts shows in its loss, its gradient and the table's."""
+    x, table, t, gl = data(200, 300, 64, dt, 8)
+    x[8, 2] = float("nan")
+    t[8] = 3
+    got, _ = run(ctx, x, table, t, 1.0, gl)
+    assert got["loss"][8].isnan() and got["grad_x"][8].isnan().all() and got["grad_table"].isnan().all()
+    others = torch.arange(200, device="cuda") != 8
+    assert got["loss"][others].isfinite().all() and got["grad_x"][others].isfinite().all()
