@@ -334,6 +334,11 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
     for (int d = 0; d < DT; d++)
         o[d] = recd_f32x16{};
     typename S::Load ks, vs;
+    if (a.d < DP)
+        for (int b = 0; b < BUFS; b++) {
+            ks.clear_behind(tid, kt[b], a.d);
+            vs.clear_behind(tid, vt[b], a.d);
+        }
     auto load = [&](int t) {
         const int64_t at = p.k0 + t * 32;
         ks.load_rows(tid, (const T *)a.k + at * a.k_stride + head * a.d, p.nk - t * 32, a.d, (uint32_t)a.k_stride * sizeof(T));
@@ -387,8 +392,8 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
     };
     bool odd = false;  // the wave's threads have seen what is not finite at the edge
     auto store = [&](int t, int b) {
-        ks.store(tid, kt[b]);
-        vs.store(tid, vt[b]);
+        ks.store(tid, kt[b], a.d);
+        vs.store(tid, vt[b], a.d);
         if (t >= edge && __any(vs.not_finite(tid))) {
             vt[b].make_finite(tid, S::LOADERS);  // (what the thread has stored itself)
             odd = true;
@@ -526,6 +531,10 @@ template <typename T, int DP, bool CAP> __global__ __launch_bounds__(64, (sizeof
     float slope = 0.0f, slope_n = 0.0f, m = -INFINITY, l = 0.0f;
     recd_f32x16 o[DT];
     typename S::Load ks, vs;
+    if (a.d < DP) {
+        ks.clear_behind(lane, kt, a.d);
+        vs.clear_behind(lane, vt, a.d);
+    }
     auto load_q = [&](int hd) {
         const int h = hd * a.group + head_in;
 #pragma unroll
@@ -578,8 +587,8 @@ template <typename T, int DP, bool CAP> __global__ __launch_bounds__(64, (sizeof
             write();
     for (int t = t0; t < t1;) {
         S::sync();
-        ks.store(lane, kt);
-        vs.store(lane, vt);
+        ks.store(lane, kt, a.d);
+        vs.store(lane, vt, a.d);
         const bool clear = __any(vs.not_finite(lane));
         S::sync();
         const bool last = t + 1 == t1, more = last && head + 1 < head_end;
@@ -981,6 +990,11 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
     for (int d = 0; d < DT; d++)
         o[d] = recd_f32x16{};
     typename S::Load ks, vs;
+    if (a.d < DP)
+        for (int b = 0; b < BUFS; b++) {
+            ks.clear_behind(tid, kt[b], a.d);
+            vs.clear_behind(tid, vt[b], a.d);
+        }
     auto load = [&](int t) {
         const int64_t at = p.k0 + t * 32;
         ks.load_rows(tid, (const T *)a.k + at * a.k_stride + head * a.d, p.nk - t * 32, a.d, (uint32_t)a.k_stride * sizeof(T));
@@ -993,8 +1007,8 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
         const int buf = BUFS == 1 ? 0 : t & 1;
         if constexpr (BUFS == 1)
             S::sync();
-        ks.store(tid, kt[buf]);
-        vs.store(tid, vt[buf]);
+        ks.store(tid, kt[buf], a.d);
+        vs.store(tid, vt[buf], a.d);
         const bool clear = t >= edge && any_wave<S::SHARED>(__any(ks.not_finite(tid)), says[t & 1], wave, lane);
         if (!S::SHARED || t < edge)
             S::sync();
@@ -1159,6 +1173,11 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
     auto at_edge = [&](int t) { return KEPT * PHASES == 1 || t * S::ROWS < whole_row || (t + 1) * S::ROWS > p.rows; };
     bool odd = false;  // something that is not finite in a tile at the edge
     typename S::Load qs, gs;
+    if (a.d < DP)
+        for (int b = 0; b < BUFS; b++) {
+            qs.clear_behind(tid, qt[b], a.d);
+            gs.clear_behind(tid, gt[b], a.d);
+        }
     float n_from = 0.0f, n_delta = 0.0f, n_slope = 0.0f;
     float n_pos = 0.0f;
     int n_lim = 0;
@@ -1195,8 +1214,8 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
         const int buf = BUFS == 1 ? 0 : t & 1;
         if constexpr (BUFS == 1)
             S::sync();
-        qs.store(tid, qt[buf]);
-        gs.store(tid, gt[buf]);
+        qs.store(tid, qt[buf], a.d);
+        gs.store(tid, gt[buf], a.d);
         if (tid < S::ROWS) {
             const int i = recd_product_row(tid);
             row_from[buf][i] = n_from;

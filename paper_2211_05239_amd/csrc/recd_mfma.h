@@ -133,10 +133,11 @@ template <typename T, int ROWS, int DP> struct RecdTile {
             return u.f;
         }
     }
+    __device__ inline void put_at(int row, int column, Piece v) { *reinterpret_cast<Piece *>(at + row * LD + column) = v; }
     __device__ inline void put(int piece, Piece v)
     {
         constexpr int PR = DP / E;
-        *reinterpret_cast<Piece *>(at + (piece / PR) * LD + (piece % PR) * E) = v;
+        put_at(piece / PR, piece % PR * E, v);
     }
     // zeros in the place of all that is not finite, by `threads` threads of which this is `tid`, each in the pieces that it puts
     __device__ inline void make_finite(int tid, int threads)
@@ -151,8 +152,9 @@ template <typename T, int ROWS, int DP> struct RecdTile {
 
 // Rows of a tile from memory into registers and on into LDS, by THREADS threads of which this is `tid`.  A thread's
 // addresses are 32-bit offsets from the tile's first row, which is the same for all: bytes(r) is that of row r < 128.  Rows
-// behind the last one and elements behind a head's last one are read from the last one's place instead: their
-// scores are masked, or meet zeros in the other operand, or belong to sums that nobody stores.
+// behind the last one and elements behind a row's last one are read from the last one's place instead.  The scores of such
+// rows are masked; such elements go to the padding behind a tile's rows, and zeros stand in their place (clear_behind), as in the
+// kept operand: an infinity against that one's zeros would turn the sum of the others into a NaN.
 template <typename T, int ROWS, int DP, int THREADS> struct RecdStream {
     using Tile = RecdTile<T, ROWS, DP>;
     using Piece = typename Tile::Piece;
@@ -188,12 +190,26 @@ template <typename T, int ROWS, int DP, int THREADS> struct RecdStream {
     }
     // the tile's row of a thread's piece i
     static __device__ inline int row(int tid, int i) { return (tid + i * THREADS) / (DP / Tile::E); }
-    __device__ inline void store(int tid, Tile &t)
+    __device__ inline void store(int tid, Tile &t, int d)
     {
 #pragma unroll
         for (int i = 0; i < PT; i++)
             if (tid + i * THREADS < Tile::PIECES)
-                t.put(tid + i * THREADS, held[i]);
+                t.put_at((tid + i * THREADS) / (DP / Tile::E), column(tid, i) < d ? column(tid, i) : DP, held[i]);
+    }
+    // zeros behind the rows' d elements, which stay there, in the places where the thread would put pieces
+    static __device__ inline void clear_behind(int tid, Tile &t, int d)
+    {
+#pragma unroll
+        for (int i = 0; i < PT; i++)
+            if (tid + i * THREADS < Tile::PIECES && column(tid, i) >= d)
+                t.put(tid + i * THREADS, Piece{});
+    }
+    // the first element of a thread's piece i
+    static __device__ inline int column(int tid, int i)
+    {
+        constexpr int PR = DP / Tile::E;
+        return (THREADS % PR == 0 ? tid : tid + i * THREADS) % PR * Tile::E;
     }
 };
 

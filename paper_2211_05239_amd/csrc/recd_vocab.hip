@@ -103,6 +103,8 @@ template <typename T, int DP, int N, bool MEAN> __global__ __launch_bounds__(kBl
             o[j][d] = recd_f32x16{};
     }
     RecdStream<T, 32, DP, 64> stream;
+    if (a.D < DP)
+        stream.clear_behind(lane, tile, a.D);
     auto load = [&](int64_t t) {
         const int64_t first = t * 128 + 32 * wave;
         if (first < a.V)
@@ -115,7 +117,7 @@ template <typename T, int DP, int N, bool MEAN> __global__ __launch_bounds__(kBl
         if (left <= 0)
             break;
         recd_wave_sync();
-        stream.store(lane, tile);
+        stream.store(lane, tile, a.D);
         recd_wave_sync();
         if (t + 1 < t1)
             load(t + 1);
@@ -334,12 +336,15 @@ __global__ __launch_bounds__(64 * W) void k_vocab_forward(ForwardArgs a)
             }
     };
     RecdStream<T, VT, DP, 64 * W> stream;
+    if (a.D < DP)
+        for (auto &tile : tiles_lds)
+            stream.clear_behind(threadIdx.x, tile, a.D);
     auto load = [&](int64_t t) {
         stream.load_rows(threadIdx.x, (const T *)a.table + t * VT * a.D, rows_left(a.V - t * VT), a.D, a.D * sizeof(T));
     };
     if (t0 < t1) {
         load(t0);
-        stream.store(threadIdx.x, tiles_lds[0]);
+        stream.store(threadIdx.x, tiles_lds[0], a.D);
         if (t0 + 1 < t1)
             load(t0 + 1);
         __syncthreads();
@@ -350,7 +355,7 @@ __global__ __launch_bounds__(64 * W) void k_vocab_forward(ForwardArgs a)
     for (int64_t t = t0; t < t1; t++) {
         const int next = buf + 1 == BUFS ? 0 : buf + 1;
         if (t + 1 < t1) {
-            stream.store(threadIdx.x, tiles_lds[next]);
+            stream.store(threadIdx.x, tiles_lds[next], a.D);
             if (t + 2 < t1)
                 load(t + 2);
         }
@@ -603,6 +608,9 @@ template <typename T, int DP, int N, int W, bool SHARED> __global__ __launch_bou
     Frag wf[N][KS];
     recd_f32x16 o[N][DT], s[2][N];
     RecdStream<T, XT, DP, 64 * W> stream;
+    if (a.D < DP)
+        for (auto &tile : tiles_lds)
+            stream.clear_behind(threadIdx.x, tile, a.D);
     float next_lse = 0.0f, next_g = 0.0f;
     int32_t next_t = -1, piece_t[decltype(stream)::PT];
     auto load = [&](int t) {
@@ -624,7 +632,7 @@ template <typename T, int DP, int N, int W, bool SHARED> __global__ __launch_bou
 #pragma unroll
         for (int i = 0; i < decltype(stream)::PT; i++)
             stream.held[i] = piece_t[i] < 0 ? typename decltype(stream)::Piece{} : stream.held[i];
-        stream.store(threadIdx.x, tiles_lds[b]);
+        stream.store(threadIdx.x, tiles_lds[b], a.D);
         if (threadIdx.x < XT) {
             const int i = recd_product_row(threadIdx.x);  // a lane reads those of four neighbouring sums at a time
             lse[b][i] = next_lse;

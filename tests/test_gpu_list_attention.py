@@ -527,3 +527,32 @@ def test_fp16_gradients_of_rows_that_rise(ctx):
         some = (g.double().abs().sum((1, 2)) > 0) & (size > 2.0 ** -10)
         off = (got["grad_q"].double().cpu() - ref["grad_q"][0])[some].norm(dim=(1, 2)) / ref["grad_q"][0][some].norm(dim=(1, 2))
         assert off.max() < 0.02      # every row to its own size (2^-11 in the operands, the output stored in 16 bits)
+
+
+@pytest.mark.parametrize("dt", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("name", list(PLANTED))
+@pytest.mark.parametrize("d,softcap", [(24, 0.0), (40, 0.0), (40, 5.0), (80, 0.0)])
+def test_an_infinite_last_element_of_a_head(ctx, dt, name, d, softcap):
+    """A key whose last elements are infinite, against queries that are positive there, scores -inf (capped: -cap), however
+    much wider than the head a tile is: it has no weight, and no part in the others' gradients."""
+    lq, lk, H, G = PLANTED[name]
+    if name == "groups" and d != 80:
+        H, G = 4, 4
+    qo, ko = offsets(lq), offsets(lk)
+    Q, K = int(qo[-1]), int(ko[-1])
+    q, k, v, g = du.rand((Q, H, d), dt, 1), du.rand((K, G, d), dt, 2), du.rand((K, G, d), dt, 3), du.rand((Q, H, d), dt, 4)
+    j = int(ko[1]) + lk[1] // 2
+    q[..., -3:] = q[..., -3:].abs() + 0.1
+    k[j, :, -3:] = -float("inf")
+    got = run(ctx, q, k, v, qo, ko, dict(scale=d ** -0.5, softcap=softcap), g)
+    fine = k.clone()
+    fine[j, :, -3:] = -1000.0 if dt != "f32" else -1e6   # next to no weight
+    ref = du.attention_ref(q, fine, v, qo, ko, scale=d ** -0.5, softcap=softcap, g=g)
+    for n in ("out", "lse"):
+        du.within(got[n], *ref[n], what=n)
+    if not softcap:      # (the stand-in's weight is 1e-14 and less, the infinity's none)
+        assert not got["grad_k"][j].any() and not got["grad_v"][j].any()
+    others = torch.ones(K, dtype=torch.bool)
+    others[j] = False
+    for n in ("grad_k", "grad_v"):
+        du.within(got[n][others.cuda()], ref[n][0][others], ref[n][1][others], what=n)

@@ -375,3 +375,10 @@ def test_a_row_with_a_target_that_is_not_finite(ctx, dt):
     assert got["loss"][8].isnan() and got["grad_x"][8].isnan().all() and got["grad_table"].isnan().all()
     others = torch.arange(200, device="cuda") != 8
     assert got["loss"][others].isfinite().all() and got["grad_x"][others].isfinite().all()
+
+
+@pytest.mark.parametrize("dt", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("n,V,D", [(60, 400, 40), (300, 700, 72), (300, 500, 200)])
+def test_infinite_last_elements_of_a_table_row(ctx, dt, n, V, D):
+    """However much wider than the row a tile is."""
+    infinite_elements(ctx, dt, n, V, D, slice(-3, None))
