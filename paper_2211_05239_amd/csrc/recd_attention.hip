@@ -176,20 +176,19 @@ template <int DT, int PHASES> __device__ inline void join_sums(recd_f32x16 (&o)[
 }
 
 // cap * log2(e) * tanh(x) + (more - base) from x' = 2 log2(e) x, and a quarter of the derivative, (1 - tanh^2) / 4.
-// tanh(x) = 1 - 2 r with r = 1 / (1 + e^2x), off by 2^-23 wherever x lies.  That is enough beside 16-bit operands, where the
-// caller's `more` also brings the 1 along (base = cap * log2(e)).  For fp32 small x take Lambert's continued fraction,
-// x (945 + 105 x^2 + x^4) / (945 + 420 x^2 + 15 x^4), off by 2e-9 of x at 1/2.
-template <typename T> struct Capped {
+// tanh(x) = 1 - 2 r with r = 1 / (1 + e^2x), off by 2^-23 wherever x lies, and the score by 2^-22 of the cap.  That is enough
+// beside 16-bit operands for caps up to 256 (6e-5), where the caller's `more` also brings the 1 along (base = cap * log2(e)).
+// Elsewhere (WIDE) small x take Lambert's continued fraction, x (945 + 105 x^2 + x^4) / (945 + 420 x^2 + 15 x^4), off by 2e-9 of
+// x at 1/2: a score far below its cap keeps all its bits.
+enum Cap { NO_CAP, CAP_16, CAP_WIDE };
+template <int CAP> struct Capped {
     float cap, cap_n2, base;  // cap * log2(e), -2 times that, and what `more` has to hold besides
-    __device__ inline Capped(float c, bool used)
-        : cap(c * kRecdLog2e), cap_n2(-2.0f * c * kRecdLog2e), base(used && sizeof(T) == 2 ? c * kRecdLog2e : 0.0f)
-    {
-    }
+    __device__ inline Capped(float c) : cap(c * kRecdLog2e), cap_n2(-2.0f * c * kRecdLog2e), base(CAP == CAP_16 ? c * kRecdLog2e : 0.0f) {}
     __device__ inline float value(float x2, float more, float &quarter) const
     {
         const float r = __builtin_amdgcn_rcpf(1.0f + recd_exp2(x2));
         quarter = r - r * r;
-        if constexpr (sizeof(T) == 4) {
+        if constexpr (CAP == CAP_WIDE) {
             const float x = x2 * (0.5f * kRecdLn2), y = x * x;
             float t = 1.0f - 2.0f * r;
             if (fabsf(x) < 0.5f)
@@ -272,7 +271,7 @@ template <typename T, int DP, int KEPT> constexpr int kResident = (sizeof(T) == 
 // current one's sums while the current scores become exponentials.  The caps, biases and masks of the next scores, and
 // the check of the running maximum, stand behind it.  Three buffers in LDS make it one barrier a turn; waves that stream for
 // themselves need two and none.
-template <typename T, int DP, int KEPT, int PHASES, bool CAP>
+template <typename T, int DP, int KEPT, int PHASES, int CAP>
 __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void k_attention(Args a)
 {
     using S = Shape<T, DP, KEPT, PHASES>;
@@ -317,7 +316,7 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
     const float scale = fabsf(a.scale), c = scale * kRecdLog2e;
     const bool plain = !CAP && !a.slopes && c > 0.0f;
     const float by = plain ? c : 1.0f;
-    const Capped<T> capped(a.cap, CAP);
+    const Capped<CAP> capped(a.cap);
     const float to_cap = CAP ? 2.0f * kRecdLog2e * scale / a.cap : 0.0f;
 
     Frag qf[KS];
@@ -500,7 +499,7 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
 
 // The forward kernel for lists of few rows: a wave to itself goes through one head after the other, whose rows are on
 // their way while it works at the one before, so that a wave finds its list once for all of them.
-template <typename T, int DP, bool CAP> __global__ __launch_bounds__(64, (sizeof(T) == 2 && DP <= 32 ? 4 : kResident<T, DP, 1>)) void k_attention_one(Args a)
+template <typename T, int DP, int CAP> __global__ __launch_bounds__(64, (sizeof(T) == 2 && DP <= 32 ? 4 : kResident<T, DP, 1>)) void k_attention_one(Args a)
 {
     constexpr int KS = DP / 16, DT = DP / 32;
     using Mma = RecdMma<T>;
@@ -525,7 +524,7 @@ template <typename T, int DP, bool CAP> __global__ __launch_bounds__(64, (sizeof
     const int64_t q_row = p.q0 + query;
     const float posf = (float)(p.pos0 + query);
     const float c = a.scale * kRecdLog2e;
-    const Capped<T> capped(a.cap, CAP);
+    const Capped<CAP> capped(a.cap);
     const float to_cap = CAP ? 2.0f * kRecdLog2e * a.scale / a.cap : 0.0f;
     Frag qf[KS], qn[KS];
     float slope = 0.0f, slope_n = 0.0f, m = -INFINITY, l = 0.0f;
@@ -920,7 +919,7 @@ template <int DT> __device__ inline void scale_sums(recd_f32x16 (&o)[DT], float 
 }
 
 // 32 query rows a wave, keys and values stream past.
-template <typename T, int DP, int KEPT, int PHASES, bool CAP>
+template <typename T, int DP, int KEPT, int PHASES, int CAP>
 __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void k_attention_grad_q(Args a)
 {
     using S = Shape<T, DP, KEPT, PHASES>;
@@ -959,7 +958,7 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
     const float posf = (float)(p.pos0 + query);
     float lift = kHalf<T> ? kFirstLift : 1.0f;
     const float c = a.scale * kRecdLog2e;
-    const Capped<T> capped(a.cap, CAP);
+    const Capped<CAP> capped(a.cap);
     const float to_cap = CAP ? 2.0f * kRecdLog2e * a.scale / a.cap : 0.0f;
 
     // delta = g . o, which the gradients by keys need too
@@ -1096,7 +1095,7 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
 
 // Keys stay, queries and their gradients stream past.  What a score needs of its row stands in LDS in the order of
 // the sums' registers: four neighbours are read at a time.
-template <typename T, int DP, int KEPT, int PHASES, bool CAP>
+template <typename T, int DP, int KEPT, int PHASES, int CAP>
 __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void k_attention_grad_kv(Args a)
 {
     using S = Shape<T, DP, KEPT, PHASES>;
@@ -1153,7 +1152,7 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
     // probabilities are held 2^kLiftP larger, by their exponents; ds by that and the rest of its lift
     float lift = kHalf<T> ? kFirstLift * 0x1p-15f : 1.0f;
     const float c = a.scale * kRecdLog2e;
-    const Capped<T> capped(a.cap, CAP);
+    const Capped<CAP> capped(a.cap);
     const float to_cap = CAP ? 2.0f * kRecdLog2e * a.scale / a.cap : 0.0f;
     // the first row that sees the block's first key
     int from_row = 0;
@@ -1515,7 +1514,7 @@ int heads_at_once(const recd_ctx *ctx, const Tiling &t, int G, int64_t lists)
 }
 
 
-template <typename T, int DP, bool CAP> void launch_one(Which w, const Args &a, Division v, hipStream_t st)
+template <typename T, int DP, int CAP> void launch_one(Which w, const Args &a, Division v, hipStream_t st)
 {
     constexpr int KV = sizeof(T) == 2 && DP > 64 ? 2 : 1;
     constexpr bool WIDE = sizeof(T) == 4 && DP > 64;
@@ -1552,7 +1551,12 @@ template <typename T, int DP, bool CAP> void launch_one(Which w, const Args &a, 
 
 template <typename T, int DP> void launch_width(Which w, const Args &a, Division v, hipStream_t st)
 {
-    a.cap != 0.0f ? launch_one<T, DP, true>(w, a, v, st) : launch_one<T, DP, false>(w, a, v, st);
+    if (a.cap == 0.0f)
+        launch_one<T, DP, NO_CAP>(w, a, v, st);
+    else if (sizeof(T) == 4 || a.cap > 256.0f)
+        launch_one<T, DP, CAP_WIDE>(w, a, v, st);
+    else
+        launch_one<T, DP, sizeof(T) == 2 ? CAP_16 : CAP_WIDE>(w, a, v, st);
 }
 
 template <typename T> void launch(Which w, const Args &a, Division v, hipStream_t st)

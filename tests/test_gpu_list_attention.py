@@ -556,3 +556,18 @@ def test_an_infinite_last_element_of_a_head(ctx, dt, name, d, softcap):
     others[j] = False
     for n in ("grad_k", "grad_v"):
         du.within(got[n][others.cuda()], ref[n][0][others], ref[n][1][others], what=n)
+
+
+@pytest.mark.parametrize("dt", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("name", list(PLANTED))
+def test_a_cap_far_above_the_scores_changes_nothing(ctx, dt, name):
+    """cap * tanh(z / cap) is z where cap is large (by z^3 / 3 cap^2, 1e-11 here): no accuracy goes with the cap's size."""
+    lq, lk, H, G = PLANTED[name]
+    d = 64
+    qo, ko = offsets(lq), offsets(lk)
+    q, k, v, g = (du.rand((n, h, d), dt, s) for s, (n, h) in enumerate(((int(qo[-1]), H), (int(ko[-1]), G), (int(ko[-1]), G), (int(qo[-1]), H))))
+    how = dict(scale=d ** -0.5, causal=True)
+    ref = du.attention_ref(q, k, v, qo, ko, g=g, **how)
+    got = run(ctx, q, k, v, qo, ko, dict(how, softcap=2.0 ** 22), g)
+    for n, t in got.items():
+        du.within(t, *ref[n], what=n)
