@@ -311,7 +311,7 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
     const int H = a.G * a.group;
     const int64_t q_row = p.q0 + query, at_row = q_row * H + head * a.group + head_in;
     const float slope = a.slopes && there ? a.slopes[head * a.group + head_in] * kRecdLog2e : 0.0f;
-    const float posf = (float)(p.pos0 + query);
+    const int pos = p.pos0 + query;
     // the sign of the scale goes into the queries; what is neither capped nor biased stays unscaled until the exponent
     const float scale = fabsf(a.scale), c = scale * kRecdLog2e;
     const bool plain = !CAP && !a.slopes && c > 0.0f;
@@ -351,7 +351,7 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
     };
     auto settle = [&](int j0, recd_f32x16 &x) {
         if (a.slopes) {
-            const float far = posf - (float)(j0 + (lane >> 5));
+            const float far = (float)(pos - j0 - (lane >> 5));  // (whole numbers: positions may pass 2^24)
 #pragma unroll
             for (int r = 0; r < 16; r++) {
                 const float bias = capped.base - slope * fabsf(far - (float)recd_score_row(r, 0));
@@ -522,7 +522,7 @@ template <typename T, int DP, int CAP> __global__ __launch_bounds__(64, (sizeof(
     const int t0 = split * each < tiles ? split * each : tiles, t1 = t0 + each < tiles ? t0 + each : tiles;
     const int H = a.G * a.group;
     const int64_t q_row = p.q0 + query;
-    const float posf = (float)(p.pos0 + query);
+    const int pos = p.pos0 + query;
     const float c = a.scale * kRecdLog2e;
     const Capped<CAP> capped(a.cap);
     const float to_cap = CAP ? 2.0f * kRecdLog2e * a.scale / a.cap : 0.0f;
@@ -608,7 +608,7 @@ template <typename T, int DP, int CAP> __global__ __launch_bounds__(64, (sizeof(
         auto finish = [&](auto registers) {
             constexpr int NR = registers.value;
             if (a.slopes) {
-                const float far = posf - (float)(j0 + (lane >> 5));
+                const float far = (float)(pos - j0 - (lane >> 5));  // (whole numbers: positions may pass 2^24)
 #pragma unroll
                 for (int r = 0; r < NR; r++) {
                     const float bias = capped.base - slope * fabsf(far - (float)recd_score_row(r, 0));
@@ -955,7 +955,7 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
     const int edge = ONE ? 0 : p.limit(first, a.group) / 32;
     const int H = a.G * a.group;
     const int64_t q_row = p.q0 + query;
-    const float posf = (float)(p.pos0 + query);
+    const int pos = p.pos0 + query;
     float lift = kHalf<T> ? kFirstLift : 1.0f;
     const float c = a.scale * kRecdLog2e;
     const Capped<CAP> capped(a.cap);
@@ -1042,7 +1042,7 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
         auto finish = [&](auto registers) {
             constexpr int NR = registers.value;
             if (a.slopes) {
-                const float far = posf - (float)(j0 + (lane >> 5));
+                const float far = (float)(pos - j0 - (lane >> 5));  // (whole numbers: positions may pass 2^24)
 #pragma unroll
                 for (int r = 0; r < NR; r++)
                     s[r] = ds_of(s[r], dp[r], from - slope * fabsf(far - (float)recd_score_row(r, 0)));
@@ -1129,7 +1129,7 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
         return;
     const int j0 = first + 32 * kept, j = j0 + (lane & 31);
     const bool there = j < p.nk;
-    const float jf = (float)j;
+    const float jf = (float)(j - first);  // positions count from the block's first key, as whole numbers may pass 2^24
     const int H = a.G * a.group;
     Frag kf[IN_LDS ? 1 : KS], vf[IN_LDS ? 1 : KS];
     const int kept_at = IN_LDS ? (32 * kept + (lane & 31)) * lds.k.LD + (lane >> 5) * 8 : 0;
@@ -1204,7 +1204,7 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
             n_delta = a.delta[(p.q0 + query) * H + h];
             n_slope = a.slopes ? a.slopes[h] * kRecdLog2e : 0.0f;
             n_lim = p.limit_at(query);
-            n_pos = (float)(p.pos0 + query);
+            n_pos = (float)(p.pos0 + query - first);
         }
     };
     if (t0 < t1)

@@ -571,3 +571,20 @@ def test_a_cap_far_above_the_scores_changes_nothing(ctx, dt, name):
     got = run(ctx, q, k, v, qo, ko, dict(how, softcap=2.0 ** 22), g)
     for n, t in got.items():
         du.within(t, *ref[n], what=n)
+
+
+@pytest.mark.parametrize("causal", [False, True])
+def test_distances_beyond_2_to_24(ctx, causal):
+    """Positions that fp32 does not hold: the last queries of a list of 2^24 + 101 rows see their neighbours at exact distances."""
+    n, tail, d = 2 ** 24 + 101, 400, 8
+    k, v = (torch.zeros(n, 1, d, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    kt, vt = du.rand((tail, 1, d), "bf16", 1), du.rand((tail, 1, d), "bf16", 2)
+    k[-tail:], v[-tail:] = kt.cuda(), vt.cuda()
+    q, g = du.rand((5, 1, d), "bf16", 3), du.rand((5, 1, d), "bf16", 4)
+    how = dict(scale=0.3, slopes=torch.tensor([0.5]), causal=causal)
+    ref = du.attention_ref(q, kt, vt, offsets([5]), offsets([tail]), g=g, **how)   # (beyond the tail exp(-200))
+    got = run(ctx, q, k, v, offsets([5]), offsets([n]), how, g)
+    for name in ("out", "lse", "grad_q"):
+        du.within(got[name], *ref[name], what=name)
+    for name in ("grad_k", "grad_v"):
+        du.within(got[name][-tail:], *ref[name], what=name)
