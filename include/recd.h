@@ -101,6 +101,7 @@ typedef enum {
 #define RECD_MAX_ROW_BYTES 4096
 /* Largest row, in elements, of calls 29 and 30, and largest head of calls 31 and 32. */
 #define RECD_MAX_DENSE_D 256
+#define RECD_MAX_VOCAB 2147483136LL  /* and most rows of the table of calls 29 and 30 */
 #define RECD_MAX_HEAD_DIM 128
 
 /* Create a context bound to `device` and to `hip_stream` (a hipStream_t passed as void*; NULL =
@@ -595,7 +596,8 @@ recd_status recd_layer_norm_backward(recd_ctx *ctx, int64_t n, int D, recd_dtype
                                      float *grad_bias);
 
 /* 29. Softmax cross entropy of rows x [n, D] against the V rows of a table as the vocabulary; the logits
- *     z[i, v] = scale * <x_i, table_v> are never stored (scale: not 0).  D at most RECD_MAX_DENSE_D; V and n below 2^31.
+ *     z[i, v] = scale * <x_i, table_v> are never stored (scale: not 0).  D at most RECD_MAX_DENSE_D, V at most
+ *     RECD_MAX_VOCAB, n below 2^31.
  *     targets: device int64 [n], a row of the table each; a negative one marks a row without a target (loss 0, no
  *     gradients, and its elements and its grad_loss reach no other row's and not the table's).  So does one of V and
  *     more, unless RECD_OPT_VALIDATE is set (RECD_EBOUNDS).

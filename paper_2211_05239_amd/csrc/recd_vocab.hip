@@ -47,6 +47,9 @@ template <typename T, int DP> constexpr int kFewTiles = sizeof(T) == 4 || DP > 1
 // Rows of a tile that are there, of `left` behind its first.
 __device__ inline int rows_left(int64_t left) { return left < 128 ? (int)left : 128; }
 
+// Rows of x that a launch goes through: one holds less than 2^32 threads.
+__host__ inline int64_t most_at_once(int64_t n) { return n < (int64_t)1 << 24 ? n : (int64_t)1 << 24; }
+
 struct ForwardArgs {
     int64_t n, V;
     int D;
@@ -531,7 +534,7 @@ __global__ __launch_bounds__(1024) void k_vocab_lift(int64_t n, int64_t V, const
 }
 
 // What the table's gradient needs of a row (its lse in powers of two, its weight, its target), and the gradient by the row:
-// a wave per row.
+// a wave per row, and rows in turns beyond what a launch takes.
 template <typename T>
 __global__ __launch_bounds__(kBlock) void k_vocab_rows(int64_t n, int64_t V, int D, float scale, const T *__restrict__ table,
                                                        const int64_t *__restrict__ targets, const float *__restrict__ lse,
@@ -541,32 +544,31 @@ __global__ __launch_bounds__(kBlock) void k_vocab_rows(int64_t n, int64_t V, int
 {
     constexpr int E = 16 / sizeof(T);
     const int lane = threadIdx.x & 63;
-    const int64_t row = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6);
-    if (row >= n)
-        return;
-    const int64_t t = targets[row];
-    const bool has = t >= 0 && t < V;
-    // (a row whose logits are not all numbers, or one of them infinite, has no gradient that is one)
-    const float g = !has ? 0.0f : fabsf(lse[row]) < INFINITY ? grad_loss[row] : NAN;
-    if (lane == 0 && row_g) {
-        row_lse[row] = has ? lse[row] * kRecdLog2e : INFINITY;
-        row_g[row] = lift ? g * *lift : g;
-        row_t[row] = has ? (int32_t)t : -1;
-    }
-    if (!grad_x)
-        return;
-    for (int v = lane; v < D / E; v += 64) {
-        float a[E], b[E];
-        for (int e = 0; e < E; e++)
-            a[e] = b[e] = 0.0f;
-        if (has) {
-            recd_load16(table + t * D + v * E, b);
-            for (int e = 0; e < E; e++)
-                a[e] = mean_row[row * D + v * E + e];
+    for (int64_t row = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6); row < n; row += (int64_t)gridDim.x * kWaves) {
+        const int64_t t = targets[row];
+        const bool has = t >= 0 && t < V;
+        // (a row whose logits are not all numbers, or one of them infinite, has no gradient that is one)
+        const float g = !has ? 0.0f : fabsf(lse[row]) < INFINITY ? grad_loss[row] : NAN;
+        if (lane == 0 && row_g) {
+            row_lse[row] = has ? lse[row] * kRecdLog2e : INFINITY;
+            row_g[row] = lift ? g * *lift : g;
+            row_t[row] = has ? (int32_t)t : -1;
         }
-        for (int e = 0; e < E; e++)
-            a[e] = scale * g * (a[e] - b[e]);
-        recd_store16(grad_x + row * D + v * E, a);
+        if (!grad_x)
+            continue;
+        for (int v = lane; v < D / E; v += 64) {
+            float a[E], b[E];
+            for (int e = 0; e < E; e++)
+                a[e] = b[e] = 0.0f;
+            if (has) {
+                recd_load16(table + t * D + v * E, b);
+                for (int e = 0; e < E; e++)
+                    a[e] = mean_row[row * D + v * E + e];
+            }
+            for (int e = 0; e < E; e++)
+                a[e] = scale * g * (a[e] - b[e]);
+            recd_store16(grad_x + row * D + v * E, a);
+        }
     }
 }
 
@@ -833,8 +835,9 @@ recd_status check_vocab(recd_ctx *ctx, int64_t n, int64_t V, int D, recd_dtype d
 {
     if (!ctx)
         return RECD_EINVAL;
-    if (n < 0 || V < 0 || V > ((int64_t)1 << 31) - 1 || n > ((int64_t)1 << 31) - 1)
-        return recd_fail(ctx, RECD_EINVAL, "n=%lld or V=%lld outside [0, 2^31)", (long long)n, (long long)V);
+    if (n < 0 || V < 0 || V > RECD_MAX_VOCAB || n > ((int64_t)1 << 31) - 1)
+        return recd_fail(ctx, RECD_EINVAL, "n=%lld outside [0, 2^31) or V=%lld outside [0, %lld]", (long long)n, (long long)V,
+                         (long long)RECD_MAX_VOCAB);
     if ((int)dt < 0 || (int)dt > 2)
         return recd_fail(ctx, RECD_EINVAL, "unknown dtype");
     if (!(fabsf(scale) > 0.0f) || !(fabsf(scale) < INFINITY))
@@ -996,26 +999,31 @@ recd_status recd_vocab_loss(recd_ctx *ctx, int64_t n, int64_t V, int D, recd_dty
     RECD_HIP(ctx, hipSetDevice(ctx->device));
     if (ctx->validate)
         RECD_TRY(validate_targets(ctx, n, V, targets));
-    const ForwardShape s = forward_shape(ctx, n, V, D, dt, mean_row != nullptr);
-    WsCarver size(nullptr);
-    auto carve = [&](WsCarver &c, ForwardArgs &a) {
-        a.part_m = c.take<float>((size_t)s.splits * n);
-        a.part_l = c.take<float>((size_t)s.splits * n);
-        a.part_o = mean_row ? c.take<float>((size_t)s.splits * n * D) : nullptr;
-    };
-    ForwardArgs a{n, V, D, fabsf(scale) * kRecdLog2e, scale < 0, x, table, s.row_blocks, s.splits, s.tiles_per_split};
-    carve(size, a);
     ctx->plan.valid = false;  // the parts overwrite the workspace a backward plan would live in
-    RECD_TRY(recd_reserve(ctx, size.off));
-    WsCarver c(ctx->ws);
-    carve(c, a);
-    recd_with_type(dt, [&](auto t) {
-        using T = decltype(t);
-        with_width(D, [&](auto w) { launch_forward<T, w.value>(a, s.share, ctx->stream); });
-        hipLaunchKernelGGL((k_vocab_join<T>), dim3((unsigned)((n + kWaves - 1) / kWaves)), dim3(kBlock), 0, ctx->stream, n, V,
-                           D, scale, s.splits, a.part_m, a.part_l, a.part_o, (const T *)x, (const T *)table, targets, loss,
-                           lse, mean_row);
-    });
+    const int64_t most = most_at_once(n);
+    for (int64_t at = 0; at < n; at += most) {
+        const int64_t rows = n - at < most ? n - at : most;
+        const void *part_x = (const char *)x + at * D * (int64_t)elem_size(dt);
+        const ForwardShape s = forward_shape(ctx, rows, V, D, dt, mean_row != nullptr);
+        ForwardArgs a{rows, V, D, fabsf(scale) * kRecdLog2e, scale < 0, part_x, table, s.row_blocks, s.splits, s.tiles_per_split};
+        auto carve = [&](WsCarver &c) {
+            a.part_m = c.take<float>((size_t)s.splits * rows);
+            a.part_l = c.take<float>((size_t)s.splits * rows);
+            a.part_o = mean_row ? c.take<float>((size_t)s.splits * rows * D) : nullptr;
+        };
+        WsCarver size(nullptr);
+        carve(size);
+        RECD_TRY(recd_reserve(ctx, size.off));
+        WsCarver c(ctx->ws);
+        carve(c);
+        recd_with_type(dt, [&](auto t) {
+            using T = decltype(t);
+            with_width(D, [&](auto w) { launch_forward<T, w.value>(a, s.share, ctx->stream); });
+            hipLaunchKernelGGL((k_vocab_join<T>), dim3((unsigned)((rows + kWaves - 1) / kWaves)), dim3(kBlock), 0, ctx->stream, rows,
+                               V, D, scale, s.splits, a.part_m, a.part_l, a.part_o, (const T *)part_x, (const T *)table,
+                               targets + at, loss + at, lse + at, mean_row ? mean_row + at * D : nullptr);
+        });
+    }
     RECD_HIP(ctx, hipGetLastError());
     return RECD_OK;
 }
@@ -1062,7 +1070,7 @@ recd_status recd_vocab_loss_backward(recd_ctx *ctx, int64_t n, int64_t V, int D,
     recd_with_type(dt, [&](auto t) {
         using T = decltype(t);
         if (n > 0)
-            hipLaunchKernelGGL((k_vocab_rows<T>), dim3((unsigned)((n + kWaves - 1) / kWaves)), dim3(kBlock), 0, ctx->stream, n,
+            hipLaunchKernelGGL((k_vocab_rows<T>), dim3((unsigned)((most_at_once(n) + kWaves - 1) / kWaves)), dim3(kBlock), 0, ctx->stream, n,
                                V, D, scale, (const T *)table, targets, lse, mean_row, grad_loss, lift, row_lse, row_g, row_t,
                                (T *)grad_x);
         if (!grad_table)

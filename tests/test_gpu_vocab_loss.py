@@ -382,3 +382,43 @@ def test_a_row_with_a_target_that_is_not_finite(ctx, dt):
 def test_infinite_last_elements_of_a_table_row(ctx, dt, n, V, D):
     """However much wider than the row a tile is."""
     infinite_elements(ctx, dt, n, V, D, slice(-3, None))
+
+
+def test_more_rows_than_a_launch_holds(ctx):
+    """2^26 rows and a few: 2^32 threads, at 64 a row, are more than one launch takes."""
+    n, V, D = (1 << 26) + 5, 33, 8
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(3)
+    x = torch.empty(n, D, dtype=torch.bfloat16, device="cuda").normal_(generator=gen)
+    t = torch.randint(-3, V, (n,), device="cuda", generator=gen)
+    table = du.rand((V, D), "bf16", 2).cuda()
+    gl = torch.full((n,), 1.0, device="cuda")
+    loss, lse = torch.empty(n, device="cuda"), torch.empty(n, device="cuda")
+    mean = torch.empty(n, D, device="cuda")
+    gx, gt = torch.full_like(x, float("nan")), torch.full_like(table, float("nan"))
+    ctx.vocab_loss(x, table, t, 1.0, loss, lse, mean)
+    ctx.vocab_loss_backward(x, table, t, 1.0, lse, mean, gl, gx, gt)
+    del mean
+    for a in (0, (1 << 24) - 500, (1 << 25) - 500, 3 * (1 << 24) - 500, n - 1000):
+        rows = slice(a, a + 1000)
+        ref = du.loss_ref(x[rows].cpu(), table.cpu(), t[rows].cpu(), 1.0, gl[rows].cpu())
+        for got, k in ((loss, "loss"), (lse, "lse"), (gx, "grad_x")):
+            du.within(got[rows], *ref[k], what=f"{k} from {a}")
+    want, size = torch.zeros(V, D, dtype=torch.float64, device="cuda"), torch.zeros(V, D, dtype=torch.float64, device="cuda")
+    for a in range(0, n, 1 << 22):
+        xs, ts = x[a:a + (1 << 22)].double(), t[a:a + (1 << 22)]
+        w = torch.softmax(xs @ table.double().t(), 1)
+        w[torch.arange(len(ts), device="cuda"), ts.clamp(min=0)] -= 1.0
+        w[ts < 0] = 0.0
+        want += w.t().contiguous() @ xs
+        size += w.abs().t().contiguous() @ xs.abs()
+    # weights rounded by u, and sums of n terms in order, whose roundings are of random sign: off by 4 E sqrt(n) of the terms' sizes
+    assert ((gt.double() - want).abs() <= (du.U[gt.dtype] + 4 * du.E * n ** 0.5) * size).all()
+
+
+def test_more_table_rows_than_a_launch_holds_are_refused(ctx):
+    from paper_2211_05239_amd import recd
+    lib, h = recd._lib, ctx._h
+    a = torch.zeros(4096, device="cuda")
+    p = a.data_ptr()
+    assert lib.recd_vocab_loss(h, 4, (1 << 31) - 511, 64, 0, p, p, p, 1.0, p, p, None) == recd.RECD_EINVAL
