@@ -1037,7 +1037,7 @@ recd_status recd_vocab_loss_backward(recd_ctx *ctx, int64_t n, int64_t V, int D,
         return recd_fail(ctx, RECD_EINVAL, "a vocabulary without rows");
     if (!grad_x && !grad_table && n > 0)
         return recd_fail(ctx, RECD_EINVAL, "neither grad_x nor grad_table");
-    if (n > 0 && (!x || !table || !targets || !lse || !grad_loss || (grad_x && !mean_row)))
+    if ((n > 0 && (!x || !targets || !lse || !grad_loss || (grad_x && !mean_row))) || (V > 0 && (n > 0 || grad_table) && !table))
         return recd_fail(ctx, RECD_EINVAL, "null pointer argument");
     if (((uintptr_t)x | (uintptr_t)table | (uintptr_t)grad_x | (uintptr_t)grad_table) % 16)
         return recd_fail(ctx, RECD_EINVAL, "x, table and their gradients must be aligned to 16 bytes");
