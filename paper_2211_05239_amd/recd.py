@@ -486,7 +486,8 @@ class Context:
     def layer_norm(self, x, weight, bias, eps: float, y, stats=None):
         """y = layer norm of the rows of x [n, D]; stats (float32 [n, 2]: mean, 1 / deviation) for the backward."""
         n, D = x.shape
-        assert y.shape == x.shape and y.dtype == x.dtype and (stats is None or stats.numel() >= 2 * n)
+        assert y.shape == x.shape and y.dtype == x.dtype
+        assert stats is None or (stats.numel() >= 2 * n and stats.dtype == torch.float32)
         self._check(_lib.recd_layer_norm(self._h, n, D, _DT[x.dtype], _ptr(x), _param(weight, D), _param(bias, D), eps,
                                          _ptr(y), _ptr(stats)))
 

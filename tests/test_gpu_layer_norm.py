@@ -170,3 +170,12 @@ def test_refusals(ctx):
     assert lib.recd_layer_norm_backward(h, 4, 64, 0, p, None, None, p, p, None, None) == bad
     assert lib.recd_layer_norm_backward(h, 4, 64, 0, p, None, st, p, p + 8, None, None) == bad
     assert lib.recd_layer_norm(h, 0, 64, 0, None, None, None, EPS, None, None) == recd.RECD_OK
+
+
+@pytest.mark.parametrize("dt", [torch.float16, torch.bfloat16, torch.float64])
+def test_statistics_of_another_type_are_refused(ctx, dt):
+    """They are eight bytes a row, whatever the rows' type."""
+    x = du.rand((40, 32), "bf16", 1).cuda()
+    with pytest.raises(AssertionError):
+        ctx.layer_norm(x, None, None, 1e-5, torch.empty_like(x), torch.zeros(40, 2, dtype=dt, device="cuda"))
+    ctx.layer_norm(x, None, None, 1e-5, torch.empty_like(x), torch.zeros(40, 2, device="cuda"))
