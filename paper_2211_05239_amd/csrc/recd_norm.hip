@@ -27,7 +27,7 @@ __device__ inline float group_sum(float v, int glog)
 }
 
 template <typename T, int P>
-__global__ __launch_bounds__(kBlock) void k_layer_norm(int64_t n, int D, int glog, const T *__restrict__ x,
+__global__ __launch_bounds__(kBlock) void k_layer_norm(int64_t n, int D, int glog, const T *x,  // (may be y)
                                                        const float *__restrict__ weight, const float *__restrict__ bias,
                                                        float eps, T *y, float2 *stats)
 {

@@ -179,3 +179,19 @@ def test_statistics_of_another_type_are_refused(ctx, dt):
     with pytest.raises(AssertionError):
         ctx.layer_norm(x, None, None, 1e-5, torch.empty_like(x), torch.zeros(40, 2, dtype=dt, device="cuda"))
     ctx.layer_norm(x, None, None, 1e-5, torch.empty_like(x), torch.zeros(40, 2, device="cuda"))
+
+
+@pytest.mark.parametrize("dt", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("n,D", [(1, 16), (37, 8), (5000, 128), (9001, 520)])   # (the last: several rows a wave, three pieces a lane)
+def test_in_place(ctx, dt, n, D):
+    """y may be x, and grad_x may be grad_y: the same bits, row after row of a lane's."""
+    x, g = du.rand((n, D), dt, 1), du.rand((n, D), dt, 2)
+    w, b = du.rand((D,), "f32", 3), du.rand((D,), "f32", 4)
+    want = run(ctx, x, w, b, g)
+    y, stats, x = x.cuda(), torch.empty(n, 2, device="cuda"), x.cuda()
+    ctx.layer_norm(y, w.cuda(), b.cuda(), EPS, y, stats)
+    gx = g.cuda()
+    gw, gb = torch.empty(D, device="cuda"), torch.empty(D, device="cuda")
+    ctx.layer_norm_backward(x, w.cuda(), stats, gx, gx, gw, gb)
+    for got, k in ((y, "y"), (gx, "grad_x"), (gw, "grad_weight"), (gb, "grad_bias")):
+        assert du.same_bits(got, want[k]), k
