@@ -103,6 +103,8 @@ typedef enum {
 #define RECD_MAX_DENSE_D 256
 #define RECD_MAX_VOCAB 2147483136LL  /* and most rows of the table of calls 29 and 30 */
 #define RECD_MAX_HEAD_DIM 128
+/* Longest list of calls 31 and 32: its keys, and its queries times the heads. */
+#define RECD_MAX_LIST 2147221504LL
 
 /* Create a context bound to `device` and to `hip_stream` (a hipStream_t passed as void*; NULL =
  * the default stream).  `workspace_hint_bytes` pre-allocates the device workspace (0 = grow on
@@ -626,6 +628,7 @@ recd_status recd_vocab_loss_backward(recd_ctx *ctx, int64_t n, int64_t V, int D,
  *       out_i = sum over the visible j of softmax(z_i)_j v_j;  a row that sees no key gives 0 (and lse = -inf)
  *     What a row does not see does not reach it, be it infinite or NaN, nor its gradients.  Gradients of what does see it
  *     are not finite where the formula's are not; whether infinite or NaN is not said.
+ *     A launch holds 2^32 threads: tiles of 32 rows of a list and key head beyond about 2^26 (short lists) are refused.
  *     Heads: query head h reads key head h / (heads / kv_heads).  One query row per list is the form for serving a new
  *     token; keys are split over blocks where there are few tiles. */
 typedef struct recd_attention {

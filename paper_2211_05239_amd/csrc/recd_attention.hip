@@ -1369,9 +1369,11 @@ recd_status check_attention(recd_ctx *ctx, const recd_attention *a, const void *
                          a->head_dim, RECD_MAX_HEAD_DIM);
     if (a->lists < 0 || a->max_q < 0 || a->max_k < 0 || a->q_rows < 0 || a->k_rows < 0)
         return recd_fail(ctx, RECD_EINVAL, "lists, max_q, max_k, q_rows or k_rows < 0");
-    const int64_t most = ((int64_t)1 << 31) - 1;
+    // (rows are counted in 32 bits, up to a tile of every split behind the last one)
+    const int64_t most = RECD_MAX_LIST;
     if (a->lists > most / 2 || a->max_q > most / a->heads || a->max_k > most)
-        return recd_fail(ctx, RECD_EINVAL, "lists, max_q * heads or max_k of 2^31 and more");
+        return recd_fail(ctx, RECD_EINVAL, "lists, max_q * heads or max_k too large (%lld, %lld, %lld)", (long long)(most / 2),
+                         (long long)most, (long long)most);
     if (!(a->softcap >= 0.0f) || a->softcap == INFINITY)
         return recd_fail(ctx, RECD_EINVAL, "softcap must be 0 (none) or positive");
     if (a->prefix && !a->causal)
@@ -1499,7 +1501,15 @@ int log2_of(int n)
     return l;
 }
 
-unsigned grid_of(const Args &a) { return (unsigned)((a.slots * a.splits + 7) / 8 * 8 * ((a.G + a.heads - 1) / a.heads)); }
+int64_t blocks_of(int64_t slots, int splits, int G, int heads) { return (slots * splits + 7) / 8 * 8 * ((G + heads - 1) / heads); }
+unsigned grid_of(const Args &a) { return (unsigned)blocks_of(a.slots, a.splits, a.G, a.heads); }
+
+// A launch holds less than 2^32 threads.
+bool launch_holds(const Tiling &t, int splits, int G, int heads)
+{
+    const int threads = t.division == ONE_WAVE ? 64 : t.division == PHASES ? 256 : 512;
+    return blocks_of(t.slots, splits, G, heads) < ((int64_t)1 << 32) / threads;
+}
 
 // Key heads that a block of one wave goes through, the next head's rows on their way while it works at one: as many as
 // leave four rounds of waves (about twelve a compute unit at a time).  Forward, with and without, in us: 8192 lists of up to
@@ -1619,8 +1629,8 @@ recd_status recd_list_attention(recd_ctx *ctx, const recd_attention *d, const vo
     if (splits > kMostSplits)
         splits = kMostSplits;
     a.splits = (int)(splits < 1 ? 1 : splits);
-    if (a.slots * a.splits / 8 + 1 > ((int64_t)1 << 27) / a.G)
-        return recd_fail(ctx, RECD_EINVAL, "too many tiles");
+    if (!launch_holds(t, a.splits, a.G, a.heads))
+        return recd_fail(ctx, RECD_EINVAL, "more tiles than a launch holds");
     int2 *tiles;
     auto carve = [&](WsCarver &c) {
         tiles = t.table ? c.take<int2>(t.slots) : nullptr;
@@ -1686,8 +1696,8 @@ recd_status recd_list_attention_backward(recd_ctx *ctx, const recd_attention *d,
     a.gv_stride = grad_v_stride;
     const Tiling tq = tiling(ctx, d, d->q_rows, d->max_q, a.group, d->k_rows, d->max_k);
     const Tiling tk = tiling(ctx, d, d->k_rows, d->max_k, 1, d->q_rows * a.group, d->max_q * a.group);
-    if (tq.slots / 8 + 1 > ((int64_t)1 << 27) / a.G || tk.slots / 8 + 1 > ((int64_t)1 << 27) / a.G)
-        return recd_fail(ctx, RECD_EINVAL, "too many tiles");
+    if (!launch_holds(tq, 1, a.G, 1) || !launch_holds(tk, 1, a.G, 1))
+        return recd_fail(ctx, RECD_EINVAL, "more tiles than a launch holds");
     int2 *tiles_q, *tiles_k;
     float *delta;
     auto carve = [&](WsCarver &c) {

@@ -588,3 +588,23 @@ def test_distances_beyond_2_to_24(ctx, causal):
         du.within(got[name], *ref[name], what=name)
     for name in ("grad_k", "grad_v"):
         du.within(got[name][-tail:], *ref[name], what=name)
+
+
+def test_lengths_and_tiles_beyond_a_launch_are_refused(ctx):
+    """By the descriptor alone, before anything is launched or read."""
+    import ctypes as C
+
+    from paper_2211_05239_amd import recd
+    buf = torch.zeros(4096, device="cuda")
+    p = buf.data_ptr()
+    good = dict(heads=4, kv_heads=4, head_dim=16, dtype=0, lists=1, max_q=4, max_k=4, q_rows=4, k_rows=4, q_offsets=p,
+                k_offsets=p, q_stride=64, k_stride=64, v_stride=64, scale=1.0, softcap=0.0, slopes=None, prefix=None, causal=1)
+    most = (1 << 31) - (1 << 18)
+    many = dict(lists=1 << 27, q_rows=1 << 27, k_rows=1 << 27, max_q=3, max_k=3)
+    for kw in (dict(max_k=most + 1, k_rows=most + 1), dict(max_q=most // 4 + 1, q_rows=most // 4 + 1), many,
+               dict(many, lists=1 << 25, q_rows=1 << 25, k_rows=1 << 25, heads=32, kv_heads=32, q_stride=512, k_stride=512, v_stride=512)):
+        a = recd._Attention(**dict(good, **kw))
+        s = (a.q_stride, a.k_stride, a.v_stride)
+        assert recd._lib.recd_list_attention_backward(ctx._h, C.byref(a), p, p, p, p, p, p, p, p, p, *s) == recd.RECD_EINVAL, kw
+        if a.kv_heads == 4:   # (the forward pass of many short lists goes through several heads in a block)
+            assert recd._lib.recd_list_attention(ctx._h, C.byref(a), p, p, p, p, None) == recd.RECD_EINVAL, kw
