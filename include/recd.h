@@ -123,7 +123,8 @@ recd_status recd_set_option(recd_ctx *ctx, recd_option opt, int64_t value);
 /* Message of the last failing call on this context ("" if none). Valid until the next call. */
 const char *recd_last_error(const recd_ctx *ctx);
 const char *recd_status_string(recd_status s);
-/* Upper bound of the workspace any call needs for these sizes (N = ids in the KJT). */
+/* Upper bound of the workspace any of calls 1 to 26 needs for these sizes (N = ids in the KJT).  Those of calls 27 to 32
+ * have functions of their own, beside them. */
 recd_status recd_workspace_bytes(int F, int64_t B, int64_t N, int D, size_t *out_bytes);
 
 /* 1. KJT -> IKJT (Sec. 4.2 "InverseKeyedJaggedTensor": rows holding exactly the same list — same
@@ -580,8 +581,13 @@ recd_status recd_build_ikjt_noalloc(recd_ctx *ctx, int F, int64_t B, int64_t N,
  *     are also rounded to the type where they enter a matrix product);
  *   - row pointers are aligned to 16 bytes, and a row's (a head's) bytes are a multiple of 16;
  *   - sums are taken in an order that depends on the sizes and types alone: the same call gives the same bits;
- *   - calls use the context's workspace as stated, growing it on demand, and so drop a pending backward plan.
- *     Inside a captured graph the workspace must be large enough already (an earlier call of the sizes made it so). */
+ *   - calls use the context's workspace, growing it on demand, and so drop a pending backward plan.  What a pair of calls
+ *     takes on a device, both directions and every optional output among them, the functions *_workspace_bytes say, for exactly
+ *     these sizes (a smaller call may take more: it is split further).  A captured call needs it beforehand, and as a
+ *     workspace that grows is a new one, a context whose calls a graph holds is created with the largest of all
+ *     calls that it is to make (`workspace_hint_bytes`). */
+recd_status recd_layer_norm_workspace_bytes(int device, int64_t n, int D, recd_dtype dtype, size_t *out_bytes);
+recd_status recd_vocab_loss_workspace_bytes(int device, int64_t n, int64_t V, int D, recd_dtype dtype, size_t *out_bytes);
 
 /* 27. Layer norm of the rows of x [n, D] (device, D * element size at most RECD_MAX_ROW_BYTES):
  *       y = (x - mean) / sqrt(mean((x - mean)^2) + eps) * weight + bias
@@ -592,7 +598,7 @@ recd_status recd_layer_norm(recd_ctx *ctx, int64_t n, int D, recd_dtype dtype, c
 
 /* 28. Gradients of call 27.  grad_y, grad_x: device [n, D] of dtype (grad_x may be grad_y).
  *     grad_weight, grad_bias: device fp32 [D], overwritten with the sums over all rows; either or both may be NULL.
- *     Workspace: up to 32 * D bytes for every compute unit. */
+ *     Workspace: 32 * D bytes for every compute unit at most. */
 recd_status recd_layer_norm_backward(recd_ctx *ctx, int64_t n, int D, recd_dtype dtype, const void *x, const float *weight,
                                      const float *stats, const void *grad_y, void *grad_x, float *grad_weight,
                                      float *grad_bias);
@@ -606,16 +612,15 @@ recd_status recd_layer_norm_backward(recd_ctx *ctx, int64_t n, int D, recd_dtype
  *     loss: device fp32 [n], lse[i] - z[i, targets[i]].   lse: device fp32 [n], log(sum over v of exp(z[i, v])).
  *     mean_row: device fp32 [n, D] or NULL; receives sum over v of exp(z[i, v] - lse[i]) * table_v, from which call 30
  *     has the gradient by x without a second pass over the table.
- *     Workspace: the splits' maxima and sums, and with mean_row their means: splits * n * (D + 2) * 4 bytes, where splits
- *     times row blocks (of 32 to 256 rows) are at most 16 to a compute unit. */
+ *     Workspace: maxima, sums and (with mean_row) means of the splits that a call of few rows cuts the table into; rows beyond
+ *     2^24 go in turns. */
 recd_status recd_vocab_loss(recd_ctx *ctx, int64_t n, int64_t V, int D, recd_dtype dtype, const void *x, const void *table,
                             const int64_t *targets, float scale, float *loss, float *lse, float *mean_row);
 
 /* 30. Gradients of call 29 for grad_loss (device fp32 [n]: the weight of every row's loss).
  *     lse, mean_row: from call 29 on the same inputs (mean_row is read for grad_x only).
  *     grad_x: device [n, D] of dtype, or NULL.   grad_table: device [V, D] of dtype, overwritten (every row), or NULL.
- *     Workspace: 12 bytes a row, and where few groups of table rows (R = 128 or 256) are shared between blocks their parts:
- *     8 * R * D bytes for every block that the card holds at a time. */
+ *     Workspace: 12 bytes a row of x, and where blocks share table rows the parts of their sums. */
 recd_status recd_vocab_loss_backward(recd_ctx *ctx, int64_t n, int64_t V, int D, recd_dtype dtype, const void *x,
                                      const void *table, const int64_t *targets, float scale, const float *lse,
                                      const float *mean_row, const float *grad_loss, void *grad_x, void *grad_table);
@@ -645,10 +650,14 @@ typedef struct recd_attention {
     int causal;
 } recd_attention;
 
+/* Workspace of calls 31 and 32, by the sizes in `sizes` (its pointers and strides are not looked at). */
+recd_status recd_list_attention_workspace_bytes(int device, const recd_attention *sizes, size_t *out_bytes);
+
 /*     q [q_rows, heads, head_dim], k and v [k_rows, kv_heads, head_dim]: device, rows apart by their strides.
  *     out: device [q_rows, heads, head_dim], dense.   lse: device fp32 [q_rows, heads] for call 32, or NULL.
- *     Workspace: 8 bytes for every list and every 32 query rows of a key head, and where keys are split
- *     splits * q_rows * heads * (head_dim + 2) * 4 bytes (there are few query rows then, and at least 512 keys to a split).  RECD_OPT_VALIDATE checks the offsets and bounds. */
+ *     Workspace: 8 bytes for every list and every 32 query rows of a key head, and where keys are split the splits' maxima, sums
+ *     and outputs (there are few query rows then, and at least 512 keys to a split).
+ *     RECD_OPT_VALIDATE checks the offsets and bounds. */
 recd_status recd_list_attention(recd_ctx *ctx, const recd_attention *a, const void *q, const void *k, const void *v, void *out,
                                 float *lse);
 

@@ -1395,7 +1395,7 @@ recd_status check_attention(recd_ctx *ctx, const recd_attention *a, const void *
 recd_status validate_lists(recd_ctx *ctx, const recd_attention *a)
 {
     ctx->plan.valid = false;
-    RECD_TRY(recd_reserve(ctx, 512));
+    RECD_TRY(recd_reserve(ctx, RECD_VALIDATE_BYTES));
     int *err = reinterpret_cast<int *>(ctx->ws);
     RECD_HIP(ctx, hipMemsetAsync(err, 0, sizeof(int), ctx->stream));
     hipLaunchKernelGGL(k_validate_list_offsets, dim3(64), dim3(256), 0, ctx->stream, a->lists, a->q_rows, a->max_q,
@@ -1595,9 +1595,85 @@ void launch_tiles(const recd_attention *d, const Side *sides, int n, hipStream_t
                            d->k_offsets, one, two);
 }
 
+// How a forward call is cut, into `a`.
+Tiling forward_tiling(const recd_ctx *ctx, const recd_attention *d, Args &a)
+{
+    const Tiling t = tiling(ctx, d, d->q_rows, d->max_q, a.group, d->k_rows, d->max_k);
+    a.slots = t.slots;
+    a.tiles_per_list = t.tiles_per_list;
+    a.heads = heads_at_once(ctx, t, a.G, d->lists);
+    // Few tiles: a tile's keys are split over blocks, at least 512 keys each (one query against 30 000 keys 14 us, with 256
+    // 14, with 1024 17; 8 against 16 384 each 20.7, 22.3, 20.5), until two blocks a compute unit are at work (37 queries
+    // against up to 16 384 keys 43 us, with one 46, with four 46); tiles of one wave eight.
+    const int64_t blocks = (int64_t)ctx->num_cu * (t.division == ONE_WAVE ? 8 : 2), have = t.slots * a.G > 0 ? t.slots * a.G : 1;
+    int64_t splits = (blocks + have - 1) / have;
+    if (splits > d->max_k / 512)
+        splits = d->max_k / 512;
+    if (splits > kMostSplits)
+        splits = kMostSplits;
+    a.splits = (int)(splits < 1 ? 1 : splits);
+    return t;
+}
+
+void carve_forward(WsCarver &c, const Tiling &t, Args &a, int2 *&tiles)
+{
+    tiles = t.table ? c.take<int2>(t.slots) : nullptr;
+    a.part_m = a.splits > 1 ? c.take<float>(a.splits * a.part_rows) : nullptr;
+    a.part_l = a.splits > 1 ? c.take<float>(a.splits * a.part_rows) : nullptr;
+    a.part_o = a.splits > 1 ? c.take<float>(a.splits * a.part_rows * a.d) : nullptr;
+}
+
+// The tiles by queries and by keys of a backward call.
+struct BackwardTiling {
+    Tiling q, k;
+
+    BackwardTiling(const recd_ctx *ctx, const recd_attention *d, const Args &a)
+        : q(tiling(ctx, d, d->q_rows, d->max_q, a.group, d->k_rows, d->max_k)),
+          k(tiling(ctx, d, d->k_rows, d->max_k, 1, d->q_rows * a.group, d->max_q * a.group))
+    {
+    }
+    void carve(WsCarver &c, Args &a, int2 *&tiles_q, int2 *&tiles_k) const
+    {
+        tiles_q = q.table ? c.take<int2>(q.slots) : nullptr;
+        tiles_k = k.table ? c.take<int2>(k.slots) : nullptr;
+        a.delta = c.take<float>(a.part_rows);
+    }
+};
+
 } // namespace
 
 extern "C" {
+
+recd_status recd_list_attention_workspace_bytes(int device, const recd_attention *sizes, size_t *out_bytes)
+{
+    recd_ctx c;
+    if (!sizes || !out_bytes)
+        return RECD_EINVAL;
+    static const int64_t nothing = 0;
+    recd_attention d = *sizes;  // with what the check asks for in the place of pointers and strides
+    d.q_offsets = d.k_offsets = &nothing;
+    d.q_stride = (int64_t)d.heads * d.head_dim;
+    d.k_stride = d.v_stride = (int64_t)d.kv_heads * d.head_dim;
+    d.prefix = nullptr;
+    const void *some = reinterpret_cast<const void *>(16);
+    RECD_TRY(check_attention(&c, &d, some, some, some));
+    RECD_TRY(recd_sizing_context(&c, device));
+    *out_bytes = RECD_VALIDATE_BYTES;
+    if (d.lists == 0)
+        return RECD_OK;
+    Args a = common_args(&d, some, some, some);
+    int2 *tiles, *tiles_k;
+    if (d.q_rows > 0) {
+        WsCarver forward(nullptr);
+        const Tiling t = forward_tiling(&c, &d, a);
+        carve_forward(forward, t, a, tiles);
+        *out_bytes = larger(*out_bytes, forward.off);
+    }
+    WsCarver backward(nullptr);
+    BackwardTiling(&c, &d, a).carve(backward, a, tiles, tiles_k);
+    *out_bytes = larger(*out_bytes, backward.off);
+    return RECD_OK;
+}
 
 recd_status recd_list_attention(recd_ctx *ctx, const recd_attention *d, const void *q, const void *k, const void *v, void *out,
                                 float *lse)
@@ -1615,37 +1691,18 @@ recd_status recd_list_attention(recd_ctx *ctx, const recd_attention *d, const vo
     Args a = common_args(d, q, k, v);
     a.out = out;
     a.lse = lse;
-    const Tiling t = tiling(ctx, d, d->q_rows, d->max_q, a.group, d->k_rows, d->max_k);
-    a.slots = t.slots;
-    a.tiles_per_list = t.tiles_per_list;
-    a.heads = heads_at_once(ctx, t, a.G, d->lists);
-    // Few tiles: a tile's keys are split over blocks, at least 512 keys each (one query against 30 000 keys 14 us, with 256
-    // 14, with 1024 17; 8 against 16 384 each 20.7, 22.3, 20.5), until two blocks a compute unit are at work (37 queries
-    // against up to 16 384 keys 43 us, with one 46, with four 46); tiles of one wave eight.
-    const int64_t blocks = (int64_t)ctx->num_cu * (t.division == ONE_WAVE ? 8 : 2), have = t.slots * a.G > 0 ? t.slots * a.G : 1;
-    int64_t splits = (blocks + have - 1) / have;
-    if (splits > d->max_k / 512)
-        splits = d->max_k / 512;
-    if (splits > kMostSplits)
-        splits = kMostSplits;
-    a.splits = (int)(splits < 1 ? 1 : splits);
+    const Tiling t = forward_tiling(ctx, d, a);
     if (!launch_holds(t, a.splits, a.G, a.heads))
         return recd_fail(ctx, RECD_EINVAL, "more tiles than a launch holds");
     int2 *tiles;
-    auto carve = [&](WsCarver &c) {
-        tiles = t.table ? c.take<int2>(t.slots) : nullptr;
-        a.part_m = a.splits > 1 ? c.take<float>(a.splits * a.part_rows) : nullptr;
-        a.part_l = a.splits > 1 ? c.take<float>(a.splits * a.part_rows) : nullptr;
-        a.part_o = a.splits > 1 ? c.take<float>(a.splits * a.part_rows * a.d) : nullptr;
-    };
     WsCarver size(nullptr);
-    carve(size);
+    carve_forward(size, t, a, tiles);
     if (size.off) {
         ctx->plan.valid = false;  // tiles and parts overwrite the workspace a backward plan would live in
         RECD_TRY(recd_reserve(ctx, size.off));
     }
     WsCarver c(ctx->ws);
-    carve(c);
+    carve_forward(c, t, a, tiles);
     a.tiles = tiles;
     const Side side{t.slots, a.group, t.R, false, tiles};
     launch_tiles(d, &side, t.table ? 1 : 0, ctx->stream);
@@ -1694,24 +1751,17 @@ recd_status recd_list_attention_backward(recd_ctx *ctx, const recd_attention *d,
     a.gq_stride = grad_q_stride;
     a.gk_stride = grad_k_stride;
     a.gv_stride = grad_v_stride;
-    const Tiling tq = tiling(ctx, d, d->q_rows, d->max_q, a.group, d->k_rows, d->max_k);
-    const Tiling tk = tiling(ctx, d, d->k_rows, d->max_k, 1, d->q_rows * a.group, d->max_q * a.group);
+    const BackwardTiling tilings(ctx, d, a);
+    const Tiling &tq = tilings.q, &tk = tilings.k;
     if (!launch_holds(tq, 1, a.G, 1) || !launch_holds(tk, 1, a.G, 1))
         return recd_fail(ctx, RECD_EINVAL, "more tiles than a launch holds");
     int2 *tiles_q, *tiles_k;
-    float *delta;
-    auto carve = [&](WsCarver &c) {
-        tiles_q = tq.table ? c.take<int2>(tq.slots) : nullptr;
-        tiles_k = tk.table ? c.take<int2>(tk.slots) : nullptr;
-        delta = c.take<float>(a.part_rows);
-    };
     WsCarver size(nullptr);
-    carve(size);
+    tilings.carve(size, a, tiles_q, tiles_k);
     ctx->plan.valid = false;
     RECD_TRY(recd_reserve(ctx, size.off));
     WsCarver c(ctx->ws);
-    carve(c);
-    a.delta = delta;
+    tilings.carve(c, a, tiles_q, tiles_k);
     hipStream_t st = ctx->stream;
     Side sides[2];
     int listed = 0;

@@ -75,6 +75,22 @@ recd_status recd_reserve(recd_ctx *ctx, size_t bytes)
     return RECD_OK;
 }
 
+recd_status recd_sizing_context(recd_ctx *ctx, int device)
+{
+    int cus = 0;
+    if (device < 0)
+        return RECD_EINVAL;
+    if (hipSetDevice(device) != hipSuccess ||
+        hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, device) != hipSuccess) {
+        (void)hipGetLastError();
+        return RECD_EHIP;
+    }
+    ctx->device = device;
+    if (cus > 0)
+        ctx->num_cu = cus;
+    return RECD_OK;
+}
+
 constexpr int kTimerPairs = 1024;
 
 void recd_time_begin(recd_ctx *ctx, int slot, hipStream_t st)

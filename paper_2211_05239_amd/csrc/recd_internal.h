@@ -146,6 +146,10 @@ recd_status recd_check_rows(recd_ctx *ctx, int F, const int64_t *rows);
 // After a builder wrote {U, M} into ctx->build_counts_dev: publish them to the host asynchronously.
 recd_status recd_publish_build_counts(recd_ctx *ctx);
 recd_status recd_reserve(recd_ctx *ctx, size_t bytes);
+// Makes `ctx`, which no call has created, good for asking how a call on `device` would be cut.
+recd_status recd_sizing_context(recd_ctx *ctx, int device);
+// What validation takes of the workspace.
+constexpr size_t RECD_VALIDATE_BYTES = 512;
 // Behind the last kernel of a plain or weighted build of N ids: where a plan for these outputs may start.
 recd_status recd_mark_build(recd_ctx *ctx, int F, int64_t B, int64_t N, const int32_t *inverse, const int64_t *u_values);
 // Looks up the current device's copy of the static scratch array (with `device` current).
@@ -179,6 +183,7 @@ struct WsCarver {
     }
 };
 
+static inline size_t larger(size_t a, size_t b) { return a > b ? a : b; }
 static inline size_t elem_size(recd_dtype dt) { return dt == RECD_F32 ? 4 : 2; }
 
 // Tables of up to this many features travel to a kernel by value.

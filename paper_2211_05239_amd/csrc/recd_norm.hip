@@ -240,9 +240,25 @@ template <typename T, typename F> void with_pieces(int P, F f)
     }
 }
 
+size_t sums_bytes(const recd_ctx *ctx, int64_t n, int D, recd_dtype dt)
+{
+    return (size_t)norm_blocks(ctx, n, row_shape(D * (int)elem_size(dt) / 16).glog) * 2 * D * 4;
+}
+
 } // namespace
 
 extern "C" {
+
+recd_status recd_layer_norm_workspace_bytes(int device, int64_t n, int D, recd_dtype dt, size_t *out_bytes)
+{
+    recd_ctx c;
+    if (!out_bytes)
+        return RECD_EINVAL;
+    RECD_TRY(check_norm(&c, n, D, dt));
+    RECD_TRY(recd_sizing_context(&c, device));
+    *out_bytes = sums_bytes(&c, n, D, dt);
+    return RECD_OK;
+}
 
 recd_status recd_layer_norm(recd_ctx *ctx, int64_t n, int D, recd_dtype dt, const void *x, const float *weight,
                             const float *bias, float eps, void *y, float *stats)
@@ -286,7 +302,7 @@ recd_status recd_layer_norm_backward(recd_ctx *ctx, int64_t n, int D, recd_dtype
     float *part = nullptr;
     if (sums) {
         ctx->plan.valid = false;  // the partial sums overwrite the workspace a backward plan would live in
-        RECD_TRY(recd_reserve(ctx, (size_t)blocks * 2 * D * 4));
+        RECD_TRY(recd_reserve(ctx, sums_bytes(ctx, n, D, dt)));
         part = reinterpret_cast<float *>(ctx->ws);
     }
     if (n > 0)

@@ -850,7 +850,7 @@ recd_status check_vocab(recd_ctx *ctx, int64_t n, int64_t V, int D, recd_dtype d
 recd_status validate_targets(recd_ctx *ctx, int64_t n, int64_t V, const int64_t *targets)
 {
     ctx->plan.valid = false;
-    RECD_TRY(recd_reserve(ctx, 512));
+    RECD_TRY(recd_reserve(ctx, RECD_VALIDATE_BYTES));
     int *err = reinterpret_cast<int *>(ctx->ws);
     RECD_HIP(ctx, hipMemsetAsync(err, 0, sizeof(int), ctx->stream));
     hipLaunchKernelGGL(k_validate_targets, dim3(64), dim3(256), 0, ctx->stream, n, V, targets, err);
@@ -968,6 +968,34 @@ template <typename T, int DP> TableShape table_shape(const recd_ctx *ctx, int64_
     return s;
 }
 
+TableShape any_table_shape(const recd_ctx *ctx, int64_t n, int64_t V, int D, recd_dtype dt)
+{
+    TableShape shape{};
+    recd_with_type(dt, [&](auto t) { with_width(D, [&](auto w) { shape = table_shape<decltype(t), w.value>(ctx, n, V, D); }); });
+    return shape;
+}
+
+void carve_parts(WsCarver &c, ForwardArgs &a, bool mean)
+{
+    a.part_m = c.take<float>((size_t)a.splits * a.n);
+    a.part_l = c.take<float>((size_t)a.splits * a.n);
+    a.part_o = mean ? c.take<float>((size_t)a.splits * a.n * a.D) : nullptr;
+}
+
+struct TableWs {
+    float *parts, *row_lse, *row_g, *lift;
+    int32_t *row_t;
+
+    void carve(WsCarver &c, const TableShape &shape, int64_t n, int D, recd_dtype dt)
+    {
+        parts = shape.shared ? c.take<float>((size_t)2 * shape.blocks * shape.R * D) : nullptr;
+        row_lse = c.take<float>(n);
+        row_g = c.take<float>(n);
+        row_t = c.take<int32_t>(n);
+        lift = dt == RECD_F16 && n > 0 ? c.take<float>(1) : nullptr;
+    }
+};
+
 template <typename T, int DP> void launch_grad_table(const TableGradArgs &a, const TableShape &s, hipStream_t st)
 {
     constexpr int N = kTiles<T, DP>, W = kManyWaves<T, DP>;
@@ -983,6 +1011,34 @@ template <typename T, int DP> void launch_grad_table(const TableGradArgs &a, con
 } // namespace
 
 extern "C" {
+
+recd_status recd_vocab_loss_workspace_bytes(int device, int64_t n, int64_t V, int D, recd_dtype dt, size_t *out_bytes)
+{
+    recd_ctx c;
+    if (!out_bytes)
+        return RECD_EINVAL;
+    RECD_TRY(check_vocab(&c, n, V, D, dt, 1.0f));
+    RECD_TRY(recd_sizing_context(&c, device));
+    *out_bytes = 0;
+    if (V == 0)
+        return RECD_OK;
+    size_t most = RECD_VALIDATE_BYTES;
+    if (n > 0)
+        for (const bool mean : {false, true}) {  // (they are split differently)
+            const ForwardShape s = forward_shape(&c, most_at_once(n), V, D, dt, mean);
+            ForwardArgs a{};
+            a.n = most_at_once(n);
+            a.D = D;
+            a.splits = s.splits;
+            WsCarver parts(nullptr);
+            carve_parts(parts, a, mean);
+            most = larger(most, parts.off);
+        }
+    WsCarver table(nullptr);
+    TableWs().carve(table, any_table_shape(&c, n, V, D, dt), n, D, dt);
+    *out_bytes = larger(most, table.off);
+    return RECD_OK;
+}
 
 recd_status recd_vocab_loss(recd_ctx *ctx, int64_t n, int64_t V, int D, recd_dtype dt, const void *x, const void *table,
                             const int64_t *targets, float scale, float *loss, float *lse, float *mean_row)
@@ -1006,16 +1062,11 @@ recd_status recd_vocab_loss(recd_ctx *ctx, int64_t n, int64_t V, int D, recd_dty
         const void *part_x = (const char *)x + at * D * (int64_t)elem_size(dt);
         const ForwardShape s = forward_shape(ctx, rows, V, D, dt, mean_row != nullptr);
         ForwardArgs a{rows, V, D, fabsf(scale) * kRecdLog2e, scale < 0, part_x, table, s.row_blocks, s.splits, s.tiles_per_split};
-        auto carve = [&](WsCarver &c) {
-            a.part_m = c.take<float>((size_t)s.splits * rows);
-            a.part_l = c.take<float>((size_t)s.splits * rows);
-            a.part_o = mean_row ? c.take<float>((size_t)s.splits * rows * D) : nullptr;
-        };
         WsCarver size(nullptr);
-        carve(size);
+        carve_parts(size, a, mean_row != nullptr);
         RECD_TRY(recd_reserve(ctx, size.off));
         WsCarver c(ctx->ws);
-        carve(c);
+        carve_parts(c, a, mean_row != nullptr);
         recd_with_type(dt, [&](auto t) {
             using T = decltype(t);
             with_width(D, [&](auto w) { launch_forward<T, w.value>(a, s.share, ctx->stream); });
@@ -1046,26 +1097,22 @@ recd_status recd_vocab_loss_backward(recd_ctx *ctx, int64_t n, int64_t V, int D,
     RECD_HIP(ctx, hipSetDevice(ctx->device));
     if (ctx->validate && n > 0)
         RECD_TRY(validate_targets(ctx, n, V, targets));
-    const bool lifted = dt == RECD_F16 && grad_table && n > 0;
-    WsCarver size(nullptr);
-    float *row_lse, *row_g, *lift, *parts;
-    int32_t *row_t;
     TableShape shape{};
-    if (grad_table)
-        recd_with_type(dt, [&](auto t) { with_width(D, [&](auto w) { shape = table_shape<decltype(t), w.value>(ctx, n, V, D); }); });
-    auto carve = [&](WsCarver &c) {
-        parts = shape.shared ? c.take<float>((size_t)2 * shape.blocks * shape.R * D) : nullptr;
-        row_lse = grad_table ? c.take<float>(n) : nullptr;
-        row_g = grad_table ? c.take<float>(n) : nullptr;
-        row_t = grad_table ? c.take<int32_t>(n) : nullptr;
-        lift = lifted ? c.take<float>(1) : nullptr;
-    };
-    carve(size);
+    TableWs ws{};
+    WsCarver size(nullptr);
+    if (grad_table) {
+        shape = any_table_shape(ctx, n, V, D, dt);
+        ws.carve(size, shape, n, D, dt);
+    }
     ctx->plan.valid = false;
     RECD_TRY(recd_reserve(ctx, size.off));
-    WsCarver c(ctx->ws);
-    carve(c);
-    if (lifted)
+    if (grad_table) {
+        WsCarver c(ctx->ws);
+        ws.carve(c, shape, n, D, dt);
+    }
+    float *const row_lse = ws.row_lse, *const row_g = ws.row_g, *const lift = ws.lift;
+    int32_t *const row_t = ws.row_t;
+    if (lift && n > 0)
         hipLaunchKernelGGL(k_vocab_lift, dim3(1), dim3(1024), 0, ctx->stream, n, V, targets, grad_loss, lift);
     recd_with_type(dt, [&](auto t) {
         using T = decltype(t);
@@ -1075,7 +1122,7 @@ recd_status recd_vocab_loss_backward(recd_ctx *ctx, int64_t n, int64_t V, int D,
                                (T *)grad_x);
         if (!grad_table)
             return;
-        TableGradArgs a{n, V, D, fabsf(scale) * kRecdLog2e, scale, scale < 0, x, table, row_lse, row_g, lift, row_t, grad_table, shape.blocks, parts};
+        TableGradArgs a{n, V, D, fabsf(scale) * kRecdLog2e, scale, scale < 0, x, table, row_lse, row_g, lift, row_t, grad_table, shape.blocks, ws.parts};
         with_width(D, [&](auto w) { launch_grad_table<T, w.value>(a, shape, ctx->stream); });
     });
     RECD_HIP(ctx, hipGetLastError());

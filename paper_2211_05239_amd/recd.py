@@ -54,6 +54,7 @@ EXPORTED = [
     "recd_build_ikjt_runs", "recd_ikjt_run_index", "recd_pooled_lookup_expand", "recd_last_ikjt_run_count",
     "recd_backward_plan_runs", "recd_layer_norm", "recd_layer_norm_backward", "recd_vocab_loss",
     "recd_vocab_loss_backward", "recd_list_attention", "recd_list_attention_backward",
+    "recd_layer_norm_workspace_bytes", "recd_vocab_loss_workspace_bytes", "recd_list_attention_workspace_bytes",
 ]
 
 
@@ -129,6 +130,9 @@ _lib.recd_layer_norm.argtypes = [_vp, C.c_int64, C.c_int, C.c_int, _vp, _vp, _vp
 _lib.recd_layer_norm_backward.argtypes = [_vp, C.c_int64, C.c_int, C.c_int] + [_vp] * 7
 _lib.recd_vocab_loss.argtypes = [_vp, C.c_int64, C.c_int64, C.c_int, C.c_int, _vp, _vp, _vp, C.c_float, _vp, _vp, _vp]
 _lib.recd_vocab_loss_backward.argtypes = [_vp, C.c_int64, C.c_int64, C.c_int, C.c_int, _vp, _vp, _vp, C.c_float] + [_vp] * 5
+_lib.recd_layer_norm_workspace_bytes.argtypes = [C.c_int, C.c_int64, C.c_int, C.c_int, C.POINTER(C.c_size_t)]
+_lib.recd_vocab_loss_workspace_bytes.argtypes = [C.c_int, C.c_int64, C.c_int64, C.c_int, C.c_int, C.POINTER(C.c_size_t)]
+_lib.recd_list_attention_workspace_bytes.argtypes = [C.c_int, C.POINTER(_Attention), C.POINTER(C.c_size_t)]
 _lib.recd_list_attention.argtypes = [_vp, C.POINTER(_Attention)] + [_vp] * 5
 _lib.recd_list_attention_backward.argtypes = [_vp, C.POINTER(_Attention)] + [_vp] * 9 + [C.c_int64] * 3
 _lib.recd_internal_kernel_ms.argtypes = [_vp, C.c_int, C.c_int, C.POINTER(C.c_double), C.POINTER(C.c_double),
@@ -166,12 +170,31 @@ def _rows_ptr(t: torch.Tensor):
     return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
 
 
-def workspace_bytes(F: int, B: int, N: int, D: int) -> int:
+def _bytes_of(name: str, *args) -> int:
     out = C.c_size_t(0)
-    st = _lib.recd_workspace_bytes(F, B, N, D, C.byref(out))
+    st = getattr(_lib, name)(*args, C.byref(out))
     if st != RECD_OK:
-        raise RecdError(st, "recd_workspace_bytes")
+        raise RecdError(st, name)
     return int(out.value)
+
+
+def workspace_bytes(F: int, B: int, N: int, D: int) -> int:
+    return _bytes_of("recd_workspace_bytes", F, B, N, D)
+
+
+def layer_norm_workspace_bytes(n: int, D: int, dtype: torch.dtype, device: int = 0) -> int:
+    return _bytes_of("recd_layer_norm_workspace_bytes", device, n, D, _DT[dtype])
+
+
+def vocab_loss_workspace_bytes(n: int, V: int, D: int, dtype: torch.dtype, device: int = 0) -> int:
+    return _bytes_of("recd_vocab_loss_workspace_bytes", device, n, V, D, _DT[dtype])
+
+
+def list_attention_workspace_bytes(heads: int, kv_heads: int, head_dim: int, dtype: torch.dtype, lists: int, max_q: int, max_k: int,
+                                   q_rows: int, k_rows: int, device: int = 0) -> int:
+    a = _Attention(heads=heads, kv_heads=kv_heads, head_dim=head_dim, dtype=_DT[dtype], lists=lists, max_q=max_q, max_k=max_k,
+                   q_rows=q_rows, k_rows=k_rows)
+    return _bytes_of("recd_list_attention_workspace_bytes", device, C.byref(a))
 
 
 class Context:
