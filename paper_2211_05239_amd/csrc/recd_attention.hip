@@ -25,11 +25,10 @@
 // the results depend on the sizes alone.
 //
 // What is rounded to 16 bits for them, beside the operands: the exponentials (as the second product's operand must be) and ds,
-// both with an error of half a unit in their last place, which sums average; and delta = g . o takes the output as it was
-// stored.  Gradients by queries and keys so lie 2.8e-3 (bf16, relative in the 2-norm) from the exact ones where the rounding of the
-// result alone is 1.7e-3.  delta from unrounded sums would take two products more in the gradients by queries (by their count
-// about a quarter of the backward pass of long lists), and ds in two roundings as many again in both: neither is taken.  fp32
-// rounds nothing.
+// both with an error of half a unit in their last place, which sums average; delta = g . o starts from the output as it was
+// stored and is settled to fp32 by the gradients by queries (see there).  Gradients by queries so lie 2.5e-3 (short lists) to 2.9e-3
+// from the exact ones (bf16, relative in the 2-norm) where the rounding of the result alone is 1.7e-3.  ds in two roundings would take
+// a product more in both kernels (by their count a sixth of the backward pass): not taken.  fp32 rounds nothing.
 //
 // Tiles of lists are found without a scan: the tiles of list l take the slots from floor(rows before l / R) + l on,
 // which never overlap as ceil(n / R) <= floor((before + n) / R) - floor(before / R) + 1.
@@ -217,6 +216,21 @@ template <typename T, int DT> __device__ inline void store_columns(T *row, const
         }
 }
 
+// o += f * the row's columns.
+template <typename T, int DT> __device__ inline void add_columns(recd_f32x16 (&o)[DT], float f, const T *row, int d, int lane)
+{
+    asm volatile("" : "+v"(lane));  // columns that no register holds through the kernel's loop
+#pragma unroll
+    for (int t = 0; t < DT; t++)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+            const int col = 32 * t + recd_sums_row(r, lane);
+            const T *four = row + (col < d ? col : 0);  // (behind the head's end: sums that nobody stores)
+            for (int q = 0; q < 4; q++)
+                o[t][r + q] += f * (float)four[q];
+        }
+}
+
 // What is masked enters the products with weight 0, which is not enough where it is an infinity or a NaN: 0 * NaN is a NaN,
 // in rows of the tile that do not see it.  Only tiles at the mask's edge hold what some of their rows see and others do not: the
 // streamed rows of those are looked through on their way to LDS, zeros take the place of what is not finite there (after the scores,
@@ -266,6 +280,10 @@ __device__ inline void add_not_finite(int s0, int s1, int d, Row row_of, Sees se
 // Waves that a SIMD is to hold at once, as far as the registers go round: two hide each other's waits and fill the
 // matrix cores and the vector units in turn.
 template <typename T, int DP, int KEPT> constexpr int kResident = (sizeof(T) == 4 && DP > 32) || (KEPT == 1 && DP > 64) ? 1 : 2;
+
+// The gradients by queries of 64 wide heads, whose registers pass a third of all by a few: three with what does not fit in memory, in
+// place of two.  32 lists of 2048 rows, 8 heads on 2, with a cap, backward 1566 us against 1654.
+template <typename T, int DP, int KEPT> constexpr int kResidentQ = sizeof(T) == 2 && DP == 64 && KEPT > 1 ? 3 : kResident<T, DP, KEPT>;
 
 // 32 query rows a wave.  The loop is pipelined over tiles of 32 keys: one turn multiplies the next tile's scores and the
 // current one's sums while the current scores become exponentials.  The caps, biases and masks of the next scores, and
@@ -919,12 +937,22 @@ template <int DT> __device__ inline void scale_sums(recd_f32x16 (&o)[DT], float 
 }
 
 // 32 query rows a wave, keys and values stream past.
+//
+// With 16 bits delta has to settle.  ds_j = p_j (dp_j - delta) is the difference of two nearly equal numbers where one key has almost
+// all of a row's weight, and delta = g . o of the output as it was rounded is off by e, up to half a unit of its last place: at
+// p = 0.95 .. 0.99 that was 7 % of the row's gradient in the median and more than all of it at worst (bf16), at 0.99 .. 0.999 85 %.
+// As the p_j sum up to 1, the sum of p_j (dp_j - delta) is -e, and the gradients by keys take delta without it.  A row's own
+// gradient needs sum_j p_j k_j for that, another product; taking the keys from the heaviest one's place, sum_j ds_j (k_j - k*),
+// leaves e (sum_j p_j k_j - k*), which vanishes as the weight on one key (or on several that are the same) grows, where e
+// counts; elsewhere ds is large beside it.  Where a wave has all of a list's keys at once, e is known before ds is made.  Now 0.3 % in
+// the median for all p.  fp32 has delta to 2^-24 already.
+// (the same product added instead: gradients 5 to 30 % slower; the rows in question done again: 15 % on long lists with slopes)
 template <typename T, int DP, int KEPT, int PHASES, int CAP>
-__global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void k_attention_grad_q(Args a)
+__global__ __launch_bounds__(64 * KEPT * PHASES, (kResidentQ<T, DP, KEPT>)) void k_attention_grad_q(Args a)
 {
     using S = Shape<T, DP, KEPT, PHASES>;
     static_assert(KEPT == 1 || PHASES == 1);
-    constexpr bool ONE = KEPT * PHASES == 1;
+    constexpr bool ONE = KEPT * PHASES == 1, SETTLES = sizeof(T) == 2;
     constexpr int KS = DP / 16, DT = DP / 32, BUFS = S::SHARED ? 2 : 1;
     using Mma = RecdMma<T>;
     using Frag = typename Mma::Frag;
@@ -932,6 +960,7 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
         typename S::Tile k[S::OWN][BUFS], v[S::OWN][BUFS];
     } lds;
     __shared__ int says[2][KEPT * PHASES];
+    __shared__ float of_phase[SETTLES && PHASES > 1 ? PHASES : 1][4][64];
     Problem p;
     int head, head_end, tile, split;
     if (!find_tile(a, p, head, head_end, tile, split))
@@ -961,7 +990,7 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
     const Capped<CAP> capped(a.cap);
     const float to_cap = CAP ? 2.0f * kRecdLog2e * a.scale / a.cap : 0.0f;
 
-    // delta = g . o, which the gradients by keys need too
+    // delta = g . o, to begin with of the output as it is stored
     const int h = head * a.group + head_in;
     const int64_t at_row = q_row * H + h;
     Frag qf[KS], gf[KS];
@@ -976,9 +1005,11 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
             delta += (float)gf[k][e] * (float)out[e];
     }
     delta += __shfl_xor(delta, 32);
-    if (there && lane < 32 && phase == 0)
-        a.delta[at_row] = delta;
+    const float stored = delta;
     delta *= lift;
+    // sum of p (dp - delta); the heaviest key's weight (from an eighth on), its place and a quarter of its score's derivative
+    float rest = 0.0f, heaviest = 0.125f, bend = 1.0f;
+    int heavy = -1;
     const float slope = a.slopes && there ? a.slopes[h] * kRecdLog2e : 0.0f;
     float from = there ? a.lse_in[at_row] * kRecdLog2e : 0.0f;
     if (from == -INFINITY)
@@ -1033,11 +1064,15 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
         }
         if (clear)
             make_finite();
-        // the exponent, then p, then ds
-        auto ds_of = [&](float x, float d, float more) {
+        // ds into s; where delta is still to settle first p, what it is the weight of in dp, and with a cap a quarter of the derivative in w
+        recd_f32x16 w;
+        auto score = [&](int r, float more) {
             float quarter = 1.0f;
-            const float z = CAP ? capped.value(x * to_cap, more, quarter) : x * c + more;
-            return recd_exp2(z) * (d * lift - delta) * quarter;
+            const float z = CAP ? capped.value(s[r] * to_cap, more, quarter) : s[r] * c + more;
+            const float p = recd_exp2(z), of = dp[r] * lift - delta;
+            s[r] = SETTLES ? p : p * of * quarter;
+            dp[r] = of;
+            w[r] = quarter;
         };
         auto finish = [&](auto registers) {
             constexpr int NR = registers.value;
@@ -1045,23 +1080,60 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
                 const float far = (float)(pos - j0 - (lane >> 5));  // (whole numbers: positions may pass 2^24)
 #pragma unroll
                 for (int r = 0; r < NR; r++)
-                    s[r] = ds_of(s[r], dp[r], from - slope * fabsf(far - (float)recd_score_row(r, 0)));
+                    score(r, from - slope * fabsf(far - (float)recd_score_row(r, 0)));
             } else {
 #pragma unroll
                 for (int r = 0; r < NR; r++)
-                    s[r] = ds_of(s[r], dp[r], from);
+                    score(r, from);
             }
             if (j0 + 2 * NR > wave_full) {
                 asm volatile("");  // a branch: only the tiles at the mask's edge pay for it
                 const int to = lim - j0 - (lane >> 5);
 #pragma unroll
                 for (int r = 0; r < NR; r++)
-                    s[r] = recd_score_row(r, 0) >= to ? 0.0f : s[r];
+                    if (recd_score_row(r, 0) >= to)
+                        s[r] = dp[r] = w[r] = 0.0f;
             }
+            if constexpr (SETTLES) {
+                if (ONE && t1 == 1) {  // all keys at once: so is what is left of delta
+#pragma unroll
+                    for (int r = 0; r < NR; r++)
+                        rest += s[r] * dp[r];
+                    rest += __shfl_xor(rest, 32);
+#pragma unroll
+                    for (int r = 0; r < NR; r++)
+                        s[r] *= CAP ? (dp[r] - rest) * w[r] : dp[r] - rest;
+                    return;
+                }
+                float top = s[0];
+#pragma unroll
+                for (int r = 1; r < NR; r++)
+                    top = fmaxf(top, s[r]);
+                if (__any(top > heaviest))
+#pragma unroll
+                    for (int r = 0; r < NR; r++)
+                        if (s[r] > heaviest) {
+                            heaviest = s[r];
+                            heavy = t * 16 + r;  // (its place below)
+                            if (CAP)
+                                bend = w[r];
+                        }
+#pragma unroll
+                for (int r = 0; r < NR; r++) {
+                    s[r] *= dp[r];
+                    rest += s[r];
+                    if (CAP)
+                        s[r] *= w[r];
+                }
+            }
+        };
+        auto add = [&](auto registers) {
+            constexpr int NR = registers.value;
             if constexpr (kHalf<T>) {
                 const float f = keep_in_range<NR>(s, o);
                 lift *= f;
                 delta *= f;
+                rest *= f;
             }
 #pragma unroll
             for (int h = 0; h < NR / 8; h++) {
@@ -1071,24 +1143,57 @@ __global__ __launch_bounds__(64 * KEPT * PHASES, (kResident<T, DP, KEPT>)) void 
                     o[d] = Mma::mul(kt[buf].columns(16 * h, 32 * d, lane), sf, o[d]);
             }
         };
-        if (ONE && wave_end - j0 <= 16)  // the other registers hold no key of the list
+        if (ONE && wave_end - j0 <= 16) {  // the other registers hold no key of the list
             finish(std::integral_constant<int, 8>{});
-        else
+            add(std::integral_constant<int, 8>{});
+        } else {
             finish(std::integral_constant<int, 16>{});
+            add(std::integral_constant<int, 16>{});
+        }
     }
     if (odd) {
         const T *keys = (const T *)a.k + p.k0 * a.k_stride + head * a.d;
         add_not_finite<false, T>(t0 > edge ? t0 * 32 : edge * 32, t1 * 32 < p.nk ? t1 * 32 : p.nk, a.d,
                                  [&](int j) { return keys + j * a.k_stride; }, [&](int j) { return j < lim; }, o, lane);
     }
-    if constexpr (kHalf<T>)
+    if constexpr (kHalf<T>) {
         scale_sums<DT>(o, inverse_power(lift));
+        rest *= inverse_power(lift);
+    }
+    if constexpr (SETTLES) {
+        heavy = heavy < 0 ? -1 : (heavy >> 4) * 32 + recd_score_row(heavy & 15, lane);
+        // of the two halves of the wave, and of the phases in their order; of equal weights the first key
+        auto take = [&](float more, float weight, float curve, int place) {
+            rest += more;
+            if (weight > heaviest || (weight == heaviest && (uint32_t)place < (uint32_t)heavy)) {
+                heaviest = weight;
+                bend = curve;
+                heavy = place;
+            }
+        };
+        if (!ONE || t1 > 1)
+            take(__shfl_xor(rest, 32), __shfl_xor(heaviest, 32), __shfl_xor(bend, 32), __shfl_xor(heavy, 32));
+        if constexpr (PHASES > 1) {
+            of_phase[phase][0][lane] = rest;
+            of_phase[phase][1][lane] = heaviest;
+            of_phase[phase][2][lane] = bend;
+            of_phase[phase][3][lane] = __int_as_float(heavy);
+            __syncthreads();
+            if (phase == 0)
+                for (int ph = 1; ph < PHASES; ph++)
+                    take(of_phase[ph][0][lane], of_phase[ph][1][lane], of_phase[ph][2][lane], __float_as_int(of_phase[ph][3][lane]));
+        }
+    }
     if constexpr (PHASES > 1) {
         static_assert(sizeof(lds) >= 64 * 16 * DT * sizeof(float));
         join_sums<DT, PHASES>(o, reinterpret_cast<float *>(&lds), 0, phase, lane);
     }
     if (phase)
         return;
+    if (there && lane < 32)
+        a.delta[at_row] = stored + rest;
+    if (SETTLES && there && heavy >= 0)
+        add_columns<T, DT>(o, -rest * bend, (const T *)a.k + (p.k0 + heavy) * a.k_stride + (int64_t)head * a.d, a.d, lane);
     if (there)
         store_columns<T, DT>((T *)a.gq + q_row * a.gq_stride + (int64_t)h * a.d, o, (CAP ? 4.0f : 1.0f) * a.scale, a.d, lane);
 }

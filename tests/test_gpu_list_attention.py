@@ -608,3 +608,70 @@ def test_lengths_and_tiles_beyond_a_launch_are_refused(ctx):
         assert recd._lib.recd_list_attention_backward(ctx._h, C.byref(a), p, p, p, p, p, p, p, p, p, *s) == recd.RECD_EINVAL, kw
         if a.kv_heads == 4:   # (the forward pass of many short lists goes through several heads in a block)
             assert recd._lib.recd_list_attention(ctx._h, C.byref(a), p, p, p, p, None) == recd.RECD_EINVAL, kw
+
+
+# (a wave to a list: all its keys in one tile, and in several; phases; groups)
+@pytest.mark.parametrize("dt", ["f16", "bf16"])
+@pytest.mark.parametrize("lens,H,G,d", [([20, 31, 7], 2, 2, 32), ([60, 100], 1, 1, 64), ([150, 260], 2, 1, 64), ([300] * 20, 8, 4, 128)])
+@pytest.mark.parametrize("softcap,copies", [(0.0, False), (60.0, False), (0.0, True)])
+def test_gradients_of_rows_that_one_key_takes(ctx, dt, lens, H, G, d, softcap, copies):
+    """Rows whose weight lies on one key (or on two that are the same, with the same value): what is left, p_j (dp_j - delta), keeps
+    its accuracy though dp and delta are nearly equal there and delta is at first taken from the rounded output.
+
+    With e what that delta is off by, u a rounding to the type, eta what fp32 leaves of a probability and tau of dp: weights
+    are rounded, u (|ds| + p |e|); the sum of p (dp - delta) gives e back but for eta and tau, exactly for the gradients by keys; in those
+    by queries e remains beside the heaviest key's k* alone, as e (sum p k - k*)."""
+    o = offsets(lens)
+    K = int(o[-1])
+    gen = torch.Generator().manual_seed(5)
+    k, v, g = du.rand((K, G, d), dt, 2), du.rand((K, G, d), dt, 3), du.rand((K, H, d), dt, 4)
+    q = torch.empty(K, H, d, dtype=k.dtype)
+    for a, b in zip(o[:-1].tolist(), o[1:].tolist()):
+        if copies:
+            half = (b - a) // 2
+            k[a + half:a + 2 * half], v[a + half:a + 2 * half] = k[a:a + half], v[a:a + half]
+        for h in range(H):
+            keys = k[a:b, h // (H // G)].double()
+            to = keys[torch.randperm(b - a, generator=gen)]
+            z = torch.linspace(2.0, 25.0, b - a, dtype=torch.float64)[torch.randperm(b - a, generator=gen)][:, None]
+            q[a:b, h] = (to * z / to.square().sum(1, keepdim=True)).to(q.dtype)
+    got = {n: t.double().cpu() for n, t in run(ctx, q, k, v, o, o, dict(scale=1.0, softcap=softcap), g).items()}
+    u, E, peaked = du.U[q.dtype], du.E, 0
+    tiny = 2.0 ** -25 if dt == "f16" else 0.0
+    for a, b in zip(o[:-1].tolist(), o[1:].tolist()):
+        for G_ in range(G):
+            ks, vs = k[a:b, G_].double(), v[a:b, G_].double()
+            gk, gk_off = torch.zeros_like(ks), torch.zeros(b - a, dtype=torch.float64)
+            for h in range(G_ * (H // G), (G_ + 1) * (H // G)):
+                qs, gs = q[a:b, h].double(), g[a:b, h].double()
+                s = qs @ ks.t()
+                t = torch.tanh(s / softcap) if softcap else torch.zeros_like(s)
+                z, bend = (softcap * t if softcap else s), 1 - t * t
+                p = torch.softmax(z, 1)
+                dp = gs @ vs.t()
+                delta = (p * dp).sum(1, keepdim=True)
+                out = p @ vs
+                ds = p * bend * (dp - delta)
+                dz = 2 * E * (d / 16 + 4) * (qs.abs() @ ks.abs().t()) + 8 * E * (z.abs() + torch.logsumexp(z, 1)[:, None].abs() + softcap)
+                eta = 4 * dz.max(1, keepdim=True).values + 16 * E
+                tau = 4 * E * (d + 8) * (gs.abs() @ vs.abs().t()).max(1, keepdim=True).values
+                e = (gs.abs() * (u * out.abs() + (u + 2 * eta) * (p @ vs.abs()))).sum(1, keepdim=True) + tau
+                left = eta * (p * (dp - delta).abs()).sum(1, keepdim=True) + tau + eta * e   # of delta, once settled
+                kn, big = ks.norm(dim=1), ks.norm(dim=1).max()
+                top = p.argmax(1)
+                apart = ((p * bend) @ ks - bend.gather(1, top[:, None]) * ks[top]).norm(dim=1)
+                want = ds @ ks
+                fp32 = (p * (eta * (dp - delta).abs() + tau)) @ kn + (left * big)[:, 0] * 2
+                bound = u * want.norm(dim=1) + u * (ds.abs() + p * e) @ kn + e[:, 0] * apart + fp32 \
+                    + tiny * (b - a) * (ds.abs().max(1).values + e[:, 0]) * big
+                off = (got["grad_q"][a:b, h] - want).norm(dim=1)
+                assert (off <= bound).all(), float((off / bound).max())
+                peaked += int(((1 - p.max(1).values) < 1e-3).sum())
+                gk += ds.t() @ qs
+                qn = qs.norm(dim=1)
+                gk_off += u * ds.abs().t() @ qn + (p * (eta * (dp - delta).abs() + tau + left)).t() @ qn \
+                    + tiny * (b - a) * ds.abs().max(0).values * qn.max()
+            off = (got["grad_k"][a:b, G_] - gk).norm(dim=1)
+            bound = u * gk.norm(dim=1) + gk_off
+            assert (off <= bound).all(), float((off / bound).max())
+    assert copies or peaked > 5
