@@ -13,9 +13,10 @@
 //
 // Bound by the matrix cores and, beside them, by the vector units: a score costs an exponential (with the cap two and a
 // reciprocal, each a quarter of the rate) where it costs 4 d operations of the matrix cores forward.  32 lists of 2048 rows, 8 heads
-// on 4 of 128 bf16: 816 us forward (674 TFLOP/s at 4 nq nk d operations; 355 us, 774 under the causal mask) and 2183 us
-// backward (630 at 10 nq nk d); 8 heads on 2 of 64 354 us (777) and 1289 (533), with a cap 509 (540) and 1502 (457).  A large
-// product reaches 1384.  Short lists are bound by the chain of one tile (load, two products, exponentials, store) and by what
+// on 4 of 128 bf16: 658 us forward (835 TFLOP/s at 4 nq nk d operations; 368 us, 748 under the causal mask) and 2167 us
+// backward (634 at 10 nq nk d); 8 heads on 2 of 64 355 us (774) and 1321 (520), with a cap 463 (594) and 1589 (432).  A large
+// product reaches 1384; at heads of 128 the vector instructions fill less than half of the time by count, and what the rest of
+// the distance goes to is not shown.  Short lists are bound by the chain of one tile (load, two products, exponentials, store) and by what
 // is idle in tiles of 32, single rows by the keys' and values' bytes.
 //
 // Three kernels of one shape: 32 rows of the kept side (queries; in the last kernel keys) a wave in registers, the other
@@ -235,7 +236,8 @@ template <typename T, int DT> __device__ inline void add_columns(recd_f32x16 (&o
 // in rows of the tile that do not see it.  Only tiles at the mask's edge hold what some of their rows see and others do not: the
 // streamed rows of those are looked through on their way to LDS, zeros take the place of what is not finite there (after the scores,
 // which need it as it is), and at the kernel's end every row is given what of it the row does see.  The looking through costs
-// three operations a word of such tiles, and what is found the reading of those tiles' rows once more, however much it is.
+// an operation a word of such tiles, and what is found the reading of those tiles' rows once more, however much it is: 2048 rows, 4
+// heads on 2 of 128 bf16, both passes 147 us, with one infinite gradient 191, with nothing else 253, with one infinite value 168.
 
 // Whether any of a block's waves says so, or a wave that streams for itself.
 template <bool SHARED, int WAVES> __device__ inline bool any_wave(bool mine, int (&says)[WAVES], int wave, int lane)
@@ -946,7 +948,9 @@ template <int DT> __device__ inline void scale_sums(recd_f32x16 (&o)[DT], float 
 // leaves e (sum_j p_j k_j - k*), which vanishes as the weight on one key (or on several that are the same) grows, where e
 // counts; elsewhere ds is large beside it.  Where a wave has all of a list's keys at once, e is known before ds is made.  Now 0.3 % in
 // the median for all p.  fp32 has delta to 2^-24 already.
-// (the same product added instead: gradients 5 to 30 % slower; the rows in question done again: 15 % on long lists with slopes)
+// (the same product added instead: gradients 5 to 30 % slower; the rows in question done again: 15 % on long lists with slopes.)
+// It costs an addition, half a maximum and in few tiles a search a score, and registers: short lists of 32 wide heads hold three waves
+// a SIMD where they held four, and their gradients by queries take 66 us for 50.
 template <typename T, int DP, int KEPT, int PHASES, int CAP>
 __global__ __launch_bounds__(64 * KEPT * PHASES, (kResidentQ<T, DP, KEPT>)) void k_attention_grad_q(Args a)
 {

@@ -11,15 +11,17 @@
 // 6 are needed at least.  The backward pass turns the sides round: table rows stay in registers, and the rows x
 // stream past them.
 //
-// Both passes are bound by the matrix cores and the exponentials beside them.  4096 rows against 1 M x 128 bf16, 4 nVD
-// operations a pass: 1.82 ms forward with the mean row (1.15 PFLOP/s) and 2.0 ms for the table's gradient (1.05), at the
+// In 16 bits both passes are bound by the matrix cores and the exponentials beside them.  4096 rows against 1 M x 128 bf16, 4 nVD
+// operations a pass: 1.83 ms forward with the mean row (1.15 PFLOP/s) and 2.04 ms for the table's gradient (1.03), at the
 // 1.9 GHz that the card's power leaves them, the matrix cores busy 55 % of the cycles; a large product reaches 1.38 PFLOP/s.
-// 1500 rows against 100 000 x 64 fp32: 334 and 348 us, 115 and 110 TFLOP/s of the 153 of a large product.
+// 1500 rows against 100 000 x 64 fp32: 342 and 344 us, 112 TFLOP/s of the 153 of a large product; by count the vector
+// instructions take a fifth of the products' cycles there, so what the rest goes to is not shown.
 //
 // The vocabulary is cut into splits where there are few rows; their (maximum, sum, mean) are joined in the order of the
 // splits.  Exponentials are rounded to the tables' type for the second product, as the other operand of the matrix
 // cores has it; fp16 ones are scaled by powers of two so that small ones keep their bits.  Sums, maxima and products'
-// sums are held in fp32.
+// sums are held in fp32.  Where a row is predicted well its gradients are what is left of 1 - p_t: the table's gradient takes the
+// 1 off before rounding, and the mean row's largest weight is exact (kSlack).
 #include "recd_internal.h"
 #include "recd_mfma.h"
 
@@ -63,8 +65,8 @@ struct ForwardArgs {
 
 // Few rows: the block's waves hold the same 32 * N rows and each streams table rows of its own, 32 at a time through LDS
 // of its own, so that nobody waits for anybody.  Their sums are joined at the end.  37 rows against 100 000 x 64 fp32 take 15 us
-// (25.6 MB, 1.7 TB/s), 32 against 300 000 x 128 bf16 33 (77 MB, 2.3 TB/s): bound by the chain of load, product and exponentials
-// of the few tiles that each wave has.
+// (25.6 MB, 1.7 TB/s), 32 against 300 000 x 128 bf16 32 (77 MB, 2.4 TB/s): half of what a large copy reaches.  forward_shape gives one
+// row block about a hundred splits, so that most compute units have no block at all.
 template <typename T, int DP, int N, bool MEAN> __global__ __launch_bounds__(kBlock) void k_vocab_forward_few(ForwardArgs a)
 {
     constexpr int KS = DP / 16, DT = DP / 32;
@@ -900,7 +902,9 @@ ForwardShape forward_shape(const recd_ctx *ctx, int64_t n, int64_t V, int D, rec
     s.row_blocks = (int)((n + rows - 1) / rows);
     // A die takes every eighth split, all row blocks of it, and holds one or two blocks a CU at a time (the registers of
     // the sums decide): the number of splits whose rounds are fullest, few of them before many whose parts have to
-    // be joined; at least two tiles each.
+    // be joined; at least two tiles each.  What a split costs is put too high for one row block (100 splits, however large the
+    // table), and many rows leave fewer than eight splits and dies without work: bf16 rows of 128 with the mean row from 70 000
+    // (7 splits) to 300 000 (one split, one die), fp32 ones from about 50 000.
     const int64_t at_once = (int64_t)ctx->num_cu / 8 * (mean && D > 64 ? 1 : 2);
     int64_t splits = 1;
     double best = 1e30;
