@@ -942,15 +942,18 @@ template <int DT> __device__ inline void scale_sums(recd_f32x16 (&o)[DT], float 
 //
 // With 16 bits delta has to settle.  ds_j = p_j (dp_j - delta) is the difference of two nearly equal numbers where one key has almost
 // all of a row's weight, and delta = g . o of the output as it was rounded is off by e, up to half a unit of its last place: at
-// p = 0.95 .. 0.99 that was 7 % of the row's gradient in the median and more than all of it at worst (bf16), at 0.99 .. 0.999 85 %.
+// p = 0.95 .. 0.99 that alone is 7 % of the row's gradient in the median and more than all of it at worst (bf16, by calculation in 64
+// bits with the output rounded), at 0.99 .. 0.999 85 %.
 // As the p_j sum up to 1, the sum of p_j (dp_j - delta) is -e, and the gradients by keys take delta without it.  A row's own
 // gradient needs sum_j p_j k_j for that, another product; taking the keys from the heaviest one's place, sum_j ds_j (k_j - k*),
 // leaves e (sum_j p_j k_j - k*), which vanishes as the weight on one key (or on several that are the same) grows, where e
-// counts; elsewhere ds is large beside it.  Where a wave has all of a list's keys at once, e is known before ds is made.  Now 0.3 % in
-// the median for all p.  fp32 has delta to 2^-24 already.
-// (the same product added instead: gradients 5 to 30 % slower; the rows in question done again: 15 % on long lists with slopes.)
+// counts; elsewhere ds is large beside it.  Where a wave has all of a list's keys at once, e is known before ds is made.  Measured, one
+// list of 700 rows: bf16 0.2 to 0.35 % in the median for all p and 4 % in the worst row, fp16 0.03 to 0.05 % with worst rows below
+// 0.5 %, but at p > 0.999 2 % (heads of 64) and 12 % (128).  fp32 has delta to 2^-24 already.
+// (that product added instead: backward 4 to 12 % slower at heads of 64, 10 to 30 in lists of one wave, 22 to 35, with spills, at heads
+// of 128; the rows in question done again: 10 to 15 % on long lists with slopes.)
 // It costs an addition, half a maximum and in few tiles a search a score, and registers: short lists of 32 wide heads hold three waves
-// a SIMD where they held four, and their gradients by queries take 66 us for 50.
+// a SIMD where they held four, and their gradients by queries take 66 us for 50 (that the waves are the cause is not shown).
 template <typename T, int DP, int KEPT, int PHASES, int CAP>
 __global__ __launch_bounds__(64 * KEPT * PHASES, (kResidentQ<T, DP, KEPT>)) void k_attention_grad_q(Args a)
 {
