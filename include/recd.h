@@ -22,7 +22,8 @@
  *   26. the backward's plan of a batch with a run index
  * and what a sequence model does with the rows of its unique lists:
  *   27, 28. layer norm and its gradients   29, 30. softmax cross entropy against a table and its gradients
- *   31, 32. attention inside lists and its gradients
+ *   31, 32. attention inside lists and its gradients   33, 34. dropout and its gradient
+ *   35, 36. a dense layer and its gradients
  *
  * General rules
  *   - Every array argument marked "device" is a pointer into GPU memory owned by the caller and
@@ -669,6 +670,66 @@ recd_status recd_list_attention(recd_ctx *ctx, const recd_attention *a, const vo
 recd_status recd_list_attention_backward(recd_ctx *ctx, const recd_attention *a, const void *q, const void *k, const void *v,
                                          const void *out, const float *lse, const void *grad_out, void *grad_q, void *grad_k,
                                          void *grad_v, int64_t grad_q_stride, int64_t grad_k_stride, int64_t grad_v_stride);
+
+/* ---- Dense layers, dropout, answers ------------------------------------------------------------------------------
+ * The general rules of the dense operators above hold for these calls too. */
+
+/* A mask that is made of a counter where it is needed and never stored: element (row, column) of a call stays where 16 bits of
+ * the generator Philox 4x32 with 10 rounds, key `seed`, counter {column / 8 | row's bits above 32 from bit 16 on, row, call}, are
+ * not below p * 2^16 (rounded; column % 8 takes the 128 bits' halves of words in their order, low ones first), and is scaled by
+ * 1 / (1 - p) for the rounded p.  What does not stay is 0, be it infinite or NaN.  The same numbers give the same mask, in every
+ * operator, type and direction; every use in a step takes a `call` of its own. */
+typedef struct recd_dropout_mask {
+    double p;                  /* in [0, 1) */
+    uint64_t seed, call;
+    const int64_t *step;       /* device, one number that is added to `call`, read when the kernels run (a captured step
+                                  gets another mask at each replay), or NULL */
+} recd_dropout_mask;
+
+/* 33. Dropout of the rows of x [n, D] (device, dense) behind a residual:  out = residual + mask * x / (1 - p).
+ *     residual: device [n, D] or NULL.  out: device [n, D]; may be x or residual.  No workspace.  D at most 65536, n below 2^48. */
+recd_status recd_dropout(recd_ctx *ctx, int64_t n, int D, recd_dtype dtype, const recd_dropout_mask *mask, const void *x,
+                         const void *residual, void *out);
+
+/* 34. Gradient of call 33 by x:  grad_x = mask * grad_out / (1 - p)  (grad_x may be grad_out); that by the residual is grad_out. */
+recd_status recd_dropout_backward(recd_ctx *ctx, int64_t n, int D, recd_dtype dtype, const recd_dropout_mask *mask,
+                                  const void *grad_out, void *grad_x);
+
+/* GELU: z times the normal distribution's function of z.  SiLU: z / (1 + exp(-z)).  ReLU's slope at 0 is 0. */
+typedef enum { RECD_ACT_NONE = 0, RECD_ACT_RELU = 1, RECD_ACT_GELU = 2, RECD_ACT_SILU = 3 } recd_activation;
+
+typedef struct recd_dense_layer {
+    int64_t n;                                     /* rows, below 2^31 */
+    int in, out;                                   /* widths, at most 65536; rows' bytes a multiple of 16 */
+    recd_dtype dtype;
+    recd_activation act;
+    int64_t x_stride, residual_stride, y_stride;   /* elements from row to row, less than 16 MiB */
+    const recd_dropout_mask *dropout;              /* host, or NULL; rows and columns are those of y */
+} recd_dense_layer;
+
+/* Workspace of calls 35 and 36, by the sizes, activation and p in `sizes` (its strides are not looked at). */
+recd_status recd_dense_workspace_bytes(int device, const recd_dense_layer *sizes, size_t *out_bytes);
+
+/* 35. A dense layer:  z = x w^T + bias,  y = residual + dropout(act(z)).
+ *     x: device [n, in].   w: device [out, in], dense, of dtype.   bias: device fp32 [out] or NULL.   residual: device [n, out] or
+ *     NULL.   y: device [n, out]; may be residual, row for row.   sums: device fp32 [n, out], receives z for call 36, or NULL.
+ *     Up to 64 rows are the form for serving.
+ *     Workspace: where few tiles of rows and features would leave the card idle, the contraction is split, 4 bytes a split and
+ *     element of y. */
+recd_status recd_dense(recd_ctx *ctx, const recd_dense_layer *a, const void *x, const void *w, const float *bias,
+                       const void *residual, float *sums, void *y);
+
+/* 36. Gradients of call 35 by x, w and bias (that by the residual is grad_y):
+ *       gz = mask * grad_y / (1 - p) * act'(z),   grad_x = gz w,   grad_w = gz^T x,   grad_bias = sum over rows of gz
+ *     sums: z from call 35; or NULL, and with an activation z is made again from x, w and bias.  That takes 2 n in out operations
+ *     in place of 8 bytes of traffic for each z: quicker for `in` up to about a thousand in 16 bits (a hundred in fp32).
+ *     grad_y: device [n, out].   grad_x: device [n, in].   grad_w: device [out, in], dense, of dtype, overwritten.
+ *     grad_bias: device fp32 [out], overwritten.  Each of the three may be NULL; none may be an input.
+ *     gz is rounded to dtype where it enters the products.
+ *     Workspace: gz [n, out], w transposed, sums of splits (call 35), and column sums of blocks of rows. */
+recd_status recd_dense_backward(recd_ctx *ctx, const recd_dense_layer *a, const void *x, const void *w, const float *bias,
+                                const float *sums, const void *grad_y, int64_t grad_y_stride, void *grad_x,
+                                int64_t grad_x_stride, void *grad_w, float *grad_bias);
 
 #ifdef __cplusplus
 }

@@ -1,0 +1,148 @@
+// What becomes of a row's elements on their way out of a product's sums: bias, activation, dropout, residual, and the
+// gradients of these.  Eight neighbouring columns of a row at a time, in 32 bits.
+#pragma once
+
+#include "recd_internal.h"
+#include "recd_vec.h"
+
+// ---- dropout -----------------------------------------------------------------------------------------------------
+// Philox 4x32 with 10 rounds (Salmon, Moraes, Dror, Shaw: Parallel random numbers: as easy as 1, 2, 3, 2011) of the key `seed`
+// and the counter (column / 8 | row's upper bits, row, call): 16 of its 128 bits for each of eight neighbours, and an
+// element stays where they are not below `cut` = p * 2^16.  The mask of a place is the same in every kernel and both
+// directions, and is never stored.  With 32 bits an element the generator would take twice the products (20 of 32 x 32
+// bits for eight elements now, a quarter of the vector units' rate each); a p between the steps of 2^-16 is rounded to one
+// and the kept elements are scaled for the rounded one, so the expected value is exact.
+struct RecdMask {
+    uint32_t k0, k1, cut;
+    float by;
+    uint64_t call;
+    const int64_t *step;
+};
+
+constexpr int RECD_MAX_WIDTH = 65536;  // of a row that has a mask or goes through a layer
+
+// Checks the mask a caller describes and brings it into the kernels' form; no mask: cut = 0.
+recd_status recd_make_mask(recd_ctx *ctx, const recd_dropout_mask *m, RecdMask *out);
+
+struct RecdBits {
+    uint32_t w[4];
+    __device__ inline bool keep(int e, uint32_t cut) const { return ((e & 1) ? w[e >> 1] >> 16 : w[e >> 1] & 0xffffu) >= cut; }
+};
+
+// The call's number, with what the device adds to it.
+__device__ inline uint64_t recd_mask_call(const RecdMask &m) { return m.step ? m.call + (uint64_t)*m.step : m.call; }
+
+__device__ inline RecdBits recd_mask_bits(const RecdMask &m, uint64_t call, int64_t row, int piece)
+{
+    uint32_t a = (uint32_t)piece + ((uint32_t)(row >> 32) << 16), b = (uint32_t)row, c = (uint32_t)call, d = (uint32_t)(call >> 32);
+    uint32_t k0 = m.k0, k1 = m.k1;
+#pragma unroll
+    for (int i = 0; i < 10; i++) {
+        const uint64_t u = (uint64_t)a * 0xD2511F53u, v = (uint64_t)c * 0xCD9E8D57u;
+        a = (uint32_t)(v >> 32) ^ b ^ k0;
+        b = (uint32_t)v;
+        c = (uint32_t)(u >> 32) ^ d ^ k1;
+        d = (uint32_t)u;
+        k0 += 0x9E3779B9u;
+        k1 += 0xBB67AE85u;
+    }
+    return RecdBits{{a, b, c, d}};
+}
+
+// v times 1 / (1 - p) where it stays, 0 (also for an infinity or a NaN) where it does not.
+__device__ inline void recd_mask_apply(const RecdMask &m, const RecdBits &bits, float *v)
+{
+#pragma unroll
+    for (int e = 0; e < 8; e++)
+        v[e] = bits.keep(e, m.cut) ? v[e] * m.by : 0.0f;
+}
+
+// ---- activations -------------------------------------------------------------------------------------------------
+// GELU is z * P(z) with the normal distribution's P.  For a >= 0, P(-a) = exp(-a^2 / 2) * t * poly(t), t = 1 / (1 + 0.3 a): a
+// polynomial of degree 7, fitted to erfcx(a / sqrt(2)) / 2 / t over a in [0, 14.5], where it is off by 1.7e-7 of the value.  In 32 bits
+// P(-a) is off by 9e-7 of itself up to a = 4, beyond by what a^2's rounding leaves of the exponential.  No cancellation on
+// either side, and the slope P(z) + z exp(-z^2 / 2) / sqrt(2 pi) shares the exponential.
+struct RecdNormal {
+    float P, e;  // P(z), exp(-z^2 / 2)
+};
+
+__device__ inline RecdNormal recd_normal(float z)
+{
+    const float a = fabsf(z), t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.3f, a, 1.0f));
+    float p = 0.03542371094226837f;
+    p = __builtin_fmaf(p, t, -0.15615835785865784f);
+    p = __builtin_fmaf(p, t, 0.2045566290616989f);
+    p = __builtin_fmaf(p, t, -0.05203389376401901f);
+    p = __builtin_fmaf(p, t, 0.12769171595573425f);
+    p = __builtin_fmaf(p, t, 0.10017596185207367f);
+    p = __builtin_fmaf(p, t, 0.12071213126182556f);
+    p = __builtin_fmaf(p, t, 0.11963200569152832f);
+    const float e = __builtin_amdgcn_exp2f(z * z * -0.7213475204444817f);
+    p = p * t * e;
+    return {z < 0.0f ? p : 1.0f - p, e};
+}
+
+__device__ inline float recd_sigmoid(float z) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z * -1.4426950408889634f)); }
+
+// v[e] = act(v[e]); `act` is the same for all lanes.
+__device__ inline void recd_activate(int act, float *v)
+{
+    if (act == RECD_ACT_RELU) {
+#pragma unroll
+        for (int e = 0; e < 8; e++)
+            v[e] = v[e] <= 0.0f ? 0.0f : v[e];  // (a NaN stays)
+    } else if (act == RECD_ACT_GELU) {
+#pragma unroll
+        for (int e = 0; e < 8; e++)
+            v[e] *= recd_normal(v[e]).P;
+    } else if (act == RECD_ACT_SILU) {
+#pragma unroll
+        for (int e = 0; e < 8; e++)
+            v[e] *= recd_sigmoid(v[e]);
+    }
+}
+
+// g[e] *= act'(z[e]).  ReLU's slope at 0 is 0.
+__device__ inline void recd_activate_back(int act, const float *z, float *g)
+{
+    if (act == RECD_ACT_RELU) {
+#pragma unroll
+        for (int e = 0; e < 8; e++)
+            g[e] = z[e] <= 0.0f ? 0.0f : g[e];
+    } else if (act == RECD_ACT_GELU) {
+#pragma unroll
+        for (int e = 0; e < 8; e++) {
+            const RecdNormal n = recd_normal(z[e]);
+            g[e] *= __builtin_fmaf(z[e] * 0.3989422804014327f, n.e, n.P);
+        }
+    } else if (act == RECD_ACT_SILU) {
+#pragma unroll
+        for (int e = 0; e < 8; e++) {
+            const float s = recd_sigmoid(z[e]);
+            g[e] *= s * (1.0f + z[e] * (1.0f - s));
+        }
+    }
+}
+
+// ---- rows' elements, eight at a time -------------------------------------------------------------------------------
+// The first `count` (8, or 4 at the end of a row of 4-byte elements) of the eight elements at p, aligned to 16 bytes.
+template <typename T> __device__ inline void recd_load8(const T *p, int count, float *v)
+{
+    recd_load16(p, v);
+    if constexpr (sizeof(T) == 4) {
+        if (count == 8)
+            recd_load16(p + 4, v + 4);
+        else
+#pragma unroll
+            for (int e = 4; e < 8; e++)
+                v[e] = 0.0f;
+    }
+}
+
+template <typename T> __device__ inline void recd_store8(T *p, int count, const float *v)
+{
+    recd_store16(p, v);
+    if constexpr (sizeof(T) == 4)
+        if (count == 8)
+            recd_store16(p + 4, v + 4);
+}

@@ -8,7 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
-from typing import Optional, Sequence
+from typing import NamedTuple, Optional, Sequence
 
 import torch
 
@@ -39,6 +39,7 @@ KERNEL_SLOTS = {"lookup_expand": 0, "expand_uncovered": 1, "lookup_unique": 2, "
                 "hash_insert": 5, "grad_lists_sum": 6, "grad_rows_sum": 7, "emit": 8}
 RECD_POOL_SUM, RECD_POOL_MEAN, RECD_POOL_MAX = 0, 1, 2
 RECD_NOALLOC_MAX_LISTS = 65536
+ACTIVATION = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
 POOLING = {"sum": RECD_POOL_SUM, "mean": RECD_POOL_MEAN, "max": RECD_POOL_MAX}
 
 EXPORTED = [
@@ -55,6 +56,7 @@ EXPORTED = [
     "recd_backward_plan_runs", "recd_layer_norm", "recd_layer_norm_backward", "recd_vocab_loss",
     "recd_vocab_loss_backward", "recd_list_attention", "recd_list_attention_backward",
     "recd_layer_norm_workspace_bytes", "recd_vocab_loss_workspace_bytes", "recd_list_attention_workspace_bytes",
+    "recd_dropout", "recd_dropout_backward", "recd_dense", "recd_dense_backward", "recd_dense_workspace_bytes",
 ]
 
 
@@ -65,6 +67,17 @@ class _Attention(C.Structure):
                 ("k_rows", C.c_int64), ("q_offsets", C.c_void_p), ("k_offsets", C.c_void_p),
                 ("q_stride", C.c_int64), ("k_stride", C.c_int64), ("v_stride", C.c_int64), ("scale", C.c_float),
                 ("softcap", C.c_float), ("slopes", C.c_void_p), ("prefix", C.c_void_p), ("causal", C.c_int)]
+
+
+class _Mask(C.Structure):
+    """recd_dropout_mask of the header."""
+    _fields_ = [("p", C.c_double), ("seed", C.c_uint64), ("call", C.c_uint64), ("step", C.c_void_p)]
+
+
+class _Dense(C.Structure):
+    """recd_dense_layer of the header."""
+    _fields_ = [("n", C.c_int64), ("inner", C.c_int), ("outer", C.c_int), ("dtype", C.c_int), ("act", C.c_int),
+                ("x_stride", C.c_int64), ("residual_stride", C.c_int64), ("y_stride", C.c_int64), ("dropout", C.POINTER(_Mask))]
 
 
 _vp = C.c_void_p
@@ -135,6 +148,11 @@ _lib.recd_vocab_loss_workspace_bytes.argtypes = [C.c_int, C.c_int64, C.c_int64, 
 _lib.recd_list_attention_workspace_bytes.argtypes = [C.c_int, C.POINTER(_Attention), C.POINTER(C.c_size_t)]
 _lib.recd_list_attention.argtypes = [_vp, C.POINTER(_Attention)] + [_vp] * 5
 _lib.recd_list_attention_backward.argtypes = [_vp, C.POINTER(_Attention)] + [_vp] * 9 + [C.c_int64] * 3
+_lib.recd_dropout.argtypes = [_vp, C.c_int64, C.c_int, C.c_int, C.POINTER(_Mask), _vp, _vp, _vp]
+_lib.recd_dropout_backward.argtypes = [_vp, C.c_int64, C.c_int, C.c_int, C.POINTER(_Mask), _vp, _vp]
+_lib.recd_dense.argtypes = [_vp, C.POINTER(_Dense)] + [_vp] * 6
+_lib.recd_dense_backward.argtypes = [_vp, C.POINTER(_Dense)] + [_vp] * 5 + [C.c_int64, _vp, C.c_int64, _vp, _vp]
+_lib.recd_dense_workspace_bytes.argtypes = [C.c_int, C.POINTER(_Dense), C.POINTER(C.c_size_t)]
 _lib.recd_internal_kernel_ms.argtypes = [_vp, C.c_int, C.c_int, C.POINTER(C.c_double), C.POINTER(C.c_double),
                                          C.POINTER(C.c_int)]
 _lib.recd_internal_kernel_ms.restype = C.c_int
@@ -170,6 +188,26 @@ def _rows_ptr(t: torch.Tensor):
     return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
 
 
+def _matrix_ptr(t: torch.Tensor):
+    """(address, elements from row to row) of rows [n, width] that are dense in themselves."""
+    assert t.is_cuda and t.dim() == 2 and t.stride(1) == 1
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+class Dropout(NamedTuple):
+    """A mask that drops with probability p, made of a counter: the same (p, seed, call + step) give the same mask.  Every use in a
+    training step takes a `call` of its own; step: int64 tensor of one number on the device that is added to it when the kernels
+    run, for steps that are captured into a graph."""
+    p: float
+    seed: int
+    call: int = 0
+    step: Optional[torch.Tensor] = None
+
+    def _mask(self) -> _Mask:
+        assert self.step is None or (self.step.dtype == torch.int64 and self.step.numel() == 1)
+        return _Mask(self.p, self.seed & (1 << 64) - 1, self.call & (1 << 64) - 1, _ptr(self.step))
+
+
 def _bytes_of(name: str, *args) -> int:
     out = C.c_size_t(0)
     st = getattr(_lib, name)(*args, C.byref(out))
@@ -195,6 +233,13 @@ def list_attention_workspace_bytes(heads: int, kv_heads: int, head_dim: int, dty
     a = _Attention(heads=heads, kv_heads=kv_heads, head_dim=head_dim, dtype=_DT[dtype], lists=lists, max_q=max_q, max_k=max_k,
                    q_rows=q_rows, k_rows=k_rows)
     return _bytes_of("recd_list_attention_workspace_bytes", device, C.byref(a))
+
+
+def dense_workspace_bytes(n: int, inner: int, outer: int, dtype: torch.dtype, act: str = "none", dropout: Optional[Dropout] = None,
+                          device: int = 0) -> int:
+    mask = C.pointer(dropout._mask()) if dropout is not None else None
+    return _bytes_of("recd_dense_workspace_bytes", device,
+                     C.byref(_Dense(n, inner, outer, _DT[dtype], ACTIVATION[act], 0, 0, 0, mask)))
 
 
 class Context:
@@ -574,3 +619,51 @@ class Context:
         (gq, sq), (gk, sk), (gv, sv) = _rows_ptr(grad_q), _rows_ptr(grad_k), _rows_ptr(grad_v)
         self._check(_lib.recd_list_attention_backward(self._h, C.byref(a), pq, pk, pv, _ptr(out), _ptr(lse), _ptr(grad_out),
                                                       gq, gk, gv, sq, sk, sv))
+
+    # -- dropout and dense layers ---------------------------------------------------------------
+    def dropout(self, x, drop: Dropout, out, residual=None):
+        """out = residual + x * mask / (1 - p), rows [n, D]; out may be x or residual."""
+        n, D = x.shape
+        assert out.shape == x.shape and out.dtype == x.dtype
+        assert residual is None or (residual.shape == x.shape and residual.dtype == x.dtype)
+        self._check(_lib.recd_dropout(self._h, n, D, _DT[x.dtype], C.byref(drop._mask()), _ptr(x), _ptr(residual), _ptr(out)))
+
+    def dropout_backward(self, grad_out, drop: Dropout, grad_x):
+        """grad_x = grad_out * mask / (1 - p); grad_x may be grad_out."""
+        n, D = grad_out.shape
+        assert grad_x.shape == grad_out.shape and grad_x.dtype == grad_out.dtype
+        self._check(_lib.recd_dropout_backward(self._h, n, D, _DT[grad_out.dtype], C.byref(drop._mask()), _ptr(grad_out), _ptr(grad_x)))
+
+    @staticmethod
+    def _dense(x, w, bias, act, dropout, sums, residual=None, y=None):
+        (n, inner), outer = x.shape, w.shape[0]
+        assert w.shape[1] == inner and w.dtype == x.dtype
+        assert sums is None or (sums.numel() == n * outer and sums.dtype == torch.float32)
+        mask = C.pointer(dropout._mask()) if dropout is not None else None
+        px, sx = _matrix_ptr(x)
+        pr, sr = _matrix_ptr(residual) if residual is not None else (None, 0)
+        py, sy = _matrix_ptr(y) if y is not None else (None, 0)
+        a = _Dense(n, inner, outer, _DT[x.dtype], ACTIVATION[act], sx, sr, sy, mask)
+        return a, px, _ptr(w), _param(bias, outer), pr, _ptr(sums), py
+
+    def dense(self, x, w, bias, y, *, act: str = "none", dropout: Optional[Dropout] = None, residual=None, sums=None):
+        """y = residual + dropout(act(x w^T + bias)): x [n, in], w [out, in], bias float32 [out] or None, y and residual [n, out]
+        (rows of x, y and residual may be strided).  act: "none", "relu", "gelu" or "silu".  sums (float32 [n, out]) receives
+        x w^T + bias for the backward."""
+        shape = (x.shape[0], w.shape[0])
+        assert y.shape == shape and y.dtype == x.dtype
+        assert residual is None or (residual.shape == shape and residual.dtype == x.dtype)
+        a, px, pw, pb, pr, ps, py = self._dense(x, w, bias, act, dropout, sums, residual, y)
+        self._check(_lib.recd_dense(self._h, C.byref(a), px, pw, pb, pr, ps, py))
+
+    def dense_backward(self, x, w, bias, grad_y, grad_x=None, grad_w=None, grad_bias=None, *, act: str = "none",
+                       dropout: Optional[Dropout] = None, sums=None):
+        """Gradients of dense (that by the residual is grad_y), any of the three: grad_x [n, in] (rows may be strided), grad_w
+        [out, in], grad_bias float32 [out].  Without sums, x w^T + bias is made again where there is an activation."""
+        a, px, pw, pb, _, ps, _ = self._dense(x, w, bias, act, dropout, sums)
+        assert grad_y.shape == (x.shape[0], w.shape[0]) and grad_y.dtype == x.dtype
+        assert grad_x is None or (grad_x.shape == x.shape and grad_x.dtype == x.dtype)
+        assert grad_w is None or (grad_w.shape == w.shape and grad_w.dtype == x.dtype)
+        (pg, sg), (pgx, sgx) = _matrix_ptr(grad_y), _matrix_ptr(grad_x) if grad_x is not None else (None, 0)
+        self._check(_lib.recd_dense_backward(self._h, C.byref(a), px, pw, pb, ps, pg, sg, pgx, sgx, _ptr(grad_w),
+                                             _param(grad_bias, w.shape[0])))
