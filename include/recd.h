@@ -23,7 +23,7 @@
  * and what a sequence model does with the rows of its unique lists:
  *   27, 28. layer norm and its gradients   29, 30. softmax cross entropy against a table and its gradients
  *   31, 32. attention inside lists and its gradients   33, 34. dropout and its gradient
- *   35, 36. a dense layer and its gradients
+ *   35, 36. a dense layer and its gradients   37. the most likely ids of a table, log probabilities, entropy
  *
  * General rules
  *   - Every array argument marked "device" is a pointer into GPU memory owned by the caller and
@@ -730,6 +730,26 @@ recd_status recd_dense(recd_ctx *ctx, const recd_dense_layer *a, const void *x, 
 recd_status recd_dense_backward(recd_ctx *ctx, const recd_dense_layer *a, const void *x, const void *w, const float *bias,
                                 const float *sums, const void *grad_y, int64_t grad_y_stride, void *grad_x,
                                 int64_t grad_x_stride, void *grad_w, float *grad_bias);
+
+/* 37. Answers: rows x [n, D] scored against the V rows of a table, z[i, v] = scale * <x_i, table_v> (types, sizes and scale as in
+ *     call 29; the logits are never stored).
+ *     given: device int64 [n] or NULL, an id each.  logp: device fp32 [n], with given and only with it: receives
+ *     z[i, given[i]] - lse[i]; 0 where given[i] is negative, or V and more (with RECD_OPT_VALIDATE that is RECD_EBOUNDS).
+ *     lse: device fp32 [n] or NULL, log(sum over v of exp(z[i, v])).
+ *     entropy: device fp32 [n] or NULL, minus the sum over v of p log p, p = exp(z[i, v] - lse[i]).
+ *     k: 0 .. RECD_MAX_ANSWERS, at most V.  top_ids: device int64 [n, k], top_logp: device fp32 [n, k] (k > 0): the k largest
+ *     logits' ids and log probabilities, the largest first.  Logits are put in order as 64-bit sums of exact products give them, and
+ *     of equal ones the lowest id comes first; a NaN counts as -infinity.  (Where x or the table is not finite, or a row's sum of
+ *     absolute products could pass the range of fp32, 32-bit sums choose which logits are looked at.)
+ *     The gradient of logp is that of call 30 with the opposite sign.
+ *     Up to 256 rows are the form for serving.  Rows of large batches go in turns.
+ *     Workspace: 4 bytes for every row and 64 rows of the table (k > 0), of at most 512 MiB or 64 rows in a turn, and 12 bytes a row
+ *     and split of the table. */
+#define RECD_MAX_ANSWERS 64
+recd_status recd_vocab_answers_workspace_bytes(int device, int64_t n, int64_t V, int D, recd_dtype dtype, int k, size_t *out_bytes);
+recd_status recd_vocab_answers(recd_ctx *ctx, int64_t n, int64_t V, int D, recd_dtype dtype, const void *x, const void *table,
+                               float scale, const int64_t *given, int k, float *logp, float *entropy, float *lse,
+                               int64_t *top_ids, float *top_logp);
 
 #ifdef __cplusplus
 }

@@ -1,0 +1,746 @@
+// Answers of rows x [n, D] scored against a whole table [V, D]: sum of the softmax and its entropy, the log probability of a given
+// id, and the k most likely ids.
+//
+//   z_iv = scale * x_i . W_v,  lse_i = log sum_v exp(z_iv),  logp_i = z_i,given(i) - lse_i
+//   H_i = -sum_v p_iv log p_iv = log s + t / s  with  s = sum_v exp(z_iv - m),  t = sum_v exp(z_iv - m) (m - z_iv)
+//
+// The logits [n, V] are never stored.  The first kernel streams the table once past rows that stay in registers, with a running
+// maximum m, s and t per row, and writes the largest logit of every chunk of 64 table rows.  The k best ids lie in chunks whose
+// largest logit is among the k best ones' (to the error of 32 bits): the second kernel finds these few chunks for each
+// row and computes their logits again, in 64 bits, which puts neighbours in rank in order that 32 bits do not tell apart.
+// Both terms of H are at least 0, so nothing cancels where one id has nearly all of the weight.
+#include "recd_internal.h"
+#include "recd_mfma.h"
+
+#include <math.h>
+
+namespace {
+
+constexpr int kChunk = 64;       // table rows
+constexpr int kWaves = 4;        // of the kernel of few rows
+constexpr int kMany = 8;         // of the kernel of many rows
+constexpr int kFewRows = 256;
+
+struct StreamArgs {
+    int64_t n, V;
+    int D;
+    float c, scale;      // |scale| * log2(e), |scale|; the sign goes into the kept side
+    bool negative;
+    const void *x, *table;
+    int row_blocks, splits;
+    int64_t chunks, each;            // chunks of a split (a multiple of 4 in the kernel of many rows)
+    float *part_m, *part_s, *part_t; // [splits][n], in powers of two
+    float *best;                     // [n][stride]: the chunks' largest logits, or null
+    int64_t stride;
+    uint32_t *widest;                // [splits][waves]: the largest absolute value in the split's table rows, as an integer
+};
+
+// The larger of `top` and the absolute values in a piece: of 16-bit values in both halves.
+template <typename T> __device__ inline uint32_t widest_of(uint32_t top, typename RecdPiece<T>::type piece)
+{
+    typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+    const recd_u32x4 b = __builtin_bit_cast(recd_u32x4, piece);
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        if constexpr (sizeof(T) == 4)
+            top = max(top, b[i] & 0x7fffffffu);
+        else
+            top = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, top),
+                                                                        __builtin_bit_cast(u16x2, b[i] & 0x7fff7fffu)));
+    }
+    return top;
+}
+
+// The wave's largest, as the bits of a float.
+template <typename T> __device__ inline uint32_t widest_float(uint32_t top)
+{
+    if constexpr (sizeof(T) == 2) {
+        const uint32_t a = top & 0xffffu, b = top >> 16, both = a > b ? a : b;
+        top = __builtin_bit_cast(uint32_t, (float)__builtin_bit_cast(T, (unsigned short)both)) & 0x7fffffffu;  // (a NaN's is above an infinity's)
+    }
+    for (int o = 32; o; o >>= 1)
+        top = max(top, (uint32_t)__shfl_xor((int)top, o));
+    return top;
+}
+
+struct Running {
+    float m = -INFINITY, s = 0.0f, t = 0.0f;  // maximum (in powers of two), sum of e, sum of e * log2(e)
+
+    __device__ inline void rescale(float top)
+    {
+        const float now = fmaxf(m, top);
+        if (now == m)
+            return;
+        // (m = -inf: nothing has been added up)
+        const float f = m == -INFINITY ? 0.0f : recd_exp2(m - now), by = m == -INFINITY ? 0.0f : m - now;
+        t = (t + s * by) * f;
+        s *= f;
+        m = now;
+    }
+    __device__ inline void join(float om, float os, float ot)
+    {
+        rescale(om);
+        if (om == -INFINITY)
+            return;
+        const float f = recd_exp2(om - m);
+        t += (ot + os * (om - m)) * f;
+        s += os * f;
+    }
+};
+
+// 32 scores of a lane, those of table rows from `left` on left out: returns the largest of the lane pair's 64, in which all table rows
+// of the chunk are.
+__device__ inline float largest(const recd_f32x16 (&z)[2], int left, int lane)
+{
+    float top = -INFINITY;
+    if (left >= kChunk) {
+#pragma unroll
+        for (int h = 0; h < 2; h++)
+#pragma unroll
+            for (int r = 0; r < 16; r++)
+                top = fmaxf(top, z[h][r]);
+    } else {
+#pragma unroll
+        for (int h = 0; h < 2; h++)
+#pragma unroll
+            for (int r = 0; r < 16; r++)
+                if (32 * h + recd_score_row(r, lane) < left)
+                    top = fmaxf(top, z[h][r]);
+    }
+    return fmaxf(top, __shfl_xor(top, 32));
+}
+
+__device__ inline void add_up(Running &run, const recd_f32x16 (&z)[2], float c, int left, int lane)
+{
+    const float from = run.m == -INFINITY ? 0.0f : run.m;
+    if (left >= kChunk) {
+#pragma unroll
+        for (int h = 0; h < 2; h++)
+#pragma unroll
+            for (int r = 0; r < 16; r++) {
+                const float d = __builtin_fmaf(z[h][r], c, -from), e = recd_exp2(d);
+                run.s += e;
+                run.t = __builtin_fmaf(e, d, run.t);
+            }
+    } else {
+#pragma unroll
+        for (int h = 0; h < 2; h++)
+#pragma unroll
+            for (int r = 0; r < 16; r++)
+                if (32 * h + recd_score_row(r, lane) < left) {
+                    const float d = __builtin_fmaf(z[h][r], c, -from), e = recd_exp2(d);
+                    run.s += e;
+                    run.t = __builtin_fmaf(e, d, run.t);
+                }
+    }
+}
+
+template <typename T, int KS>
+__device__ inline void keep_rows(typename RecdMma<T>::Frag (&xf)[KS], const StreamArgs &a, int64_t row, int lane)
+{
+#pragma unroll
+    for (int k = 0; k < KS; k++) {
+        xf[k] = recd_row_frag<T>((const T *)a.x + row * a.D, 16 * k, a.D, row < a.n, lane);
+        if (a.negative)
+            xf[k] = recd_negated(xf[k]);
+    }
+}
+
+// Few rows: the block's waves hold the same 32 * N rows and each streams chunks of its own through LDS of its own.
+template <typename T, int DP, int N> __global__ __launch_bounds__(64 * kWaves) void k_answers_few(StreamArgs a)
+{
+    constexpr int KS = DP / 16;
+    using Frag = typename RecdMma<T>::Frag;
+    __shared__ union {
+        RecdTile<T, 32, DP> tile[kWaves];
+        float join[kWaves][3][32 * N];
+    } lds;
+    const int rb = blockIdx.x % a.row_blocks, split = blockIdx.x / a.row_blocks;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t row0 = (int64_t)rb * 32 * N;
+    const int64_t c1 = (split + 1) * a.each < a.chunks ? (split + 1) * a.each : a.chunks;
+    RecdTile<T, 32, DP> &tile = lds.tile[wave];
+    Frag xf[N][KS];
+#pragma unroll
+    for (int j = 0; j < N; j++)
+        keep_rows<T, KS>(xf[j], a, row0 + 32 * j + (lane & 31), lane);
+    Running run[N];
+    uint32_t top_abs = 0;
+    RecdStream<T, 32, DP, 64> stream;
+    if (a.D < DP)
+        stream.clear_behind(lane, tile, a.D);
+    // half h of chunk c; one behind the table's end is the last row over again
+    auto load = [&](int64_t c, int h) {
+        const int64_t first = c * kChunk + 32 * h, from = first < a.V ? first : a.V - 1;
+        stream.load_rows(lane, (const T *)a.table + from * a.D, a.V - from < 32 ? (int)(a.V - from) : 32, a.D, a.D * sizeof(T));
+    };
+    int64_t c = split * a.each + wave;
+    if (c < c1)
+        load(c, 0);
+    for (; c < c1; c += kWaves) {
+        recd_f32x16 z[N][2];
+#pragma unroll
+        for (int h = 0; h < 2; h++) {
+            recd_wave_sync();
+            stream.store(lane, tile, a.D);
+            if (rb == 0)
+#pragma unroll
+                for (auto &piece : stream.held)
+                    top_abs = widest_of<T>(top_abs, piece);
+            recd_wave_sync();
+            if (h == 0)
+                load(c, 1);
+            else if (c + kWaves < c1)
+                load(c + kWaves, 0);
+#pragma unroll
+            for (int j = 0; j < N; j++)
+                z[j][h] = recd_f32x16{};
+#pragma unroll
+            for (int k = 0; k < KS; k++) {
+                const Frag w = tile.rows(0, 16 * k, lane);
+#pragma unroll
+                for (int j = 0; j < N; j++)
+                    z[j][h] = RecdMma<T>::mul(w, xf[j][k], z[j][h]);
+            }
+        }
+        const int left = a.V - c * kChunk < kChunk ? (int)(a.V - c * kChunk) : kChunk;
+#pragma unroll
+        for (int j = 0; j < N; j++) {
+            const float top = largest(z[j], left, lane);
+            run[j].rescale(top * a.c);
+            add_up(run[j], z[j], a.c, left, lane);
+            const int64_t row = row0 + 32 * j + (lane & 31);
+            if (a.best && lane < 32 && row < a.n)
+                a.best[row * a.stride + c] = top * a.scale;
+        }
+    }
+    if (a.widest && rb == 0) {
+        top_abs = widest_float<T>(top_abs);
+        if (lane == 0)
+            a.widest[split * kWaves + wave] = top_abs;
+    }
+    // the waves' sums in their order
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < N; j++) {
+        run[j].s += __shfl_xor(run[j].s, 32);
+        run[j].t += __shfl_xor(run[j].t, 32);
+        if (lane < 32) {
+            lds.join[wave][0][32 * j + lane] = run[j].m;
+            lds.join[wave][1][32 * j + lane] = run[j].s;
+            lds.join[wave][2][32 * j + lane] = run[j].t;
+        }
+    }
+    __syncthreads();
+    const int i = threadIdx.x;
+    if (i >= 32 * N || row0 + i >= a.n)
+        return;
+    Running all;
+    for (int w = 0; w < kWaves; w++)
+        all.join(lds.join[w][0][i], lds.join[w][1][i], lds.join[w][2][i]);
+    a.part_m[split * a.n + row0 + i] = all.m;
+    a.part_s[split * a.n + row0 + i] = all.s;
+    a.part_t[split * a.n + row0 + i] = all.t;
+}
+
+// Many rows: 32 in every wave of a block, all of which see every table row of the split, a chunk of them at a time in two
+// buffers of LDS.
+template <typename T, int DP> __global__ __launch_bounds__(64 * kMany) void k_answers_many(StreamArgs a)
+{
+    constexpr int KS = DP / 16;
+    using Frag = typename RecdMma<T>::Frag;
+    __shared__ RecdTile<T, kChunk, DP> tiles[2];
+    // the row blocks of one split side by side on one die, whose L2 then serves the split's rows to all of them
+    const int64_t total = (int64_t)a.splits * a.row_blocks, share = (total + 7) / 8;
+    const int64_t at = (int64_t)(blockIdx.x & 7) * share + (blockIdx.x >> 3);
+    if ((int64_t)(blockIdx.x >> 3) >= share || at >= total)
+        return;
+    const int split = (int)(at / a.row_blocks), rb = (int)(at - (int64_t)split * a.row_blocks);
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int64_t row = ((int64_t)rb * kMany + wave) * 32 + (lane & 31);
+    const int64_t c0 = split * a.each, c1 = c0 + a.each < a.chunks ? c0 + a.each : a.chunks;
+    Frag xf[KS];
+    keep_rows<T, KS>(xf, a, row, lane);
+    Running run;
+    uint32_t top_abs = 0;
+    RecdStream<T, kChunk, DP, 64 * kMany> stream;
+    if (a.D < DP)
+        for (auto &tile : tiles)
+            stream.clear_behind(tid, tile, a.D);
+    auto load = [&](int64_t c) {
+        const int64_t left = a.V - c * kChunk;
+        stream.load_rows(tid, (const T *)a.table + c * kChunk * a.D, left < kChunk ? (int)left : kChunk, a.D, a.D * sizeof(T));
+    };
+    auto store = [&](int buf) {
+        stream.store(tid, tiles[buf], a.D);
+        if (rb == 0)
+#pragma unroll
+            for (int i = 0; i < stream.PT; i++)
+                if (tid + i * 64 * kMany < RecdTile<T, kChunk, DP>::PIECES)
+                    top_abs = widest_of<T>(top_abs, stream.held[i]);
+    };
+    if (c0 < c1) {
+        load(c0);
+        store(0);
+        if (c0 + 1 < c1)
+            load(c0 + 1);
+    }
+    __syncthreads();
+    recd_f32x4 four = {};
+    for (int64_t c = c0; c < c1; c++) {
+        const int buf = (int)(c - c0) & 1;
+        if (c + 1 < c1) {
+            store(1 - buf);
+            if (c + 2 < c1)
+                load(c + 2);
+        }
+        recd_f32x16 z[2];
+#pragma unroll
+        for (int h = 0; h < 2; h++) {
+            z[h] = recd_f32x16{};
+#pragma unroll
+            for (int k = 0; k < KS; k++)
+                z[h] = RecdMma<T>::mul(tiles[buf].rows(32 * h, 16 * k, lane), xf[k], z[h]);
+        }
+        const int left = a.V - c * kChunk < kChunk ? (int)(a.V - c * kChunk) : kChunk;
+        const float top = largest(z, left, lane);
+        run.rescale(top * a.c);
+        add_up(run, z, a.c, left, lane);
+        if (a.best) {
+            four = recd_f32x4{four[1], four[2], four[3], top * a.scale};
+            if ((c & 3) == 3 || c + 1 == c1) {
+                for (int64_t i = c; (i & 3) != 3; i++)
+                    four = recd_f32x4{four[1], four[2], four[3], -INFINITY};
+                if (lane < 32 && row < a.n)
+                    *reinterpret_cast<recd_f32x4 *>(a.best + row * a.stride + (c & ~(int64_t)3)) = four;
+            }
+        }
+        __syncthreads();
+    }
+    if (a.widest && rb == 0) {
+        top_abs = widest_float<T>(top_abs);
+        if (lane == 0)
+            a.widest[split * kMany + wave] = top_abs;
+    }
+    run.s += __shfl_xor(run.s, 32);
+    run.t += __shfl_xor(run.t, 32);
+    if (lane < 32 && row < a.n) {
+        a.part_m[split * a.n + row] = run.m;
+        a.part_s[split * a.n + row] = run.s;
+        a.part_t[split * a.n + row] = run.t;
+    }
+}
+
+struct SelectArgs {
+    int64_t n, V;
+    int D, k, splits, widest_n;
+    float scale;
+    const void *x, *table;
+    const int64_t *given;
+    const float *part_m, *part_s, *part_t, *best;
+    const uint32_t *widest;
+    int64_t chunks, stride;
+    float *logp, *entropy, *lse, *top_logp;
+    int64_t *top_ids;
+};
+
+constexpr int kSelect = 1024, kListed = 1024, kAtOnce = 2 * kSelect / 64;
+
+// <x, row> in 64 bits, products exact; the same order for every row.
+template <typename T> __device__ inline double dot64(const double *x, const T *row, int D)
+{
+    constexpr int E = 16 / sizeof(T);
+    double s = 0.0;
+    for (int d = 0; d < D; d += E) {
+        float v[E];
+        recd_load16(row + d, v);
+#pragma unroll
+        for (int e = 0; e < E; e++)
+            s = fma(x[d + e], (double)v[e], s);
+    }
+    return s;
+}
+
+// A block a row.  Let d be what a 32-bit logit may be off by.  At least k logits are as large as the k-th largest of 256 groups'
+// largest chunks, L: so the k best are at least L - d, and stand in chunks of at least L - 2d.  These chunks are gone through in
+// their order, kAtOnce at a time, a lane to a table row; what reaches the bar is kept, the k best of it after each time, which
+// raises the bar: of equal ones the first stays.
+template <typename T> __global__ __launch_bounds__(kSelect) void k_answers_select(SelectArgs a)
+{
+    constexpr int KEPT = RECD_MAX_ANSWERS + kAtOnce * kChunk;
+    __shared__ double x[RECD_MAX_DENSE_D];
+    __shared__ double key[KEPT], sorted_key[RECD_MAX_ANSWERS];
+    __shared__ uint32_t id[KEPT], sorted_id[RECD_MAX_ANSWERS];
+    __shared__ float groups[kSelect / 4];
+    __shared__ uint32_t list[kListed], waves[kSelect / 64];
+    __shared__ double lse_all;
+    __shared__ float group_bar, abs_x[kSelect / 64];
+    __shared__ uint32_t count, listed, top_abs[kSelect / 64];
+    __shared__ int64_t next;
+    const int64_t row = blockIdx.x;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const T *xr = (const T *)a.x + row * a.D, *table = (const T *)a.table;
+    float ax = 0.0f;
+    for (int d = tid; d < a.D; d += kSelect) {
+        x[d] = (double)(float)xr[d];
+        ax += fabsf((float)xr[d]);
+    }
+    uint32_t wide = 0;
+    for (int i = tid; i < a.widest_n; i += kSelect)
+        wide = max(wide, a.widest[i]);
+    for (int o = 32; o; o >>= 1) {
+        ax += __shfl_xor(ax, o);
+        wide = max(wide, (uint32_t)__shfl_xor((int)wide, o));
+    }
+    if (lane == 0) {
+        abs_x[wave] = ax;
+        top_abs[wave] = wide;
+    }
+    if (wave == 0) {  // the splits' sums: a lane's in their order, then the lanes'
+        Running all;
+        for (int s = lane; s < a.splits; s += 64)
+            all.join(a.part_m[s * a.n + row], a.part_s[s * a.n + row], a.part_t[s * a.n + row]);
+        for (int o = 1; o < 64; o <<= 1) {
+            const float m = __shfl_down(all.m, o), s = __shfl_down(all.s, o), t = __shfl_down(all.t, o);
+            if ((lane & (2 * o - 1)) == 0)
+                all.join(m, s, t);
+        }
+        if (lane == 0) {
+            const double lse = (double)all.m * 0.6931471805599453 + log((double)all.s);
+            lse_all = lse;
+            if (a.lse)
+                a.lse[row] = (float)lse;
+            if (a.entropy)
+                a.entropy[row] = (float)(log((double)all.s) - 0.6931471805599453 * (double)all.t / (double)all.s);
+        }
+    }
+    __syncthreads();
+    if (wave == kSelect / 64 - 1 && a.given && a.logp) {
+        const int64_t g = a.given[row];
+        const bool has = g >= 0 && g < a.V;
+        double s = 0.0;
+        if (has)
+            for (int d = lane; d < a.D; d += 64)
+                s = fma(x[d], (double)(float)table[g * a.D + d], s);
+        for (int o = 32; o; o >>= 1)
+            s += __shfl_xor(s, o);
+        if (lane == 0)
+            a.logp[row] = has ? (float)(s * (double)a.scale - lse_all) : 0.0f;
+    }
+    if (a.k == 0)
+        return;
+    const float *best = a.best + row * a.stride;
+    // the groups' largest chunks
+    constexpr int64_t STRIP = 8 * kSelect;
+    float top = -INFINITY;
+    for (int64_t c = 8 * (int64_t)tid; c < a.stride; c += STRIP)
+#pragma unroll
+        for (int h = 0; h < 2; h++)
+            if (c + 4 * h < a.stride) {
+                const recd_f32x4 v = *reinterpret_cast<const recd_f32x4 *>(best + c + 4 * h);
+                for (int e = 0; e < 4; e++)
+                    top = fmaxf(top, c + 4 * h + e < a.chunks ? v[e] : -INFINITY);
+            }
+    top = fmaxf(top, __shfl_xor(top, 1));
+    top = fmaxf(top, __shfl_xor(top, 2));
+    if ((tid & 3) == 0)
+        groups[tid >> 2] = top;
+    if (tid == 0)
+        count = 0;
+    __syncthreads();
+    if (tid < kSelect / 4) {
+        const float mine = groups[tid];
+        int above = 0, equal = 0;
+        for (int i = 0; i < kSelect / 4; i++) {
+            above += groups[i] > mine;
+            equal += groups[i] == mine;
+        }
+        if (above < a.k && a.k <= above + equal)
+            group_bar = mine;  // (all that write have this value)
+    }
+    float sum_x = 0.0f;
+    uint32_t w = 0;
+    for (int i = 0; i < kSelect / 64; i++) {
+        sum_x += abs_x[i];
+        w = max(w, top_abs[i]);
+    }
+    // 2^-22 of the largest sum of absolute products for each step of the sum, and what each loses where it underflows; without a bound,
+    // where it is not finite, the chunks are those that 32 bits name, and the best of them are kept
+    const float wf = __builtin_bit_cast(float, w);
+    float d = (float)(a.D + 8) * (0x1p-22f * fabsf(a.scale) * sum_x * wf + 2e-38f * fmaxf(1.0f, fabsf(a.scale)));
+    const bool bound = d < INFINITY;
+    d = bound && sum_x != 0.0f && wf != 0.0f ? d : 0.0f;
+    __syncthreads();
+    const float chunk_bar = group_bar - 2.0f * d;
+    double bar = bound ? (double)group_bar - (double)d : -INFINITY;
+    bool full = false;  // k are kept, and only what is larger counts
+    int64_t from = 0;
+    while (from < a.chunks) {
+        // the next chunks that may hold some, in their order
+        const int64_t c = from + 8 * (int64_t)tid;
+        uint32_t may = 0;
+        for (int e = 0; e < 8; e++)
+            if (c + e < a.chunks) {
+                const float v = best[c + e];
+                if (v >= chunk_bar && !(full && (double)v + (double)d <= bar))
+                    may |= 1u << e;
+            }
+        uint32_t mine = __popc(may), upto = mine;
+        for (int o = 1; o < 64; o <<= 1) {
+            const uint32_t v = (uint32_t)__shfl_up((int)upto, o);
+            upto += lane >= o ? v : 0u;
+        }
+        if (lane == 63)
+            waves[wave] = upto;
+        if (tid == 0) {
+            listed = 0;
+            next = from + STRIP;
+        }
+        __syncthreads();
+        uint32_t before = upto - mine, all = 0;
+        for (int i = 0; i < kSelect / 64; i++) {
+            before += i < wave ? waves[i] : 0u;
+            all += waves[i];
+        }
+        for (int e = 0; e < 8; e++)
+            if (may >> e & 1) {
+                if (before < kListed)
+                    list[before] = (uint32_t)(c + e);
+                else if (before == kListed)
+                    next = c + e;
+                before++;
+            }
+        if (tid == 0)
+            listed = all < kListed ? all : kListed;
+        __syncthreads();
+        const int n = (int)listed;
+        from = next;
+        for (int l0 = 0; l0 < n; l0 += kAtOnce) {
+            for (int l = l0 + wave; l < l0 + kAtOnce && l < n; l += kSelect / 64) {
+                const int64_t chunk = list[l], v = chunk * kChunk + lane;
+                if (full && (double)best[chunk] + (double)d <= bar)
+                    continue;
+                if (v < a.V) {
+                    double z = dot64(x, table + v * a.D, a.D) * (double)a.scale;
+                    z = z == z ? z : -INFINITY;
+                    if (full ? z > bar : z >= bar) {
+                        const uint32_t to = atomicAdd(&count, 1u);
+                        key[to] = z;
+                        id[to] = (uint32_t)v;
+                    }
+                }
+            }
+            __syncthreads();
+            // the k best so far to the front, in their order
+            const int kept = (int)count;
+            for (int i = tid; i < kept; i += kSelect) {
+                const double z = key[i];
+                const uint32_t v = id[i];
+                int rank = 0;
+                for (int o = 0; o < kept; o++)
+                    rank += key[o] > z || (key[o] == z && id[o] < v);
+                if (rank < a.k) {
+                    sorted_key[rank] = z;
+                    sorted_id[rank] = v;
+                }
+            }
+            __syncthreads();
+            if (tid < a.k && tid < kept) {
+                key[tid] = sorted_key[tid];
+                id[tid] = sorted_id[tid];
+            }
+            if (tid == 0)
+                count = kept < a.k ? kept : a.k;
+            __syncthreads();
+            if ((int)count == a.k) {
+                full = true;
+                bar = key[a.k - 1];
+            }
+            __syncthreads();
+        }
+        __syncthreads();  // (next and listed have been read)
+    }
+    if (tid < a.k) {
+        a.top_ids[row * a.k + tid] = id[tid];
+        a.top_logp[row * a.k + tid] = (float)(key[tid] - lse_all);
+    }
+}
+
+// Given ids beyond the table.
+__global__ void k_validate_given(int64_t n, int64_t V, const int64_t *given, int *err)
+{
+    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += (int64_t)gridDim.x * blockDim.x)
+        if (given[i] >= V)
+            atomicOr(err, 1);
+}
+
+// ---- how a call is cut ---------------------------------------------------------------------------------------------
+
+struct Shape {
+    bool few;
+    int rows, row_blocks, splits;  // rows of a block
+    int64_t chunks, stride, each;
+};
+
+// Chunks' maxima of one turn: rows at a time so that they take 512 MiB at most, 64 rows at least.
+int64_t rows_at_once(int64_t n, int64_t V, int k)
+{
+    const int64_t chunks = (V + kChunk - 1) / kChunk;
+    int64_t rows = k ? ((int64_t)1 << 27) / (chunks > 0 ? chunks : 1) : (int64_t)1 << 22;
+    rows = rows > 64 ? rows : 64;
+    rows = rows < (int64_t)1 << 22 ? rows : (int64_t)1 << 22;
+    return n < rows ? n : rows;
+}
+
+Shape stream_shape(const recd_ctx *ctx, int64_t n, int64_t V, int D, recd_dtype dt)
+{
+    Shape s;
+    s.few = n <= kFewRows;
+    s.rows = !s.few ? 32 * kMany : n <= 32 || dt == RECD_F32 || D > 128 ? 32 : 64;
+    s.row_blocks = (int)((n + s.rows - 1) / s.rows);
+    s.chunks = (V + kChunk - 1) / kChunk;
+    s.stride = (s.chunks + 3) / 4 * 4;
+    // two blocks a compute unit
+    const int64_t units = s.few ? (s.chunks + kWaves - 1) / kWaves : s.stride / 4;  // a wave's chunk each; four chunks
+    int64_t splits = 2 * ctx->num_cu / s.row_blocks;
+    splits = splits < units ? splits : units;
+    splits = splits < 1 ? 1 : splits;
+    const int64_t each = (units + splits - 1) / splits;
+    s.each = each * 4;
+    s.splits = (int)((units + each - 1) / each);
+    return s;
+}
+
+void carve(WsCarver &c, StreamArgs &a, bool top)
+{
+    a.part_m = c.take<float>((size_t)a.splits * a.n);
+    a.part_s = c.take<float>((size_t)a.splits * a.n);
+    a.part_t = c.take<float>((size_t)a.splits * a.n);
+    a.best = top ? c.take<float>((size_t)a.n * a.stride) : nullptr;
+    a.widest = top ? c.take<uint32_t>((size_t)a.splits * kMany) : nullptr;
+}
+
+recd_status check_answers(recd_ctx *ctx, int64_t n, int64_t V, int D, recd_dtype dt, float scale, int k)
+{
+    if (!ctx)
+        return RECD_EINVAL;
+    if (n < 0 || V < 0 || V > RECD_MAX_VOCAB || n > ((int64_t)1 << 31) - 1)
+        return recd_fail(ctx, RECD_EINVAL, "n=%lld outside [0, 2^31) or V=%lld outside [0, %lld]", (long long)n, (long long)V,
+                         (long long)RECD_MAX_VOCAB);
+    if ((int)dt < 0 || (int)dt > 2)
+        return recd_fail(ctx, RECD_EINVAL, "unknown dtype");
+    if (!(fabsf(scale) > 0.0f) || !(fabsf(scale) < INFINITY))
+        return recd_fail(ctx, RECD_EINVAL, "scale must be finite and not 0");
+    if (D <= 0 || D * elem_size(dt) % 16 != 0 || D > RECD_MAX_DENSE_D)
+        return recd_fail(ctx, RECD_EINVAL, "D=%d: row bytes must be a multiple of 16, and D at most %d", D, RECD_MAX_DENSE_D);
+    if (k < 0 || k > RECD_MAX_ANSWERS || (n > 0 && k > V))
+        return recd_fail(ctx, RECD_EINVAL, "k=%d outside [0, %d] or larger than V", k, RECD_MAX_ANSWERS);
+    return RECD_OK;
+}
+
+template <typename T, int DP> void launch_stream(const StreamArgs &a, const Shape &s, hipStream_t st)
+{
+    if (s.few) {
+        const dim3 grid((unsigned)(s.splits * s.row_blocks));
+        if (s.rows == 32)
+            hipLaunchKernelGGL((k_answers_few<T, DP, 1>), grid, dim3(64 * kWaves), 0, st, a);
+        else if constexpr (sizeof(T) == 2 && DP <= 128)
+            hipLaunchKernelGGL((k_answers_few<T, DP, 2>), grid, dim3(64 * kWaves), 0, st, a);
+    } else
+        hipLaunchKernelGGL((k_answers_many<T, DP>), dim3((unsigned)(((int64_t)s.splits * s.row_blocks + 7) / 8 * 8)), dim3(64 * kMany), 0, st, a);
+}
+
+} // namespace
+
+extern "C" {
+
+recd_status recd_vocab_answers_workspace_bytes(int device, int64_t n, int64_t V, int D, recd_dtype dt, int k, size_t *out_bytes)
+{
+    recd_ctx c;
+    if (!out_bytes)
+        return RECD_EINVAL;
+    RECD_TRY(check_answers(&c, n, V, D, dt, 1.0f, k));
+    RECD_TRY(recd_sizing_context(&c, device));
+    *out_bytes = 0;
+    if (n == 0 || V == 0)
+        return RECD_OK;
+    size_t most = RECD_VALIDATE_BYTES;
+    const int64_t turn = rows_at_once(n, V, k), last = (n - 1) % turn + 1;
+    for (const int64_t rows : {turn, last}) {  // (few rows are split further)
+        const Shape s = stream_shape(&c, rows, V, D, dt);
+        StreamArgs a{};
+        a.n = rows;
+        a.splits = s.splits;
+        a.stride = s.stride;
+        WsCarver ws(nullptr);
+        carve(ws, a, k > 0);
+        most = larger(most, ws.off);
+    }
+    *out_bytes = most;
+    return RECD_OK;
+}
+
+recd_status recd_vocab_answers(recd_ctx *ctx, int64_t n, int64_t V, int D, recd_dtype dt, const void *x, const void *table, float scale,
+                               const int64_t *given, int k, float *logp, float *entropy, float *lse, int64_t *top_ids, float *top_logp)
+{
+    RECD_TRY(check_answers(ctx, n, V, D, dt, scale, k));
+    if (n == 0)
+        return RECD_OK;
+    if (V == 0)
+        return recd_fail(ctx, RECD_EINVAL, "a vocabulary without rows");
+    if (!x || !table || (logp && !given) || (given && !logp) || (k > 0 && (!top_ids || !top_logp)))
+        return recd_fail(ctx, RECD_EINVAL, "null pointer argument");
+    if (((uintptr_t)x | (uintptr_t)table) % 16)
+        return recd_fail(ctx, RECD_EINVAL, "x and table must be aligned to 16 bytes");
+    RECD_HIP(ctx, hipSetDevice(ctx->device));
+    ctx->plan.valid = false;  // the parts overwrite the workspace a backward plan would live in
+    if (ctx->validate && given) {
+        RECD_TRY(recd_reserve(ctx, RECD_VALIDATE_BYTES));
+        int *err = reinterpret_cast<int *>(ctx->ws);
+        RECD_HIP(ctx, hipMemsetAsync(err, 0, sizeof(int), ctx->stream));
+        hipLaunchKernelGGL(k_validate_given, dim3(64), dim3(256), 0, ctx->stream, n, V, given, err);
+        RECD_HIP(ctx, hipGetLastError());
+        ctx->host_pinned[0] = 0;
+        RECD_HIP(ctx, hipMemcpyAsync(ctx->host_pinned, err, sizeof(int), hipMemcpyDeviceToHost, ctx->stream));
+        RECD_HIP(ctx, hipStreamSynchronize(ctx->stream));
+        if ((int)ctx->host_pinned[0])
+            return recd_fail(ctx, RECD_EBOUNDS, "a given id is not a row of the table");
+    }
+    const int64_t turn = rows_at_once(n, V, k);
+    for (int64_t at = 0; at < n; at += turn) {
+        const int64_t rows = n - at < turn ? n - at : turn;
+        const Shape s = stream_shape(ctx, rows, V, D, dt);
+        StreamArgs a{};
+        a.n = rows;
+        a.V = V;
+        a.D = D;
+        a.c = fabsf(scale) * kRecdLog2e;
+        a.scale = fabsf(scale);
+        a.negative = scale < 0;
+        a.x = (const char *)x + at * D * (int64_t)elem_size(dt);
+        a.table = table;
+        a.row_blocks = s.row_blocks;
+        a.splits = s.splits;
+        a.chunks = s.chunks;
+        a.each = s.each;
+        a.stride = s.stride;
+        WsCarver size(nullptr);
+        carve(size, a, k > 0);
+        RECD_TRY(recd_reserve(ctx, size.off));
+        WsCarver c(ctx->ws);
+        carve(c, a, k > 0);
+        SelectArgs b{rows, V, D, k, s.splits, k > 0 ? s.splits * (s.few ? kWaves : kMany) : 0, scale, a.x, table, given ? given + at : nullptr,
+                     a.part_m, a.part_s, a.part_t, a.best, a.widest, s.chunks, s.stride, logp ? logp + at : nullptr,
+                     entropy ? entropy + at : nullptr, lse ? lse + at : nullptr, k > 0 ? top_logp + at * k : nullptr,
+                     k > 0 ? top_ids + at * k : nullptr};
+        recd_with_type(dt, [&](auto t) {
+            using T = decltype(t);
+            recd_with_width(D, [&](auto w) { launch_stream<T, w.value>(a, s, ctx->stream); });
+            hipLaunchKernelGGL((k_answers_select<T>), dim3((unsigned)rows), dim3(kSelect), 0, ctx->stream, b);
+        });
+    }
+    RECD_HIP(ctx, hipGetLastError());
+    return RECD_OK;
+}
+
+} // extern "C"

@@ -258,3 +258,20 @@ template <typename T> __device__ inline typename RecdMma<T>::Frag recd_sums_frag
 
 constexpr float kRecdLog2e = 1.4426950408889634f, kRecdLn2 = 0.6931471805599453f;
 __device__ inline float recd_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// The tiles' width for rows of D elements.
+template <typename F> void recd_with_width(int D, F f)
+{
+    if (D <= 32)
+        f(std::integral_constant<int, 32>{});
+    else if (D <= 64)
+        f(std::integral_constant<int, 64>{});
+    else if (D <= 96)
+        f(std::integral_constant<int, 96>{});
+    else if (D <= 128)
+        f(std::integral_constant<int, 128>{});
+    else if (D <= 192)
+        f(std::integral_constant<int, 192>{});
+    else
+        f(std::integral_constant<int, 256>{});
+}

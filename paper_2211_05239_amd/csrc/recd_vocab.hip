@@ -865,23 +865,6 @@ recd_status validate_targets(recd_ctx *ctx, int64_t n, int64_t V, const int64_t 
     return RECD_OK;
 }
 
-// The tiles' width for rows of D elements.
-template <typename F> void with_width(int D, F f)
-{
-    if (D <= 32)
-        f(std::integral_constant<int, 32>{});
-    else if (D <= 64)
-        f(std::integral_constant<int, 64>{});
-    else if (D <= 96)
-        f(std::integral_constant<int, 96>{});
-    else if (D <= 128)
-        f(std::integral_constant<int, 128>{});
-    else if (D <= 192)
-        f(std::integral_constant<int, 192>{});
-    else
-        f(std::integral_constant<int, 256>{});
-}
-
 // How a forward call is cut: `share` is the kernel of few rows, whose waves stream for themselves and whose rows stay in every
 // one of them. In us, it against the other, loss alone and with the mean row: 128 rows bf16 against 300 000 x 128 35, 66 /
 // 63, 99; 256 rows 45, 77 / 64, 101; 512 rows 67, 122 / 68, 110; 256 rows fp32 against 100 000 x 64 40, 70 / 51, 91.
@@ -975,7 +958,7 @@ template <typename T, int DP> TableShape table_shape(const recd_ctx *ctx, int64_
 TableShape any_table_shape(const recd_ctx *ctx, int64_t n, int64_t V, int D, recd_dtype dt)
 {
     TableShape shape{};
-    recd_with_type(dt, [&](auto t) { with_width(D, [&](auto w) { shape = table_shape<decltype(t), w.value>(ctx, n, V, D); }); });
+    recd_with_type(dt, [&](auto t) { recd_with_width(D, [&](auto w) { shape = table_shape<decltype(t), w.value>(ctx, n, V, D); }); });
     return shape;
 }
 
@@ -1073,7 +1056,7 @@ recd_status recd_vocab_loss(recd_ctx *ctx, int64_t n, int64_t V, int D, recd_dty
         carve_parts(c, a, mean_row != nullptr);
         recd_with_type(dt, [&](auto t) {
             using T = decltype(t);
-            with_width(D, [&](auto w) { launch_forward<T, w.value>(a, s.share, ctx->stream); });
+            recd_with_width(D, [&](auto w) { launch_forward<T, w.value>(a, s.share, ctx->stream); });
             hipLaunchKernelGGL((k_vocab_join<T>), dim3((unsigned)((rows + kWaves - 1) / kWaves)), dim3(kBlock), 0, ctx->stream, rows,
                                V, D, scale, s.splits, a.part_m, a.part_l, a.part_o, (const T *)part_x, (const T *)table,
                                targets + at, loss + at, lse + at, mean_row ? mean_row + at * D : nullptr);
@@ -1127,7 +1110,7 @@ recd_status recd_vocab_loss_backward(recd_ctx *ctx, int64_t n, int64_t V, int D,
         if (!grad_table)
             return;
         TableGradArgs a{n, V, D, fabsf(scale) * kRecdLog2e, scale, scale < 0, x, table, row_lse, row_g, lift, row_t, grad_table, shape.blocks, ws.parts};
-        with_width(D, [&](auto w) { launch_grad_table<T, w.value>(a, shape, ctx->stream); });
+        recd_with_width(D, [&](auto w) { launch_grad_table<T, w.value>(a, shape, ctx->stream); });
     });
     RECD_HIP(ctx, hipGetLastError());
     return RECD_OK;

@@ -39,6 +39,7 @@ KERNEL_SLOTS = {"lookup_expand": 0, "expand_uncovered": 1, "lookup_unique": 2, "
                 "hash_insert": 5, "grad_lists_sum": 6, "grad_rows_sum": 7, "emit": 8}
 RECD_POOL_SUM, RECD_POOL_MEAN, RECD_POOL_MAX = 0, 1, 2
 RECD_NOALLOC_MAX_LISTS = 65536
+RECD_MAX_ANSWERS = 64
 ACTIVATION = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
 POOLING = {"sum": RECD_POOL_SUM, "mean": RECD_POOL_MEAN, "max": RECD_POOL_MAX}
 
@@ -57,6 +58,7 @@ EXPORTED = [
     "recd_vocab_loss_backward", "recd_list_attention", "recd_list_attention_backward",
     "recd_layer_norm_workspace_bytes", "recd_vocab_loss_workspace_bytes", "recd_list_attention_workspace_bytes",
     "recd_dropout", "recd_dropout_backward", "recd_dense", "recd_dense_backward", "recd_dense_workspace_bytes",
+    "recd_vocab_answers", "recd_vocab_answers_workspace_bytes",
 ]
 
 
@@ -153,6 +155,8 @@ _lib.recd_dropout_backward.argtypes = [_vp, C.c_int64, C.c_int, C.c_int, C.POINT
 _lib.recd_dense.argtypes = [_vp, C.POINTER(_Dense)] + [_vp] * 6
 _lib.recd_dense_backward.argtypes = [_vp, C.POINTER(_Dense)] + [_vp] * 5 + [C.c_int64, _vp, C.c_int64, _vp, _vp]
 _lib.recd_dense_workspace_bytes.argtypes = [C.c_int, C.POINTER(_Dense), C.POINTER(C.c_size_t)]
+_lib.recd_vocab_answers.argtypes = [_vp, C.c_int64, C.c_int64, C.c_int, C.c_int, _vp, _vp, C.c_float, _vp, C.c_int] + [_vp] * 5
+_lib.recd_vocab_answers_workspace_bytes.argtypes = [C.c_int, C.c_int64, C.c_int64, C.c_int, C.c_int, C.c_int, C.POINTER(C.c_size_t)]
 _lib.recd_internal_kernel_ms.argtypes = [_vp, C.c_int, C.c_int, C.POINTER(C.c_double), C.POINTER(C.c_double),
                                          C.POINTER(C.c_int)]
 _lib.recd_internal_kernel_ms.restype = C.c_int
@@ -240,6 +244,10 @@ def dense_workspace_bytes(n: int, inner: int, outer: int, dtype: torch.dtype, ac
     mask = C.pointer(dropout._mask()) if dropout is not None else None
     return _bytes_of("recd_dense_workspace_bytes", device,
                      C.byref(_Dense(n, inner, outer, _DT[dtype], ACTIVATION[act], 0, 0, 0, mask)))
+
+
+def vocab_answers_workspace_bytes(n: int, V: int, D: int, dtype: torch.dtype, k: int, device: int = 0) -> int:
+    return _bytes_of("recd_vocab_answers_workspace_bytes", device, n, V, D, _DT[dtype], k)
 
 
 class Context:
@@ -667,3 +675,20 @@ class Context:
         (pg, sg), (pgx, sgx) = _matrix_ptr(grad_y), _matrix_ptr(grad_x) if grad_x is not None else (None, 0)
         self._check(_lib.recd_dense_backward(self._h, C.byref(a), px, pw, pb, ps, pg, sg, pgx, sgx, _ptr(grad_w),
                                              _param(grad_bias, w.shape[0])))
+
+    # -- answers --------------------------------------------------------------------------------
+    def vocab_answers(self, x, table, scale: float, given=None, logp=None, entropy=None, lse=None, top_ids=None, top_logp=None):
+        """Rows x [n, D] scored against all rows of table [V, D]: the log probability of given (int64 [n], with logp), the entropy,
+        the logarithm of the sum of the exponentials (float32 [n] each), and the k most likely ids, top_ids (int64 [n, k]) and
+        top_logp (float32 [n, k]); what is None is left out."""
+        n, D = x.shape
+        assert table.shape[1] == D and table.dtype == x.dtype
+        assert given is None or (given.dtype == torch.int64 and given.numel() == n)
+        for t in (logp, entropy, lse):
+            assert t is None or (t.numel() == n and t.dtype == torch.float32)
+        k = 0 if top_ids is None else top_ids.shape[1]
+        assert (top_ids is None) == (top_logp is None)
+        assert top_ids is None or (top_ids.shape == top_logp.shape == (n, k) and top_ids.dtype == torch.int64
+                                   and top_logp.dtype == torch.float32)
+        self._check(_lib.recd_vocab_answers(self._h, n, table.shape[0], D, _DT[x.dtype], _ptr(x), _ptr(table), scale, _ptr(given), k,
+                                            _ptr(logp), _ptr(entropy), _ptr(lse), _ptr(top_ids), _ptr(top_logp)))
