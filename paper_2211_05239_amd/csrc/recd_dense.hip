@@ -633,8 +633,10 @@ struct BackwardPlan {
     {
         WsCarver c(ws);
         const size_t e = elem_size(a->dtype);
-        need_gz = a->act != RECD_ACT_NONE || masked;
-        again = a->act != RECD_ACT_NONE && !sums;
+        // (without rows the gradients of w and bias are zero, and nothing is needed for them)
+        grad_x = grad_x && a->n > 0;
+        need_gz = a->n > 0 && (a->act != RECD_ACT_NONE || masked);
+        again = a->n > 0 && a->act != RECD_ACT_NONE && !sums;
         gz = need_gz && (grad_x || grad_w) ? c.take<char>((size_t)a->n * a->out * e) : nullptr;
         wt = grad_x ? c.take<char>((size_t)a->in * a->out * e) : nullptr;
         size_t parts = 0;
@@ -654,8 +656,8 @@ struct BackwardPlan {
                 parts = larger(parts, (size_t)gw.splits * a->out * a->in);
         }
         part = parts ? c.take<float>(parts) : nullptr;
-        col_blocks = again && z.splits == 1 ? (a->n + z.side - 1) / z.side : rows_shape(ctx, a->n, a->out).blocks;
-        col_part = grad_bias ? c.take<float>((size_t)col_blocks * a->out) : nullptr;
+        col_blocks = a->n == 0 ? 0 : again && z.splits == 1 ? (a->n + z.side - 1) / z.side : rows_shape(ctx, a->n, a->out).blocks;
+        col_part = grad_bias && a->n > 0 ? c.take<float>((size_t)col_blocks * a->out) : nullptr;
         *bytes = c.off;
     }
 };
@@ -828,7 +830,7 @@ recd_status recd_dense_backward(recd_ctx *ctx, const recd_dense_layer *a, const 
             }
         }
         if (grad_bias)
-            hipLaunchKernelGGL(k_join_columns, dim3((unsigned)((out + 31) / 32)), dim3(1024), 0, st, a->n > 0 ? plan.col_blocks : 0, out,
+            hipLaunchKernelGGL(k_join_columns, dim3((unsigned)((out + 31) / 32)), dim3(1024), 0, st, plan.col_blocks, out,
                                plan.col_part, grad_bias);
         if (a->n > 0 && grad_x) {
             hipLaunchKernelGGL((k_transpose<T>), dim3((unsigned)((in + 63) / 64), (unsigned)((out + 63) / 64)), dim3(kBlock), 0, st, out, in,

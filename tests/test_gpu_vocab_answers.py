@@ -1,0 +1,274 @@
+"""Answers against a table (log probabilities, entropy, the most likely ids) against 64 bits, and what the calls refuse."""
+import math
+
+import pytest
+import torch
+
+from tests import dense_util as du
+from tests import layers_util as lu
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def recd():
+    from paper_2211_05239_amd import recd as mod
+    return mod
+
+
+@pytest.fixture(scope="module")
+def ctx(recd):
+    c = recd.Context(0)
+    yield c
+    c.close()
+
+
+def data(n, V, D, dt, seed, std=1.5):
+    x, table = du.rand((n, D), dt, seed), du.rand((V, D), dt, seed + 1, std / D ** 0.5)
+    given = torch.randint(0, V, (n,), generator=torch.Generator().manual_seed(seed + 2))
+    given[::5] = -1
+    given[1::7] = V - 1
+    return x, table, given
+
+
+def run(ctx, x, table, scale, given, k):
+    n, nan = len(x), float("nan")
+    got = {t: torch.full((n,), nan, device="cuda") for t in ("logp", "entropy", "lse")}
+    got["top_logp"], ids = torch.full((n, k), nan, device="cuda"), torch.full((n, k), -7, dtype=torch.int64, device="cuda")
+    ctx.vocab_answers(x.cuda(), table.cuda(), scale, given.cuda(), got["logp"], got["entropy"], got["lse"], ids if k else None, got["top_logp"] if k else None)
+    torch.cuda.synchronize()
+    return got, ids.cpu()
+
+
+def check(ctx, x, table, scale, given, k, z=None):
+    ref, want = lu.answers_ref(x, table, scale, given, k, z)
+    got, ids = run(ctx, x, table, scale, given, k)
+    for t, v in got.items():
+        du.within(v, *ref[t], what=t)
+    assert torch.equal(ids, want)
+    return got, ids
+
+
+# rows: few (one, tiles' edges) and many; tables: one row, a chunk's edges, four chunks' edges, several splits; k: none to all
+@pytest.mark.parametrize("dt", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("n,V,D,k", [(1, 1, 16, 1), (1, 63, 64, 63), (33, 64, 24, 64), (5, 65, 128, 0), (64, 129, 40, 5), (65, 1000, 96, 64),
+                                     (128, 257, 128, 1), (129, 999, 72, 10), (256, 640, 192, 7), (257, 255, 64, 8), (300, 4097, 64, 64),
+                                     (300, 257, 256, 1), (40, 3001, 256, 50), (700, 1640, 200, 12), (2, 20_000, 32, 64), (3, 30, 8, 30)])
+def test_sizes(ctx, dt, n, V, D, k):
+    check(ctx, *(lambda x, t, g: (x, t, 1.0, g))(*data(n, V, D, dt, n + V)), k)
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [50, 300])
+@pytest.mark.parametrize("scale", [-0.7, 0.02, 30.0])
+def test_scales(ctx, dt, n, scale):
+    """A negative scale turns the order round; a large one leaves one id with nearly all of the weight."""
+    x, table, given = data(n, 1500, 64, dt, 9)
+    check(ctx, x, table, scale, given, 9)
+
+
+@pytest.mark.parametrize("n", [3, 260])
+def test_neighbours_in_rank_that_32_bits_do_not_tell_apart(ctx, n):
+    """Rows of the table that differ by 2^-23 of one element: 32-bit sums round the difference away, the order is that of 64 bits."""
+    x = du.rand((n, 64), "f32", 1)
+    x[:, 0] = 1.0
+    table = du.rand((3000, 64), "f32", 2, 0.1)
+    near = torch.randperm(3000, generator=torch.Generator().manual_seed(3))[:200]
+    table[near] = du.rand((1, 64), "f32", 4, 0.1) + 3.0 * x[:1] / 64
+    table[near, 0] = 1.0 + torch.arange(200) * 2.0 ** -23
+    x[:] = x[:1]
+    x[1:, 5] += 0.01
+    _, ids = check(ctx, x, table, 1.0, torch.zeros(n, dtype=torch.int64), 64)
+    assert torch.equal(ids[0], near.flip(0)[:64])
+
+
+@pytest.mark.parametrize("n", [3, 260])
+def test_of_equal_logits_the_lowest_id_comes_first(ctx, n):
+    """Many copies of one row, over many chunks; and rows x of zeros, whose logits are all equal."""
+    x, table, given = data(n, 5000, 40, "bf16", 5)
+    best = table[(x[:1].double() @ table.double().t()).argmax()].clone()
+    table[torch.randperm(5000, generator=torch.Generator().manual_seed(3))[:700]] = best
+    x[1] = 0.0
+    _, ids = check(ctx, x, table, 1.0, given, 33)
+    assert torch.equal(ids[1], torch.arange(33))
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_a_table_of_one_row_over_and_over(ctx, dt):
+    """All chunks may hold the best: more of them than are listed at a time (1024 chunks are 65 536 rows)."""
+    x = du.rand((3, 16), dt, 1)
+    table = du.rand((1, 16), dt, 2).expand(150_000, 16).contiguous()
+    _, ids = run(ctx, x, table, 1.0, torch.zeros(3, dtype=torch.int64), 64)
+    assert torch.equal(ids, torch.arange(64).expand(3, 64))
+    table[149_999] += x[0] / 8
+    table[70_001] -= x[0] / 8
+    got, ids = run(ctx, x, table, 1.0, torch.zeros(3, dtype=torch.int64), 64)
+    assert ids[0].tolist() == [149_999] + list(range(63))
+    assert (got["entropy"].double().cpu() - math.log(150_000)).abs().max() < 1e-3
+
+
+def test_certain_answers(ctx):
+    """One id with all of the weight but 2^-10 to 2^-40 of it: the entropy is what is left, without cancellation."""
+    table = torch.zeros(500, 4)
+    table[77, 0] = 1.0
+    x = torch.zeros(31, 4)
+    x[:, 0] = torch.arange(10, 41) * math.log(2.0)
+    check(ctx, x, table, 1.0, torch.full((31,), 77), 2)
+
+
+@pytest.mark.parametrize("n", [30, 300])
+def test_rows_and_tables_that_are_not_finite(ctx, n):
+    """A row stays by itself; a NaN among the logits counts as -infinity in the order, and every call ends."""
+    x, table, given = data(n, 2000, 32, "f32", 7)
+    want, ids = run(ctx, x, table, 1.0, given, 8)
+    bad = x.clone()
+    bad[3, 5], bad[4, 0], bad[5] = float("nan"), float("inf"), -float("inf")
+    got, jds = run(ctx, bad, table, 1.0, given, 8)
+    rows = torch.ones(n, dtype=torch.bool)
+    rows[3:6] = False
+    assert torch.equal(ids[rows], jds[rows])
+    for k in want:
+        assert du.same_bits(got[k][rows.cuda()], want[k][rows.cuda()]), k
+    assert torch.equal(jds[3], torch.arange(8)) and not got["lse"][3:6].isfinite().any()
+    assert ((jds >= 0) & (jds < 2000)).all()
+    hole = table.clone()
+    hole[11] = float("nan")
+    got, jds = run(ctx, x, hole, 1.0, given, 8)
+    assert not (jds == 11).any() and ((jds >= 0) & (jds < 2000)).all()
+    z = lu.logits(x, table, 1.0)
+    z[:, 11] = -math.inf
+    assert torch.equal(jds[:, 0], z.argmax(1))
+
+
+def test_values_near_the_ends_of_the_range(ctx):
+    """Logits so small that their products underflow, and sums that could pass the range: k different ids all the same."""
+    for size in (1e-30, 1e-20, 1e18, 1e25):
+        x, table, given = data(20, 700, 16, "f32", 3)
+        got, ids = run(ctx, x * size, table * size, 1.0, given, 20)
+        assert all(len(set(r)) == 20 and 0 <= min(r) and max(r) < 700 for r in ids.tolist()), size
+
+
+@pytest.mark.parametrize("n", [4, 300])
+def test_what_is_left_out(recd, ctx, n):
+    x, table, given = data(n, 3000, 64, "bf16", 8)
+    want, ids = run(ctx, x, table, 1.0, given, 5)
+    x, table, given = x.cuda(), table.cuda(), given.cuda()
+    one = torch.empty(n, device="cuda")
+    for name, at in (("entropy", 5), ("lse", 6)):
+        args = [x, table, 1.0, None, None, None, None, None, None]
+        args[at] = one.fill_(7.0)
+        ctx.vocab_answers(*args)
+        assert du.same_bits(one, want[name])
+    ctx.vocab_answers(x, table, 1.0, given, one)
+    assert du.same_bits(one, want["logp"])
+    top, logs = torch.empty(n, 5, dtype=torch.int64, device="cuda"), torch.empty(n, 5, device="cuda")
+    ctx.vocab_answers(x, table, 1.0, top_ids=top, top_logp=logs)
+    assert torch.equal(top.cpu(), ids) and du.same_bits(logs, want["top_logp"])
+    ctx.vocab_answers(x, table, 1.0)
+
+
+def test_log_probabilities_are_the_losses(recd, ctx):
+    """Beside call 29 on the same rows: both are off by what 32-bit sums are."""
+    x, table, given = data(400, 3000, 64, "f16", 4)
+    got, _ = run(ctx, x, table, 1.0, given, 0)
+    loss, lse = torch.empty(400, device="cuda"), torch.empty(400, device="cuda")
+    ctx.vocab_loss(x.cuda(), table.cuda(), given.cuda(), 1.0, loss, lse)
+    ref, _ = lu.answers_ref(x, table, 1.0, given, 0)
+    for a, b, k in ((loss, -got["logp"], "logp"), (lse, got["lse"], "lse")):
+        assert ((a - b).abs().double().cpu() <= 2 * ref[k][1] + 4 * du.E * ref[k][0].abs()).all()
+
+
+@pytest.mark.parametrize("V", [8, 300])
+def test_given_ids_beyond_the_table(recd, ctx, V):
+    x, table, given = data(20, V, 32, "f32", 6)
+    given[3] = V
+    check(ctx, x, table, 1.0, given, 3)
+    c = recd.Context(0)
+    c.set_option(recd.RECD_OPT_VALIDATE, 1)
+    with pytest.raises(recd.RecdError) as e:
+        run(c, x, table, 1.0, given, 3)
+    assert e.value.status == recd.RECD_EBOUNDS
+    given[3] = -5
+    check(c, x, table, 1.0, given, 3)
+    c.close()
+
+
+def test_streams_graphs_and_larger_calls_between(recd):
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        V, D, k, many = 4000, 64, 10, 3000
+        x, table, given = (t.cuda() for t in data(many, V, D, "bf16", 3))
+        c = recd.Context(0, workspace_hint_bytes=max(recd.vocab_answers_workspace_bytes(m, V, D, x.dtype, k) for m in (40, many)))
+
+        def outputs(m):
+            return [torch.zeros(m, device="cuda") for _ in range(3)] + [torch.zeros(m, k, dtype=torch.int64, device="cuda"), torch.zeros(m, k, device="cuda")]
+
+        def work(m, o):
+            c.vocab_answers(x[:m], table, 1.0, given[:m], *o)
+
+        small, want, large = outputs(40), outputs(40), outputs(many)
+        work(40, want)
+        s.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            work(40, small)
+        for _ in range(3):
+            work(many, large)
+            for o in small:
+                o.fill_(-1)
+            graph.replay()
+            s.synchronize()
+            for a, b in zip(small, want):
+                assert torch.equal(a, b)
+        assert torch.equal(large[3][:40], want[3])
+        c.close()
+
+
+@pytest.mark.parametrize("n,V,D,k", [(40, 300_000, 64, 10), (3000, 40_000, 64, 4), (9000, 1_000_003, 8, 1), (300_000, 100, 8, 0)])
+def test_workspace(recd, n, V, D, k):
+    dtype = torch.bfloat16
+    x, table = torch.zeros(n, D, dtype=dtype, device="cuda"), torch.randn(V, D, device="cuda").to(dtype)
+    x[:, 0] = 1.0
+    lse = torch.empty(n, device="cuda")
+    ids, logs = (torch.empty(n, k, dtype=torch.int64, device="cuda"), torch.empty(n, k, device="cuda")) if k else (None, None)
+
+    def use(c):
+        c.vocab_answers(x, table, 1.0, None, None, None, lse, ids, logs)
+
+    want = recd.vocab_answers_workspace_bytes(n, V, D, dtype, k)
+
+    def taken(hint, use):
+        torch.cuda.synchronize()
+        before = torch.cuda.mem_get_info()[0]
+        c = recd.Context(0, workspace_hint_bytes=hint)
+        use(c)
+        torch.cuda.synchronize()
+        after = torch.cuda.mem_get_info()[0]
+        c.close()
+        return before - after
+
+    taken(0, use)  # (kernels are loaded)
+    held = taken(want, use)
+    assert held == taken(want, lambda c: None)
+    assert abs(held - taken(0, use)) <= 1 << 21  # (memory is handed out in pieces of this size)
+    assert torch.equal(lse, lse[:1].expand(n)) or k  # (rows of several turns)
+    if k:
+        assert torch.equal(ids, ids[:1].expand(n, k))
+
+
+def test_refusals(recd, ctx):
+    lib, h, bad = recd._lib, ctx._h, recd.RECD_EINVAL
+    t = torch.zeros(64 * 64, device="cuda")
+    p = t.data_ptr()
+
+    def call(n=4, V=8, D=64, dt=0, x=p, table=p, scale=1.0, given=None, k=0, logp=None, entropy=None, lse=None, ids=None, logs=None):
+        return lib.recd_vocab_answers(h, n, V, D, dt, x, table, scale, given, k, logp, entropy, lse, ids, logs)
+
+    assert call(n=-1) == bad and call(V=-1) == bad and call(D=3) == bad and call(D=260) == bad and call(dt=3) == bad and call(V=0) == bad
+    for scale in (0.0, float("inf"), float("nan")):
+        assert call(scale=scale) == bad
+    assert call(k=9, ids=p, logs=p) == bad and call(k=-1) == bad and call(V=80, k=65, ids=p, logs=p) == bad
+    assert call(k=2, ids=p) == bad and call(k=2, logs=p) == bad and call(given=p) == bad and call(logp=p) == bad
+    assert call(x=None) == bad and call(table=None) == bad and call(x=p + 4) == bad and call(table=p + 8) == bad
+    assert b"aligned" in lib.recd_last_error(h)
+    assert call(n=0, x=None, table=None) == recd.RECD_OK
