@@ -726,7 +726,7 @@ recd_status recd_dense(recd_ctx *ctx, const recd_dense_layer *a, const void *x, 
  *     grad_y: device [n, out].   grad_x: device [n, in].   grad_w: device [out, in], dense, of dtype, overwritten.
  *     grad_bias: device fp32 [out], overwritten.  Each of the three may be NULL; none may be an input.
  *     gz is rounded to dtype where it enters the products.
- *     Workspace: gz [n, out], w transposed, sums of splits (call 35), and column sums of blocks of rows. */
+ *     Workspace: gz [n, out] (with an activation or dropout), sums of splits (call 35), and column sums of blocks of rows. */
 recd_status recd_dense_backward(recd_ctx *ctx, const recd_dense_layer *a, const void *x, const void *w, const float *bias,
                                 const float *sums, const void *grad_y, int64_t grad_y_stride, void *grad_x,
                                 int64_t grad_x_stride, void *grad_w, float *grad_bias);

@@ -3,9 +3,9 @@
 //   z = x w^T + bias,  y = residual + dropout(act(z))
 //   gz = dropout'(grad_y) act'(z),  grad_x = gz w,  grad_w = gz^T x,  grad_bias = sum over rows of gz
 //
-// Every product is C[i, j] = sum over k of P[i, k] Q[j, k], either with both operands' rows along k (the layer itself and, with w
-// transposed into the workspace, grad_x), or with both along i and j (grad_w, which sums over the rows).  Blocks stage
-// tiles of both through registers into two buffers of LDS; a wave multiplies TI x TJ tiles of 32 x 32 on the matrix cores, features
+// Every product is C[i, j] = sum over k of P[i, k] Q[j, k].  An operand's rows in memory run along k (both of the layer itself), or along i
+// or j (w for grad_x, both for grad_w, which sums over the rows).  Tiles of both go into LDS by loads that write there, a step
+// ahead; a wave multiplies TI x TJ tiles of 32 x 32 on the matrix cores, features
 // as the product's rows and rows of x as its columns, so that a lane ends up with four neighbouring features of one row.  The sums go
 // through LDS once more: bias, activation, dropout, residual and the store work on eight neighbouring features a lane.
 #include "recd_epilogue.h"
@@ -44,10 +44,23 @@ struct ProductArgs {
     Epilogue e;
 };
 
-// Eight (`count`) sums of row `row` from column `col` on.  `b`: the columns' bias.
+// Eight neighbouring elements of a row, as they lie in memory.
+template <typename T> struct Eight {
+    typename RecdPiece<T>::type piece[sizeof(T) / 2];
+    __device__ inline void load(const char *at, int count)
+    {
+        using Piece = typename RecdPiece<T>::type;
+        piece[0] = *reinterpret_cast<const Piece *>(at);
+        if constexpr (sizeof(T) == 4)
+            piece[1] = count == 8 ? *reinterpret_cast<const Piece *>(at + 16) : Piece{};
+    }
+    __device__ inline float operator[](int e) const { return (float)piece[e * (int)sizeof(T) / 16][e % (16 / (int)sizeof(T))]; }
+};
+
+// Eight (`count`) sums of row `row` from column `col` on.  `b`: the columns' bias, `other`: the residual's or grad_y's elements.
 template <typename T, int KIND>
 __device__ inline void finish(const Epilogue &e, uint64_t call, int64_t row, int col, int count, int n_j, const float *b, float *z,
-                              float *col_sum)
+                              const Eight<T> &other, float *col_sum)
 {
     float v[8];
     if constexpr (KIND == FORWARD) {
@@ -59,15 +72,14 @@ __device__ inline void finish(const Epilogue &e, uint64_t call, int64_t row, int
         recd_activate(e.act, v);
         if (e.mask.cut)
             recd_mask_apply(e.mask, recd_mask_bits(e.mask, call, e.row0 + row, col >> 3), v);
-        if (e.other) {
-            float r[8];
-            recd_load8(reinterpret_cast<const T *>(reinterpret_cast<const char *>(e.other) + row * e.other_stride) + col, count, r);
+        if (e.other)
 #pragma unroll
             for (int i = 0; i < 8; i++)
-                v[i] += r[i];
-        }
+                v[i] += other[i];
     } else if constexpr (KIND == GRAD) {
-        recd_load8(reinterpret_cast<const T *>(reinterpret_cast<const char *>(e.other) + row * e.other_stride) + col, count, v);
+#pragma unroll
+        for (int i = 0; i < 8; i++)
+            v[i] = other[i];
         if (e.mask.cut)
             recd_mask_apply(e.mask, recd_mask_bits(e.mask, call, e.row0 + row, col >> 3), v);
         if (e.act != RECD_ACT_NONE) {
@@ -101,82 +113,146 @@ __device__ inline void load_bias(const float *bias, int col, int count, float *b
                 b[i] = bias[col + i];
 }
 
-// Tiles of one operand from memory through registers into LDS.  COLS: rows of a tile are k, of SIDE columns; else rows are
-// the SIDE rows, of BK elements along k, and row f of 32 stands where it is row f of the product (recd_tile_row).  Rows and
-// columns behind the operand's end are read from the last one's place: what comes of them is not stored.  Places
-// behind k's end are zero.
-template <typename T, bool COLS, int SIDE, int BK, int THREADS> struct Loader {
-    using Tile = typename std::conditional<COLS, RecdTile<T, BK, SIDE>, RecdTile<T, SIDE, BK>>::type;
-    using Piece = typename Tile::Piece;
-    static constexpr int E = Tile::E, PR = (COLS ? SIDE : BK) / E, PT = Tile::PIECES / THREADS;
-    static_assert(Tile::PIECES % THREADS == 0, "whole pieces a thread");
-    Piece held[PT];
+// A quarter of a step of the contraction: 16 bytes of k of a row in each half wave.
+template <typename T> struct Quarter {
+    using Frag = typename RecdMma<T>::Frag;
+    static __device__ inline recd_f32x16 mul(Frag a, Frag b, recd_f32x16 c) { return RecdMma<T>::mul(a, b, c); }
+};
+template <> struct Quarter<float> {
+    using Frag = recd_f32x4;
+    static __device__ inline recd_f32x16 mul(Frag a, Frag b, recd_f32x16 c)
+    {
+#pragma unroll
+        for (int e = 0; e < 4; e++)
+            c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], b[e], c, 0, 0, 0);
+        return c;
+    }
+};
+
+// Tiles of one operand, two of them in LDS, which the loads write to by themselves.  COLS: a tile's rows are BK values of k, of SIDE
+// columns; else they are the SIDE rows, of BK elements along k (128 bytes: shorter ones ask the L2 twice for each line).  Rows and columns behind the operand's end are read
+// from the last one's place: what comes of them is not stored.
+//
+// A load of a wave fills 1024 bytes of LDS in its lanes' order; which 16 bytes of memory a lane brings is free.  So that the
+// lanes that read at a time meet in no bank, piece c of row r stands at place c ^ (r >> 1 & 7) of the row (reads of one piece from 16 rows), and
+// with COLS 64-byte segment s at place s ^ (r & 3 ^ r >> 2 & 2) (transposing reads take a segment of four rows at a time; 32-bit ones two
+// segments of rows 4 apart, with r >> 1); rows of 128 bytes, two segments of which take the banks, at place s ^ (r >> 1 & 1).
+template <typename T, bool COLS, int SIDE, int WAVES> struct Operand {
+    using Piece = typename RecdPiece<T>::type;
+    using Frag = typename Quarter<T>::Frag;
+    static constexpr int E = 16 / sizeof(T), BK = 128 / sizeof(T), BYTES = SIDE * 128, ROW = COLS ? SIDE * (int)sizeof(T) : 128;
+    static constexpr int PT = BYTES / 1024 / WAVES;  // loads of a wave
+    static_assert(BYTES % (1024 * WAVES) == 0, "whole loads a wave");
     uint32_t off[PT];
     const char *base;
 
-    // `first`: the first row's (COLS: column's) element at the first k
-    __device__ inline void begin(int tid, const void *first, uint32_t stride, int left)
+    static __device__ inline int turn(int r)
     {
-        base = reinterpret_cast<const char *>(first);
+        if constexpr (!COLS)
+            return r >> 1 & 7;
+        else if constexpr (ROW == 128)
+            return (r >> 1 & 1) << 2;
+        else
+            return ((r & 3) ^ (sizeof(T) == 4 ? r >> 1 & 2 : r >> 2 & 2)) << 2;
+    }
+    // row and piece of a lane's bytes of the wave's load i
+    static __device__ inline void place(int wave, int lane, int i, int &r, int &c)
+    {
+        const int at = (wave * PT + i) * 1024 + lane * 16;
+        r = at / ROW;
+        c = (at % ROW / 16) ^ turn(r);
+    }
+    // `first`: the first row's (COLS: column's) element at the first k; `left` rows (columns) are there
+    __device__ inline void begin(int wave, int lane, const char *first, uint32_t stride, int left)
+    {
+        base = first;
 #pragma unroll
         for (int i = 0; i < PT; i++) {
-            const int r = (tid + i * THREADS) / PR, c = (tid + i * THREADS) % PR;
+            int r, c;
+            place(wave, lane, i, r, c);
             if constexpr (COLS)
                 off[i] = (uint32_t)r * stride + 16u * (uint32_t)(c * E < left ? c : left / E - 1);
             else
                 off[i] = (uint32_t)(r < left ? r : left - 1) * stride + 16u * (uint32_t)c;
         }
     }
-    // `k_left` > 0: what is left of k from this tile on
-    __device__ inline void load(int tid, uint32_t stride, int64_t k_left)
+    __device__ inline void step(uint32_t stride) { base += COLS ? (int64_t)BK * stride : 128; }
+    // the wave's load i of a tile, all of which is there: waited for by vmcnt
+    __device__ inline void send(char *to, int wave, int i) const
     {
-        if (k_left >= BK) {
-#pragma unroll
-            for (int i = 0; i < PT; i++)
-                held[i] = *reinterpret_cast<const Piece *>(base + off[i]);
-        } else {
-#pragma unroll
-            for (int i = 0; i < PT; i++) {
-                const int r = (tid + i * THREADS) / PR, c = (tid + i * THREADS) % PR;
-                const bool in = COLS ? r < k_left : c * E < k_left;
-                const uint32_t back = COLS ? (uint32_t)r * stride : 16u * (uint32_t)c;
-                held[i] = *reinterpret_cast<const Piece *>(base + (in ? off[i] : off[i] - back));
-                if (!in)
-                    held[i] = Piece{};
-            }
-        }
-        base += COLS ? (int64_t)BK * stride : (int64_t)BK * sizeof(T);
+        using Global = const __attribute__((address_space(1))) void;
+        using Local = __attribute__((address_space(3))) void;
+        __builtin_amdgcn_global_load_lds((Global *)(base + off[i]), (Local *)(to + (wave * PT + i) * 1024), 16, 0, 0);
     }
-    __device__ inline void store(int tid, Tile &t)
+    // the last tile, of which `k_left` > 0 are there and zeros stand behind them: through registers
+    __device__ inline void bring(char *to, int wave, int lane, uint32_t stride, int k_left)
     {
 #pragma unroll
         for (int i = 0; i < PT; i++) {
-            const int r = (tid + i * THREADS) / PR, c = (tid + i * THREADS) % PR;
-            t.put_at(COLS ? r : (r & ~31) | recd_tile_row(r & 31), c * E, held[i]);
+            int r, c;
+            place(wave, lane, i, r, c);
+            const bool in = COLS ? r < k_left : c * E < k_left;
+            const uint32_t back = COLS ? (uint32_t)r * stride : 16u * (uint32_t)c;
+            Piece v = *reinterpret_cast<const Piece *>(base + (in ? off[i] : off[i] - back));
+            if (!in)
+                v = Piece{};
+            *reinterpret_cast<Piece *>(to + (wave * PT + i) * 1024 + lane * 16) = v;
+        }
+    }
+    // rows (columns) side .. side + 32 as the product has them, a quarter of the tile's k: 16 bytes of it in each half wave
+    static __device__ inline Frag fragment(const char *from, int side, int quarter, int lane)
+    {
+        const int k = quarter * BK / 4 + (lane >> 5) * E;
+        if constexpr (!COLS) {
+            const int r = side + (lane & 31);
+            return *reinterpret_cast<const Piece *>(from + r * ROW + 16 * ((k / E) ^ turn(r)));
+        } else if constexpr (sizeof(T) == 4) {
+            Frag f;
+            const int col = side + (lane & 31);
+#pragma unroll
+            for (int e = 0; e < E; e++)
+                f[e] = *reinterpret_cast<const T *>(from + (k + e) * ROW + 16 * ((col / E) ^ turn(k + e)) + 4 * (col % E));
+            return f;
+        } else {
+            // 16 lanes name four rows of 16 columns, 8 bytes each; each of them receives one column
+            using Half4 = __attribute__((address_space(3))) recd_s16x4;
+            const int i = lane & 15, col = side + 16 * (lane >> 4 & 1) + 4 * (i & 3);
+            union {
+                recd_s16x4 four[2];
+                Frag f;
+            } u;
+#pragma unroll
+            for (int h = 0; h < 2; h++) {
+                const int r = k + 4 * h + (i >> 2);
+                u.four[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Half4 *)(from + r * ROW + 16 * ((col / E) ^ turn(r)) + 2 * (col % E)));
+            }
+            return u.f;
         }
     }
 };
 
-template <typename Tile, bool COLS> __device__ inline auto fragment(const Tile &t, int side, int k, int lane)
+// The wave's loads into LDS, but for the last N, have arrived and its LDS reads and writes are done, and that holds for all waves of
+// the block.
+template <int N = 0> __device__ inline void arrive()
 {
-    if constexpr (COLS)
-        return t.columns(k, side, lane);
-    else
-        return t.rows(side, k, lane);
+    static_assert(N < 16);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_s_waitcnt(N | 7 << 4);  // vmcnt N, lgkmcnt 0
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 }
 
-template <typename T, bool COLS, int WI, int WJ, int TI, int TJ, int KIND>
+template <typename T, bool PCOLS, bool QCOLS, int WI, int WJ, int TI, int TJ, int KIND>
 __global__ __launch_bounds__(64 * WI * WJ) void k_product(ProductArgs a)
 {
-    constexpr int THREADS = 64 * WI * WJ, BI = 32 * WI * TI, BJ = 32 * WJ * TJ, BK = 128 / sizeof(T);
-    using Mma = RecdMma<T>;
-    using LoadP = Loader<T, COLS, BI, BK, THREADS>;
-    using LoadQ = Loader<T, COLS, BJ, BK, THREADS>;
-    constexpr int LDW = 32 * TJ + 4;
+    constexpr int THREADS = 64 * WI * WJ, BI = 32 * WI * TI, BJ = 32 * WJ * TJ;
+    using P = Operand<T, PCOLS, BI, WI * WJ>;
+    using Q = Operand<T, QCOLS, BJ, WI * WJ>;
+    constexpr int BK = P::BK, LDW = 32 * TJ + 4;
     __shared__ union {
         struct {
-            typename LoadP::Tile p[2];
-            typename LoadQ::Tile q[2];
+            alignas(16) char p[2][P::BYTES];
+            alignas(16) char q[2][Q::BYTES];
         } t;
         float out[WI * WJ][32 * LDW];
         float cols[WI][BJ];
@@ -191,7 +267,28 @@ __global__ __launch_bounds__(64 * WI * WJ) void k_product(ProductArgs a)
     const int ti = 8 * band + in_band % high, tj = in_band / high;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wi = wave / WJ, wj = wave % WJ;
     const int64_t i0 = (int64_t)ti * BI, k0 = split * a.k_each, k1 = k0 + a.k_each < a.K ? k0 + a.k_each : a.K;
-    const int j0 = tj * BJ;
+    const int j0 = tj * BJ, rows = a.n_i - i0 < BI ? (int)(a.n_i - i0) : BI;
+
+    // LPR lanes a row of the wave's columns, eight columns each, RP rows at a time
+    constexpr int LPR = 4 * TJ, RP = 64 / LPR, PASSES = 32 / RP;
+    const int piece = lane % LPR, col = j0 + 32 * TJ * wj + 8 * piece;
+    const int count = a.n_j - col >= 8 ? 8 : a.n_j - col;
+    const bool in = count > 0;
+    // the residual's or grad_y's elements of the wave's rows 32 i .. 32 i + 32, on their way before they are needed
+    Eight<T> other[PASSES];
+    const bool with_other = KIND != PLAIN && in && !a.part && a.e.other;
+    auto fetch = [&](int i) {
+        if (with_other)
+#pragma unroll
+            for (int pass = 0; pass < PASSES; pass++) {
+                const int r = 32 * (wi * TI + i) + pass * RP + lane / LPR;
+                if (r < rows)
+                    other[pass].load(reinterpret_cast<const char *>(a.e.other) + i0 * a.e.other_stride + (uint32_t)r * (uint32_t)a.e.other_stride +
+                                         (uint32_t)col * (uint32_t)sizeof(T),
+                                     count);
+            }
+    };
+    fetch(0);
 
     recd_f32x16 acc[TI][TJ];
 #pragma unroll
@@ -200,54 +297,97 @@ __global__ __launch_bounds__(64 * WI * WJ) void k_product(ProductArgs a)
         for (int j = 0; j < TJ; j++)
             acc[i][j] = recd_f32x16{};
     if (k0 < k1) {
-        LoadP lp;
-        LoadQ lq;
+        P lp;
+        Q lq;
         const uint32_t ps = (uint32_t)a.p_stride, qs = (uint32_t)a.q_stride;
-        const char *p = (const char *)a.p + (COLS ? k0 * a.p_stride + i0 * (int64_t)sizeof(T) : i0 * a.p_stride + k0 * (int64_t)sizeof(T));
-        const char *q = (const char *)a.q + (COLS ? k0 * a.q_stride + j0 * (int64_t)sizeof(T) : j0 * a.q_stride + k0 * (int64_t)sizeof(T));
-        lp.begin(tid, p, ps, a.n_i - i0 < BI ? (int)(a.n_i - i0) : BI);
-        lq.begin(tid, q, qs, a.n_j - j0 < BJ ? a.n_j - j0 : BJ);
-        const int64_t steps = (k1 - k0 + BK - 1) / BK;
-        lp.load(tid, ps, k1 - k0);
-        lq.load(tid, qs, k1 - k0);
-        lp.store(tid, lds.t.p[0]);
-        lq.store(tid, lds.t.q[0]);
-        __syncthreads();
-        for (int64_t s = 0; s < steps; s++) {
-            const int buf = (int)(s & 1);
-            if (s + 1 < steps) {
-                lp.load(tid, ps, k1 - k0 - (s + 1) * BK);
-                lq.load(tid, qs, k1 - k0 - (s + 1) * BK);
-            }
+        lp.begin(wave, lane, (const char *)a.p + (PCOLS ? k0 * a.p_stride + i0 * (int64_t)sizeof(T) : i0 * a.p_stride + k0 * (int64_t)sizeof(T)), ps, rows);
+        lq.begin(wave, lane, (const char *)a.q + (QCOLS ? k0 * a.q_stride + j0 * (int64_t)sizeof(T) : j0 * a.q_stride + k0 * (int64_t)sizeof(T)), qs,
+                 a.n_j - j0 < BJ ? a.n_j - j0 : BJ);
+        const int whole = (int)((k1 - k0) / BK), tail = (int)((k1 - k0) % BK), steps = whole + (tail ? 1 : 0);
+        // loads from .. to of the tile that comes next, which goes to place `buf`: first P's, then Q's
+        constexpr int LOADS = P::PT + Q::PT;
+        auto send = [&](int buf, int from, int to) {
 #pragma unroll
-            for (int k = 0; k < BK; k += 16) {
-                typename Mma::Frag pf[TI], qf[TJ];
+            for (int i = from; i < to; i++)
+                if (i < P::PT)
+                    lp.send(lds.t.p[buf], wave, i);
+                else
+                    lq.send(lds.t.q[buf], wave, i - P::PT);
+        };
+        auto sent = [&] {
+            lp.step(ps);
+            lq.step(qs);
+        };
+        auto bring = [&](int buf) {
+            lp.bring(lds.t.p[buf], wave, lane, ps, tail);
+            lq.bring(lds.t.q[buf], wave, lane, qs, tail);
+        };
+        typename Quarter<T>::Frag pf[2][TI], qf[2][TJ];
+        auto read = [&](int s, int quarter) {
+#pragma unroll
+            for (int i = 0; i < TI; i++)
+                pf[quarter & 1][i] = P::fragment(lds.t.p[s & 1], 32 * (wi * TI + i), quarter, lane);
+#pragma unroll
+            for (int j = 0; j < TJ; j++)
+                qf[quarter & 1][j] = Q::fragment(lds.t.q[s & 1], 32 * (wj * TJ + j), quarter, lane);
+        };
+        // A step: four quarters, whose fragments are read while the matrix cores have the quarter before.  Before the last one the
+        // next tile is there and this one has been read, whose place the next but one takes: its loads go out between the
+        // products of that quarter, as the matrix cores would wait for a row of them to be taken (8192^3: 1.02 PFLOP/s in a row, 1.24
+        // between; spread over two quarters some arrive late, 3 % less in the gradients).
+        auto step = [&](int s, auto more) {
+#pragma unroll
+            for (int quarter = 0; quarter < 4; quarter++) {
+                if (quarter < 3)
+                    read(s, quarter + 1);
+                else {
+                    arrive();
+                    if (s + 2 == whole && tail)
+                        bring(s & 1);
+                    read(s + 1, 0);  // (behind the last tile: what an older one left, for nobody)
+                }
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int i = 0; i < TI; i++)
-                    pf[i] = fragment<typename LoadP::Tile, COLS>(lds.t.p[buf], 32 * (wi * TI + i), k, lane);
 #pragma unroll
-                for (int j = 0; j < TJ; j++)
-                    qf[j] = fragment<typename LoadQ::Tile, COLS>(lds.t.q[buf], 32 * (wj * TJ + j), k, lane);
-#pragma unroll
-                for (int i = 0; i < TI; i++)
-#pragma unroll
-                    for (int j = 0; j < TJ; j++)
-                        acc[i][j] = Mma::mul(qf[j], pf[i], acc[i][j]);
+                    for (int j = 0; j < TJ; j++) {
+                        constexpr int MANY = TI * TJ;
+                        const int m = i * TJ + j;
+                        acc[i][j] = Quarter<T>::mul(qf[quarter & 1][j], pf[quarter & 1][i], acc[i][j]);
+                        __builtin_amdgcn_sched_barrier(0);
+                        if (more.value && quarter == 3) {
+                            send(s & 1, m * LOADS / MANY, (m + 1) * LOADS / MANY);
+                            __builtin_amdgcn_sched_barrier(0);
+                        }
+                    }
             }
-            if (s + 1 < steps) {
-                lp.store(tid, lds.t.p[1 - buf]);
-                lq.store(tid, lds.t.q[1 - buf]);
-            }
-            __syncthreads();
+        };
+        if (whole > 0) {
+            send(0, 0, LOADS);
+            sent();
+        } else
+            bring(0);
+        if (whole > 1) {
+            send(1, 0, LOADS);
+            sent();
+            arrive<LOADS>();
+        } else {
+            if (whole == 1 && tail)
+                bring(1);
+            arrive();
         }
+        read(0, 0);
+        int s = 0;
+        for (; s + 2 < whole; s++) {
+            step(s, std::true_type{});
+            sent();
+        }
+        for (; s < steps; s++)
+            step(s, std::false_type{});
+        arrive();
     }
 
-    // LPR lanes a row of the wave's columns
-    constexpr int LPR = 4 * TJ, RP = 64 / LPR;
     float *mine = lds.out[wave];
-    const int piece = lane % LPR, col = j0 + 32 * TJ * wj + 8 * piece;
-    const int count = a.n_j - col >= 8 ? 8 : a.n_j - col;
-    const bool in = count > 0;
     float b[8], col_sum[8];
     load_bias(KIND != PLAIN && in && !a.part ? a.e.bias : nullptr, col, count, b);
 #pragma unroll
@@ -264,20 +404,25 @@ __global__ __launch_bounds__(64 * WI * WJ) void k_product(ProductArgs a)
                 *reinterpret_cast<recd_f32x4 *>(mine + (lane & 31) * LDW + 32 * j + recd_sums_row(r, lane)) =
                     recd_f32x4{acc[i][j][r], acc[i][j][r + 1], acc[i][j][r + 2], acc[i][j][r + 3]};
         recd_wave_sync();
+        Eight<T> now[PASSES];
 #pragma unroll
-        for (int pass = 0; pass < 32 / RP; pass++) {
-            const int r = pass * RP + lane / LPR;
-            const int64_t row = i0 + 32 * (wi * TI + i) + r;
+        for (int pass = 0; pass < PASSES; pass++)
+            now[pass] = other[pass];
+        if (i + 1 < TI)
+            fetch(i + 1);
+#pragma unroll
+        for (int pass = 0; pass < PASSES; pass++) {
+            const int in_wave = pass * RP + lane / LPR, r = 32 * (wi * TI + i) + in_wave;
             float z[8];
 #pragma unroll
             for (int e = 0; e < 8; e += 4)
-                *reinterpret_cast<recd_f32x4 *>(z + e) = *reinterpret_cast<const recd_f32x4 *>(mine + r * LDW + 8 * piece + e);
-            if (!in || row >= a.n_i)
+                *reinterpret_cast<recd_f32x4 *>(z + e) = *reinterpret_cast<const recd_f32x4 *>(mine + in_wave * LDW + 8 * piece + e);
+            if (!in || r >= rows)
                 continue;
             if (a.part)
-                recd_store8(a.part + ((int64_t)split * a.n_i + row) * a.n_j + col, count, z);
+                recd_store8(a.part + ((int64_t)split * a.n_i + i0 + r) * a.n_j + col, count, z);
             else
-                finish<T, KIND>(a.e, call, row, col, count, a.n_j, b, z, col_sum);
+                finish<T, KIND>(a.e, call, i0 + r, col, count, a.n_j, b, z, now[pass], col_sum);
         }
     }
     if constexpr (KIND == GRAD) {
@@ -343,7 +488,10 @@ template <typename T, int KIND> __global__ __launch_bounds__(kBlock) void k_rows
                 }
             else if (a.z)
                 recd_load8(a.z + row * a.n_j + col, count, z);
-            finish<T, KIND>(a.e, call, row, col, count, a.n_j, b, z, col_sum);
+            Eight<T> other{};
+            if (KIND != PLAIN && a.e.other)
+                other.load(reinterpret_cast<const char *>(a.e.other) + row * a.e.other_stride + (int64_t)col * sizeof(T), count);
+            finish<T, KIND>(a.e, call, row, col, count, a.n_j, b, z, other, col_sum);
         }
     if constexpr (KIND == GRAD) {
         if (!a.e.col_part)
@@ -469,34 +617,10 @@ template <typename T, int RG> __global__ __launch_bounds__(64 * kFewWaves) void 
             z[e] += join[w][row][at + e];
     }
     load_bias(a.e.bias, col, count, b);
-    finish<T, FORWARD>(a.e, recd_mask_call(a.e.mask), row, col, count, a.n_j, b, z, nullptr);
-}
-
-// w [rows, cols] to wt [cols, rows], tiles of 64 x 64.
-template <typename T> __global__ __launch_bounds__(kBlock) void k_transpose(int rows, int cols, const T *__restrict__ w, T *__restrict__ wt)
-{
-    constexpr int E = 16 / sizeof(T), PR = 64 / E;
-    using Piece = typename RecdPiece<T>::type;
-    __shared__ T tile[64][64 + 2];
-    const int r0 = blockIdx.y * 64, c0 = blockIdx.x * 64;
-    for (int i = threadIdx.x; i < 64 * PR; i += kBlock) {
-        const int r = i / PR, c = i % PR * E;
-        if (r0 + r < rows && c0 + c < cols) {
-            const Piece v = *reinterpret_cast<const Piece *>(w + (int64_t)(r0 + r) * cols + c0 + c);
-            for (int e = 0; e < E; e++)
-                tile[r][c + e] = v[e];
-        }
-    }
-    __syncthreads();
-    for (int i = threadIdx.x; i < 64 * PR; i += kBlock) {
-        const int c = i / PR, r = i % PR * E;
-        if (c0 + c < cols && r0 + r < rows) {
-            Piece v;
-            for (int e = 0; e < E; e++)
-                v[e] = tile[r + e][c];
-            *reinterpret_cast<Piece *>(wt + (int64_t)(c0 + c) * rows + r0 + r) = v;
-        }
-    }
+    Eight<T> other{};
+    if (a.e.other)
+        other.load(reinterpret_cast<const char *>(a.e.other) + row * a.e.other_stride + (int64_t)col * sizeof(T), count);
+    finish<T, FORWARD>(a.e, recd_mask_call(a.e.mask), row, col, count, a.n_j, b, z, other, nullptr);
 }
 
 // ---- how a call is cut ---------------------------------------------------------------------------------------------
@@ -509,18 +633,43 @@ struct Shape {
     int64_t k_each, turn;  // rows of one launch
 };
 
-Shape product_shape(const recd_ctx *ctx, int64_t n_i, int n_j, int64_t K, recd_dtype dt)
+// What a tile of `side` costs on a compute unit, in us: a step of the contraction, and its beginning and end, for one block alone and
+// for each of those that share the unit (`resident` at a time).  `heavy`: with an activation or dropout at the end.
+struct Cost {
+    int side, resident;
+    float step_alone, step, ends_alone, ends, ends_heavy;
+};
+constexpr Cost kCost16[] = {{256, 1, 1.5f, 1.7f, 9.0f, 8.0f, 20.0f}, {128, 2, 0.6f, 0.52f, 3.0f, 3.5f, 5.0f}, {64, 4, 0.38f, 0.19f, 1.0f, 3.0f, 4.0f}};
+constexpr Cost kCost32[] = {{128, 2, 2.2f, 1.9f, 3.0f, 3.5f, 5.0f}, {64, 4, 0.75f, 0.5f, 1.0f, 3.0f, 4.0f}};
+
+// The tile and the number of splits of least cost: by rounds of blocks on the compute units, and with splits by the launch that adds
+// them up and its traffic (8 bytes a sum at about 4.5 TB/s).  Measured (us, 16 bits; side / splits): 16 384 x 8192 -> 1024, grad_w 256/1 434,
+// 256/2 283, 128/1 310, 64/1 445; 4096 x 2048 -> 2048 256/1 53, 128/1 40, 64/1 52; 512 x 4096 -> 1024 256/8 31, 128/4 20, 64/1 27, 64/2 16;
+// 128 x 8192 -> 1024 128/8 19, 64/1 55, 64/8 14.5; 300 007 x 128 -> 512 with GELU and dropout 256/1 243, 128/1 205.
+Shape product_shape(const recd_ctx *ctx, int64_t n_i, int n_j, int64_t K, recd_dtype dt, bool heavy)
 {
     const int bk = 128 / (int)elem_size(dt);
-    auto tiles = [&](int side) { return ((n_i + side - 1) / side) * ((n_j + side - 1) / side); };
+    const int64_t steps = (K + bk - 1) / bk;
     Shape s;
-    s.side = dt != RECD_F32 && tiles(256) >= ctx->num_cu ? 256 : tiles(128) >= ctx->num_cu ? 128 : 64;
-    const int64_t cus = 2 * ctx->num_cu, steps = (K + bk - 1) / bk;
+    s.side = 64;
     int64_t splits = 1;
-    if (tiles(s.side) < ctx->num_cu) {
-        splits = cus / tiles(s.side);
-        splits = splits < steps / 4 ? splits : steps / 4;
-        splits = splits < 1 ? 1 : splits > 256 ? 256 : splits;
+    double least = 1e30;
+    const Cost *costs = dt == RECD_F32 ? kCost32 : kCost16, *const end = costs + (dt == RECD_F32 ? 2 : 3);
+    for (; costs != end; costs++) {
+        const Cost &c = *costs;
+        const int64_t tiles = ((n_i + c.side - 1) / c.side) * ((n_j + c.side - 1) / c.side);
+        for (int64_t k = 1; k <= 256 && (k == 1 || 4 * k <= steps); k += k < 4 ? 1 : k / 2) {
+            const int64_t blocks = (tiles * k + ctx->num_cu - 1) / ctx->num_cu, each = (steps + k - 1) / k;
+            const double alone = (double)((blocks + c.resident - 1) / c.resident) * ((double)each * c.step_alone + c.ends_alone);
+            const double shared = (double)blocks * ((double)each * c.step + (heavy && k == 1 ? c.ends_heavy : c.ends));
+            const double join = k == 1 ? 0.0 : 5.0 + (double)k * (double)n_i * n_j * 8.0 / 4.5e6;
+            const double cost = (alone > shared ? alone : blocks == 1 ? alone : shared) + join;
+            if (cost < least) {
+                least = cost;
+                splits = k;
+                s.side = c.side;
+            }
+        }
     }
     const int64_t each = steps ? (steps + splits - 1) / splits : 1;
     s.k_each = each * bk;
@@ -535,7 +684,7 @@ Shape product_shape(const recd_ctx *ctx, int64_t n_i, int n_j, int64_t K, recd_d
     return s;
 }
 
-template <typename T, bool COLS, int KIND> void launch_product(ProductArgs a, const Shape &s, hipStream_t st)
+template <typename T, bool PCOLS, bool QCOLS, int KIND> void launch_product(ProductArgs a, const Shape &s, hipStream_t st)
 {
     const int64_t n = a.n_i;
     for (int64_t i0 = 0; i0 < n; i0 += s.turn) {
@@ -545,7 +694,7 @@ template <typename T, bool COLS, int KIND> void launch_product(ProductArgs a, co
         b.tiles_j = s.tiles_j;
         b.splits = s.splits;
         b.k_each = s.k_each;
-        b.p = (const char *)a.p + (COLS ? i0 * (int64_t)sizeof(T) : i0 * a.p_stride);
+        b.p = (const char *)a.p + (PCOLS ? i0 * (int64_t)sizeof(T) : i0 * a.p_stride);
         if (a.e.other)
             b.e.other = (const char *)a.e.other + i0 * a.e.other_stride;
         if (a.e.out)
@@ -558,11 +707,11 @@ template <typename T, bool COLS, int KIND> void launch_product(ProductArgs a, co
         const dim3 grid((unsigned)(((int64_t)b.tiles_i * b.tiles_j * b.splits + 7) / 8 * 8));
         if (s.side == 256) {
             if constexpr (sizeof(T) == 2)
-                hipLaunchKernelGGL((k_product<T, COLS, 2, 4, 4, 2, KIND>), grid, dim3(512), 0, st, b);
+                hipLaunchKernelGGL((k_product<T, PCOLS, QCOLS, 2, 4, 4, 2, KIND>), grid, dim3(512), 0, st, b);
         } else if (s.side == 128)
-            hipLaunchKernelGGL((k_product<T, COLS, 2, 2, 2, 2, KIND>), grid, dim3(256), 0, st, b);
+            hipLaunchKernelGGL((k_product<T, PCOLS, QCOLS, 2, 2, 2, 2, KIND>), grid, dim3(256), 0, st, b);
         else
-            hipLaunchKernelGGL((k_product<T, COLS, 2, 2, 1, 1, KIND>), grid, dim3(256), 0, st, b);
+            hipLaunchKernelGGL((k_product<T, PCOLS, QCOLS, 2, 2, 1, 1, KIND>), grid, dim3(256), 0, st, b);
     }
 }
 
@@ -607,13 +756,13 @@ struct ForwardPlan {
     Shape shape;
     float *part;
 
-    void make(const recd_ctx *ctx, const recd_dense_layer *a, char *ws, size_t *bytes)
+    void make(const recd_ctx *ctx, const recd_dense_layer *a, bool heavy, char *ws, size_t *bytes)
     {
         WsCarver c(ws);
         few = a->n <= kFewRows;
         part = nullptr;
         if (!few) {
-            shape = product_shape(ctx, a->n, a->out, a->in, a->dtype);
+            shape = product_shape(ctx, a->n, a->out, a->in, a->dtype, heavy);
             if (shape.splits > 1)
                 part = c.take<float>((size_t)shape.splits * a->n * a->out);
         }
@@ -625,7 +774,7 @@ struct BackwardPlan {
     bool need_gz, again;   // gz differs from grad_y; z is made again
     Shape z, gx, gw;
     int64_t col_blocks;
-    char *gz, *wt;
+    char *gz;
     float *part, *col_part;  // (one array of parts serves the products in turn)
 
     void make(const recd_ctx *ctx, const recd_dense_layer *a, bool masked, bool sums, bool grad_x, bool grad_w, bool grad_bias, char *ws,
@@ -638,20 +787,19 @@ struct BackwardPlan {
         need_gz = a->n > 0 && (a->act != RECD_ACT_NONE || masked);
         again = a->n > 0 && a->act != RECD_ACT_NONE && !sums;
         gz = need_gz && (grad_x || grad_w) ? c.take<char>((size_t)a->n * a->out * e) : nullptr;
-        wt = grad_x ? c.take<char>((size_t)a->in * a->out * e) : nullptr;
         size_t parts = 0;
         if (again) {
-            z = product_shape(ctx, a->n, a->out, a->in, a->dtype);
+            z = product_shape(ctx, a->n, a->out, a->in, a->dtype, true);
             if (z.splits > 1)
                 parts = larger(parts, (size_t)z.splits * a->n * a->out);
         }
         if (grad_x) {
-            gx = product_shape(ctx, a->n, a->in, a->out, a->dtype);
+            gx = product_shape(ctx, a->n, a->in, a->out, a->dtype, false);
             if (gx.splits > 1)
                 parts = larger(parts, (size_t)gx.splits * a->n * a->in);
         }
         if (grad_w) {
-            gw = product_shape(ctx, a->out, a->in, a->n, a->dtype);
+            gw = product_shape(ctx, a->out, a->in, a->n, a->dtype, false);
             if (gw.splits > 1)
                 parts = larger(parts, (size_t)gw.splits * a->out * a->in);
         }
@@ -709,7 +857,7 @@ recd_status recd_dense_workspace_bytes(int device, const recd_dense_layer *sizes
     if (sizes->n == 0)
         return RECD_OK;
     size_t forward, kept, again;
-    ForwardPlan().make(&c, sizes, nullptr, &forward);
+    ForwardPlan().make(&c, sizes, sizes->act != RECD_ACT_NONE || mask.cut, nullptr, &forward);
     BackwardPlan().make(&c, sizes, mask.cut != 0, true, true, true, true, nullptr, &kept);
     BackwardPlan().make(&c, sizes, mask.cut != 0, false, true, true, true, nullptr, &again);
     *out_bytes = larger(forward, larger(kept, again));
@@ -734,11 +882,11 @@ recd_status recd_dense(recd_ctx *ctx, const recd_dense_layer *a, const void *x, 
     RECD_HIP(ctx, hipSetDevice(ctx->device));
     ForwardPlan plan;
     size_t bytes;
-    plan.make(ctx, a, nullptr, &bytes);
+    plan.make(ctx, a, a->act != RECD_ACT_NONE || mask.cut, nullptr, &bytes);
     if (bytes) {
         ctx->plan.valid = false;  // the parts overwrite the workspace a backward plan would live in
         RECD_TRY(recd_reserve(ctx, bytes));
-        plan.make(ctx, a, ctx->ws, &bytes);
+        plan.make(ctx, a, a->act != RECD_ACT_NONE || mask.cut, ctx->ws, &bytes);
     }
     ProductArgs p{};
     p.n_i = a->n;
@@ -762,7 +910,7 @@ recd_status recd_dense(recd_ctx *ctx, const recd_dense_layer *a, const void *x, 
                 hipLaunchKernelGGL((k_few<T, 4>), grid, block, 0, ctx->stream, p);
             return;
         }
-        launch_product<T, false, FORWARD>(p, plan.shape, ctx->stream);
+        launch_product<T, false, false, FORWARD>(p, plan.shape, ctx->stream);
         if (plan.part) {
             RowsArgs r{a->n, a->out, 0, plan.shape.splits, plan.part, nullptr, 0, p.e};
             launch_rows<T, FORWARD>(ctx, r, ctx->stream);
@@ -822,7 +970,7 @@ recd_status recd_dense_backward(recd_ctx *ctx, const recd_dense_layer *a, const 
                 p.q_stride = in * e;
                 p.part = plan.z.splits > 1 ? plan.part : nullptr;
                 p.e = ep;
-                launch_product<T, false, GRAD>(p, plan.z, st);
+                launch_product<T, false, false, GRAD>(p, plan.z, st);
             }
             if (!plan.again || plan.z.splits > 1) {
                 RowsArgs r{a->n, out, 0, plan.again ? plan.z.splits : 1, plan.again ? plan.part : nullptr, plan.again ? nullptr : sums, 0, ep};
@@ -833,20 +981,18 @@ recd_status recd_dense_backward(recd_ctx *ctx, const recd_dense_layer *a, const 
             hipLaunchKernelGGL(k_join_columns, dim3((unsigned)((out + 31) / 32)), dim3(1024), 0, st, plan.col_blocks, out,
                                plan.col_part, grad_bias);
         if (a->n > 0 && grad_x) {
-            hipLaunchKernelGGL((k_transpose<T>), dim3((unsigned)((in + 63) / 64), (unsigned)((out + 63) / 64)), dim3(kBlock), 0, st, out, in,
-                               (const T *)w, (T *)plan.wt);
             ProductArgs p{};
             p.n_i = a->n;
             p.n_j = in;
             p.K = out;
             p.p = gz;
-            p.q = plan.wt;
+            p.q = w;
             p.p_stride = gz_stride;
-            p.q_stride = out * e;
+            p.q_stride = in * e;
             p.part = plan.gx.splits > 1 ? plan.part : nullptr;
             p.e.out = grad_x;
             p.e.out_stride = grad_x_stride * e;
-            launch_product<T, false, PLAIN>(p, plan.gx, st);
+            launch_product<T, false, true, PLAIN>(p, plan.gx, st);
             if (p.part) {
                 RowsArgs r{a->n, in, 0, plan.gx.splits, p.part, nullptr, 0, p.e};
                 launch_rows<T, PLAIN>(ctx, r, st);
@@ -864,7 +1010,7 @@ recd_status recd_dense_backward(recd_ctx *ctx, const recd_dense_layer *a, const 
             p.part = plan.gw.splits > 1 ? plan.part : nullptr;
             p.e.out = grad_w;
             p.e.out_stride = in * e;
-            launch_product<T, true, PLAIN>(p, plan.gw, st);
+            launch_product<T, true, true, PLAIN>(p, plan.gw, st);
             if (p.part) {
                 RowsArgs r{out, in, 0, plan.gw.splits, p.part, nullptr, 0, p.e};
                 launch_rows<T, PLAIN>(ctx, r, st);
