@@ -344,58 +344,49 @@ struct SelectArgs {
     int64_t *top_ids;
 };
 
-constexpr int kSelect = 1024, kListed = 1024, kAtOnce = 2 * kSelect / 64;
+constexpr int kGroups = 256, kListed = 1024;
 
-// <x, row> in 64 bits, products exact; the same order for every row.
-template <typename T> __device__ inline double dot64(const double *x, const T *row, int D)
-{
-    constexpr int E = 16 / sizeof(T);
-    double s = 0.0;
-    for (int d = 0; d < D; d += E) {
-        float v[E];
-        recd_load16(row + d, v);
-#pragma unroll
-        for (int e = 0; e < E; e++)
-            s = fma(x[d + e], (double)v[e], s);
-    }
-    return s;
-}
+// `a` before `b` in the answers' order.
+__device__ inline bool before(double za, uint32_t a, double zb, uint32_t b) { return za > zb || (za == zb && a < b); }
 
 // A block a row.  Let d be what a 32-bit logit may be off by.  At least k logits are as large as the k-th largest of 256 groups'
-// largest chunks, L: so the k best are at least L - d, and stand in chunks of at least L - 2d.  These chunks are gone through in
-// their order, kAtOnce at a time, a lane to a table row; what reaches the bar is kept, the k best of it after each time, which
-// raises the bar: of equal ones the first stays.
-template <typename T> __global__ __launch_bounds__(kSelect) void k_answers_select(SelectArgs a)
+// largest chunks, L: so the k best are at least L - d, and stand in chunks of at least L - 2d.  The logits of these chunks are
+// computed again, a row of the table by neighbouring lanes, in an order that is the same for all rows, and what reaches the bar is
+// kept.  Where there is no more room the k best of it stay, the last of which is the new bar.
+template <typename T, int NT> __global__ __launch_bounds__(NT) void k_answers_select(SelectArgs a, int llog)
 {
-    constexpr int KEPT = RECD_MAX_ANSWERS + kAtOnce * kChunk;
-    __shared__ double x[RECD_MAX_DENSE_D];
-    __shared__ double key[KEPT], sorted_key[RECD_MAX_ANSWERS];
-    __shared__ uint32_t id[KEPT], sorted_id[RECD_MAX_ANSWERS];
-    __shared__ float groups[kSelect / 4];
-    __shared__ uint32_t list[kListed], waves[kSelect / 64];
+    constexpr int WAVES = NT / 64, E = 16 / sizeof(T), KEPT = 2 * WAVES * kChunk < 1024 ? 1024 : 2 * WAVES * kChunk;
+    using Piece = typename RecdPiece<T>::type;
+    __shared__ double key[KEPT];
+    __shared__ uint32_t id[KEPT], list[kListed];
+    __shared__ float groups[NT];
     __shared__ double lse_all;
-    __shared__ float group_bar, abs_x[kSelect / 64];
-    __shared__ uint32_t count, listed, top_abs[kSelect / 64];
-    __shared__ int64_t next;
+    __shared__ float group_bar, abs_x[WAVES];
+    __shared__ uint32_t count, listed, taken, top_abs[WAVES];
     const int64_t row = blockIdx.x;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const T *xr = (const T *)a.x + row * a.D, *table = (const T *)a.table;
-    float ax = 0.0f;
-    for (int d = tid; d < a.D; d += kSelect) {
-        x[d] = (double)(float)xr[d];
-        ax += fabsf((float)xr[d]);
+    // the lane's piece of a row, and of x: products of two of them are exact in 64 bits
+    const int at = lane & ((1 << llog) - 1);
+    const bool has_piece = at * E < a.D;
+    double x[E];
+#pragma unroll
+    for (int e = 0; e < E; e++)
+        x[e] = 0.0;
+    if (has_piece) {
+        float v[E];
+        recd_load16(xr + at * E, v);
+#pragma unroll
+        for (int e = 0; e < E; e++)
+            x[e] = (double)v[e];
     }
-    uint32_t wide = 0;
-    for (int i = tid; i < a.widest_n; i += kSelect)
-        wide = max(wide, a.widest[i]);
-    for (int o = 32; o; o >>= 1) {
-        ax += __shfl_xor(ax, o);
-        wide = max(wide, (uint32_t)__shfl_xor((int)wide, o));
-    }
-    if (lane == 0) {
-        abs_x[wave] = ax;
-        top_abs[wave] = wide;
-    }
+    auto part = [&](const Piece &v) {
+        double z = 0.0;
+#pragma unroll
+        for (int e = 0; e < E; e++)
+            z = fma(x[e], (double)(float)v[e], z);
+        return z;
+    };
     if (wave == 0) {  // the splits' sums: a lane's in their order, then the lanes'
         Running all;
         for (int s = lane; s < a.splits; s += 64)
@@ -414,53 +405,72 @@ template <typename T> __global__ __launch_bounds__(kSelect) void k_answers_selec
                 a.entropy[row] = (float)(log((double)all.s) - 0.6931471805599453 * (double)all.t / (double)all.s);
         }
     }
-    __syncthreads();
-    if (wave == kSelect / 64 - 1 && a.given && a.logp) {
-        const int64_t g = a.given[row];
-        const bool has = g >= 0 && g < a.V;
-        double s = 0.0;
-        if (has)
-            for (int d = lane; d < a.D; d += 64)
-                s = fma(x[d], (double)(float)table[g * a.D + d], s);
-        for (int o = 32; o; o >>= 1)
-            s += __shfl_xor(s, o);
-        if (lane == 0)
-            a.logp[row] = has ? (float)(s * (double)a.scale - lse_all) : 0.0f;
+    float ax = 0.0f;
+    for (int d = tid; d < a.D; d += NT)
+        ax += fabsf((float)xr[d]);
+    uint32_t wide = 0;
+    for (int i = tid; i < a.widest_n; i += NT)
+        wide = max(wide, a.widest[i]);
+    for (int o = 32; o; o >>= 1) {
+        ax += __shfl_xor(ax, o);
+        wide = max(wide, (uint32_t)__shfl_xor((int)wide, o));
     }
-    if (a.k == 0)
-        return;
+    if (lane == 0) {
+        abs_x[wave] = ax;
+        top_abs[wave] = wide;
+    }
+    // the groups' largest chunks: every 256th one
     const float *best = a.best + row * a.stride;
-    // the groups' largest chunks
-    constexpr int64_t STRIP = 8 * kSelect;
-    float top = -INFINITY;
-    for (int64_t c = 8 * (int64_t)tid; c < a.stride; c += STRIP)
-#pragma unroll
-        for (int h = 0; h < 2; h++)
-            if (c + 4 * h < a.stride) {
-                const recd_f32x4 v = *reinterpret_cast<const recd_f32x4 *>(best + c + 4 * h);
-                for (int e = 0; e < 4; e++)
-                    top = fmaxf(top, c + 4 * h + e < a.chunks ? v[e] : -INFINITY);
-            }
-    top = fmaxf(top, __shfl_xor(top, 1));
-    top = fmaxf(top, __shfl_xor(top, 2));
-    if ((tid & 3) == 0)
-        groups[tid >> 2] = top;
+    if (a.k) {
+        float top = -INFINITY;
+#pragma unroll 8
+        for (int64_t c = tid; c < a.chunks; c += NT)
+            top = fmaxf(top, best[c]);
+        groups[tid] = top;
+    }
     if (tid == 0)
         count = 0;
     __syncthreads();
-    if (tid < kSelect / 4) {
+    if (wave == WAVES - 1 && a.given) {
+        const int64_t g = a.given[row];
+        const bool has = g >= 0 && g < a.V;
+        Piece v{};
+        if (has && has_piece)
+            v = *reinterpret_cast<const Piece *>(table + g * a.D + at * E);
+        double z = part(v);
+        for (int o = 1; o < 1 << llog; o <<= 1)
+            z += __shfl_xor(z, o);
+        if (lane == 0)
+            a.logp[row] = has ? (float)(z * (double)a.scale - lse_all) : 0.0f;
+    }
+    if (a.k == 0)
+        return;
+    if constexpr (NT > kGroups) {
+        float top = groups[tid % kGroups];
+        for (int i = 1; i < NT / kGroups; i++)
+            top = fmaxf(top, groups[tid % kGroups + i * kGroups]);
+        __syncthreads();
+        if (tid < kGroups)
+            groups[tid] = top;
+        __syncthreads();
+    }
+    if (tid < kGroups) {
         const float mine = groups[tid];
         int above = 0, equal = 0;
-        for (int i = 0; i < kSelect / 4; i++) {
-            above += groups[i] > mine;
-            equal += groups[i] == mine;
+        for (int i = 0; i < kGroups; i += 4) {
+            const recd_f32x4 v = *reinterpret_cast<const recd_f32x4 *>(groups + i);
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                above += v[e] > mine;
+                equal += v[e] == mine;
+            }
         }
         if (above < a.k && a.k <= above + equal)
             group_bar = mine;  // (all that write have this value)
     }
     float sum_x = 0.0f;
     uint32_t w = 0;
-    for (int i = 0; i < kSelect / 64; i++) {
+    for (int i = 0; i < WAVES; i++) {
         sum_x += abs_x[i];
         w = max(w, top_abs[i]);
     }
@@ -472,94 +482,137 @@ template <typename T> __global__ __launch_bounds__(kSelect) void k_answers_selec
     d = bound && sum_x != 0.0f && wf != 0.0f ? d : 0.0f;
     __syncthreads();
     const float chunk_bar = group_bar - 2.0f * d;
+    // what is kept comes before (bar, bar_id): the smallest of the k best so far, or all that may be among them
     double bar = bound ? (double)group_bar - (double)d : -INFINITY;
-    bool full = false;  // k are kept, and only what is larger counts
-    int64_t from = 0;
-    while (from < a.chunks) {
-        // the next chunks that may hold some, in their order
-        const int64_t c = from + 8 * (int64_t)tid;
-        uint32_t may = 0;
-        for (int e = 0; e < 8; e++)
-            if (c + e < a.chunks) {
-                const float v = best[c + e];
-                if (v >= chunk_bar && !(full && (double)v + (double)d <= bar))
-                    may |= 1u << e;
-            }
-        uint32_t mine = __popc(may), upto = mine;
-        for (int o = 1; o < 64; o <<= 1) {
-            const uint32_t v = (uint32_t)__shfl_up((int)upto, o);
-            upto += lane >= o ? v : 0u;
-        }
-        if (lane == 63)
-            waves[wave] = upto;
-        if (tid == 0) {
-            listed = 0;
-            next = from + STRIP;
+    uint32_t bar_id = 0xffffffffu;
+    auto may_hold = [&](int64_t c) {
+        const double v = (double)best[c] + (double)d;
+        return v > bar || (v == bar && (uint64_t)c * kChunk < bar_id);
+    };
+    // what is kept, in order; of more than k the k best
+    auto settle = [&] {
+        const int kept = (int)count;
+        int size = 2;
+        while (size < kept)
+            size <<= 1;
+        for (int i = kept + tid; i < size; i += NT) {
+            key[i] = -INFINITY;
+            id[i] = 0xffffffffu;
         }
         __syncthreads();
-        uint32_t before = upto - mine, all = 0;
-        for (int i = 0; i < kSelect / 64; i++) {
-            before += i < wave ? waves[i] : 0u;
-            all += waves[i];
-        }
-        for (int e = 0; e < 8; e++)
-            if (may >> e & 1) {
-                if (before < kListed)
-                    list[before] = (uint32_t)(c + e);
-                else if (before == kListed)
-                    next = c + e;
-                before++;
-            }
-        if (tid == 0)
-            listed = all < kListed ? all : kListed;
-        __syncthreads();
-        const int n = (int)listed;
-        from = next;
-        for (int l0 = 0; l0 < n; l0 += kAtOnce) {
-            for (int l = l0 + wave; l < l0 + kAtOnce && l < n; l += kSelect / 64) {
-                const int64_t chunk = list[l], v = chunk * kChunk + lane;
-                if (full && (double)best[chunk] + (double)d <= bar)
-                    continue;
-                if (v < a.V) {
-                    double z = dot64(x, table + v * a.D, a.D) * (double)a.scale;
-                    z = z == z ? z : -INFINITY;
-                    if (full ? z > bar : z >= bar) {
-                        const uint32_t to = atomicAdd(&count, 1u);
-                        key[to] = z;
-                        id[to] = (uint32_t)v;
+        for (int run = 2; run <= size; run <<= 1)
+            for (int o = run >> 1; o; o >>= 1) {
+                for (int i = tid; i < size >> 1; i += NT) {
+                    const int p = (i & ~(o - 1)) << 1 | (i & (o - 1)), q = p | o;
+                    const double zp = key[p], zq = key[q];
+                    const uint32_t ip = id[p], iq = id[q];
+                    if (before(zq, iq, zp, ip) == ((p & run) == 0)) {
+                        key[p] = zq;
+                        key[q] = zp;
+                        id[p] = iq;
+                        id[q] = ip;
                     }
                 }
+                __syncthreads();
             }
-            __syncthreads();
-            // the k best so far to the front, in their order
-            const int kept = (int)count;
-            for (int i = tid; i < kept; i += kSelect) {
-                const double z = key[i];
-                const uint32_t v = id[i];
-                int rank = 0;
-                for (int o = 0; o < kept; o++)
-                    rank += key[o] > z || (key[o] == z && id[o] < v);
-                if (rank < a.k) {
-                    sorted_key[rank] = z;
-                    sorted_id[rank] = v;
+        if (kept >= a.k) {
+            bar = key[a.k - 1];
+            bar_id = id[a.k - 1];
+        }
+        if (tid == 0)
+            count = kept < a.k ? kept : a.k;
+        __syncthreads();
+    };
+    // the chunk's logits, by the wave: eight loads at a time of as many table rows as the lanes hold.  Their lanes' parts are added up
+    // in one tree for all of them: at each of its first steps a lane hands half of the sums to its neighbour and takes the other half
+    // over, so that at the end every lane has sums of its own
+    auto logits = [&](int64_t chunk) {
+        const int per = 64 >> llog;  // table rows of a load
+        for (int r = 0; r < kChunk; r += 8 * per) {
+            Piece v[8];
+            const uint32_t first = (uint32_t)(chunk * kChunk) + (uint32_t)(r + (lane >> llog));
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                v[i] = Piece{};
+                if (has_piece && r + i * per < kChunk && first + i * per < a.V)
+                    v[i] = *reinterpret_cast<const Piece *>(table + (int64_t)(first + i * per) * a.D + at * E);
+            }
+            double z[8];
+#pragma unroll
+            for (int i = 0; i < 8; i++)
+                z[i] = part(v[i]);
+            int have = 8, mine = 0;  // sums of the lane, and which load's the first of them is
+#pragma unroll
+            for (int step = 0; step < 3; step++)
+                if (step < llog) {
+                    const int o = 1 << step, half = 4 >> step;
+                    const bool upper = lane & o;
+#pragma unroll
+                    for (int i = 0; i < half; i++) {
+                        const double give = upper ? z[i] : z[i + half], keep = upper ? z[i + half] : z[i];
+                        z[i] = keep + __shfl_xor(give, o);
+                    }
+                    have = half;
+                    mine += upper ? half : 0;
+                }
+            for (int o = 8; o < 1 << llog; o <<= 1)
+                z[0] += __shfl_xor(z[0], o);
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                const int load = mine + i;
+                const uint32_t v = first + load * per;
+                double s = z[i] * (double)a.scale;
+                s = s == s ? s : -INFINITY;
+                if (i < have && at < 8 && r + load * per < kChunk && v < a.V && before(s, v, bar, bar_id)) {
+                    const uint32_t slot = atomicAdd(&count, 1u);
+                    key[slot] = s;
+                    id[slot] = v;
                 }
             }
-            __syncthreads();
-            if (tid < a.k && tid < kept) {
-                key[tid] = sorted_key[tid];
-                id[tid] = sorted_id[tid];
-            }
-            if (tid == 0)
-                count = kept < a.k ? kept : a.k;
-            __syncthreads();
-            if ((int)count == a.k) {
-                full = true;
-                bar = key[a.k - 1];
-            }
-            __syncthreads();
         }
-        __syncthreads();  // (next and listed have been read)
+    };
+    int64_t range = a.chunks;  // chunks that are listed at a time: all, or where these are too many, as many as there is room for
+    for (int64_t from = 0; from < a.chunks;) {
+        const int64_t to = a.chunks - from < range ? a.chunks : from + range;
+        if (tid == 0)
+            listed = taken = 0;
+        __syncthreads();
+#pragma unroll 8
+        for (int64_t c = from + tid; c < to; c += NT)
+            if (best[c] >= chunk_bar && may_hold(c)) {
+                const uint32_t slot = atomicAdd(&listed, 1u);
+                if (slot < kListed)
+                    list[slot] = (uint32_t)c;
+            }
+        __syncthreads();
+        const uint32_t n = listed;
+        __syncthreads();
+        if (n > kListed) {
+            range = kListed;
+            continue;
+        }
+        // waves take chunks while there is room for what all of them could find in theirs
+        for (bool more = n > 0; more;) {
+            while (*(volatile uint32_t *)&count <= KEPT - WAVES * kChunk) {
+                uint32_t l = 0;
+                if (lane == 0)
+                    l = atomicAdd(&taken, 1u);
+                l = __builtin_amdgcn_readfirstlane(l);
+                if (l >= n)
+                    break;
+                const int64_t chunk = list[l];
+                if (may_hold(chunk))
+                    logits(chunk);
+            }
+            __syncthreads();
+            more = taken < n;
+            __syncthreads();
+            if (more)
+                settle();
+        }
+        from = to;
     }
+    settle();
     if (tid < a.k) {
         a.top_ids[row * a.k + tid] = id[tid];
         a.top_logp[row * a.k + tid] = (float)(key[tid] - lse_all);
@@ -736,7 +789,14 @@ recd_status recd_vocab_answers(recd_ctx *ctx, int64_t n, int64_t V, int D, recd_
         recd_with_type(dt, [&](auto t) {
             using T = decltype(t);
             recd_with_width(D, [&](auto w) { launch_stream<T, w.value>(a, s, ctx->stream); });
-            hipLaunchKernelGGL((k_answers_select<T>), dim3((unsigned)rows), dim3(kSelect), 0, ctx->stream, b);
+            int llog = 0;  // lanes of a row
+            while ((int)(16 / sizeof(T)) << llog < D)
+                llog++;
+            // blocks of sixteen waves where there are too few rows to fill the card with blocks of four
+            if (rows <= 2 * ctx->num_cu)
+                hipLaunchKernelGGL((k_answers_select<T, 1024>), dim3((unsigned)rows), dim3(1024), 0, ctx->stream, b, llog);
+            else
+                hipLaunchKernelGGL((k_answers_select<T, 256>), dim3((unsigned)rows), dim3(256), 0, ctx->stream, b, llog);
         });
     }
     RECD_HIP(ctx, hipGetLastError());
