@@ -24,7 +24,7 @@ constexpr int kFewRows = 256;
 struct StreamArgs {
     int64_t n, V;
     int D;
-    float c, scale;      // |scale| * log2(e), |scale|; the sign goes into the kept side
+    float c;             // |scale| * log2(e); the sign goes into the kept side
     bool negative;
     const void *x, *table;
     int row_blocks, splits;
@@ -88,51 +88,45 @@ struct Running {
     }
 };
 
-// 32 scores of a lane, those of table rows from `left` on left out: returns the largest of the lane pair's 64, in which all table rows
-// of the chunk are.
-__device__ inline float largest(const recd_f32x16 (&z)[2], int left, int lane)
-{
-    float top = -INFINITY;
-    if (left >= kChunk) {
-#pragma unroll
-        for (int h = 0; h < 2; h++)
-#pragma unroll
-            for (int r = 0; r < 16; r++)
-                top = fmaxf(top, z[h][r]);
-    } else {
-#pragma unroll
-        for (int h = 0; h < 2; h++)
-#pragma unroll
-            for (int r = 0; r < 16; r++)
-                if (32 * h + recd_score_row(r, lane) < left)
-                    top = fmaxf(top, z[h][r]);
-    }
-    return fmaxf(top, __shfl_xor(top, 32));
-}
-
-__device__ inline void add_up(Running &run, const recd_f32x16 (&z)[2], float c, int left, int lane)
+// Scores of 32 table rows, half of them in each lane of a pair, into the running sums; `left` of these rows are there.  Returns the
+// largest logit in powers of two.  It is found among what the exponentials are taken of anyway, z * c - m: the maximum of the scores
+// themselves would take an operation more for each.
+__device__ inline float add_up(Running &run, recd_f32x16 z, float c, int left, int lane)
 {
     const float from = run.m == -INFINITY ? 0.0f : run.m;
-    if (left >= kChunk) {
 #pragma unroll
-        for (int h = 0; h < 2; h++)
+    for (int r = 0; r < 16; r++)
+        z[r] = __builtin_fmaf(z[r], c, -from);
+    if (left < 32) {
+        asm volatile("" : "+v"(left));  // a branch: the last chunk alone pays for the comparisons
 #pragma unroll
-            for (int r = 0; r < 16; r++) {
-                const float d = __builtin_fmaf(z[h][r], c, -from), e = recd_exp2(d);
-                run.s += e;
-                run.t = __builtin_fmaf(e, d, run.t);
-            }
-    } else {
-#pragma unroll
-        for (int h = 0; h < 2; h++)
-#pragma unroll
-            for (int r = 0; r < 16; r++)
-                if (32 * h + recd_score_row(r, lane) < left) {
-                    const float d = __builtin_fmaf(z[h][r], c, -from), e = recd_exp2(d);
-                    run.s += e;
-                    run.t = __builtin_fmaf(e, d, run.t);
-                }
+        for (int r = 0; r < 16; r++)
+            z[r] = recd_score_row(r, lane) < left ? z[r] : -1e30f;
     }
+    float top = -INFINITY;  // (of nothing but NaN)
+#pragma unroll
+    for (int r = 0; r < 16; r += 2)
+        top = fmaxf(fmaxf(top, z[r]), z[r + 1]);
+    top = fmaxf(top, __shfl_xor(top, 32));
+    const bool moves = (top > 0.0f || run.m == -INFINITY) && top > -INFINITY && left > 0;
+    auto exponentials = [&](auto moved, float by) {
+#pragma unroll
+        for (int r = 0; r < 16; r++) {
+            const float d = moved.value ? z[r] + by : z[r], e = recd_exp2(d);
+            run.s += e;
+            run.t = __builtin_fmaf(e, d, run.t);
+        }
+    };
+    if (__any(moves)) {  // (seldom; both ways have exponentials of their own, or the other one would copy all scores)
+        const float by = moves ? -top : 0.0f;
+        const float f = run.m == -INFINITY ? 0.0f : recd_exp2(by);  // (nothing has been added up)
+        run.t = moves ? (run.t + run.s * by) * f : run.t;
+        run.s = moves ? run.s * f : run.s;
+        run.m = moves ? from + top : run.m;
+        exponentials(std::true_type{}, by);
+    } else
+        exponentials(std::false_type{}, 0.0f);
+    return left > 0 ? from + top : -INFINITY;
 }
 
 template <typename T, int KS>
@@ -178,7 +172,8 @@ template <typename T, int DP, int N> __global__ __launch_bounds__(64 * kWaves) v
     if (c < c1)
         load(c, 0);
     for (; c < c1; c += kWaves) {
-        recd_f32x16 z[N][2];
+        const int left = a.V - c * kChunk < kChunk ? (int)(a.V - c * kChunk) : kChunk;
+        float top[N];
 #pragma unroll
         for (int h = 0; h < 2; h++) {
             recd_wave_sync();
@@ -192,26 +187,28 @@ template <typename T, int DP, int N> __global__ __launch_bounds__(64 * kWaves) v
                 load(c, 1);
             else if (c + kWaves < c1)
                 load(c + kWaves, 0);
+            recd_f32x16 z[N];
 #pragma unroll
             for (int j = 0; j < N; j++)
-                z[j][h] = recd_f32x16{};
+                z[j] = recd_f32x16{};
 #pragma unroll
             for (int k = 0; k < KS; k++) {
                 const Frag w = tile.rows(0, 16 * k, lane);
 #pragma unroll
                 for (int j = 0; j < N; j++)
-                    z[j][h] = RecdMma<T>::mul(w, xf[j][k], z[j][h]);
+                    z[j] = RecdMma<T>::mul(w, xf[j][k], z[j]);
+            }
+#pragma unroll
+            for (int j = 0; j < N; j++) {
+                const float half = add_up(run[j], z[j], a.c, left - 32 * h, lane);
+                top[j] = h ? fmaxf(top[j], half) : half;
             }
         }
-        const int left = a.V - c * kChunk < kChunk ? (int)(a.V - c * kChunk) : kChunk;
 #pragma unroll
         for (int j = 0; j < N; j++) {
-            const float top = largest(z[j], left, lane);
-            run[j].rescale(top * a.c);
-            add_up(run[j], z[j], a.c, left, lane);
             const int64_t row = row0 + 32 * j + (lane & 31);
             if (a.best && lane < 32 && row < a.n)
-                a.best[row * a.stride + c] = top * a.scale;
+                a.best[row * a.stride + c] = top[j] * kRecdLn2;
         }
     }
     if (a.widest && rb == 0) {
@@ -245,7 +242,7 @@ template <typename T, int DP, int N> __global__ __launch_bounds__(64 * kWaves) v
 
 // Many rows: 32 in every wave of a block, all of which see every table row of the split, a chunk of them at a time in two
 // buffers of LDS.
-template <typename T, int DP> __global__ __launch_bounds__(64 * kMany) void k_answers_many(StreamArgs a)
+template <typename T, int DP> __global__ __launch_bounds__(64 * kMany, sizeof(T) == 2 && DP <= 128 ? 4 : 2) void k_answers_many(StreamArgs a)
 {
     constexpr int KS = DP / 16;
     using Frag = typename RecdMma<T>::Frag;
@@ -294,20 +291,18 @@ template <typename T, int DP> __global__ __launch_bounds__(64 * kMany) void k_an
             if (c + 2 < c1)
                 load(c + 2);
         }
-        recd_f32x16 z[2];
+        const int left = a.V - c * kChunk < kChunk ? (int)(a.V - c * kChunk) : kChunk;
+        float top = -INFINITY;
 #pragma unroll
         for (int h = 0; h < 2; h++) {
-            z[h] = recd_f32x16{};
+            recd_f32x16 z = {};
 #pragma unroll
             for (int k = 0; k < KS; k++)
-                z[h] = RecdMma<T>::mul(tiles[buf].rows(32 * h, 16 * k, lane), xf[k], z[h]);
+                z = RecdMma<T>::mul(tiles[buf].rows(32 * h, 16 * k, lane), xf[k], z);
+            top = fmaxf(top, add_up(run, z, a.c, left - 32 * h, lane));
         }
-        const int left = a.V - c * kChunk < kChunk ? (int)(a.V - c * kChunk) : kChunk;
-        const float top = largest(z, left, lane);
-        run.rescale(top * a.c);
-        add_up(run, z, a.c, left, lane);
         if (a.best) {
-            four = recd_f32x4{four[1], four[2], four[3], top * a.scale};
+            four = recd_f32x4{four[1], four[2], four[3], top * kRecdLn2};
             if ((c & 3) == 3 || c + 1 == c1) {
                 for (int64_t i = c; (i & 3) != 3; i++)
                     four = recd_f32x4{four[1], four[2], four[3], -INFINITY};
@@ -445,28 +440,29 @@ template <typename T, int NT> __global__ __launch_bounds__(NT) void k_answers_se
     }
     if (a.k == 0)
         return;
-    if constexpr (NT > kGroups) {
-        float top = groups[tid % kGroups];
-        for (int i = 1; i < NT / kGroups; i++)
-            top = fmaxf(top, groups[tid % kGroups + i * kGroups]);
-        __syncthreads();
-        if (tid < kGroups)
-            groups[tid] = top;
-        __syncthreads();
-    }
-    if (tid < kGroups) {
-        const float mine = groups[tid];
-        int above = 0, equal = 0;
-        for (int i = 0; i < kGroups; i += 4) {
-            const recd_f32x4 v = *reinterpret_cast<const recd_f32x4 *>(groups + i);
+    if (wave == 0) {
+        // the k-th largest of the groups, bit by bit, of integers in the floats' order
+        constexpr int MINE = kGroups / 64;
+        uint32_t g[MINE];
 #pragma unroll
-            for (int e = 0; e < 4; e++) {
-                above += v[e] > mine;
-                equal += v[e] == mine;
-            }
+        for (int i = 0; i < MINE; i++) {
+            float top = -INFINITY;
+            for (int n = lane + 64 * i; n < NT; n += kGroups)
+                top = fmaxf(top, groups[n]);
+            const uint32_t b = __builtin_bit_cast(uint32_t, top);
+            g[i] = b ^ (b >> 31 ? 0xffffffffu : 0x80000000u);
         }
-        if (above < a.k && a.k <= above + equal)
-            group_bar = mine;  // (all that write have this value)
+        uint32_t bar = 0;
+        for (uint32_t bit = 0x80000000u; bit; bit >>= 1) {
+            int reach = 0;
+#pragma unroll
+            for (int i = 0; i < MINE; i++)
+                reach += __popcll(__ballot(g[i] >= (bar | bit)));
+            if (reach >= a.k)
+                bar |= bit;
+        }
+        if (lane == 0)
+            group_bar = __builtin_bit_cast(float, bar ^ (bar >> 31 ? 0x80000000u : 0xffffffffu));
     }
     float sum_x = 0.0f;
     uint32_t w = 0;
@@ -489,9 +485,34 @@ template <typename T, int NT> __global__ __launch_bounds__(NT) void k_answers_se
         const double v = (double)best[c] + (double)d;
         return v > bar || (v == bar && (uint64_t)c * kChunk < bar_id);
     };
+    auto ranked = [&](int kept) {
+        if (kept >= a.k) {
+            bar = key[a.k - 1];
+            bar_id = id[a.k - 1];
+        }
+        if (tid == 0)
+            count = kept < a.k ? kept : a.k;
+        __syncthreads();
+    };
     // what is kept, in order; of more than k the k best
     auto settle = [&] {
         const int kept = (int)count;
+        if (kept <= NT) {  // a thread's place is the number of those before it
+            const double z = tid < kept ? key[tid] : 0.0;
+            const uint32_t v = tid < kept ? id[tid] : 0;
+            int place = 0;
+            if (tid < kept)
+                for (int i = 0; i < kept; i++)
+                    place += before(key[i], id[i], z, v);
+            __syncthreads();
+            if (tid < kept) {
+                key[place] = z;
+                id[place] = v;
+            }
+            __syncthreads();
+            ranked(kept);
+            return;
+        }
         int size = 2;
         while (size < kept)
             size <<= 1;
@@ -515,13 +536,7 @@ template <typename T, int NT> __global__ __launch_bounds__(NT) void k_answers_se
                 }
                 __syncthreads();
             }
-        if (kept >= a.k) {
-            bar = key[a.k - 1];
-            bar_id = id[a.k - 1];
-        }
-        if (tid == 0)
-            count = kept < a.k ? kept : a.k;
-        __syncthreads();
+        ranked(kept);
     };
     // the chunk's logits, by the wave: eight loads at a time of as many table rows as the lanes hold.  Their lanes' parts are added up
     // in one tree for all of them: at each of its first steps a lane hands half of the sums to its neighbour and takes the other half
@@ -653,9 +668,22 @@ Shape stream_shape(const recd_ctx *ctx, int64_t n, int64_t V, int D, recd_dtype 
     s.row_blocks = (int)((n + s.rows - 1) / s.rows);
     s.chunks = (V + kChunk - 1) / kChunk;
     s.stride = (s.chunks + 3) / 4 * 4;
-    // two blocks a compute unit
+    // Two blocks a compute unit at a time: of few rows as many splits as give these, of many the number whose rounds are fullest
+    // (70 000 rows have 274 blocks of rows: with one split most units would have one of them, and some two)
     const int64_t units = s.few ? (s.chunks + kWaves - 1) / kWaves : s.stride / 4;  // a wave's chunk each; four chunks
-    int64_t splits = 2 * ctx->num_cu / s.row_blocks;
+    const int64_t slots = 2 * ctx->num_cu;
+    int64_t splits = slots / s.row_blocks;
+    if (!s.few) {
+        double best = 1e30;
+        for (int64_t k = 1; k <= slots && k <= units; k++) {
+            const int64_t rounds = (k * s.row_blocks + slots - 1) / slots;
+            const double cost = (double)(rounds * slots) / (double)(k * s.row_blocks) + 0.02 * (double)(k * s.row_blocks) / (double)slots;
+            if (cost < best) {
+                best = cost;
+                splits = k;
+            }
+        }
+    }
     splits = splits < units ? splits : units;
     splits = splits < 1 ? 1 : splits;
     const int64_t each = (units + splits - 1) / splits;
@@ -768,7 +796,6 @@ recd_status recd_vocab_answers(recd_ctx *ctx, int64_t n, int64_t V, int D, recd_
         a.V = V;
         a.D = D;
         a.c = fabsf(scale) * kRecdLog2e;
-        a.scale = fabsf(scale);
         a.negative = scale < 0;
         a.x = (const char *)x + at * D * (int64_t)elem_size(dt);
         a.table = table;
