@@ -533,10 +533,10 @@ __global__ __launch_bounds__(1024) void k_join_columns(int64_t blocks, int n_j, 
     out[col] = s;
 }
 
-// Few rows: 16 features a block, whose waves take equal parts of the contraction, straight from memory to the matrix cores; their sums
-// are added up in LDS in the waves' order.
-constexpr int kFewWaves = 8;
-
+// Few rows: 16 features a block, whose waves take equal parts of the contraction (or of a split of it), straight from memory to the
+// matrix cores; their sums are added up in LDS in the waves' order.  What bounds it is how many loads a compute unit has on their way: eight waves
+// with sixteen of each operand (fp32: sixteen with eight) for up to 16 rows.  One row 4096 -> 4096 bf16: 9.3 us a call, sixteen waves 11.3, four
+// 14.2; fp32 16.8, eight waves 20.1.
 template <typename T> struct Mma16;
 template <> struct Mma16<_Float16> {
     using Frag = recd_f16x8;
@@ -574,9 +574,9 @@ template <typename T> __device__ inline typename Mma16<T>::Frag few_frag(const c
     return u.f;
 }
 
-template <typename T, int RG> __global__ __launch_bounds__(64 * kFewWaves) void k_few(ProductArgs a)
+template <typename T, int RG, int W, int UNROLL> __global__ __launch_bounds__(64 * W) void k_few(ProductArgs a)
 {
-    __shared__ float join[kFewWaves][16 * RG][16 + 4];
+    __shared__ float join[W][16 * RG][16 + 4];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int j0 = blockIdx.x * 16, n = (int)a.n_i, K = (int)a.K;
     const int j = j0 + (lane & 15) < a.n_j ? j0 + (lane & 15) : a.n_j - 1;
@@ -591,10 +591,11 @@ template <typename T, int RG> __global__ __launch_bounds__(64 * kFewWaves) void 
 #pragma unroll
     for (int g = 0; g < RG; g++)
         acc[g] = recd_f32x4{};
-    const int chunks = (K + 31) / 32, each = (chunks + kFewWaves - 1) / kFewWaves;
-    const int c1 = (wave + 1) * each < chunks ? (wave + 1) * each : chunks;
-#pragma unroll 4
-    for (int c = wave * each; c < c1; c++) {
+    const int of_split = (int)(a.k_each / 32), c0 = (int)blockIdx.y * of_split, each = (of_split + W - 1) / W;
+    const int all = (K + 31) / 32 < c0 + of_split ? (K + 31) / 32 : c0 + of_split;
+    const int c1 = c0 + (wave + 1) * each < all ? c0 + (wave + 1) * each : all;
+#pragma unroll UNROLL
+    for (int c = c0 + wave * each; c < c1; c++) {
         const int k = 32 * c + 8 * (lane >> 4);
         const auto qf = few_frag<T>(q, k, K);
 #pragma unroll
@@ -613,8 +614,12 @@ template <typename T, int RG> __global__ __launch_bounds__(64 * kFewWaves) void 
 #pragma unroll
     for (int e = 0; e < 8; e++) {
         z[e] = 0.0f;
-        for (int w = 0; w < kFewWaves; w++)
+        for (int w = 0; w < W; w++)
             z[e] += join[w][row][at + e];
+    }
+    if (a.part) {
+        recd_store8(a.part + ((int64_t)blockIdx.y * n + row) * a.n_j + col, count, z);
+        return;
     }
     load_bias(a.e.bias, col, count, b);
     Eight<T> other{};
@@ -759,13 +764,21 @@ struct ForwardPlan {
     void make(const recd_ctx *ctx, const recd_dense_layer *a, bool heavy, char *ws, size_t *bytes)
     {
         WsCarver c(ws);
-        few = a->n <= kFewRows;
+        // The kernel of few rows reads all of them for every 16 features, the tiles' for 64 (us: 64 rows 4096 -> 4096 bf16 23 and 15, 37 rows
+        // 512 -> 128 fp32 7.3 and 9.5).  Few features leave most of the card idle: then the contraction is split, if it is long
+        few = a->n <= 16 || (a->n <= kFewRows && a->in <= 512);
         part = nullptr;
-        if (!few) {
+        if (few) {
+            const int64_t chunks = (a->in + 31) / 32, blocks = (a->out + 15) / 16;
+            int64_t splits = ctx->num_cu / blocks < chunks / 32 ? ctx->num_cu / blocks : chunks / 32;
+            splits = splits < 1 ? 1 : splits > 8 ? 8 : splits;
+            const int64_t each = (chunks + splits - 1) / splits;
+            shape.k_each = 32 * each;
+            shape.splits = (int)((chunks + each - 1) / each);
+        } else
             shape = product_shape(ctx, a->n, a->out, a->in, a->dtype, heavy);
-            if (shape.splits > 1)
-                part = c.take<float>((size_t)shape.splits * a->n * a->out);
-        }
+        if (shape.splits > 1)
+            part = c.take<float>((size_t)shape.splits * a->n * a->out);
         *bytes = c.off;
     }
 };
@@ -901,16 +914,17 @@ recd_status recd_dense(recd_ctx *ctx, const recd_dense_layer *a, const void *x, 
     recd_with_type(a->dtype, [&](auto t) {
         using T = decltype(t);
         if (plan.few) {
-            const dim3 grid((unsigned)((a->out + 15) / 16)), block(64 * kFewWaves);
+            const dim3 grid((unsigned)((a->out + 15) / 16), (unsigned)plan.shape.splits);
+            constexpr int W = sizeof(T) == 4 ? 16 : 8;
+            p.k_each = plan.shape.k_each;
             if (a->n <= 16)
-                hipLaunchKernelGGL((k_few<T, 1>), grid, block, 0, ctx->stream, p);
+                hipLaunchKernelGGL((k_few<T, 1, W, 128 / W>), grid, dim3(64 * W), 0, ctx->stream, p);
             else if (a->n <= 32)
-                hipLaunchKernelGGL((k_few<T, 2>), grid, block, 0, ctx->stream, p);
+                hipLaunchKernelGGL((k_few<T, 2, 8, 4>), grid, dim3(64 * 8), 0, ctx->stream, p);
             else
-                hipLaunchKernelGGL((k_few<T, 4>), grid, block, 0, ctx->stream, p);
-            return;
-        }
-        launch_product<T, false, false, FORWARD>(p, plan.shape, ctx->stream);
+                hipLaunchKernelGGL((k_few<T, 4, 8, 4>), grid, dim3(64 * 8), 0, ctx->stream, p);
+        } else
+            launch_product<T, false, false, FORWARD>(p, plan.shape, ctx->stream);
         if (plan.part) {
             RowsArgs r{a->n, a->out, 0, plan.shape.splits, plan.part, nullptr, 0, p.e};
             launch_rows<T, FORWARD>(ctx, r, ctx->stream);

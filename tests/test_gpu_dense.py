@@ -89,6 +89,18 @@ def test_cuts(recd, ctx, dt, n, K, N):
         assert du.same_bits(a[k], again[k]), k
 
 
+# few rows and a long contraction: split, with tails, or by tiles
+@pytest.mark.parametrize("dt", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("n", [1, 7, 16, 17, 50])
+@pytest.mark.parametrize("K,N", [(4104, 72), (8200, 16), (2048, 520), (1032, 24)])
+def test_few_rows_of_many_elements(recd, ctx, dt, n, K, N):
+    x, w, b, r, g = data(n, K, N, dt, residual=True)
+    a = check(recd, ctx, x, w, b, r, g, "gelu", 0.1, kept=True)
+    again = run(recd, ctx, x, w, b, r, g, "gelu", 0.1, kept=True)
+    for k in a:
+        assert du.same_bits(a[k], again[k]), k
+
+
 @pytest.mark.parametrize("dt", ["f32", "f16", "bf16"])
 @pytest.mark.parametrize("act", ["none", "relu", "gelu", "silu"])
 @pytest.mark.parametrize("n", [40, 200])
