@@ -39,9 +39,9 @@ __device__ inline RecdBits recd_mask_bits(const RecdMask &m, uint64_t call, int6
 #pragma unroll
     for (int i = 0; i < 10; i++) {
         const uint64_t u = (uint64_t)a * 0xD2511F53u, v = (uint64_t)c * 0xCD9E8D57u;
-        a = (uint32_t)(v >> 32) ^ b ^ k0;
+        a = __builtin_amdgcn_bitop3_b32((uint32_t)(v >> 32), b, k0, 0x96);  // xor of the three
         b = (uint32_t)v;
-        c = (uint32_t)(u >> 32) ^ d ^ k1;
+        c = __builtin_amdgcn_bitop3_b32((uint32_t)(u >> 32), d, k1, 0x96);
         d = (uint32_t)u;
         k0 += 0x9E3779B9u;
         k1 += 0xBB67AE85u;
