@@ -3,8 +3,11 @@
 A batch's lists of one feature are deduplicated; the rows of the unique lists are looked up, normalised, attend to the
 rows before them in their list, and are scored against the whole table: row i of a list is to predict id i + 1.  A
 unique list's loss counts as often as the batch holds the list, so loss and gradients are those of the whole batch.
+With --hidden a feed-forward block follows the attention, and with --dropout its layers and the attention's projection drop
+elements of their outputs; the copies of a list in a batch then share one mask.  At the end the most likely next ids of some lists
+are printed.
 
-    python examples/next_id.py [--steps 50] [--dtype f32|f16|bf16]
+    python examples/next_id.py [--steps 50] [--dtype f32|f16|bf16] [--hidden 512] [--dropout 0.1]
 """
 import argparse
 import os
@@ -46,10 +49,12 @@ class Lists:
 
 
 class NextId:
-    """Table, one attention layer with a residual, and a norm before each of attention and loss."""
+    """Table, one attention layer with a residual, and a norm before each of attention and loss; with `hidden` a feed-forward block
+    of that width, with a norm and a residual of its own."""
 
-    def __init__(self, rows, D, heads, kv_heads, dtype="f32", seed=0):
+    def __init__(self, rows, D, heads, kv_heads, dtype="f32", seed=0, hidden=0, dropout=0.0):
         self.ctx = recd.Context(0)
+        self.hidden, self.dropout, self.seed, self.steps = hidden, dropout, seed, 0
         self.D, self.heads, self.kv_heads, self.d = D, heads, kv_heads, D // heads
         self.dtype = DTYPE[dtype]
         g = torch.Generator(device="cuda").manual_seed(seed)
@@ -62,12 +67,20 @@ class NextId:
                        "w_out": normal(heads * self.d, D, std=(heads * self.d) ** -0.5), "norm1": torch.ones(D, device="cuda"),
                        "bias1": torch.zeros(D, device="cuda"), "norm2": torch.ones(D, device="cuda"),
                        "bias2": torch.zeros(D, device="cuda")}
+        if hidden:
+            self.params.update(w_up=normal(hidden, D, std=D ** -0.5), bias_up=torch.zeros(hidden, device="cuda"),
+                               w_down=normal(D, hidden, std=hidden ** -0.5), bias_down=torch.zeros(D, device="cuda"),
+                               norm3=torch.ones(D, device="cuda"), bias3=torch.zeros(D, device="cuda"))
         self.squares = {n: torch.zeros_like(p) for n, p in self.params.items()}
         self.slopes = 2.0 ** (-8.0 * torch.arange(1, heads + 1, device="cuda", dtype=torch.float32) / heads)
         self.scale = 1.0                                                    # of the logits
 
     def how(self):
         return dict(scale=self.d ** -0.5, slopes=self.slopes, causal=True)
+
+    def _drop(self, which, train=True):
+        """The mask of the step's use number `which` of dropout, or None."""
+        return recd.Dropout(self.dropout, self.seed, 3 * self.steps + which) if train and self.dropout else None
 
     def _heads(self, qkv):
         rows = qkv.view(qkv.shape[0], self.heads + 2 * self.kv_heads, self.d)
@@ -86,9 +99,21 @@ class NextId:
         q, k, v = self._heads(s["qkv"])
         s["out"], s["lse"] = new(M, self.heads, self.d), new(M, self.heads, dtype=torch.float32)
         c.list_attention(q, k, v, lists.offsets, lists.offsets, lists.longest, lists.longest, s["out"], s["lse"], **self.how())
-        s["y"] = s["emb"] + s["out"].view(M, -1) @ s["w_out"]
+        drop = self._drop(0, train)
+        if drop:
+            s["y"] = new(M, D)
+            c.dropout((s["out"].view(M, -1) @ s["w_out"]).contiguous(), drop, s["y"], residual=s["emb"])
+        else:
+            s["y"] = s["emb"] + s["out"].view(M, -1) @ s["w_out"]
+        s["z"] = s["y"]
+        if self.hidden:
+            s["w_up"], s["w_down"] = p["w_up"].to(dt), p["w_down"].to(dt)
+            s["f"], s["stats3"], s["up"], s["z"] = new(M, D), new(M, 2, dtype=torch.float32), new(M, self.hidden), new(M, D)
+            c.layer_norm(s["y"], p["norm3"], p["bias3"], EPS, s["f"], s["stats3"])
+            c.dense(s["f"], s["w_up"], p["bias_up"], s["up"], act="gelu", dropout=self._drop(1, train))
+            c.dense(s["up"], s["w_down"], p["bias_down"], s["z"], residual=s["y"], dropout=self._drop(2, train))
         s["x"], s["stats2"] = new(M, D), new(M, 2, dtype=torch.float32)
-        c.layer_norm(s["y"], p["norm2"], p["bias2"], EPS, s["x"], s["stats2"])
+        c.layer_norm(s["z"], p["norm2"], p["bias2"], EPS, s["x"], s["stats2"])
         s["loss"], s["logsum"] = new(M, dtype=torch.float32), new(M, dtype=torch.float32)
         s["mean_row"] = new(M, D, dtype=torch.float32) if train else None
         c.vocab_loss(s["x"], s["table"], lists.targets, self.scale, s["loss"], s["logsum"], s["mean_row"])
@@ -105,9 +130,20 @@ class NextId:
         c.vocab_loss_backward(s["x"], s["table"], lists.targets, self.scale, s["logsum"], s["mean_row"], lists.weight * up,
                               g_x, g_table)
         g_y = like(s["y"])
-        c.layer_norm_backward(s["y"], p["norm2"], s["stats2"], g_x, g_y, grads["norm2"], grads["bias2"])
-        grads["w_out"] = s["out"].view(M, -1).t() @ g_y
-        g_out = (g_y @ s["w_out"].t()).view_as(s["out"])
+        c.layer_norm_backward(s["z"], p["norm2"], s["stats2"], g_x, g_y, grads["norm2"], grads["bias2"])
+        if self.hidden:
+            grads.update({n: like(p[n]) for n in ("bias_up", "bias_down", "norm3", "bias3")}, w_up=like(s["w_up"]), w_down=like(s["w_down"]))
+            g_up, g_f, g_n = like(s["up"]), like(s["f"]), like(s["y"])
+            c.dense_backward(s["up"], s["w_down"], p["bias_down"], g_y, g_up, grads["w_down"], grads["bias_down"], dropout=self._drop(2))
+            c.dense_backward(s["f"], s["w_up"], p["bias_up"], g_up, g_f, grads["w_up"], grads["bias_up"], act="gelu", dropout=self._drop(1))
+            c.layer_norm_backward(s["y"], p["norm3"], s["stats3"], g_f, g_n, grads["norm3"], grads["bias3"])
+            g_y = g_y + g_n
+        g_proj, drop = g_y, self._drop(0)
+        if drop:
+            g_proj = like(g_y)
+            c.dropout_backward(g_y, drop, g_proj)
+        grads["w_out"] = s["out"].view(M, -1).t() @ g_proj
+        g_out = (g_proj @ s["w_out"].t()).view_as(s["out"])
         g_qkv = like(s["qkv"])
         c.list_attention_backward(*self._heads(s["qkv"]), lists.offsets, lists.offsets, lists.longest, lists.longest, s["out"],
                                   s["lse"], g_out, *self._heads(g_qkv), **self.how())
@@ -130,7 +166,20 @@ class NextId:
         for n, g in self.backward(lists, s).items():
             self.squares[n] += g * g
             self.params[n] -= lr * g / (self.squares[n].sqrt() + 1e-10)     # Adagrad
+        self.steps += 1
         return loss
+
+    def answers(self, lists, k):
+        """Serving: of the last row of every list that has one, the k most likely next ids with their log probabilities, and the
+        entropy."""
+        _, s = self.forward(lists, train=False)
+        lens = lists.offsets.diff()
+        last = (lists.offsets[1:] - 1)[lens > 0]
+        x, n = s["x"][last], last.numel()
+        ids, logp = torch.empty(n, k, dtype=torch.int64, device="cuda"), torch.empty(n, k, device="cuda")
+        entropy = torch.empty(n, device="cuda")
+        self.ctx.vocab_answers(x, s["table"], self.scale, entropy=entropy, top_ids=ids, top_logp=logp)
+        return ids, logp, entropy
 
     def last_rows(self, lists, s):
         """Serving: the newest position of every list alone, against the keys and values that the list has so far."""
@@ -163,13 +212,18 @@ def main():
     a.add_argument("--dim", type=int, default=128)
     a.add_argument("--heads", type=int, default=4)
     a.add_argument("--kv-heads", type=int, default=2)
+    a.add_argument("--hidden", type=int, default=0)
+    a.add_argument("--dropout", type=float, default=0.0)
     a = a.parse_args()
-    model = NextId(a.rows, a.dim, a.heads, a.kv_heads, a.dtype)
+    model = NextId(a.rows, a.dim, a.heads, a.kv_heads, a.dtype, hidden=a.hidden, dropout=a.dropout)
     for i in range(a.steps):
         lists = Lists(model.ctx, *batch(a.batch, a.rows, a.longest, i % 8))
         loss = model.step(lists, 0.05)
         if i % 10 == 0 or i == a.steps - 1:
             print(f"step {i}: loss {float(loss):.4f}, {lists.U} unique lists of {a.batch}, {lists.M} rows", flush=True)
+    ids, logp, entropy = model.answers(lists, 3)
+    for i in range(min(3, len(ids))):
+        print(f"next of list {i}: {ids[i].tolist()}, log probabilities {[round(v, 3) for v in logp[i].tolist()]}, entropy {float(entropy[i]):.3f}")
 
 
 if __name__ == "__main__":
