@@ -98,7 +98,7 @@ __device__ inline void finish(const Epilogue &e, uint64_t call, int64_t row, int
         for (int i = 0; i < 8; i++)
             v[i] = z[i];
     }
-    recd_store8(reinterpret_cast<T *>(reinterpret_cast<char *>(e.out) + row * e.out_stride) + col, count, v);
+    recd_store8_past(reinterpret_cast<T *>(reinterpret_cast<char *>(e.out) + row * e.out_stride) + col, count, v);
 }
 
 __device__ inline void load_bias(const float *bias, int col, int count, float *b)

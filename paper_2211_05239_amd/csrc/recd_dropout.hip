@@ -54,7 +54,7 @@ __global__ __launch_bounds__(kBlock) void k_dropout(int64_t pieces, int per_row,
 #pragma unroll
                     for (int e = 0; e < 8; e++)
                         v[i][e] += r[i][e];
-                recd_store8(out + rows[i] * D + cols[i] * 8, D - cols[i] * 8 >= 8 ? 8 : 4, v[i]);
+                recd_store8_past(out + rows[i] * D + cols[i] * 8, D - cols[i] * 8 >= 8 ? 8 : 4, v[i]);
             }
         at += kPieces * threads;
     }
