@@ -513,6 +513,46 @@ template <typename T, int KIND> __global__ __launch_bounds__(kBlock) void k_rows
     }
 }
 
+// A product of SLICES splits or more: 64 pieces of eight sums a block, whose waves add up equal parts of the splits in their order; the
+// waves' sums then go through LDS, in order too.  One lane after the other split, as k_rows has it, waits for memory each time and
+// leaves most of the card idle where the sums are few (grad_w of 300 007 x 64 -> 64 bf16 81 us, here 23; of 128 -> 512 123 and 110); four
+// waves 26 and 110, sixteen 24 and 112.
+constexpr int SLICES = 8;
+
+template <typename T> __global__ __launch_bounds__(64 * SLICES) void k_join(RowsArgs a)
+{
+    __shared__ float sums[SLICES][64][8 + 1];
+    const int lane = threadIdx.x & 63, slice = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t at = (int64_t)blockIdx.x * 64 + lane, row = at / a.per_row;
+    const int col = 8 * (int)(at - row * a.per_row), count = a.n_j - col >= 8 ? 8 : a.n_j - col;
+    float z[8];
+#pragma unroll
+    for (int e = 0; e < 8; e++)
+        z[e] = 0.0f;
+    if (row < a.n_i) {
+        const int each = (a.splits + SLICES - 1) / SLICES, last = (slice + 1) * each < a.splits ? (slice + 1) * each : a.splits;
+#pragma unroll 4
+        for (int s = slice * each; s < last; s++) {
+            float v[8];
+            recd_load8(a.parts + ((int64_t)s * a.n_i + row) * a.n_j + col, count, v);
+#pragma unroll
+            for (int e = 0; e < 8; e++)
+                z[e] += v[e];
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < 8; e++)
+        sums[slice][lane][e] = z[e];
+    __syncthreads();
+    if (slice || row >= a.n_i)
+        return;
+    for (int s = 1; s < SLICES; s++)
+#pragma unroll
+        for (int e = 0; e < 8; e++)
+            z[e] += sums[s][lane][e];
+    finish<T, PLAIN>(a.e, 0, row, col, count, a.n_j, nullptr, z, Eight<T>{}, nullptr);
+}
+
 // Adds up the blocks' column sums in their order: 32 columns by 32 threads, blocks in steps of 32, then the threads' sums.
 __global__ __launch_bounds__(1024) void k_join_columns(int64_t blocks, int n_j, const float *__restrict__ part, float *out)
 {
@@ -638,20 +678,23 @@ struct Shape {
     int64_t k_each, turn;  // rows of one launch
 };
 
-// What a tile of `side` costs on a compute unit, in us: a step of the contraction, and its beginning and end, for one block alone and
-// for each of those that share the unit (`resident` at a time).  `heavy`: with an activation or dropout at the end.
+// What a tile of `side` costs on a compute unit, in us: a step of the contraction, and its beginning and end, for one block alone
+// (`turned`: both operands' rows run along i and j, as grad_w has them) and for each of those that share the unit (`resident` at a time).
+// `heavy`: with an activation or dropout at the end.
 struct Cost {
     int side, resident;
-    float step_alone, step, ends_alone, ends, ends_heavy;
+    float step_alone, step_turned, step, ends_alone, ends, ends_heavy;
 };
-constexpr Cost kCost16[] = {{256, 1, 1.5f, 1.7f, 9.0f, 8.0f, 20.0f}, {128, 2, 0.6f, 0.52f, 3.0f, 3.5f, 5.0f}, {64, 4, 0.38f, 0.19f, 1.0f, 3.0f, 4.0f}};
-constexpr Cost kCost32[] = {{128, 2, 2.2f, 1.9f, 3.0f, 3.5f, 5.0f}, {64, 4, 0.75f, 0.5f, 1.0f, 3.0f, 4.0f}};
+constexpr Cost kCost16[] = {{256, 1, 1.5f, 1.5f, 1.7f, 9.0f, 8.0f, 20.0f},
+                            {128, 2, 0.6f, 0.85f, 0.52f, 3.0f, 3.5f, 5.0f},
+                            {64, 4, 0.38f, 0.38f, 0.19f, 1.0f, 3.0f, 4.0f}};
+constexpr Cost kCost32[] = {{128, 2, 2.2f, 2.2f, 1.9f, 3.0f, 3.5f, 5.0f}, {64, 4, 0.75f, 0.75f, 0.5f, 1.0f, 3.0f, 4.0f}};
 
 // The tile and the number of splits of least cost: by rounds of blocks on the compute units, and with splits by the launch that adds
 // them up and its traffic (8 bytes a sum at about 4.5 TB/s).  Measured (us, 16 bits; side / splits): 16 384 x 8192 -> 1024, grad_w 256/1 434,
-// 256/2 283, 128/1 310, 64/1 445; 4096 x 2048 -> 2048 256/1 53, 128/1 40, 64/1 52; 512 x 4096 -> 1024 256/8 31, 128/4 20, 64/1 27, 64/2 16;
+// 256/2 283, 128/1 310, 64/1 445; 16 384 x 2048 -> 1024, grad_w 128/2 122, 128/4 82, 256/6 87; 4096 x 2048 -> 2048 256/1 53, 128/1 40, 64/1 52; 512 x 4096 -> 1024 256/8 31, 128/4 20, 64/1 27, 64/2 16;
 // 128 x 8192 -> 1024 128/8 19, 64/1 55, 64/8 14.5; 300 007 x 128 -> 512 with GELU and dropout 256/1 243, 128/1 205.
-Shape product_shape(const recd_ctx *ctx, int64_t n_i, int n_j, int64_t K, recd_dtype dt, bool heavy)
+Shape product_shape(const recd_ctx *ctx, int64_t n_i, int n_j, int64_t K, recd_dtype dt, bool heavy, bool turned = false)
 {
     const int bk = 128 / (int)elem_size(dt);
     const int64_t steps = (K + bk - 1) / bk;
@@ -665,7 +708,7 @@ Shape product_shape(const recd_ctx *ctx, int64_t n_i, int n_j, int64_t K, recd_d
         const int64_t tiles = ((n_i + c.side - 1) / c.side) * ((n_j + c.side - 1) / c.side);
         for (int64_t k = 1; k <= 256 && (k == 1 || 4 * k <= steps); k += k < 4 ? 1 : k / 2) {
             const int64_t blocks = (tiles * k + ctx->num_cu - 1) / ctx->num_cu, each = (steps + k - 1) / k;
-            const double alone = (double)((blocks + c.resident - 1) / c.resident) * ((double)each * c.step_alone + c.ends_alone);
+            const double alone = (double)((blocks + c.resident - 1) / c.resident) * ((double)each * (turned ? c.step_turned : c.step_alone) + c.ends_alone);
             const double shared = (double)blocks * ((double)each * c.step + (heavy && k == 1 ? c.ends_heavy : c.ends));
             const double join = k == 1 ? 0.0 : 5.0 + (double)k * (double)n_i * n_j * 8.0 / 4.5e6;
             const double cost = (alone > shared ? alone : blocks == 1 ? alone : shared) + join;
@@ -751,6 +794,11 @@ template <typename T, int KIND> void launch_rows(const recd_ctx *ctx, RowsArgs a
     const RowsShape s = rows_shape(ctx, a.n_i, a.n_j);
     a.per_row = (a.n_j + 7) / 8;
     a.rows_each = s.each;
+    if constexpr (KIND == PLAIN)
+        if (a.splits >= SLICES) {
+            hipLaunchKernelGGL((k_join<T>), dim3((unsigned)((a.n_i * a.per_row + 63) / 64)), dim3(64 * SLICES), 0, st, a);
+            return;
+        }
     hipLaunchKernelGGL((k_rows<T, KIND>), dim3((unsigned)s.groups, (unsigned)s.blocks), dim3(kBlock), 0, st, a, s.clog);
 }
 
@@ -812,7 +860,7 @@ struct BackwardPlan {
                 parts = larger(parts, (size_t)gx.splits * a->n * a->in);
         }
         if (grad_w) {
-            gw = product_shape(ctx, a->out, a->in, a->n, a->dtype, false);
+            gw = product_shape(ctx, a->out, a->in, a->n, a->dtype, false, true);
             if (gw.splits > 1)
                 parts = larger(parts, (size_t)gw.splits * a->out * a->in);
         }

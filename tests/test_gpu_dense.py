@@ -71,6 +71,13 @@ def test_sizes(recd, ctx, dt, n, K, N):
     check(recd, ctx, *data(n, K, N, dt), "gelu", 0.1)
 
 
+# sums of many splits: of the rows for w's gradient, of the features for x's
+@pytest.mark.parametrize("dt,n,K,N", [("bf16", 20_011, 64, 24), ("f16", 5003, 8, 8), ("f32", 9001, 20, 12), ("f32", 2999, 132, 68),
+                                      ("bf16", 70, 24, 16_384), ("f32", 65, 4, 8188)])
+def test_many_splits(recd, ctx, dt, n, K, N):
+    check(recd, ctx, *data(n, K, N, dt), "none", 0.1)
+
+
 @pytest.mark.parametrize("n,K,N", [(1, 4, 4), (37, 12, 20), (100, 36, 4), (129, 68, 132), (1000, 4, 100)])
 def test_widths_of_four(recd, ctx, n, K, N):
     """fp32 rows that end in half a piece of eight."""
