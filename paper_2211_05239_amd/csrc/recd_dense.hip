@@ -673,7 +673,7 @@ template <typename T, int RG, int W, int UNROLL> __global__ __launch_bounds__(64
 constexpr int kFewRows = 64;
 
 struct Shape {
-    int side;              // rows and columns of a block's tile
+    int side, side_j;      // rows and columns of a block's tile
     int tiles_i, tiles_j, splits;
     int64_t k_each, turn;  // rows of one launch
 };
@@ -682,30 +682,33 @@ struct Shape {
 // (`turned`: both operands' rows run along i and j, as grad_w has them) and for each of those that share the unit (`resident` at a time).
 // `heavy`: with an activation or dropout at the end.
 struct Cost {
-    int side, resident;
+    int side, side_j, resident;
     float step_alone, step_turned, step, ends_alone, ends, ends_heavy;
 };
-constexpr Cost kCost16[] = {{256, 1, 1.5f, 1.5f, 1.7f, 9.0f, 8.0f, 20.0f},
-                            {128, 2, 0.6f, 0.85f, 0.52f, 3.0f, 3.5f, 5.0f},
-                            {64, 4, 0.38f, 0.38f, 0.19f, 1.0f, 3.0f, 4.0f}};
-constexpr Cost kCost32[] = {{128, 2, 2.2f, 2.2f, 1.9f, 3.0f, 3.5f, 5.0f}, {64, 4, 0.75f, 0.75f, 0.5f, 1.0f, 3.0f, 4.0f}};
+constexpr Cost kCost16[] = {{256, 256, 1, 1.5f, 1.5f, 1.7f, 9.0f, 8.0f, 20.0f},
+                            {128, 128, 2, 0.6f, 0.85f, 0.52f, 3.0f, 3.5f, 5.0f},
+                            {64, 64, 4, 0.38f, 0.38f, 0.19f, 1.0f, 3.0f, 4.0f}};
+constexpr Cost kCost32[] = {{128, 128, 2, 2.2f, 2.2f, 1.9f, 3.0f, 3.5f, 5.0f},
+                            {64, 64, 4, 0.75f, 0.75f, 0.5f, 1.0f, 3.0f, 4.0f},
+                            {128, 32, 4, 0.75f, 0.75f, 0.5f, 1.0f, 3.0f, 4.0f}};
 
 // The tile and the number of splits of least cost: by rounds of blocks on the compute units, and with splits by the launch that adds
 // them up and its traffic (8 bytes a sum at about 4.5 TB/s).  Measured (us, 16 bits; side / splits): 16 384 x 8192 -> 1024, grad_w 256/1 434,
 // 256/2 283, 128/1 310, 64/1 445; 16 384 x 2048 -> 1024, grad_w 128/2 122, 128/4 82, 256/6 87; 4096 x 2048 -> 2048 256/1 53, 128/1 40, 64/1 52; 512 x 4096 -> 1024 256/8 31, 128/4 20, 64/1 27, 64/2 16;
-// 128 x 8192 -> 1024 128/8 19, 64/1 55, 64/8 14.5; 300 007 x 128 -> 512 with GELU and dropout 256/1 243, 128/1 205.
+// 128 x 8192 -> 1024 128/8 19, 64/1 55, 64/8 14.5; 300 007 x 128 -> 512 with GELU and dropout 256/1 243, 128/1 205; 32 bits: 18 307 x 5072 -> 140 64/1 327,
+// 128 x 32/1 295, 2000 x 2048 -> 160 64/4 27, 128 x 32/3 23.
 Shape product_shape(const recd_ctx *ctx, int64_t n_i, int n_j, int64_t K, recd_dtype dt, bool heavy, bool turned = false)
 {
     const int bk = 128 / (int)elem_size(dt);
     const int64_t steps = (K + bk - 1) / bk;
     Shape s;
-    s.side = 64;
+    s.side = s.side_j = 64;
     int64_t splits = 1;
     double least = 1e30;
-    const Cost *costs = dt == RECD_F32 ? kCost32 : kCost16, *const end = costs + (dt == RECD_F32 ? 2 : 3);
+    const Cost *costs = dt == RECD_F32 ? kCost32 : kCost16, *const end = costs + 3;
     for (; costs != end; costs++) {
         const Cost &c = *costs;
-        const int64_t tiles = ((n_i + c.side - 1) / c.side) * ((n_j + c.side - 1) / c.side);
+        const int64_t tiles = ((n_i + c.side - 1) / c.side) * ((n_j + c.side_j - 1) / c.side_j);
         for (int64_t k = 1; k <= 256 && (k == 1 || 4 * k <= steps); k += k < 4 ? 1 : k / 2) {
             const int64_t blocks = (tiles * k + ctx->num_cu - 1) / ctx->num_cu, each = (steps + k - 1) / k;
             const double alone = (double)((blocks + c.resident - 1) / c.resident) * ((double)each * (turned ? c.step_turned : c.step_alone) + c.ends_alone);
@@ -716,6 +719,7 @@ Shape product_shape(const recd_ctx *ctx, int64_t n_i, int n_j, int64_t K, recd_d
                 least = cost;
                 splits = k;
                 s.side = c.side;
+                s.side_j = c.side_j;
             }
         }
     }
@@ -724,7 +728,7 @@ Shape product_shape(const recd_ctx *ctx, int64_t n_i, int n_j, int64_t K, recd_d
     s.splits = (int)((steps + each - 1) / each);
     if (s.splits < 1)
         s.splits = 1;
-    s.tiles_j = (n_j + s.side - 1) / s.side;
+    s.tiles_j = (n_j + s.side_j - 1) / s.side_j;
     // blocks of one launch: below 2^22
     const int64_t most = ((int64_t)1 << 22) / s.tiles_j * s.side;
     s.turn = s.splits > 1 || n_i <= most ? n_i : most;
@@ -756,6 +760,9 @@ template <typename T, bool PCOLS, bool QCOLS, int KIND> void launch_product(Prod
         if (s.side == 256) {
             if constexpr (sizeof(T) == 2)
                 hipLaunchKernelGGL((k_product<T, PCOLS, QCOLS, 2, 4, 4, 2, KIND>), grid, dim3(512), 0, st, b);
+        } else if (s.side_j == 32) {
+            if constexpr (sizeof(T) == 4)
+                hipLaunchKernelGGL((k_product<T, PCOLS, QCOLS, 4, 1, 1, 1, KIND>), grid, dim3(256), 0, st, b);
         } else if (s.side == 128)
             hipLaunchKernelGGL((k_product<T, PCOLS, QCOLS, 2, 2, 2, 2, KIND>), grid, dim3(256), 0, st, b);
         else

@@ -78,6 +78,12 @@ def test_many_splits(recd, ctx, dt, n, K, N):
     check(recd, ctx, *data(n, K, N, dt), "none", 0.1)
 
 
+# fp32 tiles of few columns, in each product: tiles of 64 would take the card once more
+@pytest.mark.parametrize("n,K,N", [(18_307, 68, 140), (18_307, 140, 68), (70, 140, 18_308)])
+def test_narrow_tiles(recd, ctx, n, K, N):
+    check(recd, ctx, *data(n, K, N, "f32", residual=True), "silu", 0.1)
+
+
 @pytest.mark.parametrize("n,K,N", [(1, 4, 4), (37, 12, 20), (100, 36, 4), (129, 68, 132), (1000, 4, 100)])
 def test_widths_of_four(recd, ctx, n, K, N):
     """fp32 rows that end in half a piece of eight."""
