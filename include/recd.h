@@ -740,7 +740,8 @@ recd_status recd_dense_backward(recd_ctx *ctx, const recd_dense_layer *a, const 
  *     k: 0 .. RECD_MAX_ANSWERS, at most V.  top_ids: device int64 [n, k], top_logp: device fp32 [n, k] (k > 0): the k largest
  *     logits' ids and log probabilities, the largest first.  Logits are put in order as 64-bit sums of exact products give them, and
  *     of equal ones the lowest id comes first; a NaN counts as -infinity.  (Where x or the table is not finite, or a row's sum of
- *     absolute products could pass the range of fp32, 32-bit sums choose which logits are looked at.)
+ *     absolute products could pass 4e37, 32-bit sums choose which logits are looked at.)  Of a row with a logit of +infinity
+ *     or NaN lse, entropy and the log probabilities are NaN; of one with -infinity the entropy may be.
  *     The gradient of logp is that of call 30 with the opposite sign.
  *     Up to 256 rows are the form for serving.  Rows of large batches go in turns.
  *     Workspace: 4 bytes for every row and 64 rows of the table (k > 0), of at most 512 MiB or 64 rows in a turn, and 12 bytes a row

@@ -88,12 +88,17 @@ struct Running {
     }
 };
 
+// In the place of a logit, in powers of two behind the running maximum, where there is no row: below all that a row has whose sums of
+// absolute products are less than kReach (2 log2(e) times that), and still finite behind another maximum.
+constexpr float kReach = 4e37f, kBehind = -1.4e38f;
+
 // Scores of 32 table rows, half of them in each lane of a pair, into the running sums; `left` of these rows are there.  Returns the
 // largest logit in powers of two.  It is found among what the exponentials are taken of anyway, z * c - m: the maximum of the scores
-// themselves would take an operation more for each.
+// themselves would take an operation more for each.  Behind an infinite logit the maximum starts again: the sums are NaN for good, but
+// the chunks' largest logits are still asked for.
 __device__ inline float add_up(Running &run, recd_f32x16 z, float c, int left, int lane)
 {
-    const float from = run.m == -INFINITY ? 0.0f : run.m;
+    const float from = __builtin_isinf(run.m) ? 0.0f : run.m;
 #pragma unroll
     for (int r = 0; r < 16; r++)
         z[r] = __builtin_fmaf(z[r], c, -from);
@@ -101,7 +106,7 @@ __device__ inline float add_up(Running &run, recd_f32x16 z, float c, int left, i
         asm volatile("" : "+v"(left));  // a branch: the last chunk alone pays for the comparisons
 #pragma unroll
         for (int r = 0; r < 16; r++)
-            z[r] = recd_score_row(r, lane) < left ? z[r] : -1e30f;
+            z[r] = recd_score_row(r, lane) < left ? z[r] : kBehind;
     }
     float top = -INFINITY;  // (of nothing but NaN)
 #pragma unroll
@@ -471,10 +476,10 @@ template <typename T, int NT> __global__ __launch_bounds__(NT) void k_answers_se
         w = max(w, top_abs[i]);
     }
     // 2^-22 of the largest sum of absolute products for each step of the sum, and what each loses where it underflows; without a bound,
-    // where it is not finite, the chunks are those that 32 bits name, and the best of them are kept
+    // where the sum is not finite or could pass the range, the chunks are those that 32 bits name, and the best of them are kept
     const float wf = __builtin_bit_cast(float, w);
     float d = (float)(a.D + 8) * (0x1p-22f * fabsf(a.scale) * sum_x * wf + 2e-38f * fmaxf(1.0f, fabsf(a.scale)));
-    const bool bound = d < INFINITY;
+    const bool bound = sum_x * wf * fmaxf(1.0f, fabsf(a.scale)) < kReach;
     d = bound && sum_x != 0.0f && wf != 0.0f ? d : 0.0f;
     __syncthreads();
     const float chunk_bar = group_bar - 2.0f * d;

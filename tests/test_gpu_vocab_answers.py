@@ -148,6 +148,39 @@ def test_values_near_the_ends_of_the_range(ctx):
         assert all(len(set(r)) == 20 and 0 <= min(r) and max(r) < 700 for r in ids.tolist()), size
 
 
+@pytest.mark.parametrize("n", [3, 300])
+def test_one_infinite_logit(ctx, n):
+    """The other ids keep their order behind it (whole numbers: sums of 32 bits are exact)."""
+    g = torch.Generator().manual_seed(2)
+    x, table = torch.randint(1, 4, (n, 16), generator=g).float(), torch.randint(-40, 41, (3000, 16), generator=g).float()
+    table[77, 3] = math.inf
+    got, ids = run(ctx, x, table, 1.0, torch.zeros(n, dtype=torch.int64), 20)
+    z = x.double() @ table.double().t()
+    z, order = torch.sort(z, dim=1, descending=True, stable=True)
+    assert torch.equal(ids, order[:, :20]) and not got["lse"].isfinite().any()
+
+
+@pytest.mark.parametrize("n", [3, 300])
+def test_logits_far_below_the_best(ctx, n):
+    """The last chunk has one row: what stands in the places behind it is no logit, however low the others are."""
+    x, table = torch.zeros(n, 4), torch.zeros(193, 4)
+    x[:, 0] = 1e16
+    table[:, 0] = -9e17
+    table[[0, 64, 128, 192], 0] = torch.tensor([0.0, -1e17, -2e17, -3e17])
+    _, ids = run(ctx, x, table, 1.0, torch.zeros(n, dtype=torch.int64), 4)
+    assert torch.equal(ids, torch.tensor([0, 64, 128, 192]).expand(n, 4))
+
+
+@pytest.mark.parametrize("n", [20, 300])
+def test_sums_that_pass_the_range(ctx, n):
+    """Some 32-bit sums are infinite or NaN, of finite rows: k different ids all the same."""
+    for size in (3e18, 1e19, 3e19, 1e20):
+        x, table, given = data(n, 1900, 16, "f32", 3)
+        for x, table in ((x, table), (x.abs(), table.abs())):
+            _, ids = run(ctx, x * size, table * size, 1.0, given, 20)
+            assert all(len(set(r)) == 20 and 0 <= min(r) and max(r) < 1900 for r in ids.tolist()), size
+
+
 @pytest.mark.parametrize("n", [4, 300])
 def test_what_is_left_out(recd, ctx, n):
     x, table, given = data(n, 3000, 64, "bf16", 8)
