@@ -242,25 +242,28 @@ template <int N = 0> __device__ inline void arrive()
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 }
 
+// Two tiles of each operand, then the sums on their way out.
+template <int WI, int WJ, int TI, int TJ> union ProductLds {
+    struct {
+        alignas(16) char p[2][32 * WI * TI * 128];
+        alignas(16) char q[2][32 * WJ * TJ * 128];
+    } t;
+    float out[WI * WJ][32 * (32 * TJ + 4)];
+    float cols[WI][32 * WJ * TJ];
+};
+
+// Block `block` of a product.
 template <typename T, bool PCOLS, bool QCOLS, int WI, int WJ, int TI, int TJ, int KIND>
-__global__ __launch_bounds__(64 * WI * WJ) void k_product(ProductArgs a)
+__device__ inline void product(const ProductArgs &a, unsigned block, ProductLds<WI, WJ, TI, TJ> &lds)
 {
     constexpr int THREADS = 64 * WI * WJ, BI = 32 * WI * TI, BJ = 32 * WJ * TJ;
     using P = Operand<T, PCOLS, BI, WI * WJ>;
     using Q = Operand<T, QCOLS, BJ, WI * WJ>;
     constexpr int BK = P::BK, LDW = 32 * TJ + 4;
-    __shared__ union {
-        struct {
-            alignas(16) char p[2][P::BYTES];
-            alignas(16) char q[2][Q::BYTES];
-        } t;
-        float out[WI * WJ][32 * LDW];
-        float cols[WI][BJ];
-    } lds;
     // neighbouring tiles on one die, whose L2 then serves what they share: eight tiles of rows by all of the columns, columns slowest
     const int64_t tiles = (int64_t)a.tiles_i * a.tiles_j, total = tiles * a.splits, each = (total + 7) / 8;
-    const int64_t at = (int64_t)(blockIdx.x & 7) * each + (blockIdx.x >> 3);
-    if ((int64_t)(blockIdx.x >> 3) >= each || at >= total)
+    const int64_t at = (int64_t)(block & 7) * each + (block >> 3);
+    if ((int64_t)(block >> 3) >= each || at >= total)
         return;
     const int split = (int)(at / tiles), in_split = (int)(at - split * tiles), band = in_split / (8 * a.tiles_j);
     const int in_band = in_split - band * 8 * a.tiles_j, high = a.tiles_i - 8 * band < 8 ? a.tiles_i - 8 * band : 8;
@@ -447,6 +450,27 @@ __global__ __launch_bounds__(64 * WI * WJ) void k_product(ProductArgs a)
                 a.e.col_part[(int64_t)ti * a.n_j + j0 + c] = s;
             }
     }
+}
+
+template <typename T, bool PCOLS, bool QCOLS, int WI, int WJ, int TI, int TJ, int KIND>
+__global__ __launch_bounds__(64 * WI * WJ) void k_product(ProductArgs a)
+{
+    __shared__ ProductLds<WI, WJ, TI, TJ> lds;
+    product<T, PCOLS, QCOLS, WI, WJ, TI, TJ, KIND>(a, blockIdx.x, lds);
+}
+
+// The gradients of x and w in one launch, where both have the same tile: the blocks of one fill what the other would leave idle at its end.
+// The `blocks_w` of w's gradient come first, as they mostly take longer.  Both, us in two launches and in one: 512 x 512 -> 512 bf16 12.0
+// and 9.2, 2000 x 128 -> 512 bf16 14.8 and 12.2, 300 x 2048 -> 512 fp32 25.3 and 20.5, 5021 x 516 -> 260 fp32 50.1 and 45.7, 16 384 x 8192 ->
+// 1024 bf16 574 and 562, 300 007 x 128 -> 512 bf16 177 and 166; 65 536 x 1024 -> 512 bf16 168 and 170.
+template <typename T, int WI, int WJ, int TI, int TJ>
+__global__ __launch_bounds__(64 * WI * WJ) void k_gradients(ProductArgs x, ProductArgs w, unsigned blocks_w)
+{
+    __shared__ ProductLds<WI, WJ, TI, TJ> lds;
+    if (blockIdx.x < blocks_w)
+        product<T, true, true, WI, WJ, TI, TJ, PLAIN>(w, blockIdx.x, lds);
+    else
+        product<T, false, true, WI, WJ, TI, TJ, PLAIN>(x, blockIdx.x - blocks_w, lds);
 }
 
 // The same from sums that are there: the splits' in `parts` (added up in their order), or z itself, or none.
@@ -736,16 +760,37 @@ Shape product_shape(const recd_ctx *ctx, int64_t n_i, int n_j, int64_t K, recd_d
     return s;
 }
 
+// f(tile's waves and tiles of them as constants), of the tile that a shape names
+template <typename T, typename F> void with_tile(const Shape &s, F f)
+{
+    auto tile = [&]<int WI, int WJ, int TI, int TJ>() { f.template operator()<WI, WJ, TI, TJ>(); };
+    if (s.side == 256) {
+        if constexpr (sizeof(T) == 2)
+            tile.template operator()<2, 4, 4, 2>();
+    } else if (s.side_j == 32) {
+        if constexpr (sizeof(T) == 4)
+            tile.template operator()<4, 1, 1, 1>();
+    } else if (s.side == 128)
+        tile.template operator()<2, 2, 2, 2>();
+    else
+        tile.template operator()<2, 2, 1, 1>();
+}
+
+unsigned product_blocks(ProductArgs &a, const Shape &s)
+{
+    a.tiles_i = (int)((a.n_i + s.side - 1) / s.side);
+    a.tiles_j = s.tiles_j;
+    a.splits = s.splits;
+    a.k_each = s.k_each;
+    return (unsigned)(((int64_t)a.tiles_i * a.tiles_j * a.splits + 7) / 8 * 8);
+}
+
 template <typename T, bool PCOLS, bool QCOLS, int KIND> void launch_product(ProductArgs a, const Shape &s, hipStream_t st)
 {
     const int64_t n = a.n_i;
     for (int64_t i0 = 0; i0 < n; i0 += s.turn) {
         ProductArgs b = a;
         b.n_i = n - i0 < s.turn ? n - i0 : s.turn;
-        b.tiles_i = (int)((b.n_i + s.side - 1) / s.side);
-        b.tiles_j = s.tiles_j;
-        b.splits = s.splits;
-        b.k_each = s.k_each;
         b.p = (const char *)a.p + (PCOLS ? i0 * (int64_t)sizeof(T) : i0 * a.p_stride);
         if (a.e.other)
             b.e.other = (const char *)a.e.other + i0 * a.e.other_stride;
@@ -756,17 +801,10 @@ template <typename T, bool PCOLS, bool QCOLS, int KIND> void launch_product(Prod
         if (a.e.col_part)
             b.e.col_part = a.e.col_part + i0 / s.side * a.n_j;
         b.e.row0 = a.e.row0 + i0;
-        const dim3 grid((unsigned)(((int64_t)b.tiles_i * b.tiles_j * b.splits + 7) / 8 * 8));
-        if (s.side == 256) {
-            if constexpr (sizeof(T) == 2)
-                hipLaunchKernelGGL((k_product<T, PCOLS, QCOLS, 2, 4, 4, 2, KIND>), grid, dim3(512), 0, st, b);
-        } else if (s.side_j == 32) {
-            if constexpr (sizeof(T) == 4)
-                hipLaunchKernelGGL((k_product<T, PCOLS, QCOLS, 4, 1, 1, 1, KIND>), grid, dim3(256), 0, st, b);
-        } else if (s.side == 128)
-            hipLaunchKernelGGL((k_product<T, PCOLS, QCOLS, 2, 2, 2, 2, KIND>), grid, dim3(256), 0, st, b);
-        else
-            hipLaunchKernelGGL((k_product<T, PCOLS, QCOLS, 2, 2, 1, 1, KIND>), grid, dim3(256), 0, st, b);
+        const unsigned blocks = product_blocks(b, s);
+        with_tile<T>(s, [&]<int WI, int WJ, int TI, int TJ>() {
+            hipLaunchKernelGGL((k_product<T, PCOLS, QCOLS, WI, WJ, TI, TJ, KIND>), dim3(blocks), dim3(64 * WI * WJ), 0, st, b);
+        });
     }
 }
 
@@ -843,7 +881,8 @@ struct BackwardPlan {
     Shape z, gx, gw;
     int64_t col_blocks;
     char *gz;
-    float *part, *col_part;  // (one array of parts serves the products in turn)
+    bool together;         // the gradients of x and w go into one launch
+    float *part, *part_w, *col_part;  // (z's and grad_x's parts in turn; grad_w's)
 
     void make(const recd_ctx *ctx, const recd_dense_layer *a, bool masked, bool sums, bool grad_x, bool grad_w, bool grad_bias, char *ws,
               size_t *bytes)
@@ -855,7 +894,7 @@ struct BackwardPlan {
         need_gz = a->n > 0 && (a->act != RECD_ACT_NONE || masked);
         again = a->n > 0 && a->act != RECD_ACT_NONE && !sums;
         gz = need_gz && (grad_x || grad_w) ? c.take<char>((size_t)a->n * a->out * e) : nullptr;
-        size_t parts = 0;
+        size_t parts = 0, parts_w = 0;
         if (again) {
             z = product_shape(ctx, a->n, a->out, a->in, a->dtype, true);
             if (z.splits > 1)
@@ -869,9 +908,16 @@ struct BackwardPlan {
         if (grad_w) {
             gw = product_shape(ctx, a->out, a->in, a->n, a->dtype, false, true);
             if (gw.splits > 1)
-                parts = larger(parts, (size_t)gw.splits * a->out * a->in);
+                parts_w = (size_t)gw.splits * a->out * a->in;
         }
-        part = parts ? c.take<float>(parts) : nullptr;
+        together = grad_x && grad_w && gx.side == gw.side && gx.side_j == gw.side_j && gx.turn == a->n;
+        if (!together) {
+            parts = larger(parts, parts_w);
+            part = part_w = parts ? c.take<float>(parts) : nullptr;
+        } else {
+            part = parts ? c.take<float>(parts) : nullptr;
+            part_w = parts_w ? c.take<float>(parts_w) : nullptr;
+        }
         col_blocks = a->n == 0 ? 0 : again && z.splits == 1 ? (a->n + z.side - 1) / z.side : rows_shape(ctx, a->n, a->out).blocks;
         col_part = grad_bias && a->n > 0 ? c.take<float>((size_t)col_blocks * a->out) : nullptr;
         *bytes = c.off;
@@ -1049,42 +1095,44 @@ recd_status recd_dense_backward(recd_ctx *ctx, const recd_dense_layer *a, const 
         if (grad_bias)
             hipLaunchKernelGGL(k_join_columns, dim3((unsigned)((out + 31) / 32)), dim3(1024), 0, st, plan.col_blocks, out,
                                plan.col_part, grad_bias);
-        if (a->n > 0 && grad_x) {
-            ProductArgs p{};
-            p.n_i = a->n;
-            p.n_j = in;
-            p.K = out;
-            p.p = gz;
-            p.q = w;
-            p.p_stride = gz_stride;
-            p.q_stride = in * e;
-            p.part = plan.gx.splits > 1 ? plan.part : nullptr;
-            p.e.out = grad_x;
-            p.e.out_stride = grad_x_stride * e;
-            launch_product<T, false, true, PLAIN>(p, plan.gx, st);
-            if (p.part) {
-                RowsArgs r{a->n, in, 0, plan.gx.splits, p.part, nullptr, 0, p.e};
-                launch_rows<T, PLAIN>(ctx, r, st);
-            }
+        ProductArgs px{}, pw{};
+        px.n_i = a->n;
+        px.n_j = in;
+        px.K = out;
+        px.p = gz;
+        px.q = w;
+        px.p_stride = gz_stride;
+        px.q_stride = in * e;
+        px.part = a->n > 0 && grad_x && plan.gx.splits > 1 ? plan.part : nullptr;
+        px.e.out = grad_x;
+        px.e.out_stride = grad_x_stride * e;
+        pw.n_i = out;
+        pw.n_j = in;
+        pw.K = a->n;
+        pw.p = gz;
+        pw.q = x;
+        pw.p_stride = gz_stride;
+        pw.q_stride = a->x_stride * e;
+        pw.part = grad_w && plan.gw.splits > 1 ? plan.part_w : nullptr;
+        pw.e.out = grad_w;
+        pw.e.out_stride = in * e;
+        if (plan.together) {
+            const unsigned blocks_w = product_blocks(pw, plan.gw), blocks_x = product_blocks(px, plan.gx);
+            with_tile<T>(plan.gx, [&]<int WI, int WJ, int TI, int TJ>() {
+                hipLaunchKernelGGL((k_gradients<T, WI, WJ, TI, TJ>), dim3(blocks_w + blocks_x), dim3(64 * WI * WJ), 0, st, px, pw, blocks_w);
+            });
+        } else {
+            if (a->n > 0 && grad_x)
+                launch_product<T, false, true, PLAIN>(px, plan.gx, st);
+            if (px.part)  // (its place is grad_w's too)
+                launch_rows<T, PLAIN>(ctx, RowsArgs{a->n, in, 0, plan.gx.splits, px.part, nullptr, 0, px.e}, st);
+            if (grad_w)
+                launch_product<T, true, true, PLAIN>(pw, plan.gw, st);
         }
-        if (grad_w) {
-            ProductArgs p{};
-            p.n_i = out;
-            p.n_j = in;
-            p.K = a->n;
-            p.p = gz;
-            p.q = x;
-            p.p_stride = gz_stride;
-            p.q_stride = a->x_stride * e;
-            p.part = plan.gw.splits > 1 ? plan.part : nullptr;
-            p.e.out = grad_w;
-            p.e.out_stride = in * e;
-            launch_product<T, true, true, PLAIN>(p, plan.gw, st);
-            if (p.part) {
-                RowsArgs r{out, in, 0, plan.gw.splits, p.part, nullptr, 0, p.e};
-                launch_rows<T, PLAIN>(ctx, r, st);
-            }
-        }
+        if (plan.together && px.part)
+            launch_rows<T, PLAIN>(ctx, RowsArgs{a->n, in, 0, plan.gx.splits, px.part, nullptr, 0, px.e}, st);
+        if (pw.part)
+            launch_rows<T, PLAIN>(ctx, RowsArgs{out, in, 0, plan.gw.splits, pw.part, nullptr, 0, pw.e}, st);
     });
     RECD_HIP(ctx, hipGetLastError());
     return RECD_OK;
