@@ -57,18 +57,28 @@ template <typename T> struct Eight {
     __device__ inline float operator[](int e) const { return (float)piece[e * (int)sizeof(T) / 16][e % (16 / (int)sizeof(T))]; }
 };
 
-// Eight (`count`) sums of row `row` from column `col` on.  `b`: the columns' bias, `other`: the residual's or grad_y's elements.
+template <typename T> __device__ inline void store_half(T *to, int half, const float *v)
+{
+    typedef T T4 __attribute__((ext_vector_type(4)));
+    const float *h = half ? v + 4 : v;
+    *reinterpret_cast<T4 *>(to + 4 * half) = T4{(T)h[0], (T)h[1], (T)h[2], (T)h[3]};
+}
+
+// Eight (`count`) sums of row `row` from column `col` on.  `b`: the columns' bias, `other`: the residual's or grad_y's elements.  `half`: the
+// one half of them that is wanted (FORWARD), or -1.
 template <typename T, int KIND>
 __device__ inline void finish(const Epilogue &e, uint64_t call, int64_t row, int col, int count, int n_j, const float *b, float *z,
-                              const Eight<T> &other, float *col_sum)
+                              const Eight<T> &other, float *col_sum, int half = -1)
 {
     float v[8];
     if constexpr (KIND == FORWARD) {
 #pragma unroll
         for (int i = 0; i < 8; i++)
             v[i] = z[i] + b[i];
-        if (e.sums)
+        if (e.sums && half < 0)
             recd_store8(e.sums + row * n_j + col, count, v);
+        else if (e.sums)
+            store_half(e.sums + row * n_j + col, half, v);
         recd_activate(e.act, v);
         if (e.mask.cut)
             recd_mask_apply(e.mask, recd_mask_bits(e.mask, call, e.row0 + row, col >> 3), v);
@@ -98,7 +108,11 @@ __device__ inline void finish(const Epilogue &e, uint64_t call, int64_t row, int
         for (int i = 0; i < 8; i++)
             v[i] = z[i];
     }
-    recd_store8_past(reinterpret_cast<T *>(reinterpret_cast<char *>(e.out) + row * e.out_stride) + col, count, v);
+    T *to = reinterpret_cast<T *>(reinterpret_cast<char *>(e.out) + row * e.out_stride) + col;
+    if (half < 0)
+        recd_store8_past(to, count, v);
+    else
+        store_half(to, half, v);
 }
 
 __device__ inline void load_bias(const float *bias, int col, int count, float *b)
@@ -601,6 +615,8 @@ __global__ __launch_bounds__(1024) void k_join_columns(int64_t blocks, int n_j, 
 // matrix cores; their sums are added up in LDS in the waves' order.  What bounds it is how many loads a compute unit has on their way: eight waves
 // with sixteen of each operand (fp32: sixteen with eight) for up to 16 rows.  One row 4096 -> 4096 bf16: 9.3 us a call, sixteen waves 11.3, four
 // 14.2; fp32 16.8, eight waves 20.1.
+// PARTS: of at most 16 / PARTS rows and features, the matrix instruction's 16 rows and columns hold PARTS neighbouring pieces of the contraction
+// each: the sums of a piece with itself count, and every load still brings 16 pieces of 64 bytes of w.
 template <typename T> struct Mma16;
 template <> struct Mma16<_Float16> {
     using Frag = recd_f16x8;
@@ -638,29 +654,32 @@ template <typename T> __device__ inline typename Mma16<T>::Frag few_frag(const c
     return u.f;
 }
 
-template <typename T, int RG, int W, int UNROLL> __global__ __launch_bounds__(64 * W) void k_few(ProductArgs a)
+template <typename T, int RG, int W, int UNROLL, int PARTS = 1> __global__ __launch_bounds__(64 * W) void k_few(ProductArgs a)
 {
+    constexpr int FE = 16 / PARTS;  // features, and with parts rows
+    static_assert(PARTS == 1 || RG == 1);
     __shared__ float join[W][16 * RG][16 + 4];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int j0 = blockIdx.x * 16, n = (int)a.n_i, K = (int)a.K;
-    const int j = j0 + (lane & 15) < a.n_j ? j0 + (lane & 15) : a.n_j - 1;
+    const int j0 = blockIdx.x * FE, n = (int)a.n_i, K = (int)a.K, part = (lane & 15) / FE;
+    const int j = j0 + (lane & (FE - 1)) < a.n_j ? j0 + (lane & (FE - 1)) : a.n_j - 1;
     const char *q = (const char *)a.q + j * a.q_stride;
     const char *p[RG];
 #pragma unroll
     for (int g = 0; g < RG; g++) {
-        const int i = 16 * g + (lane & 15);
+        const int i = 16 * g + (lane & (FE - 1));
         p[g] = (const char *)a.p + (i < n ? i : n - 1) * a.p_stride;
     }
     recd_f32x4 acc[RG];
 #pragma unroll
     for (int g = 0; g < RG; g++)
         acc[g] = recd_f32x4{};
-    const int of_split = (int)(a.k_each / 32), c0 = (int)blockIdx.y * of_split, each = (of_split + W - 1) / W;
-    const int all = (K + 31) / 32 < c0 + of_split ? (K + 31) / 32 : c0 + of_split;
+    constexpr int STEP = 32 * PARTS;
+    const int of_split = (int)(a.k_each / STEP), c0 = (int)blockIdx.y * of_split, each = (of_split + W - 1) / W;
+    const int all = (K + STEP - 1) / STEP < c0 + of_split ? (K + STEP - 1) / STEP : c0 + of_split;
     const int c1 = c0 + (wave + 1) * each < all ? c0 + (wave + 1) * each : all;
 #pragma unroll UNROLL
     for (int c = c0 + wave * each; c < c1; c++) {
-        const int k = 32 * c + 8 * (lane >> 4);
+        const int k = STEP * c + 32 * part + 8 * (lane >> 4);
         const auto qf = few_frag<T>(q, k, K);
 #pragma unroll
         for (int g = 0; g < RG; g++)
@@ -670,16 +689,22 @@ template <typename T, int RG, int W, int UNROLL> __global__ __launch_bounds__(64
     for (int g = 0; g < RG; g++)
         *reinterpret_cast<recd_f32x4 *>(&join[wave][16 * g + (lane & 15)][4 * (lane >> 4)]) = acc[g];
     __syncthreads();
-    const int row = threadIdx.x >> 1, at = 8 * (threadIdx.x & 1), col = j0 + at;
-    if (row >= 16 * RG || row >= n || col >= a.n_j)
+    // eight sums of a row; with four parts the block has one half of them
+    const int row = PARTS == 1 ? threadIdx.x >> 1 : threadIdx.x, at = PARTS == 1 ? 8 * (threadIdx.x & 1) : 0, col = (j0 + at) & ~7;
+    const int half = PARTS == 4 ? j0 >> 2 & 1 : -1;
+    if (row >= (PARTS == 1 ? 16 * RG : FE) || row >= n || col >= a.n_j)
         return;
     const int count = a.n_j - col >= 8 ? 8 : a.n_j - col;
     float z[8], b[8];
 #pragma unroll
     for (int e = 0; e < 8; e++) {
         z[e] = 0.0f;
+        if (PARTS == 4 && e >> 2 != half)
+            continue;
         for (int w = 0; w < W; w++)
-            z[e] += join[w][row][at + e];
+#pragma unroll
+            for (int h = 0; h < PARTS; h++)  // (products of one part with another are for nobody)
+                z[e] += join[w][row + FE * h][PARTS == 4 ? (e & 3) + 4 * h : at + 8 * h + e];
     }
     if (a.part) {
         recd_store8(a.part + ((int64_t)blockIdx.y * n + row) * a.n_j + col, count, z);
@@ -689,7 +714,7 @@ template <typename T, int RG, int W, int UNROLL> __global__ __launch_bounds__(64
     Eight<T> other{};
     if (a.e.other)
         other.load(reinterpret_cast<const char *>(a.e.other) + row * a.e.other_stride + (int64_t)col * sizeof(T), count);
-    finish<T, FORWARD>(a.e, recd_mask_call(a.e.mask), row, col, count, a.n_j, b, z, other, nullptr);
+    finish<T, FORWARD>(a.e, recd_mask_call(a.e.mask), row, col, count, a.n_j, b, z, other, nullptr, half);
 }
 
 // ---- how a call is cut ---------------------------------------------------------------------------------------------
@@ -851,6 +876,7 @@ template <typename T, int KIND> void launch_rows(const recd_ctx *ctx, RowsArgs a
 
 struct ForwardPlan {
     bool few;
+    int parts;             // of k_few
     Shape shape;
     float *part;
 
@@ -868,6 +894,18 @@ struct ForwardPlan {
             const int64_t each = (chunks + splits - 1) / splits;
             shape.k_each = 32 * each;
             shape.splits = (int)((chunks + each - 1) / each);
+            // Blocks of fewer features in place of splits and the launch that adds them up, up to 64 KiB of w a block, which a unit fetches in
+            // about 5 us (us a call, splits and parts: one row 4096 -> 1024 bf16 10.4 and 6.8, 8192 -> 1024 11.2 and 9.3, eight rows,
+            // 128 KiB, 12.1 and 13.6); without splits for long rows of 16 bits (one row 8192 -> 4096 22.3 and 16.3, 1024 -> 8192 7.1 and 9.1, fp32
+            // 2048 -> 4096 9.4 and 14.3)
+            const int row_bytes = a->in * (int)elem_size(a->dtype);
+            parts = a->n <= 4 ? 4 : a->n <= 8 ? 2 : 1;
+            if (row_bytes > (1 << 12) * parts || (shape.splits == 1 && (a->dtype == RECD_F32 || a->in < 4096)))
+                parts = 1;
+            if (parts > 1) {
+                shape.k_each = (a->in + 32 * parts - 1) / (32 * parts) * (32 * parts);
+                shape.splits = 1;
+            }
         } else
             shape = product_shape(ctx, a->n, a->out, a->in, a->dtype, heavy);
         if (shape.splits > 1)
@@ -1015,10 +1053,15 @@ recd_status recd_dense(recd_ctx *ctx, const recd_dense_layer *a, const void *x, 
     recd_with_type(a->dtype, [&](auto t) {
         using T = decltype(t);
         if (plan.few) {
-            const dim3 grid((unsigned)((a->out + 15) / 16), (unsigned)plan.shape.splits);
+            const int features = 16 / plan.parts;
+            const dim3 grid((unsigned)((a->out + features - 1) / features), (unsigned)plan.shape.splits);
             constexpr int W = sizeof(T) == 4 ? 16 : 8;
             p.k_each = plan.shape.k_each;
-            if (a->n <= 16)
+            if (plan.parts == 4)
+                hipLaunchKernelGGL((k_few<T, 1, W, 128 / W, 4>), grid, dim3(64 * W), 0, ctx->stream, p);
+            else if (plan.parts == 2)
+                hipLaunchKernelGGL((k_few<T, 1, W, 128 / W, 2>), grid, dim3(64 * W), 0, ctx->stream, p);
+            else if (a->n <= 16)
                 hipLaunchKernelGGL((k_few<T, 1, W, 128 / W>), grid, dim3(64 * W), 0, ctx->stream, p);
             else if (a->n <= 32)
                 hipLaunchKernelGGL((k_few<T, 2, 8, 4>), grid, dim3(64 * 8), 0, ctx->stream, p);

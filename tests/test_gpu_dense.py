@@ -71,6 +71,20 @@ def test_sizes(recd, ctx, dt, n, K, N):
     check(recd, ctx, *data(n, K, N, dt), "gelu", 0.1)
 
 
+# one to eight rows in blocks of four and eight features: ends of the contraction, of the features, of the rows, rows too long for it
+@pytest.mark.parametrize("dt", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("n", [1, 3, 4, 5, 8, 9])
+@pytest.mark.parametrize("K,N", [(2048, 8), (2056, 24), (4096, 200), (4104, 4104), (8192, 72), (8200, 16), (20_000, 40)])
+def test_few_rows_of_long_ones(recd, ctx, dt, n, K, N):
+    check(recd, ctx, *data(n, K, N, dt, residual=True), "silu", 0.1, kept=True)
+
+
+def test_few_rows_of_widths_of_four(recd, ctx):
+    for n in (1, 4, 7):
+        for K, N in ((2052, 4), (4100, 12), (2044, 60)):
+            check(recd, ctx, *data(n, K, N, "f32", residual=True), "gelu", 0.1, wide=True)
+
+
 # sums of many splits: of the rows for w's gradient, of the features for x's
 @pytest.mark.parametrize("dt,n,K,N", [("bf16", 20_011, 64, 24), ("f16", 5003, 8, 8), ("f32", 9001, 20, 12), ("f32", 2999, 132, 68),
                                       ("bf16", 70, 24, 16_384), ("f32", 65, 4, 8188)])
