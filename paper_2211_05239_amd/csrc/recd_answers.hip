@@ -9,6 +9,12 @@
 // largest logit is among the k best ones' (to the error of 32 bits): the second kernel finds these few chunks for each
 // row and computes their logits again, in 64 bits, which puts neighbours in rank in order that 32 bits do not tell apart.
 // Both terms of H are at least 0, so nothing cancels where one id has nearly all of the weight.
+//
+// What bounds them.  Many rows: the vector units.  A logit takes the matrix cores 2 D operations, and the vector units about eight
+// instructions' time: the product with scale, half a maximum, the exponential (four), the two sums.  4096 rows of 1 M x 128 bf16
+// take 1410 us of 1550, 0.74 PFLOP/s beside a large product's 1.40, vector units 72 % busy; the second kernel 215, 64-bit products
+// of the listed chunks.  Few rows: the table's way from memory, 1 M x 128 bf16 at 4.7 TB/s (54 us for one row without ids), and
+// for small tables the two launches and the chains of their loads (37 rows of 100 000 x 64 fp32: 18 and 15 us).
 #include "recd_internal.h"
 #include "recd_mfma.h"
 
@@ -19,7 +25,7 @@ namespace {
 constexpr int kChunk = 64;       // table rows
 constexpr int kWaves = 4;        // of the kernel of few rows
 constexpr int kMany = 8;         // of the kernel of many rows
-constexpr int kFewRows = 256;
+constexpr int kFewRows = 256;   // of 300 000 x 128 bf16, eight ids: 256 rows 71 us here, 300 rows by the kernel of many 97
 
 struct StreamArgs {
     int64_t n, V;
@@ -246,7 +252,8 @@ template <typename T, int DP, int N> __global__ __launch_bounds__(64 * kWaves) v
 }
 
 // Many rows: 32 in every wave of a block, all of which see every table row of the split, a chunk of them at a time in two
-// buffers of LDS.
+// buffers of LDS.  Four waves a SIMD for 16-bit rows of up to 128 (the stream of 4096 rows of 1 M x 128 bf16: 1370 us; of the compiler's own
+// choice of three 1530, of five 1480, of six 1770).
 template <typename T, int DP> __global__ __launch_bounds__(64 * kMany, sizeof(T) == 2 && DP <= 128 ? 4 : 2) void k_answers_many(StreamArgs a)
 {
     constexpr int KS = DP / 16;
@@ -387,8 +394,10 @@ template <typename T, int NT> __global__ __launch_bounds__(NT) void k_answers_se
             z = fma(x[e], (double)(float)v[e], z);
         return z;
     };
-    if (wave == 0) {  // the splits' sums: a lane's in their order, then the lanes'
+    // what does not depend on the chunks, by one wave: the splits' sums, a lane's in their order, then the lanes'; the given id
+    auto rest = [&] {
         Running all;
+#pragma unroll 4
         for (int s = lane; s < a.splits; s += 64)
             all.join(a.part_m[s * a.n + row], a.part_s[s * a.n + row], a.part_t[s * a.n + row]);
         for (int o = 1; o < 64; o <<= 1) {
@@ -396,15 +405,34 @@ template <typename T, int NT> __global__ __launch_bounds__(NT) void k_answers_se
             if ((lane & (2 * o - 1)) == 0)
                 all.join(m, s, t);
         }
+        const double lse = (double)all.m * 0.6931471805599453 + log((double)all.s);
         if (lane == 0) {
-            const double lse = (double)all.m * 0.6931471805599453 + log((double)all.s);
             lse_all = lse;
             if (a.lse)
                 a.lse[row] = (float)lse;
             if (a.entropy)
                 a.entropy[row] = (float)(log((double)all.s) - 0.6931471805599453 * (double)all.t / (double)all.s);
         }
+        if (!a.given)
+            return;
+        const int64_t g = a.given[row];
+        const bool has = g >= 0 && g < a.V;
+        Piece v{};
+        if (has && has_piece)
+            v = *reinterpret_cast<const Piece *>(table + g * a.D + at * E);
+        double z = part(v);
+        for (int o = 1; o < 1 << llog; o <<= 1)
+            z += __shfl_xor(z, o);
+        if (lane == 0)
+            a.logp[row] = has ? (float)(z * (double)a.scale - lse) : 0.0f;
+    };
+    if (a.k == 0) {
+        if (wave == 0)
+            rest();
+        return;
     }
+    if (NT == 256 && wave == WAVES - 1)
+        rest();
     float ax = 0.0f;
     for (int d = tid; d < a.D; d += NT)
         ax += fabsf((float)xr[d]);
@@ -421,30 +449,14 @@ template <typename T, int NT> __global__ __launch_bounds__(NT) void k_answers_se
     }
     // the groups' largest chunks: every 256th one
     const float *best = a.best + row * a.stride;
-    if (a.k) {
-        float top = -INFINITY;
+    float top = -INFINITY;
 #pragma unroll 8
-        for (int64_t c = tid; c < a.chunks; c += NT)
-            top = fmaxf(top, best[c]);
-        groups[tid] = top;
-    }
+    for (int64_t c = tid; c < a.chunks; c += NT)
+        top = fmaxf(top, best[c]);
+    groups[tid] = top;
     if (tid == 0)
         count = 0;
     __syncthreads();
-    if (wave == WAVES - 1 && a.given) {
-        const int64_t g = a.given[row];
-        const bool has = g >= 0 && g < a.V;
-        Piece v{};
-        if (has && has_piece)
-            v = *reinterpret_cast<const Piece *>(table + g * a.D + at * E);
-        double z = part(v);
-        for (int o = 1; o < 1 << llog; o <<= 1)
-            z += __shfl_xor(z, o);
-        if (lane == 0)
-            a.logp[row] = has ? (float)(z * (double)a.scale - lse_all) : 0.0f;
-    }
-    if (a.k == 0)
-        return;
     if (wave == 0) {
         // the k-th largest of the groups, bit by bit, of integers in the floats' order
         constexpr int MINE = kGroups / 64;
@@ -611,6 +623,8 @@ template <typename T, int NT> __global__ __launch_bounds__(NT) void k_answers_se
             range = kListed;
             continue;
         }
+        if (NT > 256 && from == 0 && wave == WAVES - 1)
+            rest();  // (here, where the other waves have something else to do: 37 rows of 100 000 x 64 fp32 34.5 -> 33.2 us)
         // waves take chunks while there is room for what all of them could find in theirs
         for (bool more = n > 0; more;) {
             while (*(volatile uint32_t *)&count <= KEPT - WAVES * kChunk) {
@@ -673,7 +687,8 @@ Shape stream_shape(const recd_ctx *ctx, int64_t n, int64_t V, int D, recd_dtype 
     s.row_blocks = (int)((n + s.rows - 1) / s.rows);
     s.chunks = (V + kChunk - 1) / kChunk;
     s.stride = (s.chunks + 3) / 4 * 4;
-    // Two blocks a compute unit at a time: of few rows as many splits as give these, of many the number whose rounds are fullest
+    // Two blocks a compute unit at a time: of few rows as many splits as give these (37 rows of 1 M x 128 bf16 76 us, three blocks 83,
+    // four 80), of many the number whose rounds are fullest
     // (70 000 rows have 274 blocks of rows: with one split most units would have one of them, and some two)
     const int64_t units = s.few ? (s.chunks + kWaves - 1) / kWaves : s.stride / 4;  // a wave's chunk each; four chunks
     const int64_t slots = 2 * ctx->num_cu;
@@ -824,7 +839,7 @@ recd_status recd_vocab_answers(recd_ctx *ctx, int64_t n, int64_t V, int D, recd_
             int llog = 0;  // lanes of a row
             while ((int)(16 / sizeof(T)) << llog < D)
                 llog++;
-            // blocks of sixteen waves where there are too few rows to fill the card with blocks of four
+            // blocks of sixteen waves where there are too few rows to fill the card with blocks of four (37 rows of 100 000 x 64: 19 and 51 us)
             if (rows <= 2 * ctx->num_cu)
                 hipLaunchKernelGGL((k_answers_select<T, 1024>), dim3((unsigned)rows), dim3(1024), 0, ctx->stream, b, llog);
             else

@@ -5,9 +5,16 @@
 //
 // Every product is C[i, j] = sum over k of P[i, k] Q[j, k].  An operand's rows in memory run along k (both of the layer itself), or along i
 // or j (w for grad_x, both for grad_w, which sums over the rows).  Tiles of both go into LDS by loads that write there, a step
-// ahead; a wave multiplies TI x TJ tiles of 32 x 32 on the matrix cores, features
-// as the product's rows and rows of x as its columns, so that a lane ends up with four neighbouring features of one row.  The sums go
-// through LDS once more: bias, activation, dropout, residual and the store work on eight neighbouring features a lane.
+// ahead; a wave multiplies TI x TJ tiles of 32 x 32 on the matrix cores, features as the product's rows and rows of x as its columns, so
+// that a lane ends up with four neighbouring features of one row.  The sums go through LDS once more: bias, activation, dropout, residual
+// and the store work on eight neighbouring features a lane.
+//
+// What bounds them.  Large products: loads into LDS and the matrix cores beside each other (8192^3 bf16 1.23 PFLOP/s; without the loads
+// 2.0, the loads alone as fast as 1.65; the matrix cores are 51 % busy at 1.85 GHz).  16 384 x 8192 -> 1024 with SiLU, both
+// directions: 790-835 us for 0.82 TFLOP.  Short contractions: what is done at a tile's end, on the vector units.  300 007 x 128 -> 512 with
+// GELU and dropout takes about 45 instructions an element, half of them the mask's ten rounds: 200 us forward, where memory would need 76,
+// 236 for gz; plain 102.  Few rows: w's way from memory, as far as one call's latency lets it (one row 4096 -> 16 384 bf16 5.0 TB/s).
+// Small fp32 products: a unit has one or two tiles (5021 x 516 -> 260: 395 tiles of 64, 23 us, of which the matrix cores need 9).
 #include "recd_epilogue.h"
 #include "recd_mfma.h"
 
@@ -144,8 +151,8 @@ template <> struct Quarter<float> {
 };
 
 // Tiles of one operand, two of them in LDS, which the loads write to by themselves.  COLS: a tile's rows are BK values of k, of SIDE
-// columns; else they are the SIDE rows, of BK elements along k (128 bytes: shorter ones ask the L2 twice for each line).  Rows and columns behind the operand's end are read
-// from the last one's place: what comes of them is not stored.
+// columns; else they are the SIDE rows, of BK elements along k (128 bytes: shorter ones ask the L2 twice for each line).  Rows and
+// columns behind the operand's end are read from the last one's place: what comes of them is not stored.
 //
 // A load of a wave fills 1024 bytes of LDS in its lanes' order; which 16 bytes of memory a lane brings is free.  So that the
 // lanes that read at a time meet in no bank, piece c of row r stands at place c ^ (r >> 1 & 7) of the row (reads of one piece from 16 rows), and
@@ -743,9 +750,10 @@ constexpr Cost kCost32[] = {{128, 128, 2, 2.2f, 2.2f, 1.9f, 3.0f, 3.5f, 5.0f},
 
 // The tile and the number of splits of least cost: by rounds of blocks on the compute units, and with splits by the launch that adds
 // them up and its traffic (8 bytes a sum at about 4.5 TB/s).  Measured (us, 16 bits; side / splits): 16 384 x 8192 -> 1024, grad_w 256/1 434,
-// 256/2 283, 128/1 310, 64/1 445; 16 384 x 2048 -> 1024, grad_w 128/2 122, 128/4 82, 256/6 87; 4096 x 2048 -> 2048 256/1 53, 128/1 40, 64/1 52; 512 x 4096 -> 1024 256/8 31, 128/4 20, 64/1 27, 64/2 16;
-// 128 x 8192 -> 1024 128/8 19, 64/1 55, 64/8 14.5; 300 007 x 128 -> 512 with GELU and dropout 256/1 243, 128/1 205; 32 bits: 18 307 x 5072 -> 140 64/1 327,
-// 128 x 32/1 295, 2000 x 2048 -> 160 64/4 27, 128 x 32/3 23.
+// 256/2 283, 128/1 310, 64/1 445; 16 384 x 2048 -> 1024, grad_w 128/2 122, 128/4 82, 256/6 87; 4096 x 2048 -> 2048 256/1 53, 128/1 40,
+// 64/1 52; 512 x 4096 -> 1024 256/8 31, 128/4 20, 64/1 27, 64/2 16; 128 x 8192 -> 1024 128/8 19, 64/1 55, 64/8 14.5; 300 007 x 128 -> 512
+// with GELU and dropout 256/1 243, 128/1 205; 32 bits: 18 307 x 5072 -> 140 64/1 327, 128 x 32/1 295, 2000 x 2048 -> 160 64/4 27,
+// 128 x 32/3 23.
 Shape product_shape(const recd_ctx *ctx, int64_t n_i, int n_j, int64_t K, recd_dtype dt, bool heavy, bool turned = false)
 {
     const int bk = 128 / (int)elem_size(dt);
@@ -760,7 +768,8 @@ Shape product_shape(const recd_ctx *ctx, int64_t n_i, int n_j, int64_t K, recd_d
         const int64_t tiles = ((n_i + c.side - 1) / c.side) * ((n_j + c.side_j - 1) / c.side_j);
         for (int64_t k = 1; k <= 256 && (k == 1 || 4 * k <= steps); k += k < 4 ? 1 : k / 2) {
             const int64_t blocks = (tiles * k + ctx->num_cu - 1) / ctx->num_cu, each = (steps + k - 1) / k;
-            const double alone = (double)((blocks + c.resident - 1) / c.resident) * ((double)each * (turned ? c.step_turned : c.step_alone) + c.ends_alone);
+            const double step_alone = turned ? c.step_turned : c.step_alone;
+            const double alone = (double)((blocks + c.resident - 1) / c.resident) * ((double)each * step_alone + c.ends_alone);
             const double shared = (double)blocks * ((double)each * c.step + (heavy && k == 1 ? c.ends_heavy : c.ends));
             const double join = k == 1 ? 0.0 : 5.0 + (double)k * (double)n_i * n_j * 8.0 / 4.5e6;
             const double cost = (alone > shared ? alone : blocks == 1 ? alone : shared) + join;

@@ -14,8 +14,8 @@ namespace {
 constexpr int kBlock = 256, kPieces = 4;
 
 // A lane takes 16 bytes of a row at a time: eight 16-bit elements, or four 32-bit ones, whose neighbouring lane has the other half
-// of the mask's piece (and makes its bits again: lanes of eight elements each, 32 bytes apart, ask for half lines, 96 us in place of 79 for both directions of
-// 50 021 x 516).
+// of the mask's piece (and makes its bits again: lanes of eight elements each, 32 bytes apart, ask for half lines, 96 us in place of 79 for
+// both directions of 50 021 x 516).
 template <typename T, bool RES>
 __global__ __launch_bounds__(kBlock) void k_dropout(int64_t pieces, int per_row, int D, RecdMask mask, const T *x,  // (may be out)
                                                     const T *res, T *out)
