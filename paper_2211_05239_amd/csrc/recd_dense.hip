@@ -275,7 +275,7 @@ template <int WI, int WJ, int TI, int TJ> union ProductLds {
 
 // Block `block` of a product.
 template <typename T, bool PCOLS, bool QCOLS, int WI, int WJ, int TI, int TJ, int KIND>
-__device__ inline void product(const ProductArgs &a, unsigned block, ProductLds<WI, WJ, TI, TJ> &lds)
+__device__ inline void product(ProductArgs a, unsigned block, ProductLds<WI, WJ, TI, TJ> &lds)
 {
     constexpr int THREADS = 64 * WI * WJ, BI = 32 * WI * TI, BJ = 32 * WJ * TJ;
     using P = Operand<T, PCOLS, BI, WI * WJ>;
@@ -482,8 +482,8 @@ __global__ __launch_bounds__(64 * WI * WJ) void k_product(ProductArgs a)
 
 // The gradients of x and w in one launch, where both have the same tile: the blocks of one fill what the other would leave idle at its end.
 // The `blocks_w` of w's gradient come first, as they mostly take longer.  Both, us in two launches and in one: 512 x 512 -> 512 bf16 12.0
-// and 9.2, 2000 x 128 -> 512 bf16 14.8 and 12.2, 300 x 2048 -> 512 fp32 25.3 and 20.5, 5021 x 516 -> 260 fp32 50.1 and 45.7, 16 384 x 8192 ->
-// 1024 bf16 574 and 562, 300 007 x 128 -> 512 bf16 177 and 166; 65 536 x 1024 -> 512 bf16 168 and 170.
+// and 9.2, 2000 x 128 -> 512 bf16 14.8 and 12.2, 300 x 2048 -> 512 fp32 25.3 and 20.5, 5021 x 516 -> 260 fp32 50.1 and 45.7, 300 007 x 128 ->
+// 512 bf16 177 and 166; tiles of 256, one of which fills a unit, stay in two (16 384 x 8192 -> 1024 bf16 with gz and the sums 776 and 800).
 template <typename T, int WI, int WJ, int TI, int TJ>
 __global__ __launch_bounds__(64 * WI * WJ) void k_gradients(ProductArgs x, ProductArgs w, unsigned blocks_w)
 {
@@ -957,7 +957,7 @@ struct BackwardPlan {
             if (gw.splits > 1)
                 parts_w = (size_t)gw.splits * a->out * a->in;
         }
-        together = grad_x && grad_w && gx.side == gw.side && gx.side_j == gw.side_j && gx.turn == a->n;
+        together = grad_x && grad_w && gx.side == gw.side && gx.side_j == gw.side_j && gx.side < 256 && gx.turn == a->n;
         if (!together) {
             parts = larger(parts, parts_w);
             part = part_w = parts ? c.take<float>(parts) : nullptr;
@@ -1171,7 +1171,8 @@ recd_status recd_dense_backward(recd_ctx *ctx, const recd_dense_layer *a, const 
         if (plan.together) {
             const unsigned blocks_w = product_blocks(pw, plan.gw), blocks_x = product_blocks(px, plan.gx);
             with_tile<T>(plan.gx, [&]<int WI, int WJ, int TI, int TJ>() {
-                hipLaunchKernelGGL((k_gradients<T, WI, WJ, TI, TJ>), dim3(blocks_w + blocks_x), dim3(64 * WI * WJ), 0, st, px, pw, blocks_w);
+                if constexpr (32 * WI * TI < 256)
+                    hipLaunchKernelGGL((k_gradients<T, WI, WJ, TI, TJ>), dim3(blocks_w + blocks_x), dim3(64 * WI * WJ), 0, st, px, pw, blocks_w);
             });
         } else {
             if (a->n > 0 && grad_x)
