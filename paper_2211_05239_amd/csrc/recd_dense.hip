@@ -12,8 +12,8 @@
 // What bounds them.  Large products: loads into LDS and the matrix cores beside each other (8192^3 bf16 1.23 PFLOP/s; without the loads
 // 2.0, the loads alone as fast as 1.65; the matrix cores are 51 % busy at 1.85 GHz).  16 384 x 8192 -> 1024 with SiLU, both
 // directions: 790-835 us for 0.82 TFLOP.  Short contractions: what is done at a tile's end, on the vector units.  300 007 x 128 -> 512 with
-// GELU and dropout takes about 45 instructions an element, half of them the mask's ten rounds: 200 us forward, where memory would need 76,
-// 236 for gz; plain 102.  Few rows: w's way from memory, as far as one call's latency lets it (one row 4096 -> 16 384 bf16 5.0 TB/s).
+// GELU and dropout takes about 42 instructions' time an element, GELU more than half of it: 186 us forward, where memory would need 76,
+// 210 for gz; without both 97.  Few rows: w's way from memory, as far as one call's latency lets it (one row 4096 -> 16 384 bf16 5.0 TB/s).
 // Small fp32 products: a unit has one or two tiles (5021 x 516 -> 260: 395 tiles of 64, 23 us, of which the matrix cores need 9).
 #include "recd_epilogue.h"
 #include "recd_mfma.h"
@@ -74,7 +74,7 @@ template <typename T> __device__ inline void store_half(T *to, int half, const f
 // Eight (`count`) sums of row `row` from column `col` on.  `b`: the columns' bias, `other`: the residual's or grad_y's elements.  `half`: the
 // one half of them that is wanted (FORWARD), or -1.
 template <typename T, int KIND>
-__device__ inline void finish(const Epilogue &e, uint64_t call, int64_t row, int col, int count, int n_j, const float *b, float *z,
+__device__ inline void finish(const Epilogue &e, const RecdBits &bits, int64_t row, int col, int count, int n_j, const float *b, float *z,
                               const Eight<T> &other, float *col_sum, int half = -1)
 {
     float v[8];
@@ -88,7 +88,7 @@ __device__ inline void finish(const Epilogue &e, uint64_t call, int64_t row, int
             store_half(e.sums + row * n_j + col, half, v);
         recd_activate(e.act, v);
         if (e.mask.cut)
-            recd_mask_apply(e.mask, recd_mask_bits(e.mask, call, e.row0 + row, col >> 3), v);
+            recd_mask_apply(e.mask, bits, v);
         if (e.other)
 #pragma unroll
             for (int i = 0; i < 8; i++)
@@ -98,7 +98,7 @@ __device__ inline void finish(const Epilogue &e, uint64_t call, int64_t row, int
         for (int i = 0; i < 8; i++)
             v[i] = other[i];
         if (e.mask.cut)
-            recd_mask_apply(e.mask, recd_mask_bits(e.mask, call, e.row0 + row, col >> 3), v);
+            recd_mask_apply(e.mask, bits, v);
         if (e.act != RECD_ACT_NONE) {
 #pragma unroll
             for (int i = 0; i < 8; i++)
@@ -417,7 +417,8 @@ __device__ inline void product(ProductArgs a, unsigned block, ProductLds<WI, WJ,
 #pragma unroll
     for (int i = 0; i < 8; i++)
         col_sum[i] = 0.0f;
-    const uint64_t call = KIND != PLAIN && !a.part ? recd_mask_call(a.e.mask) : 0;
+    const bool masked = KIND != PLAIN && !a.part && a.e.mask.cut;
+    const RecdMaskPiece mask = masked ? recd_mask_piece(a.e.mask, recd_mask_call(a.e.mask), col >> 3) : RecdMaskPiece{};
 #pragma unroll
     for (int i = 0; i < TI; i++) {
         recd_wave_sync();
@@ -434,6 +435,12 @@ __device__ inline void product(ProductArgs a, unsigned block, ProductLds<WI, WJ,
             now[pass] = other[pass];
         if (i + 1 < TI)
             fetch(i + 1);
+        // all of the masks' bits beside each other: a row's rounds wait for each other
+        RecdBits bits[PASSES] = {};
+        if (masked)
+#pragma unroll
+            for (int pass = 0; pass < PASSES; pass++)
+                bits[pass] = recd_mask_bits(a.e.mask, mask, (uint32_t)(a.e.row0 + i0) + (uint32_t)(32 * (wi * TI + i) + pass * RP + lane / LPR));
 #pragma unroll
         for (int pass = 0; pass < PASSES; pass++) {
             const int in_wave = pass * RP + lane / LPR, r = 32 * (wi * TI + i) + in_wave;
@@ -446,7 +453,7 @@ __device__ inline void product(ProductArgs a, unsigned block, ProductLds<WI, WJ,
             if (a.part)
                 recd_store8(a.part + ((int64_t)split * a.n_i + i0 + r) * a.n_j + col, count, z);
             else
-                finish<T, KIND>(a.e, call, i0 + r, col, count, a.n_j, b, z, now[pass], col_sum);
+                finish<T, KIND>(a.e, bits[pass], i0 + r, col, count, a.n_j, b, z, now[pass], col_sum);
         }
     }
     if constexpr (KIND == GRAD) {
@@ -516,7 +523,7 @@ template <typename T, int KIND> __global__ __launch_bounds__(kBlock) void k_rows
 #pragma unroll
     for (int i = 0; i < 8; i++)
         col_sum[i] = 0.0f;
-    const uint64_t call = KIND != PLAIN ? recd_mask_call(a.e.mask) : 0;
+    const RecdMaskPiece mask = KIND != PLAIN && a.e.mask.cut ? recd_mask_piece(a.e.mask, recd_mask_call(a.e.mask), piece) : RecdMaskPiece{};
     if (piece < a.per_row)
         for (int64_t row = first + (threadIdx.x >> clog); row < last; row += kBlock >> clog) {
             float z[8];
@@ -536,7 +543,8 @@ template <typename T, int KIND> __global__ __launch_bounds__(kBlock) void k_rows
             Eight<T> other{};
             if (KIND != PLAIN && a.e.other)
                 other.load(reinterpret_cast<const char *>(a.e.other) + row * a.e.other_stride + (int64_t)col * sizeof(T), count);
-            finish<T, KIND>(a.e, call, row, col, count, a.n_j, b, z, other, col_sum);
+            const RecdBits bits = KIND != PLAIN && a.e.mask.cut ? recd_mask_bits(a.e.mask, mask, (uint32_t)(a.e.row0 + row)) : RecdBits{};
+            finish<T, KIND>(a.e, bits, row, col, count, a.n_j, b, z, other, col_sum);
         }
     if constexpr (KIND == GRAD) {
         if (!a.e.col_part)
@@ -595,7 +603,7 @@ template <typename T> __global__ __launch_bounds__(64 * SLICES) void k_join(Rows
 #pragma unroll
         for (int e = 0; e < 8; e++)
             z[e] += sums[s][lane][e];
-    finish<T, PLAIN>(a.e, 0, row, col, count, a.n_j, nullptr, z, Eight<T>{}, nullptr);
+    finish<T, PLAIN>(a.e, RecdBits{}, row, col, count, a.n_j, nullptr, z, Eight<T>{}, nullptr);
 }
 
 // Adds up the blocks' column sums in their order: 32 columns by 32 threads, blocks in steps of 32, then the threads' sums.
@@ -721,7 +729,8 @@ template <typename T, int RG, int W, int UNROLL, int PARTS = 1> __global__ __lau
     Eight<T> other{};
     if (a.e.other)
         other.load(reinterpret_cast<const char *>(a.e.other) + row * a.e.other_stride + (int64_t)col * sizeof(T), count);
-    finish<T, FORWARD>(a.e, recd_mask_call(a.e.mask), row, col, count, a.n_j, b, z, other, nullptr, half);
+    const RecdBits bits = a.e.mask.cut ? recd_mask_bits(a.e.mask, recd_mask_call(a.e.mask), a.e.row0 + row, col >> 3) : RecdBits{};
+    finish<T, FORWARD>(a.e, bits, row, col, count, a.n_j, b, z, other, nullptr, half);
 }
 
 // ---- how a call is cut ---------------------------------------------------------------------------------------------

@@ -32,20 +32,52 @@ struct RecdBits {
 // The call's number, with what the device adds to it.
 __device__ inline uint64_t recd_mask_call(const RecdMask &m) { return m.step ? m.call + (uint64_t)*m.step : m.call; }
 
+__device__ inline void recd_philox(uint32_t &a, uint32_t &b, uint32_t &c, uint32_t &d, uint32_t k0, uint32_t k1)
+{
+    const uint64_t u = (uint64_t)a * 0xD2511F53u, v = (uint64_t)c * 0xCD9E8D57u;
+    a = __builtin_amdgcn_bitop3_b32((uint32_t)(v >> 32), b, k0, 0x96);  // xor of the three
+    b = (uint32_t)v;
+    c = __builtin_amdgcn_bitop3_b32((uint32_t)(u >> 32), d, k1, 0x96);
+    d = (uint32_t)u;
+}
+
+// What a column's piece has of the first three rounds in all rows below 2^32: of their six products the rows need two.  The state (a, b, c, d)
+// begins as (piece, row, call); a of the second round and c of the third follow from the row alone or from both, the others from the piece.
+// (Both directions of a layer 128 -> 512 with GELU and dropout on 300 007 rows: 600 us without it, 594 with it, and 584 where the
+// rows of a lane are made beside each other besides.)
+struct RecdMaskPiece {
+    uint32_t a1, d1, b2, c3, d3;  // a1 without the row, c3 without d2
+};
+
+__device__ inline RecdMaskPiece recd_mask_piece(const RecdMask &m, uint64_t call, int piece)
+{
+    const uint64_t u1 = (uint64_t)(uint32_t)piece * 0xD2511F53u, v1 = (uint64_t)(uint32_t)call * 0xCD9E8D57u;
+    const uint32_t c1 = (uint32_t)(u1 >> 32) ^ (uint32_t)(call >> 32) ^ m.k1;
+    const uint64_t v2 = (uint64_t)c1 * 0xCD9E8D57u;
+    const uint32_t a2 = (uint32_t)(v2 >> 32) ^ (uint32_t)v1 ^ (m.k0 + 0x9E3779B9u);
+    const uint64_t u3 = (uint64_t)a2 * 0xD2511F53u;
+    return RecdMaskPiece{(uint32_t)(v1 >> 32) ^ m.k0, (uint32_t)u1, (uint32_t)v2, (uint32_t)(u3 >> 32) ^ (m.k1 + 2 * 0xBB67AE85u), (uint32_t)u3};
+}
+
+__device__ inline RecdBits recd_mask_bits(const RecdMask &m, const RecdMaskPiece &p, uint32_t row)
+{
+    const uint64_t u2 = (uint64_t)(p.a1 ^ row) * 0xD2511F53u;
+    const uint32_t c2 = __builtin_amdgcn_bitop3_b32((uint32_t)(u2 >> 32), p.d1, m.k1 + 0xBB67AE85u, 0x96);
+    const uint64_t v3 = (uint64_t)c2 * 0xCD9E8D57u;
+    uint32_t a = __builtin_amdgcn_bitop3_b32((uint32_t)(v3 >> 32), p.b2, m.k0 + 2 * 0x9E3779B9u, 0x96);
+    uint32_t b = (uint32_t)v3, c = p.c3 ^ (uint32_t)u2, d = p.d3;
+#pragma unroll
+    for (uint32_t i = 3; i < 10; i++)
+        recd_philox(a, b, c, d, m.k0 + i * 0x9E3779B9u, m.k1 + i * 0xBB67AE85u);
+    return RecdBits{{a, b, c, d}};
+}
+
 __device__ inline RecdBits recd_mask_bits(const RecdMask &m, uint64_t call, int64_t row, int piece)
 {
     uint32_t a = (uint32_t)piece + ((uint32_t)(row >> 32) << 16), b = (uint32_t)row, c = (uint32_t)call, d = (uint32_t)(call >> 32);
-    uint32_t k0 = m.k0, k1 = m.k1;
 #pragma unroll
-    for (int i = 0; i < 10; i++) {
-        const uint64_t u = (uint64_t)a * 0xD2511F53u, v = (uint64_t)c * 0xCD9E8D57u;
-        a = __builtin_amdgcn_bitop3_b32((uint32_t)(v >> 32), b, k0, 0x96);  // xor of the three
-        b = (uint32_t)v;
-        c = __builtin_amdgcn_bitop3_b32((uint32_t)(u >> 32), d, k1, 0x96);
-        d = (uint32_t)u;
-        k0 += 0x9E3779B9u;
-        k1 += 0xBB67AE85u;
-    }
+    for (uint32_t i = 0; i < 10; i++)
+        recd_philox(a, b, c, d, m.k0 + i * 0x9E3779B9u, m.k1 + i * 0xBB67AE85u);
     return RecdBits{{a, b, c, d}};
 }
 
