@@ -568,11 +568,11 @@ template <typename T, int KIND> __global__ __launch_bounds__(kBlock) void k_rows
 
 // A product of SLICES splits or more: 64 pieces of eight sums a block, whose waves add up equal parts of the splits in their order; the
 // waves' sums then go through LDS, in order too.  One lane after the other split, as k_rows has it, waits for memory each time and
-// leaves most of the card idle where the sums are few (grad_w of 300 007 x 64 -> 64 bf16 81 us, here 23; of 128 -> 512 123 and 110); four
-// waves 26 and 110, sixteen 24 and 112.
+// leaves most of the card idle where the sums are few (grad_w of 300 007 x 64 -> 64 bf16 81 us, here 23; of 128 -> 512 123 and 110; 27 rows
+// 5844 -> 60 fp32 20.5 and 10.5, 100 rows 8192 -> 256 bf16 17.0 and 10.2); four waves 26 and 110 for the first two, sixteen 24 and 112.
 constexpr int SLICES = 8;
 
-template <typename T> __global__ __launch_bounds__(64 * SLICES) void k_join(RowsArgs a)
+template <typename T, int KIND> __global__ __launch_bounds__(64 * SLICES) void k_join(RowsArgs a)
 {
     __shared__ float sums[SLICES][64][8 + 1];
     const int lane = threadIdx.x & 63, slice = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -603,7 +603,15 @@ template <typename T> __global__ __launch_bounds__(64 * SLICES) void k_join(Rows
 #pragma unroll
         for (int e = 0; e < 8; e++)
             z[e] += sums[s][lane][e];
-    finish<T, PLAIN>(a.e, RecdBits{}, row, col, count, a.n_j, nullptr, z, Eight<T>{}, nullptr);
+    float b[8];
+    load_bias(KIND != PLAIN ? a.e.bias : nullptr, col, count, b);
+    Eight<T> other{};
+    if (KIND != PLAIN && a.e.other)
+        other.load(reinterpret_cast<const char *>(a.e.other) + row * a.e.other_stride + (int64_t)col * sizeof(T), count);
+    RecdBits bits{};
+    if (KIND != PLAIN && a.e.mask.cut)
+        bits = recd_mask_bits(a.e.mask, recd_mask_call(a.e.mask), a.e.row0 + row, col >> 3);
+    finish<T, KIND>(a.e, bits, row, col, count, a.n_j, b, z, other, nullptr);
 }
 
 // Adds up the blocks' column sums in their order: 32 columns by 32 threads, blocks in steps of 32, then the threads' sums.
@@ -882,9 +890,9 @@ template <typename T, int KIND> void launch_rows(const recd_ctx *ctx, RowsArgs a
     const RowsShape s = rows_shape(ctx, a.n_i, a.n_j);
     a.per_row = (a.n_j + 7) / 8;
     a.rows_each = s.each;
-    if constexpr (KIND == PLAIN)
+    if constexpr (KIND != GRAD)  // (which takes column sums besides)
         if (a.splits >= SLICES) {
-            hipLaunchKernelGGL((k_join<T>), dim3((unsigned)((a.n_i * a.per_row + 63) / 64)), dim3(64 * SLICES), 0, st, a);
+            hipLaunchKernelGGL((k_join<T, KIND>), dim3((unsigned)((a.n_i * a.per_row + 63) / 64)), dim3(64 * SLICES), 0, st, a);
             return;
         }
     hipLaunchKernelGGL((k_rows<T, KIND>), dim3((unsigned)s.groups, (unsigned)s.blocks), dim3(kBlock), 0, st, a, s.clog);
@@ -1150,6 +1158,16 @@ recd_status recd_dense_backward(recd_ctx *ctx, const recd_dense_layer *a, const 
             }
             if (!plan.again || plan.z.splits > 1) {
                 RowsArgs r{a->n, out, 0, plan.again ? plan.z.splits : 1, plan.again ? plan.part : nullptr, plan.again ? nullptr : sums, 0, ep};
+                if (r.parts && r.splits >= 2 * SLICES) {
+                    // their sum first, in the first one's place (27 rows 5844 -> 60 fp32 with SiLU: gz and grad_bias 23.4 us without, 16.3 with
+                    // it; from eight splits on 64 rows 4096 -> 128 bf16 13.8 and 16.7)
+                    RowsArgs z = r;
+                    z.e = Epilogue{};
+                    z.e.out = plan.part;
+                    z.e.out_stride = out * (int64_t)sizeof(float);
+                    launch_rows<float, PLAIN>(ctx, z, st);
+                    r.splits = 1;
+                }
                 launch_rows<T, GRAD>(ctx, r, st);
             }
         }

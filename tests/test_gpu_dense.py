@@ -92,6 +92,14 @@ def test_many_splits(recd, ctx, dt, n, K, N):
     check(recd, ctx, *data(n, K, N, dt), "none", 0.1)
 
 
+# ... and of a long contraction, in the layer itself and where z is made again
+@pytest.mark.parametrize("act,p", [("gelu", 0.1), ("none", 0.0)])
+@pytest.mark.parametrize("dt,n,K,N", [("f32", 27, 5844, 60), ("bf16", 65, 8192, 40), ("f16", 100, 3080, 8), ("f32", 70, 2052, 4)])
+def test_many_splits_of_a_long_contraction(recd, ctx, dt, n, K, N, act, p):
+    check(recd, ctx, *data(n, K, N, dt, residual=True), act, p)
+    check(recd, ctx, *data(n, K, N, dt, bias=False), act, p, wide=True, kept=True)
+
+
 # fp32 tiles of few columns, in each product: tiles of 64 would take the card once more
 @pytest.mark.parametrize("n,K,N", [(18_307, 68, 140), (18_307, 140, 68), (70, 140, 18_308)])
 def test_narrow_tiles(recd, ctx, n, K, N):
