@@ -96,15 +96,15 @@ __device__ inline void finish(const Epilogue &e, const RecdBits &bits, int64_t r
     } else if constexpr (KIND == GRAD) {
 #pragma unroll
         for (int i = 0; i < 8; i++)
-            v[i] = other[i];
-        if (e.mask.cut)
-            recd_mask_apply(e.mask, bits, v);
+            v[i] = e.mask.cut ? other[i] * e.mask.by : other[i];
         if (e.act != RECD_ACT_NONE) {
 #pragma unroll
             for (int i = 0; i < 8; i++)
                 z[i] += b[i];
             recd_activate_back(e.act, z, v);
         }
+        if (e.mask.cut)  // (last: the slope of a z that is not finite may be a NaN, and what is dropped is 0 whatever z is)
+            recd_mask_drop(e.mask, bits, v);
 #pragma unroll
         for (int i = 0; i < 8; i++)
             col_sum[i] += v[i];

@@ -81,12 +81,21 @@ __device__ inline RecdBits recd_mask_bits(const RecdMask &m, uint64_t call, int6
     return RecdBits{{a, b, c, d}};
 }
 
-// v times 1 / (1 - p) where it stays, 0 (also for an infinity or a NaN) where it does not.
+// 0 (also for an infinity or a NaN) where an element does not stay.
+__device__ inline void recd_mask_drop(const RecdMask &m, const RecdBits &bits, float *v)
+{
+#pragma unroll
+    for (int e = 0; e < 8; e++)
+        v[e] = bits.keep(e, m.cut) ? v[e] : 0.0f;
+}
+
+// v times 1 / (1 - p) where it stays, 0 where it does not.
 __device__ inline void recd_mask_apply(const RecdMask &m, const RecdBits &bits, float *v)
 {
 #pragma unroll
     for (int e = 0; e < 8; e++)
-        v[e] = bits.keep(e, m.cut) ? v[e] * m.by : 0.0f;
+        v[e] *= m.by;
+    recd_mask_drop(m, bits, v);
 }
 
 // ---- activations -------------------------------------------------------------------------------------------------
