@@ -94,6 +94,30 @@ struct Running {
     }
 };
 
+// The same of one lane along its part of the table, with sums whose loss does not grow with it: sixteen scores at a time are added up in 32
+// bits behind the maximum, and their sums in 64 bits behind the whole number next to it, so that a move to a larger maximum only
+// multiplies by a power of two; every score is rounded by one factor, whatever moves come after it.  (With 32-bit sums that every score was added
+// to, one logit over a million equal ones left lse off by 0.018 where 131 072 rows take the table in one split, a thousand times what
+// the logits' own roundings leave.)  t stays behind the maximum itself, as it would cancel against log s otherwise.
+struct Along {
+    float m = -INFINITY, unit = 1.0f;  // 2^(m - rint(m)), which s and t are to be divided by
+    double s = 0.0, t = 0.0;
+
+    __device__ inline void move(float now, float by)
+    {
+        const int shift = (int)fminf(fmaxf(rintf(m) - rintf(now), -2000.0f), 0.0f);
+        t = ldexp(fma(s, (double)by, t), shift);
+        s = ldexp(s, shift);
+        unit = recd_exp2(now - rintf(now));
+        m = now;
+    }
+    __device__ inline void add(float ds, float dt)
+    {
+        s += (double)(ds * unit);
+        t += (double)(dt * unit);
+    }
+};
+
 // In the place of a logit, in powers of two behind the running maximum, where there is no row: below all that a row has whose sums of
 // absolute products are less than kReach (2 log2(e) times that), and still finite behind another maximum.
 constexpr float kReach = 4e37f, kBehind = -1.4e38f;
@@ -102,7 +126,7 @@ constexpr float kReach = 4e37f, kBehind = -1.4e38f;
 // largest logit in powers of two.  It is found among what the exponentials are taken of anyway, z * c - m: the maximum of the scores
 // themselves would take an operation more for each.  Behind an infinite logit the maximum starts again: the sums are NaN for good, but
 // the chunks' largest logits are still asked for.
-__device__ inline float add_up(Running &run, recd_f32x16 z, float c, int left, int lane)
+__device__ inline float add_up(Along &run, recd_f32x16 z, float c, int left, int lane)
 {
     const float from = __builtin_isinf(run.m) ? 0.0f : run.m;
 #pragma unroll
@@ -121,19 +145,20 @@ __device__ inline float add_up(Running &run, recd_f32x16 z, float c, int left, i
     top = fmaxf(top, __shfl_xor(top, 32));
     const bool moves = (top > 0.0f || run.m == -INFINITY) && top > -INFINITY && left > 0;
     auto exponentials = [&](auto moved, float by) {
+        float s = 0.0f, t = 0.0f;
 #pragma unroll
         for (int r = 0; r < 16; r++) {
             const float d = moved.value ? z[r] + by : z[r], e = recd_exp2(d);
-            run.s += e;
-            run.t = __builtin_fmaf(e, d, run.t);
+            s += e;
+            t = __builtin_fmaf(e, d, t);
         }
+        run.add(s, t);
     };
     if (__any(moves)) {  // (seldom; both ways have exponentials of their own, or the other one would copy all scores)
-        const float by = moves ? -top : 0.0f;
-        const float f = run.m == -INFINITY ? 0.0f : recd_exp2(by);  // (nothing has been added up)
-        run.t = moves ? (run.t + run.s * by) * f : run.t;
-        run.s = moves ? run.s * f : run.s;
-        run.m = moves ? from + top : run.m;
+        // (by the rounded maxima, so that the scores and the sums so far move by the same; of a first one nothing has been added up)
+        const float now = from + top, by = !moves ? 0.0f : run.m == -INFINITY ? -top : run.m - now;
+        if (moves)
+            run.move(now, by);
         exponentials(std::true_type{}, by);
     } else
         exponentials(std::false_type{}, 0.0f);
@@ -169,7 +194,7 @@ template <typename T, int DP, int N> __global__ __launch_bounds__(64 * kWaves) v
 #pragma unroll
     for (int j = 0; j < N; j++)
         keep_rows<T, KS>(xf[j], a, row0 + 32 * j + (lane & 31), lane);
-    Running run[N];
+    Along run[N];
     uint32_t top_abs = 0;
     RecdStream<T, 32, DP, 64> stream;
     if (a.D < DP)
@@ -235,8 +260,8 @@ template <typename T, int DP, int N> __global__ __launch_bounds__(64 * kWaves) v
         run[j].t += __shfl_xor(run[j].t, 32);
         if (lane < 32) {
             lds.join[wave][0][32 * j + lane] = run[j].m;
-            lds.join[wave][1][32 * j + lane] = run[j].s;
-            lds.join[wave][2][32 * j + lane] = run[j].t;
+            lds.join[wave][1][32 * j + lane] = (float)(run[j].s / run[j].unit);
+            lds.join[wave][2][32 * j + lane] = (float)(run[j].t / run[j].unit);
         }
     }
     __syncthreads();
@@ -270,7 +295,7 @@ template <typename T, int DP> __global__ __launch_bounds__(64 * kMany, sizeof(T)
     const int64_t c0 = split * a.each, c1 = c0 + a.each < a.chunks ? c0 + a.each : a.chunks;
     Frag xf[KS];
     keep_rows<T, KS>(xf, a, row, lane);
-    Running run;
+    Along run;
     uint32_t top_abs = 0;
     RecdStream<T, kChunk, DP, 64 * kMany> stream;
     if (a.D < DP)
@@ -333,8 +358,8 @@ template <typename T, int DP> __global__ __launch_bounds__(64 * kMany, sizeof(T)
     run.t += __shfl_xor(run.t, 32);
     if (lane < 32 && row < a.n) {
         a.part_m[split * a.n + row] = run.m;
-        a.part_s[split * a.n + row] = run.s;
-        a.part_t[split * a.n + row] = run.t;
+        a.part_s[split * a.n + row] = (float)(run.s / run.unit);
+        a.part_t[split * a.n + row] = (float)(run.t / run.unit);
     }
 }
 

@@ -1,0 +1,95 @@
+"""Answers where sums are long, rows have no finite logit, single table rows are far larger than the rest, and rows go in turns."""
+import math
+
+import pytest
+import torch
+
+from tests import dense_util as du
+from tests import layers_util as lu
+from tests.dense_util import E
+
+pytestmark = pytest.mark.gpu
+
+# The sums of the exponentials: of 16 in a lane (15 E), times one factor (4 E), added up in 64 bits whatever the table's length; the joins of
+# waves, splits and lanes, 24 at most, are an E each besides the exponentials that bring them to one maximum (2 E each).  With the
+# exponential's and the logarithm's own error: 128 E.
+SUM = 128 * E
+
+
+@pytest.fixture(scope="module")
+def recd():
+    from paper_2211_05239_amd import recd as mod
+    return mod
+
+
+@pytest.fixture(scope="module")
+def ctx(recd):
+    c = recd.Context(0)
+    yield c
+    c.close()
+
+
+def answers(ctx, x, table, scale=1.0, k=0):
+    n = len(x)
+    lse, entropy = torch.empty(n, device="cuda"), torch.empty(n, device="cuda")
+    ids, logs = (torch.empty(n, k, dtype=torch.int64, device="cuda"), torch.empty(n, k, device="cuda")) if k else (None, None)
+    ctx.vocab_answers(x, table, scale, entropy=entropy, lse=lse, top_ids=ids, top_logp=logs)
+    return lse, entropy, ids, logs
+
+
+# by the kernel of many rows in one split, in a few, and by that of few rows
+@pytest.mark.parametrize("n,V,k", [(131_072, 1_000_001, 0), (9000, 1_000_001, 2), (300, 1_000_001, 2), (3, 4_000_001, 2)])
+def test_one_large_logit_over_many_equal_ones(ctx, n, V, k):
+    """Adding the same small value over and over rounds the same way each time.  One row of the table has the logit a, all others b, with
+    (V - 1) exp(b - a) from 2^-6 to 2^6; in 64 bits: lse = a + log1p((V - 1) exp(b - a)).  Products and sums of the logits are exact: a is a multiple of 2^-3, b 0."""
+    table = torch.zeros(V, 8, dtype=torch.bfloat16, device="cuda")
+    table[:, 1] = 1.0
+    table[V // 3, 1] = 0.0
+    table[V // 3, 0] = 1.0
+    x = torch.zeros(n, 8, dtype=torch.bfloat16, device="cuda")
+    gap = math.log(V) + (torch.arange(n, device="cuda") % 97 - 48) * math.log(2.0) / 8
+    x[:, 0] = (gap.double() * 8).round().bfloat16() / 8
+    lse, entropy, ids, logs = answers(ctx, x, table, 1.0, k)
+    a = x[:, 0].double()
+    q = (V - 1) * torch.exp(-a)                                                       # b = 0
+    want = a + torch.log1p(q)
+    p0, rest = 1 / (1 + q), q / (1 + q)
+    H = p0 * torch.log1p(q) + rest * want
+    # a logit in powers of two, less the maximum, is off by three roundings of up to 1.45 a
+    dz = 8 * E * a
+    assert ((lse.double() - want).abs() <= dz + SUM + E * want.abs()).all(), float((lse.double() - want).abs().max())
+    assert ((entropy.double() - H).abs() <= dz * (1 + H) + SUM * (1 + H) + 4 * E * (1 + H) * want).all(), float((entropy.double() - H).abs().max())
+    if k:
+        other = 0 if V // 3 else 1
+        assert (ids[:, 0] == V // 3).all() and (ids[:, 1] == other).all()
+        assert ((logs[:, 1].double() + want).abs() <= dz + SUM + E * want.abs()).all()
+
+
+@pytest.mark.parametrize("dt,n,V,D", [("bf16", 70_000, 30_011, 16), ("f32", 70_000, 10_001, 8), ("f16", 300, 200_003, 16), ("f32", 3, 1_000_003, 16)])
+def test_sums_do_not_lose_with_the_table(ctx, dt, n, V, D):
+    """Against 64 bits, with a bound of the sums that does not grow with V."""
+    x, table = du.rand((n, D), dt, 1), du.rand((V, D), dt, 2, 2.0 / D ** 0.5)
+    lse, entropy, _, _ = answers(ctx, x.cuda(), table.cuda())
+    rows = torch.randperm(n, generator=torch.Generator().manual_seed(3))[:20]
+    x = x[rows]
+    z = x.double() @ table.double().t()
+    size = x.double().abs() @ table.double().abs().t()
+    want = torch.logsumexp(z, 1)
+    p = (z - want[:, None]).exp()
+    H = torch.special.entr(p).sum(1)
+    dz = 4 * E * (D + 8) * size + 8 * E * (z.abs() + want.abs()[:, None])
+    assert ((lse.cpu()[rows].double() - want).abs() <= (p * dz).sum(1) + SUM + 2 * E * want.abs()).all()
+    dH = ((p * (z - want[:, None] + H[:, None]).abs()) * dz).sum(1)
+    assert ((entropy.cpu()[rows].double() - H).abs() <= dH + SUM * (1 + H) + 2 * E * H).all()
+
+
+def test_rows_in_turns(recd, ctx):
+    """9000 rows of 1 000 003 go in two turns: every row is the same, and as a small call has it."""
+    n, V, D = 9000, 1_000_003, 8
+    x, table = torch.zeros(n, D, dtype=torch.bfloat16, device="cuda"), torch.randn(V, D, device="cuda").bfloat16()
+    x[:, 0] = 1.0
+    lse, entropy, ids, logs = answers(ctx, x, table, 1.0, 1)
+    few = answers(ctx, x[:5], table, 1.0, 1)
+    for a, b in ((lse, few[0]), (entropy, few[1]), (logs[:, 0], few[3][:, 0])):
+        assert ((a.double() - b[0].double()).abs() <= 2 * SUM * (1 + b[0].double().abs())).all()
+    assert (ids == few[2][0]).all()
