@@ -103,10 +103,13 @@ struct Along {
     float m = -INFINITY, unit = 1.0f;  // 2^(m - rint(m)), which s and t are to be divided by
     double s = 0.0, t = 0.0;
 
-    __device__ inline void move(float now, float by)
+    // The sums move by what the maximum does as it is held, that is rounded: 0 in the last digits of a large one, where the scores' own
+    // difference to it may still be anything.
+    __device__ inline void move(float now)
     {
         const int shift = (int)fminf(fmaxf(rintf(m) - rintf(now), -2000.0f), 0.0f);
-        t = ldexp(fma(s, (double)by, t), shift);
+        const double by = m == -INFINITY ? 0.0 : (double)(m - now);  // (of a first one nothing has been added up)
+        t = ldexp(fma(s, by, t), shift);
         s = ldexp(s, shift);
         unit = recd_exp2(now - rintf(now));
         m = now;
@@ -155,11 +158,9 @@ __device__ inline float add_up(Along &run, recd_f32x16 z, float c, int left, int
         run.add(s, t);
     };
     if (__any(moves)) {  // (seldom; both ways have exponentials of their own, or the other one would copy all scores)
-        // (by the rounded maxima, so that the scores and the sums so far move by the same; of a first one nothing has been added up)
-        const float now = from + top, by = !moves ? 0.0f : run.m == -INFINITY ? -top : run.m - now;
         if (moves)
-            run.move(now, by);
-        exponentials(std::true_type{}, by);
+            run.move(from + top);
+        exponentials(std::true_type{}, moves ? -top : 0.0f);
     } else
         exponentials(std::false_type{}, 0.0f);
     return left > 0 ? from + top : -INFINITY;

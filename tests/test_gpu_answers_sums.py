@@ -83,6 +83,26 @@ def test_sums_do_not_lose_with_the_table(ctx, dt, n, V, D):
     assert ((entropy.cpu()[rows].double() - H).abs() <= dH + SUM * (1 + H) + 2 * E * H).all()
 
 
+@pytest.mark.parametrize("n", [3, 300])
+@pytest.mark.parametrize("size", [1e4, 1e7, 1e10, 1e15, 1e25])
+def test_large_logits(ctx, n, size):
+    """The difference of a score and the running maximum has digits that the maximum itself is rounded off."""
+    g = torch.Generator().manual_seed(4)
+    x, table = torch.rand(n, 4, generator=g) + 0.5, torch.rand(700, 4, generator=g) - 0.5
+    for order in (1, -1):
+        rows = table[(table.sum(1) * order).argsort()] * size        # the maximum rises all along, or comes first
+        lse, entropy, ids, _ = answers(ctx, x.cuda(), rows.cuda(), 1.0, 3)
+        z = x.double() @ rows.double().t()
+        want = torch.logsumexp(z, 1)
+        p = (z - want[:, None]).exp()
+        dz = 4 * E * 12 * (x.double() @ rows.double().abs().t()) + 8 * E * (z.abs() + want.abs()[:, None])
+        assert lse.isfinite().all() and entropy.isfinite().all()
+        # a logit is off by far more than 1 from 1e10 on: what the others can add to the largest is log(700) at most
+        assert ((lse.double().cpu() - want).abs() <= dz.max(1).values + SUM + E * want.abs()).all()
+        assert (entropy >= 0).all() and (entropy <= math.log(700) + 1e-3).all()
+        assert torch.equal(ids.cpu(), z.sort(dim=1, descending=True, stable=True)[1][:, :3])
+
+
 def test_rows_in_turns(recd, ctx):
     """9000 rows of 1 000 003 go in two turns: every row is the same, and as a small call has it."""
     n, V, D = 9000, 1_000_003, 8
