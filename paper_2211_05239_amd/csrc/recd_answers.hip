@@ -121,48 +121,50 @@ struct Along {
     }
 };
 
-// In the place of a logit, in powers of two behind the running maximum, where there is no row: below all that a row has whose sums of
-// absolute products are less than kReach (2 log2(e) times that), and still finite behind another maximum.
-constexpr float kReach = 4e37f, kBehind = -1.4e38f;
+// Below this a sum of absolute products leaves 32-bit sums finite, in whatever order, and the logits in powers of two too.
+constexpr float kReach = 4e37f;
 
 // Scores of 32 table rows, half of them in each lane of a pair, into the running sums; `left` of these rows are there.  Returns the
 // largest logit in powers of two.  It is found among what the exponentials are taken of anyway, z * c - m: the maximum of the scores
-// themselves would take an operation more for each.  Behind an infinite logit the maximum starts again: the sums are NaN for good, but
-// the chunks' largest logits are still asked for.
+// themselves would take an operation more for each.  Behind the table's end stand scores of one of its rows over again (its last one's),
+// which leave the maximum as it is; only the sums leave them out.  Behind an infinite logit the maximum starts again: the sums are NaN for
+// good, but the chunks' largest logits are still asked for.
 __device__ inline float add_up(Along &run, recd_f32x16 z, float c, int left, int lane)
 {
     const float from = __builtin_isinf(run.m) ? 0.0f : run.m;
 #pragma unroll
     for (int r = 0; r < 16; r++)
         z[r] = __builtin_fmaf(z[r], c, -from);
-    if (left < 32) {
-        asm volatile("" : "+v"(left));  // a branch: the last chunk alone pays for the comparisons
-#pragma unroll
-        for (int r = 0; r < 16; r++)
-            z[r] = recd_score_row(r, lane) < left ? z[r] : kBehind;
-    }
     float top = -INFINITY;  // (of nothing but NaN)
 #pragma unroll
     for (int r = 0; r < 16; r += 2)
         top = fmaxf(fmaxf(top, z[r]), z[r + 1]);
     top = fmaxf(top, __shfl_xor(top, 32));
     const bool moves = (top > 0.0f || run.m == -INFINITY) && top > -INFINITY && left > 0;
-    auto exponentials = [&](auto moved, float by) {
+    auto exponentials = [&](auto moved, auto ends, float by) {
         float s = 0.0f, t = 0.0f;
 #pragma unroll
         for (int r = 0; r < 16; r++) {
-            const float d = moved.value ? z[r] + by : z[r], e = recd_exp2(d);
+            float d = moved.value ? z[r] + by : z[r];
+            if (ends.value)
+                d = recd_score_row(r, lane) < left ? d : -1000.0f;  // (whose exponential is 0)
+            const float e = recd_exp2(d);
             s += e;
             t = __builtin_fmaf(e, d, t);
         }
         run.add(s, t);
     };
-    if (__any(moves)) {  // (seldom; both ways have exponentials of their own, or the other one would copy all scores)
+    // (maxima move seldom; all ways have exponentials of their own, or the others would copy all scores)
+    if (__any(moves) || left < 32) {
         if (moves)
             run.move(from + top);
-        exponentials(std::true_type{}, moves ? -top : 0.0f);
+        const float by = moves ? -top : 0.0f;
+        if (left < 32)
+            exponentials(std::true_type{}, std::true_type{}, by);
+        else
+            exponentials(std::true_type{}, std::false_type{}, by);
     } else
-        exponentials(std::false_type{}, 0.0f);
+        exponentials(std::false_type{}, std::false_type{}, 0.0f);
     return left > 0 ? from + top : -INFINITY;
 }
 

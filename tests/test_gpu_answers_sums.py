@@ -103,6 +103,37 @@ def test_large_logits(ctx, n, size):
         assert torch.equal(ids.cpu(), z.sort(dim=1, descending=True, stable=True)[1][:, :3])
 
 
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [3, 300])
+@pytest.mark.parametrize("V", [1, 31, 64, 65, 200, 4097])
+def test_rows_with_no_finite_logit(ctx, dt, n, V):
+    """-infinity everywhere: so is lse, what stands behind the table's last row is no logit, and of equal ones the lowest ids come first."""
+    x, table = du.rand((n, 16), dt, 1), du.rand((V, 16), dt, 2).abs()
+    table[:, 0] = 1.0
+    x[1] = 0.0
+    x[1, 0] = -math.inf
+    k = min(V, 5)
+    lse, _, ids, _ = answers(ctx, x.cuda(), table.cuda(), 1.0, k)
+    assert lse[1].item() == -math.inf and torch.equal(ids[1].cpu(), torch.arange(k))
+    rest = [i for i in range(n) if i != 1]
+    z = lu.logits(x[rest[:20]], table, 1.0)
+    assert torch.equal(ids.cpu()[rest[:20]], z.sort(dim=1, descending=True, stable=True)[1][:, :k])
+    assert lse[rest].isfinite().all()
+
+
+def test_logits_below_the_places_behind_the_table(ctx):
+    """Finite logits near the end of the range, in a table that ends inside a tile."""
+    for V in (1, 3, 33, 70):
+        for a in (-5e37, -1.2e38, -2e38):
+            table = torch.zeros(V, 4)
+            table[:, 0] = 1.0
+            x = torch.zeros(300, 4)
+            x[:, 0] = a
+            for m in (3, 300):
+                lse, _, _, _ = answers(ctx, x[:m].cuda(), table.cuda())
+                assert ((lse.double().cpu() - (x[:m, 0].double() + math.log(V))).abs() <= 4 * E * abs(a)).all(), (V, a)
+
+
 def test_rows_in_turns(recd, ctx):
     """9000 rows of 1 000 003 go in two turns: every row is the same, and as a small call has it."""
     n, V, D = 9000, 1_000_003, 8
