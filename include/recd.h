@@ -725,7 +725,10 @@ recd_status recd_dense(recd_ctx *ctx, const recd_dense_layer *a, const void *x, 
  *     in place of 8 bytes of traffic for each z: quicker for `in` up to about a thousand in 16 bits (a hundred in fp32).
  *     grad_y: device [n, out].   grad_x: device [n, in].   grad_w: device [out, in], dense, of dtype, overwritten.
  *     grad_bias: device fp32 [out], overwritten.  Each of the three may be NULL; none may be an input.
- *     gz is rounded to dtype where it enters the products.
+ *     gz is rounded to dtype where it enters the products (grad_bias is summed before that).  Of fp16 it is held times a power of two of
+ *     the call, which another launch finds from the largest finite grad_y: none of it passes the range, what is above 2^-28 of the
+ *     largest keeps fp16's digits, and what is below 2^-39 of it is 0.
+ *     What dropout dropped has gz = 0, be grad_y or z infinite or NaN there.
  *     Workspace: gz [n, out] (with an activation or dropout), sums of splits (call 35), and column sums of blocks of rows. */
 recd_status recd_dense_backward(recd_ctx *ctx, const recd_dense_layer *a, const void *x, const void *w, const float *bias,
                                 const float *sums, const void *grad_y, int64_t grad_y_stride, void *grad_x,

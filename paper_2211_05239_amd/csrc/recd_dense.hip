@@ -38,7 +38,93 @@ struct Epilogue {
     int64_t out_stride;
     float *sums;           // FORWARD: receives z [n_i, n_j], or null
     float *col_part;       // GRAD: sums of gz over the rows of a block, [blocks][n_j], or null
+    const uint32_t *largest;  // fp16, GRAD: k_largest's, or null
+    float *unit;              // fp16: what gz is held times; GRAD writes it for what is made of gz (with `largest`), or null
 };
+
+// gz of fp16 is held times a power of two of the call, which grad_x and grad_w are divided by: as it is, it would lose digits below 2^-14 and
+// vanish below 2^-25, where gradients may well lie that no one has scaled up, and grad_y / (1 - p) could pass 65504.  The power brings the
+// largest finite |grad_y| / (1 - p) * 1.13 (no slope is steeper: GELU's is 1.129 at most) to between 2^14 and 2^15, so that whole digits are left down to
+// 2^-28 of it, and something down to 2^-39.  It is found by a launch that reads grad_y (300 007 x 128 -> 512 with GELU and dropout, both directions: 581 -> 656 us).  bf16 has the
+// range of fp32 and needs none of it.
+constexpr int kLargest = 256;  // blocks of k_largest, four a lane here
+
+__device__ inline float gz_unit(const Epilogue &e)
+{
+    const recd_u32x4 v = *reinterpret_cast<const recd_u32x4 *>(e.largest + 4 * (threadIdx.x & 63));
+    uint32_t top = max(max(v[0], v[1]), max(v[2], v[3]));
+#pragma unroll
+    for (int o = 32; o; o >>= 1)
+        top = max(top, (uint32_t)__shfl_xor((int)top, o));
+    if (top == 0)
+        return 1.0f;
+    const float bound = (float)__builtin_bit_cast(_Float16, (unsigned short)top) * e.mask.by * 1.13f;
+    return ldexpf(1.0f, 15 - (int)((__builtin_bit_cast(uint32_t, bound) >> 23) - 126u));
+}
+
+// What the sums are multiplied by on their way out.  `first`: one block of the call's.
+template <typename T, int KIND> __device__ inline float unit_of(const Epilogue &e, bool first)
+{
+    if constexpr (std::is_same<T, _Float16>::value && KIND == GRAD) {
+        if (e.largest) {
+            const float unit = gz_unit(e);
+            if (first && threadIdx.x == 0)
+                *e.unit = unit;
+            return unit;
+        }
+    } else if constexpr (std::is_same<T, _Float16>::value && KIND == PLAIN) {
+        if (e.unit)
+            return 1.0f / *e.unit;
+    }
+    return 1.0f;
+}
+
+// Block by block, the largest finite |g| of rows [n, 8 * per_row], as the bits of an fp16.
+__global__ __launch_bounds__(1024) void k_largest(int64_t n, int per_row, const char *g, int64_t stride, uint32_t *out)
+{
+    typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+    __shared__ uint32_t tops[16];
+    // from the last row to the first, which the next launch then finds in the caches: `at` counts from the end
+    const int64_t pieces = n * per_row, threads = (int64_t)kLargest * 1024, drow = threads / per_row;
+    const int dcol = (int)(threads - drow * per_row);
+    int64_t at = (int64_t)blockIdx.x * 1024 + threadIdx.x, row = at / per_row;
+    int col = (int)(at - row * per_row);
+    u16x2 top = {0, 0};
+    while (at < pieces) {
+        recd_u32x4 v[4];
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            v[i] = recd_u32x4{};
+            if (at + i * threads < pieces)
+                v[i] = *reinterpret_cast<const recd_u32x4 *>(g + (n - 1 - row) * stride + 16 * col);
+            row += drow;
+            col += dcol;
+            if (col >= per_row) {
+                col -= per_row;
+                row++;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 4; i++)
+#pragma unroll
+            for (int w = 0; w < 4; w++) {
+                const u16x2 b = __builtin_bit_cast(u16x2, v[i][w] & 0x7fff7fffu);
+                top = __builtin_elementwise_max(top, u16x2{(unsigned short)(b[0] < 0x7c00 ? b[0] : 0), (unsigned short)(b[1] < 0x7c00 ? b[1] : 0)});
+            }
+        at += 4 * threads;
+    }
+    uint32_t all = top[0] > top[1] ? top[0] : top[1];
+    for (int o = 32; o; o >>= 1)
+        all = max(all, (uint32_t)__shfl_xor((int)all, o));
+    if ((threadIdx.x & 63) == 0)
+        tops[threadIdx.x >> 6] = all;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int w = 1; w < 16; w++)
+            all = max(all, tops[w]);
+        out[blockIdx.x] = all;
+    }
+}
 
 struct ProductArgs {
     int64_t n_i;
@@ -75,7 +161,7 @@ template <typename T> __device__ inline void store_half(T *to, int half, const f
 // one half of them that is wanted (FORWARD), or -1.
 template <typename T, int KIND>
 __device__ inline void finish(const Epilogue &e, const RecdBits &bits, int64_t row, int col, int count, int n_j, const float *b, float *z,
-                              const Eight<T> &other, float *col_sum, int half = -1)
+                              const Eight<T> &other, float *col_sum, float unit = 1.0f, int half = -1)
 {
     float v[8];
     if constexpr (KIND == FORWARD) {
@@ -115,6 +201,10 @@ __device__ inline void finish(const Epilogue &e, const RecdBits &bits, int64_t r
         for (int i = 0; i < 8; i++)
             v[i] = z[i];
     }
+    if constexpr (std::is_same<T, _Float16>::value && KIND != FORWARD)
+#pragma unroll
+        for (int i = 0; i < 8; i++)
+            v[i] *= unit;
     T *to = reinterpret_cast<T *>(reinterpret_cast<char *>(e.out) + row * e.out_stride) + col;
     if (half < 0)
         recd_store8_past(to, count, v);
@@ -418,6 +508,7 @@ __device__ inline void product(ProductArgs a, unsigned block, ProductLds<WI, WJ,
     for (int i = 0; i < 8; i++)
         col_sum[i] = 0.0f;
     const bool masked = KIND != PLAIN && !a.part && a.e.mask.cut;
+    const float unit = a.part ? 1.0f : unit_of<T, KIND>(a.e, block == 0);
     const RecdMaskPiece mask = masked ? recd_mask_piece(a.e.mask, recd_mask_call(a.e.mask), col >> 3) : RecdMaskPiece{};
 #pragma unroll
     for (int i = 0; i < TI; i++) {
@@ -453,7 +544,7 @@ __device__ inline void product(ProductArgs a, unsigned block, ProductLds<WI, WJ,
             if (a.part)
                 recd_store8(a.part + ((int64_t)split * a.n_i + i0 + r) * a.n_j + col, count, z);
             else
-                finish<T, KIND>(a.e, bits[pass], i0 + r, col, count, a.n_j, b, z, now[pass], col_sum);
+                finish<T, KIND>(a.e, bits[pass], i0 + r, col, count, a.n_j, b, z, now[pass], col_sum, unit);
         }
     }
     if constexpr (KIND == GRAD) {
@@ -523,6 +614,7 @@ template <typename T, int KIND> __global__ __launch_bounds__(kBlock) void k_rows
 #pragma unroll
     for (int i = 0; i < 8; i++)
         col_sum[i] = 0.0f;
+    const float unit = unit_of<T, KIND>(a.e, blockIdx.x == 0 && blockIdx.y == 0);
     const RecdMaskPiece mask = KIND != PLAIN && a.e.mask.cut ? recd_mask_piece(a.e.mask, recd_mask_call(a.e.mask), piece) : RecdMaskPiece{};
     if (piece < a.per_row)
         for (int64_t row = first + (threadIdx.x >> clog); row < last; row += kBlock >> clog) {
@@ -544,7 +636,7 @@ template <typename T, int KIND> __global__ __launch_bounds__(kBlock) void k_rows
             if (KIND != PLAIN && a.e.other)
                 other.load(reinterpret_cast<const char *>(a.e.other) + row * a.e.other_stride + (int64_t)col * sizeof(T), count);
             const RecdBits bits = KIND != PLAIN && a.e.mask.cut ? recd_mask_bits(a.e.mask, mask, (uint32_t)(a.e.row0 + row)) : RecdBits{};
-            finish<T, KIND>(a.e, bits, row, col, count, a.n_j, b, z, other, col_sum);
+            finish<T, KIND>(a.e, bits, row, col, count, a.n_j, b, z, other, col_sum, unit);
         }
     if constexpr (KIND == GRAD) {
         if (!a.e.col_part)
@@ -599,6 +691,7 @@ template <typename T, int KIND> __global__ __launch_bounds__(64 * SLICES) void k
     __syncthreads();
     if (slice || row >= a.n_i)
         return;
+    const float unit = unit_of<T, KIND>(a.e, false);  // (of gz itself column sums are taken besides: never here)
     for (int s = 1; s < SLICES; s++)
 #pragma unroll
         for (int e = 0; e < 8; e++)
@@ -611,7 +704,7 @@ template <typename T, int KIND> __global__ __launch_bounds__(64 * SLICES) void k
     RecdBits bits{};
     if (KIND != PLAIN && a.e.mask.cut)
         bits = recd_mask_bits(a.e.mask, recd_mask_call(a.e.mask), a.e.row0 + row, col >> 3);
-    finish<T, KIND>(a.e, bits, row, col, count, a.n_j, b, z, other, nullptr);
+    finish<T, KIND>(a.e, bits, row, col, count, a.n_j, b, z, other, nullptr, unit);
 }
 
 // Adds up the blocks' column sums in their order: 32 columns by 32 threads, blocks in steps of 32, then the threads' sums.
@@ -738,7 +831,7 @@ template <typename T, int RG, int W, int UNROLL, int PARTS = 1> __global__ __lau
     if (a.e.other)
         other.load(reinterpret_cast<const char *>(a.e.other) + row * a.e.other_stride + (int64_t)col * sizeof(T), count);
     const RecdBits bits = a.e.mask.cut ? recd_mask_bits(a.e.mask, recd_mask_call(a.e.mask), a.e.row0 + row, col >> 3) : RecdBits{};
-    finish<T, FORWARD>(a.e, bits, row, col, count, a.n_j, b, z, other, nullptr, half);
+    finish<T, FORWARD>(a.e, bits, row, col, count, a.n_j, b, z, other, nullptr, 1.0f, half);
 }
 
 // ---- how a call is cut ---------------------------------------------------------------------------------------------
@@ -945,6 +1038,8 @@ struct BackwardPlan {
     Shape z, gx, gw;
     int64_t col_blocks;
     char *gz;
+    uint32_t *largest;     // of k_largest, where gz is of fp16
+    float *unit;
     bool together;         // the gradients of x and w go into one launch
     float *part, *part_w, *col_part;  // (z's and grad_x's parts in turn; grad_w's)
 
@@ -958,6 +1053,9 @@ struct BackwardPlan {
         need_gz = a->n > 0 && (a->act != RECD_ACT_NONE || masked);
         again = a->n > 0 && a->act != RECD_ACT_NONE && !sums;
         gz = need_gz && (grad_x || grad_w) ? c.take<char>((size_t)a->n * a->out * e) : nullptr;
+        const bool scaled = need_gz && (grad_x || grad_w) && a->dtype == RECD_F16;
+        largest = scaled ? c.take<uint32_t>(kLargest) : nullptr;
+        unit = scaled ? c.take<float>(1) : nullptr;
         size_t parts = 0, parts_w = 0;
         if (again) {
             z = product_shape(ctx, a->n, a->out, a->in, a->dtype, true);
@@ -1075,7 +1173,7 @@ recd_status recd_dense(recd_ctx *ctx, const recd_dense_layer *a, const void *x, 
     p.p_stride = a->x_stride * e;
     p.q_stride = a->in * e;
     p.part = plan.part;
-    p.e = Epilogue{(int)a->act, mask, 0, bias, residual, a->residual_stride * e, y, a->y_stride * e, sums, nullptr};
+    p.e = Epilogue{(int)a->act, mask, 0, bias, residual, a->residual_stride * e, y, a->y_stride * e, sums, nullptr, nullptr, nullptr};
     recd_with_type(a->dtype, [&](auto t) {
         using T = decltype(t);
         if (plan.few) {
@@ -1141,7 +1239,10 @@ recd_status recd_dense_backward(recd_ctx *ctx, const recd_dense_layer *a, const 
         // gz, and its column sums
         const void *gz = plan.gz ? plan.gz : grad_y;
         const int64_t gz_stride = plan.gz ? out * e : grad_y_stride * e;
-        Epilogue ep{(int)a->act, mask, 0, bias, grad_y, grad_y_stride * e, plan.gz, out * e, nullptr, plan.col_part};
+        Epilogue ep{(int)a->act, mask, 0, bias, grad_y, grad_y_stride * e, plan.gz, out * e, nullptr, plan.col_part, plan.largest, plan.unit};
+        if (plan.largest)
+            hipLaunchKernelGGL(k_largest, dim3(kLargest), dim3(1024), 0, st, a->n, out / 8, (const char *)grad_y, grad_y_stride * e,
+                               plan.largest);
         if (a->n > 0 && (plan.gz || plan.col_part)) {
             if (plan.again) {
                 ProductArgs p{};
@@ -1185,6 +1286,7 @@ recd_status recd_dense_backward(recd_ctx *ctx, const recd_dense_layer *a, const 
         px.part = a->n > 0 && grad_x && plan.gx.splits > 1 ? plan.part : nullptr;
         px.e.out = grad_x;
         px.e.out_stride = grad_x_stride * e;
+        px.e.unit = pw.e.unit = plan.unit;
         pw.n_i = out;
         pw.n_j = in;
         pw.K = a->n;
