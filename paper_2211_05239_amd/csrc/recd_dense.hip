@@ -1111,7 +1111,7 @@ recd_status check_rows(recd_ctx *ctx, const char *what, const void *p, int64_t s
     const int64_t e = (int64_t)elem_size(dt);
     if (!p)
         return recd_fail(ctx, RECD_EINVAL, "%s: null pointer argument", what);
-    if ((uintptr_t)p % 16 || stride * e % 16 || stride < width || stride * e >= (int64_t)1 << 24)
+    if ((uintptr_t)p % 16 || stride < width || stride >= ((int64_t)1 << 24) / e || stride * e % 16)
         return recd_fail(ctx, RECD_EINVAL, "%s: rows of %d must be aligned to 16 bytes, not overlap and lie less than 16 MiB apart", what,
                          width);
     return RECD_OK;

@@ -151,3 +151,36 @@ def test_fp16_gradients_in_a_graph(recd):
         rows = torch.arange(n, device="cuda") != 3
         assert du.same_bits(small[0][rows], want[0][rows])
         c.close()
+
+
+@pytest.mark.parametrize("m", [1, 5, 16, 40, 64])
+def test_few_rows_far_apart(recd, ctx, m):
+    """Rows nearly 16 MiB apart in the forms of few rows: the bits of rows that lie densely."""
+    K, N, stride = 64, 40, (1 << 23) - 8
+    x, w, b, r = (t.cuda() for t in (du.rand((m, K), "bf16", 1), du.rand((N, K), "bf16", 2, 0.1), du.rand((N,), "f32", 3), du.rand((m, N), "bf16", 4)))
+    want, y = torch.empty_like(r), torch.full_like(r, float("nan"))
+    ctx.dense(x, w, b, want, act="gelu", residual=r)
+    far = torch.zeros((m - 1) * stride + 64, dtype=torch.bfloat16, device="cuda")
+    xs = far.as_strided((m, K), (stride, 1))
+    xs.copy_(x)
+    ctx.dense(xs, w, b, y, act="gelu", residual=r)
+    assert du.same_bits(y, want)
+    ys = far.as_strided((m, N), (stride, 1))
+    ys.copy_(r)
+    ctx.dense(x, w, b, ys, act="gelu", residual=ys)
+    assert du.same_bits(ys, want)
+
+
+def test_distances_whose_bytes_pass_64_bits(recd, ctx):
+    import ctypes as C
+    t = torch.zeros(64 * 64, device="cuda")
+    p = t.data_ptr()
+    for far in (1 << 62, (1 << 62) + 64, (1 << 63) - 64):
+        for place in range(3):
+            strides = [64, 64, 64]
+            strides[place] = far
+            a = recd._Dense(4, 64, 64, 0, 0, *strides, None)
+            assert recd._lib.recd_dense(ctx._h, C.byref(a), p, p, None, p, None, p) == recd.RECD_EINVAL
+        a = recd._Dense(4, 64, 64, 0, 0, 64, 64, 64, None)
+        assert recd._lib.recd_dense_backward(ctx._h, C.byref(a), p, p, None, None, p, far, p, 64, p, None) == recd.RECD_EINVAL
+        assert recd._lib.recd_dense_backward(ctx._h, C.byref(a), p, p, None, None, p, 64, p, far, p, None) == recd.RECD_EINVAL
