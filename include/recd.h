@@ -747,8 +747,8 @@ recd_status recd_dense_backward(recd_ctx *ctx, const recd_dense_layer *a, const 
  *     or NaN lse, entropy and the log probabilities are NaN; of one with -infinity the entropy may be.
  *     The gradient of logp is that of call 30 with the opposite sign.
  *     Up to 256 rows are the form for serving.  Rows of large batches go in turns.
- *     Workspace: 4 bytes for every row and 64 rows of the table (k > 0), of at most 512 MiB or 64 rows in a turn, and 12 bytes a row
- *     and split of the table. */
+ *     Workspace: 4 bytes for every row and 64 rows of the table (k > 0), of at most 512 MiB or 64 rows in a turn, 4 for 64 rows of the
+ *     table, and 12 bytes a row and split of the table. */
 #define RECD_MAX_ANSWERS 64
 recd_status recd_vocab_answers_workspace_bytes(int device, int64_t n, int64_t V, int D, recd_dtype dtype, int k, size_t *out_bytes);
 recd_status recd_vocab_answers(recd_ctx *ctx, int64_t n, int64_t V, int D, recd_dtype dtype, const void *x, const void *table,

@@ -38,7 +38,7 @@ struct StreamArgs {
     float *part_m, *part_s, *part_t; // [splits][n], in powers of two
     float *best;                     // [n][stride]: the chunks' largest logits, or null
     int64_t stride;
-    uint32_t *widest;                // [splits][waves]: the largest absolute value in the split's table rows, as an integer
+    uint32_t *widest;                // [chunks]: the largest absolute value in a chunk's table rows, as an integer, or null
 };
 
 // The larger of `top` and the absolute values in a piece: of 16-bit values in both halves.
@@ -57,6 +57,18 @@ template <typename T> __device__ inline uint32_t widest_of(uint32_t top, typenam
     return top;
 }
 
+// The wave's largest, without a way through LDS: neighbours, then rows of 16 lanes, then these to the next ones.
+__device__ inline uint32_t wave_top(uint32_t v)
+{
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xb1, 0xf, 0xf, true));   // lanes ^ 1
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4e, 0xf, 0xf, true));   // lanes ^ 2
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x141, 0xf, 0xf, true));  // mirrored in eight
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x140, 0xf, 0xf, true));  // mirrored in sixteen
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x142, 0xa, 0xf, false)); // lane 15 of a row to the next
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x143, 0xc, 0xf, false)); // lane 31 to the upper half
+    return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
+}
+
 // The wave's largest, as the bits of a float.
 template <typename T> __device__ inline uint32_t widest_float(uint32_t top)
 {
@@ -64,9 +76,7 @@ template <typename T> __device__ inline uint32_t widest_float(uint32_t top)
         const uint32_t a = top & 0xffffu, b = top >> 16, both = a > b ? a : b;
         top = __builtin_bit_cast(uint32_t, (float)__builtin_bit_cast(T, (unsigned short)both)) & 0x7fffffffu;  // (a NaN's is above an infinity's)
     }
-    for (int o = 32; o; o >>= 1)
-        top = max(top, (uint32_t)__shfl_xor((int)top, o));
-    return top;
+    return wave_top(top);
 }
 
 struct Running {
@@ -198,7 +208,6 @@ template <typename T, int DP, int N> __global__ __launch_bounds__(64 * kWaves) v
     for (int j = 0; j < N; j++)
         keep_rows<T, KS>(xf[j], a, row0 + 32 * j + (lane & 31), lane);
     Along run[N];
-    uint32_t top_abs = 0;
     RecdStream<T, 32, DP, 64> stream;
     if (a.D < DP)
         stream.clear_behind(lane, tile, a.D);
@@ -213,11 +222,12 @@ template <typename T, int DP, int N> __global__ __launch_bounds__(64 * kWaves) v
     for (; c < c1; c += kWaves) {
         const int left = a.V - c * kChunk < kChunk ? (int)(a.V - c * kChunk) : kChunk;
         float top[N];
+        uint32_t top_abs = 0;
 #pragma unroll
         for (int h = 0; h < 2; h++) {
             recd_wave_sync();
             stream.store(lane, tile, a.D);
-            if (rb == 0)
+            if (rb == 0 && a.widest)
 #pragma unroll
                 for (auto &piece : stream.held)
                     top_abs = widest_of<T>(top_abs, piece);
@@ -249,11 +259,11 @@ template <typename T, int DP, int N> __global__ __launch_bounds__(64 * kWaves) v
             if (a.best && lane < 32 && row < a.n)
                 a.best[row * a.stride + c] = top[j] * kRecdLn2;
         }
-    }
-    if (a.widest && rb == 0) {
-        top_abs = widest_float<T>(top_abs);
-        if (lane == 0)
-            a.widest[split * kWaves + wave] = top_abs;
+        if (rb == 0 && a.widest) {
+            top_abs = widest_float<T>(top_abs);
+            if (lane == 0)
+                a.widest[c] = top_abs;
+        }
     }
     // the waves' sums in their order
     __syncthreads();
@@ -287,6 +297,7 @@ template <typename T, int DP> __global__ __launch_bounds__(64 * kMany, sizeof(T)
     constexpr int KS = DP / 16;
     using Frag = typename RecdMma<T>::Frag;
     __shared__ RecdTile<T, kChunk, DP> tiles[2];
+    __shared__ uint32_t tops[2][kMany];
     // the row blocks of one split side by side on one die, whose L2 then serves the split's rows to all of them
     const int64_t total = (int64_t)a.splits * a.row_blocks, share = (total + 7) / 8;
     const int64_t at = (int64_t)(blockIdx.x & 7) * share + (blockIdx.x >> 3);
@@ -299,7 +310,6 @@ template <typename T, int DP> __global__ __launch_bounds__(64 * kMany, sizeof(T)
     Frag xf[KS];
     keep_rows<T, KS>(xf, a, row, lane);
     Along run;
-    uint32_t top_abs = 0;
     RecdStream<T, kChunk, DP, 64 * kMany> stream;
     if (a.D < DP)
         for (auto &tile : tiles)
@@ -308,17 +318,24 @@ template <typename T, int DP> __global__ __launch_bounds__(64 * kMany, sizeof(T)
         const int64_t left = a.V - c * kChunk;
         stream.load_rows(tid, (const T *)a.table + c * kChunk * a.D, left < kChunk ? (int)left : kChunk, a.D, a.D * sizeof(T));
     };
-    auto store = [&](int buf) {
+    // the blocks of a split's rows find the chunks' largest values in turns: this one's is `turn` chunks away
+    int turn = a.widest ? rb : INT32_MAX;
+    auto store = [&](int buf, int turn) {
         stream.store(tid, tiles[buf], a.D);
-        if (rb == 0)
+        if (turn == 0) {
+            uint32_t top_abs = 0;
 #pragma unroll
             for (int i = 0; i < stream.PT; i++)
                 if (tid + i * 64 * kMany < RecdTile<T, kChunk, DP>::PIECES)
                     top_abs = widest_of<T>(top_abs, stream.held[i]);
+            top_abs = widest_float<T>(top_abs);
+            if (lane == 0)
+                tops[buf][wave] = top_abs;
+        }
     };
     if (c0 < c1) {
         load(c0);
-        store(0);
+        store(0, turn);
         if (c0 + 1 < c1)
             load(c0 + 1);
     }
@@ -326,11 +343,18 @@ template <typename T, int DP> __global__ __launch_bounds__(64 * kMany, sizeof(T)
     recd_f32x4 four = {};
     for (int64_t c = c0; c < c1; c++) {
         const int buf = (int)(c - c0) & 1;
+        const int next = turn ? turn - 1 : a.row_blocks - 1;
         if (c + 1 < c1) {
-            store(1 - buf);
+            store(1 - buf, next);
             if (c + 2 < c1)
                 load(c + 2);
         }
+        if (turn == 0 && wave == 0) {
+            const uint32_t top_abs = wave_top(lane < kMany ? tops[buf][lane] : 0);
+            if (lane == 0)
+                a.widest[c] = top_abs;
+        }
+        turn = next;
         const int left = a.V - c * kChunk < kChunk ? (int)(a.V - c * kChunk) : kChunk;
         float top = -INFINITY;
 #pragma unroll
@@ -352,11 +376,6 @@ template <typename T, int DP> __global__ __launch_bounds__(64 * kMany, sizeof(T)
         }
         __syncthreads();
     }
-    if (a.widest && rb == 0) {
-        top_abs = widest_float<T>(top_abs);
-        if (lane == 0)
-            a.widest[split * kMany + wave] = top_abs;
-    }
     run.s += __shfl_xor(run.s, 32);
     run.t += __shfl_xor(run.t, 32);
     if (lane < 32 && row < a.n) {
@@ -368,7 +387,7 @@ template <typename T, int DP> __global__ __launch_bounds__(64 * kMany, sizeof(T)
 
 struct SelectArgs {
     int64_t n, V;
-    int D, k, splits, widest_n;
+    int D, k, splits;
     float scale;
     const void *x, *table;
     const int64_t *given;
@@ -384,10 +403,11 @@ constexpr int kGroups = 256, kListed = 1024;
 // `a` before `b` in the answers' order.
 __device__ inline bool before(double za, uint32_t a, double zb, uint32_t b) { return za > zb || (za == zb && a < b); }
 
-// A block a row.  Let d be what a 32-bit logit may be off by.  At least k logits are as large as the k-th largest of 256 groups'
-// largest chunks, L: so the k best are at least L - d, and stand in chunks of at least L - 2d.  The logits of these chunks are
-// computed again, a row of the table by neighbouring lanes, in an order that is the same for all rows, and what reaches the bar is
-// kept.  Where there is no more room the k best of it stay, the last of which is the new bar.
+// A block a row.  Let d be what a 32-bit logit of a chunk may be off by, which goes by the largest value in the chunk, so that a row of large
+// values widens its own chunk alone.  At least k logits are as large as the k-th largest, L, of what the 256 groups' chunks have for
+// certain, their largest logit less d: so the k best stand in chunks whose largest one and d reach L.  The logits of these chunks are
+// computed again, a row of the table by neighbouring lanes, in an order that is the same for all rows, and what reaches L is kept.  Where there is no
+// more room the k best of it stay, the last of which is the new bar.
 template <typename T, int NT> __global__ __launch_bounds__(NT) void k_answers_select(SelectArgs a, int llog)
 {
     constexpr int WAVES = NT / 64, E = 16 / sizeof(T), KEPT = 2 * WAVES * kChunk < 1024 ? 1024 : 2 * WAVES * kChunk;
@@ -396,7 +416,7 @@ template <typename T, int NT> __global__ __launch_bounds__(NT) void k_answers_se
     __shared__ uint32_t id[KEPT], list[kListed];
     __shared__ float groups[NT];
     __shared__ double lse_all;
-    __shared__ float group_bar, abs_x[WAVES];
+    __shared__ float group_bar;
     __shared__ uint32_t count, listed, taken, top_abs[WAVES];
     const int64_t row = blockIdx.x;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -461,27 +481,33 @@ template <typename T, int NT> __global__ __launch_bounds__(NT) void k_answers_se
     }
     if (NT == 256 && wave == WAVES - 1)
         rest();
-    float ax = 0.0f;
-    for (int d = tid; d < a.D; d += NT)
-        ax += fabsf((float)xr[d]);
-    uint32_t wide = 0;
-    for (int i = tid; i < a.widest_n; i += NT)
-        wide = max(wide, a.widest[i]);
-    for (int o = 32; o; o >>= 1) {
-        ax += __shfl_xor(ax, o);
-        wide = max(wide, (uint32_t)__shfl_xor((int)wide, o));
-    }
-    if (lane == 0) {
-        abs_x[wave] = ax;
-        top_abs[wave] = wide;
-    }
+    // 2^-22 of the largest sum of absolute products for each step of the sum, and what each loses where it underflows
+    float sum_x = 0.0f;
+#pragma unroll
+    for (int e = 0; e < E; e++)
+        sum_x += fabsf((float)x[e]);
+    for (int o = 1; o < 1 << llog; o <<= 1)
+        sum_x += __shfl_xor(sum_x, o);
+    const float reach = sum_x * fmaxf(1.0f, fabsf(a.scale)), by_wide = (float)(a.D + 8) * (0x1p-22f * fabsf(a.scale) * sum_x);
+    const float underflow = (float)(a.D + 8) * (2e-38f * fmaxf(1.0f, fabsf(a.scale)));
+    auto off = [&](uint32_t wide) {
+        const float w = __builtin_bit_cast(float, wide);
+        return sum_x != 0.0f && w != 0.0f && reach * w < kReach ? by_wide * w + underflow : 0.0f;
+    };
     // the groups' largest chunks: every 256th one
     const float *best = a.best + row * a.stride;
     float top = -INFINITY;
+    uint32_t wide = 0;
 #pragma unroll 8
-    for (int64_t c = tid; c < a.chunks; c += NT)
-        top = fmaxf(top, best[c]);
+    for (int64_t c = tid; c < a.chunks; c += NT) {
+        const uint32_t w = a.widest[c];
+        top = fmaxf(top, best[c] - off(w));
+        wide = max(wide, w);
+    }
     groups[tid] = top;
+    wide = wave_top(wide);
+    if (lane == 0)
+        top_abs[wave] = wide;
     if (tid == 0)
         count = 0;
     __syncthreads();
@@ -509,26 +535,18 @@ template <typename T, int NT> __global__ __launch_bounds__(NT) void k_answers_se
         if (lane == 0)
             group_bar = __builtin_bit_cast(float, bar ^ (bar >> 31 ? 0x80000000u : 0xffffffffu));
     }
-    float sum_x = 0.0f;
-    uint32_t w = 0;
-    for (int i = 0; i < WAVES; i++) {
-        sum_x += abs_x[i];
-        w = max(w, top_abs[i]);
-    }
-    // 2^-22 of the largest sum of absolute products for each step of the sum, and what each loses where it underflows; without a bound,
-    // where the sum is not finite or could pass the range, the chunks are those that 32 bits name, and the best of them are kept
-    const float wf = __builtin_bit_cast(float, w);
-    float d = (float)(a.D + 8) * (0x1p-22f * fabsf(a.scale) * sum_x * wf + 2e-38f * fmaxf(1.0f, fabsf(a.scale)));
-    const bool bound = sum_x * wf * fmaxf(1.0f, fabsf(a.scale)) < kReach;
-    d = bound && sum_x != 0.0f && wf != 0.0f ? d : 0.0f;
+    for (int i = 0; i < WAVES; i++)
+        wide = max(wide, top_abs[i]);
+    // without a bound, where the sum is not finite or could pass the range, the chunks are those that 32 bits name, and the best of them are kept
+    const bool bound = reach * __builtin_bit_cast(float, wide) < kReach;
     __syncthreads();
-    const float chunk_bar = group_bar - 2.0f * d;
     // what is kept comes before (bar, bar_id): the smallest of the k best so far, or all that may be among them
-    double bar = bound ? (double)group_bar - (double)d : -INFINITY;
+    const double chunk_bar = group_bar;
+    double bar = bound ? chunk_bar : -INFINITY;
     uint32_t bar_id = 0xffffffffu;
     auto may_hold = [&](int64_t c) {
-        const double v = (double)best[c] + (double)d;
-        return v > bar || (v == bar && (uint64_t)c * kChunk < bar_id);
+        const double v = (double)best[c] + (double)off(a.widest[c]);
+        return v >= chunk_bar && (v > bar || (v == bar && (uint64_t)c * kChunk < bar_id));
     };
     auto ranked = [&](int kept) {
         if (kept >= a.k) {
@@ -639,7 +657,7 @@ template <typename T, int NT> __global__ __launch_bounds__(NT) void k_answers_se
         __syncthreads();
 #pragma unroll 8
         for (int64_t c = from + tid; c < to; c += NT)
-            if (best[c] >= chunk_bar && may_hold(c)) {
+            if (may_hold(c)) {
                 const uint32_t slot = atomicAdd(&listed, 1u);
                 if (slot < kListed)
                     list[slot] = (uint32_t)c;
@@ -746,7 +764,7 @@ void carve(WsCarver &c, StreamArgs &a, bool top)
     a.part_s = c.take<float>((size_t)a.splits * a.n);
     a.part_t = c.take<float>((size_t)a.splits * a.n);
     a.best = top ? c.take<float>((size_t)a.n * a.stride) : nullptr;
-    a.widest = top ? c.take<uint32_t>((size_t)a.splits * kMany) : nullptr;
+    a.widest = top ? c.take<uint32_t>((size_t)a.stride) : nullptr;
 }
 
 recd_status check_answers(recd_ctx *ctx, int64_t n, int64_t V, int D, recd_dtype dt, float scale, int k)
@@ -857,7 +875,7 @@ recd_status recd_vocab_answers(recd_ctx *ctx, int64_t n, int64_t V, int D, recd_
         RECD_TRY(recd_reserve(ctx, size.off));
         WsCarver c(ctx->ws);
         carve(c, a, k > 0);
-        SelectArgs b{rows, V, D, k, s.splits, k > 0 ? s.splits * (s.few ? kWaves : kMany) : 0, scale, a.x, table, given ? given + at : nullptr,
+        SelectArgs b{rows, V, D, k, s.splits, scale, a.x, table, given ? given + at : nullptr,
                      a.part_m, a.part_s, a.part_t, a.best, a.widest, s.chunks, s.stride, logp ? logp + at : nullptr,
                      entropy ? entropy + at : nullptr, lse ? lse + at : nullptr, k > 0 ? top_logp + at * k : nullptr,
                      k > 0 ? top_ids + at * k : nullptr};

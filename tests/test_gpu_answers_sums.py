@@ -134,6 +134,43 @@ def test_logits_below_the_places_behind_the_table(ctx):
                 assert ((lse.double().cpu() - (x[:m, 0].double() + math.log(V))).abs() <= 4 * E * abs(a)).all(), (V, a)
 
 
+# an outlier in the table: in its first, a middle and its last row (that of a part of a chunk)
+@pytest.mark.parametrize("dt", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("n", [3, 300])
+@pytest.mark.parametrize("at,by", [(0, 1e4), (7777, -1e4), (20_000, 300.0)])
+def test_one_row_of_large_values(ctx, dt, n, at, by):
+    x, table = du.rand((n, 64), dt, 1), du.rand((20_001, 64), dt, 2, 0.2)
+    table[at, 5] = by
+    lse, entropy, ids, logs = answers(ctx, x.cuda(), table.cuda(), 1.0, 9)
+    some = torch.arange(0, n, 1 + n // 40)
+    ref, want = lu.answers_ref(x[some], table, 1.0, torch.zeros(len(some), dtype=torch.int64), 9)
+    assert torch.equal(ids.cpu()[some], want)
+    for t, v in (("lse", lse), ("entropy", entropy), ("top_logp", logs)):
+        du.within(v.cpu()[some], *ref[t], what=t)
+
+
+@pytest.mark.parametrize("n", [30, 600])
+def test_one_row_of_large_values_does_not_bring_all_of_the_table_up_again(ctx, n):
+    """A call takes no more than a few times as long (all logits again in 64 bits: forty times and more)."""
+    V, D, k = 300_000, 128, 8
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x, table = (torch.randn(m, D, device="cuda", generator=g).bfloat16() for m in (n, V))
+    times = []
+    for outlier in (False, True):
+        if outlier:
+            table[V // 2, 7] = 10_000.0
+        best = math.inf
+        for _ in range(6):
+            start, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            start.record()
+            answers(ctx, x, table, 1.0, k)
+            end.record()
+            end.synchronize()
+            best = min(best, start.elapsed_time(end))
+        times.append(best)
+    assert times[1] < 4 * times[0], times
+
+
 def test_rows_in_turns(recd, ctx):
     """9000 rows of 1 000 003 go in two turns: every row is the same, and as a small call has it."""
     n, V, D = 9000, 1_000_003, 8
