@@ -680,7 +680,7 @@ recd_status recd_list_attention_backward(recd_ctx *ctx, const recd_attention *a,
  * 1 / (1 - p) for the rounded p.  What does not stay is 0, be it infinite or NaN.  The same numbers give the same mask, in every
  * operator, type and direction; every use in a step takes a `call` of its own. */
 typedef struct recd_dropout_mask {
-    double p;                  /* in [0, 1) */
+    double p;                  /* in [0, 1), below 1 - 2^-17 (which would round to 1) */
     uint64_t seed, call;
     const int64_t *step;       /* device, one number that is added to `call`, read when the kernels run (a captured step
                                   gets another mask at each replay), or NULL */
@@ -744,7 +744,9 @@ recd_status recd_dense_backward(recd_ctx *ctx, const recd_dense_layer *a, const 
  *     logits' ids and log probabilities, the largest first.  Logits are put in order as 64-bit sums of exact products give them, and
  *     of equal ones the lowest id comes first; a NaN counts as -infinity.  (Where x or the table is not finite, or a row's sum of
  *     absolute products could pass 4e37, 32-bit sums choose which logits are looked at.)  Of a row with a logit of +infinity
- *     or NaN lse, entropy and the log probabilities are NaN; of one with -infinity the entropy may be.
+ *     or NaN lse, entropy and the log probabilities are NaN; of one with -infinity the entropy may be; of one with nothing else lse is
+ *     -infinity and the log probabilities are NaN.
+ *     The sums over the table lose no more with many rows of it than with few: sixteen exponentials are added up in 32 bits, the rest in 64.
  *     The gradient of logp is that of call 30 with the opposite sign.
  *     Up to 256 rows are the form for serving.  Rows of large batches go in turns.
  *     Workspace: 4 bytes for every row and 64 rows of the table (k > 0), of at most 512 MiB or 64 rows in a turn, 4 for 64 rows of the

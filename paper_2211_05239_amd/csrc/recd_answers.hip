@@ -10,11 +10,14 @@
 // row and computes their logits again, in 64 bits, which puts neighbours in rank in order that 32 bits do not tell apart.
 // Both terms of H are at least 0, so nothing cancels where one id has nearly all of the weight.
 //
-// What bounds them.  Many rows: the vector units.  A logit takes the matrix cores 2 D operations, and the vector units about eight
-// instructions' time: the product with scale, half a maximum, the exponential (four), the two sums.  4096 rows of 1 M x 128 bf16
-// take 1410 us of 1550, 0.74 PFLOP/s beside a large product's 1.40, vector units 72 % busy; the second kernel 215, 64-bit products
-// of the listed chunks.  Few rows: the table's way from memory, 1 M x 128 bf16 at 4.7 TB/s (54 us for one row without ids), and
-// for small tables the two launches and the chains of their loads (37 rows of 100 000 x 64 fp32: 18 and 15 us).
+// What bounds them.  Many rows: the vector units.  A logit takes the matrix cores 2 D operations, and the vector units about seven instructions:
+// the product with scale, half a maximum, the exponential (twice the time of another), the two sums.  4096 rows of 1 M x 128 bf16 take 1600 to 1700
+// us, the clock's share in it, 0.65 PFLOP/s beside a large product's 1.40: 1430 at least in the first kernel, which has the vector units 67 % busy
+// and the matrix cores 33 %, its waves waiting 43 % of their time (each at the exchange of its pairs' maxima, before its exponentials); 230 in the
+// second, which is bound by memory: the chunks' maxima twice and the listed chunks, 1.09 GB at 4.8 TB/s.  Few rows: the table's way from
+// memory, 1 M x 128 bf16 at 5.5 TB/s (46 us for one row without ids), and for small tables the two launches and the chains of their loads (37 rows of
+// 100 000 x 64 fp32: 17 and 15 us).  More ids than a table has chunks: all of it is computed again in 64 bits, and put in order a
+// thousand at a time (4096 rows of 2000 x 64 bf16 with 64 ids: 266 us).
 #include "recd_internal.h"
 #include "recd_mfma.h"
 
@@ -25,7 +28,7 @@ namespace {
 constexpr int kChunk = 64;       // table rows
 constexpr int kWaves = 4;        // of the kernel of few rows
 constexpr int kMany = 8;         // of the kernel of many rows
-constexpr int kFewRows = 256;   // of 300 000 x 128 bf16, eight ids: 256 rows 71 us here, 300 rows by the kernel of many 97
+constexpr int kFewRows = 256;   // of 300 000 x 128 bf16, eight ids: 256 rows 73 us here, 300 rows by the kernel of many 96
 
 struct StreamArgs {
     int64_t n, V;
@@ -290,8 +293,8 @@ template <typename T, int DP, int N> __global__ __launch_bounds__(64 * kWaves) v
 }
 
 // Many rows: 32 in every wave of a block, all of which see every table row of the split, a chunk of them at a time in two
-// buffers of LDS.  Four waves a SIMD for 16-bit rows of up to 128 (the stream of 4096 rows of 1 M x 128 bf16: 1370 us; of the compiler's own
-// choice of three 1530, of five 1480, of six 1770).
+// buffers of LDS.  Four waves a SIMD for 16-bit rows of up to 128 (the stream of 4096 rows of 1 M x 128 bf16, when
+// its sums were of 32 bits: 1370 us; of the compiler's own choice of three 1530, of five 1480, of six 1770).
 template <typename T, int DP> __global__ __launch_bounds__(64 * kMany, sizeof(T) == 2 && DP <= 128 ? 4 : 2) void k_answers_many(StreamArgs a)
 {
     constexpr int KS = DP / 16;

@@ -10,10 +10,10 @@
 // and the store work on eight neighbouring features a lane.
 //
 // What bounds them.  Large products: loads into LDS and the matrix cores beside each other (8192^3 bf16 1.23 PFLOP/s; without the loads
-// 2.0, the loads alone as fast as 1.65; the matrix cores are 51 % busy at 1.85 GHz).  16 384 x 8192 -> 1024 with SiLU, both
+// 2.0, the loads alone as fast as 1.65; the matrix cores are 62 % busy at 1.85 GHz).  16 384 x 8192 -> 1024 with SiLU, both
 // directions: 790-835 us for 0.82 TFLOP.  Short contractions: what is done at a tile's end, on the vector units.  300 007 x 128 -> 512 with
-// GELU and dropout takes about 42 instructions' time an element, GELU more than half of it: 186 us forward, where memory would need 76,
-// 210 for gz; without both 97.  Few rows: w's way from memory, as far as one call's latency lets it (one row 4096 -> 16 384 bf16 5.0 TB/s).
+// GELU and dropout takes 36 instructions' time an element forward and 44 for gz, GELU more than half of it, with the vector units 73 and 74 %
+// busy: 200 us forward, where memory would need 76, 220 for gz; without both 97.  Few rows: w's way from memory, as far as one call's latency lets it (one row 4096 -> 16 384 bf16 5.0 TB/s).
 // Small fp32 products: a unit has one or two tiles (5021 x 516 -> 260: 395 tiles of 64, 23 us, of which the matrix cores need 9).
 #include "recd_epilogue.h"
 #include "recd_mfma.h"
@@ -27,6 +27,10 @@ constexpr int kBlock = 256;
 enum { FORWARD = 0, GRAD = 1, PLAIN = 2 };
 
 // What becomes of the sums.  Strides in bytes.
+//
+// gz is rounded to the layer's type on its way to the gradients' products: the matrix cores take 16-bit operands, and two halves of each
+// would be twice the products and twice gz's traffic, for gradients that are rounded to 16 bits themselves (in bf16 they lie 2.3e-3 from the exact
+// ones, 1.7e-3 by their own rounding).  grad_bias is summed before the rounding; a layer of fp32 rounds nothing.
 struct Epilogue {
     int act;
     RecdMask mask;
