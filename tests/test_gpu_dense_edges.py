@@ -184,3 +184,23 @@ def test_distances_whose_bytes_pass_64_bits(recd, ctx):
         a = recd._Dense(4, 64, 64, 0, 0, 64, 64, 64, None)
         assert recd._lib.recd_dense_backward(ctx._h, C.byref(a), p, p, None, None, p, far, p, 64, p, None) == recd.RECD_EINVAL
         assert recd._lib.recd_dense_backward(ctx._h, C.byref(a), p, p, None, None, p, 64, p, far, p, None) == recd.RECD_EINVAL
+
+
+@pytest.mark.parametrize("n,K,N", [(300, 64, 72), (5003, 8, 8), (70, 24, 16_384)])
+@pytest.mark.parametrize("wide", [False, True])
+def test_any_of_the_fp16_gradients(recd, ctx, n, K, N, wide):
+    """Each by itself has the bits that it has beside the others, also from rows inside of wider ones that hold infinities."""
+    x, w, b, g = (t.cuda() for t in (du.rand((n, K), "f16", 1, 0.01), du.rand((N, K), "f16", 2, 10.0), du.rand((N,), "f32", 3), du.rand((n, N), "f16", 4, 2.0 ** -18)))
+    if wide:
+        big = torch.full((n, N + 48), float("inf"), dtype=g.dtype, device="cuda")
+        big[:, 16:-32] = g
+        g = big[:, 16:-32]
+    for how in (dict(act="gelu"), dict(act="silu", dropout=recd.Dropout(0.2, 1, 2)), dict(dropout=recd.Dropout(0.2, 1, 2)), dict()):
+        full = [torch.empty_like(x), torch.empty_like(w), torch.empty_like(b)]
+        ctx.dense_backward(x, w, b, g, *full, **how)
+        assert all(t.isfinite().all() and t.any() for t in full)
+        for mask in range(1, 8):
+            some = [torch.full_like(t, 3.0) if mask >> i & 1 else None for i, t in enumerate(full)]
+            ctx.dense_backward(x, w, b, g, *some, **how)
+            for a, want in zip(some, full):
+                assert a is None or du.same_bits(a, want)
